@@ -56,6 +56,7 @@ typedef enum {
 #define PSGD_W_RANK_DEFICIENT 1 /* a pivot of the orthogonalisation fell below tolerance */
 #define PSGD_W_NOT_CONVERGED 2  /* the eigen-solver of the refresh hit its sweep limit */
 #define PSGD_W_TIMEOUT 4        /* a bounded wait inside a kernel ran out (results of that step are invalid) */
+#define PSGD_W_LABEL 8          /* a label is neither a column nor the ignored one (psgd_xent_*: that row's loss is NaN, its gradient 0) */
 
 /* options for psgd_set_option */
 #define PSGD_OPT_ERROR_FORM 1   /* 0 (default): e_i <- Delta_i - P~ Q_i^T  (Algorithm 2, last line)
@@ -319,6 +320,70 @@ psgd_status psgd_gemm_nt_tf32(const float* A /*DEVICE*/, const float* B /*DEVICE
 psgd_status psgd_backproject_static(const float* M /*DEVICE*/, const float* P_hat /*DEVICE*/,
                                     float* Q_node /*DEVICE*/, float* Q_mean /*DEVICE*/,
                                     int64_t m, int64_t n, int r, int N, psgd_stream stream);
+
+/*
+ * Training operators: where the gradients that the compressor takes come from in a decoder-style language model whose
+ * activations are kept in 8 bits between the forward and the backward pass.  (Additions of this library: the paper takes the
+ * gradients as given.)  All calls are stream-ordered, allocate nothing and never synchronise; every DEVICE buffer is the
+ * caller's.  Matrices are row-major with unit column stride and a row stride ld.. in elements; "aligned operand" means a
+ * 16-byte aligned pointer and, with more than one row, a row stride that is a multiple of 8 elements.  `status` (DEVICE, one int, may
+ * be NULL) collects PSGD_W_* bits and is never cleared by the library.  `workspace` (DEVICE, 256-byte aligned) holds at least
+ * the bytes the matching query reports, may hold anything before the call, and is free again for later work on the stream.
+ * Sizes are at most 2^30 per dimension; T = 0 is allowed (loss 0, weight gradients 0).
+ */
+#define PSGD_DT_F32 0
+#define PSGD_DT_BF16 1
+
+/*
+ * Softmax cross entropy of the last layer.  H [T][D] hidden states, W [V][D] vocabulary matrix (both bfloat16, aligned operands),
+ * labels [T] in 0..V-1 or `ignore`, weight [T] float32 or NULL (1 everywhere):
+ *     l = H W^T,  lse_t = log sum_v exp(l_tv),  token_loss_t = lse_t - l_{t,labels_t} (0 where ignored),
+ *     loss = sum_t weight_t token_loss_t / Z,  Z = sum of weight_t over the rows that are not ignored (loss 0 where Z = 0),
+ *     dH = d loss / d H [T][D],  dW = d loss / d W [V][D], both bfloat16.
+ * loss: 1 float, token_loss and lse: [T] float32.  The logits are never stored; psgd_xent_grad keeps 16 bits per logit of a
+ * bounded number of tokens at a time in the workspace.  dW may be a slot of a bfloat16 gradient stack.
+ */
+psgd_status psgd_xent_workspace(int64_t T, int64_t V, int64_t D, int grad, size_t* bytes /*HOST*/);
+psgd_status psgd_xent_loss(const void* H /*DEVICE*/, int64_t ldh, const void* W /*DEVICE*/, int64_t ldw, const int64_t* labels /*DEVICE*/,
+                           const float* weight /*DEVICE*/, int64_t ignore, int64_t T, int64_t V, int64_t D, float* loss /*DEVICE*/,
+                           float* token_loss /*DEVICE*/, float* lse /*DEVICE*/, int* status /*DEVICE*/, void* workspace /*DEVICE*/,
+                           size_t workspace_bytes, psgd_stream stream);
+psgd_status psgd_xent_grad(const void* H /*DEVICE*/, int64_t ldh, const void* W /*DEVICE*/, int64_t ldw, const int64_t* labels /*DEVICE*/,
+                           const float* weight /*DEVICE*/, int64_t ignore, int64_t T, int64_t V, int64_t D, float* loss /*DEVICE*/,
+                           float* token_loss /*DEVICE*/, float* lse /*DEVICE*/, void* dH /*DEVICE*/, int64_t lddh, void* dW /*DEVICE*/,
+                           int64_t lddw, int* status /*DEVICE*/, void* workspace /*DEVICE*/, size_t workspace_bytes, psgd_stream stream);
+
+/*
+ * Activation checkpoints in 8 bits.  A checkpoint of x [T][F] is q [T][32 G] int8 (16-byte aligned; G = ceil(F / 32), padded with
+ * zeros) and scales [T][G] bytes: per row and group of 32 values a power of two 2^e, e the smallest integer with
+ * max|x| <= 127 * 2^e (kept within -126..121; byte e + 127), and q = rint(x / 2^e), ties to even, within -127..127.  A group
+ * that holds an infinity or a NaN has the byte 255 and stands for NaN.  The values q 2^e are exact in bfloat16 and float32.
+ * x is float32 or bfloat16 (dtype).
+ */
+psgd_status psgd_act_pack(const void* x /*DEVICE*/, int64_t ldx, int dtype, int64_t T, int64_t F, int8_t* q /*DEVICE*/, uint8_t* scales /*DEVICE*/,
+                          psgd_stream stream);
+psgd_status psgd_act_unpack(const int8_t* q /*DEVICE*/, const uint8_t* scales /*DEVICE*/, int64_t T, int64_t F, void* x /*DEVICE*/, int64_t ldx, int dtype,
+                            psgd_stream stream);
+
+/*
+ * Weight gradient of a linear layer y = x W^T (W [O][F]) from the checkpoint of its input: dW = dY^T x^, dY [T][O] bfloat16 (aligned
+ * operand), dW [O][F] float32 or bfloat16 (dtype), float32 sums of exact products.  dW may be a slot of a gradient stack.
+ */
+psgd_status psgd_act_wgrad_workspace(int64_t T, int64_t O, int64_t F, size_t* bytes /*HOST*/);
+psgd_status psgd_act_wgrad(const void* dY /*DEVICE*/, int64_t lddy, const int8_t* q /*DEVICE*/, const uint8_t* scales /*DEVICE*/, int64_t T, int64_t O, int64_t F,
+                           void* dW /*DEVICE*/, int64_t lddw, int dtype, int* status /*DEVICE*/, void* workspace /*DEVICE*/, size_t workspace_bytes,
+                           psgd_stream stream);
+
+/*
+ * Gated unit h = silu(gate) up of a feed-forward block, all matrices [T][F] bfloat16.  The forward pass packs gate and up in the
+ * same pass over them; the backward pass reads the checkpoints:  d_gate = dh up s (1 + gate (1 - s)), d_up = dh gate s,
+ * s = 1 / (1 + exp(-gate)), and, where h is not NULL, h again (for the weight gradient of the layer behind the unit).
+ */
+psgd_status psgd_swiglu_forward(const void* gate /*DEVICE*/, int64_t ldg, const void* up /*DEVICE*/, int64_t ldu, int64_t T, int64_t F, void* h /*DEVICE*/, int64_t ldh,
+                                int8_t* q_gate /*DEVICE*/, uint8_t* s_gate /*DEVICE*/, int8_t* q_up /*DEVICE*/, uint8_t* s_up /*DEVICE*/, psgd_stream stream);
+psgd_status psgd_swiglu_backward(const void* dh /*DEVICE*/, int64_t lddh, const int8_t* q_gate /*DEVICE*/, const uint8_t* s_gate /*DEVICE*/,
+                                 const int8_t* q_up /*DEVICE*/, const uint8_t* s_up /*DEVICE*/, int64_t T, int64_t F, void* d_gate /*DEVICE*/, int64_t ldg,
+                                 void* d_up /*DEVICE*/, int64_t ldu, void* h /*DEVICE*/, int64_t ldh, psgd_stream stream);
 
 #ifdef __cplusplus
 }

@@ -16,4 +16,16 @@ from .binding import (  # noqa: F401
     KERNEL_FAMILIES,
 )
 from .stack import StreamedStack  # noqa: F401,E402
+from .training import (  # noqa: F401,E402
+    ActivationCheckpoint,
+    CrossEntropy,
+    CrossEntropyGrad,
+    PSGD_W_LABEL,
+    linear_cross_entropy,
+    linear_cross_entropy_grad,
+    pack_activation,
+    swiglu_backward,
+    swiglu_forward,
+    weight_gradient,
+)
 from .exchange import ExchangedStack, slot_offsets  # noqa: F401,E402

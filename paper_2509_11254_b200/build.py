@@ -6,10 +6,10 @@ import subprocess
 import sys
 
 HERE = os.path.dirname(os.path.abspath(__file__))
-SRC = os.path.join(HERE, "csrc", "psgd_api.cu")
+SRCS = [os.path.join(HERE, "csrc", f) for f in ("psgd_api.cu", "psgd_lm.cu")]     # compiled side by side
 LIB = os.path.join(HERE, "libpsgd.so")
-DEPS = [SRC, os.path.join(HERE, "csrc", "psgd_kernels.cuh"),
-        os.path.join(os.path.dirname(HERE), "include", "psgd.h")]
+OBJ_DIR = os.path.join(HERE, "_build")
+HEADER = os.path.join(os.path.dirname(HERE), "include", "psgd.h")
 
 
 def nvcc_path():
@@ -23,20 +23,27 @@ def needs_build():
     if not os.path.exists(LIB):
         return True
     t = os.path.getmtime(LIB)
-    deps = DEPS + [os.path.join(HERE, "csrc", f) for f in os.listdir(os.path.join(HERE, "csrc"))]
+    deps = [HEADER] + [os.path.join(HERE, "csrc", f) for f in os.listdir(os.path.join(HERE, "csrc"))]
     return any(os.path.getmtime(d) > t for d in deps if os.path.exists(d))
 
 
 def build_library(force=False, verbose=False):
     if not force and not needs_build():
         return LIB
-    cmd = [nvcc_path(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-           "-Xptxas", "-v" if verbose else "-O3", "-shared", "-Xcompiler", "-fPIC", "-o", LIB, SRC]
-    res = subprocess.run(cmd, capture_output=True, text=True)
+    flags = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-Xptxas", "-v" if verbose else "-O3",
+             "-Xcompiler", "-fPIC"]
+    os.makedirs(OBJ_DIR, exist_ok=True)
+    objs = [os.path.join(OBJ_DIR, os.path.basename(s)[:-3] + ".o") for s in SRCS]
+    jobs = [subprocess.Popen([nvcc_path(), *flags, "-c", "-o", o, s], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+            for s, o in zip(SRCS, objs)]
+    said = [j.communicate()[0] for j in jobs]
+    if any(j.returncode != 0 for j in jobs):
+        raise RuntimeError("nvcc failed:\n" + "".join(said))
+    res = subprocess.run([nvcc_path(), "-gencode", "arch=compute_100a,code=sm_100a", "-shared", "-o", LIB, *objs], capture_output=True, text=True)
     if res.returncode != 0:
         raise RuntimeError("nvcc failed:\n" + res.stdout + res.stderr)
     if verbose:
-        print(res.stderr)
+        print("".join(said))
     return LIB
 
 

@@ -15,6 +15,7 @@
 #include <utility>
 #include <vector>
 
+#include "psgd_host.cuh"
 #include "psgd_kernels.cuh"
 #include "psgd_fused.cuh"
 #include "psgd_gemm_tc.cuh"
@@ -29,9 +30,6 @@ constexpr int MAX_R = 128;
 constexpr int MAX_L = 160;  // widest refresh block
 constexpr int PENDING_TC_MIN_R = 8;    // above this many columns the pending-residual projection runs on the tensor cores by default
 constexpr int REFRESH_F32_TAIL = 4;   // float32-accurate sweeps that end a refresh whose early sweeps ran in TF32
-
-inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
-inline int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
 struct Layout {
     size_t flags, defic, Pnode, Pmean, Phat, Qnode, part, gram, T, dbar, Y, Z, V, U, total;
@@ -112,16 +110,6 @@ struct psgd_handle {
 };
 
 namespace {
-
-// Multiprocessors of the current device; 148 (a B200) when no device is visible, so that a handle can still be
-// created and sized on a machine without one.
-int device_sms() {
-    int dev = 0, sms = 0;
-    if (cudaGetDevice(&dev) == cudaSuccess && cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess && sms > 0)
-        return sms;
-    cudaGetLastError();
-    return 148;
-}
 
 // K splits of the tensor-core product with M rows and K columns: enough CTAs for about two per SM,
 // at least 8 K-blocks of 32 each
@@ -334,42 +322,7 @@ struct Launcher {
     }
 };
 
-// Opt a kernel in to `bytes` of dynamic shared memory: the attribute is set once per (device, kernel) and raised
-// only when a larger size is asked for.
-void set_smem_attr(const void* kernel, size_t bytes) {
-    static std::mutex mu;
-    static std::map<std::pair<int, const void*>, size_t> done;
-    int dev = 0;
-    cudaGetDevice(&dev);
-    std::lock_guard<std::mutex> lock(mu);
-    size_t& have = done[std::make_pair(dev, kernel)];
-    if (bytes > have) {
-        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-        have = bytes;
-    }
-}
-template <typename K>
-void allow_smem(K kernel, size_t bytes) {
-    if (bytes > 48 * 1024) set_smem_attr((const void*)kernel, bytes);
-}
-
-inline bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
-
 // ---- TMA tensor maps ----------------------------------------------------------
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-EncodeTiledFn encode_tiled_fn() {
-    static EncodeTiledFn fn = nullptr;
-    if (!fn) {
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult qr;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &qr) == cudaSuccess &&
-            qr == cudaDriverEntryPointSuccess)
-            fn = (EncodeTiledFn)p;
-    }
-    return fn;
-}
 // Rank-3 map over [count*N][m][n] float32 with tiles of `rows` rows x bw columns of one node; out-of-range reads give zeros.
 bool encode_tile_map(CUtensorMap* map, const void* base, int64_t n, int64_t m, int64_t mats, int bw, int rows,
                      CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_NONE, bool bf16 = false) {

@@ -1,0 +1,375 @@
+// Host side of the training operators declared in include/psgd.h: softmax cross entropy of the last layer with its
+// gradients, 8-bit activation checkpoints, the weight gradient from them, and the gated unit.  Argument checks, workspace
+// layout and the stream-ordered sequence of kernels; nothing here allocates, synchronises or keeps anything between calls.
+#include "../../include/psgd.h"
+
+#include <algorithm>
+
+#include "psgd_act.cuh"
+#include "psgd_host.cuh"
+#include "psgd_tile.cuh"
+#include "psgd_xent.cuh"
+
+using namespace psgd;
+
+namespace {
+
+constexpr int64_t MAX_EXTENT = (int64_t)1 << 30;
+constexpr int KACC_F32 = 64;       // stages (4096 of k) per accumulator where the result is float32, see plan_tiles
+
+struct TilePlan { int mt, nt, kb, full, S, kbps, units, gm; };
+
+// Tiles of an M x N product over `pairs` CTA pairs.  The last, partly filled wave of R tiles is cut into S pieces of k each so
+// that ceil(R S / pairs) rounds of ceil(kb / S) stages take least; a round costs about 8 stages of its own (epilogue
+// and the pieces' way through memory), adding the pieces up about half a stage each.
+TilePlan plan_tiles(int64_t M, int64_t N, int64_t K, int pairs, bool split) {
+    TilePlan p{};
+    p.mt = ceil_div(M, TG_BM);
+    p.nt = ceil_div(N, TG_BN);
+    p.kb = ceil_div(K, TG_BK);
+    const int64_t tiles = (int64_t)p.mt * p.nt;
+    const int R = (int)(tiles % pairs);
+    p.full = (int)(tiles - R);
+    p.S = 1;
+    p.kbps = p.kb;
+    if (split && R > 0) {
+        double best = 1e300;
+        for (int S = 1; S <= std::min(p.kb, 2 * pairs); ++S) {
+            const int kbps = ceil_div(p.kb, S);
+            if (ceil_div(p.kb, kbps) != S) continue;                   // no empty pieces
+            const double cost = (double)ceil_div((int64_t)R * S, pairs) * (kbps + 8) + (S > 1 ? 4 + 0.5 * S : 0.0);
+            if (cost < best) { best = cost; p.S = S; p.kbps = kbps; }
+        }
+    }
+    p.units = p.full + R * p.S;
+    // raster: all row tiles next to each other while the row operand fits beside the rest in L2, else as many as make the
+    // pairs at work cover all columns
+    p.gm = (M * K * 2 <= (40 << 20)) ? p.mt : std::min(p.mt, std::max(8, std::min(32, pairs / p.nt)));
+    return p;
+}
+size_t part_bytes(const TilePlan& p) { return p.S > 1 ? (size_t)(p.units - p.full) * TG_PART * 4 : 0; }
+int tail_counters(const TilePlan& p) { return p.S > 1 ? 2 * ((p.units - p.full) / p.S) : 0; }
+
+// bfloat16 matrix, `rows` rows of `cols` with row stride ld (elements): boxes of 64 columns and `box` rows, 128-byte swizzle
+bool encode_operand(CUtensorMap* map, const void* p, int64_t rows, int64_t cols, int64_t ld, int box) {
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    if (rows == 1) ld = align_up(cols, 8);                             // the stride of a single row is never used
+    cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    cuuint64_t strides[1] = {(cuuint64_t)ld * 2};
+    cuuint32_t b[2] = {64, (cuuint32_t)box};
+    cuuint32_t es[2] = {1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, (void*)p, dims, strides, b, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// C = A B^T summed over k.  A: [M][K] (AMN false) or [K][M] (AMN true), B likewise with N.
+template <int EPI, bool AMN, bool BMN>
+psgd_status launch_tile(const void* A, int64_t lda, const void* B, int64_t ldb, int64_t M, int64_t N, int64_t K, const TilePlan& p, TileArgs a, int pairs, cudaStream_t st) {
+    CUtensorMap ma, mb;
+    if (!(AMN ? encode_operand(&ma, A, K, M, lda, TG_BK) : encode_operand(&ma, A, M, K, lda, 128)) ||
+        !(BMN ? encode_operand(&mb, B, K, N, ldb, TG_BK) : encode_operand(&mb, B, N, K, ldb, 128)))
+        return PSGD_E_CUDA;
+    a.M = (int)M; a.N = (int)N; a.K = (int)K;
+    a.mt = p.mt; a.nt = p.nt; a.kb = p.kb; a.full = p.full; a.S = p.S; a.kbps = p.kbps; a.units = p.units; a.gm = p.gm;
+    const size_t smem = tile_smem_bytes();
+    allow_smem(k_tile<EPI, AMN, BMN>, smem);
+    k_tile<EPI, AMN, BMN><<<2 * std::min(p.units, pairs), TG_THREADS, smem, st>>>(ma, mb, a);
+    return cudaGetLastError() == cudaSuccess ? PSGD_OK : PSGD_E_CUDA;
+}
+
+bool operand_ok(const void* p, int64_t rows, int64_t cols, int64_t ld) { return aligned16(p) && ld >= cols && (rows == 1 || ld % 8 == 0); }
+bool extent_ok(int64_t v) { return v >= 1 && v <= MAX_EXTENT; }
+
+// ---- cross entropy ----
+constexpr int64_t XENT_PIECE_LOGITS = (int64_t)1 << 28;   // logits whose 16-bit form the workspace holds at a time (512 MiB)
+
+struct XentPlan {
+    int pairs, nseg;
+    int64_t ldq, piece, pieces;
+    TilePlan logits, dh, dw;          // of a whole piece
+    size_t inv, done, counters, stats, label_logit, q, part, acc, total;
+    int n_counters;
+};
+// Tokens are taken in pieces, all columns at a time, so that the stored exponents stay within a fixed size however many
+// tokens there are; a piece has at least 1024 tokens, below which the products with the vocabulary matrix would be bound by reading it.
+XentPlan plan_xent(int64_t T, int64_t V, int64_t D, bool grad) {
+    XentPlan x{};
+    x.pairs = std::max(1, device_sms() / 2);
+    x.nseg = ceil_div(V, XE_SEG);
+    x.ldq = (int64_t)x.nseg * XE_SEG;
+    x.pieces = 1;
+    x.piece = T;
+    if (grad) {
+        const int64_t fit = std::max<int64_t>(1024, XENT_PIECE_LOGITS / x.ldq / TG_BM * TG_BM);
+        x.pieces = ceil_div(T, fit);
+        x.piece = std::min<int64_t>(T, align_up(ceil_div(T, x.pieces), TG_BM));
+        x.pieces = ceil_div(T, x.piece);
+    }
+    x.logits = plan_tiles(x.piece, V, D, x.pairs, false);
+    size_t at = 256;                                  // the status word of calls that bring none
+    auto take = [&](size_t bytes) { const size_t o = at; at = align_up(at + bytes, 256); return o; };
+    x.inv = take(4);
+    x.done = take(4);
+    if (grad) {
+        x.dh = plan_tiles(x.piece, D, V, x.pairs, true);
+        x.dw = plan_tiles(V, D, x.piece, x.pairs, true);
+        x.n_counters = std::max(1, 4 * x.pairs);      // two per tail tile, fewer than `pairs` tail tiles
+    }
+    x.counters = take((size_t)x.n_counters * 4);
+    x.stats = take((size_t)x.piece * x.nseg * 8);
+    x.label_logit = take((size_t)x.piece * 4);
+    if (grad) {
+        x.q = take((size_t)x.piece * x.ldq * 2);
+        size_t part = std::max(part_bytes(x.dh), part_bytes(x.dw));
+        if (x.pieces > 1) {                           // the last piece may be shorter
+            const int64_t last = T - (x.pieces - 1) * x.piece;
+            part = std::max(part, std::max(part_bytes(plan_tiles(last, D, V, x.pairs, true)), part_bytes(plan_tiles(V, D, last, x.pairs, true))));
+            x.acc = take((size_t)V * D * 4);
+        }
+        x.part = take(part);
+    }
+    x.total = at;
+    return x;
+}
+
+psgd_status xent(const void* H, int64_t ldh, const void* W, int64_t ldw, const int64_t* labels, const float* weight, int64_t ignore, int64_t T, int64_t V, int64_t D,
+                 float* loss, float* token_loss, float* lse, bool grad, void* dH, int64_t lddh, void* dW, int64_t lddw, int* status, void* ws, size_t ws_bytes, cudaStream_t st) {
+    if (T < 0 || T > MAX_EXTENT || !extent_ok(V) || !extent_ok(D)) return PSGD_E_INVALID;
+    if (!W || !loss || !ws || (T > 0 && (!H || !labels || !token_loss || !lse)) || (grad && (!dW || (T > 0 && !dH)))) return PSGD_E_NULL;
+    if (!operand_ok(W, V, D, ldw) || (T > 0 && !operand_ok(H, T, D, ldh)) || (grad && ((T > 0 && lddh < D) || lddw < D))) return PSGD_E_INVALID;
+    if ((uintptr_t)ws & 255) return PSGD_E_INVALID;
+    if (T == 0) {                                     // no token: loss 0, no gradient
+        if (cudaMemsetAsync(loss, 0, 4, st) != cudaSuccess) return PSGD_E_CUDA;
+        if (grad && cudaMemset2DAsync(dW, (size_t)lddw * 2, 0, (size_t)D * 2, (size_t)V, st) != cudaSuccess) return PSGD_E_CUDA;
+        return PSGD_OK;
+    }
+    const XentPlan x = plan_xent(T, V, D, grad);
+    if (ws_bytes < x.total) return PSGD_E_WORKSPACE;
+    char* w = (char*)ws;
+    int* stat = status ? status : (int*)w;
+    float* inv = (float*)(w + x.inv);
+    int* done = (int*)(w + x.done);
+    int* counters = (int*)(w + x.counters);
+    if (grad) k_xent_norm<<<1, 1024, 0, st>>>((const long long*)labels, weight, T, ignore, (int)V, inv, done, (int)((x.stats - x.done) / 4));
+
+    RowsArgs r{};
+    r.V = (int)V; r.nseg = x.nseg;
+    r.stats = (const float2*)(w + x.stats);
+    r.label_logit = (const float*)(w + x.label_logit);
+    r.ignore = ignore; r.ldq = x.ldq; r.status = stat; r.q = grad ? (unsigned short*)(w + x.q) : nullptr;
+    r.done = done; r.all_rows = T; r.all_labels = (const long long*)labels; r.all_weight = weight; r.all_loss = token_loss; r.mean = loss;
+    auto parts_of = [&](int64_t rows) {               // CTAs per row of k_xent_rows: two waves of eight per multiprocessor, at least 2048 columns each
+        return (int)std::max<int64_t>(1, std::min<int64_t>({(2 * 8 * 2 * (int64_t)x.pairs + rows - 1) / rows, (V + 2047) / 2048, 1024}));
+    };
+    int64_t report = 0;
+    for (int64_t t0 = 0; t0 < T; t0 += x.piece) {
+        const int64_t rows = std::min<int64_t>(x.piece, T - t0);
+        report += grad ? rows * parts_of(rows) : ceil_div(rows, XE_THREADS / 32);
+    }
+    if (report > INT32_MAX) return PSGD_E_INVALID;
+    r.done_at = (int)report;
+
+    for (int64_t t0 = 0; t0 < T; t0 += x.piece) {
+        const int64_t rows = std::min<int64_t>(x.piece, T - t0);
+        const bool first = t0 == 0, last = t0 + rows == T;
+        const char* h = (const char*)H + (size_t)t0 * ldh * 2;
+        TileArgs a{};
+        a.status = stat;
+        a.labels = (const long long*)labels + t0;
+        a.stats = (float2*)(w + x.stats);
+        a.label_logit = (float*)(w + x.label_logit);
+        a.q = r.q; a.ldq = x.ldq; a.nseg = x.nseg;
+        if (!grad) { a.clear = done; a.clear_n = 1; }
+        const TilePlan pl = rows == x.piece ? x.logits : plan_tiles(rows, V, D, x.pairs, false);
+        psgd_status s = grad ? launch_tile<EPI_SOFTMAX, false, false>(h, ldh, W, ldw, rows, V, D, pl, a, x.pairs, st)
+                             : launch_tile<EPI_LOSS, false, false>(h, ldh, W, ldw, rows, V, D, pl, a, x.pairs, st);
+        if (s != PSGD_OK) return s;
+        r.rows = (int)rows;
+        r.labels = (const long long*)labels + t0;
+        r.weight = weight ? weight + t0 : nullptr;
+        r.loss = token_loss + t0;
+        r.lse = lse + t0;
+        if (!grad) {
+            k_xent_loss<<<ceil_div(rows, XE_THREADS / 32), XE_THREADS, 0, st>>>(r);
+            continue;
+        }
+        k_xent_rows<<<dim3((unsigned)rows, parts_of(rows)), XE_THREADS, 0, st>>>(r);
+        // dH = dL W: contraction over the vocabulary;  dW = dL^T H: over the tokens
+        TileArgs g{};
+        g.status = stat;
+        g.scale = inv;
+        g.part = (float*)(w + x.part);
+        g.counters = counters;
+        g.out = (char*)dH + (size_t)t0 * lddh * 2;
+        g.ldo = lddh;
+        g.vec = ((uintptr_t)g.out & 7) == 0 && lddh % 4 == 0;
+        s = launch_tile<EPI_STORE, false, true>(r.q, x.ldq, W, ldw, rows, D, V, rows == x.piece ? x.dh : plan_tiles(rows, D, V, x.pairs, true), g, x.pairs, st);
+        if (s != PSGD_OK) return s;
+        float* acc = (float*)(w + x.acc);
+        g.addend = first ? nullptr : acc;
+        if (last) {
+            g.out = dW; g.ldo = lddw;
+            g.vec = ((uintptr_t)dW & 7) == 0 && lddw % 4 == 0 && (first || D % 4 == 0);
+        } else {
+            g.out = acc; g.ldo = D; g.out_f32 = 1; g.scale = nullptr;
+            g.vec = D % 4 == 0;
+        }
+        s = launch_tile<EPI_STORE, true, true>(r.q, x.ldq, h, ldh, V, D, rows, rows == x.piece ? x.dw : plan_tiles(V, D, rows, x.pairs, true), g, x.pairs, st);
+        if (s != PSGD_OK) return s;
+    }
+    return cudaGetLastError() == cudaSuccess ? PSGD_OK : PSGD_E_CUDA;
+}
+
+// ---- 8-bit activations ----
+struct ActGrid { dim3 grid, block; };
+// 256 threads: a row's units side by side, as many rows as fit; enough CTAs for eight per multiprocessor, at least two rows per thread
+ActGrid act_grid(int64_t T, int G) {
+    const int units = 4 * G, across = ceil_div(units, 256);
+    const int bx = (int)align_up(ceil_div(units, across), 4);
+    const int by = std::max(1, 256 / bx);
+    const int64_t rows = ceil_div(T, by);
+    const int64_t y = std::min<int64_t>({rows, 65535, std::max<int64_t>(ceil_div((int64_t)device_sms() * 16, across), ceil_div(rows, 8))});
+    return {dim3(ceil_div(units, bx), (unsigned)y), dim3(bx, by)};
+}
+bool act_ok(int64_t T, int64_t F) { return T >= 0 && T <= MAX_EXTENT && extent_ok(F); }
+bool vec8(const void* p, int64_t ld, int dtype) { return aligned16(p) && ld % (dtype == PSGD_DT_BF16 ? 8 : 4) == 0; }
+bool dtype_ok(int dtype) { return dtype == PSGD_DT_F32 || dtype == PSGD_DT_BF16; }
+bool ckpt_ok(const void* q) { return ((uintptr_t)q & 15) == 0; }
+
+struct WgradPlan { int pairs; int64_t ldx; TilePlan p; size_t counters, x, part, total; int n_counters; };
+WgradPlan plan_wgrad(int64_t T, int64_t O, int64_t F) {
+    WgradPlan g{};
+    g.pairs = std::max(1, device_sms() / 2);
+    g.ldx = (int64_t)align_up(F, ACT_GROUP);
+    g.p = plan_tiles(O, F, T, g.pairs, true);
+    g.n_counters = tail_counters(g.p);
+    size_t at = 256;
+    auto take = [&](size_t bytes) { const size_t o = at; at = align_up(at + bytes, 256); return o; };
+    g.counters = take((size_t)g.n_counters * 4);
+    g.x = take((size_t)T * g.ldx * 2);
+    g.part = take(part_bytes(g.p));
+    g.total = at;
+    return g;
+}
+
+psgd_status last_error() { return cudaGetLastError() == cudaSuccess ? PSGD_OK : PSGD_E_CUDA; }
+
+}  // namespace
+
+extern "C" {
+
+psgd_status psgd_xent_workspace(int64_t T, int64_t V, int64_t D, int grad, size_t* bytes) {
+    if (!bytes) return PSGD_E_NULL;
+    if (T < 0 || T > MAX_EXTENT || !extent_ok(V) || !extent_ok(D)) return PSGD_E_INVALID;
+    *bytes = T == 0 ? 256 : plan_xent(T, V, D, grad != 0).total;
+    return PSGD_OK;
+}
+
+psgd_status psgd_xent_loss(const void* H, int64_t ldh, const void* W, int64_t ldw, const int64_t* labels, const float* weight, int64_t ignore, int64_t T, int64_t V,
+                           int64_t D, float* loss, float* token_loss, float* lse, int* status, void* ws, size_t ws_bytes, psgd_stream stream) try {
+    return xent(H, ldh, W, ldw, labels, weight, ignore, T, V, D, loss, token_loss, lse, false, nullptr, 0, nullptr, 0, status, ws, ws_bytes, (cudaStream_t)stream);
+} catch (...) {
+    return PSGD_E_CUDA;
+}
+
+psgd_status psgd_xent_grad(const void* H, int64_t ldh, const void* W, int64_t ldw, const int64_t* labels, const float* weight, int64_t ignore, int64_t T, int64_t V,
+                           int64_t D, float* loss, float* token_loss, float* lse, void* dH, int64_t lddh, void* dW, int64_t lddw, int* status, void* ws, size_t ws_bytes,
+                           psgd_stream stream) try {
+    return xent(H, ldh, W, ldw, labels, weight, ignore, T, V, D, loss, token_loss, lse, true, dH, lddh, dW, lddw, status, ws, ws_bytes, (cudaStream_t)stream);
+} catch (...) {
+    return PSGD_E_CUDA;
+}
+
+psgd_status psgd_act_pack(const void* x, int64_t ldx, int dtype, int64_t T, int64_t F, int8_t* q, uint8_t* scales, psgd_stream stream) {
+    if (!act_ok(T, F) || !dtype_ok(dtype)) return PSGD_E_INVALID;
+    if (T == 0) return PSGD_OK;
+    if (!x || !q || !scales) return PSGD_E_NULL;
+    if (ldx < F || !ckpt_ok(q)) return PSGD_E_INVALID;
+    const ActShape s{T, (int)F, ceil_div(F, ACT_GROUP)};
+    const ActGrid g = act_grid(T, s.G);
+    if (dtype == PSGD_DT_BF16) k_act_pack<<<g.grid, g.block, 0, (cudaStream_t)stream>>>(s, (const __nv_bfloat16*)x, ldx, vec8(x, ldx, dtype), q, scales);
+    else k_act_pack<<<g.grid, g.block, 0, (cudaStream_t)stream>>>(s, (const float*)x, ldx, vec8(x, ldx, dtype), q, scales);
+    return last_error();
+}
+
+psgd_status psgd_act_unpack(const int8_t* q, const uint8_t* scales, int64_t T, int64_t F, void* x, int64_t ldx, int dtype, psgd_stream stream) {
+    if (!act_ok(T, F) || !dtype_ok(dtype)) return PSGD_E_INVALID;
+    if (T == 0) return PSGD_OK;
+    if (!x || !q || !scales) return PSGD_E_NULL;
+    if (ldx < F || !ckpt_ok(q)) return PSGD_E_INVALID;
+    const ActShape s{T, (int)F, ceil_div(F, ACT_GROUP)};
+    const ActGrid g = act_grid(T, s.G);
+    if (dtype == PSGD_DT_BF16) k_act_unpack<<<g.grid, g.block, 0, (cudaStream_t)stream>>>(s, q, scales, (__nv_bfloat16*)x, ldx, vec8(x, ldx, dtype), nullptr, 0);
+    else k_act_unpack<<<g.grid, g.block, 0, (cudaStream_t)stream>>>(s, q, scales, (float*)x, ldx, vec8(x, ldx, dtype), nullptr, 0);
+    return last_error();
+}
+
+psgd_status psgd_act_wgrad_workspace(int64_t T, int64_t O, int64_t F, size_t* bytes) {
+    if (!bytes) return PSGD_E_NULL;
+    if (!act_ok(T, F) || !extent_ok(O)) return PSGD_E_INVALID;
+    *bytes = T == 0 ? 256 : plan_wgrad(T, O, F).total;
+    return PSGD_OK;
+}
+
+psgd_status psgd_act_wgrad(const void* dY, int64_t lddy, const int8_t* q, const uint8_t* scales, int64_t T, int64_t O, int64_t F, void* dW, int64_t lddw, int dtype,
+                           int* status, void* ws, size_t ws_bytes, psgd_stream stream) try {
+    cudaStream_t st = (cudaStream_t)stream;
+    if (!act_ok(T, F) || !extent_ok(O) || !dtype_ok(dtype)) return PSGD_E_INVALID;
+    if (!dW || !ws || (T > 0 && (!dY || !q || !scales))) return PSGD_E_NULL;
+    if (lddw < F || ((uintptr_t)ws & 255) || (T > 0 && (!operand_ok(dY, T, O, lddy) || !ckpt_ok(q)))) return PSGD_E_INVALID;
+    if (T == 0) {
+        const size_t es = dtype == PSGD_DT_F32 ? 4 : 2;
+        return cudaMemset2DAsync(dW, (size_t)lddw * es, 0, (size_t)F * es, (size_t)O, st) == cudaSuccess ? PSGD_OK : PSGD_E_CUDA;
+    }
+    const WgradPlan g = plan_wgrad(T, O, F);
+    if (ws_bytes < g.total) return PSGD_E_WORKSPACE;
+    char* w = (char*)ws;
+    const ActShape s{T, (int)F, ceil_div(F, ACT_GROUP)};
+    const ActGrid ag = act_grid(T, s.G);
+    k_act_unpack<<<ag.grid, ag.block, 0, st>>>(s, q, scales, (__nv_bfloat16*)(w + g.x), g.ldx, true, (int*)(w + g.counters), g.n_counters);
+    TileArgs a{};
+    a.status = status ? status : (int*)w;
+    a.out = dW; a.ldo = lddw; a.out_f32 = dtype == PSGD_DT_F32;
+    a.vec = ((uintptr_t)dW & (a.out_f32 ? 15 : 7)) == 0 && lddw % 4 == 0;
+    a.kacc = a.out_f32 ? KACC_F32 : 0;
+    a.part = (float*)(w + g.part);
+    a.counters = (int*)(w + g.counters);
+    return launch_tile<EPI_STORE, true, true>(dY, lddy, w + g.x, g.ldx, O, F, T, g.p, a, g.pairs, st);
+} catch (...) {
+    return PSGD_E_CUDA;
+}
+
+psgd_status psgd_swiglu_forward(const void* gate, int64_t ldg, const void* up, int64_t ldu, int64_t T, int64_t F, void* h, int64_t ldh, int8_t* q_gate, uint8_t* s_gate,
+                                int8_t* q_up, uint8_t* s_up, psgd_stream stream) {
+    if (!act_ok(T, F)) return PSGD_E_INVALID;
+    if (T == 0) return PSGD_OK;
+    if (!gate || !up || !h || !q_gate || !s_gate || !q_up || !s_up) return PSGD_E_NULL;
+    if (ldg < F || ldu < F || ldh < F || !ckpt_ok(q_gate) || !ckpt_ok(q_up)) return PSGD_E_INVALID;
+    const ActShape s{T, (int)F, ceil_div(F, ACT_GROUP)};
+    const ActGrid g = act_grid(T, s.G);
+    const int vec = (vec8(gate, ldg, 1) ? 1 : 0) | (vec8(up, ldu, 1) ? 2 : 0) | (vec8(h, ldh, 1) ? 4 : 0);
+    k_swiglu_forward<<<g.grid, g.block, 0, (cudaStream_t)stream>>>(s, (const __nv_bfloat16*)gate, ldg, (const __nv_bfloat16*)up, ldu, (__nv_bfloat16*)h, ldh, vec, q_gate,
+                                                                   s_gate, q_up, s_up);
+    return last_error();
+}
+
+psgd_status psgd_swiglu_backward(const void* dh, int64_t lddh, const int8_t* q_gate, const uint8_t* s_gate, const int8_t* q_up, const uint8_t* s_up, int64_t T, int64_t F,
+                                 void* d_gate, int64_t ldg, void* d_up, int64_t ldu, void* h, int64_t ldh, psgd_stream stream) {
+    if (!act_ok(T, F)) return PSGD_E_INVALID;
+    if (T == 0) return PSGD_OK;
+    if (!dh || !q_gate || !s_gate || !q_up || !s_up || !d_gate || !d_up) return PSGD_E_NULL;
+    if (lddh < F || ldg < F || ldu < F || (h && ldh < F) || !ckpt_ok(q_gate) || !ckpt_ok(q_up)) return PSGD_E_INVALID;
+    const ActShape s{T, (int)F, ceil_div(F, ACT_GROUP)};
+    const ActGrid g = act_grid(T, s.G);
+    const int vec = (vec8(dh, lddh, 1) ? 1 : 0) | (vec8(d_gate, ldg, 1) ? 2 : 0) | (vec8(d_up, ldu, 1) ? 4 : 0) | (h && vec8(h, ldh, 1) ? 8 : 0);
+    const auto run = [&](auto kernel) {
+        kernel<<<g.grid, g.block, 0, (cudaStream_t)stream>>>(s, (const __nv_bfloat16*)dh, lddh, q_gate, s_gate, q_up, s_up, (__nv_bfloat16*)d_gate, ldg, (__nv_bfloat16*)d_up,
+                                                             ldu, (__nv_bfloat16*)h, ldh, vec);
+    };
+    if (h) run(k_swiglu_backward<true>);
+    else run(k_swiglu_backward<false>);
+    return last_error();
+}
+
+}  // extern "C"

@@ -1,0 +1,462 @@
+// Tensor-core products of bfloat16 matrices for the training operators: the logits of the last layer (with the softmax
+// statistics in the epilogue), the two gradients of that layer, and the weight gradient of a linear layer.
+//
+//     C [M][N] = sum_k A(m, k) B(n, k),     operands bfloat16, sums in float32 (tensor memory).
+//
+// Either operand lies in memory with k contiguous ("K-major", rows of the matrix) or with m (n) contiguous ("MN-major":
+// the gradients contract over tokens, the slow index of every activation), which the shared-memory descriptors and
+// the instruction descriptor express, so that no operand is ever transposed in memory.
+//
+// One unit of work is a 256 x 256 tile of C (or a range of k of one), computed by a PAIR of CTAs (tcgen05.mma cta_group::2):
+// each CTA holds 128 rows of A, half of the columns' rows of B and 128 rows of the accumulator, so that per multiprocessor
+// and 64 of k 32 KB are fetched for 128 x 256 x 64 products: half of what two separate 128 x 256 tiles would fetch.  The grid is
+// persistent (one pair per two multiprocessors).  Roles: one thread issues the TMA loads into a six-stage ring, one
+// thread of the even CTA issues the MMAs, eight warps of each CTA work on the accumulators, of which tensor memory
+// holds two (512 columns), so that the epilogue of a unit runs beside the MMAs of the next.
+//
+// Whole waves of tiles run with all of k; the tiles of the last, partly filled wave are split over k so that every pair has
+// work.  Their partial sums go to the workspace and the last pair to arrive at a tile adds them in the order of k:
+// nobody waits, and the result does not depend on who is last.
+// Every wait on an mbarrier is bounded: one that runs out sets PSGD_W_TIMEOUT in the status word and the kernel ends.
+#pragma once
+#include <cuda_bf16.h>
+
+#include "psgd_ptx.cuh"
+
+namespace psgd {
+
+constexpr int TG_BM = 256;                    // rows of C per unit (128 per CTA)
+constexpr int TG_BN = 256;                    // columns of C per unit
+constexpr int TG_BK = 64;                     // k per stage: 128 bytes of bfloat16, one swizzle row
+constexpr int TG_STAGES = 6;
+constexpr int TG_HALF_BYTES = 128 * TG_BK * 2;          // one operand of one stage in one CTA
+constexpr int TG_STAGE_BYTES = 2 * TG_HALF_BYTES;
+constexpr int TG_EPI_WARPS = 8;
+constexpr int TG_THREADS = 64 + 32 * TG_EPI_WARPS;      // warp 0: TMA, warp 1: MMA and tensor-memory owner, warps 2-9: epilogue
+constexpr int TG_STAGING = 4096;              // per epilogue warp: a block turned from row-per-lane to row-contiguous
+constexpr int TG_PART = TG_BM * TG_BN;        // floats of one partial tile
+constexpr int XE_SEG = 128;                   // columns that share one softmax reference (the part of a tile one warp sees)
+
+inline size_t tile_smem_bytes() { return (size_t)TG_STAGES * TG_STAGE_BYTES + TG_EPI_WARPS * TG_STAGING + 1024 + 256; }
+
+enum TileEpilogue { EPI_LOSS = 0, EPI_SOFTMAX = 1, EPI_STORE = 2 };
+
+struct TileArgs {
+    int M, N, K;
+    int mt, nt, kb;            // tiles along M and N, stages along K
+    int full;                  // tiles done in one piece (the first `full` in raster order)
+    int S, kbps;               // pieces and stages per piece of every later tile
+    int units;
+    int gm;                    // raster: groups of gm row tiles, column by column
+    int kacc;                  // stages summed in one accumulator (0: all of them)
+    int* status;               // device status word
+    // EPI_STORE: out = scale * (sum + addend)
+    void* out;
+    long long ldo;             // elements
+    int out_f32, vec;          // vec: `out` (and its rows) aligned for 4 elements per store
+    const float* addend;       // [M][N] float32 or nullptr
+    const float* scale;        // DEVICE scalar or nullptr
+    float* part;               // [pieces][2][256][128]
+    int* counters;             // [tail tiles][2], zero
+    // EPI_LOSS, EPI_SOFTMAX
+    const long long* labels;
+    float2* stats;             // [M][nseg]: maximum and sum of exp(l - maximum) of each segment
+    float* label_logit;        // [M]
+    unsigned short* q;         // [M][ldq]: (maximum - l) log2(e) in steps of 2^-10, 65535 for "nothing left"
+    long long ldq;
+    int nseg;
+    int* clear;                // words to zero before the next kernel
+    int clear_n;
+};
+
+// Shared-memory matrix descriptors, 128-byte swizzle.  K-major: rows of 128 bytes, groups of 8 rows 1024 bytes apart.
+// MN-major: rows hold 64 consecutive m, groups of 8 k are 1024 bytes apart, blocks of 64 m TG_HALF_BYTES / 2 apart.
+template <bool MN>
+__device__ __forceinline__ unsigned long long tile_desc(unsigned addr) {
+    unsigned long long d = (unsigned long long)((addr >> 4) & 0x3FFF);
+    d |= (unsigned long long)(MN ? (TG_HALF_BYTES / 2) >> 4 : 1) << 16;
+    d |= (unsigned long long)(1024 >> 4) << 32;
+    d |= (unsigned long long)1 << 46;
+    d |= (unsigned long long)2 << 61;
+    return d;
+}
+// D float32, A and B bfloat16, M = 256 over the pair
+template <bool AMN, bool BMN>
+__device__ __forceinline__ unsigned tile_idesc(int n) {
+    return (1u << 4) | (1u << 7) | (1u << 10) | ((AMN ? 1u : 0u) << 15) | ((BMN ? 1u : 0u) << 16) | ((unsigned)(n >> 3) << 17) | ((unsigned)(TG_BM >> 4) << 24);
+}
+__device__ __forceinline__ void pair_mma(unsigned d, unsigned long long da, unsigned long long db, unsigned idesc, unsigned acc) {
+    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n"
+                 ::"r"(d), "l"(da), "l"(db), "r"(idesc), "r"(acc) : "memory");
+}
+// arrives on the barrier at this offset in both CTAs once every MMA issued so far has completed
+__device__ __forceinline__ void pair_commit(unsigned bar) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n" ::"r"(bar), "h"((unsigned short)3) : "memory");
+}
+// box into this CTA's shared memory, bytes counted by a barrier of the pair's even CTA
+__device__ __forceinline__ void pair_tma_2d(unsigned dst, const CUtensorMap* map, int x, int y, unsigned bar) {
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+__device__ __forceinline__ unsigned cluster_addr(unsigned local, unsigned rank) {
+    unsigned r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(r) : "r"(local), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ void mbar_arrive_cluster(unsigned bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];\n" ::"r"(bar) : "memory");
+}
+// 32 lanes x 32 consecutive columns of tensor memory -> 32 registers (lane = row of the accumulator)
+__device__ __forceinline__ void tmem_ld32(unsigned taddr, float (&f)[32]) {
+    unsigned v[32];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, "
+        "%23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]),
+          "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]),
+          "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+        : "r"(taddr) : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;\n" ::: "memory");
+#pragma unroll
+    for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(v[j]);
+}
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ unsigned pack_bf16(float lo, float hi) {
+    __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<unsigned*>(&h);
+}
+
+struct TileUnit { int m0, n0, kb0, kb1, piece, tail; };   // piece: index of the partial tile, -1 for a whole tile
+__device__ __forceinline__ TileUnit tile_unit(const TileArgs& a, int u) {
+    TileUnit w;
+    int tile = u;
+    w.kb0 = 0;
+    w.kb1 = a.kb;
+    w.piece = -1;
+    w.tail = 0;
+    if (u >= a.full) {
+        const int v = u - a.full;
+        w.tail = v / a.S;
+        tile = a.full + w.tail;
+        if (a.S > 1) {
+            w.piece = v;
+            w.kb0 = (v - w.tail * a.S) * a.kbps;
+            w.kb1 = min(a.kb, w.kb0 + a.kbps);
+        }
+    }
+    const int per = a.gm * a.nt, g = tile / per, in = tile - g * per;
+    const int rows = min(a.gm, a.mt - g * a.gm);
+    const int n = in / rows;
+    w.m0 = (g * a.gm + in - n * rows) * TG_BM;
+    w.n0 = n * TG_BN;
+    return w;
+}
+
+constexpr float LOG2E = 1.4426950408889634f;
+constexpr float XE_STEPS = 1024.f;            // steps per factor of two in the stored exponents
+constexpr float XE_MAGIC = 8388608.f;         // 2^23: adding it leaves the rounded whole number in the low mantissa bits
+constexpr unsigned XE_NONE = 65535u;
+
+template <int EPI, bool AMN, bool BMN>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TG_THREADS, 1)
+k_tile(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const TileArgs a) {
+    extern __shared__ __align__(16) unsigned char tg_smem_raw[];
+    // the offset of everything in shared memory is the same in both CTAs of the pair (descriptors and commits rely on it)
+    unsigned char* base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(tg_smem_raw) + 1023) & ~(uintptr_t)1023);
+    unsigned char* staging = base + (size_t)TG_STAGES * TG_STAGE_BYTES;
+    unsigned long long* bars = reinterpret_cast<unsigned long long*>(staging + TG_EPI_WARPS * TG_STAGING);
+    const unsigned bar_full = smem_u32(bars), bar_empty = bar_full + 8 * TG_STAGES;
+    const unsigned bar_accf = bar_empty + 8 * TG_STAGES, bar_acce = bar_accf + 16;
+    unsigned* tmem_slot = reinterpret_cast<unsigned*>(bars + 2 * TG_STAGES + 4);
+    int* last_slot = reinterpret_cast<int*>(tmem_slot + 1);
+    const unsigned smem_base = smem_u32(base);
+
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int rank = blockIdx.x & 1, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+
+    if (tid == 0) {
+        for (int s = 0; s < TG_STAGES; ++s) { mbar_init(bar_full + 8 * s, 1); mbar_init(bar_empty + 8 * s, 1); }
+        for (int b = 0; b < 2; ++b) { mbar_init(bar_accf + 8 * b, 1); mbar_init(bar_acce + 8 * b, 2 * TG_EPI_WARPS); }
+        asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;\n" ::"r"(smem_u32(tmem_slot)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;\n" ::: "memory");
+    }
+    if (EPI != EPI_STORE && blockIdx.x == 0)
+        for (int i = tid; i < a.clear_n; i += TG_THREADS) a.clear[i] = 0;
+    asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
+    __syncthreads();
+    cluster_arrive_release();
+    cluster_wait_acquire();
+    asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+    const unsigned tmem = *tmem_slot;
+    bool dead = false;
+
+    if (warp == 0) {
+        // ---- TMA producer of this CTA: its 128 rows of A and its half of B ----
+        if (lane == 0) {
+            int s = 0, filled = 0;
+            unsigned par = 1;                                  // a fresh barrier counts as released
+            for (int u = pair; u < a.units && !dead; u += pairs) {
+                const TileUnit w = tile_unit(a, u);
+                const int nh = (min(TG_BN, a.N - w.n0) + 31) / 32 * 16;
+                const int m = w.m0 + rank * 128, n = w.n0 + rank * nh;
+                for (int kb = w.kb0; kb < w.kb1 && !dead; ++kb) {
+                    mbar_wait_ready(bar_empty + 8 * s, par, a.status, dead);
+                    if (dead) break;
+                    const unsigned bar = cluster_addr(bar_full + 8 * s, 0);
+                    if (rank == 0) mbar_expect_tx(bar_full + 8 * s, 2 * TG_STAGE_BYTES);
+                    const unsigned da = smem_base + s * TG_STAGE_BYTES, db = da + TG_HALF_BYTES;
+                    const int k = kb * TG_BK;
+                    if (AMN) {
+                        pair_tma_2d(da, &tmA, m, k, bar);
+                        pair_tma_2d(da + TG_HALF_BYTES / 2, &tmA, m + 64, k, bar);
+                    } else {
+                        pair_tma_2d(da, &tmA, k, m, bar);
+                    }
+                    if (BMN) {
+                        pair_tma_2d(db, &tmB, n, k, bar);
+                        pair_tma_2d(db + TG_HALF_BYTES / 2, &tmB, n + 64, k, bar);
+                    } else {
+                        pair_tma_2d(db, &tmB, k, n, bar);
+                    }
+                    if (++s == TG_STAGES) { s = 0; par ^= 1; }
+                    if (filled < TG_STAGES) ++filled;
+                }
+            }
+            // every copy has landed and every release has arrived here before the CTA may go
+            for (int i = 0; i < filled && !dead; ++i) {
+                if (filled < TG_STAGES) mbar_wait_ready(bar_empty + 8 * i, 0u, a.status, dead);
+                else {
+                    mbar_wait_ready(bar_empty + 8 * s, par, a.status, dead);
+                    if (++s == TG_STAGES) { s = 0; par ^= 1; }
+                }
+            }
+            if (dead)
+                for (int i = 0; i < 200; ++i) __nanosleep(1000);   // copies in flight land
+        }
+    } else if (warp == 1) {
+        // ---- MMA issuer (even CTA) ----
+        if (lane == 0 && rank == 0) {
+            int s = 0, it = 0;
+            unsigned par = 0;
+            for (int u = pair; u < a.units && !dead; u += pairs) {
+                const TileUnit w = tile_unit(a, u);
+                const unsigned idesc = tile_idesc<AMN, BMN>((min(TG_BN, a.N - w.n0) + 31) / 32 * 32);
+                for (int k0 = w.kb0; k0 < w.kb1 && !dead; ++it) {
+                    const int k1 = a.kacc > 0 ? min(w.kb1, k0 + a.kacc) : w.kb1;
+                    const unsigned d = tmem + (unsigned)((it & 1) * TG_BN);
+                    if (it >= 2) {
+                        mbar_wait_ready(bar_acce + 8 * (it & 1), (unsigned)(((it >> 1) - 1) & 1), a.status, dead);
+                        asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+                    }
+                    for (int kb = k0; kb < k1 && !dead; ++kb) {
+                        mbar_wait_ready(bar_full + 8 * s, par, a.status, dead);
+                        if (dead) break;
+                        asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+                        const unsigned sa = smem_base + s * TG_STAGE_BYTES;
+                        const unsigned long long da = tile_desc<AMN>(sa), db = tile_desc<BMN>(sa + TG_HALF_BYTES);
+#pragma unroll
+                        for (int k = 0; k < TG_BK / 16; ++k)   // 16 of k: 32 bytes along a K-major row, two groups of 8 rows of an MN-major tile
+                            pair_mma(d, da + (unsigned long long)(k * (AMN ? 2048 >> 4 : 32 >> 4)), db + (unsigned long long)(k * (BMN ? 2048 >> 4 : 32 >> 4)), idesc,
+                                     (kb > k0 || k > 0) ? 1u : 0u);
+                        pair_commit(bar_empty + 8 * s);
+                        if (++s == TG_STAGES) { s = 0; par ^= 1; }
+                    }
+                    if (!dead) pair_commit(bar_accf + 8 * (it & 1));
+                    k0 = k1;
+                }
+            }
+        }
+    } else {
+        // ---- epilogue ----
+        const int quarter = warp & 3;                          // the tensor-memory lanes this warp may read
+        const int half = (warp - 2) >> 2;                      // columns half * 128 ... + 127
+        const unsigned lane_base = tmem + ((unsigned)(quarter * 32) << 16) + (unsigned)(half * 128);
+        float4* xb = reinterpret_cast<float4*>(staging + (size_t)(warp - 2) * TG_STAGING);
+        const int lrow = lane >> 3, lch = lane & 7;            // row-contiguous phase: row within a group of 4, 16-byte unit
+        const unsigned acce0 = cluster_addr(bar_acce, 0);
+        int it = 0;
+        for (int u = pair; u < a.units; u += pairs) {
+            const TileUnit w = tile_unit(a, u);
+            const int brow0 = w.m0 + rank * 128 + quarter * 32, col_base = w.n0 + half * 128;
+            if (EPI == EPI_STORE) {
+                const float scale = a.scale ? __ldg(a.scale) : 1.f;
+                // 32 x 32 block, a row per lane -> rows of 128 bytes through the staging buffer -> out
+                auto emit = [&](const float (&v)[32], int col0, const float* addend, long long lda) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) xb[lane * 8 + (j ^ (lane & 7))] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+                    __syncwarp();
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int br = 4 * i + lrow, row = brow0 + br, col = col0 + 4 * lch;
+                        float4 x = xb[br * 8 + (lch ^ (br & 7))];
+                        if (row < a.M && col < a.N) {
+                            if (a.vec && col + 4 <= a.N) {
+                                if (addend) {
+                                    const float4 y = *reinterpret_cast<const float4*>(addend + (size_t)row * lda + col);
+                                    x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+                                }
+                                x.x *= scale; x.y *= scale; x.z *= scale; x.w *= scale;
+                                if (a.out_f32) *reinterpret_cast<float4*>((float*)a.out + (size_t)row * a.ldo + col) = x;
+                                else *reinterpret_cast<uint2*>((__nv_bfloat16*)a.out + (size_t)row * a.ldo + col) = make_uint2(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w));
+                            } else {
+                                const float e[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                                for (int c = 0; c < 4; ++c)
+                                    if (col + c < a.N) {
+                                        const float y = (e[c] + (addend ? addend[(size_t)row * lda + col + c] : 0.f)) * scale;
+                                        if (a.out_f32) ((float*)a.out)[(size_t)row * a.ldo + col + c] = y;
+                                        else ((__nv_bfloat16*)a.out)[(size_t)row * a.ldo + col + c] = __float2bfloat16_rn(y);
+                                    }
+                            }
+                        }
+                    }
+                    __syncwarp();
+                };
+                // partial tiles: [column][row of this CTA], lanes of a warp side by side
+                float* part = w.piece >= 0 ? a.part + ((size_t)w.piece * 2 + rank) * (TG_PART / 2) + (size_t)(half * 128) * 128 + quarter * 32 + lane : nullptr;
+                for (int k0 = w.kb0; k0 < w.kb1; ++it) {
+                    const int k1 = a.kacc > 0 ? min(w.kb1, k0 + a.kacc) : w.kb1;
+                    mbar_wait_warp(bar_accf + 8 * (it & 1), (unsigned)((it >> 1) & 1), a.status, dead);
+                    asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+#pragma unroll 1
+                    for (int c = 0; c < 4; ++c) {
+                        if (col_base + 32 * c >= a.N) break;
+                        float v[32];
+                        tmem_ld32(lane_base + (unsigned)((it & 1) * TG_BN + 32 * c), v);
+                        if (part) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) {
+                                float* p = part + (size_t)(32 * c + j) * 128;
+                                *p = k0 > w.kb0 ? *p + v[j] : v[j];
+                            }
+                        } else {
+                            if (k0 > w.kb0) emit(v, col_base + 32 * c, (const float*)a.out, a.ldo);
+                            else emit(v, col_base + 32 * c, a.addend, a.N);
+                        }
+                    }
+                    asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster(acce0 + 8 * (it & 1));
+                    k0 = k1;
+                }
+                if (part) {
+                    // the last CTA to bring its rows of this tile adds the pieces in order
+                    __threadfence();
+                    asm volatile("bar.sync 1, 256;\n" ::: "memory");
+                    if (warp == 2 && lane == 0) *last_slot = atomicAdd(a.counters + 2 * w.tail + rank, 1) == a.S - 1;
+                    asm volatile("bar.sync 1, 256;\n" ::: "memory");
+                    if (*last_slot) {
+                        __threadfence();
+                        if (warp == 2 && lane == 0) a.counters[2 * w.tail + rank] = 0;   // as it was found
+                        const float* p0 = a.part + ((size_t)w.tail * a.S * 2 + rank) * (TG_PART / 2) + (size_t)(half * 128) * 128 + quarter * 32 + lane;
+#pragma unroll 1
+                        for (int c = 0; c < 4; ++c) {
+                            if (col_base + 32 * c >= a.N) break;
+                            float v[32];
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) v[j] = 0.f;
+                            for (int s = 0; s < a.S; ++s)
+#pragma unroll
+                                for (int j = 0; j < 32; ++j) v[j] += __ldcg(p0 + (size_t)s * TG_PART + (size_t)(32 * c + j) * 128);
+                            emit(v, col_base + 32 * c, a.addend, a.N);
+                        }
+                    }
+                }
+            } else {
+                // ---- softmax statistics of this warp's 128 columns, and the exponents in 16 bits ----
+                const int row = brow0 + lane;
+                const bool live = row < a.M;
+                const int b = it & 1;
+                const int label_col = live ? (int)min(max(a.labels[row] - (long long)col_base, -1ll), (long long)XE_SEG) : -1;   // column of the label within the segment
+                mbar_wait_warp(bar_accf + 8 * b, (unsigned)((it >> 1) & 1), a.status, dead);
+                asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+                const unsigned taddr = lane_base + (unsigned)(b * TG_BN);
+                const int ncols = min(XE_SEG, a.N - col_base);                     // (<= 0: nothing of this segment exists)
+                if (ncols > 0) {
+                    float top = -INFINITY;
+#pragma unroll 1
+                    for (int c = 0; c < XE_SEG / 32; ++c) {
+                        if (32 * c >= ncols) break;
+                        float v[32];
+                        tmem_ld32(taddr + 32 * c, v);
+                        if (32 * c + 32 <= ncols) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) top = fmaxf(top, v[j]);
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) if (32 * c + j < ncols) top = fmaxf(top, v[j]);
+                        }
+                        if (__any_sync(0xffffffffu, (label_col >> 5) == c)) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) if (label_col == 32 * c + j) a.label_logit[row] = v[j];
+                        }
+                    }
+                    const float ref = top == -INFINITY ? 0.f : top;                // nothing but -inf: exp(-inf - 0) = 0
+                    float sum = 0.f;
+#pragma unroll 1
+                    for (int c = 0; c < XE_SEG / 64; ++c) {
+                        if (64 * c >= ncols) break;
+                        unsigned pk[32];
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            float v[32];
+                            tmem_ld32(taddr + 64 * c + 32 * h, v);
+                            const int left = ncols - 64 * c - 32 * h;
+                            if (left < 32) {
+#pragma unroll
+                                for (int j = 0; j < 32; ++j) if (j >= left) v[j] = -INFINITY;
+                            }
+                            float part = 0.f;
+#pragma unroll
+                            for (int j = 0; j < 32; j += 2) {
+                                const float t0 = (v[j] - ref) * LOG2E, t1 = (v[j + 1] - ref) * LOG2E;     // <= 0
+                                part += ex2(t0) + ex2(t1);
+                                if (EPI == EPI_SOFTMAX) {
+                                    const float q0 = fminf(fmaf(t0, -XE_STEPS, XE_MAGIC), XE_MAGIC + 65535.f);
+                                    const float q1 = fminf(fmaf(t1, -XE_STEPS, XE_MAGIC), XE_MAGIC + 65535.f);
+                                    pk[16 * h + j / 2] = __byte_perm(__float_as_uint(q0), __float_as_uint(q1), 0x5410);
+                                }
+                            }
+                            sum += part;
+                        }
+                        if (EPI == EPI_SOFTMAX) {
+                            uint4* xq = reinterpret_cast<uint4*>(xb);
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) xq[lane * 8 + (j ^ (lane & 7))] = make_uint4(pk[4 * j], pk[4 * j + 1], pk[4 * j + 2], pk[4 * j + 3]);
+                            __syncwarp();
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                const int br = 4 * i + lrow;
+                                if (brow0 + br < a.M)      // rows of q are padded to whole segments
+                                    *reinterpret_cast<uint4*>(a.q + (size_t)(brow0 + br) * a.ldq + col_base + 64 * c + 8 * lch) = xq[br * 8 + (lch ^ (br & 7))];
+                            }
+                            __syncwarp();
+                        }
+                    }
+                    if (live) a.stats[(size_t)row * a.nseg + col_base / XE_SEG] = make_float2(top, sum);
+                }
+                asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(acce0 + 8 * b);
+                ++it;
+            }
+        }
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
+    __syncthreads();
+    cluster_arrive_release();
+    cluster_wait_acquire();
+    if (warp == 1) {
+        asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;\n" ::"r"(tmem) : "memory");
+    }
+}
+
+}  // namespace psgd

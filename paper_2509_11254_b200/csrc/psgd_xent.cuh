@@ -1,0 +1,196 @@
+// Row kernels of the last layer's softmax cross entropy.
+//
+//   lse_t = log sum_v exp(l_tv),   loss_t = lse_t - l_{t, y_t}   (0 where y_t is the ignored label),
+//   loss = sum_t w_t loss_t / Z,   Z = sum of w_t over the rows that count   (0 where Z = 0),
+//   d loss / d l_tv = w_t (exp(l_tv - lse_t) - [v = y_t]) / Z.
+//
+// The product kernel leaves, per row and segment of 128 columns, the maximum and the sum of exp(l - maximum), and per logit the
+// distance from its segment's maximum in steps of 2^-10 in the base-two exponent (16 bits, at most 3.4e-4 of relative error in p,
+// a sixth of the rounding of a bfloat16; the sums come from the unrounded logits).  k_xent_rows joins the segments of a row and
+// rewrites the 16 bits of every logit as the bfloat16 gradient w_t (p - [v = y_t]), the one rounding between the logits and the
+// products that follow.  1 / Z is left to those products' epilogues: it would put the same rounding error on every row.
+// Sums over rows and segments are formed in a fixed order; the last CTA to finish adds up the loss.
+#pragma once
+#include "psgd_tile.cuh"
+
+namespace psgd {
+
+constexpr int XE_THREADS = 256;
+constexpr int XE_W_LABEL = 8;      // == PSGD_W_LABEL
+
+struct RowsArgs {
+    int rows, V, nseg;
+    const float2* stats;
+    const float* label_logit;
+    const long long* labels;       // of these rows
+    long long ignore;
+    const float* weight;           // of these rows, or nullptr
+    float* loss;                   // of these rows
+    float* lse;
+    unsigned short* q;             // k_xent_rows: exponents in, gradients out
+    long long ldq;
+    int* status;
+    // the mean over all rows, by the last CTA
+    int* done;
+    int done_at;                   // CTAs that report, over all launches of this call
+    long long all_rows;
+    const long long* all_labels;
+    const float* all_weight;
+    const float* all_loss;
+    float* mean;
+};
+
+// weight of a row in the loss; `bad` rows have a label that is neither ignored nor a column
+__device__ __forceinline__ float row_weight(const float* weight, long long i, long long label, long long ignore, int V, bool& bad) {
+    const bool in = label >= 0 && label < V;
+    bad = !in && label != ignore;
+    return in && label != ignore ? (weight ? weight[i] : 1.f) : 0.f;
+}
+
+// Sums over the block of two values (fixed order); the result is valid in thread 0.
+template <int N>
+__device__ __forceinline__ double2 block_sum2(double x, double y) {
+    __shared__ double sx[N / 32], sy[N / 32];
+#pragma unroll
+    for (int o = 16; o; o >>= 1) { x += __shfl_xor_sync(0xffffffffu, x, o); y += __shfl_xor_sync(0xffffffffu, y, o); }
+    if ((threadIdx.x & 31) == 0) { sx[threadIdx.x >> 5] = x; sy[threadIdx.x >> 5] = y; }
+    __syncthreads();
+    if (threadIdx.x == 0)
+        for (int i = 1; i < N / 32; ++i) { x += sx[i]; y += sy[i]; }
+    return make_double2(x, y);
+}
+
+// 1 / Z, and the counters of the following kernels set to zero.  One CTA.
+__global__ void __launch_bounds__(1024) k_xent_norm(const long long* labels, const float* weight, long long rows, long long ignore, int V, float* inv, int* clear, int clear_n) {
+    for (int i = threadIdx.x; i < clear_n; i += 1024) clear[i] = 0;
+    double z = 0.0;
+    for (long long i = threadIdx.x; i < rows; i += 1024) {
+        bool bad;
+        z += row_weight(weight, i, labels[i], ignore, V, bad);
+    }
+    const double2 s = block_sum2<1024>(z, 0.0);
+    if (threadIdx.x == 0) *inv = s.x != 0.0 ? (float)(1.0 / s.x) : 0.f;
+}
+
+// the last CTA to get here adds up the loss of all rows
+__device__ __forceinline__ void report_rows(const RowsArgs& a) {
+    __shared__ int last;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        __threadfence();
+        last = atomicAdd(a.done, 1) == a.done_at - 1;
+    }
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    double num = 0.0, z = 0.0;
+    for (long long i = threadIdx.x; i < a.all_rows; i += XE_THREADS) {
+        bool bad;
+        const float w = row_weight(a.all_weight, i, a.all_labels[i], a.ignore, a.V, bad);
+        const float l = __ldcg(a.all_loss + i);
+        num += bad ? (double)l : (double)w * (double)l;        // a bad row's NaN reaches the mean
+        z += w;
+    }
+    const double2 s = block_sum2<XE_THREADS>(num, z);
+    if (threadIdx.x == 0) *a.mean = (s.y != 0.0 || s.x != s.x) ? (float)(s.x / s.y) : 0.f;
+}
+
+__device__ __forceinline__ void merge_stat(float& top, float& sum, float t, float s) {
+    const float m = fmaxf(top, t), r = m == -INFINITY ? 0.f : m;
+    sum = sum * ex2((top - r) * LOG2E) + s * ex2((t - r) * LOG2E);
+    top = m;
+}
+__device__ __forceinline__ void warp_stat(float& top, float& sum) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+        const float t = __shfl_xor_sync(0xffffffffu, top, o), s = __shfl_xor_sync(0xffffffffu, sum, o);
+        merge_stat(top, sum, t, s);
+    }
+}
+__device__ __forceinline__ void write_loss(const RowsArgs& a, int row, float lse) {
+    const long long label = a.labels[row];
+    const bool in = label >= 0 && label < a.V;
+    a.lse[row] = lse;
+    if (label == a.ignore) a.loss[row] = 0.f;
+    else if (in) a.loss[row] = lse - a.label_logit[row];
+    else { a.loss[row] = NAN; atomicOr(a.status, XE_W_LABEL); }
+}
+
+// Loss only: one warp per row.
+__global__ void __launch_bounds__(XE_THREADS) k_xent_loss(RowsArgs a) {
+    const int row = blockIdx.x * (XE_THREADS / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    if (row < a.rows) {
+        float top = -INFINITY, sum = 0.f;
+        for (int j = lane; j < a.nseg; j += 32) {
+            const float2 s = a.stats[(size_t)row * a.nseg + j];
+            merge_stat(top, sum, s.x, s.y);
+        }
+        warp_stat(top, sum);
+        if (lane == 0) write_loss(a, row, top + logf(sum));
+    }
+    report_rows(a);
+}
+
+// Loss and gradient of the logits: blockIdx.x = row, blockIdx.y = part of its columns.
+__global__ void __launch_bounds__(XE_THREADS) k_xent_rows(RowsArgs a) {
+    __shared__ float2 ws[XE_THREADS / 32];
+    const int row = blockIdx.x, tid = threadIdx.x;
+    const float2* st = a.stats + (size_t)row * a.nseg;
+    float top = -INFINITY, sum = 0.f;
+    for (int j = tid; j < a.nseg; j += XE_THREADS) merge_stat(top, sum, st[j].x, st[j].y);
+    warp_stat(top, sum);
+    if ((tid & 31) == 0) ws[tid >> 5] = make_float2(top, sum);
+    __syncthreads();
+    top = ws[0].x;
+    sum = ws[0].y;
+#pragma unroll
+    for (int i = 1; i < XE_THREADS / 32; ++i) merge_stat(top, sum, ws[i].x, ws[i].y);
+    const float lse = top + logf(sum);
+    if (blockIdx.y == 0 && tid == 0) write_loss(a, row, lse);
+
+    const long long label = a.labels[row];
+    bool bad;
+    const float w = row_weight(a.weight, row, label, a.ignore, a.V, bad);
+    const bool counts = !bad && label != a.ignore;
+    const float poison = lse - lse;                               // 0, or NaN where the row's logits were not finite
+    uint4* q = reinterpret_cast<uint4*>(a.q + (size_t)row * a.ldq);
+    const int units = (a.V + 7) / 8, per = (units + gridDim.y - 1) / gridDim.y;
+    const int u0 = blockIdx.y * per, u1 = min(units, u0 + per);
+    const int lunit = counts ? (int)(label >> 3) : -1;
+    constexpr int UN = 4;
+    for (int b = u0 + tid; b < u1; b += XE_THREADS * UN) {
+        uint4 v[UN];
+        float ref[UN];
+#pragma unroll
+        for (int i = 0; i < UN; ++i) {
+            const int u = b + i * XE_THREADS;
+            if (u < u1) { v[i] = q[u]; ref[i] = __ldg(&st[u / (XE_SEG / 8)].x); }
+        }
+#pragma unroll
+        for (int i = 0; i < UN; ++i) {
+            const int u = b + i * XE_THREADS;
+            if (u >= u1) break;
+            const float off = (ref[i] - lse) * LOG2E + poison;    // exponent of the segment's largest p
+            const unsigned x[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+            float d[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const unsigned bits = (j & 1) ? x[j / 2] >> 16 : x[j / 2] & 0xffffu;
+                const float steps = __uint_as_float(0x4B000000u | bits) - XE_MAGIC;
+                const float p = ex2(fmaf(steps, -1.f / XE_STEPS, off));
+                d[j] = (bits == XE_NONE ? poison : p) * w;
+            }
+            if (u == lunit) {
+                const int at = (int)(label & 7);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) if (j == at) d[j] -= w;
+            }
+            uint4 o = make_uint4(pack_bf16(d[0], d[1]), pack_bf16(d[2], d[3]), pack_bf16(d[4], d[5]), pack_bf16(d[6], d[7]));
+            if (!counts) o = make_uint4(0u, 0u, 0u, 0u);
+            q[u] = o;
+        }
+    }
+    report_rows(a);
+}
+
+}  // namespace psgd
