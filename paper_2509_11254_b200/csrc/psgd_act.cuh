@@ -121,9 +121,7 @@ __global__ void __launch_bounds__(256) k_act_pack(ActShape s, const X* x, long l
 }
 
 template <typename X>
-__global__ void __launch_bounds__(256) k_act_unpack(ActShape s, const int8_t* q, const uint8_t* scales, X* x, long long ldx, bool vec, int* clear, int clear_n) {
-    if (blockIdx.x == 0 && blockIdx.y == 0)
-        for (int i = threadIdx.y * blockDim.x + threadIdx.x; i < clear_n; i += blockDim.x * blockDim.y) clear[i] = 0;
+__global__ void __launch_bounds__(256) k_act_unpack(ActShape s, const int8_t* q, const uint8_t* scales, X* x, long long ldx, bool vec) {
     const ActCursor c = act_cursor();
     if (c.col >= s.F) return;
 #pragma unroll 2

@@ -15,40 +15,40 @@ using namespace psgd;
 namespace {
 
 constexpr int64_t MAX_EXTENT = (int64_t)1 << 30;
-constexpr int KACC_F32 = 64;       // stages (4096 of k) per accumulator where the result is float32, see plan_tiles
+constexpr int KACC_F32 = 32;       // stages (2048 of k) per accumulator where the result is float32: the tensor cores' additions truncate, and the
+                                   // error grows with the number of additions into one running sum (16384 of k: 1.3e-6 with 64, 0.6e-6 with 32)
 
-struct TilePlan { int mt, nt, kb, full, S, kbps, units, gm; };
+struct TilePlan { int mt, nt, kb, bn, full, S, kbps, tail, units, gm; };
 
-// Tiles of an M x N product over `pairs` CTA pairs.  The last, partly filled wave of R tiles is cut into S pieces of k each so
-// that ceil(R S / pairs) rounds of ceil(kb / S) stages take least; a round costs about 8 stages of its own (epilogue
-// and the pieces' way through memory), adding the pieces up about half a stage each.
-TilePlan plan_tiles(int64_t M, int64_t N, int64_t K, int pairs, bool split) {
+// Tiles of an M x N product over `pairs` CTA pairs.  The last, partly filled wave of R tiles may be cut into S pieces of k each, and
+// the tiles may be 192 or 128 columns wide instead of 256; both are chosen for the least time in units of one 256-column stage:
+// a round of units costs its stages and about 6 of its own, joining the pieces a launch and their way through memory.
+TilePlan plan_tiles(int64_t M, int64_t N, int64_t K, int pairs, bool store) {
     TilePlan p{};
     p.mt = ceil_div(M, TG_BM);
-    p.nt = ceil_div(N, TG_BN);
     p.kb = ceil_div(K, TG_BK);
-    const int64_t tiles = (int64_t)p.mt * p.nt;
-    const int R = (int)(tiles % pairs);
-    p.full = (int)(tiles - R);
-    p.S = 1;
-    p.kbps = p.kb;
-    if (split && R > 0) {
-        double best = 1e300;
-        for (int S = 1; S <= std::min(p.kb, 2 * pairs); ++S) {
+    double best = 1e300;
+    for (int bn = TG_BN; bn >= (store ? 128 : TG_BN); bn -= 64) {
+        const int nt = ceil_div(N, bn);
+        const double stage = bn == 256 ? 1.0 : bn == 192 ? 0.80 : 0.60;        // narrower tiles fetch more bytes per product
+        const int64_t tiles = (int64_t)p.mt * nt;
+        const int R = (int)(tiles % pairs);
+        const double whole = (double)(tiles / pairs) * (p.kb + 1) * stage;
+        for (int S = 1; S <= (store && R > 0 ? std::min(p.kb, 2 * pairs) : 1); ++S) {
             const int kbps = ceil_div(p.kb, S);
-            if (ceil_div(p.kb, kbps) != S) continue;                   // no empty pieces
-            const double cost = (double)ceil_div((int64_t)R * S, pairs) * (kbps + 8) + (S > 1 ? 4 + 0.5 * S : 0.0);
-            if (cost < best) { best = cost; p.S = S; p.kbps = kbps; }
+            if (ceil_div(p.kb, kbps) != S) continue;                           // no empty pieces
+            double cost = whole + (R > 0 ? (double)ceil_div((int64_t)R * S, pairs) * (kbps + 6) * stage : 0.0);
+            if (S > 1) cost += 12 + 0.06 * R * S;
+            if (cost < best) { best = cost; p.bn = bn; p.nt = nt; p.S = S; p.kbps = kbps; p.tail = R; p.full = (int)(tiles - R); }
         }
     }
-    p.units = p.full + R * p.S;
+    p.units = p.full + p.tail * p.S;
     // raster: all row tiles next to each other while the row operand fits beside the rest in L2, else as many as make the
     // pairs at work cover all columns
     p.gm = (M * K * 2 <= (40 << 20)) ? p.mt : std::min(p.mt, std::max(8, std::min(32, pairs / p.nt)));
     return p;
 }
 size_t part_bytes(const TilePlan& p) { return p.S > 1 ? (size_t)(p.units - p.full) * TG_PART * 4 : 0; }
-int tail_counters(const TilePlan& p) { return p.S > 1 ? 2 * ((p.units - p.full) / p.S) : 0; }
 
 // bfloat16 matrix, `rows` rows of `cols` with row stride ld (elements): boxes of 64 columns and `box` rows, 128-byte swizzle
 bool encode_operand(CUtensorMap* map, const void* p, int64_t rows, int64_t cols, int64_t ld, int box) {
@@ -68,13 +68,14 @@ template <int EPI, bool AMN, bool BMN>
 psgd_status launch_tile(const void* A, int64_t lda, const void* B, int64_t ldb, int64_t M, int64_t N, int64_t K, const TilePlan& p, TileArgs a, int pairs, cudaStream_t st) {
     CUtensorMap ma, mb;
     if (!(AMN ? encode_operand(&ma, A, K, M, lda, TG_BK) : encode_operand(&ma, A, M, K, lda, 128)) ||
-        !(BMN ? encode_operand(&mb, B, K, N, ldb, TG_BK) : encode_operand(&mb, B, N, K, ldb, 128)))
+        !(BMN ? encode_operand(&mb, B, K, N, ldb, TG_BK) : encode_operand(&mb, B, N, K, ldb, p.bn / 2)))
         return PSGD_E_CUDA;
     a.M = (int)M; a.N = (int)N; a.K = (int)K;
-    a.mt = p.mt; a.nt = p.nt; a.kb = p.kb; a.full = p.full; a.S = p.S; a.kbps = p.kbps; a.units = p.units; a.gm = p.gm;
+    a.mt = p.mt; a.nt = p.nt; a.kb = p.kb; a.bn = p.bn; a.full = p.full; a.S = p.S; a.kbps = p.kbps; a.tail = p.tail; a.units = p.units; a.gm = p.gm;
     const size_t smem = tile_smem_bytes();
     allow_smem(k_tile<EPI, AMN, BMN>, smem);
     k_tile<EPI, AMN, BMN><<<2 * std::min(p.units, pairs), TG_THREADS, smem, st>>>(ma, mb, a);
+    if (p.S > 1) k_join<<<dim3(p.tail, p.bn / 32, 2), 128, 0, st>>>(a);
     return cudaGetLastError() == cudaSuccess ? PSGD_OK : PSGD_E_CUDA;
 }
 
@@ -88,8 +89,7 @@ struct XentPlan {
     int pairs, nseg;
     int64_t ldq, piece, pieces;
     TilePlan logits, dh, dw;          // of a whole piece
-    size_t inv, done, counters, stats, label_logit, q, part, acc, total;
-    int n_counters;
+    size_t inv, done, stats, label_logit, q, part, acc, total;
 };
 // Tokens are taken in pieces, all columns at a time, so that the stored exponents stay within a fixed size however many
 // tokens there are; a piece has at least 1024 tokens, below which the products with the vocabulary matrix would be bound by reading it.
@@ -114,9 +114,7 @@ XentPlan plan_xent(int64_t T, int64_t V, int64_t D, bool grad) {
     if (grad) {
         x.dh = plan_tiles(x.piece, D, V, x.pairs, true);
         x.dw = plan_tiles(V, D, x.piece, x.pairs, true);
-        x.n_counters = std::max(1, 4 * x.pairs);      // two per tail tile, fewer than `pairs` tail tiles
     }
-    x.counters = take((size_t)x.n_counters * 4);
     x.stats = take((size_t)x.piece * x.nseg * 8);
     x.label_logit = take((size_t)x.piece * 4);
     if (grad) {
@@ -150,8 +148,7 @@ psgd_status xent(const void* H, int64_t ldh, const void* W, int64_t ldw, const i
     int* stat = status ? status : (int*)w;
     float* inv = (float*)(w + x.inv);
     int* done = (int*)(w + x.done);
-    int* counters = (int*)(w + x.counters);
-    if (grad) k_xent_norm<<<1, 1024, 0, st>>>((const long long*)labels, weight, T, ignore, (int)V, inv, done, (int)((x.stats - x.done) / 4));
+    if (grad) k_xent_norm<<<1, 1024, 0, st>>>((const long long*)labels, weight, T, ignore, (int)V, inv, done);
 
     RowsArgs r{};
     r.V = (int)V; r.nseg = x.nseg;
@@ -200,7 +197,6 @@ psgd_status xent(const void* H, int64_t ldh, const void* W, int64_t ldw, const i
         g.status = stat;
         g.scale = inv;
         g.part = (float*)(w + x.part);
-        g.counters = counters;
         g.out = (char*)dH + (size_t)t0 * lddh * 2;
         g.ldo = lddh;
         g.vec = ((uintptr_t)g.out & 7) == 0 && lddh % 4 == 0;
@@ -237,16 +233,14 @@ bool vec8(const void* p, int64_t ld, int dtype) { return aligned16(p) && ld % (d
 bool dtype_ok(int dtype) { return dtype == PSGD_DT_F32 || dtype == PSGD_DT_BF16; }
 bool ckpt_ok(const void* q) { return ((uintptr_t)q & 15) == 0; }
 
-struct WgradPlan { int pairs; int64_t ldx; TilePlan p; size_t counters, x, part, total; int n_counters; };
+struct WgradPlan { int pairs; int64_t ldx; TilePlan p; size_t x, part, total; };
 WgradPlan plan_wgrad(int64_t T, int64_t O, int64_t F) {
     WgradPlan g{};
     g.pairs = std::max(1, device_sms() / 2);
     g.ldx = (int64_t)align_up(F, ACT_GROUP);
     g.p = plan_tiles(O, F, T, g.pairs, true);
-    g.n_counters = tail_counters(g.p);
     size_t at = 256;
     auto take = [&](size_t bytes) { const size_t o = at; at = align_up(at + bytes, 256); return o; };
-    g.counters = take((size_t)g.n_counters * 4);
     g.x = take((size_t)T * g.ldx * 2);
     g.part = take(part_bytes(g.p));
     g.total = at;
@@ -300,8 +294,8 @@ psgd_status psgd_act_unpack(const int8_t* q, const uint8_t* scales, int64_t T, i
     if (ldx < F || !ckpt_ok(q)) return PSGD_E_INVALID;
     const ActShape s{T, (int)F, ceil_div(F, ACT_GROUP)};
     const ActGrid g = act_grid(T, s.G);
-    if (dtype == PSGD_DT_BF16) k_act_unpack<<<g.grid, g.block, 0, (cudaStream_t)stream>>>(s, q, scales, (__nv_bfloat16*)x, ldx, vec8(x, ldx, dtype), nullptr, 0);
-    else k_act_unpack<<<g.grid, g.block, 0, (cudaStream_t)stream>>>(s, q, scales, (float*)x, ldx, vec8(x, ldx, dtype), nullptr, 0);
+    if (dtype == PSGD_DT_BF16) k_act_unpack<<<g.grid, g.block, 0, (cudaStream_t)stream>>>(s, q, scales, (__nv_bfloat16*)x, ldx, vec8(x, ldx, dtype));
+    else k_act_unpack<<<g.grid, g.block, 0, (cudaStream_t)stream>>>(s, q, scales, (float*)x, ldx, vec8(x, ldx, dtype));
     return last_error();
 }
 
@@ -327,14 +321,13 @@ psgd_status psgd_act_wgrad(const void* dY, int64_t lddy, const int8_t* q, const 
     char* w = (char*)ws;
     const ActShape s{T, (int)F, ceil_div(F, ACT_GROUP)};
     const ActGrid ag = act_grid(T, s.G);
-    k_act_unpack<<<ag.grid, ag.block, 0, st>>>(s, q, scales, (__nv_bfloat16*)(w + g.x), g.ldx, true, (int*)(w + g.counters), g.n_counters);
+    k_act_unpack<<<ag.grid, ag.block, 0, st>>>(s, q, scales, (__nv_bfloat16*)(w + g.x), g.ldx, true);
     TileArgs a{};
     a.status = status ? status : (int*)w;
     a.out = dW; a.ldo = lddw; a.out_f32 = dtype == PSGD_DT_F32;
     a.vec = ((uintptr_t)dW & (a.out_f32 ? 15 : 7)) == 0 && lddw % 4 == 0;
     a.kacc = a.out_f32 ? KACC_F32 : 0;
     a.part = (float*)(w + g.part);
-    a.counters = (int*)(w + g.counters);
     return launch_tile<EPI_STORE, true, true>(dY, lddy, w + g.x, g.ldx, O, F, T, g.p, a, g.pairs, st);
 } catch (...) {
     return PSGD_E_CUDA;

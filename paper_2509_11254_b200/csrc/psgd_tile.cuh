@@ -15,8 +15,8 @@
 // holds two (512 columns), so that the epilogue of a unit runs beside the MMAs of the next.
 //
 // Whole waves of tiles run with all of k; the tiles of the last, partly filled wave are split over k so that every pair has
-// work.  Their partial sums go to the workspace and the last pair to arrive at a tile adds them in the order of k:
-// nobody waits, and the result does not depend on who is last.
+// work.  Their partial sums go to the workspace and k_join adds them in the order of k (a fixed order, no atomics; letting
+// the last pair to arrive add them up alone cost 25 us of a 172 us product, one multiprocessor cannot read faster).
 // Every wait on an mbarrier is bounded: one that runs out sets PSGD_W_TIMEOUT in the status word and the kernel ends.
 #pragma once
 #include <cuda_bf16.h>
@@ -44,8 +44,10 @@ enum TileEpilogue { EPI_LOSS = 0, EPI_SOFTMAX = 1, EPI_STORE = 2 };
 struct TileArgs {
     int M, N, K;
     int mt, nt, kb;            // tiles along M and N, stages along K
+    int bn;                    // columns per tile
     int full;                  // tiles done in one piece (the first `full` in raster order)
     int S, kbps;               // pieces and stages per piece of every later tile
+    int tail;                  // later tiles
     int units;
     int gm;                    // raster: groups of gm row tiles, column by column
     int kacc;                  // stages summed in one accumulator (0: all of them)
@@ -56,8 +58,7 @@ struct TileArgs {
     int out_f32, vec;          // vec: `out` (and its rows) aligned for 4 elements per store
     const float* addend;       // [M][N] float32 or nullptr
     const float* scale;        // DEVICE scalar or nullptr
-    float* part;               // [pieces][2][256][128]
-    int* counters;             // [tail tiles][2], zero
+    float* part;               // partial tiles [S][tail][2][256 columns][128 rows]
     // EPI_LOSS, EPI_SOFTMAX
     const long long* labels;
     float2* stats;             // [M][nseg]: maximum and sum of exp(l - maximum) of each segment
@@ -103,22 +104,28 @@ __device__ __forceinline__ unsigned cluster_addr(unsigned local, unsigned rank) 
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(r) : "r"(local), "r"(rank));
     return r;
 }
+// Arrival on a barrier of the pair's other CTA.  What it announces is that tensor memory has been read (tcgen05.wait::ld came
+// before); no global write has to be visible for that, and a release at cluster scope would wait for all of them.
 __device__ __forceinline__ void mbar_arrive_cluster(unsigned bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];\n" ::"r"(bar) : "memory");
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];\n" ::"r"(bar) : "memory");
 }
-// 32 lanes x 32 consecutive columns of tensor memory -> 32 registers (lane = row of the accumulator)
-__device__ __forceinline__ void tmem_ld32(unsigned taddr, float (&f)[32]) {
-    unsigned v[32];
+// 32 lanes x 32 consecutive columns of tensor memory -> 32 registers (lane = row of the accumulator); valid after tmem_wait
+__device__ __forceinline__ void tmem_ld32(unsigned taddr, float (&v)[32]) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, "
         "%23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n"
-        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]),
-          "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]),
-          "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+        : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]),
+          "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]), "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]),
+          "=f"(v[23]), "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
         : "r"(taddr) : "memory");
-    asm volatile("tcgen05.wait::ld.sync.aligned;\n" ::: "memory");
-#pragma unroll
-    for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(v[j]);
+}
+// the loaded registers pass through the wait, so that nothing that uses them can be scheduled before it
+__device__ __forceinline__ void tmem_wait(float (&v)[32]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;\n"
+                 : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]), "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]),
+                   "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]), "+f"(v[16]), "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]), "+f"(v[22]),
+                   "+f"(v[23]), "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]), "+f"(v[29]), "+f"(v[30]), "+f"(v[31])
+                 :: "memory");
 }
 __device__ __forceinline__ float ex2(float x) {
     float y;
@@ -130,30 +137,72 @@ __device__ __forceinline__ unsigned pack_bf16(float lo, float hi) {
     return *reinterpret_cast<unsigned*>(&h);
 }
 
-struct TileUnit { int m0, n0, kb0, kb1, piece, tail; };   // piece: index of the partial tile, -1 for a whole tile
+struct TileUnit { int m0, n0, kb0, kb1, piece; };   // piece: index of the partial tile, -1 for a whole tile
+__device__ __forceinline__ void tile_origin(const TileArgs& a, int tile, int& m0, int& n0) {
+    const int per = a.gm * a.nt, g = tile / per, in = tile - g * per;
+    const int rows = min(a.gm, a.mt - g * a.gm);
+    const int n = in / rows;
+    m0 = (g * a.gm + in - n * rows) * TG_BM;
+    n0 = n * a.bn;
+}
 __device__ __forceinline__ TileUnit tile_unit(const TileArgs& a, int u) {
     TileUnit w;
     int tile = u;
     w.kb0 = 0;
     w.kb1 = a.kb;
     w.piece = -1;
-    w.tail = 0;
-    if (u >= a.full) {
-        const int v = u - a.full;
-        w.tail = v / a.S;
-        tile = a.full + w.tail;
-        if (a.S > 1) {
-            w.piece = v;
-            w.kb0 = (v - w.tail * a.S) * a.kbps;
-            w.kb1 = min(a.kb, w.kb0 + a.kbps);
+    if (u >= a.full && a.S > 1) {
+        // all tiles' first pieces, then all second pieces: pairs at work together read the same range of k and share operands in L2
+        w.piece = u - a.full;
+        const int s = w.piece / a.tail;
+        tile = a.full + w.piece - s * a.tail;
+        w.kb0 = s * a.kbps;
+        w.kb1 = min(a.kb, w.kb0 + a.kbps);
+    }
+    tile_origin(a, tile, w.m0, w.n0);
+    return w;
+}
+
+// A 32 x 32 block of C, a row per lane -> rows of 128 bytes through the warp's staging buffer -> out (+ addend, * scale).
+// Row-per-lane stores would touch 32 lines per instruction.
+__device__ __forceinline__ void emit_block(const TileArgs& a, float4* xb, const float (&v)[32], int row0, int col0, const float* addend, long long lda, float scale) {
+    const int lane = threadIdx.x & 31, lrow = lane >> 3, lch = lane & 7;        // row within a group of 4, 16-byte unit
+    const int col = col0 + 4 * lch;
+    const bool wide = a.vec && col + 4 <= a.N;
+    float4 y[8];
+    if (addend && wide) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int row = row0 + 4 * i + lrow;
+            if (row < a.M) y[i] = *reinterpret_cast<const float4*>(addend + (size_t)row * lda + col);
         }
     }
-    const int per = a.gm * a.nt, g = tile / per, in = tile - g * per;
-    const int rows = min(a.gm, a.mt - g * a.gm);
-    const int n = in / rows;
-    w.m0 = (g * a.gm + in - n * rows) * TG_BM;
-    w.n0 = n * TG_BN;
-    return w;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) xb[lane * 8 + (j ^ (lane & 7))] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int br = 4 * i + lrow, row = row0 + br;
+        float4 x = xb[br * 8 + (lch ^ (br & 7))];
+        if (row < a.M && col < a.N) {
+            if (wide) {
+                if (addend) { x.x += y[i].x; x.y += y[i].y; x.z += y[i].z; x.w += y[i].w; }
+                x.x *= scale; x.y *= scale; x.z *= scale; x.w *= scale;
+                if (a.out_f32) *reinterpret_cast<float4*>((float*)a.out + (size_t)row * a.ldo + col) = x;
+                else *reinterpret_cast<uint2*>((__nv_bfloat16*)a.out + (size_t)row * a.ldo + col) = make_uint2(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w));
+            } else {
+                const float e[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    if (col + c < a.N) {
+                        const float z = (e[c] + (addend ? addend[(size_t)row * lda + col + c] : 0.f)) * scale;
+                        if (a.out_f32) ((float*)a.out)[(size_t)row * a.ldo + col + c] = z;
+                        else ((__nv_bfloat16*)a.out)[(size_t)row * a.ldo + col + c] = __float2bfloat16_rn(z);
+                    }
+            }
+        }
+    }
+    __syncwarp();
 }
 
 constexpr float LOG2E = 1.4426950408889634f;
@@ -172,7 +221,6 @@ k_tile(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
     const unsigned bar_full = smem_u32(bars), bar_empty = bar_full + 8 * TG_STAGES;
     const unsigned bar_accf = bar_empty + 8 * TG_STAGES, bar_acce = bar_accf + 16;
     unsigned* tmem_slot = reinterpret_cast<unsigned*>(bars + 2 * TG_STAGES + 4);
-    int* last_slot = reinterpret_cast<int*>(tmem_slot + 1);
     const unsigned smem_base = smem_u32(base);
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -200,17 +248,19 @@ k_tile(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
     if (warp == 0) {
         // ---- TMA producer of this CTA: its 128 rows of A and its half of B ----
         if (lane == 0) {
+            // bytes of B per stage: K-major boxes have bn / 2 rows, MN-major ones come in blocks of 64
+            const unsigned b_bytes = BMN ? (a.bn > 128 ? TG_HALF_BYTES : TG_HALF_BYTES / 2) : (unsigned)a.bn / 2 * TG_BK * 2;
             int s = 0, filled = 0;
             unsigned par = 1;                                  // a fresh barrier counts as released
             for (int u = pair; u < a.units && !dead; u += pairs) {
                 const TileUnit w = tile_unit(a, u);
-                const int nh = (min(TG_BN, a.N - w.n0) + 31) / 32 * 16;
+                const int nh = (min(a.bn, a.N - w.n0) + 31) / 32 * 16;
                 const int m = w.m0 + rank * 128, n = w.n0 + rank * nh;
                 for (int kb = w.kb0; kb < w.kb1 && !dead; ++kb) {
                     mbar_wait_ready(bar_empty + 8 * s, par, a.status, dead);
                     if (dead) break;
                     const unsigned bar = cluster_addr(bar_full + 8 * s, 0);
-                    if (rank == 0) mbar_expect_tx(bar_full + 8 * s, 2 * TG_STAGE_BYTES);
+                    if (rank == 0) mbar_expect_tx(bar_full + 8 * s, 2 * (TG_HALF_BYTES + b_bytes));
                     const unsigned da = smem_base + s * TG_STAGE_BYTES, db = da + TG_HALF_BYTES;
                     const int k = kb * TG_BK;
                     if (AMN) {
@@ -221,7 +271,7 @@ k_tile(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
                     }
                     if (BMN) {
                         pair_tma_2d(db, &tmB, n, k, bar);
-                        pair_tma_2d(db + TG_HALF_BYTES / 2, &tmB, n + 64, k, bar);
+                        if (a.bn > 128) pair_tma_2d(db + TG_HALF_BYTES / 2, &tmB, n + 64, k, bar);
                     } else {
                         pair_tma_2d(db, &tmB, k, n, bar);
                     }
@@ -247,7 +297,7 @@ k_tile(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
             unsigned par = 0;
             for (int u = pair; u < a.units && !dead; u += pairs) {
                 const TileUnit w = tile_unit(a, u);
-                const unsigned idesc = tile_idesc<AMN, BMN>((min(TG_BN, a.N - w.n0) + 31) / 32 * 32);
+                const unsigned idesc = tile_idesc<AMN, BMN>((min(a.bn, a.N - w.n0) + 31) / 32 * 32);
                 for (int k0 = w.kb0; k0 < w.kb1 && !dead; ++it) {
                     const int k1 = a.kacc > 0 ? min(w.kb1, k0 + a.kacc) : w.kb1;
                     const unsigned d = tmem + (unsigned)((it & 1) * TG_BN);
@@ -276,155 +326,130 @@ k_tile(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
     } else {
         // ---- epilogue ----
         const int quarter = warp & 3;                          // the tensor-memory lanes this warp may read
-        const int half = (warp - 2) >> 2;                      // columns half * 128 ... + 127
-        const unsigned lane_base = tmem + ((unsigned)(quarter * 32) << 16) + (unsigned)(half * 128);
+        const int half = (warp - 2) >> 2;                      // columns half * bn / 2 ...
+        const int hn = a.bn >> 1;
+        const unsigned lane_base = tmem + ((unsigned)(quarter * 32) << 16) + (unsigned)(half * hn);
         float4* xb = reinterpret_cast<float4*>(staging + (size_t)(warp - 2) * TG_STAGING);
-        const int lrow = lane >> 3, lch = lane & 7;            // row-contiguous phase: row within a group of 4, 16-byte unit
         const unsigned acce0 = cluster_addr(bar_acce, 0);
         int it = 0;
-        for (int u = pair; u < a.units; u += pairs) {
-            const TileUnit w = tile_unit(a, u);
-            const int brow0 = w.m0 + rank * 128 + quarter * 32, col_base = w.n0 + half * 128;
-            if (EPI == EPI_STORE) {
-                const float scale = a.scale ? __ldg(a.scale) : 1.f;
-                // 32 x 32 block, a row per lane -> rows of 128 bytes through the staging buffer -> out
-                auto emit = [&](const float (&v)[32], int col0, const float* addend, long long lda) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) xb[lane * 8 + (j ^ (lane & 7))] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-                    __syncwarp();
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int br = 4 * i + lrow, row = brow0 + br, col = col0 + 4 * lch;
-                        float4 x = xb[br * 8 + (lch ^ (br & 7))];
-                        if (row < a.M && col < a.N) {
-                            if (a.vec && col + 4 <= a.N) {
-                                if (addend) {
-                                    const float4 y = *reinterpret_cast<const float4*>(addend + (size_t)row * lda + col);
-                                    x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
-                                }
-                                x.x *= scale; x.y *= scale; x.z *= scale; x.w *= scale;
-                                if (a.out_f32) *reinterpret_cast<float4*>((float*)a.out + (size_t)row * a.ldo + col) = x;
-                                else *reinterpret_cast<uint2*>((__nv_bfloat16*)a.out + (size_t)row * a.ldo + col) = make_uint2(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w));
-                            } else {
-                                const float e[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-                                for (int c = 0; c < 4; ++c)
-                                    if (col + c < a.N) {
-                                        const float y = (e[c] + (addend ? addend[(size_t)row * lda + col + c] : 0.f)) * scale;
-                                        if (a.out_f32) ((float*)a.out)[(size_t)row * a.ldo + col + c] = y;
-                                        else ((__nv_bfloat16*)a.out)[(size_t)row * a.ldo + col + c] = __float2bfloat16_rn(y);
-                                    }
-                            }
-                        }
-                    }
-                    __syncwarp();
-                };
-                // partial tiles: [column][row of this CTA], lanes of a warp side by side
-                float* part = w.piece >= 0 ? a.part + ((size_t)w.piece * 2 + rank) * (TG_PART / 2) + (size_t)(half * 128) * 128 + quarter * 32 + lane : nullptr;
+        if (EPI == EPI_STORE) {
+            const float scale = a.scale ? __ldg(a.scale) : 1.f;
+            for (int u = pair; u < a.units; u += pairs) {
+                const TileUnit w = tile_unit(a, u);
+                const int row0 = w.m0 + rank * 128 + quarter * 32, col_base = w.n0 + half * hn;
+                const int chunks = min(hn / 32, max(0, (a.N - col_base + 31) / 32));      // blocks of 32 columns that exist
+                // partial tiles: lanes of a warp (rows) side by side
+                float* part = w.piece >= 0 ? a.part + ((size_t)w.piece * 2 + rank) * (TG_PART / 2) + (size_t)(half * hn) * 128 + quarter * 32 + lane : nullptr;
                 for (int k0 = w.kb0; k0 < w.kb1; ++it) {
                     const int k1 = a.kacc > 0 ? min(w.kb1, k0 + a.kacc) : w.kb1;
                     mbar_wait_warp(bar_accf + 8 * (it & 1), (unsigned)((it >> 1) & 1), a.status, dead);
                     asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
 #pragma unroll 1
-                    for (int c = 0; c < 4; ++c) {
-                        if (col_base + 32 * c >= a.N) break;
+                    for (int c = 0; c < chunks; ++c) {
                         float v[32];
                         tmem_ld32(lane_base + (unsigned)((it & 1) * TG_BN + 32 * c), v);
+                        tmem_wait(v);
+                        if (c == chunks - 1) {                 // the last read: the accumulator is free
+                            asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive_cluster(acce0 + 8 * (it & 1));
+                        }
+                        const bool more = k0 > w.kb0;          // the sum so far lies where this one goes
                         if (part) {
+                            float* p = part + (size_t)(32 * c) * 128;
+                            if (more) {
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) {
-                                float* p = part + (size_t)(32 * c + j) * 128;
-                                *p = k0 > w.kb0 ? *p + v[j] : v[j];
+                                for (int j = 0; j < 32; ++j) v[j] += p[j * 128];
                             }
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) p[j * 128] = v[j];
                         } else {
-                            if (k0 > w.kb0) emit(v, col_base + 32 * c, (const float*)a.out, a.ldo);
-                            else emit(v, col_base + 32 * c, a.addend, a.N);
+                            emit_block(a, xb, v, row0, col_base + 32 * c, more ? (const float*)a.out : a.addend, more ? a.ldo : (long long)a.N, scale);
                         }
                     }
-                    asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive_cluster(acce0 + 8 * (it & 1));
+                    if (chunks == 0 && lane == 0) mbar_arrive_cluster(acce0 + 8 * (it & 1));
                     k0 = k1;
                 }
-                if (part) {
-                    // the last CTA to bring its rows of this tile adds the pieces in order
-                    __threadfence();
-                    asm volatile("bar.sync 1, 256;\n" ::: "memory");
-                    if (warp == 2 && lane == 0) *last_slot = atomicAdd(a.counters + 2 * w.tail + rank, 1) == a.S - 1;
-                    asm volatile("bar.sync 1, 256;\n" ::: "memory");
-                    if (*last_slot) {
-                        __threadfence();
-                        if (warp == 2 && lane == 0) a.counters[2 * w.tail + rank] = 0;   // as it was found
-                        const float* p0 = a.part + ((size_t)w.tail * a.S * 2 + rank) * (TG_PART / 2) + (size_t)(half * 128) * 128 + quarter * 32 + lane;
-#pragma unroll 1
-                        for (int c = 0; c < 4; ++c) {
-                            if (col_base + 32 * c >= a.N) break;
-                            float v[32];
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) v[j] = 0.f;
-                            for (int s = 0; s < a.S; ++s)
-#pragma unroll
-                                for (int j = 0; j < 32; ++j) v[j] += __ldcg(p0 + (size_t)s * TG_PART + (size_t)(32 * c + j) * 128);
-                            emit(v, col_base + 32 * c, a.addend, a.N);
-                        }
-                    }
-                }
-            } else {
-                // ---- softmax statistics of this warp's 128 columns, and the exponents in 16 bits ----
-                const int row = brow0 + lane;
-                const bool live = row < a.M;
+            }
+        } else {
+            // ---- softmax statistics of this warp's 128 columns, and the exponents in 16 bits ----
+            const int lrow = lane >> 3, lch = lane & 7;
+            auto label_of = [&](const TileUnit& w) {           // column of the row's label, -1 where there is no row
+                const int row = w.m0 + rank * 128 + quarter * 32 + lane;
+                return row < a.M ? a.labels[row] : -1ll;
+            };
+            TileUnit next = tile_unit(a, pair);
+            long long next_label = label_of(next);
+            for (int u = pair; u < a.units; u += pairs, ++it) {
+                const TileUnit w = next;
+                const int row0 = w.m0 + rank * 128 + quarter * 32, col_base = w.n0 + half * XE_SEG, row = row0 + lane;
                 const int b = it & 1;
-                const int label_col = live ? (int)min(max(a.labels[row] - (long long)col_base, -1ll), (long long)XE_SEG) : -1;   // column of the label within the segment
+                const int label_col = (int)min(max(next_label - (long long)col_base, -1ll), (long long)XE_SEG);   // within the segment
+                if (u + pairs < a.units) {                     // asked for a tile ahead
+                    next = tile_unit(a, u + pairs);
+                    next_label = label_of(next);
+                }
                 mbar_wait_warp(bar_accf + 8 * b, (unsigned)((it >> 1) & 1), a.status, dead);
                 asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
                 const unsigned taddr = lane_base + (unsigned)(b * TG_BN);
                 const int ncols = min(XE_SEG, a.N - col_base);                     // (<= 0: nothing of this segment exists)
+                float top = -INFINITY, sum = 0.f;
                 if (ncols > 0) {
-                    float top = -INFINITY;
-#pragma unroll 1
-                    for (int c = 0; c < XE_SEG / 32; ++c) {
-                        if (32 * c >= ncols) break;
-                        float v[32];
-                        tmem_ld32(taddr + 32 * c, v);
-                        if (32 * c + 32 <= ncols) {
+                    // pass 1: the maximum (and the label's logit where it is among these columns)
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) top = fmaxf(top, v[j]);
+                    for (int c = 0; c < XE_SEG / 64; ++c) {
+                        float v[2][32];
+                        tmem_ld32(taddr + 64 * c, v[0]);
+                        tmem_ld32(taddr + 64 * c + 32, v[1]);
+                        tmem_wait(v[0]);
+                        tmem_wait(v[1]);
+                        const int left = ncols - 64 * c;
+                        float t[4] = {top, -INFINITY, -INFINITY, -INFINITY};
+                        if (left >= 64) {
+#pragma unroll
+                            for (int j = 0; j < 64; ++j) t[j & 3] = fmaxf(t[j & 3], v[j >> 5][j & 31]);
                         } else {
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) if (32 * c + j < ncols) top = fmaxf(top, v[j]);
+                            for (int j = 0; j < 64; ++j) if (j < left) t[j & 3] = fmaxf(t[j & 3], v[j >> 5][j & 31]);
                         }
-                        if (__any_sync(0xffffffffu, (label_col >> 5) == c)) {
+                        top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
+                        if (__any_sync(0xffffffffu, (label_col >> 6) == c)) {
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) if (label_col == 32 * c + j) a.label_logit[row] = v[j];
+                            for (int j = 0; j < 64; ++j) if (label_col == 64 * c + j) a.label_logit[row] = v[j >> 5][j & 31];
                         }
                     }
+                    // pass 2: exponents and their sum
                     const float ref = top == -INFINITY ? 0.f : top;                // nothing but -inf: exp(-inf - 0) = 0
-                    float sum = 0.f;
-#pragma unroll 1
+                    float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
                     for (int c = 0; c < XE_SEG / 64; ++c) {
                         if (64 * c >= ncols) break;
+                        float v[2][32];
+                        tmem_ld32(taddr + 64 * c, v[0]);
+                        tmem_ld32(taddr + 64 * c + 32, v[1]);
+                        tmem_wait(v[0]);
+                        tmem_wait(v[1]);
+                        if (64 * c + 64 >= ncols || c == XE_SEG / 64 - 1) {        // the last read: the accumulator is free
+                            asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive_cluster(acce0 + 8 * b);
+                        }
+                        const int left = ncols - 64 * c;
+                        if (left < 64) {
+#pragma unroll
+                            for (int j = 0; j < 64; ++j) if (j >= left) v[j >> 5][j & 31] = -INFINITY;
+                        }
                         unsigned pk[32];
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            float v[32];
-                            tmem_ld32(taddr + 64 * c + 32 * h, v);
-                            const int left = ncols - 64 * c - 32 * h;
-                            if (left < 32) {
-#pragma unroll
-                                for (int j = 0; j < 32; ++j) if (j >= left) v[j] = -INFINITY;
+                        for (int j = 0; j < 64; j += 2) {
+                            const float t0 = (v[j >> 5][j & 31] - ref) * LOG2E, t1 = (v[j >> 5][(j & 31) + 1] - ref) * LOG2E;     // <= 0
+                            part[j & 2] += ex2(t0);
+                            part[(j & 2) + 1] += ex2(t1);
+                            if (EPI == EPI_SOFTMAX) {
+                                const float q0 = fminf(fmaf(t0, -XE_STEPS, XE_MAGIC), XE_MAGIC + 65535.f);
+                                const float q1 = fminf(fmaf(t1, -XE_STEPS, XE_MAGIC), XE_MAGIC + 65535.f);
+                                pk[j / 2] = __byte_perm(__float_as_uint(q0), __float_as_uint(q1), 0x5410);
                             }
-                            float part = 0.f;
-#pragma unroll
-                            for (int j = 0; j < 32; j += 2) {
-                                const float t0 = (v[j] - ref) * LOG2E, t1 = (v[j + 1] - ref) * LOG2E;     // <= 0
-                                part += ex2(t0) + ex2(t1);
-                                if (EPI == EPI_SOFTMAX) {
-                                    const float q0 = fminf(fmaf(t0, -XE_STEPS, XE_MAGIC), XE_MAGIC + 65535.f);
-                                    const float q1 = fminf(fmaf(t1, -XE_STEPS, XE_MAGIC), XE_MAGIC + 65535.f);
-                                    pk[16 * h + j / 2] = __byte_perm(__float_as_uint(q0), __float_as_uint(q1), 0x5410);
-                                }
-                            }
-                            sum += part;
                         }
                         if (EPI == EPI_SOFTMAX) {
                             uint4* xq = reinterpret_cast<uint4*>(xb);
@@ -434,18 +459,18 @@ k_tile(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
 #pragma unroll
                             for (int i = 0; i < 8; ++i) {
                                 const int br = 4 * i + lrow;
-                                if (brow0 + br < a.M)      // rows of q are padded to whole segments
-                                    *reinterpret_cast<uint4*>(a.q + (size_t)(brow0 + br) * a.ldq + col_base + 64 * c + 8 * lch) = xq[br * 8 + (lch ^ (br & 7))];
+                                if (row0 + br < a.M)           // rows of q are padded to whole segments
+                                    *reinterpret_cast<uint4*>(a.q + (size_t)(row0 + br) * a.ldq + col_base + 64 * c + 8 * lch) = xq[br * 8 + (lch ^ (br & 7))];
                             }
                             __syncwarp();
                         }
                     }
-                    if (live) a.stats[(size_t)row * a.nseg + col_base / XE_SEG] = make_float2(top, sum);
+                    sum = (part[0] + part[1]) + (part[2] + part[3]);
+                    if (row < a.M) a.stats[(size_t)row * a.nseg + col_base / XE_SEG] = make_float2(top, sum);
+                } else {
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster(acce0 + 8 * b);
                 }
-                asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
-                __syncwarp();
-                if (lane == 0) mbar_arrive_cluster(acce0 + 8 * b);
-                ++it;
             }
         }
     }
@@ -457,6 +482,26 @@ k_tile(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
         asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;\n" ::"r"(tmem) : "memory");
     }
+}
+
+// Adds the pieces of the split tiles: blockIdx.x = tail tile, .y = 32 columns of it, .z = half of its rows; a warp per 32 rows.
+__global__ void __launch_bounds__(128) k_join(TileArgs a) {
+    __shared__ float4 xb[4][TG_STAGING / 16];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    int m0, n0;
+    tile_origin(a, a.full + blockIdx.x, m0, n0);
+    const int c = 32 * blockIdx.y, row0 = m0 + blockIdx.z * 128 + warp * 32;
+    if (n0 + c >= a.N || row0 >= a.M) return;
+    const float* p = a.part + ((size_t)blockIdx.x * 2 + blockIdx.z) * (TG_PART / 2) + (size_t)c * 128 + warp * 32 + lane;
+    const size_t step = (size_t)a.tail * TG_PART;
+    float v[32];
+#pragma unroll
+    for (int j = 0; j < 32; ++j) v[j] = p[(size_t)j * 128];
+#pragma unroll 2
+    for (int s = 1; s < a.S; ++s)
+#pragma unroll
+        for (int j = 0; j < 32; ++j) v[j] += p[(size_t)s * step + (size_t)j * 128];
+    emit_block(a, xb[warp], v, row0, n0 + c, a.addend, a.N, a.scale ? __ldg(a.scale) : 1.f);
 }
 
 }  // namespace psgd

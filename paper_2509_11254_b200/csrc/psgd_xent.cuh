@@ -60,9 +60,9 @@ __device__ __forceinline__ double2 block_sum2(double x, double y) {
     return make_double2(x, y);
 }
 
-// 1 / Z, and the counters of the following kernels set to zero.  One CTA.
-__global__ void __launch_bounds__(1024) k_xent_norm(const long long* labels, const float* weight, long long rows, long long ignore, int V, float* inv, int* clear, int clear_n) {
-    for (int i = threadIdx.x; i < clear_n; i += 1024) clear[i] = 0;
+// 1 / Z, and the counter of the row kernels set to zero.  One CTA.
+__global__ void __launch_bounds__(1024) k_xent_norm(const long long* labels, const float* weight, long long rows, long long ignore, int V, float* inv, int* done) {
+    if (threadIdx.x == 0) *done = 0;
     double z = 0.0;
     for (long long i = threadIdx.x; i < rows; i += 1024) {
         bool bad;
