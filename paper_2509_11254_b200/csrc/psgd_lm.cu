@@ -72,6 +72,7 @@ psgd_status launch_tile(const void* A, int64_t lda, const void* B, int64_t ldb, 
         return PSGD_E_CUDA;
     a.M = (int)M; a.N = (int)N; a.K = (int)K;
     a.mt = p.mt; a.nt = p.nt; a.kb = p.kb; a.bn = p.bn; a.full = p.full; a.S = p.S; a.kbps = p.kbps; a.tail = p.tail; a.units = p.units; a.gm = p.gm;
+    a.by_group = fast_div((unsigned)p.gm * p.nt); a.by_gm = fast_div(p.gm); a.by_rest = fast_div(std::max(1, p.mt % p.gm)); a.by_tail = fast_div(std::max(1, p.tail));
     const size_t smem = tile_smem_bytes();
     allow_smem(k_tile<EPI, AMN, BMN>, smem);
     k_tile<EPI, AMN, BMN><<<2 * std::min(p.units, pairs), TG_THREADS, smem, st>>>(ma, mb, a);
@@ -96,8 +97,8 @@ struct XentPlan {
 XentPlan plan_xent(int64_t T, int64_t V, int64_t D, bool grad) {
     XentPlan x{};
     x.pairs = std::max(1, device_sms() / 2);
-    x.nseg = ceil_div(V, XE_SEG);
-    x.ldq = (int64_t)x.nseg * XE_SEG;
+    x.nseg = ceil_div(V, grad ? XE_SEG : XE_SEG_LOSS);
+    x.ldq = (int64_t)align_up(V, XE_SEG);
     x.pieces = 1;
     x.piece = T;
     if (grad) {

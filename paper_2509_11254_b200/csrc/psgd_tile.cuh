@@ -35,11 +35,20 @@ constexpr int TG_EPI_WARPS = 8;
 constexpr int TG_THREADS = 64 + 32 * TG_EPI_WARPS;      // warp 0: TMA, warp 1: MMA and tensor-memory owner, warps 2-9: epilogue
 constexpr int TG_STAGING = 4096;              // per epilogue warp: a block turned from row-per-lane to row-contiguous
 constexpr int TG_PART = TG_BM * TG_BN;        // floats of one partial tile
-constexpr int XE_SEG = 128;                   // columns that share one softmax reference (the part of a tile one warp sees)
+constexpr int XE_SEG_LOSS = 128, XE_SEG = 64; // columns per softmax statistic: loss only, and where exponents are kept relative to its maximum
 
 inline size_t tile_smem_bytes() { return (size_t)TG_STAGES * TG_STAGE_BYTES + TG_EPI_WARPS * TG_STAGING + 1024 + 256; }
 
 enum TileEpilogue { EPI_LOSS = 0, EPI_SOFTMAX = 1, EPI_STORE = 2 };
+
+// Division by a launch constant: q = n * mul >> shift for 0 <= n < 2^31 (mul = floor(2^shift / d) + 1, shift = 31 + ceil(log2 d)).
+struct FastDiv { unsigned mul, shift; };
+inline FastDiv fast_div(unsigned d) {
+    unsigned l = 0;
+    while ((1ull << l) < d) ++l;
+    return {(unsigned)(((unsigned long long)1 << (31 + l)) / d + 1), 31 + l};
+}
+__device__ __forceinline__ int operator/(int n, FastDiv d) { return (int)(((unsigned long long)(unsigned)n * d.mul) >> d.shift); }
 
 struct TileArgs {
     int M, N, K;
@@ -50,6 +59,7 @@ struct TileArgs {
     int tail;                  // later tiles
     int units;
     int gm;                    // raster: groups of gm row tiles, column by column
+    FastDiv by_group, by_gm, by_rest, by_tail;   // gm * nt, gm, rows of the last group, tail
     int kacc;                  // stages summed in one accumulator (0: all of them)
     int* status;               // device status word
     // EPI_STORE: out = scale * (sum + addend)
@@ -65,7 +75,7 @@ struct TileArgs {
     float* label_logit;        // [M]
     unsigned short* q;         // [M][ldq]: (maximum - l) log2(e) in steps of 2^-10, 65535 for "nothing left"
     long long ldq;
-    int nseg;
+    int nseg;                  // statistics per row
     int* clear;                // words to zero before the next kernel
     int clear_n;
 };
@@ -139,9 +149,10 @@ __device__ __forceinline__ unsigned pack_bf16(float lo, float hi) {
 
 struct TileUnit { int m0, n0, kb0, kb1, piece; };   // piece: index of the partial tile, -1 for a whole tile
 __device__ __forceinline__ void tile_origin(const TileArgs& a, int tile, int& m0, int& n0) {
-    const int per = a.gm * a.nt, g = tile / per, in = tile - g * per;
-    const int rows = min(a.gm, a.mt - g * a.gm);
-    const int n = in / rows;
+    const int g = tile / a.by_group, in = tile - g * (a.gm * a.nt);
+    const bool rest = (g + 1) * a.gm > a.mt;
+    const int rows = rest ? a.mt - g * a.gm : a.gm;
+    const int n = in / (rest ? a.by_rest : a.by_gm);
     m0 = (g * a.gm + in - n * rows) * TG_BM;
     n0 = n * a.bn;
 }
@@ -154,7 +165,7 @@ __device__ __forceinline__ TileUnit tile_unit(const TileArgs& a, int u) {
     if (u >= a.full && a.S > 1) {
         // all tiles' first pieces, then all second pieces: pairs at work together read the same range of k and share operands in L2
         w.piece = u - a.full;
-        const int s = w.piece / a.tail;
+        const int s = w.piece / a.by_tail;
         tile = a.full + w.piece - s * a.tail;
         w.kb0 = s * a.kbps;
         w.kb1 = min(a.kb, w.kb0 + a.kbps);
@@ -373,8 +384,12 @@ k_tile(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
             }
         } else {
             // ---- softmax statistics of this warp's 128 columns, and the exponents in 16 bits ----
+            // 64 columns at a time, each read from tensor memory once: those reads take the MMAs' bandwidth to it (two passes, maximum first,
+            // cost 900 of the 9400 cycles of a 256 x 256 x 768 tile)
+            constexpr int CH = 64;
+            constexpr int SEG = EPI == EPI_LOSS ? XE_SEG_LOSS : XE_SEG;
             const int lrow = lane >> 3, lch = lane & 7;
-            auto label_of = [&](const TileUnit& w) {           // column of the row's label, -1 where there is no row
+            auto label_of = [&](const TileUnit& w) {           // the row's label, -1 where there is no row
                 const int row = w.m0 + rank * 128 + quarter * 32 + lane;
                 return row < a.M ? a.labels[row] : -1ll;
             };
@@ -382,9 +397,9 @@ k_tile(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
             long long next_label = label_of(next);
             for (int u = pair; u < a.units; u += pairs, ++it) {
                 const TileUnit w = next;
-                const int row0 = w.m0 + rank * 128 + quarter * 32, col_base = w.n0 + half * XE_SEG, row = row0 + lane;
+                const int row0 = w.m0 + rank * 128 + quarter * 32, col_base = w.n0 + half * 128, row = row0 + lane;
                 const int b = it & 1;
-                const int label_col = (int)min(max(next_label - (long long)col_base, -1ll), (long long)XE_SEG);   // within the segment
+                const int label_col = (int)min(max(next_label - (long long)col_base, -1ll), 128ll);   // among this warp's columns
                 if (u + pairs < a.units) {                     // asked for a tile ahead
                     next = tile_unit(a, u + pairs);
                     next_label = label_of(next);
@@ -392,85 +407,67 @@ k_tile(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
                 mbar_wait_warp(bar_accf + 8 * b, (unsigned)((it >> 1) & 1), a.status, dead);
                 asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
                 const unsigned taddr = lane_base + (unsigned)(b * TG_BN);
-                const int ncols = min(XE_SEG, a.N - col_base);                     // (<= 0: nothing of this segment exists)
+                const int ncols = min(128, a.N - col_base);                        // (<= 0: none of these columns exists)
                 float top = -INFINITY, sum = 0.f;
-                if (ncols > 0) {
-                    // pass 1: the maximum (and the label's logit where it is among these columns)
 #pragma unroll
-                    for (int c = 0; c < XE_SEG / 64; ++c) {
-                        float v[2][32];
-                        tmem_ld32(taddr + 64 * c, v[0]);
-                        tmem_ld32(taddr + 64 * c + 32, v[1]);
-                        tmem_wait(v[0]);
-                        tmem_wait(v[1]);
-                        const int left = ncols - 64 * c;
-                        float t[4] = {top, -INFINITY, -INFINITY, -INFINITY};
-                        if (left >= 64) {
-#pragma unroll
-                            for (int j = 0; j < 64; ++j) t[j & 3] = fmaxf(t[j & 3], v[j >> 5][j & 31]);
-                        } else {
-#pragma unroll
-                            for (int j = 0; j < 64; ++j) if (j < left) t[j & 3] = fmaxf(t[j & 3], v[j >> 5][j & 31]);
-                        }
-                        top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
-                        if (__any_sync(0xffffffffu, (label_col >> 6) == c)) {
-#pragma unroll
-                            for (int j = 0; j < 64; ++j) if (label_col == 64 * c + j) a.label_logit[row] = v[j >> 5][j & 31];
-                        }
+                for (int c = 0; c < 128 / CH; ++c) {
+                    const int left = ncols - CH * c;
+                    if (left <= 0) break;
+                    float v[2][32];
+                    tmem_ld32(taddr + CH * c, v[0]);
+                    tmem_ld32(taddr + CH * c + 32, v[1]);
+                    tmem_wait(v[0]);
+                    tmem_wait(v[1]);
+                    if (left <= CH || c == 128 / CH - 1) {                         // the last read: the accumulator is free
+                        asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive_cluster(acce0 + 8 * b);
                     }
-                    // pass 2: exponents and their sum
-                    const float ref = top == -INFINITY ? 0.f : top;                // nothing but -inf: exp(-inf - 0) = 0
-                    float part[4] = {0.f, 0.f, 0.f, 0.f};
+                    if (left < CH) {
 #pragma unroll
-                    for (int c = 0; c < XE_SEG / 64; ++c) {
-                        if (64 * c >= ncols) break;
-                        float v[2][32];
-                        tmem_ld32(taddr + 64 * c, v[0]);
-                        tmem_ld32(taddr + 64 * c + 32, v[1]);
-                        tmem_wait(v[0]);
-                        tmem_wait(v[1]);
-                        if (64 * c + 64 >= ncols || c == XE_SEG / 64 - 1) {        // the last read: the accumulator is free
-                            asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
-                            __syncwarp();
-                            if (lane == 0) mbar_arrive_cluster(acce0 + 8 * b);
-                        }
-                        const int left = ncols - 64 * c;
-                        if (left < 64) {
+                        for (int j = 0; j < CH; ++j) if (j >= left) v[j >> 5][j & 31] = -INFINITY;
+                    }
+                    if (__any_sync(0xffffffffu, (label_col >> 6) == c)) {
 #pragma unroll
-                            for (int j = 0; j < 64; ++j) if (j >= left) v[j >> 5][j & 31] = -INFINITY;
-                        }
-                        unsigned pk[32];
+                        for (int j = 0; j < CH; ++j) if (label_col == CH * c + j) a.label_logit[row] = v[j >> 5][j & 31];
+                    }
+                    float t[4] = {EPI == EPI_LOSS ? top : -INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                        for (int j = 0; j < 64; j += 2) {
-                            const float t0 = (v[j >> 5][j & 31] - ref) * LOG2E, t1 = (v[j >> 5][(j & 31) + 1] - ref) * LOG2E;     // <= 0
-                            part[j & 2] += ex2(t0);
-                            part[(j & 2) + 1] += ex2(t1);
-                            if (EPI == EPI_SOFTMAX) {
-                                const float q0 = fminf(fmaf(t0, -XE_STEPS, XE_MAGIC), XE_MAGIC + 65535.f);
-                                const float q1 = fminf(fmaf(t1, -XE_STEPS, XE_MAGIC), XE_MAGIC + 65535.f);
-                                pk[j / 2] = __byte_perm(__float_as_uint(q0), __float_as_uint(q1), 0x5410);
-                            }
-                        }
+                    for (int j = 0; j < CH; ++j) t[j & 3] = fmaxf(t[j & 3], v[j >> 5][j & 31]);
+                    const float m = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
+                    const float ref = m == -INFINITY ? 0.f : m;                    // nothing but -inf: exp(-inf - 0) = 0
+                    float part[4] = {EPI == EPI_LOSS ? sum * ex2((top - ref) * LOG2E) : 0.f, 0.f, 0.f, 0.f};
+                    unsigned pk[CH / 2];
+#pragma unroll
+                    for (int j = 0; j < CH; j += 2) {
+                        const float t0 = (v[j >> 5][j & 31] - ref) * LOG2E, t1 = (v[j >> 5][(j & 31) + 1] - ref) * LOG2E;     // <= 0
+                        part[j & 2] += ex2(t0);
+                        part[(j & 2) + 1] += ex2(t1);
                         if (EPI == EPI_SOFTMAX) {
-                            uint4* xq = reinterpret_cast<uint4*>(xb);
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) xq[lane * 8 + (j ^ (lane & 7))] = make_uint4(pk[4 * j], pk[4 * j + 1], pk[4 * j + 2], pk[4 * j + 3]);
-                            __syncwarp();
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) {
-                                const int br = 4 * i + lrow;
-                                if (row0 + br < a.M)           // rows of q are padded to whole segments
-                                    *reinterpret_cast<uint4*>(a.q + (size_t)(row0 + br) * a.ldq + col_base + 64 * c + 8 * lch) = xq[br * 8 + (lch ^ (br & 7))];
-                            }
-                            __syncwarp();
+                            const float q0 = fminf(fmaf(t0, -XE_STEPS, XE_MAGIC), XE_MAGIC + 65535.f);
+                            const float q1 = fminf(fmaf(t1, -XE_STEPS, XE_MAGIC), XE_MAGIC + 65535.f);
+                            pk[j / 2] = __byte_perm(__float_as_uint(q0), __float_as_uint(q1), 0x5410);
                         }
                     }
+                    top = m;
                     sum = (part[0] + part[1]) + (part[2] + part[3]);
-                    if (row < a.M) a.stats[(size_t)row * a.nseg + col_base / XE_SEG] = make_float2(top, sum);
-                } else {
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive_cluster(acce0 + 8 * b);
+                    if (EPI == EPI_SOFTMAX) {
+                        if (row < a.M) a.stats[(size_t)row * a.nseg + (col_base + CH * c) / SEG] = make_float2(top, sum);
+                        uint4* xq = reinterpret_cast<uint4*>(xb);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) xq[lane * 8 + (j ^ (lane & 7))] = make_uint4(pk[4 * j], pk[4 * j + 1], pk[4 * j + 2], pk[4 * j + 3]);
+                        __syncwarp();
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const int br = 4 * i + lrow;
+                            if (row0 + br < a.M)               // rows of q are padded to whole segments
+                                *reinterpret_cast<uint4*>(a.q + (size_t)(row0 + br) * a.ldq + col_base + CH * c + 8 * lch) = xq[br * 8 + (lch ^ (br & 7))];
+                        }
+                        __syncwarp();
+                    }
                 }
+                if (EPI == EPI_LOSS && ncols > 0 && row < a.M) a.stats[(size_t)row * a.nseg + col_base / SEG] = make_float2(top, sum);
+                if (ncols <= 0 && lane == 0) mbar_arrive_cluster(acce0 + 8 * b);
             }
         }
     }

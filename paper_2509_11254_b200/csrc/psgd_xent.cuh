@@ -4,7 +4,7 @@
 //   loss = sum_t w_t loss_t / Z,   Z = sum of w_t over the rows that count   (0 where Z = 0),
 //   d loss / d l_tv = w_t (exp(l_tv - lse_t) - [v = y_t]) / Z.
 //
-// The product kernel leaves, per row and segment of 128 columns, the maximum and the sum of exp(l - maximum), and per logit the
+// The product kernel leaves, per row and segment of 64 columns (128 without gradients), the maximum and the sum of exp(l - maximum), and per logit the
 // distance from its segment's maximum in steps of 2^-10 in the base-two exponent (16 bits, at most 3.4e-4 of relative error in p,
 // a sixth of the rounding of a bfloat16; the sums come from the unrounded logits).  k_xent_rows joins the segments of a row and
 // rewrites the 16 bits of every logit as the bfloat16 gradient w_t (p - [v = y_t]), the one rounding between the logits and the
@@ -84,12 +84,22 @@ __device__ __forceinline__ void report_rows(const RowsArgs& a) {
     if (!last) return;
     __threadfence();
     double num = 0.0, z = 0.0;
-    for (long long i = threadIdx.x; i < a.all_rows; i += XE_THREADS) {
-        bool bad;
-        const float w = row_weight(a.all_weight, i, a.all_labels[i], a.ignore, a.V, bad);
-        const float l = __ldcg(a.all_loss + i);
-        num += bad ? (double)l : (double)w * (double)l;        // a bad row's NaN reaches the mean
-        z += w;
+    constexpr int UN = 16;                                     // rows in flight per thread: alone on the GPU, this is all latency
+    for (long long b = threadIdx.x; b < a.all_rows; b += UN * XE_THREADS) {
+        float w[UN], l[UN];
+        bool bad[UN];
+#pragma unroll
+        for (int j = 0; j < UN; ++j) {
+            const long long i = b + j * XE_THREADS;
+            const bool in = i < a.all_rows;
+            w[j] = row_weight(in ? a.all_weight : nullptr, i, in ? a.all_labels[i] : a.ignore, a.ignore, a.V, bad[j]);
+            l[j] = in ? __ldcg(a.all_loss + i) : 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < UN; ++j) {
+            num += bad[j] ? (double)l[j] : (double)w[j] * (double)l[j];   // a bad row's NaN reaches the mean
+            z += w[j];
+        }
     }
     const double2 s = block_sum2<XE_THREADS>(num, z);
     if (threadIdx.x == 0) *a.mean = (s.y != 0.0 || s.x != s.x) ? (float)(s.x / s.y) : 0.f;
@@ -121,9 +131,12 @@ __global__ void __launch_bounds__(XE_THREADS) k_xent_loss(RowsArgs a) {
     const int row = blockIdx.x * (XE_THREADS / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
     if (row < a.rows) {
         float top = -INFINITY, sum = 0.f;
-        for (int j = lane; j < a.nseg; j += 32) {
-            const float2 s = a.stats[(size_t)row * a.nseg + j];
-            merge_stat(top, sum, s.x, s.y);
+        for (int j = lane; j < a.nseg; j += 8 * 32) {
+            float2 s[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[i] = j + 32 * i < a.nseg ? a.stats[(size_t)row * a.nseg + j + 32 * i] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) merge_stat(top, sum, s[i].x, s[i].y);
         }
         warp_stat(top, sum);
         if (lane == 0) write_loss(a, row, top + logf(sum));
