@@ -41,15 +41,18 @@ __device__ __forceinline__ void mbar_wait(unsigned bar, unsigned parity, int* fl
     dead = true;
     atomicOr(flags, FU_W_TIMEOUT);
 }
-// For a role played by a single thread whose barrier has usually completed already: a non-blocking test first.
-__device__ __forceinline__ void mbar_wait_ready(unsigned bar, unsigned parity, int* flags, bool& dead) {
+__device__ __forceinline__ bool mbar_test(unsigned bar, unsigned parity) {   // never blocks
     unsigned ok;
     asm volatile(
         "{\n.reg .pred p;\n"
         "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n"
         "selp.u32 %0, 1, 0, p;\n}\n"
         : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-    if (!ok) mbar_wait(bar, parity, flags, dead);
+    return ok != 0;
+}
+// For a role played by a single thread whose barrier has usually completed already: a non-blocking test first.
+__device__ __forceinline__ void mbar_wait_ready(unsigned bar, unsigned parity, int* flags, bool& dead) {
+    if (!mbar_test(bar, parity)) mbar_wait(bar, parity, flags, dead);
 }
 // The same wait for a whole warp (all 32 lanes must call it): lane 0 polls, pausing between polls, so that a waiting
 // warp puts one request at a time on the barrier instead of 32 (many warps polling at full rate slow down every other

@@ -137,6 +137,21 @@ __device__ __forceinline__ void tmem_wait(float (&v)[32]) {
                    "+f"(v[23]), "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]), "+f"(v[29]), "+f"(v[30]), "+f"(v[31])
                  :: "memory");
 }
+// One lane of a converged warp, the same one every time.  The warps that issue TMA loads and MMAs run their loops with all lanes and
+// enter only the issue itself with one: descriptors and addresses then stay in uniform registers, which takes an MMA
+// from 75 to 41 cycles of issue (a loop inside `if (lane == 0)` moves each operand to a uniform register every time).
+__device__ __forceinline__ bool elect_one() {
+    unsigned one;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}\n" : "=r"(one));
+    return one != 0;
+}
+// Wait of such a warp: a test that has usually succeeded, else polling; all lanes agree on `dead`.
+__device__ __forceinline__ void mbar_wait_all(unsigned bar, unsigned parity, int* flags, bool& dead) {
+    if (!__all_sync(0xffffffffu, mbar_test(bar, parity))) {
+        mbar_wait(bar, parity, flags, dead);
+        dead = __any_sync(0xffffffffu, dead);
+    }
+}
 __device__ __forceinline__ float ex2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -258,19 +273,20 @@ k_tile(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
 
     if (warp == 0) {
         // ---- TMA producer of this CTA: its 128 rows of A and its half of B ----
-        if (lane == 0) {
-            // bytes of B per stage: K-major boxes have bn / 2 rows, MN-major ones come in blocks of 64
-            const unsigned b_bytes = BMN ? (a.bn > 128 ? TG_HALF_BYTES : TG_HALF_BYTES / 2) : (unsigned)a.bn / 2 * TG_BK * 2;
-            int s = 0, filled = 0;
-            unsigned par = 1;                                  // a fresh barrier counts as released
-            for (int u = pair; u < a.units && !dead; u += pairs) {
-                const TileUnit w = tile_unit(a, u);
-                const int nh = (min(a.bn, a.N - w.n0) + 31) / 32 * 16;
-                const int m = w.m0 + rank * 128, n = w.n0 + rank * nh;
-                for (int kb = w.kb0; kb < w.kb1 && !dead; ++kb) {
-                    mbar_wait_ready(bar_empty + 8 * s, par, a.status, dead);
-                    if (dead) break;
-                    const unsigned bar = cluster_addr(bar_full + 8 * s, 0);
+        // bytes of B per stage: K-major boxes have bn / 2 rows, MN-major ones come in blocks of 64
+        const unsigned b_bytes = BMN ? (a.bn > 128 ? TG_HALF_BYTES : TG_HALF_BYTES / 2) : (unsigned)a.bn / 2 * TG_BK * 2;
+        const unsigned full0 = cluster_addr(bar_full, 0);
+        int s = 0, filled = 0;
+        unsigned par = 1;                                      // a fresh barrier counts as released
+        for (int u = pair; u < a.units && !dead; u += pairs) {
+            const TileUnit w = tile_unit(a, u);
+            const int nh = (min(a.bn, a.N - w.n0) + 31) / 32 * 16;
+            const int m = w.m0 + rank * 128, n = w.n0 + rank * nh;
+            for (int kb = w.kb0; kb < w.kb1; ++kb) {
+                mbar_wait_all(bar_empty + 8 * s, par, a.status, dead);
+                if (dead) break;
+                if (elect_one()) {
+                    const unsigned bar = full0 + 8 * s;
                     if (rank == 0) mbar_expect_tx(bar_full + 8 * s, 2 * (TG_HALF_BYTES + b_bytes));
                     const unsigned da = smem_base + s * TG_STAGE_BYTES, db = da + TG_HALF_BYTES;
                     const int k = kb * TG_BK;
@@ -286,24 +302,23 @@ k_tile(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
                     } else {
                         pair_tma_2d(db, &tmB, k, n, bar);
                     }
-                    if (++s == TG_STAGES) { s = 0; par ^= 1; }
-                    if (filled < TG_STAGES) ++filled;
                 }
+                __syncwarp();
+                if (++s == TG_STAGES) { s = 0; par ^= 1; }
+                if (filled < TG_STAGES) ++filled;
             }
-            // every copy has landed and every release has arrived here before the CTA may go
-            for (int i = 0; i < filled && !dead; ++i) {
-                if (filled < TG_STAGES) mbar_wait_ready(bar_empty + 8 * i, 0u, a.status, dead);
-                else {
-                    mbar_wait_ready(bar_empty + 8 * s, par, a.status, dead);
-                    if (++s == TG_STAGES) { s = 0; par ^= 1; }
-                }
-            }
-            if (dead)
-                for (int i = 0; i < 200; ++i) __nanosleep(1000);   // copies in flight land
         }
+        // every copy has landed and every release has arrived here before the CTA may go
+        if (filled < TG_STAGES) { s = 0; par = 0; }
+        for (int i = 0; i < filled && !dead; ++i) {
+            mbar_wait_all(bar_empty + 8 * s, par, a.status, dead);
+            if (++s == TG_STAGES) { s = 0; par ^= 1; }
+        }
+        if (dead)
+            for (int i = 0; i < 200; ++i) __nanosleep(1000);   // copies in flight land
     } else if (warp == 1) {
         // ---- MMA issuer (even CTA) ----
-        if (lane == 0 && rank == 0) {
+        if (rank == 0) {
             int s = 0, it = 0;
             unsigned par = 0;
             for (int u = pair; u < a.units && !dead; u += pairs) {
@@ -313,23 +328,25 @@ k_tile(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
                     const int k1 = a.kacc > 0 ? min(w.kb1, k0 + a.kacc) : w.kb1;
                     const unsigned d = tmem + (unsigned)((it & 1) * TG_BN);
                     if (it >= 2) {
-                        mbar_wait_ready(bar_acce + 8 * (it & 1), (unsigned)(((it >> 1) - 1) & 1), a.status, dead);
+                        mbar_wait_all(bar_acce + 8 * (it & 1), (unsigned)(((it >> 1) - 1) & 1), a.status, dead);
                         asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
                     }
-                    for (int kb = k0; kb < k1 && !dead; ++kb) {
-                        mbar_wait_ready(bar_full + 8 * s, par, a.status, dead);
+                    for (int kb = k0; kb < k1; ++kb) {
+                        mbar_wait_all(bar_full + 8 * s, par, a.status, dead);
                         if (dead) break;
-                        asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
                         const unsigned sa = smem_base + s * TG_STAGE_BYTES;
                         const unsigned long long da = tile_desc<AMN>(sa), db = tile_desc<BMN>(sa + TG_HALF_BYTES);
+                        if (elect_one()) {
 #pragma unroll
-                        for (int k = 0; k < TG_BK / 16; ++k)   // 16 of k: 32 bytes along a K-major row, two groups of 8 rows of an MN-major tile
-                            pair_mma(d, da + (unsigned long long)(k * (AMN ? 2048 >> 4 : 32 >> 4)), db + (unsigned long long)(k * (BMN ? 2048 >> 4 : 32 >> 4)), idesc,
-                                     (kb > k0 || k > 0) ? 1u : 0u);
-                        pair_commit(bar_empty + 8 * s);
+                            for (int k = 0; k < TG_BK / 16; ++k)   // 16 of k: 32 bytes along a K-major row, two groups of 8 rows of an MN-major tile
+                                pair_mma(d, da + (unsigned long long)(k * (AMN ? 2048 >> 4 : 32 >> 4)), db + (unsigned long long)(k * (BMN ? 2048 >> 4 : 32 >> 4)), idesc,
+                                         (kb > k0 || k > 0) ? 1u : 0u);
+                            pair_commit(bar_empty + 8 * s);
+                            if (kb == k1 - 1) pair_commit(bar_accf + 8 * (it & 1));
+                        }
+                        __syncwarp();
                         if (++s == TG_STAGES) { s = 0; par ^= 1; }
                     }
-                    if (!dead) pair_commit(bar_accf + 8 * (it & 1));
                     k0 = k1;
                 }
             }
