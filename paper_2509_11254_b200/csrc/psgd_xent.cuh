@@ -87,18 +87,19 @@ __device__ __forceinline__ void report_rows(const RowsArgs& a) {
     constexpr int UN = 16;                                     // rows in flight per thread: alone on the GPU, this is all latency
     for (long long b = threadIdx.x; b < a.all_rows; b += UN * XE_THREADS) {
         float w[UN], l[UN];
-        bool bad[UN];
+        long long label[UN];
 #pragma unroll
-        for (int j = 0; j < UN; ++j) {
-            const long long i = b + j * XE_THREADS;
-            const bool in = i < a.all_rows;
-            w[j] = row_weight(in ? a.all_weight : nullptr, i, in ? a.all_labels[i] : a.ignore, a.ignore, a.V, bad[j]);
-            l[j] = in ? __ldcg(a.all_loss + i) : 0.f;
+        for (int j = 0; j < UN; ++j) {                         // loads without branches around them, so that they are all in flight
+            const long long i = min(b + j * XE_THREADS, a.all_rows - 1);
+            label[j] = __ldg(a.all_labels + i);
+            l[j] = __ldcg(a.all_loss + i);
+            w[j] = a.all_weight ? __ldg(a.all_weight + i) : 1.f;
         }
 #pragma unroll
         for (int j = 0; j < UN; ++j) {
-            num += bad[j] ? (double)l[j] : (double)w[j] * (double)l[j];   // a bad row's NaN reaches the mean
-            z += w[j];
+            const bool in = label[j] >= 0 && label[j] < a.V, skip = label[j] == a.ignore || b + j * XE_THREADS >= a.all_rows;
+            num += skip ? 0.0 : in ? (double)w[j] * (double)l[j] : (double)l[j];   // a bad row's NaN reaches the mean
+            z += skip || !in ? 0.0 : (double)w[j];
         }
     }
     const double2 s = block_sum2<XE_THREADS>(num, z);
