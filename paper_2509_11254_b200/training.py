@@ -15,6 +15,7 @@ from __future__ import annotations
 import contextlib
 import ctypes as C
 from collections import namedtuple
+from functools import lru_cache
 
 import torch
 
@@ -22,118 +23,134 @@ from .binding import PSGDError, _check, lib
 
 PSGD_W_LABEL = 8
 GROUP = 32
+_BF16 = torch.bfloat16
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1}
 
 CrossEntropy = namedtuple("CrossEntropy", "loss token_loss lse")
 CrossEntropyGrad = namedtuple("CrossEntropyGrad", "loss token_loss lse d_hidden d_weight")
 
+_empty = torch.empty
+
 
 # ---- arguments ----------------------------------------------------------------------------------------------------
-def _matrix(t, name, dtypes=(torch.bfloat16,), shape=None, device=None):
-    """A CUDA matrix with unit column stride; returns it."""
+def _name(dtype):
+    return str(dtype).replace("torch.", "")
+
+
+def _matrix(t, name, dtypes=(_BF16,), shape=None, device=None):
+    """Refuses what is not a CUDA matrix with unit column stride; returns (rows, columns, row stride in elements)."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise PSGDError(f"{name} must be a CUDA tensor")
     if t.dtype not in dtypes:
-        raise PSGDError(f"{name} must be {' or '.join(str(d).replace('torch.', '') for d in dtypes)}, not {str(t.dtype).replace('torch.', '')}")
-    if t.dim() != 2 or (shape is not None and tuple(t.shape) != tuple(shape)):
-        raise PSGDError(f"{name} must have shape {tuple(shape) if shape is not None else '(rows, columns)'}, not {tuple(t.shape)}")
-    if t.shape[1] < 1:
+        raise PSGDError(f"{name} must be {' or '.join(map(_name, dtypes))}, not {_name(t.dtype)}")
+    size = t.shape
+    if len(size) != 2 or (shape is not None and size != shape):
+        raise PSGDError(f"{name} must have shape {tuple(shape) if shape is not None else '(rows, columns)'}, not {tuple(size)}")
+    rows, cols = size
+    if cols < 1:
         raise PSGDError(f"{name} has no columns")
-    if t.stride(1) != 1 and t.shape[1] > 1 or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+    ld, one = t.stride()
+    if rows <= 1:
+        ld = cols                                   # the stride of a single row is never used
+    if one != 1 and cols > 1 or ld < cols:
         raise PSGDError(f"{name} must have unit column stride and rows that do not overlap")
     if device is not None and t.device != device:
         raise PSGDError(f"{name} is on {t.device}, expected {device}")
-    return t
+    return rows, cols, ld
 
 
 def _vector(t, name, dtype, n, device):
+    """The address of a contiguous CUDA vector."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != dtype or t.shape != (n,) or not t.is_contiguous() or t.device != device:
-        raise PSGDError(f"{name} must be a contiguous {str(dtype).replace('torch.', '')} tensor of {n} elements on {device}")
-    return t
+        raise PSGDError(f"{name} must be a contiguous {_name(dtype)} tensor of {n} elements on {device}")
+    return t.data_ptr()
 
 
 def _status(t, device):
-    return _vector(t, "status", torch.int32, 1, device).data_ptr() if t is not None else None
+    return _vector(t, "status", torch.int32, 1, device) if t is not None else None
 
 
-def _ld(t):
-    """Row stride in elements (of a single row: its length)."""
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
-
-
-def _operand(t):
-    """`t` itself where the tensor cores' loads can read it in place (16-byte aligned rows), else a copy with padded rows."""
-    if t.data_ptr() % 16 == 0 and (t.shape[0] <= 1 or t.stride(0) % 8 == 0):
-        return t
-    rows, cols = t.shape
-    return torch.empty((rows, -(-cols // 8) * 8), dtype=t.dtype, device=t.device)[:, :cols].copy_(t)
+def _operand(t, rows, cols, ld):
+    """(tensor, row stride): `t` itself where the tensor cores' loads can read it in place (16-byte aligned rows), else a copy with padded rows."""
+    if t.data_ptr() % 16 == 0 and (rows <= 1 or ld % 8 == 0):
+        return t, ld
+    ld = -(-cols // 8) * 8
+    return _empty((rows, ld), dtype=t.dtype, device=t.device)[:, :cols].copy_(t), ld
 
 
 @contextlib.contextmanager
 def _on_other(device, stream):
     with torch.cuda.device(device), torch.cuda.stream(stream):
-        yield C.c_void_p(stream.cuda_stream)
+        yield stream.cuda_stream
 
 
 class _OnCurrent:
     """The common case without the cost of switching: the tensor's device is current and so is its stream."""
 
+    __slots__ = ("stream",)
+
     def __init__(self, stream):
-        self.ptr = C.c_void_p(stream)
+        self.stream = stream
 
     def __enter__(self):
-        return self.ptr
+        return self.stream
 
     def __exit__(self, *a):
         return False
+
+
+# the handle of the current stream without the object around it, where torch has it
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
 def _on(device, stream):
     """Makes `device` and `stream` current, so that what is allocated inside belongs to that stream."""
     if stream is None:
         if device.index == torch.cuda.current_device():
-            return _OnCurrent(torch.cuda.current_stream(device).cuda_stream)
+            return _OnCurrent(_raw_stream(device.index))
         stream = torch.cuda.current_stream(device)
     return _on_other(device, stream)
 
 
+@lru_cache(maxsize=256)
+def _workspace_bytes(call, *args):
+    """What a workspace query of the library answers; `args` end with the device index (the answer depends on its multiprocessors)."""
+    n = C.c_size_t()
+    _check(getattr(lib(), call)(*args[:-1], C.byref(n)))
+    return n.value
+
+
 # ---- cross entropy ------------------------------------------------------------------------------------------------
 def _xent(grad, hidden, weight, labels, token_weight, ignore_index, d_hidden, d_weight, status, stream):
-    _matrix(hidden, "hidden")
-    T, D = hidden.shape
+    T, D, ldh = _matrix(hidden, "hidden")
     dev = hidden.device
-    _matrix(weight, "weight", device=dev)
-    if weight.shape[1] != D or weight.shape[0] < 1:
+    V, Dw, ldw = _matrix(weight, "weight", device=dev)
+    if Dw != D or V < 1:
         raise PSGDError(f"weight must have shape (vocabulary, {D}), not {tuple(weight.shape)}")
-    V = weight.shape[0]
-    _vector(labels, "labels", torch.int64, T, dev)
-    if token_weight is not None:
-        _vector(token_weight, "token_weight", torch.float32, T, dev)
-    if d_hidden is not None:
-        _matrix(d_hidden, "d_hidden", shape=(T, D), device=dev)
-    if d_weight is not None:
-        _matrix(d_weight, "d_weight", shape=(V, D), device=dev)
-    st = _status(status, dev)
-    L = lib()
-    nbytes = C.c_size_t()
+    at_labels = _vector(labels, "labels", torch.int64, T, dev)
+    at_weight = _vector(token_weight, "token_weight", torch.float32, T, dev) if token_weight is not None else None
+    lddh = _matrix(d_hidden, "d_hidden", shape=(T, D), device=dev)[2] if d_hidden is not None else D
+    lddw = _matrix(d_weight, "d_weight", shape=(V, D), device=dev)[2] if d_weight is not None else D
+    at_status = _status(status, dev)
     with _on(dev, stream) as s:
-        _check(L.psgd_xent_workspace(T, V, D, int(grad), C.byref(nbytes)))
-        hidden, weight = _operand(hidden), _operand(weight)
-        ws = torch.empty((nbytes.value,), dtype=torch.uint8, device=dev)
-        rows = torch.empty((2, T), dtype=torch.float32, device=dev)
-        loss = torch.empty((), dtype=torch.float32, device=dev)
-        token_loss, lse = rows[0], rows[1]
-        args = [hidden.data_ptr(), _ld(hidden), weight.data_ptr(), _ld(weight), labels.data_ptr(), token_weight.data_ptr() if token_weight is not None else None,
-                ignore_index, T, V, D, loss.data_ptr(), token_loss.data_ptr(), lse.data_ptr()]
-        if not grad:
-            _check(L.psgd_xent_loss(*args, st, ws.data_ptr(), nbytes.value, s))
-            return CrossEntropy(loss, token_loss, lse)
-        if d_hidden is None:
-            d_hidden = torch.empty((T, D), dtype=torch.bfloat16, device=dev)
-        if d_weight is None:
-            d_weight = torch.empty((V, D), dtype=torch.bfloat16, device=dev)
-        _check(L.psgd_xent_grad(*args, d_hidden.data_ptr(), _ld(d_hidden), d_weight.data_ptr(), _ld(d_weight), st, ws.data_ptr(), nbytes.value, s))
-        return CrossEntropyGrad(loss, token_loss, lse, d_hidden, d_weight)
+        nbytes = _workspace_bytes("psgd_xent_workspace", T, V, D, int(grad), dev.index)
+        hidden, ldh = _operand(hidden, T, D, ldh)
+        weight, ldw = _operand(weight, V, D, ldw)
+        ws = _empty(nbytes, dtype=torch.uint8, device=dev)
+        out = _empty(2 * T + 1, dtype=torch.float32, device=dev)
+        at = out.data_ptr()                         # token_loss, lse, loss side by side
+        args = (hidden.data_ptr(), ldh, weight.data_ptr(), ldw, at_labels, at_weight, ignore_index, T, V, D, at + 8 * T, at, at + 4 * T)
+        if grad:
+            if d_hidden is None:
+                d_hidden = _empty((T, D), dtype=_BF16, device=dev)
+            if d_weight is None:
+                d_weight = _empty((V, D), dtype=_BF16, device=dev)
+            _check(lib().psgd_xent_grad(*args, d_hidden.data_ptr(), lddh, d_weight.data_ptr(), lddw, at_status, ws.data_ptr(), nbytes, s))
+        else:
+            _check(lib().psgd_xent_loss(*args, at_status, ws.data_ptr(), nbytes, s))
+    token_loss, lse, loss = out.split_with_sizes((T, T, 1))
+    loss = loss.view(())
+    return CrossEntropyGrad(loss, token_loss, lse, d_hidden, d_weight) if grad else CrossEntropy(loss, token_loss, lse)
 
 
 def linear_cross_entropy(hidden, weight, labels, token_weight=None, ignore_index=-100, status=None, stream=None):
@@ -158,51 +175,58 @@ def linear_cross_entropy_grad(hidden, weight, labels, token_weight=None, ignore_
 class ActivationCheckpoint:
     """A matrix [T, F] kept in 8 bits: `q` [T, 32 G] int8 and one power-of-two scale byte per row and group of 32 values, `scales` [T, G]."""
 
-    __slots__ = ("q", "scales", "shape")
+    __slots__ = ("shape", "device", "groups", "_buf", "_q", "_s")
 
     def __init__(self, T, F, device):
         G = -(-F // GROUP)
-        self.shape = (T, F)
-        self.q = torch.empty((T, G * GROUP), dtype=torch.int8, device=device)
-        self.scales = torch.empty((T, G), dtype=torch.uint8, device=device)
+        self.shape, self.groups, self.device = (T, F), G, device
+        self._buf = _empty(T * G * (GROUP + 1), dtype=torch.uint8, device=device)     # q, then scales
+        self._q = self._buf.data_ptr()
+        self._s = self._q + T * G * GROUP
 
     @property
-    def device(self):
-        return self.q.device
+    def q(self):
+        T, G = self.shape[0], self.groups
+        return self._buf[:T * G * GROUP].view(torch.int8).view(T, G * GROUP)
+
+    @property
+    def scales(self):
+        T, G = self.shape[0], self.groups
+        return self._buf[T * G * GROUP:].view(T, G)
 
     @property
     def nbytes(self):
-        return self.q.numel() + self.scales.numel()
+        return self._buf.numel()
 
-    def unpack(self, dtype=torch.bfloat16, out=None, stream=None):
+    def unpack(self, dtype=_BF16, out=None, stream=None):
         """The values that the checkpoint stands for (exact in either type), [T, F]."""
-        if out is None and dtype not in _DTYPES:
-            raise PSGDError("dtype must be float32 or bfloat16")
+        T, F = self.shape
+        ld = F
         if out is not None:
-            _matrix(out, "out", tuple(_DTYPES), self.shape, self.device)
+            ld = _matrix(out, "out", tuple(_DTYPES), self.shape, self.device)[2]
+        elif dtype not in _DTYPES:
+            raise PSGDError("dtype must be float32 or bfloat16")
         with _on(self.device, stream) as s:
             if out is None:
-                out = torch.empty(self.shape, dtype=dtype, device=self.device)
-            _check(lib().psgd_act_unpack(self.q.data_ptr(), self.scales.data_ptr(), *self.shape, out.data_ptr(), _ld(out), _DTYPES[out.dtype], s))
+                out = _empty((T, F), dtype=dtype, device=self.device)
+            _check(lib().psgd_act_unpack(self._q, self._s, T, F, out.data_ptr(), ld, _DTYPES[out.dtype], s))
         return out
 
 
 def pack_activation(x, stream=None):
     """x [T, F] (bfloat16 or float32) in 8 bits: an ActivationCheckpoint."""
-    _matrix(x, "x", tuple(_DTYPES))
-    T, F = x.shape
+    T, F, ld = _matrix(x, "x", tuple(_DTYPES))
     with _on(x.device, stream) as s:
         kept = ActivationCheckpoint(T, F, x.device)
-        _check(lib().psgd_act_pack(x.data_ptr(), _ld(x), _DTYPES[x.dtype], T, F, kept.q.data_ptr(), kept.scales.data_ptr(), s))
+        _check(lib().psgd_act_pack(x.data_ptr(), ld, _DTYPES[x.dtype], T, F, kept._q, kept._s, s))
     return kept
 
 
-def _kept(c, name, device=None, shape=None):
+def _kept(c, name, device, shape=None):
     if not isinstance(c, ActivationCheckpoint):
         raise PSGDError(f"{name} must be an ActivationCheckpoint")
-    if (device is not None and c.device != device) or (shape is not None and tuple(c.shape) != tuple(shape)):
+    if c.device != device or (shape is not None and c.shape != shape):
         raise PSGDError(f"{name} does not match the other arguments' shape or device")
-    return c
 
 
 def weight_gradient(dy, kept, dtype=torch.float32, out=None, status=None, stream=None):
@@ -210,54 +234,49 @@ def weight_gradient(dy, kept, dtype=torch.float32, out=None, status=None, stream
 
     float32 sums of exact products, written as `dtype` (float32 or bfloat16) or into `out` (for instance a slot of a gradient stack).
     """
-    _matrix(dy, "dy")
-    T, O = dy.shape
+    T, O, ldy = _matrix(dy, "dy")
     dev = dy.device
     _kept(kept, "kept", dev)
     if kept.shape[0] != T:
         raise PSGDError(f"dy has {T} rows, the checkpoint {kept.shape[0]}")
-    F = kept.shape[1]
+    F = ldo = kept.shape[1]
     if out is not None:
-        _matrix(out, "out", tuple(_DTYPES), (O, F), dev)
+        ldo = _matrix(out, "out", tuple(_DTYPES), (O, F), dev)[2]
     elif dtype not in _DTYPES:
         raise PSGDError("dtype must be float32 or bfloat16")
-    st = _status(status, dev)
-    L = lib()
-    nbytes = C.c_size_t()
+    at_status = _status(status, dev)
     with _on(dev, stream) as s:
-        _check(L.psgd_act_wgrad_workspace(T, O, F, C.byref(nbytes)))
-        dy = _operand(dy)
-        ws = torch.empty((nbytes.value,), dtype=torch.uint8, device=dev)
+        nbytes = _workspace_bytes("psgd_act_wgrad_workspace", T, O, F, dev.index)
+        dy, ldy = _operand(dy, T, O, ldy)
+        ws = _empty(nbytes, dtype=torch.uint8, device=dev)
         if out is None:
-            out = torch.empty((O, F), dtype=dtype, device=dev)
-        _check(L.psgd_act_wgrad(dy.data_ptr(), _ld(dy), kept.q.data_ptr(), kept.scales.data_ptr(), T, O, F, out.data_ptr(), _ld(out), _DTYPES[out.dtype], st,
-                                ws.data_ptr(), nbytes.value, s))
+            out = _empty((O, F), dtype=dtype, device=dev)
+        _check(lib().psgd_act_wgrad(dy.data_ptr(), ldy, kept._q, kept._s, T, O, F, out.data_ptr(), ldo, _DTYPES[out.dtype], at_status, ws.data_ptr(), nbytes, s))
     return out
 
 
 def swiglu_forward(gate, up, stream=None):
     """h = silu(gate) * up, [T, F] bfloat16.  Returns (h, checkpoint of gate, checkpoint of up), made in one pass."""
-    _matrix(gate, "gate")
-    T, F = gate.shape
+    T, F, ldg = _matrix(gate, "gate")
     dev = gate.device
-    _matrix(up, "up", shape=(T, F), device=dev)
+    ldu = _matrix(up, "up", shape=(T, F), device=dev)[2]
     with _on(dev, stream) as s:
-        h = torch.empty((T, F), dtype=torch.bfloat16, device=dev)
+        h = _empty((T, F), dtype=_BF16, device=dev)
         kg, ku = ActivationCheckpoint(T, F, dev), ActivationCheckpoint(T, F, dev)
-        _check(lib().psgd_swiglu_forward(gate.data_ptr(), _ld(gate), up.data_ptr(), _ld(up), T, F, h.data_ptr(), F, kg.q.data_ptr(), kg.scales.data_ptr(),
-                                         ku.q.data_ptr(), ku.scales.data_ptr(), s))
+        _check(lib().psgd_swiglu_forward(gate.data_ptr(), ldg, up.data_ptr(), ldu, T, F, h.data_ptr(), F, kg._q, kg._s, ku._q, ku._s, s))
     return h, kg, ku
 
 
 def swiglu_backward(dh, gate, up, recompute=False, stream=None):
     """Gradients (d_gate, d_up) of h = silu(gate) * up from dh [T, F] bfloat16 and the two checkpoints; with `recompute` also h again."""
-    _matrix(dh, "dh")
-    T, F = dh.shape
+    T, F, ld = _matrix(dh, "dh")
     dev = dh.device
     _kept(gate, "gate", dev, (T, F))
     _kept(up, "up", dev, (T, F))
     with _on(dev, stream) as s:
-        out = [torch.empty((T, F), dtype=torch.bfloat16, device=dev) for _ in range(3 if recompute else 2)]
-        _check(lib().psgd_swiglu_backward(dh.data_ptr(), _ld(dh), gate.q.data_ptr(), gate.scales.data_ptr(), up.q.data_ptr(), up.scales.data_ptr(), T, F,
-                                          out[0].data_ptr(), F, out[1].data_ptr(), F, out[2].data_ptr() if recompute else None, F, s))
-    return tuple(out)
+        d_gate = _empty((T, F), dtype=_BF16, device=dev)
+        d_up = torch.empty_like(d_gate)
+        h = torch.empty_like(d_gate) if recompute else None
+        _check(lib().psgd_swiglu_backward(dh.data_ptr(), ld, gate._q, gate._s, up._q, up._s, T, F, d_gate.data_ptr(), F, d_up.data_ptr(), F,
+                                          h.data_ptr() if recompute else None, F, s))
+    return (d_gate, d_up, h) if recompute else (d_gate, d_up)
