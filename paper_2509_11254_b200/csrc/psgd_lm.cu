@@ -220,27 +220,35 @@ psgd_status xent(const void* H, int64_t ldh, const void* W, int64_t ldw, const i
 
 // ---- 8-bit activations ----
 struct ActGrid { dim3 grid, block; };
-// 256 threads: a row's units side by side, as many rows as fit, `rows` of them per thread where there are enough to fill the GPU
-ActGrid act_grid(int64_t T, int G, int rows) {
+// 256 threads: a row's units side by side, as many rows as fit; CTAs for `resident` of them per multiprocessor
+ActGrid act_grid(int64_t T, int G, int resident) {
     const int units = 4 * G, across = ceil_div(units, 256);
     const int bx = (int)align_up(ceil_div(units, across), 4);
     const int by = std::max(1, 256 / bx);
-    const int64_t all = ceil_div(T, by), full = ceil_div((int64_t)device_sms() * 8, across);
-    const int64_t y = std::min<int64_t>({all, 65535, std::max<int64_t>(ceil_div(all, rows), full)});
-    return {dim3(ceil_div(units, bx), (unsigned)y), dim3(bx, by)};
+    const int nx = ceil_div(units, bx);
+    const int64_t y = std::min<int64_t>({ceil_div(T, by), 65535, std::max(1, device_sms() * resident / nx)});
+    return {dim3(nx, (unsigned)y), dim3(bx, by)};
+}
+// a lane per value: eight warps with four groups of a row each, as many rows at a time as keep eight such CTAs per multiprocessor busy
+ActGrid lane_grid(int64_t T, int G) {
+    const int nx = ceil_div(G, 8 * LANE_GROUPS);
+    const int64_t y = std::min<int64_t>({T, 65535, std::max(1, ceil_div((int64_t)device_sms() * 32, nx))});
+    return {dim3(nx, (unsigned)y), dim3(32, 8)};
 }
 bool act_ok(int64_t T, int64_t F) { return T >= 0 && T <= MAX_EXTENT && extent_ok(F); }
 bool vec8(const void* p, int64_t ld, int64_t F, int dtype) { return F % 8 == 0 && aligned16(p) && ld % (dtype == PSGD_DT_BF16 ? 8 : 4) == 0; }
 
 template <typename X>
-void launch_pack(const ActGrid& g, const ActShape& s, const X* x, int64_t ldx, bool vec, int8_t* q, uint8_t* scales, cudaStream_t st) {
-    if (vec) k_act_pack<X, true><<<g.grid, g.block, 0, st>>>(s, x, ldx, q, scales);
-    else k_act_pack<X, false><<<g.grid, g.block, 0, st>>>(s, x, ldx, q, scales);
+void launch_pack(const ActShape& s, const X* x, int64_t ldx, bool vec, int8_t* q, uint8_t* scales, cudaStream_t st) {
+    const ActGrid g = vec ? act_grid(s.T, s.G, PACK_CTAS) : lane_grid(s.T, s.G);
+    if (vec) k_act_pack<X><<<g.grid, g.block, 0, st>>>(s, x, ldx, q, scales);
+    else k_act_pack_any<X><<<g.grid, g.block, 0, st>>>(s, x, ldx, q, scales);
 }
 template <typename X>
-void launch_unpack(const ActGrid& g, const ActShape& s, const int8_t* q, const uint8_t* scales, X* x, int64_t ldx, bool vec, cudaStream_t st) {
-    if (vec) k_act_unpack<X, true><<<g.grid, g.block, 0, st>>>(s, q, scales, x, ldx);
-    else k_act_unpack<X, false><<<g.grid, g.block, 0, st>>>(s, q, scales, x, ldx);
+void launch_unpack(const ActShape& s, const int8_t* q, const uint8_t* scales, X* x, int64_t ldx, bool vec, cudaStream_t st) {
+    const ActGrid g = vec ? act_grid(s.T, s.G, PACK_CTAS) : lane_grid(s.T, s.G);
+    if (vec) k_act_unpack<X><<<g.grid, g.block, 0, st>>>(s, q, scales, x, ldx);
+    else k_act_unpack_any<X><<<g.grid, g.block, 0, st>>>(s, q, scales, x, ldx);
 }
 bool dtype_ok(int dtype) { return dtype == PSGD_DT_F32 || dtype == PSGD_DT_BF16; }
 bool ckpt_ok(const void* q) { return ((uintptr_t)q & 15) == 0; }
@@ -293,10 +301,9 @@ psgd_status psgd_act_pack(const void* x, int64_t ldx, int dtype, int64_t T, int6
     if (!x || !q || !scales) return PSGD_E_NULL;
     if (ldx < F || !ckpt_ok(q)) return PSGD_E_INVALID;
     const ActShape s{T, (int)F, ceil_div(F, ACT_GROUP)};
-    const ActGrid g = act_grid(T, s.G, ACT_ROWS_PACK);
     const bool vec = vec8(x, ldx, F, dtype);
-    if (dtype == PSGD_DT_BF16) launch_pack(g, s, (const __nv_bfloat16*)x, ldx, vec, q, scales, (cudaStream_t)stream);
-    else launch_pack(g, s, (const float*)x, ldx, vec, q, scales, (cudaStream_t)stream);
+    if (dtype == PSGD_DT_BF16) launch_pack(s, (const __nv_bfloat16*)x, ldx, vec, q, scales, (cudaStream_t)stream);
+    else launch_pack(s, (const float*)x, ldx, vec, q, scales, (cudaStream_t)stream);
     return last_error();
 }
 
@@ -306,10 +313,9 @@ psgd_status psgd_act_unpack(const int8_t* q, const uint8_t* scales, int64_t T, i
     if (!x || !q || !scales) return PSGD_E_NULL;
     if (ldx < F || !ckpt_ok(q)) return PSGD_E_INVALID;
     const ActShape s{T, (int)F, ceil_div(F, ACT_GROUP)};
-    const ActGrid g = act_grid(T, s.G, ACT_ROWS_PACK);
     const bool vec = vec8(x, ldx, F, dtype);
-    if (dtype == PSGD_DT_BF16) launch_unpack(g, s, q, scales, (__nv_bfloat16*)x, ldx, vec, (cudaStream_t)stream);
-    else launch_unpack(g, s, q, scales, (float*)x, ldx, vec, (cudaStream_t)stream);
+    if (dtype == PSGD_DT_BF16) launch_unpack(s, q, scales, (__nv_bfloat16*)x, ldx, vec, (cudaStream_t)stream);
+    else launch_unpack(s, q, scales, (float*)x, ldx, vec, (cudaStream_t)stream);
     return last_error();
 }
 
@@ -334,8 +340,7 @@ psgd_status psgd_act_wgrad(const void* dY, int64_t lddy, const int8_t* q, const 
     if (ws_bytes < g.total) return PSGD_E_WORKSPACE;
     char* w = (char*)ws;
     const ActShape s{T, (int)F, ceil_div(F, ACT_GROUP)};
-    const ActGrid ag = act_grid(T, s.G, ACT_ROWS_PACK);
-    launch_unpack(ag, ActShape{T, (int)g.ldx, s.G}, q, scales, (__nv_bfloat16*)(w + g.x), g.ldx, true, st);     // the padding too: its values are zeros
+    launch_unpack(ActShape{T, (int)g.ldx, s.G}, q, scales, (__nv_bfloat16*)(w + g.x), g.ldx, true, st);     // the padding too: its values are zeros
     TileArgs a{};
     a.status = status ? status : (int*)w;
     a.out = dW; a.ldo = lddw; a.out_f32 = dtype == PSGD_DT_F32;
@@ -354,12 +359,11 @@ psgd_status psgd_swiglu_forward(const void* gate, int64_t ldg, const void* up, i
     if (!gate || !up || !h || !q_gate || !s_gate || !q_up || !s_up) return PSGD_E_NULL;
     if (ldg < F || ldu < F || ldh < F || !ckpt_ok(q_gate) || !ckpt_ok(q_up)) return PSGD_E_INVALID;
     const ActShape s{T, (int)F, ceil_div(F, ACT_GROUP)};
-    const ActGrid g = act_grid(T, s.G, ACT_ROWS);
-    const auto run = [&](auto kernel) {
-        kernel<<<g.grid, g.block, 0, (cudaStream_t)stream>>>(s, (const __nv_bfloat16*)gate, ldg, (const __nv_bfloat16*)up, ldu, (__nv_bfloat16*)h, ldh, q_gate, s_gate, q_up, s_up);
-    };
-    if (vec8(gate, ldg, F, 1) && vec8(up, ldu, F, 1) && vec8(h, ldh, F, 1)) run(k_swiglu_forward<true>);
-    else run(k_swiglu_forward<false>);
+    const GatedForward a{(const __nv_bfloat16*)gate, (const __nv_bfloat16*)up, (__nv_bfloat16*)h, ldg, ldu, ldh, q_gate, q_up, s_gate, s_up};
+    const bool vec = vec8(gate, ldg, F, PSGD_DT_BF16) && vec8(up, ldu, F, PSGD_DT_BF16) && vec8(h, ldh, F, PSGD_DT_BF16);
+    const ActGrid g = vec ? act_grid(T, s.G, FORWARD_CTAS) : lane_grid(T, s.G);
+    if (vec) k_swiglu_forward<<<g.grid, g.block, 0, (cudaStream_t)stream>>>(s, a);
+    else k_swiglu_forward_any<<<g.grid, g.block, 0, (cudaStream_t)stream>>>(s, a);
     return last_error();
 }
 
@@ -370,14 +374,12 @@ psgd_status psgd_swiglu_backward(const void* dh, int64_t lddh, const int8_t* q_g
     if (!dh || !q_gate || !s_gate || !q_up || !s_up || !d_gate || !d_up) return PSGD_E_NULL;
     if (lddh < F || ldg < F || ldu < F || (h && ldh < F) || !ckpt_ok(q_gate) || !ckpt_ok(q_up)) return PSGD_E_INVALID;
     const ActShape s{T, (int)F, ceil_div(F, ACT_GROUP)};
-    const ActGrid g = act_grid(T, s.G, ACT_ROWS);
-    const auto run = [&](auto kernel) {
-        kernel<<<g.grid, g.block, 0, (cudaStream_t)stream>>>(s, (const __nv_bfloat16*)dh, lddh, q_gate, s_gate, q_up, s_up, (__nv_bfloat16*)d_gate, ldg, (__nv_bfloat16*)d_up,
-                                                             ldu, (__nv_bfloat16*)h, ldh);
-    };
-    const bool vec = vec8(dh, lddh, F, 1) && vec8(d_gate, ldg, F, 1) && vec8(d_up, ldu, F, 1) && (!h || vec8(h, ldh, F, 1));
-    if (h) vec ? run(k_swiglu_backward<true, true>) : run(k_swiglu_backward<true, false>);
-    else vec ? run(k_swiglu_backward<false, true>) : run(k_swiglu_backward<false, false>);
+    const GatedBackward a{(const __nv_bfloat16*)dh, q_gate, q_up, s_gate, s_up, (__nv_bfloat16*)d_gate, (__nv_bfloat16*)d_up, (__nv_bfloat16*)h, lddh, ldg, ldu, ldh};
+    const bool vec = vec8(dh, lddh, F, PSGD_DT_BF16) && vec8(d_gate, ldg, F, PSGD_DT_BF16) && vec8(d_up, ldu, F, PSGD_DT_BF16) && (!h || vec8(h, ldh, F, PSGD_DT_BF16));
+    const ActGrid g = vec ? act_grid(T, s.G, BACKWARD_CTAS) : lane_grid(T, s.G);
+    const auto run = [&](auto kernel) { kernel<<<g.grid, g.block, 0, (cudaStream_t)stream>>>(s, a); };
+    if (h) vec ? run(k_swiglu_backward<true>) : run(k_swiglu_backward_any<true>);
+    else vec ? run(k_swiglu_backward<false>) : run(k_swiglu_backward_any<false>);
     return last_error();
 }
 
