@@ -12,7 +12,7 @@
 // 8 values per thread there, stores of 2 bytes 16 bytes apart made the backward pass of 4096 x 2051 72 us, against 18 of 4096 x 2048).
 //
 // Measured (8.06, 10.06, 3.03 and 3.03 bytes per value; of the 6533 GB/s of a copy), 16384 x 5504: gated unit forward 128 us (87 %), backward with h
-// 153 us (91 %), pack 52 us (80 %), unpack 50 us (84 %).
+// 157 us (88 %), pack 52 us (80 %), unpack 50 us (84 %).
 #pragma once
 #include <cuda_bf16.h>
 #include <stdint.h>
@@ -145,7 +145,7 @@ __device__ __forceinline__ void gated_backward(float d, float g, float u, float&
 // once.  A thread keeps D of its rows on their way: it asks for row i + D before it works on row i, so that bytes are
 // under way all the time and not only between two bursts of work.  Rows in flight times CTAs per multiprocessor is held
 // by registers; the pairs below were the best of six each (forward 156 us with bursts of two rows, 128 us so).
-constexpr int PACK_DEPTH = 4, PACK_CTAS = 4, FORWARD_DEPTH = 3, FORWARD_CTAS = 3, BACKWARD_DEPTH = 2, BACKWARD_CTAS = 4;
+constexpr int PACK_DEPTH = 4, PACK_CTAS = 4, FORWARD_DEPTH = 3, FORWARD_CTAS = 3, BACKWARD_DEPTH = 2, BACKWARD_CTAS = 3;
 struct ActCursor { int col; long long row, step; };
 __device__ __forceinline__ ActCursor act_cursor() {
     ActCursor c;
