@@ -18,35 +18,75 @@ constexpr int64_t MAX_EXTENT = (int64_t)1 << 30;
 constexpr int KACC_F32 = 32;       // stages (2048 of k) per accumulator where the result is float32: the tensor cores' additions truncate, and the
                                    // error grows with the number of additions into one running sum (16384 of k: 1.3e-6 with 64, 0.6e-6 with 32)
 
-struct TilePlan { int mt, nt, kb, bn, full, S, kbps, tail, units, gm; };
+constexpr int ROUND_COST = 6;      // of a unit beside its stages (epilogue not overlapped, refilling the ring), in stages
+
+struct TilePlan { int64_t M, N, K; int mt, nt, kb, bn, full, S, kbps, tail, units, gm; };
+
+double stage_cost(int bn) { return bn == 256 ? 1.0 : bn == 192 ? 0.80 : 0.60; }      // narrower tiles fetch more bytes per product
+
+void finish_plan(TilePlan& p, int pairs) {
+    p.units = p.full + p.tail * p.S;
+    // raster: all row tiles next to each other while the row operand fits beside the rest in L2, else as many as make the
+    // pairs at work cover all columns
+    p.gm = (p.M * p.K * 2 <= (40 << 20)) ? p.mt : std::min(p.mt, std::max(8, std::min(32, pairs / p.nt)));
+}
 
 // Tiles of an M x N product over `pairs` CTA pairs.  The last, partly filled wave of R tiles may be cut into S pieces of k each, and
 // the tiles may be 192 or 128 columns wide instead of 256; both are chosen for the least time in units of one 256-column stage:
-// a round of units costs its stages and about 6 of its own, joining the pieces a launch and their way through memory.
+// a round of units costs its stages and ROUND_COST, joining the pieces a launch and their way through memory.
 TilePlan plan_tiles(int64_t M, int64_t N, int64_t K, int pairs, bool store) {
     TilePlan p{};
+    p.M = M; p.N = N; p.K = K;
     p.mt = ceil_div(M, TG_BM);
     p.kb = ceil_div(K, TG_BK);
     double best = 1e300;
     for (int bn = TG_BN; bn >= (store ? 128 : TG_BN); bn -= 64) {
         const int nt = ceil_div(N, bn);
-        const double stage = bn == 256 ? 1.0 : bn == 192 ? 0.80 : 0.60;        // narrower tiles fetch more bytes per product
+        const double stage = stage_cost(bn);
         const int64_t tiles = (int64_t)p.mt * nt;
         const int R = (int)(tiles % pairs);
         const double whole = (double)(tiles / pairs) * (p.kb + 1) * stage;
         for (int S = 1; S <= (store && R > 0 ? std::min(p.kb, 2 * pairs) : 1); ++S) {
             const int kbps = ceil_div(p.kb, S);
             if (ceil_div(p.kb, kbps) != S) continue;                           // no empty pieces
-            double cost = whole + (R > 0 ? (double)ceil_div((int64_t)R * S, pairs) * (kbps + 6) * stage : 0.0);
+            double cost = whole + (R > 0 ? (double)ceil_div((int64_t)R * S, pairs) * (kbps + ROUND_COST) * stage : 0.0);
             if (S > 1) cost += 12 + 0.06 * R * S;
             if (cost < best) { best = cost; p.bn = bn; p.nt = nt; p.S = S; p.kbps = kbps; p.tail = R; p.full = (int)(tiles - R); }
         }
     }
-    p.units = p.full + p.tail * p.S;
-    // raster: all row tiles next to each other while the row operand fits beside the rest in L2, else as many as make the
-    // pairs at work cover all columns
-    p.gm = (M * K * 2 <= (40 << 20)) ? p.mt : std::min(p.mt, std::max(8, std::min(32, pairs / p.nt)));
+    finish_plan(p, pairs);
     return p;
+}
+
+// Two products that share one launch (launch_products): no waves to fill, only units that must not be longer than a pair's share of
+// the whole work, so a product is cut along k, all its tiles alike, where its tiles would be.
+void plan_two(TilePlan (&p)[2], const int64_t (&M)[2], int64_t N, const int64_t (&K)[2], int pairs) {
+    double total = 0.0;
+    for (int i = 0; i < 2; ++i) {
+        TilePlan& q = p[i];
+        q = TilePlan{};
+        q.M = M[i]; q.N = N; q.K = K[i];
+        q.mt = ceil_div(q.M, TG_BM);
+        q.kb = ceil_div(q.K, TG_BK);
+        double best = 1e300;
+        for (int bn = TG_BN; bn >= 128; bn -= 64)
+            if (ceil_div(N, bn) * stage_cost(bn) < best) { best = ceil_div(N, bn) * stage_cost(bn); q.bn = bn; q.nt = ceil_div(N, bn); }
+        total += (double)q.mt * q.nt * (q.kb + ROUND_COST) * stage_cost(q.bn);
+    }
+    for (TilePlan& q : p) {
+        const int tiles = q.mt * q.nt;
+        const double most = 0.9 * total / pairs + 10;                          // cutting has a price: the pieces are added by another kernel
+        for (int S = 1;; ++S) {
+            const int kbps = ceil_div(q.kb, S);
+            if (ceil_div(q.kb, kbps) != S) continue;
+            q.S = S;
+            q.kbps = kbps;
+            if ((kbps + ROUND_COST) * stage_cost(q.bn) <= most || kbps == 1) break;
+        }
+        q.full = q.S > 1 ? 0 : tiles;
+        q.tail = q.S > 1 ? tiles : 0;
+        finish_plan(q, pairs);
+    }
 }
 size_t part_bytes(const TilePlan& p) { return p.S > 1 ? (size_t)(p.units - p.full) * TG_PART * 4 : 0; }
 
@@ -63,21 +103,66 @@ bool encode_operand(CUtensorMap* map, const void* p, int64_t rows, int64_t cols,
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// C = A B^T summed over k.  A: [M][K] (AMN false) or [K][M] (AMN true), B likewise with N.
-template <int EPI, bool AMN, bool BMN>
-psgd_status launch_tile(const void* A, int64_t lda, const void* B, int64_t ldb, int64_t M, int64_t N, int64_t K, const TilePlan& p, TileArgs a, int pairs, cudaStream_t st) {
+void set_problem(TileProblem& t, const TilePlan& p) {
+    t.M = (int)p.M; t.N = (int)p.N;
+    t.mt = p.mt; t.nt = p.nt; t.kb = p.kb; t.bn = p.bn; t.full = p.full; t.S = p.S; t.kbps = p.kbps; t.tail = p.tail; t.units = p.units; t.gm = p.gm;
+    t.by_group = fast_div((unsigned)p.gm * p.nt); t.by_gm = fast_div(p.gm); t.by_rest = fast_div(std::max(1, p.mt % p.gm)); t.by_tail = fast_div(std::max(1, p.tail));
+}
+
+// Launch that may start before the kernel in front of it on the stream has finished (the kernels wait for that themselves).
+template <typename... Args>
+bool launch_after(void (*kernel)(Args...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, bool early, const Args&... args) {
+    cudaLaunchConfig_t c{};
+    c.gridDim = grid; c.blockDim = block; c.dynamicSmemBytes = smem; c.stream = st;
+    cudaLaunchAttribute at{};
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    c.attrs = &at;
+    c.numAttrs = early ? 1 : 0;
+    return cudaLaunchKernelEx(&c, kernel, args...) == cudaSuccess;
+}
+
+struct Operand { const void* p; int64_t ld; bool mn; };      // mn: stored [K][rows], else [rows][K]
+bool encode(CUtensorMap* map, const Operand& o, int64_t rows, int64_t K, int box) {
+    return o.mn ? encode_operand(map, o.p, K, rows, o.ld, TG_BK) : encode_operand(map, o.p, rows, K, o.ld, box);
+}
+
+// One product of K-major operands with a softmax epilogue.
+template <int EPI>
+psgd_status launch_softmax(const Operand& A, const Operand& B, const TilePlan& p, TileArgs& a, int pairs, bool early, cudaStream_t st) {
     CUtensorMap ma, mb;
-    if (!(AMN ? encode_operand(&ma, A, K, M, lda, TG_BK) : encode_operand(&ma, A, M, K, lda, 128)) ||
-        !(BMN ? encode_operand(&mb, B, K, N, ldb, TG_BK) : encode_operand(&mb, B, N, K, ldb, p.bn / 2)))
-        return PSGD_E_CUDA;
-    a.M = (int)M; a.N = (int)N; a.K = (int)K;
-    a.mt = p.mt; a.nt = p.nt; a.kb = p.kb; a.bn = p.bn; a.full = p.full; a.S = p.S; a.kbps = p.kbps; a.tail = p.tail; a.units = p.units; a.gm = p.gm;
-    a.by_group = fast_div((unsigned)p.gm * p.nt); a.by_gm = fast_div(p.gm); a.by_rest = fast_div(std::max(1, p.mt % p.gm)); a.by_tail = fast_div(std::max(1, p.tail));
-    const size_t smem = tile_smem_bytes();
-    allow_smem(k_tile<EPI, AMN, BMN>, smem);
-    k_tile<EPI, AMN, BMN><<<2 * std::min(p.units, pairs), TG_THREADS, smem, st>>>(ma, mb, a);
-    if (p.S > 1) k_join<<<dim3(p.tail, p.bn / 32, 2), 128, 0, st>>>(a);
-    return cudaGetLastError() == cudaSuccess ? PSGD_OK : PSGD_E_CUDA;
+    if (!encode(&ma, A, p.M, p.K, 128) || !encode(&mb, B, p.N, p.K, p.bn / 2)) return PSGD_E_CUDA;
+    set_problem(a.p[0], p);
+    const int n = std::min(p.units, pairs);
+    a.first_q = p.units / n; a.first_r = p.units % n;
+    allow_smem(k_tile<EPI>, tile_smem_bytes());
+    return launch_after(k_tile<EPI>, dim3(2 * n), dim3(TG_THREADS), tile_smem_bytes(), st, early, ma, mb, ma, mb, a) ? PSGD_OK : PSGD_E_CUDA;
+}
+
+// One or two products (B MN-major) in one launch, then the pieces of their split tiles.  Two: the units of the first go round the pairs; the
+// pairs that have one unit fewer of it do as many units of the second meanwhile as fit in that time.
+psgd_status launch_products(int count, const Operand (&A)[2], const Operand (&B)[2], const TilePlan (&p)[2], TileArgs& a, int pairs, bool early, cudaStream_t st) {
+    CUtensorMap m[4];
+    for (int i = 0; i < count; ++i) {
+        if (!encode(&m[2 * i], A[i], p[i].M, p[i].K, 128) || !encode(&m[2 * i + 1], B[i], p[i].N, p[i].K, p[i].bn / 2)) return PSGD_E_CUDA;
+        set_problem(a.p[i], p[i]);
+        a.p[i].a_mn = A[i].mn;
+    }
+    if (count == 1) { m[2] = m[0]; m[3] = m[1]; }
+    const int second = count == 2 ? p[1].units : 0;
+    const int n = std::min(p[0].units + second, pairs);
+    a.first_q = p[0].units / n; a.first_r = p[0].units % n;
+    a.extra = 0;
+    if (second && a.first_r) {
+        const int c0 = (p[0].S > 1 ? p[0].kbps : p[0].kb) + ROUND_COST, c1 = (p[1].full ? p[1].kb : p[1].kbps) + ROUND_COST;
+        a.extra = std::min((c0 + c1 / 2) / c1, second / (n - a.first_r));
+    }
+    allow_smem(k_tile<EPI_STORE>, tile_smem_bytes());
+    if (!launch_after(k_tile<EPI_STORE>, dim3(2 * n), dim3(TG_THREADS), tile_smem_bytes(), st, early, m[0], m[1], m[2], m[3], a)) return PSGD_E_CUDA;
+    const int joins = (p[0].S > 1 ? p[0].tail : 0) + (count == 2 && p[1].S > 1 ? p[1].tail : 0);
+    const int wide = std::max(p[0].bn, count == 2 ? p[1].bn : 0);
+    if (joins && !launch_after(k_join, dim3(joins, wide / 32, 2), dim3(128), 0, st, true, a)) return PSGD_E_CUDA;
+    return PSGD_OK;
 }
 
 bool operand_ok(const void* p, int64_t rows, int64_t cols, int64_t ld) { return aligned16(p) && ld >= cols && (rows == 1 || ld % 8 == 0); }
@@ -89,11 +174,15 @@ constexpr int64_t XENT_PIECE_LOGITS = (int64_t)1 << 28;   // logits whose 16-bit
 struct XentPlan {
     int pairs, nseg;
     int64_t ldq, piece, pieces;
-    TilePlan logits, dh, dw;          // of a whole piece
+    TilePlan logits, two[2];          // of a whole piece; two: dH and dW
     size_t inv, done, stats, label_logit, q, part, acc, total;
 };
 // Tokens are taken in pieces, all columns at a time, so that the stored exponents stay within a fixed size however many
 // tokens there are; a piece has at least 1024 tokens, below which the products with the vocabulary matrix would be bound by reading it.
+void plan_gradients(TilePlan (&p)[2], int64_t rows, int64_t V, int64_t D, int pairs) {
+    const int64_t M[2] = {rows, V}, K[2] = {V, rows};
+    plan_two(p, M, D, K, pairs);
+}
 XentPlan plan_xent(int64_t T, int64_t V, int64_t D, bool grad) {
     XentPlan x{};
     x.pairs = std::max(1, device_sms() / 2);
@@ -113,17 +202,17 @@ XentPlan plan_xent(int64_t T, int64_t V, int64_t D, bool grad) {
     x.inv = take(4);
     x.done = take(4);
     if (grad) {
-        x.dh = plan_tiles(x.piece, D, V, x.pairs, true);
-        x.dw = plan_tiles(V, D, x.piece, x.pairs, true);
+        plan_gradients(x.two, x.piece, V, D, x.pairs);
     }
     x.stats = take((size_t)x.piece * x.nseg * 8);
     x.label_logit = take((size_t)x.piece * 4);
     if (grad) {
         x.q = take((size_t)x.piece * x.ldq * 2);
-        size_t part = std::max(part_bytes(x.dh), part_bytes(x.dw));
+        size_t part = part_bytes(x.two[0]) + part_bytes(x.two[1]);
         if (x.pieces > 1) {                           // the last piece may be shorter
-            const int64_t last = T - (x.pieces - 1) * x.piece;
-            part = std::max(part, std::max(part_bytes(plan_tiles(last, D, V, x.pairs, true)), part_bytes(plan_tiles(V, D, last, x.pairs, true))));
+            TilePlan last[2];
+            plan_gradients(last, T - (x.pieces - 1) * x.piece, V, D, x.pairs);
+            part = std::max(part, part_bytes(last[0]) + part_bytes(last[1]));
             x.acc = take((size_t)V * D * 4);
         }
         x.part = take(part);
@@ -149,7 +238,6 @@ psgd_status xent(const void* H, int64_t ldh, const void* W, int64_t ldw, const i
     int* stat = status ? status : (int*)w;
     float* inv = (float*)(w + x.inv);
     int* done = (int*)(w + x.done);
-    if (grad) k_xent_norm<<<1, 1024, 0, st>>>((const long long*)labels, weight, T, ignore, (int)V, inv, done);
 
     RowsArgs r{};
     r.V = (int)V; r.nseg = x.nseg;
@@ -178,10 +266,14 @@ psgd_status xent(const void* H, int64_t ldh, const void* W, int64_t ldw, const i
         a.stats = (float2*)(w + x.stats);
         a.label_logit = (float*)(w + x.label_logit);
         a.q = r.q; a.ldq = x.ldq; a.nseg = x.nseg;
-        if (!grad) { a.clear = done; a.clear_n = 1; }
-        const TilePlan pl = rows == x.piece ? x.logits : plan_tiles(rows, V, D, x.pairs, false);
-        psgd_status s = grad ? launch_tile<EPI_SOFTMAX, false, false>(h, ldh, W, ldw, rows, V, D, pl, a, x.pairs, st)
-                             : launch_tile<EPI_LOSS, false, false>(h, ldh, W, ldw, rows, V, D, pl, a, x.pairs, st);
+        if (first) {
+            a.done = done;
+            a.norm = inv; a.norm_labels = (const long long*)labels; a.norm_weight = weight; a.norm_rows = T; a.ignore = ignore;
+        }
+        const bool whole = rows == x.piece;
+        const TilePlan pl = whole ? x.logits : plan_tiles(rows, V, D, x.pairs, false);
+        const Operand oh{h, ldh, false}, ow{W, ldw, false};
+        psgd_status s = grad ? launch_softmax<EPI_SOFTMAX>(oh, ow, pl, a, x.pairs, !first, st) : launch_softmax<EPI_LOSS>(oh, ow, pl, a, x.pairs, false, st);
         if (s != PSGD_OK) return s;
         r.rows = (int)rows;
         r.labels = (const long long*)labels + t0;
@@ -189,30 +281,33 @@ psgd_status xent(const void* H, int64_t ldh, const void* W, int64_t ldw, const i
         r.loss = token_loss + t0;
         r.lse = lse + t0;
         if (!grad) {
-            k_xent_loss<<<ceil_div(rows, XE_THREADS / 32), XE_THREADS, 0, st>>>(r);
+            if (!launch_after(k_xent_loss, dim3(ceil_div(rows, XE_THREADS / 32)), dim3(XE_THREADS), 0, st, true, r)) return PSGD_E_CUDA;
             continue;
         }
-        k_xent_rows<<<dim3((unsigned)rows, parts_of(rows)), XE_THREADS, 0, st>>>(r);
+        if (!launch_after(k_xent_rows, dim3((unsigned)rows, parts_of(rows)), dim3(XE_THREADS), 0, st, true, r)) return PSGD_E_CUDA;
         // dH = dL W: contraction over the vocabulary;  dW = dL^T H: over the tokens
+        TilePlan p[2] = {x.two[0], x.two[1]};
+        if (!whole) plan_gradients(p, rows, V, D, x.pairs);
+        const Operand A[2] = {{r.q, x.ldq, false}, {r.q, x.ldq, true}}, B[2] = {{W, ldw, true}, {h, ldh, true}};
         TileArgs g{};
         g.status = stat;
-        g.scale = inv;
-        g.part = (float*)(w + x.part);
-        g.out = (char*)dH + (size_t)t0 * lddh * 2;
-        g.ldo = lddh;
-        g.vec = ((uintptr_t)g.out & 7) == 0 && lddh % 4 == 0;
-        s = launch_tile<EPI_STORE, false, true>(r.q, x.ldq, W, ldw, rows, D, V, rows == x.piece ? x.dh : plan_tiles(rows, D, V, x.pairs, true), g, x.pairs, st);
-        if (s != PSGD_OK) return s;
+        TileProblem &ph = g.p[0], &pw = g.p[1];
+        ph.scale = pw.scale = inv;
+        ph.part = (float*)(w + x.part);
+        pw.part = ph.part + part_bytes(p[0]) / 4;
+        ph.out = (char*)dH + (size_t)t0 * lddh * 2;
+        ph.ldo = lddh;
+        ph.vec = ((uintptr_t)ph.out & 7) == 0 && lddh % 4 == 0;
         float* acc = (float*)(w + x.acc);
-        g.addend = first ? nullptr : acc;
+        pw.addend = first ? nullptr : acc;
         if (last) {
-            g.out = dW; g.ldo = lddw;
-            g.vec = ((uintptr_t)dW & 7) == 0 && lddw % 4 == 0 && (first || D % 4 == 0);
+            pw.out = dW; pw.ldo = lddw;
+            pw.vec = ((uintptr_t)dW & 7) == 0 && lddw % 4 == 0 && (first || D % 4 == 0);
         } else {
-            g.out = acc; g.ldo = D; g.out_f32 = 1; g.scale = nullptr;
-            g.vec = D % 4 == 0;
+            pw.out = acc; pw.ldo = D; pw.out_f32 = 1; pw.scale = nullptr;
+            pw.vec = D % 4 == 0;
         }
-        s = launch_tile<EPI_STORE, true, true>(r.q, x.ldq, h, ldh, V, D, rows, rows == x.piece ? x.dw : plan_tiles(V, D, rows, x.pairs, true), g, x.pairs, st);
+        s = launch_products(2, A, B, p, g, x.pairs, true, st);
         if (s != PSGD_OK) return s;
     }
     return cudaGetLastError() == cudaSuccess ? PSGD_OK : PSGD_E_CUDA;
@@ -343,11 +438,14 @@ psgd_status psgd_act_wgrad(const void* dY, int64_t lddy, const int8_t* q, const 
     launch_unpack(ActShape{T, (int)g.ldx, s.G}, q, scales, (__nv_bfloat16*)(w + g.x), g.ldx, true, st);     // the padding too: its values are zeros
     TileArgs a{};
     a.status = status ? status : (int*)w;
-    a.out = dW; a.ldo = lddw; a.out_f32 = dtype == PSGD_DT_F32;
-    a.vec = ((uintptr_t)dW & (a.out_f32 ? 15 : 7)) == 0 && lddw % 4 == 0;
-    a.kacc = a.out_f32 ? KACC_F32 : 0;
-    a.part = (float*)(w + g.part);
-    return launch_tile<EPI_STORE, true, true>(dY, lddy, w + g.x, g.ldx, O, F, T, g.p, a, g.pairs, st);
+    TileProblem& t = a.p[0];
+    t.out = dW; t.ldo = lddw; t.out_f32 = dtype == PSGD_DT_F32;
+    t.vec = ((uintptr_t)dW & (t.out_f32 ? 15 : 7)) == 0 && lddw % 4 == 0;
+    t.kacc = t.out_f32 ? KACC_F32 : 0;
+    t.part = (float*)(w + g.part);
+    const Operand A[2] = {{dY, lddy, true}, {}}, B[2] = {{w + g.x, g.ldx, true}, {}};
+    const TilePlan p[2] = {g.p, {}};
+    return launch_products(1, A, B, p, a, g.pairs, true, st);
 } catch (...) {
     return PSGD_E_CUDA;
 }

@@ -50,8 +50,9 @@ inline FastDiv fast_div(unsigned d) {
 }
 __device__ __forceinline__ int operator/(int n, FastDiv d) { return (int)(((unsigned long long)(unsigned)n * d.mul) >> d.shift); }
 
-struct TileArgs {
-    int M, N, K;
+// One product and how it is cut.
+struct TileProblem {
+    int M, N;
     int mt, nt, kb;            // tiles along M and N, stages along K
     int bn;                    // columns per tile
     int full;                  // tiles done in one piece (the first `full` in raster order)
@@ -61,7 +62,7 @@ struct TileArgs {
     int gm;                    // raster: groups of gm row tiles, column by column
     FastDiv by_group, by_gm, by_rest, by_tail;   // gm * nt, gm, rows of the last group, tail
     int kacc;                  // stages summed in one accumulator (0: all of them)
-    int* status;               // device status word
+    int a_mn;                  // A is MN-major
     // EPI_STORE: out = scale * (sum + addend)
     void* out;
     long long ldo;             // elements
@@ -69,6 +70,13 @@ struct TileArgs {
     const float* addend;       // [M][N] float32 or nullptr
     const float* scale;        // DEVICE scalar or nullptr
     float* part;               // partial tiles [S][tail][2][256 columns][128 rows]
+};
+struct TileArgs {
+    TileProblem p[2];          // EPI_STORE: one or two products in one launch
+    // Who does what: the units of p[0] go round the pairs, `first_q` each and one more for the first `first_r` pairs; meanwhile the other
+    // pairs do `extra` units of p[1] each, and the rest of those go round all pairs.
+    int first_q, first_r, extra;
+    int* status;               // device status word
     // EPI_LOSS, EPI_SOFTMAX
     const long long* labels;
     float2* stats;             // [M][nseg]: maximum and sum of exp(l - maximum) of each segment
@@ -76,25 +84,27 @@ struct TileArgs {
     unsigned short* q;         // [M][ldq]: (maximum - l) log2(e) in steps of 2^-10, 65535 for "nothing left"
     long long ldq;
     int nseg;                  // statistics per row
-    int* clear;                // words to zero before the next kernel
-    int clear_n;
+    int* done;                 // counter to clear for the next kernel, or nullptr
+    // EPI_SOFTMAX: 1 / (sum of the weights of the rows that count), formed by a warp that has nothing else to do
+    float* norm;               // or nullptr
+    const long long* norm_labels;
+    const float* norm_weight;
+    long long norm_rows, ignore;
 };
 
 // Shared-memory matrix descriptors, 128-byte swizzle.  K-major: rows of 128 bytes, groups of 8 rows 1024 bytes apart.
 // MN-major: rows hold 64 consecutive m, groups of 8 k are 1024 bytes apart, blocks of 64 m TG_HALF_BYTES / 2 apart.
-template <bool MN>
-__device__ __forceinline__ unsigned long long tile_desc(unsigned addr) {
+__device__ __forceinline__ unsigned long long tile_desc(unsigned addr, bool mn) {
     unsigned long long d = (unsigned long long)((addr >> 4) & 0x3FFF);
-    d |= (unsigned long long)(MN ? (TG_HALF_BYTES / 2) >> 4 : 1) << 16;
+    d |= (unsigned long long)(mn ? (TG_HALF_BYTES / 2) >> 4 : 1) << 16;
     d |= (unsigned long long)(1024 >> 4) << 32;
     d |= (unsigned long long)1 << 46;
     d |= (unsigned long long)2 << 61;
     return d;
 }
 // D float32, A and B bfloat16, M = 256 over the pair
-template <bool AMN, bool BMN>
-__device__ __forceinline__ unsigned tile_idesc(int n) {
-    return (1u << 4) | (1u << 7) | (1u << 10) | ((AMN ? 1u : 0u) << 15) | ((BMN ? 1u : 0u) << 16) | ((unsigned)(n >> 3) << 17) | ((unsigned)(TG_BM >> 4) << 24);
+__device__ __forceinline__ unsigned tile_idesc(int n, bool amn, bool bmn) {
+    return (1u << 4) | (1u << 7) | (1u << 10) | ((amn ? 1u : 0u) << 15) | ((bmn ? 1u : 0u) << 16) | ((unsigned)(n >> 3) << 17) | ((unsigned)(TG_BM >> 4) << 24);
 }
 __device__ __forceinline__ void pair_mma(unsigned d, unsigned long long da, unsigned long long db, unsigned idesc, unsigned acc) {
     asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n"
@@ -162,83 +172,109 @@ __device__ __forceinline__ unsigned pack_bf16(float lo, float hi) {
     return *reinterpret_cast<unsigned*>(&h);
 }
 
-struct TileUnit { int m0, n0, kb0, kb1, piece; };   // piece: index of the partial tile, -1 for a whole tile
-__device__ __forceinline__ void tile_origin(const TileArgs& a, int tile, int& m0, int& n0) {
-    const int g = tile / a.by_group, in = tile - g * (a.gm * a.nt);
-    const bool rest = (g + 1) * a.gm > a.mt;
-    const int rows = rest ? a.mt - g * a.gm : a.gm;
-    const int n = in / (rest ? a.by_rest : a.by_gm);
-    m0 = (g * a.gm + in - n * rows) * TG_BM;
-    n0 = n * a.bn;
+__device__ __forceinline__ void tile_origin(const TileProblem& p, int tile, int& m0, int& n0) {
+    const int g = tile / p.by_group, in = tile - g * (p.gm * p.nt);
+    const bool rest = (g + 1) * p.gm > p.mt;
+    const int rows = rest ? p.mt - g * p.gm : p.gm;
+    const int n = in / (rest ? p.by_rest : p.by_gm);
+    m0 = (g * p.gm + in - n * rows) * TG_BM;
+    n0 = n * p.bn;
 }
-__device__ __forceinline__ TileUnit tile_unit(const TileArgs& a, int u) {
-    TileUnit w;
+struct TileUnit { int which, m0, n0, kb0, kb1, piece; };   // which: product; piece: index of the partial tile, -1 for a whole tile
+// The j-th unit of a pair; false: it has no more.
+__device__ __forceinline__ bool tile_unit(const TileArgs& a, int j, TileUnit& w) {
+    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    int u;
+    const int mine = a.first_q + (pair < a.first_r ? 1 : 0);
+    if (j < mine) {
+        w.which = 0;
+        u = pair + j * pairs;
+    } else {
+        j -= mine;
+        w.which = 1;
+        const int free_pairs = pairs - a.first_r;
+        if (pair >= a.first_r && j < a.extra) u = j * free_pairs + pair - a.first_r;
+        else u = a.extra * free_pairs + (j - (pair >= a.first_r ? a.extra : 0)) * pairs + pair;
+        if (u >= a.p[1].units) return false;
+    }
+    const TileProblem& p = a.p[w.which];
     int tile = u;
     w.kb0 = 0;
-    w.kb1 = a.kb;
+    w.kb1 = p.kb;
     w.piece = -1;
-    if (u >= a.full && a.S > 1) {
+    if (u >= p.full && p.S > 1) {
         // all tiles' first pieces, then all second pieces: pairs at work together read the same range of k and share operands in L2
-        w.piece = u - a.full;
-        const int s = w.piece / a.by_tail;
-        tile = a.full + w.piece - s * a.tail;
-        w.kb0 = s * a.kbps;
-        w.kb1 = min(a.kb, w.kb0 + a.kbps);
+        w.piece = u - p.full;
+        const int s = w.piece / p.by_tail;
+        tile = p.full + w.piece - s * p.tail;
+        w.kb0 = s * p.kbps;
+        w.kb1 = min(p.kb, w.kb0 + p.kbps);
     }
-    tile_origin(a, tile, w.m0, w.n0);
-    return w;
+    tile_origin(p, tile, w.m0, w.n0);
+    return true;
 }
 
 // A 32 x 32 block of C, a row per lane -> rows of 128 bytes through the warp's staging buffer -> out (+ addend, * scale).
 // Row-per-lane stores would touch 32 lines per instruction.
-__device__ __forceinline__ void emit_block(const TileArgs& a, float4* xb, const float (&v)[32], int row0, int col0, const float* addend, long long lda, float scale) {
+__device__ __forceinline__ void emit_block(const TileProblem& a, float4* xb, const float (&v)[32], int row0, int col0, const float* addend, long long lda, float scale) {
     const int lane = threadIdx.x & 31, lrow = lane >> 3, lch = lane & 7;        // row within a group of 4, 16-byte unit
-    const int col = col0 + 4 * lch;
-    const bool wide = a.vec && col + 4 <= a.N;
-    float4 y[8];
-    if (addend && wide) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int row = row0 + 4 * i + lrow;
-            if (row < a.M) y[i] = *reinterpret_cast<const float4*>(addend + (size_t)row * lda + col);
-        }
-    }
 #pragma unroll
     for (int j = 0; j < 8; ++j) xb[lane * 8 + (j ^ (lane & 7))] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-    __syncwarp();
+    if (a.vec && col0 + 32 <= a.N) {
+        const int col = col0 + 4 * lch;
+        float4 y[8];
+        if (addend) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int br = 4 * i + lrow, row = row0 + br;
-        float4 x = xb[br * 8 + (lch ^ (br & 7))];
-        if (row < a.M && col < a.N) {
-            if (wide) {
+            for (int i = 0; i < 8; ++i) {
+                const int row = row0 + 4 * i + lrow;
+                if (row < a.M) y[i] = *reinterpret_cast<const float4*>(addend + (size_t)row * lda + col);
+            }
+        }
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int br = 4 * i + lrow, row = row0 + br;
+            float4 x = xb[br * 8 + (lch ^ (br & 7))];
+            if (row < a.M) {
                 if (addend) { x.x += y[i].x; x.y += y[i].y; x.z += y[i].z; x.w += y[i].w; }
                 x.x *= scale; x.y *= scale; x.z *= scale; x.w *= scale;
                 if (a.out_f32) *reinterpret_cast<float4*>((float*)a.out + (size_t)row * a.ldo + col) = x;
                 else *reinterpret_cast<uint2*>((__nv_bfloat16*)a.out + (size_t)row * a.ldo + col) = make_uint2(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w));
-            } else {
-                const float e[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    if (col + c < a.N) {
-                        const float z = (e[c] + (addend ? addend[(size_t)row * lda + col + c] : 0.f)) * scale;
-                        if (a.out_f32) ((float*)a.out)[(size_t)row * a.ldo + col + c] = z;
-                        else ((__nv_bfloat16*)a.out)[(size_t)row * a.ldo + col + c] = __float2bfloat16_rn(z);
-                    }
+            }
+        }
+    } else {                                          // the last columns, or rows without alignment: a column per lane
+        const float* xf = reinterpret_cast<const float*>(xb);
+        const int col = col0 + lane;
+        __syncwarp();
+#pragma unroll 8
+        for (int br = 0; br < 32; ++br) {
+            const int row = row0 + br;
+            if (row < a.M && col < a.N) {
+                const float x = (xf[br * 32 + (((lane >> 2) ^ (br & 7)) << 2) + (lane & 3)] + (addend ? addend[(size_t)row * lda + col] : 0.f)) * scale;
+                if (a.out_f32) ((float*)a.out)[(size_t)row * a.ldo + col] = x;
+                else ((__nv_bfloat16*)a.out)[(size_t)row * a.ldo + col] = __float2bfloat16_rn(x);
             }
         }
     }
     __syncwarp();
 }
 
+// Dependent launches: a kernel of a call's chain may start while the one before it still runs; `grid_wait` returns when that one has
+// finished and its writes are visible, so everything that touches global memory comes after it.  `grid_trigger` lets the next start.
+__device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;\n" ::: "memory"); }
+__device__ __forceinline__ void grid_trigger() { asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory"); }
+
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float XE_STEPS = 1024.f;            // steps per factor of two in the stored exponents
 constexpr float XE_MAGIC = 8388608.f;         // 2^23: adding it leaves the rounded whole number in the low mantissa bits
 constexpr unsigned XE_NONE = 65535u;
 
-template <int EPI, bool AMN, bool BMN>
+// EPI_LOSS, EPI_SOFTMAX: one product of K-major operands.  EPI_STORE: products whose B is MN-major, A either.
+template <int EPI>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TG_THREADS, 1)
-k_tile(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const TileArgs a) {
+k_tile(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtensorMap tmB0, const __grid_constant__ CUtensorMap tmA1, const __grid_constant__ CUtensorMap tmB1,
+       const __grid_constant__ TileArgs a) {
+    constexpr bool BMN = EPI == EPI_STORE;
     extern __shared__ __align__(16) unsigned char tg_smem_raw[];
     // the offset of everything in shared memory is the same in both CTAs of the pair (descriptors and commits rely on it)
     unsigned char* base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(tg_smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -250,7 +286,7 @@ k_tile(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
     const unsigned smem_base = smem_u32(base);
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int rank = blockIdx.x & 1, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    const int rank = blockIdx.x & 1;
 
     if (tid == 0) {
         for (int s = 0; s < TG_STAGES; ++s) { mbar_init(bar_full + 8 * s, 1); mbar_init(bar_empty + 8 * s, 1); }
@@ -261,8 +297,6 @@ k_tile(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;\n" ::"r"(smem_u32(tmem_slot)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;\n" ::: "memory");
     }
-    if (EPI != EPI_STORE && blockIdx.x == 0)
-        for (int i = tid; i < a.clear_n; i += TG_THREADS) a.clear[i] = 0;
     asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
     __syncthreads();
     cluster_arrive_release();
@@ -270,17 +304,24 @@ k_tile(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
     asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
     const unsigned tmem = *tmem_slot;
     bool dead = false;
+    grid_trigger();
+    grid_wait();
+    if (EPI != EPI_STORE && blockIdx.x == 0 && tid == 0 && a.done) *a.done = 0;
 
     if (warp == 0) {
         // ---- TMA producer of this CTA: its 128 rows of A and its half of B ----
-        // bytes of B per stage: K-major boxes have bn / 2 rows, MN-major ones come in blocks of 64
-        const unsigned b_bytes = BMN ? (a.bn > 128 ? TG_HALF_BYTES : TG_HALF_BYTES / 2) : (unsigned)a.bn / 2 * TG_BK * 2;
         const unsigned full0 = cluster_addr(bar_full, 0);
         int s = 0, filled = 0;
         unsigned par = 1;                                      // a fresh barrier counts as released
-        for (int u = pair; u < a.units && !dead; u += pairs) {
-            const TileUnit w = tile_unit(a, u);
-            const int nh = (min(a.bn, a.N - w.n0) + 31) / 32 * 16;
+        TileUnit w;
+        for (int j = 0; !dead && tile_unit(a, j, w); ++j) {
+            const TileProblem& p = a.p[w.which];
+            const CUtensorMap* const ma = w.which ? &tmA1 : &tmA0;
+            const CUtensorMap* const mb = w.which ? &tmB1 : &tmB0;
+            const bool amn = BMN && p.a_mn, two = p.bn > 128;
+            // bytes of B per stage: K-major boxes have bn / 2 rows, MN-major ones come in blocks of 64
+            const unsigned b_bytes = BMN ? (two ? TG_HALF_BYTES : TG_HALF_BYTES / 2) : (unsigned)p.bn / 2 * TG_BK * 2;
+            const int nh = (min(p.bn, p.N - w.n0) + 31) / 32 * 16;
             const int m = w.m0 + rank * 128, n = w.n0 + rank * nh;
             for (int kb = w.kb0; kb < w.kb1; ++kb) {
                 mbar_wait_all(bar_empty + 8 * s, par, a.status, dead);
@@ -290,17 +331,17 @@ k_tile(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
                     if (rank == 0) mbar_expect_tx(bar_full + 8 * s, 2 * (TG_HALF_BYTES + b_bytes));
                     const unsigned da = smem_base + s * TG_STAGE_BYTES, db = da + TG_HALF_BYTES;
                     const int k = kb * TG_BK;
-                    if (AMN) {
-                        pair_tma_2d(da, &tmA, m, k, bar);
-                        pair_tma_2d(da + TG_HALF_BYTES / 2, &tmA, m + 64, k, bar);
+                    if (amn) {
+                        pair_tma_2d(da, ma, m, k, bar);
+                        pair_tma_2d(da + TG_HALF_BYTES / 2, ma, m + 64, k, bar);
                     } else {
-                        pair_tma_2d(da, &tmA, k, m, bar);
+                        pair_tma_2d(da, ma, k, m, bar);
                     }
                     if (BMN) {
-                        pair_tma_2d(db, &tmB, n, k, bar);
-                        if (a.bn > 128) pair_tma_2d(db + TG_HALF_BYTES / 2, &tmB, n + 64, k, bar);
+                        pair_tma_2d(db, mb, n, k, bar);
+                        if (two) pair_tma_2d(db + TG_HALF_BYTES / 2, mb, n + 64, k, bar);
                     } else {
-                        pair_tma_2d(db, &tmB, k, n, bar);
+                        pair_tma_2d(db, mb, k, n, bar);
                     }
                 }
                 __syncwarp();
@@ -321,11 +362,14 @@ k_tile(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
         if (rank == 0) {
             int s = 0, it = 0;
             unsigned par = 0;
-            for (int u = pair; u < a.units && !dead; u += pairs) {
-                const TileUnit w = tile_unit(a, u);
-                const unsigned idesc = tile_idesc<AMN, BMN>((min(a.bn, a.N - w.n0) + 31) / 32 * 32);
+            TileUnit w;
+            for (int j = 0; !dead && tile_unit(a, j, w); ++j) {
+                const TileProblem& p = a.p[w.which];
+                const bool amn = BMN && p.a_mn;
+                const unsigned idesc = tile_idesc((min(p.bn, p.N - w.n0) + 31) / 32 * 32, amn, BMN);
+                const unsigned step_a = amn ? 2048 >> 4 : 32 >> 4, step_b = BMN ? 2048 >> 4 : 32 >> 4;   // 16 of k: two groups of 8 rows, or 32 bytes of a row
                 for (int k0 = w.kb0; k0 < w.kb1 && !dead; ++it) {
-                    const int k1 = a.kacc > 0 ? min(w.kb1, k0 + a.kacc) : w.kb1;
+                    const int k1 = p.kacc > 0 ? min(w.kb1, k0 + p.kacc) : w.kb1;
                     const unsigned d = tmem + (unsigned)((it & 1) * TG_BN);
                     if (it >= 2) {
                         mbar_wait_all(bar_acce + 8 * (it & 1), (unsigned)(((it >> 1) - 1) & 1), a.status, dead);
@@ -335,12 +379,11 @@ k_tile(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
                         mbar_wait_all(bar_full + 8 * s, par, a.status, dead);
                         if (dead) break;
                         const unsigned sa = smem_base + s * TG_STAGE_BYTES;
-                        const unsigned long long da = tile_desc<AMN>(sa), db = tile_desc<BMN>(sa + TG_HALF_BYTES);
+                        const unsigned long long da = tile_desc(sa, amn), db = tile_desc(sa + TG_HALF_BYTES, BMN);
                         if (elect_one()) {
 #pragma unroll
-                            for (int k = 0; k < TG_BK / 16; ++k)   // 16 of k: 32 bytes along a K-major row, two groups of 8 rows of an MN-major tile
-                                pair_mma(d, da + (unsigned long long)(k * (AMN ? 2048 >> 4 : 32 >> 4)), db + (unsigned long long)(k * (BMN ? 2048 >> 4 : 32 >> 4)), idesc,
-                                         (kb > k0 || k > 0) ? 1u : 0u);
+                            for (int k = 0; k < TG_BK / 16; ++k)
+                                pair_mma(d, da + (unsigned long long)(k * step_a), db + (unsigned long long)(k * step_b), idesc, (kb > k0 || k > 0) ? 1u : 0u);
                             pair_commit(bar_empty + 8 * s);
                             if (kb == k1 - 1) pair_commit(bar_accf + 8 * (it & 1));
                         }
@@ -350,32 +393,54 @@ k_tile(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
                     k0 = k1;
                 }
             }
+        } else if (EPI == EPI_SOFTMAX && blockIdx.x == 1 && a.norm) {
+            double z = 0.0;
+            constexpr int UN = 8;
+            for (long long i0 = lane; i0 < a.norm_rows; i0 += 32 * UN) {
+                long long label[UN];
+                float wt[UN];
+#pragma unroll
+                for (int j = 0; j < UN; ++j) {                 // no branch around the loads: all under way together
+                    const long long i = min(i0 + 32 * j, a.norm_rows - 1);
+                    label[j] = __ldg(a.norm_labels + i);
+                    wt[j] = a.norm_weight ? __ldg(a.norm_weight + i) : 1.f;
+                }
+#pragma unroll
+                for (int j = 0; j < UN; ++j) {
+                    const bool counts = label[j] >= 0 && label[j] < a.p[0].N && label[j] != a.ignore && i0 + 32 * j < a.norm_rows;
+                    z += counts ? (double)wt[j] : 0.0;
+                }
+            }
+#pragma unroll
+            for (int o = 16; o; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+            if (lane == 0) *a.norm = z != 0.0 ? (float)(1.0 / z) : 0.f;
         }
     } else {
         // ---- epilogue ----
         const int quarter = warp & 3;                          // the tensor-memory lanes this warp may read
         const int half = (warp - 2) >> 2;                      // columns half * bn / 2 ...
-        const int hn = a.bn >> 1;
-        const unsigned lane_base = tmem + ((unsigned)(quarter * 32) << 16) + (unsigned)(half * hn);
+        const unsigned lane_base = tmem + ((unsigned)(quarter * 32) << 16);
         float4* xb = reinterpret_cast<float4*>(staging + (size_t)(warp - 2) * TG_STAGING);
         const unsigned acce0 = cluster_addr(bar_acce, 0);
         int it = 0;
         if (EPI == EPI_STORE) {
-            const float scale = a.scale ? __ldg(a.scale) : 1.f;
-            for (int u = pair; u < a.units; u += pairs) {
-                const TileUnit w = tile_unit(a, u);
+            TileUnit w;
+            for (int j = 0; tile_unit(a, j, w); ++j) {
+                const TileProblem& p = a.p[w.which];
+                const float scale = p.scale ? __ldg(p.scale) : 1.f;
+                const int hn = p.bn >> 1;
                 const int row0 = w.m0 + rank * 128 + quarter * 32, col_base = w.n0 + half * hn;
-                const int chunks = min(hn / 32, max(0, (a.N - col_base + 31) / 32));      // blocks of 32 columns that exist
+                const int chunks = row0 < p.M ? min(hn / 32, max(0, (p.N - col_base + 31) / 32)) : 0;      // blocks of 32 columns that exist
                 // partial tiles: lanes of a warp (rows) side by side
-                float* part = w.piece >= 0 ? a.part + ((size_t)w.piece * 2 + rank) * (TG_PART / 2) + (size_t)(half * hn) * 128 + quarter * 32 + lane : nullptr;
+                float* part = w.piece >= 0 ? p.part + ((size_t)w.piece * 2 + rank) * (TG_PART / 2) + (size_t)(half * hn) * 128 + quarter * 32 + lane : nullptr;
                 for (int k0 = w.kb0; k0 < w.kb1; ++it) {
-                    const int k1 = a.kacc > 0 ? min(w.kb1, k0 + a.kacc) : w.kb1;
+                    const int k1 = p.kacc > 0 ? min(w.kb1, k0 + p.kacc) : w.kb1;
                     mbar_wait_warp(bar_accf + 8 * (it & 1), (unsigned)((it >> 1) & 1), a.status, dead);
                     asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
 #pragma unroll 1
                     for (int c = 0; c < chunks; ++c) {
                         float v[32];
-                        tmem_ld32(lane_base + (unsigned)((it & 1) * TG_BN + 32 * c), v);
+                        tmem_ld32(lane_base + (unsigned)((it & 1) * TG_BN + half * hn + 32 * c), v);
                         tmem_wait(v);
                         if (c == chunks - 1) {                 // the last read: the accumulator is free
                             asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
@@ -384,15 +449,15 @@ k_tile(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
                         }
                         const bool more = k0 > w.kb0;          // the sum so far lies where this one goes
                         if (part) {
-                            float* p = part + (size_t)(32 * c) * 128;
+                            float* q = part + (size_t)(32 * c) * 128;
                             if (more) {
 #pragma unroll
-                                for (int j = 0; j < 32; ++j) v[j] += p[j * 128];
+                                for (int i = 0; i < 32; ++i) v[i] += q[i * 128];
                             }
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) p[j * 128] = v[j];
+                            for (int i = 0; i < 32; ++i) q[i * 128] = v[i];
                         } else {
-                            emit_block(a, xb, v, row0, col_base + 32 * c, more ? (const float*)a.out : a.addend, more ? a.ldo : (long long)a.N, scale);
+                            emit_block(p, xb, v, row0, col_base + 32 * c, more ? (const float*)p.out : p.addend, more ? p.ldo : (long long)p.N, scale);
                         }
                     }
                     if (chunks == 0 && lane == 0) mbar_arrive_cluster(acce0 + 8 * (it & 1));
@@ -406,25 +471,25 @@ k_tile(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
             constexpr int CH = 64;
             constexpr int SEG = EPI == EPI_LOSS ? XE_SEG_LOSS : XE_SEG;
             const int lrow = lane >> 3, lch = lane & 7;
+            const TileProblem& p = a.p[0];
             auto label_of = [&](const TileUnit& w) {           // the row's label, -1 where there is no row
                 const int row = w.m0 + rank * 128 + quarter * 32 + lane;
-                return row < a.M ? a.labels[row] : -1ll;
+                return row < p.M ? a.labels[row] : -1ll;
             };
-            TileUnit next = tile_unit(a, pair);
-            long long next_label = label_of(next);
-            for (int u = pair; u < a.units; u += pairs, ++it) {
+            TileUnit next;
+            bool going = tile_unit(a, 0, next);
+            long long next_label = going ? label_of(next) : -1ll;
+            for (; going; ++it) {
                 const TileUnit w = next;
                 const int row0 = w.m0 + rank * 128 + quarter * 32, col_base = w.n0 + half * 128, row = row0 + lane;
                 const int b = it & 1;
                 const int label_col = (int)min(max(next_label - (long long)col_base, -1ll), 128ll);   // among this warp's columns
-                if (u + pairs < a.units) {                     // asked for a tile ahead
-                    next = tile_unit(a, u + pairs);
-                    next_label = label_of(next);
-                }
+                going = tile_unit(a, it + 1, next);
+                if (going) next_label = label_of(next);        // asked for a tile ahead
                 mbar_wait_warp(bar_accf + 8 * b, (unsigned)((it >> 1) & 1), a.status, dead);
                 asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
-                const unsigned taddr = lane_base + (unsigned)(b * TG_BN);
-                const int ncols = min(128, a.N - col_base);                        // (<= 0: none of these columns exists)
+                const unsigned taddr = lane_base + (unsigned)(b * TG_BN + half * 128);
+                const int ncols = row0 < p.M ? min(128, p.N - col_base) : 0;       // (<= 0: none of these columns exists, or none of the rows)
                 float top = -INFINITY, sum = 0.f;
 #pragma unroll
                 for (int c = 0; c < 128 / CH; ++c) {
@@ -469,7 +534,7 @@ k_tile(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
                     top = m;
                     sum = (part[0] + part[1]) + (part[2] + part[3]);
                     if (EPI == EPI_SOFTMAX) {
-                        if (row < a.M) a.stats[(size_t)row * a.nseg + (col_base + CH * c) / SEG] = make_float2(top, sum);
+                        if (row < p.M) a.stats[(size_t)row * a.nseg + (col_base + CH * c) / SEG] = make_float2(top, sum);
                         uint4* xq = reinterpret_cast<uint4*>(xb);
 #pragma unroll
                         for (int j = 0; j < 8; ++j) xq[lane * 8 + (j ^ (lane & 7))] = make_uint4(pk[4 * j], pk[4 * j + 1], pk[4 * j + 2], pk[4 * j + 3]);
@@ -477,13 +542,13 @@ k_tile(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
                             const int br = 4 * i + lrow;
-                            if (row0 + br < a.M)               // rows of q are padded to whole segments
+                            if (row0 + br < p.M)               // rows of q are padded to whole segments
                                 *reinterpret_cast<uint4*>(a.q + (size_t)(row0 + br) * a.ldq + col_base + CH * c + 8 * lch) = xq[br * 8 + (lch ^ (br & 7))];
                         }
                         __syncwarp();
                     }
                 }
-                if (EPI == EPI_LOSS && ncols > 0 && row < a.M) a.stats[(size_t)row * a.nseg + col_base / SEG] = make_float2(top, sum);
+                if (EPI == EPI_LOSS && ncols > 0 && row < p.M) a.stats[(size_t)row * a.nseg + col_base / SEG] = make_float2(top, sum);
                 if (ncols <= 0 && lane == 0) mbar_arrive_cluster(acce0 + 8 * b);
             }
         }
@@ -498,24 +563,29 @@ k_tile(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
     }
 }
 
-// Adds the pieces of the split tiles: blockIdx.x = tail tile, .y = 32 columns of it, .z = half of its rows; a warp per 32 rows.
-__global__ void __launch_bounds__(128) k_join(TileArgs a) {
+// Adds the pieces of the split tiles of both products: blockIdx.x = tail tile, .y = 32 columns of it, .z = half of its rows; a warp per 32 rows.
+__global__ void __launch_bounds__(128) k_join(const __grid_constant__ TileArgs a) {
     __shared__ float4 xb[4][TG_STAGING / 16];
+    grid_trigger();
+    grid_wait();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int first = a.p[0].S > 1 ? a.p[0].tail : 0;
+    const int which = (int)blockIdx.x < first ? 0 : 1, tile = blockIdx.x - (which ? first : 0);
+    const TileProblem& p = a.p[which];
     int m0, n0;
-    tile_origin(a, a.full + blockIdx.x, m0, n0);
+    tile_origin(p, p.full + tile, m0, n0);
     const int c = 32 * blockIdx.y, row0 = m0 + blockIdx.z * 128 + warp * 32;
-    if (n0 + c >= a.N || row0 >= a.M) return;
-    const float* p = a.part + ((size_t)blockIdx.x * 2 + blockIdx.z) * (TG_PART / 2) + (size_t)c * 128 + warp * 32 + lane;
-    const size_t step = (size_t)a.tail * TG_PART;
+    if (c >= p.bn || n0 + c >= p.N || row0 >= p.M) return;
+    const float* q = p.part + ((size_t)tile * 2 + blockIdx.z) * (TG_PART / 2) + (size_t)c * 128 + warp * 32 + lane;
+    const size_t step = (size_t)p.tail * TG_PART;
     float v[32];
 #pragma unroll
-    for (int j = 0; j < 32; ++j) v[j] = p[(size_t)j * 128];
+    for (int j = 0; j < 32; ++j) v[j] = q[(size_t)j * 128];
 #pragma unroll 2
-    for (int s = 1; s < a.S; ++s)
+    for (int s = 1; s < p.S; ++s)
 #pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] += p[(size_t)s * step + (size_t)j * 128];
-    emit_block(a, xb[warp], v, row0, n0 + c, a.addend, a.N, a.scale ? __ldg(a.scale) : 1.f);
+        for (int j = 0; j < 32; ++j) v[j] += q[(size_t)s * step + (size_t)j * 128];
+    emit_block(p, xb[warp], v, row0, n0 + c, p.addend, p.N, p.scale ? __ldg(p.scale) : 1.f);
 }
 
 }  // namespace psgd

@@ -60,18 +60,6 @@ __device__ __forceinline__ double2 block_sum2(double x, double y) {
     return make_double2(x, y);
 }
 
-// 1 / Z, and the counter of the row kernels set to zero.  One CTA.
-__global__ void __launch_bounds__(1024) k_xent_norm(const long long* labels, const float* weight, long long rows, long long ignore, int V, float* inv, int* done) {
-    if (threadIdx.x == 0) *done = 0;
-    double z = 0.0;
-    for (long long i = threadIdx.x; i < rows; i += 1024) {
-        bool bad;
-        z += row_weight(weight, i, labels[i], ignore, V, bad);
-    }
-    const double2 s = block_sum2<1024>(z, 0.0);
-    if (threadIdx.x == 0) *inv = s.x != 0.0 ? (float)(1.0 / s.x) : 0.f;
-}
-
 // the last CTA to get here adds up the loss of all rows
 __device__ __forceinline__ void report_rows(const RowsArgs& a) {
     __shared__ int last;
@@ -129,6 +117,8 @@ __device__ __forceinline__ void write_loss(const RowsArgs& a, int row, float lse
 
 // Loss only: one warp per row.
 __global__ void __launch_bounds__(XE_THREADS) k_xent_loss(RowsArgs a) {
+    grid_trigger();
+    grid_wait();
     const int row = blockIdx.x * (XE_THREADS / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
     if (row < a.rows) {
         float top = -INFINITY, sum = 0.f;
@@ -147,6 +137,8 @@ __global__ void __launch_bounds__(XE_THREADS) k_xent_loss(RowsArgs a) {
 
 // Loss and gradient of the logits: blockIdx.x = row, blockIdx.y = part of its columns.
 __global__ void __launch_bounds__(XE_THREADS) k_xent_rows(RowsArgs a) {
+    grid_trigger();
+    grid_wait();
     __shared__ float2 ws[XE_THREADS / 32];
     const int row = blockIdx.x, tid = threadIdx.x;
     const float2* st = a.stats + (size_t)row * a.nseg;
