@@ -224,6 +224,7 @@ struct UnpackWork {
 };
 template <typename X>
 __global__ void __launch_bounds__(256, PACK_CTAS) k_act_unpack(ActShape s, const int8_t* __restrict__ q, const uint8_t* __restrict__ scales, X* __restrict__ x, long long ldx) {
+    grid_trigger();                                   // (before a product in the same call)
     const ActCursor c = act_cursor();
     if (c.col >= s.F) return;
     UnpackWork<X> k{c.col, s.G, q, scales, x, ldx};

@@ -46,7 +46,7 @@ TilePlan plan_tiles(int64_t M, int64_t N, int64_t K, int pairs, bool store) {
         const int64_t tiles = (int64_t)p.mt * nt;
         const int R = (int)(tiles % pairs);
         const double whole = (double)(tiles / pairs) * (p.kb + 1) * stage;
-        for (int S = 1, most = store && R > 0 ? std::min(p.kb, 2 * pairs / R + 1) : 1; S <= most; ++S) {
+        for (int S = 1; S <= (store && R > 0 ? std::min(p.kb, 2 * pairs) : 1); ++S) {
             const int kbps = ceil_div(p.kb, S);
             if (ceil_div(p.kb, kbps) != S) continue;                           // no empty pieces
             double cost = whole + (R > 0 ? (double)ceil_div((int64_t)R * S, pairs) * (kbps + ROUND_COST) * stage : 0.0);
@@ -58,7 +58,7 @@ TilePlan plan_tiles(int64_t M, int64_t N, int64_t K, int pairs, bool store) {
     return p;
 }
 
-// Two products that share one launch (launch_two): no waves to fill, only units that must not be longer than a pair's share of
+// Two products that share one launch (launch_products): no waves to fill, only units that must not be longer than a pair's share of
 // the whole work, so a product is cut along k, all its tiles alike, where its tiles would be.
 void plan_two(TilePlan (&p)[2], const int64_t (&M)[2], int64_t N, const int64_t (&K)[2], int pairs) {
     double total = 0.0;
@@ -139,53 +139,30 @@ psgd_status launch_softmax(const Operand& A, const Operand& B, const TilePlan& p
     return launch_after(k_tile<EPI>, dim3(2 * n), dim3(TG_THREADS), tile_smem_bytes(), st, early, ma, mb, ma, mb, a) ? PSGD_OK : PSGD_E_CUDA;
 }
 
-// The pieces of split tiles, after a launch of k_tile.
-bool join_pieces(const TileArgs& a, cudaStream_t st) {
-    const int joins = (a.p[0].S > 1 ? a.p[0].tail : 0) + (a.p[1].S > 1 ? a.p[1].tail : 0);
-    return !joins || launch_after(k_join, dim3(joins, std::max(a.p[0].bn, a.p[1].bn) / 32, 2), dim3(128), 0, st, true, a);
-}
-
-// Two products (B MN-major) in one launch: the units of the first go round the pairs; the pairs that have one unit fewer of it do as many
-// units of the second meanwhile as fit in that time.
-psgd_status launch_two(const Operand (&A)[2], const Operand (&B)[2], const TilePlan (&p)[2], TileArgs& a, int pairs, cudaStream_t st) {
+// One or two products (B MN-major) in one launch, then the pieces of their split tiles.  Two: the units of the first go round the pairs; the
+// pairs that have one unit fewer of it do as many units of the second meanwhile as fit in that time.
+psgd_status launch_products(int count, const Operand (&A)[2], const Operand (&B)[2], const TilePlan (&p)[2], TileArgs& a, int pairs, bool early, cudaStream_t st) {
     CUtensorMap m[4];
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < count; ++i) {
         if (!encode(&m[2 * i], A[i], p[i].M, p[i].K, 128) || !encode(&m[2 * i + 1], B[i], p[i].N, p[i].K, p[i].bn / 2)) return PSGD_E_CUDA;
         set_problem(a.p[i], p[i]);
         a.p[i].a_mn = A[i].mn;
     }
-    const int n = std::min(p[0].units + p[1].units, pairs);
+    if (count == 1) { m[2] = m[0]; m[3] = m[1]; }
+    const int second = count == 2 ? p[1].units : 0;
+    const int n = std::min(p[0].units + second, pairs);
     a.first_q = p[0].units / n; a.first_r = p[0].units % n;
     a.extra = 0;
-    if (a.first_r) {
-        const int c0 = (p[0].S > 1 ? p[0].kbps : p[0].kb) + ROUND_COST, c1 = (p[1].S > 1 ? p[1].kbps : p[1].kb) + ROUND_COST;
-        a.extra = std::min((c0 + c1 / 2) / c1, p[1].units / (n - a.first_r));
+    if (second && a.first_r) {
+        const int c0 = (p[0].S > 1 ? p[0].kbps : p[0].kb) + ROUND_COST, c1 = (p[1].full ? p[1].kb : p[1].kbps) + ROUND_COST;
+        a.extra = std::min((c0 + c1 / 2) / c1, second / (n - a.first_r));
     }
     allow_smem(k_tile<EPI_STORE>, tile_smem_bytes());
-    if (!launch_after(k_tile<EPI_STORE>, dim3(2 * n), dim3(TG_THREADS), tile_smem_bytes(), st, true, m[0], m[1], m[2], m[3], a)) return PSGD_E_CUDA;
-    return join_pieces(a, st) ? PSGD_OK : PSGD_E_CUDA;
-}
-
-// One product, A [K][M] bfloat16 and B an 8-bit checkpoint [K][N] (rows of 32 `groups` bytes).
-psgd_status launch_q8(const Operand& A, const int8_t* q, const uint8_t* scales, int groups, const TilePlan& p, TileArgs& a, int pairs, cudaStream_t st) {
-    CUtensorMap ma, mb;
-    EncodeTiledFn fn = encode_tiled_fn();
-    cuuint64_t dims[2] = {(cuuint64_t)groups * ACT_GROUP, (cuuint64_t)p.K};
-    cuuint64_t strides[1] = {(cuuint64_t)groups * ACT_GROUP};
-    cuuint32_t box[2] = {128, TG_BK};
-    cuuint32_t es[2] = {1, 1};
-    if (!fn || !encode(&ma, A, p.M, p.K, 128) ||
-        fn(&mb, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, (void*)q, dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
-           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-        return PSGD_E_CUDA;
-    set_problem(a.p[0], p);
-    a.p[0].a_mn = 1;
-    a.scales = scales; a.k_rows = (int)p.K; a.groups = groups;
-    const int n = std::min(p.units, pairs);
-    a.first_q = p.units / n; a.first_r = p.units % n;
-    allow_smem(k_tile<EPI_STORE_Q8>, tile_smem_bytes());
-    if (!launch_after(k_tile<EPI_STORE_Q8>, dim3(2 * n), dim3(TG_Q8_THREADS), tile_smem_bytes(), st, false, ma, mb, ma, mb, a)) return PSGD_E_CUDA;
-    return join_pieces(a, st) ? PSGD_OK : PSGD_E_CUDA;
+    if (!launch_after(k_tile<EPI_STORE>, dim3(2 * n), dim3(TG_THREADS), tile_smem_bytes(), st, early, m[0], m[1], m[2], m[3], a)) return PSGD_E_CUDA;
+    const int joins = (p[0].S > 1 ? p[0].tail : 0) + (count == 2 && p[1].S > 1 ? p[1].tail : 0);
+    const int wide = std::max(p[0].bn, count == 2 ? p[1].bn : 0);
+    if (joins && !launch_after(k_join, dim3(joins, wide / 32, 2), dim3(128), 0, st, true, a)) return PSGD_E_CUDA;
+    return PSGD_OK;
 }
 
 bool operand_ok(const void* p, int64_t rows, int64_t cols, int64_t ld) { return aligned16(p) && ld >= cols && (rows == 1 || ld % 8 == 0); }
@@ -330,7 +307,7 @@ psgd_status xent(const void* H, int64_t ldh, const void* W, int64_t ldw, const i
             pw.out = acc; pw.ldo = D; pw.out_f32 = 1; pw.scale = nullptr;
             pw.vec = D % 4 == 0;
         }
-        s = launch_two(A, B, p, g, x.pairs, st);
+        s = launch_products(2, A, B, p, g, x.pairs, true, st);
         if (s != PSGD_OK) return s;
     }
     return cudaGetLastError() == cudaSuccess ? PSGD_OK : PSGD_E_CUDA;
@@ -371,13 +348,15 @@ void launch_unpack(const ActShape& s, const int8_t* q, const uint8_t* scales, X*
 bool dtype_ok(int dtype) { return dtype == PSGD_DT_F32 || dtype == PSGD_DT_BF16; }
 bool ckpt_ok(const void* q) { return ((uintptr_t)q & 15) == 0; }
 
-struct WgradPlan { int pairs; TilePlan p; size_t part, total; };
+struct WgradPlan { int pairs; int64_t ldx; TilePlan p; size_t x, part, total; };
 WgradPlan plan_wgrad(int64_t T, int64_t O, int64_t F) {
     WgradPlan g{};
     g.pairs = std::max(1, device_sms() / 2);
+    g.ldx = (int64_t)align_up(F, ACT_GROUP);
     g.p = plan_tiles(O, F, T, g.pairs, true);
     size_t at = 256;
     auto take = [&](size_t bytes) { const size_t o = at; at = align_up(at + bytes, 256); return o; };
+    g.x = take((size_t)T * g.ldx * 2);
     g.part = take(part_bytes(g.p));
     g.total = at;
     return g;
@@ -455,6 +434,8 @@ psgd_status psgd_act_wgrad(const void* dY, int64_t lddy, const int8_t* q, const 
     const WgradPlan g = plan_wgrad(T, O, F);
     if (ws_bytes < g.total) return PSGD_E_WORKSPACE;
     char* w = (char*)ws;
+    const ActShape s{T, (int)F, ceil_div(F, ACT_GROUP)};
+    launch_unpack(ActShape{T, (int)g.ldx, s.G}, q, scales, (__nv_bfloat16*)(w + g.x), g.ldx, true, st);     // the padding too: its values are zeros
     TileArgs a{};
     a.status = status ? status : (int*)w;
     TileProblem& t = a.p[0];
@@ -462,7 +443,9 @@ psgd_status psgd_act_wgrad(const void* dY, int64_t lddy, const int8_t* q, const 
     t.vec = ((uintptr_t)dW & (t.out_f32 ? 15 : 7)) == 0 && lddw % 4 == 0;
     t.kacc = t.out_f32 ? KACC_F32 : 0;
     t.part = (float*)(w + g.part);
-    return launch_q8({dY, lddy, true}, q, scales, ceil_div(F, ACT_GROUP), g.p, a, g.pairs, st);
+    const Operand A[2] = {{dY, lddy, true}, {}}, B[2] = {{w + g.x, g.ldx, true}, {}};
+    const TilePlan p[2] = {g.p, {}};
+    return launch_products(1, A, B, p, a, g.pairs, true, st);
 } catch (...) {
     return PSGD_E_CUDA;
 }

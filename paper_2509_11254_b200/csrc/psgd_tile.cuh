@@ -35,15 +35,11 @@ constexpr int TG_EPI_WARPS = 8;
 constexpr int TG_THREADS = 64 + 32 * TG_EPI_WARPS;      // warp 0: TMA, warp 1: MMA and tensor-memory owner, warps 2-9: epilogue
 constexpr int TG_STAGING = 4096;              // per epilogue warp: a block turned from row-per-lane to row-contiguous
 constexpr int TG_PART = TG_BM * TG_BN;        // floats of one partial tile
-constexpr int TG_Q8_STAGES = 5;               // with an 8-bit B: the room of the sixth stage holds the ring of 8-bit boxes
-constexpr int TG_RAW = 4, TG_RAW_BYTES = TG_BK * 128;  // 64 k x 128 columns each
-constexpr int TG_CONVERT_WARPS = 4;
-constexpr int TG_Q8_THREADS = TG_THREADS + 32 * TG_CONVERT_WARPS;
 constexpr int XE_SEG_LOSS = 128, XE_SEG = 64; // columns per softmax statistic: loss only, and where exponents are kept relative to its maximum
 
 inline size_t tile_smem_bytes() { return (size_t)TG_STAGES * TG_STAGE_BYTES + TG_EPI_WARPS * TG_STAGING + 1024 + 256; }
 
-enum TileEpilogue { EPI_LOSS = 0, EPI_SOFTMAX = 1, EPI_STORE = 2, EPI_STORE_Q8 = 3 };   // Q8: B comes as an 8-bit checkpoint
+enum TileEpilogue { EPI_LOSS = 0, EPI_SOFTMAX = 1, EPI_STORE = 2 };
 
 // Division by a launch constant: q = n * mul >> shift for 0 <= n < 2^31 (mul = floor(2^shift / d) + 1, shift = 31 + ceil(log2 d)).
 struct FastDiv { unsigned mul, shift; };
@@ -81,9 +77,6 @@ struct TileArgs {
     // pairs do `extra` units of p[1] each, and the rest of those go round all pairs.
     int first_q, first_r, extra;
     int* status;               // device status word
-    // EPI_STORE_Q8: scale bytes of B [k_rows][groups]
-    const unsigned char* scales;
-    int k_rows, groups;
     // EPI_LOSS, EPI_SOFTMAX
     const long long* labels;
     float2* stats;             // [M][nseg]: maximum and sum of exp(l - maximum) of each segment
@@ -126,11 +119,6 @@ __device__ __forceinline__ void pair_tma_2d(unsigned dst, const CUtensorMap* map
     asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n"
                  ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
 }
-// box into this CTA's shared memory, bytes counted by a barrier of its own
-__device__ __forceinline__ void tma_2d(unsigned dst, const CUtensorMap* map, int x, int y, unsigned bar) {
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n"
-                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
-}
 __device__ __forceinline__ unsigned cluster_addr(unsigned local, unsigned rank) {
     unsigned r;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(r) : "r"(local), "r"(rank));
@@ -140,15 +128,6 @@ __device__ __forceinline__ unsigned cluster_addr(unsigned local, unsigned rank) 
 // before); no global write has to be visible for that, and a release at cluster scope would wait for all of them.
 __device__ __forceinline__ void mbar_arrive_cluster(unsigned bar) {
     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];\n" ::"r"(bar) : "memory");
-}
-// The same for what generic writes to shared memory announce: with release and acquire across the pair.
-__device__ __forceinline__ void mbar_release_cluster(unsigned bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];\n" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ bool mbar_try_wait_cluster(unsigned bar, unsigned parity) {
-    unsigned ok;
-    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}\n" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-    return ok != 0;
 }
 // 32 lanes x 32 consecutive columns of tensor memory -> 32 registers (lane = row of the accumulator); valid after tmem_wait
 __device__ __forceinline__ void tmem_ld32(unsigned taddr, float (&v)[32]) {
@@ -182,26 +161,6 @@ __device__ __forceinline__ void mbar_wait_all(unsigned bar, unsigned parity, int
         mbar_wait(bar, parity, flags, dead);
         dead = __any_sync(0xffffffffu, dead);
     }
-}
-// ... for a barrier that the other CTA's threads arrive on with a release
-__device__ __forceinline__ void mbar_wait_all_cluster(unsigned bar, unsigned parity, int* flags, bool& dead) {
-    for (unsigned it = 0; it < FU_WAIT_LIMIT && !dead; ++it)
-        if (__all_sync(0xffffffffu, mbar_try_wait_cluster(bar, parity))) return;
-    if (!dead) atomicOr(flags, FU_W_TIMEOUT);
-    dead = true;
-}
-// Four int8 values, each with 128 added, times a power of two (or NaN) given twice as bfloat16 -> four bfloat16, exactly.
-// A byte b below 128 under the exponent of 128 reads 128 + b, of one from 128 on the low seven bits read b itself: subtract 256 or 128.
-__device__ __forceinline__ uint2 widen4(unsigned w, __nv_bfloat162 scale) {
-    uint2 r;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const unsigned b = __byte_perm(w, 0u, i ? 0x4342 : 0x4140);                     // two bytes, each in the low half of 16 bits
-        const unsigned x = (b & 0x007f007fu) | 0x43004300u, c = (b & 0x00800080u) ^ 0x43804380u;
-        const __nv_bfloat162 v = __hmul2(__hsub2(*reinterpret_cast<const __nv_bfloat162*>(&x), *reinterpret_cast<const __nv_bfloat162*>(&c)), scale);
-        (i ? r.y : r.x) = *reinterpret_cast<const unsigned*>(&v);
-    }
-    return r;
 }
 __device__ __forceinline__ float ex2(float x) {
     float y;
@@ -311,17 +270,11 @@ constexpr float XE_MAGIC = 8388608.f;         // 2^23: adding it leaves the roun
 constexpr unsigned XE_NONE = 65535u;
 
 // EPI_LOSS, EPI_SOFTMAX: one product of K-major operands.  EPI_STORE: products whose B is MN-major, A either.
-// EPI_STORE_Q8: one product whose B is an 8-bit checkpoint [K][N]: TMA brings its bytes, four more warps per CTA write them as bfloat16
-// (exact: the scales are powers of two) into the operand's place, in the swizzle that TMA would have used.  No 16-bit copy of the
-// checkpoint exists in memory, and half the bytes of that operand come from L2.
 template <int EPI>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(EPI == EPI_STORE_Q8 ? TG_Q8_THREADS : TG_THREADS, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TG_THREADS, 1)
 k_tile(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtensorMap tmB0, const __grid_constant__ CUtensorMap tmA1, const __grid_constant__ CUtensorMap tmB1,
        const __grid_constant__ TileArgs a) {
-    constexpr bool Q8 = EPI == EPI_STORE_Q8, BMN = EPI == EPI_STORE || Q8;
-    constexpr int STAGES = Q8 ? TG_Q8_STAGES : TG_STAGES;
-    // columns of a tile per CTA: half of what is left, in whole steps of the MMA (with an 8-bit B: in whole groups of 32)
-    const auto half_columns = [](const TileProblem& p, int n0) { const int n = min(p.bn, p.N - n0); return Q8 ? (n + 63) / 64 * 32 : (n + 31) / 32 * 16; };
+    constexpr bool BMN = EPI == EPI_STORE;
     extern __shared__ __align__(16) unsigned char tg_smem_raw[];
     // the offset of everything in shared memory is the same in both CTAs of the pair (descriptors and commits rely on it)
     unsigned char* base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(tg_smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -329,8 +282,7 @@ k_tile(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtenso
     unsigned long long* bars = reinterpret_cast<unsigned long long*>(staging + TG_EPI_WARPS * TG_STAGING);
     const unsigned bar_full = smem_u32(bars), bar_empty = bar_full + 8 * TG_STAGES;
     const unsigned bar_accf = bar_empty + 8 * TG_STAGES, bar_acce = bar_accf + 16;
-    const unsigned bar_conv = bar_acce + 16, bar_rawf = bar_conv + 8 * TG_Q8_STAGES, bar_rawe = bar_rawf + 8 * TG_RAW;
-    unsigned* tmem_slot = reinterpret_cast<unsigned*>(bars + 2 * TG_STAGES + 4 + TG_Q8_STAGES + 2 * TG_RAW);
+    unsigned* tmem_slot = reinterpret_cast<unsigned*>(bars + 2 * TG_STAGES + 4);
     const unsigned smem_base = smem_u32(base);
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -339,10 +291,6 @@ k_tile(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtenso
     if (tid == 0) {
         for (int s = 0; s < TG_STAGES; ++s) { mbar_init(bar_full + 8 * s, 1); mbar_init(bar_empty + 8 * s, 1); }
         for (int b = 0; b < 2; ++b) { mbar_init(bar_accf + 8 * b, 1); mbar_init(bar_acce + 8 * b, 2 * TG_EPI_WARPS); }
-        if (Q8) {
-            for (int i = 0; i < TG_Q8_STAGES; ++i) mbar_init(bar_conv + 8 * i, 2 * TG_CONVERT_WARPS);
-            for (int i = 0; i < TG_RAW; ++i) { mbar_init(bar_rawf + 8 * i, 1); mbar_init(bar_rawe + 8 * i, TG_CONVERT_WARPS); }
-        }
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     }
     if (warp == 1) {
@@ -358,7 +306,7 @@ k_tile(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtenso
     bool dead = false;
     grid_trigger();
     grid_wait();
-    if (!BMN && blockIdx.x == 0 && tid == 0 && a.done) *a.done = 0;
+    if (EPI != EPI_STORE && blockIdx.x == 0 && tid == 0 && a.done) *a.done = 0;
 
     if (warp == 0) {
         // ---- TMA producer of this CTA: its 128 rows of A and its half of B ----
@@ -372,8 +320,9 @@ k_tile(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtenso
             const CUtensorMap* const mb = w.which ? &tmB1 : &tmB0;
             const bool amn = BMN && p.a_mn, two = p.bn > 128;
             // bytes of B per stage: K-major boxes have bn / 2 rows, MN-major ones come in blocks of 64
-            const unsigned b_bytes = Q8 ? 0 : BMN ? (two ? TG_HALF_BYTES : TG_HALF_BYTES / 2) : (unsigned)p.bn / 2 * TG_BK * 2;
-            const int m = w.m0 + rank * 128, n = w.n0 + rank * half_columns(p, w.n0);
+            const unsigned b_bytes = BMN ? (two ? TG_HALF_BYTES : TG_HALF_BYTES / 2) : (unsigned)p.bn / 2 * TG_BK * 2;
+            const int nh = (min(p.bn, p.N - w.n0) + 31) / 32 * 16;
+            const int m = w.m0 + rank * 128, n = w.n0 + rank * nh;
             for (int kb = w.kb0; kb < w.kb1; ++kb) {
                 mbar_wait_all(bar_empty + 8 * s, par, a.status, dead);
                 if (dead) break;
@@ -388,9 +337,7 @@ k_tile(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtenso
                     } else {
                         pair_tma_2d(da, ma, k, m, bar);
                     }
-                    if (Q8) {
-                        // the converting warps fetch and write B
-                    } else if (BMN) {
+                    if (BMN) {
                         pair_tma_2d(db, mb, n, k, bar);
                         if (two) pair_tma_2d(db + TG_HALF_BYTES / 2, mb, n + 64, k, bar);
                     } else {
@@ -398,15 +345,15 @@ k_tile(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtenso
                     }
                 }
                 __syncwarp();
-                if (++s == STAGES) { s = 0; par ^= 1; }
-                if (filled < STAGES) ++filled;
+                if (++s == TG_STAGES) { s = 0; par ^= 1; }
+                if (filled < TG_STAGES) ++filled;
             }
         }
         // every copy has landed and every release has arrived here before the CTA may go
-        if (filled < STAGES) { s = 0; par = 0; }
+        if (filled < TG_STAGES) { s = 0; par = 0; }
         for (int i = 0; i < filled && !dead; ++i) {
             mbar_wait_all(bar_empty + 8 * s, par, a.status, dead);
-            if (++s == STAGES) { s = 0; par ^= 1; }
+            if (++s == TG_STAGES) { s = 0; par ^= 1; }
         }
         if (dead)
             for (int i = 0; i < 200; ++i) __nanosleep(1000);   // copies in flight land
@@ -419,7 +366,7 @@ k_tile(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtenso
             for (int j = 0; !dead && tile_unit(a, j, w); ++j) {
                 const TileProblem& p = a.p[w.which];
                 const bool amn = BMN && p.a_mn;
-                const unsigned idesc = tile_idesc(2 * half_columns(p, w.n0), amn, BMN);
+                const unsigned idesc = tile_idesc((min(p.bn, p.N - w.n0) + 31) / 32 * 32, amn, BMN);
                 const unsigned step_a = amn ? 2048 >> 4 : 32 >> 4, step_b = BMN ? 2048 >> 4 : 32 >> 4;   // 16 of k: two groups of 8 rows, or 32 bytes of a row
                 for (int k0 = w.kb0; k0 < w.kb1 && !dead; ++it) {
                     const int k1 = p.kacc > 0 ? min(w.kb1, k0 + p.kacc) : w.kb1;
@@ -430,7 +377,6 @@ k_tile(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtenso
                     }
                     for (int kb = k0; kb < k1; ++kb) {
                         mbar_wait_all(bar_full + 8 * s, par, a.status, dead);
-                        if (Q8 && !dead) mbar_wait_all_cluster(bar_conv + 8 * s, par, a.status, dead);
                         if (dead) break;
                         const unsigned sa = smem_base + s * TG_STAGE_BYTES;
                         const unsigned long long da = tile_desc(sa, amn), db = tile_desc(sa + TG_HALF_BYTES, BMN);
@@ -442,7 +388,7 @@ k_tile(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtenso
                             if (kb == k1 - 1) pair_commit(bar_accf + 8 * (it & 1));
                         }
                         __syncwarp();
-                        if (++s == STAGES) { s = 0; par ^= 1; }
+                        if (++s == TG_STAGES) { s = 0; par ^= 1; }
                     }
                     k0 = k1;
                 }
@@ -469,94 +415,6 @@ k_tile(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtenso
             for (int o = 16; o; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
             if (lane == 0) *a.norm = z != 0.0 ? (float)(1.0 / z) : 0.f;
         }
-    } else if (Q8 && warp >= 2 + TG_EPI_WARPS) {
-        // ---- 8-bit B: this CTA's 64 x 128 bytes of every stage -> bfloat16 in the stage ----
-        // A thread turns one row of k (its 64 bytes of one half): 16 bytes at a time in an order that leaves both sides free of bank conflicts.
-        const int ct = tid - TG_THREADS, row = ct >> 1, hf = ct & 1;
-        const TileProblem& p = a.p[0];
-        unsigned char* raw = base + (size_t)TG_Q8_STAGES * TG_STAGE_BYTES;
-        const unsigned conv0 = cluster_addr(bar_conv, 0);
-        const CUtensorMap* const mb = &tmB0;
-        // the bytes are fetched TG_RAW - 1 stages ahead, the scales two
-        TileUnit fw, w;
-        int fj = 0, fk = 0, fr = 0;
-        unsigned fpar = 1;
-        bool fetching = tile_unit(a, 0, fw);
-        if (fetching) fk = fw.kb0;
-        auto fetch = [&]() {
-            if (!fetching) return;
-            if (warp == 2 + TG_EPI_WARPS) {
-                mbar_wait_all(bar_rawe + 8 * fr, fpar, a.status, dead);
-                if (!dead && elect_one()) {
-                    mbar_expect_tx(bar_rawf + 8 * fr, TG_RAW_BYTES);
-                    tma_2d(smem_u32(raw) + fr * TG_RAW_BYTES, mb, fw.n0 + rank * half_columns(p, fw.n0), fk * TG_BK, bar_rawf + 8 * fr);
-                }
-                __syncwarp();
-            }
-            if (++fr == TG_RAW) { fr = 0; fpar ^= 1; }
-            if (++fk == fw.kb1) {
-                fetching = tile_unit(a, ++fj, fw);
-                if (fetching) fk = fw.kb0;
-            }
-        };
-        // the two scales (groups) of this thread's 64 columns in stage (unit, kb); rows and groups that do not exist count with 1
-        auto scales_of = [&](const TileUnit& u, int kb) {
-            const int k = kb * TG_BK + row, g = ((u.n0 + rank * half_columns(p, u.n0)) >> 5) + 2 * hf;
-            const unsigned char* at = a.scales + (size_t)min(k, a.k_rows - 1) * a.groups;
-            const unsigned s0 = k < a.k_rows && g < a.groups ? __ldg(at + g) : 127u, s1 = k < a.k_rows && g + 1 < a.groups ? __ldg(at + g + 1) : 127u;
-            return s0 | s1 << 8;
-        };
-        struct Ahead { TileUnit u; int j, kb; bool ok; };
-        auto advance = [&](Ahead& x) {
-            if (++x.kb == x.u.kb1) {
-                x.ok = tile_unit(a, ++x.j, x.u);
-                x.kb = x.u.kb0;
-            }
-        };
-        Ahead ah{};
-        ah.ok = tile_unit(a, 0, ah.u);
-        ah.kb = ah.u.kb0;
-        unsigned sc[2] = {0u, 0u};
-#pragma unroll
-        for (int i = 0; i < 2; ++i) if (ah.ok) { sc[i] = scales_of(ah.u, ah.kb); advance(ah); }
-        for (int i = 0; i < TG_RAW - 1; ++i) fetch();
-        int s = 0, r = 0;
-        unsigned par = 1, rpar = 0;
-        for (int j = 0; !dead && tile_unit(a, j, w); ++j) {
-            for (int kb = w.kb0; kb < w.kb1 && !dead; ++kb) {
-                fetch();
-                const unsigned now = sc[0];
-                sc[0] = sc[1];
-                if (ah.ok) { sc[1] = scales_of(ah.u, ah.kb); advance(ah); }
-                mbar_wait_all(bar_rawf + 8 * r, rpar, a.status, dead);
-                if (!dead) mbar_wait_all(bar_empty + 8 * s, par, a.status, dead);
-                if (dead) break;
-                const uint4* from = reinterpret_cast<const uint4*>(raw + (size_t)r * TG_RAW_BYTES + row * 128 + hf * 64);
-                unsigned char* to = base + (size_t)s * TG_STAGE_BYTES + TG_HALF_BYTES + hf * (TG_HALF_BYTES / 2) + row * 128;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int c = i ^ (row & 3) ^ (hf << 1);               // 16 bytes = columns 16 c ... of this half
-                    const uint4 q = from[c];
-                    const unsigned byte = (now >> ((c >> 1) * 8)) & 0xffu;
-                    const unsigned sbits = byte == 255u ? 0x7fff7fffu : byte << 7 | byte << 23;
-                    const __nv_bfloat162 scale = *reinterpret_cast<const __nv_bfloat162*>(&sbits);
-                    const uint2 x0 = widen4(q.x ^ 0x80808080u, scale), x1 = widen4(q.y ^ 0x80808080u, scale);
-                    const uint2 x2 = widen4(q.z ^ 0x80808080u, scale), x3 = widen4(q.w ^ 0x80808080u, scale);
-                    *reinterpret_cast<uint4*>(to + (((2 * c) ^ (row & 7)) << 4)) = make_uint4(x0.x, x0.y, x1.x, x1.y);
-                    *reinterpret_cast<uint4*>(to + (((2 * c + 1) ^ (row & 7)) << 4)) = make_uint4(x2.x, x2.y, x3.x, x3.y);
-                }
-                asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
-                __syncwarp();
-                if (lane == 0) {
-                    mbar_release_cluster(conv0 + 8 * s);
-                    mbar_arrive(bar_rawe + 8 * r);
-                }
-                if (++s == STAGES) { s = 0; par ^= 1; }
-                if (++r == TG_RAW) { r = 0; rpar ^= 1; }
-            }
-        }
-        if (dead)
-            for (int i = 0; i < 200; ++i) __nanosleep(1000);               // copies in flight land
     } else {
         // ---- epilogue ----
         const int quarter = warp & 3;                          // the tensor-memory lanes this warp may read
@@ -565,7 +423,7 @@ k_tile(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtenso
         float4* xb = reinterpret_cast<float4*>(staging + (size_t)(warp - 2) * TG_STAGING);
         const unsigned acce0 = cluster_addr(bar_acce, 0);
         int it = 0;
-        if (BMN) {
+        if (EPI == EPI_STORE) {
             TileUnit w;
             for (int j = 0; tile_unit(a, j, w); ++j) {
                 const TileProblem& p = a.p[w.which];
