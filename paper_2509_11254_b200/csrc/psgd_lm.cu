@@ -46,7 +46,7 @@ TilePlan plan_tiles(int64_t M, int64_t N, int64_t K, int pairs, bool store) {
         const int64_t tiles = (int64_t)p.mt * nt;
         const int R = (int)(tiles % pairs);
         const double whole = (double)(tiles / pairs) * (p.kb + 1) * stage;
-        for (int S = 1; S <= (store && R > 0 ? std::min(p.kb, 2 * pairs) : 1); ++S) {
+        for (int S = 1, most = store && R > 0 ? std::min(p.kb, 2 * pairs / R + 1) : 1; S <= most; ++S) {
             const int kbps = ceil_div(p.kb, S);
             if (ceil_div(p.kb, kbps) != S) continue;                           // no empty pieces
             double cost = whole + (R > 0 ? (double)ceil_div((int64_t)R * S, pairs) * (kbps + ROUND_COST) * stage : 0.0);

@@ -365,6 +365,30 @@ def test_weight_gradient_matches_definition(torch, ops, T, O, F, dtype):
     assert torch.equal(out, ops.weight_gradient(dy, kept, dtype=getattr(torch, dtype)))
 
 
+@pytest.mark.parametrize("T", [1, 64, 65, 130])
+def test_weight_gradient_of_groups_that_are_not_numbers(torch, ops, T):
+    """An infinity in the last row makes the 32 input columns of its group NaN, and no others (rows behind the last one count as zeros)."""
+    O, F = 40, 200
+    g = gen(torch, T)
+    x = torch.randn(T, F, generator=g, device="cuda").to(torch.bfloat16)
+    dy = torch.randn(T, O, generator=g, device="cuda").to(torch.bfloat16)
+    x[-1, 70], x[0, 199] = float("inf"), float("nan")
+    dw = ops.weight_gradient(dy, ops.pack_activation(x))
+    bad = torch.zeros(F, dtype=torch.bool, device="cuda")
+    bad[64:96] = bad[192:200] = True
+    assert bool(torch.isnan(dw[:, bad]).all()) and bool(torch.isfinite(dw[:, ~bad]).all())
+
+
+def test_weight_gradient_of_extreme_scales(torch, ops):
+    """Groups at both ends of the scale's range come out exactly (one row: every entry is one product)."""
+    x = torch.ones(1, 96, device="cuda")
+    x[:, :32] *= 3.0e38
+    x[:, 32:64] *= 2.0 ** -125
+    kept = ops.pack_activation(x)
+    dy = torch.tensor([[0.5, -0.25]], device="cuda", dtype=torch.bfloat16)
+    assert torch.equal(ops.weight_gradient(dy, kept), dy.float().T @ kept.unpack(torch.float32))
+
+
 def test_weight_gradient_slots_and_strides(torch, ops):
     T, O, F = 333, 264, 136
     g = gen(torch, 2)
