@@ -175,7 +175,7 @@ struct XentPlan {
     int pairs, nseg;
     int64_t ldq, piece, pieces;
     TilePlan logits, two[2];          // of a whole piece; two: dH and dW
-    size_t inv, done, stats, label_logit, q, part, acc, total;
+    size_t inv, done, sums, stats, label_logit, q, part, acc, total;
 };
 // Tokens are taken in pieces, all columns at a time, so that the stored exponents stay within a fixed size however many
 // tokens there are; a piece has at least 1024 tokens, below which the products with the vocabulary matrix would be bound by reading it.
@@ -204,6 +204,7 @@ XentPlan plan_xent(int64_t T, int64_t V, int64_t D, bool grad) {
     if (grad) {
         plan_gradients(x.two, x.piece, V, D, x.pairs);
     }
+    x.sums = take((size_t)(grad ? T : ceil_div(T, XE_THREADS / 32)) * sizeof(double2));
     x.stats = take((size_t)x.piece * x.nseg * 8);
     x.label_logit = take((size_t)x.piece * 4);
     if (grad) {
@@ -244,7 +245,7 @@ psgd_status xent(const void* H, int64_t ldh, const void* W, int64_t ldw, const i
     r.stats = (const float2*)(w + x.stats);
     r.label_logit = (const float*)(w + x.label_logit);
     r.ignore = ignore; r.ldq = x.ldq; r.status = stat; r.q = grad ? (unsigned short*)(w + x.q) : nullptr;
-    r.done = done; r.all_rows = T; r.all_labels = (const long long*)labels; r.all_weight = weight; r.all_loss = token_loss; r.mean = loss;
+    r.done = done; r.sums = (double2*)(w + x.sums); r.n_sums = (int)(grad ? T : ceil_div(T, XE_THREADS / 32)); r.mean = loss;
     auto parts_of = [&](int64_t rows) {               // CTAs per row of k_xent_rows: two waves of eight per multiprocessor, at least 2048 columns each
         return (int)std::max<int64_t>(1, std::min<int64_t>({(2 * 8 * 2 * (int64_t)x.pairs + rows - 1) / rows, (V + 2047) / 2048, 1024}));
     };
@@ -276,6 +277,7 @@ psgd_status xent(const void* H, int64_t ldh, const void* W, int64_t ldw, const i
         psgd_status s = grad ? launch_softmax<EPI_SOFTMAX>(oh, ow, pl, a, x.pairs, !first, st) : launch_softmax<EPI_LOSS>(oh, ow, pl, a, x.pairs, false, st);
         if (s != PSGD_OK) return s;
         r.rows = (int)rows;
+        r.first_sum = (int)t0;                        // (without gradients there is one piece)
         r.labels = (const long long*)labels + t0;
         r.weight = weight ? weight + t0 : nullptr;
         r.loss = token_loss + t0;

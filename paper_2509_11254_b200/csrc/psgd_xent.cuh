@@ -16,6 +16,7 @@
 namespace psgd {
 
 constexpr int XE_THREADS = 256;
+constexpr int XE_ROW_CTAS = 5;     // of k_xent_rows per multiprocessor: 48 registers (with 128, two CTAs, the kernel took 139 instead of 92 us on 4096 x 32000)
 constexpr int XE_W_LABEL = 8;      // == PSGD_W_LABEL
 
 struct RowsArgs {
@@ -31,12 +32,10 @@ struct RowsArgs {
     long long ldq;
     int* status;
     // the mean over all rows, by the last CTA
+    double2* sums;                 // weighted loss and weight of one row (k_xent_rows) or of one CTA's rows (k_xent_loss), over all launches of this call
+    int n_sums, first_sum;
     int* done;
     int done_at;                   // CTAs that report, over all launches of this call
-    long long all_rows;
-    const long long* all_labels;
-    const float* all_weight;
-    const float* all_loss;
     float* mean;
 };
 
@@ -72,23 +71,14 @@ __device__ __forceinline__ void report_rows(const RowsArgs& a) {
     if (!last) return;
     __threadfence();
     double num = 0.0, z = 0.0;
-    constexpr int UN = 16;                                     // rows in flight per thread: alone on the GPU, this is all latency
-    for (long long b = threadIdx.x; b < a.all_rows; b += UN * XE_THREADS) {
-        float w[UN], l[UN];
-        long long label[UN];
+    constexpr int UN = 4;                                      // under way per thread; more registers would cost the kernel occupancy
+    for (int b = threadIdx.x; b < a.n_sums; b += UN * XE_THREADS) {
+        double2 s[UN];
 #pragma unroll
-        for (int j = 0; j < UN; ++j) {                         // loads without branches around them, so that they are all in flight
-            const long long i = min(b + j * XE_THREADS, a.all_rows - 1);
-            label[j] = __ldg(a.all_labels + i);
-            l[j] = __ldcg(a.all_loss + i);
-            w[j] = a.all_weight ? __ldg(a.all_weight + i) : 1.f;
-        }
+        for (int j = 0; j < UN; ++j) s[j] = __ldcg(a.sums + min(b + j * XE_THREADS, a.n_sums - 1));
 #pragma unroll
-        for (int j = 0; j < UN; ++j) {
-            const bool in = label[j] >= 0 && label[j] < a.V, skip = label[j] == a.ignore || b + j * XE_THREADS >= a.all_rows;
-            num += skip ? 0.0 : in ? (double)w[j] * (double)l[j] : (double)l[j];   // a bad row's NaN reaches the mean
-            z += skip || !in ? 0.0 : (double)w[j];
-        }
+        for (int j = 0; j < UN; ++j)
+            if (b + j * XE_THREADS < a.n_sums) { num += s[j].x; z += s[j].y; }
     }
     const double2 s = block_sum2<XE_THREADS>(num, z);
     if (threadIdx.x == 0) *a.mean = (s.y != 0.0 || s.x != s.x) ? (float)(s.x / s.y) : 0.f;
@@ -106,20 +96,26 @@ __device__ __forceinline__ void warp_stat(float& top, float& sum) {
         merge_stat(top, sum, t, s);
     }
 }
-__device__ __forceinline__ void write_loss(const RowsArgs& a, int row, float lse) {
+// the row's outputs; returns its share of the loss and of the weight
+__device__ __forceinline__ double2 write_loss(const RowsArgs& a, int row, float lse) {
     const long long label = a.labels[row];
-    const bool in = label >= 0 && label < a.V;
+    bool bad;
+    const float w = row_weight(a.weight, row, label, a.ignore, a.V, bad);
+    float loss = 0.f;
+    if (bad) { loss = NAN; atomicOr(a.status, XE_W_LABEL); }
+    else if (label != a.ignore) loss = lse - a.label_logit[row];
     a.lse[row] = lse;
-    if (label == a.ignore) a.loss[row] = 0.f;
-    else if (in) a.loss[row] = lse - a.label_logit[row];
-    else { a.loss[row] = NAN; atomicOr(a.status, XE_W_LABEL); }
+    a.loss[row] = loss;
+    return make_double2(bad ? (double)loss : label != a.ignore ? (double)w * (double)loss : 0.0, (double)w);     // a bad row's NaN reaches the mean
 }
 
 // Loss only: one warp per row.
-__global__ void __launch_bounds__(XE_THREADS) k_xent_loss(RowsArgs a) {
+__global__ void __launch_bounds__(XE_THREADS) k_xent_loss(const __grid_constant__ RowsArgs a) {
+    __shared__ double2 mine[XE_THREADS / 32];
     grid_trigger();
     grid_wait();
-    const int row = blockIdx.x * (XE_THREADS / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    const int warp = threadIdx.x >> 5, row = blockIdx.x * (XE_THREADS / 32) + warp, lane = threadIdx.x & 31;
+    double2 share = make_double2(0.0, 0.0);
     if (row < a.rows) {
         float top = -INFINITY, sum = 0.f;
         for (int j = lane; j < a.nseg; j += 8 * 32) {
@@ -130,13 +126,19 @@ __global__ void __launch_bounds__(XE_THREADS) k_xent_loss(RowsArgs a) {
             for (int i = 0; i < 8; ++i) merge_stat(top, sum, s[i].x, s[i].y);
         }
         warp_stat(top, sum);
-        if (lane == 0) write_loss(a, row, top + logf(sum));
+        if (lane == 0) share = write_loss(a, row, top + logf(sum));
+    }
+    if (lane == 0) mine[warp] = share;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < XE_THREADS / 32; ++i) { share.x += mine[i].x; share.y += mine[i].y; }
+        a.sums[a.first_sum + blockIdx.x] = share;
     }
     report_rows(a);
 }
 
 // Loss and gradient of the logits: blockIdx.x = row, blockIdx.y = part of its columns.
-__global__ void __launch_bounds__(XE_THREADS) k_xent_rows(RowsArgs a) {
+__global__ void __launch_bounds__(XE_THREADS, XE_ROW_CTAS) k_xent_rows(const __grid_constant__ RowsArgs a) {
     grid_trigger();
     grid_wait();
     __shared__ float2 ws[XE_THREADS / 32];
@@ -152,7 +154,7 @@ __global__ void __launch_bounds__(XE_THREADS) k_xent_rows(RowsArgs a) {
 #pragma unroll
     for (int i = 1; i < XE_THREADS / 32; ++i) merge_stat(top, sum, ws[i].x, ws[i].y);
     const float lse = top + logf(sum);
-    if (blockIdx.y == 0 && tid == 0) write_loss(a, row, lse);
+    if (blockIdx.y == 0 && tid == 0) a.sums[a.first_sum + row] = write_loss(a, row, lse);
 
     const long long label = a.labels[row];
     bool bad;
