@@ -161,7 +161,7 @@ psgd_status launch_products(int count, const Operand (&A)[2], const Operand (&B)
     if (!launch_after(k_tile<EPI_STORE>, dim3(2 * n), dim3(TG_THREADS), tile_smem_bytes(), st, early, m[0], m[1], m[2], m[3], a)) return PSGD_E_CUDA;
     const int joins = (p[0].S > 1 ? p[0].tail : 0) + (count == 2 && p[1].S > 1 ? p[1].tail : 0);
     const int wide = std::max(p[0].bn, count == 2 ? p[1].bn : 0);
-    if (joins && !launch_after(k_join, dim3(joins, wide / 32, 2), dim3(128), 0, st, true, a)) return PSGD_E_CUDA;
+    if (joins && !launch_after(k_join, dim3(joins, wide / 32, TG_BM / 32), dim3(128), 0, st, true, a)) return PSGD_E_CUDA;
     return PSGD_OK;
 }
 
@@ -299,12 +299,12 @@ psgd_status xent(const void* H, int64_t ldh, const void* W, int64_t ldw, const i
         pw.part = ph.part + part_bytes(p[0]) / 4;
         ph.out = (char*)dH + (size_t)t0 * lddh * 2;
         ph.ldo = lddh;
-        ph.vec = ((uintptr_t)ph.out & 7) == 0 && lddh % 4 == 0;
+        ph.vec = aligned16(ph.out) && lddh % 8 == 0;
         float* acc = (float*)(w + x.acc);
         pw.addend = first ? nullptr : acc;
         if (last) {
             pw.out = dW; pw.ldo = lddw;
-            pw.vec = ((uintptr_t)dW & 7) == 0 && lddw % 4 == 0 && (first || D % 4 == 0);
+            pw.vec = aligned16(dW) && lddw % 8 == 0 && (first || D % 4 == 0);
         } else {
             pw.out = acc; pw.ldo = D; pw.out_f32 = 1; pw.scale = nullptr;
             pw.vec = D % 4 == 0;
@@ -442,7 +442,7 @@ psgd_status psgd_act_wgrad(const void* dY, int64_t lddy, const int8_t* q, const 
     a.status = status ? status : (int*)w;
     TileProblem& t = a.p[0];
     t.out = dW; t.ldo = lddw; t.out_f32 = dtype == PSGD_DT_F32;
-    t.vec = ((uintptr_t)dW & (t.out_f32 ? 15 : 7)) == 0 && lddw % 4 == 0;
+    t.vec = aligned16(dW) && lddw % (t.out_f32 ? 4 : 8) == 0;
     t.kacc = t.out_f32 ? KACC_F32 : 0;
     t.part = (float*)(w + g.part);
     const Operand A[2] = {{dY, lddy, true}, {}}, B[2] = {{w + g.x, g.ldx, true}, {}};

@@ -12,7 +12,8 @@
 // and 64 of k 32 KB are fetched for 128 x 256 x 64 products: half of what two separate 128 x 256 tiles would fetch.  The grid is
 // persistent (one pair per two multiprocessors).  Roles: one thread issues the TMA loads into a six-stage ring, one
 // thread of the even CTA issues the MMAs, eight warps of each CTA work on the accumulators, of which tensor memory
-// holds two (512 columns), so that the epilogue of a unit runs beside the MMAs of the next.
+// holds two (512 columns), so that the epilogue of a unit runs beside the MMAs of the next.  (Sixteen warps leave 96 registers a
+// thread: the softmax epilogue then spills, 127 -> 160 us on 4096 x 32000 x 768.)
 //
 // Whole waves of tiles run with all of k; the tiles of the last, partly filled wave are split over k so that every pair has
 // work.  Their partial sums go to the workspace and k_join adds them in the order of k (a fixed order, no atomics; letting
@@ -33,9 +34,9 @@ constexpr int TG_HALF_BYTES = 128 * TG_BK * 2;          // one operand of one st
 constexpr int TG_STAGE_BYTES = 2 * TG_HALF_BYTES;
 constexpr int TG_EPI_WARPS = 8;
 constexpr int TG_THREADS = 64 + 32 * TG_EPI_WARPS;      // warp 0: TMA, warp 1: MMA and tensor-memory owner, warps 2-9: epilogue
-constexpr int TG_STAGING = 4096;              // per epilogue warp: a block turned from row-per-lane to row-contiguous
+constexpr int TG_STAGING = 4096;              // per epilogue warp: 32 rows of 128 bytes, turned from row-per-lane to row-contiguous
 constexpr int TG_PART = TG_BM * TG_BN;        // floats of one partial tile
-constexpr int XE_SEG_LOSS = 128, XE_SEG = 64; // columns per softmax statistic: loss only, and where exponents are kept relative to its maximum
+constexpr int XE_SEG = 64, XE_SEG_LOSS = 128; // columns per softmax statistic: where exponents are kept relative to its maximum, and loss only
 
 inline size_t tile_smem_bytes() { return (size_t)TG_STAGES * TG_STAGE_BYTES + TG_EPI_WARPS * TG_STAGING + 1024 + 256; }
 
@@ -66,7 +67,7 @@ struct TileProblem {
     // EPI_STORE: out = scale * (sum + addend)
     void* out;
     long long ldo;             // elements
-    int out_f32, vec;          // vec: `out` (and its rows) aligned for 4 elements per store
+    int out_f32, vec;          // vec: every row of `out` (and of `addend`) 16-byte aligned
     const float* addend;       // [M][N] float32 or nullptr
     const float* scale;        // DEVICE scalar or nullptr
     float* part;               // partial tiles [S][tail][2][256 columns][128 rows]
@@ -214,49 +215,73 @@ __device__ __forceinline__ bool tile_unit(const TileArgs& a, int j, TileUnit& w)
     return true;
 }
 
-// A 32 x 32 block of C, a row per lane -> rows of 128 bytes through the warp's staging buffer -> out (+ addend, * scale).
+// Half a staging buffer holds 32 rows of four 16-byte units; unit j of row r lies where neither side meets a bank twice.
+__device__ __forceinline__ int staged(int r, int j) { return r * 4 + (j ^ ((r >> 1) & 3)); }
+
+// A 32 x 32 block of C, a row per lane -> rows of 64 bytes through the warp's staging buffer -> out (+ addend, * scale).
 // Row-per-lane stores would touch 32 lines per instruction.
-__device__ __forceinline__ void emit_block(const TileProblem& a, float4* xb, const float (&v)[32], int row0, int col0, const float* addend, long long lda, float scale) {
-    const int lane = threadIdx.x & 31, lrow = lane >> 3, lch = lane & 7;        // row within a group of 4, 16-byte unit
+__device__ __forceinline__ void emit_block(const TileProblem& a, uint4* xb, float (&v)[32], int row0, int col0, const float* addend, long long lda, float scale) {
+    const int lane = threadIdx.x & 31, lrow = lane >> 2, lch = lane & 3;        // row-contiguous phase: row within a group of 8, unit
+    if (!a.out_f32 && !addend && a.vec && col0 + 32 <= a.N) {                   // 32 columns of bfloat16
 #pragma unroll
-    for (int j = 0; j < 8; ++j) xb[lane * 8 + (j ^ (lane & 7))] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-    if (a.vec && col0 + 32 <= a.N) {
-        const int col = col0 + 4 * lch;
-        float4 y[8];
-        if (addend) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int row = row0 + 4 * i + lrow;
-                if (row < a.M) y[i] = *reinterpret_cast<const float4*>(addend + (size_t)row * lda + col);
-            }
-        }
+        for (int j = 0; j < 4; ++j)
+            xb[staged(lane, j)] = make_uint4(pack_bf16(v[8 * j] * scale, v[8 * j + 1] * scale), pack_bf16(v[8 * j + 2] * scale, v[8 * j + 3] * scale),
+                                             pack_bf16(v[8 * j + 4] * scale, v[8 * j + 5] * scale), pack_bf16(v[8 * j + 6] * scale, v[8 * j + 7] * scale));
         __syncwarp();
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int br = 4 * i + lrow, row = row0 + br;
-            float4 x = xb[br * 8 + (lch ^ (br & 7))];
-            if (row < a.M) {
-                if (addend) { x.x += y[i].x; x.y += y[i].y; x.z += y[i].z; x.w += y[i].w; }
-                x.x *= scale; x.y *= scale; x.z *= scale; x.w *= scale;
-                if (a.out_f32) *reinterpret_cast<float4*>((float*)a.out + (size_t)row * a.ldo + col) = x;
-                else *reinterpret_cast<uint2*>((__nv_bfloat16*)a.out + (size_t)row * a.ldo + col) = make_uint2(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w));
-            }
+        for (int i = 0; i < 4; ++i) {
+            const int br = 8 * i + lrow;
+            if (row0 + br < a.M) *reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + (size_t)(row0 + br) * a.ldo + col0 + 8 * lch) = xb[staged(br, lch)];
         }
-    } else {                                          // the last columns, or rows without alignment: a column per lane
-        const float* xf = reinterpret_cast<const float*>(xb);
-        const int col = col0 + lane;
         __syncwarp();
-#pragma unroll 8
-        for (int br = 0; br < 32; ++br) {
-            const int row = row0 + br;
-            if (row < a.M && col < a.N) {
-                const float x = (xf[br * 32 + (((lane >> 2) ^ (br & 7)) << 2) + (lane & 3)] + (addend ? addend[(size_t)row * lda + col] : 0.f)) * scale;
-                if (a.out_f32) ((float*)a.out)[(size_t)row * a.ldo + col] = x;
-                else ((__nv_bfloat16*)a.out)[(size_t)row * a.ldo + col] = __float2bfloat16_rn(x);
-            }
-        }
+        return;
     }
-    __syncwarp();
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {                                               // 16 columns of float32 at a time
+        const int col1 = col0 + 16 * h;
+        if (col1 >= a.N) break;
+        const bool wide = a.vec && col1 + 16 <= a.N;
+        float4 y[4];
+        if (addend && wide) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int row = row0 + 8 * i + lrow;
+                if (row < a.M) y[i] = *reinterpret_cast<const float4*>(addend + (size_t)row * lda + col1 + 4 * lch);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            xb[staged(lane, j)] = make_uint4(__float_as_uint(v[16 * h + 4 * j]), __float_as_uint(v[16 * h + 4 * j + 1]), __float_as_uint(v[16 * h + 4 * j + 2]),
+                                             __float_as_uint(v[16 * h + 4 * j + 3]));
+        __syncwarp();
+        if (wide) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int br = 8 * i + lrow, row = row0 + br;
+                const uint4 u = xb[staged(br, lch)];
+                float4 x = make_float4(__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w));
+                if (row < a.M) {
+                    if (addend) { x.x += y[i].x; x.y += y[i].y; x.z += y[i].z; x.w += y[i].w; }
+                    x.x *= scale; x.y *= scale; x.z *= scale; x.w *= scale;
+                    if (a.out_f32) *reinterpret_cast<float4*>((float*)a.out + (size_t)row * a.ldo + col1 + 4 * lch) = x;
+                    else *reinterpret_cast<uint2*>((__nv_bfloat16*)a.out + (size_t)row * a.ldo + col1 + 4 * lch) = make_uint2(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w));
+                }
+            }
+        } else {                                      // the last columns, or rows without alignment: a column per lane, two rows
+            const float* xf = reinterpret_cast<const float*>(xb);
+            const int cl = lane & 15, col = col1 + cl;
+#pragma unroll 4
+            for (int i = 0; i < 16; ++i) {
+                const int br = 2 * i + (lane >> 4), row = row0 + br;
+                if (row < a.M && col < a.N) {
+                    const float x = (xf[staged(br, cl >> 2) * 4 + (cl & 3)] + (addend ? addend[(size_t)row * lda + col] : 0.f)) * scale;
+                    if (a.out_f32) ((float*)a.out)[(size_t)row * a.ldo + col] = x;
+                    else ((__nv_bfloat16*)a.out)[(size_t)row * a.ldo + col] = __float2bfloat16_rn(x);
+                }
+            }
+        }
+        __syncwarp();
+    }
 }
 
 // Dependent launches: a kernel of a call's chain may start while the one before it still runs; `grid_wait` returns when that one has
@@ -416,11 +441,11 @@ k_tile(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtenso
             if (lane == 0) *a.norm = z != 0.0 ? (float)(1.0 / z) : 0.f;
         }
     } else {
-        // ---- epilogue ----
+        // ---- epilogue: two warps per quarter of the rows, which share the columns ----
         const int quarter = warp & 3;                          // the tensor-memory lanes this warp may read
-        const int half = (warp - 2) >> 2;                      // columns half * bn / 2 ...
+        const int share = (warp - 2) >> 2;
         const unsigned lane_base = tmem + ((unsigned)(quarter * 32) << 16);
-        float4* xb = reinterpret_cast<float4*>(staging + (size_t)(warp - 2) * TG_STAGING);
+        uint4* xb = reinterpret_cast<uint4*>(staging + (size_t)(warp - 2) * TG_STAGING);
         const unsigned acce0 = cluster_addr(bar_acce, 0);
         int it = 0;
         if (EPI == EPI_STORE) {
@@ -428,21 +453,21 @@ k_tile(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtenso
             for (int j = 0; tile_unit(a, j, w); ++j) {
                 const TileProblem& p = a.p[w.which];
                 const float scale = p.scale ? __ldg(p.scale) : 1.f;
-                const int hn = p.bn >> 1;
-                const int row0 = w.m0 + rank * 128 + quarter * 32, col_base = w.n0 + half * hn;
-                const int chunks = row0 < p.M ? min(hn / 32, max(0, (p.N - col_base + 31) / 32)) : 0;      // blocks of 32 columns that exist
+                const int row0 = w.m0 + rank * 128 + quarter * 32;
+                const int chunks = row0 < p.M ? (min(p.bn, p.N - w.n0) + 31) / 32 : 0;      // blocks of 32 columns that exist
                 // partial tiles: lanes of a warp (rows) side by side
-                float* part = w.piece >= 0 ? p.part + ((size_t)w.piece * 2 + rank) * (TG_PART / 2) + (size_t)(half * hn) * 128 + quarter * 32 + lane : nullptr;
+                float* part = w.piece >= 0 ? p.part + ((size_t)w.piece * 2 + rank) * (TG_PART / 2) + quarter * 32 + lane : nullptr;
                 for (int k0 = w.kb0; k0 < w.kb1; ++it) {
                     const int k1 = p.kacc > 0 ? min(w.kb1, k0 + p.kacc) : w.kb1;
                     mbar_wait_warp(bar_accf + 8 * (it & 1), (unsigned)((it >> 1) & 1), a.status, dead);
                     asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+                    if (share >= chunks && lane == 0) mbar_arrive_cluster(acce0 + 8 * (it & 1));
 #pragma unroll 1
-                    for (int c = 0; c < chunks; ++c) {
+                    for (int c = share; c < chunks; c += TG_EPI_WARPS / 4) {
                         float v[32];
-                        tmem_ld32(lane_base + (unsigned)((it & 1) * TG_BN + half * hn + 32 * c), v);
+                        tmem_ld32(lane_base + (unsigned)((it & 1) * TG_BN + 32 * c), v);
                         tmem_wait(v);
-                        if (c == chunks - 1) {                 // the last read: the accumulator is free
+                        if (c + TG_EPI_WARPS / 4 >= chunks) {  // this warp's last read: the accumulator is free
                             asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
                             __syncwarp();
                             if (lane == 0) mbar_arrive_cluster(acce0 + 8 * (it & 1));
@@ -457,10 +482,9 @@ k_tile(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtenso
 #pragma unroll
                             for (int i = 0; i < 32; ++i) q[i * 128] = v[i];
                         } else {
-                            emit_block(p, xb, v, row0, col_base + 32 * c, more ? (const float*)p.out : p.addend, more ? p.ldo : (long long)p.N, scale);
+                            emit_block(p, xb, v, row0, w.n0 + 32 * c, more ? (const float*)p.out : p.addend, more ? p.ldo : (long long)p.N, scale);
                         }
                     }
-                    if (chunks == 0 && lane == 0) mbar_arrive_cluster(acce0 + 8 * (it & 1));
                     k0 = k1;
                 }
             }
@@ -468,9 +492,7 @@ k_tile(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtenso
             // ---- softmax statistics of this warp's 128 columns, and the exponents in 16 bits ----
             // 64 columns at a time, each read from tensor memory once: those reads take the MMAs' bandwidth to it (two passes, maximum first,
             // cost 900 of the 9400 cycles of a 256 x 256 x 768 tile)
-            constexpr int CH = 64;
-            constexpr int SEG = EPI == EPI_LOSS ? XE_SEG_LOSS : XE_SEG;
-            const int lrow = lane >> 3, lch = lane & 7;
+            const int lrow = lane >> 3, lch = lane & 7;        // row-contiguous phase: row within a group of 4, 16-byte unit
             const TileProblem& p = a.p[0];
             auto label_of = [&](const TileUnit& w) {           // the row's label, -1 where there is no row
                 const int row = w.m0 + rank * 128 + quarter * 32 + lane;
@@ -481,47 +503,47 @@ k_tile(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtenso
             long long next_label = going ? label_of(next) : -1ll;
             for (; going; ++it) {
                 const TileUnit w = next;
-                const int row0 = w.m0 + rank * 128 + quarter * 32, col_base = w.n0 + half * 128, row = row0 + lane;
+                const int row0 = w.m0 + rank * 128 + quarter * 32, col_base = w.n0 + share * 128, row = row0 + lane;
                 const int b = it & 1;
                 const int label_col = (int)min(max(next_label - (long long)col_base, -1ll), 128ll);   // among this warp's columns
                 going = tile_unit(a, it + 1, next);
                 if (going) next_label = label_of(next);        // asked for a tile ahead
                 mbar_wait_warp(bar_accf + 8 * b, (unsigned)((it >> 1) & 1), a.status, dead);
                 asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
-                const unsigned taddr = lane_base + (unsigned)(b * TG_BN + half * 128);
+                const unsigned taddr = lane_base + (unsigned)(b * TG_BN + share * 128);
                 const int ncols = row0 < p.M ? min(128, p.N - col_base) : 0;       // (<= 0: none of these columns exists, or none of the rows)
-                float top = -INFINITY, sum = 0.f;
+                float last_top = -INFINITY, last_sum = 0.f;    // EPI_LOSS: of the first 64 columns
 #pragma unroll
-                for (int c = 0; c < 128 / CH; ++c) {
-                    const int left = ncols - CH * c;
+                for (int c = 0; c < 128 / XE_SEG; ++c) {
+                    const int left = ncols - XE_SEG * c;
                     if (left <= 0) break;
                     float v[2][32];
-                    tmem_ld32(taddr + CH * c, v[0]);
-                    tmem_ld32(taddr + CH * c + 32, v[1]);
+                    tmem_ld32(taddr + XE_SEG * c, v[0]);
+                    tmem_ld32(taddr + XE_SEG * c + 32, v[1]);
                     tmem_wait(v[0]);
                     tmem_wait(v[1]);
-                    if (left <= CH || c == 128 / CH - 1) {                         // the last read: the accumulator is free
+                    if (left <= XE_SEG || c == 128 / XE_SEG - 1) {                 // the last read: the accumulator is free
                         asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
                         __syncwarp();
                         if (lane == 0) mbar_arrive_cluster(acce0 + 8 * b);
                     }
-                    if (left < CH) {
+                    if (left < XE_SEG) {
 #pragma unroll
-                        for (int j = 0; j < CH; ++j) if (j >= left) v[j >> 5][j & 31] = -INFINITY;
+                        for (int j = 0; j < XE_SEG; ++j) if (j >= left) v[j >> 5][j & 31] = -INFINITY;
                     }
                     if (__any_sync(0xffffffffu, (label_col >> 6) == c)) {
 #pragma unroll
-                        for (int j = 0; j < CH; ++j) if (label_col == CH * c + j) a.label_logit[row] = v[j >> 5][j & 31];
+                        for (int j = 0; j < XE_SEG; ++j) if (label_col == XE_SEG * c + j) a.label_logit[row] = v[j >> 5][j & 31];
                     }
-                    float t[4] = {EPI == EPI_LOSS ? top : -INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                    float t[4] = {EPI == EPI_LOSS ? last_top : -INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                    for (int j = 0; j < CH; ++j) t[j & 3] = fmaxf(t[j & 3], v[j >> 5][j & 31]);
-                    const float m = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
-                    const float ref = m == -INFINITY ? 0.f : m;                    // nothing but -inf: exp(-inf - 0) = 0
-                    float part[4] = {EPI == EPI_LOSS ? sum * ex2((top - ref) * LOG2E) : 0.f, 0.f, 0.f, 0.f};
-                    unsigned pk[CH / 2];
+                    for (int j = 0; j < XE_SEG; ++j) t[j & 3] = fmaxf(t[j & 3], v[j >> 5][j & 31]);
+                    const float top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
+                    const float ref = top == -INFINITY ? 0.f : top;                // nothing but -inf: exp(-inf - 0) = 0
+                    float part[4] = {EPI == EPI_LOSS ? last_sum * ex2((last_top - ref) * LOG2E) : 0.f, 0.f, 0.f, 0.f};
+                    unsigned pk[XE_SEG / 2];
 #pragma unroll
-                    for (int j = 0; j < CH; j += 2) {
+                    for (int j = 0; j < XE_SEG; j += 2) {
                         const float t0 = (v[j >> 5][j & 31] - ref) * LOG2E, t1 = (v[j >> 5][(j & 31) + 1] - ref) * LOG2E;     // <= 0
                         part[j & 2] += ex2(t0);
                         part[(j & 2) + 1] += ex2(t1);
@@ -531,24 +553,25 @@ k_tile(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtenso
                             pk[j / 2] = __byte_perm(__float_as_uint(q0), __float_as_uint(q1), 0x5410);
                         }
                     }
-                    top = m;
-                    sum = (part[0] + part[1]) + (part[2] + part[3]);
-                    if (EPI == EPI_SOFTMAX) {
-                        if (row < p.M) a.stats[(size_t)row * a.nseg + (col_base + CH * c) / SEG] = make_float2(top, sum);
-                        uint4* xq = reinterpret_cast<uint4*>(xb);
+                    const float sum = (part[0] + part[1]) + (part[2] + part[3]);
+                    if (EPI == EPI_LOSS) {
+                        last_top = top;
+                        last_sum = sum;
+                    } else {
+                        if (row < p.M) a.stats[(size_t)row * a.nseg + (col_base + XE_SEG * c) / XE_SEG] = make_float2(top, sum);
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) xq[lane * 8 + (j ^ (lane & 7))] = make_uint4(pk[4 * j], pk[4 * j + 1], pk[4 * j + 2], pk[4 * j + 3]);
+                        for (int j = 0; j < 8; ++j) xb[lane * 8 + (j ^ (lane & 7))] = make_uint4(pk[4 * j], pk[4 * j + 1], pk[4 * j + 2], pk[4 * j + 3]);
                         __syncwarp();
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
                             const int br = 4 * i + lrow;
                             if (row0 + br < p.M)               // rows of q are padded to whole segments
-                                *reinterpret_cast<uint4*>(a.q + (size_t)(row0 + br) * a.ldq + col_base + CH * c + 8 * lch) = xq[br * 8 + (lch ^ (br & 7))];
+                                *reinterpret_cast<uint4*>(a.q + (size_t)(row0 + br) * a.ldq + col_base + XE_SEG * c + 8 * lch) = xb[br * 8 + (lch ^ (br & 7))];
                         }
                         __syncwarp();
                     }
                 }
-                if (EPI == EPI_LOSS && ncols > 0 && row < p.M) a.stats[(size_t)row * a.nseg + col_base / SEG] = make_float2(top, sum);
+                if (EPI == EPI_LOSS && ncols > 0 && row < p.M) a.stats[(size_t)row * a.nseg + col_base / XE_SEG_LOSS] = make_float2(last_top, last_sum);
                 if (ncols <= 0 && lane == 0) mbar_arrive_cluster(acce0 + 8 * b);
             }
         }
@@ -563,9 +586,10 @@ k_tile(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtenso
     }
 }
 
-// Adds the pieces of the split tiles of both products: blockIdx.x = tail tile, .y = 32 columns of it, .z = half of its rows; a warp per 32 rows.
+// Adds the pieces of the split tiles of both products: blockIdx.x = tail tile, .y = 32 columns of it, .z = 32 rows.  Each of four warps adds 8 of the
+// columns, a row per lane, eight pieces under way at a time; each then writes 8 of the rows.
 __global__ void __launch_bounds__(128) k_join(const __grid_constant__ TileArgs a) {
-    __shared__ float4 xb[4][TG_STAGING / 16];
+    __shared__ float xs[32][33];
     grid_trigger();
     grid_wait();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -574,18 +598,31 @@ __global__ void __launch_bounds__(128) k_join(const __grid_constant__ TileArgs a
     const TileProblem& p = a.p[which];
     int m0, n0;
     tile_origin(p, p.full + tile, m0, n0);
-    const int c = 32 * blockIdx.y, row0 = m0 + blockIdx.z * 128 + warp * 32;
-    if (c >= p.bn || n0 + c >= p.N || row0 >= p.M) return;
-    const float* q = p.part + ((size_t)tile * 2 + blockIdx.z) * (TG_PART / 2) + (size_t)c * 128 + warp * 32 + lane;
+    const int c0 = 32 * blockIdx.y, row0 = m0 + blockIdx.z * 32;
+    if (c0 >= p.bn || n0 + c0 >= p.N || row0 >= p.M) return;
+    const float* q = p.part + ((size_t)tile * 2 + (blockIdx.z >> 2)) * (TG_PART / 2) + (size_t)(c0 + 8 * warp) * 128 + (blockIdx.z & 3) * 32 + lane;
     const size_t step = (size_t)p.tail * TG_PART;
-    float v[32];
+    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (n0 + c0 + 8 * warp < p.N) {
+#pragma unroll 8
+        for (int s = 0; s < p.S; ++s)
 #pragma unroll
-    for (int j = 0; j < 32; ++j) v[j] = q[(size_t)j * 128];
-#pragma unroll 2
-    for (int s = 1; s < p.S; ++s)
+            for (int j = 0; j < 8; ++j) v[j] += q[(size_t)s * step + j * 128];
+    }
 #pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] += q[(size_t)s * step + (size_t)j * 128];
-    emit_block(p, xb[warp], v, row0, n0 + c, p.addend, p.N, p.scale ? __ldg(p.scale) : 1.f);
+    for (int j = 0; j < 8; ++j) xs[lane][8 * warp + j] = v[j];
+    __syncthreads();
+    const float scale = p.scale ? __ldg(p.scale) : 1.f;
+    const int col = n0 + c0 + lane;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int row = row0 + 8 * warp + i;
+        if (row < p.M && col < p.N) {
+            const float x = (xs[8 * warp + i][lane] + (p.addend ? p.addend[(size_t)row * p.N + col] : 0.f)) * scale;
+            if (p.out_f32) ((float*)p.out)[(size_t)row * p.ldo + col] = x;
+            else ((__nv_bfloat16*)p.out)[(size_t)row * p.ldo + col] = __float2bfloat16_rn(x);
+        }
+    }
 }
 
 }  // namespace psgd

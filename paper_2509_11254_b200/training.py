@@ -175,28 +175,30 @@ def linear_cross_entropy_grad(hidden, weight, labels, token_weight=None, ignore_
 class ActivationCheckpoint:
     """A matrix [T, F] kept in 8 bits: `q` [T, 32 G] int8 and one power-of-two scale byte per row and group of 32 values, `scales` [T, G]."""
 
-    __slots__ = ("shape", "device", "groups", "_buf", "_q", "_s")
+    __slots__ = ("shape", "device", "groups", "_buf", "_at", "_q", "_s")
 
-    def __init__(self, T, F, device):
+    def __init__(self, T, F, device, buf=None, at=0):
+        """`buf`, `at`: bytes to live in and where they start (a multiple of 32), for several checkpoints in one allocation."""
         G = -(-F // GROUP)
-        self.shape, self.groups, self.device = (T, F), G, device
-        self._buf = _empty(T * G * (GROUP + 1), dtype=torch.uint8, device=device)     # q, then scales
-        self._q = self._buf.data_ptr()
+        self.shape, self.groups, self.device, self._at = (T, F), G, device, at
+        self._buf = buf if buf is not None else _empty(T * G * (GROUP + 1), dtype=torch.uint8, device=device)     # q, then scales
+        self._q = self._buf.data_ptr() + at
         self._s = self._q + T * G * GROUP
 
     @property
     def q(self):
         T, G = self.shape[0], self.groups
-        return self._buf[:T * G * GROUP].view(torch.int8).view(T, G * GROUP)
+        return self._buf[self._at:self._at + T * G * GROUP].view(torch.int8).view(T, G * GROUP)
 
     @property
     def scales(self):
         T, G = self.shape[0], self.groups
-        return self._buf[T * G * GROUP:].view(T, G)
+        at = self._at + T * G * GROUP
+        return self._buf[at:at + T * G].view(T, G)
 
     @property
     def nbytes(self):
-        return self._buf.numel()
+        return self.shape[0] * self.groups * (GROUP + 1)
 
     def unpack(self, dtype=_BF16, out=None, stream=None):
         """The values that the checkpoint stands for (exact in either type), [T, F]."""
@@ -262,7 +264,9 @@ def swiglu_forward(gate, up, stream=None):
     ldu = _matrix(up, "up", shape=(T, F), device=dev)[2]
     with _on(dev, stream) as s:
         h = _empty((T, F), dtype=_BF16, device=dev)
-        kg, ku = ActivationCheckpoint(T, F, dev), ActivationCheckpoint(T, F, dev)
+        size = -(-T * -(-F // GROUP) * (GROUP + 1) // 256) * 256
+        kg = ActivationCheckpoint(T, F, dev, _empty(2 * size, dtype=torch.uint8, device=dev))      # they are kept and used together
+        ku = ActivationCheckpoint(T, F, dev, kg._buf, size)
         _check(lib().psgd_swiglu_forward(gate.data_ptr(), ldg, up.data_ptr(), ldu, T, F, h.data_ptr(), F, kg._q, kg._s, ku._q, ku._s, s))
     return h, kg, ku
 
