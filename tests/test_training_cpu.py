@@ -1,0 +1,83 @@
+"""Host-only checks of the training operators: what their workspaces come to, and what they refuse, without touching a GPU."""
+import ctypes as C
+
+import pytest
+
+
+@pytest.fixture(scope="module")
+def L():
+    from paper_2509_11254_b200 import binding, build
+
+    build.build_library()
+    return binding.lib()
+
+
+def size(L, call, *args):
+    n = C.c_size_t(1 << 62)
+    assert getattr(L, call)(*args, C.byref(n)) == 0
+    return n.value
+
+
+def test_loss_workspace_holds_no_logits(L):
+    for T, V in ((1, 32000), (777, 50257), (16384, 131072)):
+        # 8 bytes per 128 logits (statistics), 4 + 2 bytes per token and alignment
+        assert size(L, "psgd_xent_workspace", T, V, 768, 0) <= T * (8 * (V // 128 + 1) + 16) + 4096
+
+
+def test_gradient_workspace_is_bounded_in_tokens(L):
+    """16 bits per logit of at most 2^29 logits at a time, statistics (1/8 byte per logit), float32 sums of the weight gradient once there
+    are several pieces, and partial tiles of products that are cut along their contraction."""
+    V, D = 131072, 1024
+    one = size(L, "psgd_xent_workspace", 4096, V, D, 1)
+    many = [size(L, "psgd_xent_workspace", T, V, D, 1) for T in (8192, 65536, 1 << 20)]
+    tiles = 4096 * 65536 * 4          # generous: partial tiles of both products
+    for T, n in zip((8192, 65536, 1 << 20), many):
+        assert n <= (1 << 29) * 17 // 8 + V * D * 4 + T * 16 + tiles + (1 << 20)
+    assert one <= 4096 * (V * 17 // 8) + 4096 * 16 + tiles + (1 << 20)
+    assert many[2] - many[1] <= ((1 << 20) - 65536) * 16 + tiles      # growing with tokens only by the loss's per-row terms
+    # a small vocabulary needs no pieces for a long time
+    assert size(L, "psgd_xent_workspace", 1 << 17, 1000, 64, 1) < 1 << 30
+
+
+def test_weight_gradient_workspace(L):
+    # a bfloat16 form of the checkpoint and partial tiles
+    assert size(L, "psgd_act_wgrad_workspace", 4096, 2048, 768) <= 4096 * 768 * 2 + 256 * 65536 * 4 + 4096
+    assert size(L, "psgd_act_wgrad_workspace", 0, 2048, 768) > 0
+
+
+def test_queries_refuse(L):
+    n = C.c_size_t()
+    for bad in ((-1, 10, 10), (10, 0, 10), (10, 10, 0), (1 << 31, 10, 10), (10, 1 << 31, 10), (10, 10, 1 << 31)):
+        assert L.psgd_xent_workspace(*bad, 1, C.byref(n)) == -1
+        assert L.psgd_act_wgrad_workspace(bad[0], bad[1], bad[2], C.byref(n)) == -1
+    assert L.psgd_xent_workspace(8, 8, 8, 1, None) == -2 and L.psgd_act_wgrad_workspace(8, 8, 8, None) == -2
+
+
+def test_calls_refuse_before_any_launch(L):
+    p = 1 << 20          # stands for device addresses; nothing below gets as far as using one
+    xent = lambda T=8, V=16, D=64, H=p, ldh=64, W=p, ldw=64, lab=p, loss=p, ws=p, nb=1 << 40: L.psgd_xent_loss(
+        H, ldh, W, ldw, lab, None, -100, T, V, D, loss, p, p, None, ws, nb, None)
+    assert xent(H=None) == -2 and xent(W=None) == -2 and xent(lab=None) == -2 and xent(loss=None) == -2 and xent(ws=None) == -2
+    assert xent(H=p + 8) == -1 and xent(W=p + 2) == -1 and xent(ldh=63) == -1 and xent(ldw=65) == -1 and xent(ws=p + 8) == -1
+    assert xent(T=-1) == -1 and xent(V=0) == -1 and xent(D=0) == -1 and xent(nb=0) == -3
+    assert L.psgd_act_pack(p, 64, 1, -1, 64, p, p, None) == -1 and L.psgd_act_pack(p, 64, 1, 8, 0, p, p, None) == -1
+    assert L.psgd_act_pack(p, 64, 7, 8, 64, p, p, None) == -1 and L.psgd_act_pack(p, 64, 1, 8, 64, p, None, None) == -2
+    assert L.psgd_act_pack(p, 64, 1, 0, 64, None, None, None) == 0
+    assert L.psgd_act_unpack(p + 4, p, 8, 64, p, 64, 0, None) == -1 and L.psgd_act_unpack(p, p, 8, 64, p, 63, 0, None) == -1
+    assert L.psgd_act_wgrad(p, 16, p, p, 8, 16, 64, p, 63, 0, None, p, 1 << 40, None) == -1
+    assert L.psgd_act_wgrad(p, 16, p, p, 8, 16, 64, p, 64, 0, None, p, 0, None) == -3
+    assert L.psgd_act_wgrad(p + 8, 16, p, p, 8, 16, 64, p, 64, 0, None, p, 1 << 40, None) == -1
+    assert L.psgd_swiglu_forward(p, 64, p, 64, 8, 64, p, 63, p, p, p, p, None) == -1 and L.psgd_swiglu_forward(p, 64, None, 64, 8, 64, p, 64, p, p, p, p, None) == -2
+    assert L.psgd_swiglu_backward(p, 64, p, p, p, p, 8, 64, p, 64, p, 64, p, 10, None) == -1
+
+
+def test_python_refuses_host_tensors():
+    import torch
+
+    import paper_2509_11254_b200 as p
+
+    h, w, y = torch.zeros(4, 8, dtype=torch.bfloat16), torch.zeros(5, 8, dtype=torch.bfloat16), torch.zeros(4, dtype=torch.int64)
+    for call in (lambda: p.linear_cross_entropy(h, w, y), lambda: p.linear_cross_entropy_grad(h, w, y), lambda: p.pack_activation(h), lambda: p.swiglu_forward(h, h),
+                 lambda: p.weight_gradient(h, None), lambda: p.swiglu_backward(h, None, None)):
+        with pytest.raises(p.PSGDError):
+            call()

@@ -137,6 +137,42 @@ def test_xent_in_pieces(torch, ops):
     assert torch.equal(a.d_weight, b.d_weight) and torch.equal(a.d_hidden, b.d_hidden) and torch.equal(a.loss, b.loss)
 
 
+@pytest.mark.parametrize("T,V,D,weighted", [(4500, 131072 - 5, 40, True), (5000, 131072, 36, False), (9000, 131072, 8, False)])
+def test_xent_in_pieces_of_many_tokens(torch, ops, T, V, D, weighted):
+    """Two and three pieces; widths whose rows are and are not 16-byte aligned."""
+    h, w, labels = xent_inputs(torch, T, V, D, seed=13)
+    tw = torch.rand(T, generator=gen(torch, 6), device="cuda") if weighted else None
+    r = ops.linear_cross_entropy_grad(h, w, labels, token_weight=tw)
+    step = 1500                       # the reference in 64 bits, by tokens
+    dw = torch.zeros(V, D, dtype=torch.float64, device="cuda")
+    dw_size = torch.zeros_like(dw)
+    valid = labels >= 0
+    wt = valid.double() * (1.0 if tw is None else tw.double())
+    wt = wt / wt.sum()
+    loss = 0.0
+    for a in range(0, T, step):
+        s = slice(a, min(T, a + step))
+        ref = xent_reference(torch, h[s], w, labels[s], None, -100)
+        mine = valid[s].double().sum()
+        scale = wt[s] * mine / valid[s].double().clamp(min=1)           # undo the reference's own mean over this range
+        l_err = sum_bound(D) * ref["size"] + 2.0 ** -18
+        within(r.lse[s], ref["lse"], l_err + 2.0 ** -22 * ref["lse"].abs())
+        within(r.token_loss[s], ref["token"], 2 * l_err + 2.0 ** -22 * ref["lse"].abs())
+        p_err = 3.4e-4 + 2.0 ** -12 + 2 * l_err.max()
+        dl, each = ref["dl"] * scale[:, None], (BF16 * ref["dl"] + p_err * ref["mag"]) * scale[:, None]
+        within(r.d_hidden[s], ref["dh"] * scale[:, None], (each + sum_bound(V) * (dl + each)) @ ref["w"].abs() * (1 + BF16) + (BF16 + 2.0 ** -22) * (ref["dh"] * scale[:, None]).abs() + 1e-30)
+        full = torch.exp(ref["h"] @ ref["w"].T - ref["lse"][:, None])
+        rows = torch.nonzero(valid[s])[:, 0]
+        full[rows, labels[s][rows]] -= 1
+        full *= wt[s][:, None]
+        dw += full.T @ ref["h"]
+        dw_size += (each + sum_bound(T) * (dl + each)).T @ ref["h"].abs()
+        loss += float((wt[s] * ref["token"]).sum())
+        del ref, full, dl, each
+    within(r.d_weight, dw, dw_size * (1 + BF16) + (BF16 + 2.0 ** -20) * dw.abs() + 1e-30)
+    assert abs(float(r.loss) - loss) < 1e-4
+
+
 def test_xent_all_ignored_and_no_tokens(torch, ops):
     h, w, labels = xent_inputs(torch, 40, 300, 64, seed=1)
     labels[:] = 7
@@ -529,3 +565,17 @@ def test_c_entry_points_refuse(torch, ops):
     assert L.psgd_act_pack(None, 64, 1, 8, 64, ws.data_ptr(), ws.data_ptr(), None) == -2
     assert L.psgd_act_wgrad_workspace(8, 0, 64, C.byref(n)) == -1 and L.psgd_act_wgrad_workspace(8, 16, 64, None) == -2
     assert L.psgd_swiglu_backward(h.data_ptr(), 64, None, None, None, None, 8, 64, dh.data_ptr(), 64, dh.data_ptr(), 64, None, 0, None) == -2
+
+
+# ---- together -----------------------------------------------------------------------------------------------------
+def test_operators_feed_the_compressor(torch, ops):
+    """The example: two simulated nodes, 8-bit activations, compressed gradients.  The task is a fixed map of tokens, learnt within 60 steps."""
+    import importlib.util
+    import os
+
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "compressed_training.py")
+    spec = importlib.util.spec_from_file_location("compressed_training", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    losses = example.train(steps=60, log=None)
+    assert abs(losses[0] - math.log(2000)) < 0.2 and losses[-1] < 0.1 and all(math.isfinite(v) for v in losses)
