@@ -329,7 +329,7 @@ psgd_status psgd_backproject_static(const float* M /*DEVICE*/, const float* P_ha
  * 16-byte aligned pointer and, with more than one row, a row stride that is a multiple of 8 elements.  `status` (DEVICE, one int, may
  * be NULL) collects PSGD_W_* bits and is never cleared by the library.  `workspace` (DEVICE, 256-byte aligned) holds at least
  * the bytes the matching query reports, may hold anything before the call, and is free again for later work on the stream.
- * Sizes are at most 2^30 per dimension; T = 0 is allowed (loss 0, weight gradients 0).
+ * Sizes are at most 2^30 per dimension and 2^45 for a product of two; T = 0 is allowed (loss 0, weight gradients 0).
  */
 #define PSGD_DT_F32 0
 #define PSGD_DT_BF16 1

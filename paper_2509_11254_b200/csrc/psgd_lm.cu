@@ -119,7 +119,9 @@ bool launch_after(void (*kernel)(Args...), dim3 grid, dim3 block, size_t smem, c
     at.val.programmaticStreamSerializationAllowed = 1;
     c.attrs = &at;
     c.numAttrs = early ? 1 : 0;
-    return cudaLaunchKernelEx(&c, kernel, args...) == cudaSuccess;
+    if (cudaLaunchKernelEx(&c, kernel, args...) == cudaSuccess) return true;
+    cudaGetLastError();                               // not left for whoever asks next
+    return false;
 }
 
 struct Operand { const void* p; int64_t ld; bool mn; };      // mn: stored [K][rows], else [rows][K]
@@ -167,6 +169,7 @@ psgd_status launch_products(int count, const Operand (&A)[2], const Operand (&B)
 
 bool operand_ok(const void* p, int64_t rows, int64_t cols, int64_t ld) { return aligned16(p) && ld >= cols && (rows == 1 || ld % 8 == 0); }
 bool extent_ok(int64_t v) { return v >= 1 && v <= MAX_EXTENT; }
+bool tiles_ok(int64_t M, int64_t N) { return ((M + 255) / 256) * ((N + 127) / 128) <= MAX_EXTENT; }     // units are counted in 32 bits
 
 // ---- cross entropy ----
 constexpr int64_t XENT_PIECE_LOGITS = (int64_t)1 << 29;   // logits whose 16-bit form the workspace holds at a time (1 GiB; half as many: 3 to 4 % slower)
@@ -224,7 +227,7 @@ XentPlan plan_xent(int64_t T, int64_t V, int64_t D, bool grad) {
 
 psgd_status xent(const void* H, int64_t ldh, const void* W, int64_t ldw, const int64_t* labels, const float* weight, int64_t ignore, int64_t T, int64_t V, int64_t D,
                  float* loss, float* token_loss, float* lse, bool grad, void* dH, int64_t lddh, void* dW, int64_t lddw, int* status, void* ws, size_t ws_bytes, cudaStream_t st) {
-    if (T < 0 || T > MAX_EXTENT || !extent_ok(V) || !extent_ok(D)) return PSGD_E_INVALID;
+    if (T < 0 || T > MAX_EXTENT || !extent_ok(V) || !extent_ok(D) || !tiles_ok(T, V) || !tiles_ok(V, D)) return PSGD_E_INVALID;
     if (!W || !loss || !ws || (T > 0 && (!H || !labels || !token_loss || !lse)) || (grad && (!dW || (T > 0 && !dH)))) return PSGD_E_NULL;
     if (!operand_ok(W, V, D, ldw) || (T > 0 && !operand_ok(H, T, D, ldh)) || (grad && ((T > 0 && lddh < D) || lddw < D))) return PSGD_E_INVALID;
     if ((uintptr_t)ws & 255) return PSGD_E_INVALID;
@@ -372,7 +375,7 @@ extern "C" {
 
 psgd_status psgd_xent_workspace(int64_t T, int64_t V, int64_t D, int grad, size_t* bytes) {
     if (!bytes) return PSGD_E_NULL;
-    if (T < 0 || T > MAX_EXTENT || !extent_ok(V) || !extent_ok(D)) return PSGD_E_INVALID;
+    if (T < 0 || T > MAX_EXTENT || !extent_ok(V) || !extent_ok(D) || !tiles_ok(T, V) || !tiles_ok(V, D)) return PSGD_E_INVALID;
     *bytes = T == 0 ? 256 : plan_xent(T, V, D, grad != 0).total;
     return PSGD_OK;
 }
@@ -418,7 +421,7 @@ psgd_status psgd_act_unpack(const int8_t* q, const uint8_t* scales, int64_t T, i
 
 psgd_status psgd_act_wgrad_workspace(int64_t T, int64_t O, int64_t F, size_t* bytes) {
     if (!bytes) return PSGD_E_NULL;
-    if (!act_ok(T, F) || !extent_ok(O)) return PSGD_E_INVALID;
+    if (!act_ok(T, F) || !extent_ok(O) || !tiles_ok(O, F)) return PSGD_E_INVALID;
     *bytes = T == 0 ? 256 : plan_wgrad(T, O, F).total;
     return PSGD_OK;
 }
@@ -426,7 +429,7 @@ psgd_status psgd_act_wgrad_workspace(int64_t T, int64_t O, int64_t F, size_t* by
 psgd_status psgd_act_wgrad(const void* dY, int64_t lddy, const int8_t* q, const uint8_t* scales, int64_t T, int64_t O, int64_t F, void* dW, int64_t lddw, int dtype,
                            int* status, void* ws, size_t ws_bytes, psgd_stream stream) try {
     cudaStream_t st = (cudaStream_t)stream;
-    if (!act_ok(T, F) || !extent_ok(O) || !dtype_ok(dtype)) return PSGD_E_INVALID;
+    if (!act_ok(T, F) || !extent_ok(O) || !tiles_ok(O, F) || !dtype_ok(dtype)) return PSGD_E_INVALID;
     if (!dW || !ws || (T > 0 && (!dY || !q || !scales))) return PSGD_E_NULL;
     if (lddw < F || ((uintptr_t)ws & 255) || (T > 0 && (!operand_ok(dY, T, O, lddy) || !ckpt_ok(q)))) return PSGD_E_INVALID;
     if (T == 0) {

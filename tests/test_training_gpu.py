@@ -567,6 +567,81 @@ def test_c_entry_points_refuse(torch, ops):
     assert L.psgd_swiglu_backward(h.data_ptr(), 64, None, None, None, None, 8, 64, dh.data_ptr(), 64, dh.data_ptr(), 64, None, 0, None) == -2
 
 
+# ---- streams, graphs, long offsets --------------------------------------------------------------------------------
+def test_calls_on_two_streams_at_once(torch, ops):
+    sets = [xent_inputs(torch, 700, 3000, 256, seed=s) for s in (21, 22)]
+    x = [torch.randn(500, 776, generator=gen(torch, s), device="cuda").to(torch.bfloat16) for s in (23, 24)]
+
+    def work(i, stream=None):
+        r = ops.linear_cross_entropy_grad(*sets[i], stream=stream)
+        kept = ops.pack_activation(x[i], stream=stream)
+        return [*r, ops.weight_gradient(x[i][:, :520].contiguous(), kept, stream=stream)]
+
+    want = [work(0), work(1)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(5):
+        got.append([work(i, streams[i]) for i in (0, 1)])
+    torch.cuda.synchronize()
+    for both in got:
+        for a, b in zip(both, want):
+            for u, v in zip(a, b):
+                assert torch.equal(u, v)
+
+
+def test_calls_in_a_cuda_graph(torch, ops):
+    """Captured once, replayed with other inputs in the same places."""
+    h, w, labels = xent_inputs(torch, 300, 1100, 200, seed=31)
+    x = torch.randn(300, 264, generator=gen(torch, 32), device="cuda").to(torch.bfloat16)
+
+    def work():
+        r = ops.linear_cross_entropy_grad(h, w, labels)
+        loss = ops.linear_cross_entropy(h, w, labels).loss
+        y, kg, ku = ops.swiglu_forward(x, x)
+        return [*r, loss, ops.weight_gradient(r.d_hidden, ops.pack_activation(x)), *ops.swiglu_backward(y, kg, ku, recompute=True)]
+
+    work()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = work()
+    h2, w2, labels2 = xent_inputs(torch, 300, 1100, 200, seed=33)
+    h.copy_(h2), w.copy_(w2), labels.copy_(labels2), x.neg_()
+    for t in out:
+        t.fill_(7)
+    graph.replay()
+    torch.cuda.synchronize()
+    for a, b in zip(out, work()):
+        assert torch.equal(a, b)
+
+
+def test_xent_beyond_32_bit_offsets(torch, ops):
+    """A vocabulary matrix of 2.2e9 entries; the labels lie at both ends."""
+    T, V, D = 5, 540000, 4000
+    g = gen(torch, 41)
+    h = torch.randn(T, D, generator=g, device="cuda").to(torch.bfloat16)
+    w = torch.empty(V, D, dtype=torch.bfloat16, device="cuda")
+    for a in range(0, V, 60000):
+        w[a:a + 60000] = (torch.randn(60000, D, generator=g, device="cuda") / math.sqrt(D)).to(torch.bfloat16)
+    labels = torch.tensor([0, V - 1, V - 2, -100, V // 2], device="cuda")
+    r = ops.linear_cross_entropy_grad(h, w, labels)
+    z = torch.cat([h.double() @ w[a:a + 60000].double().T for a in range(0, V, 60000)], 1)
+    lse = torch.logsumexp(z, 1)
+    within(r.lse, lse, torch.full_like(lse, 1e-4))
+    p = torch.softmax(z, 1)
+    rows = torch.tensor([0, 1, 2, 4], device="cuda")
+    p[rows, labels[rows]] -= 1
+    p[3] = 0
+    p /= 4
+    for a in (0, V // 2 - 100, V - 1000):
+        ref, size = p[:, a:a + 1000].T @ h.double(), p[:, a:a + 1000].abs().T @ h.double().abs()
+        within(r.d_weight[a:a + 1000], ref, (2 * BF16 + 1e-3) * size)
+    dh = sum(p[:, a:a + 60000] @ w[a:a + 60000].double() for a in range(0, V, 60000))
+    size = sum(p[:, a:a + 60000].abs() @ w[a:a + 60000].double().abs() for a in range(0, V, 60000))
+    within(r.d_hidden, dh, (2 * BF16 + 1e-3) * size)
+
+
 # ---- together -----------------------------------------------------------------------------------------------------
 def test_operators_feed_the_compressor(torch, ops):
     """The example: two simulated nodes, 8-bit activations, compressed gradients.  The task is a fixed map of tokens, learnt within 60 steps."""
