@@ -79,6 +79,8 @@ struct TileArgs {
     int first_q, first_r, extra;
     int* status;               // device status word
     // EPI_LOSS, EPI_SOFTMAX
+    int a_rows, a_odd;         // rows of A in a box, a multiple of 8, and whether the odd CTA has any: 128 and 1, less where all of M is one short
+                               // tile.  The rows that no box brings are zeros for good (not garbage: that would cost the MMAs' power).
     const long long* labels;
     float2* stats;             // [M][nseg]: maximum and sum of exp(l - maximum) of each segment
     float* label_logit;        // [M]
@@ -322,6 +324,12 @@ k_tile(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtenso
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;\n" ::"r"(smem_u32(tmem_slot)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;\n" ::: "memory");
     }
+    const bool short_a = !BMN && (a.a_rows < 128 || !a.a_odd);
+    if (short_a) {
+        for (int i = tid; i < TG_STAGES * (TG_HALF_BYTES / 16); i += TG_THREADS)
+            *reinterpret_cast<uint4*>(base + (size_t)(i / (TG_HALF_BYTES / 16)) * TG_STAGE_BYTES + (i % (TG_HALF_BYTES / 16)) * 16) = make_uint4(0u, 0u, 0u, 0u);
+        asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+    }
     asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
     __syncthreads();
     cluster_arrive_release();
@@ -345,6 +353,7 @@ k_tile(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtenso
             const CUtensorMap* const mb = w.which ? &tmB1 : &tmB0;
             const bool amn = BMN && p.a_mn, two = p.bn > 128;
             // bytes of B per stage: K-major boxes have bn / 2 rows, MN-major ones come in blocks of 64
+            const unsigned a_bytes = BMN ? 2 * TG_HALF_BYTES : (unsigned)(a.a_rows * TG_BK * 2) << a.a_odd;       // of both CTAs
             const unsigned b_bytes = BMN ? (two ? TG_HALF_BYTES : TG_HALF_BYTES / 2) : (unsigned)p.bn / 2 * TG_BK * 2;
             const int nh = (min(p.bn, p.N - w.n0) + 31) / 32 * 16;
             const int m = w.m0 + rank * 128, n = w.n0 + rank * nh;
@@ -353,13 +362,13 @@ k_tile(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtenso
                 if (dead) break;
                 if (elect_one()) {
                     const unsigned bar = full0 + 8 * s;
-                    if (rank == 0) mbar_expect_tx(bar_full + 8 * s, 2 * (TG_HALF_BYTES + b_bytes));
+                    if (rank == 0) mbar_expect_tx(bar_full + 8 * s, a_bytes + 2 * b_bytes);
                     const unsigned da = smem_base + s * TG_STAGE_BYTES, db = da + TG_HALF_BYTES;
                     const int k = kb * TG_BK;
                     if (amn) {
                         pair_tma_2d(da, ma, m, k, bar);
                         pair_tma_2d(da + TG_HALF_BYTES / 2, ma, m + 64, k, bar);
-                    } else {
+                    } else if (BMN || rank == 0 || a.a_odd) {
                         pair_tma_2d(da, ma, k, m, bar);
                     }
                     if (BMN) {
