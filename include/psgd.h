@@ -375,6 +375,11 @@ psgd_status psgd_act_wgrad(const void* dY /*DEVICE*/, int64_t lddy, const int8_t
                            psgd_stream stream);
 
 /*
+ * Copies a matrix of 16-bit values [rows][cols] to other row strides: for operands whose rows are not 16-byte aligned.
+ */
+psgd_status psgd_copy_rows(const void* src /*DEVICE*/, int64_t lds, int64_t rows, int64_t cols, void* dst /*DEVICE*/, int64_t ldd, psgd_stream stream);
+
+/*
  * Gated unit h = silu(gate) up of a feed-forward block, all matrices [T][F] bfloat16.  The forward pass packs gate and up in the
  * same pass over them; the backward pass reads the checkpoints:  d_gate = dh up s (1 + gate (1 - s)), d_up = dh gate s,
  * s = 1 / (1 + exp(-gate)), and, where h is not NULL, h again (for the weight gradient of the layer behind the unit).

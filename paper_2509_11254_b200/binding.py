@@ -65,6 +65,7 @@ SIGNATURES = {
     "psgd_act_unpack": (_int, [_vp, _vp, _i64, _i64, _vp, _i64, _int, _vp]),
     "psgd_act_wgrad_workspace": (_int, [_i64, _i64, _i64, C.POINTER(_sz)]),
     "psgd_act_wgrad": (_int, [_vp, _i64, _vp, _vp, _i64, _i64, _i64, _vp, _i64, _int, _vp, _vp, _sz, _vp]),
+    "psgd_copy_rows": (_int, [_vp, _i64, _i64, _i64, _vp, _i64, _vp]),
     "psgd_swiglu_forward": (_int, [_vp, _i64, _vp, _i64, _i64, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp]),
     "psgd_swiglu_backward": (_int, [_vp, _i64, _vp, _vp, _vp, _vp, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp]),
 }

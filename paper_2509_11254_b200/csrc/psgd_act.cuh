@@ -406,4 +406,21 @@ __global__ void __launch_bounds__(256) k_swiglu_backward_any(ActShape s, const _
     });
 }
 
+// rows of 16-bit values to another alignment and row stride
+__global__ void __launch_bounds__(256) k_copy_rows(ActShape s, const unsigned short* __restrict__ src, long long lds, unsigned short* __restrict__ dst, long long ldd) {
+    lane_groups(s, [&](long long r, int g0) {
+        unsigned short v[LANE_GROUPS];
+#pragma unroll
+        for (int i = 0; i < LANE_GROUPS; ++i) {
+            const int col = (g0 + i) * ACT_GROUP + threadIdx.x;
+            v[i] = col < s.F ? __ldg(src + r * lds + col) : (unsigned short)0;
+        }
+#pragma unroll
+        for (int i = 0; i < LANE_GROUPS; ++i) {
+            const int col = (g0 + i) * ACT_GROUP + threadIdx.x;
+            if (col < s.F) dst[r * ldd + col] = v[i];
+        }
+    });
+}
+
 }  // namespace psgd

@@ -20,11 +20,12 @@ constexpr int KACC_F32 = 32;       // stages (2048 of k) per accumulator where t
 
 constexpr int ROUND_COST = 6;      // of a unit beside its stages (epilogue not overlapped, refilling the ring), in stages
 
-struct TilePlan { int64_t M, N, K; int mt, nt, kb, bn, full, S, kbps, tail, units, gm; };
+struct TilePlan { int64_t M, N, K; int mt, nt, kb, bn, full, S, kbps, tail, parts, units, gm; };
 
 double stage_cost(int bn) { return bn == 256 ? 1.0 : bn == 192 ? 0.80 : 0.60; }      // narrower tiles fetch more bytes per product
 
 void finish_plan(TilePlan& p, int pairs) {
+    p.parts = p.parts || p.S > 1;
     p.units = p.full + p.tail * p.S;
     // raster: all row tiles next to each other while the row operand fits beside the rest in L2, else as many as make the
     // pairs at work cover all columns
@@ -88,7 +89,7 @@ void plan_two(TilePlan (&p)[2], const int64_t (&M)[2], int64_t N, const int64_t 
         finish_plan(q, pairs);
     }
 }
-size_t part_bytes(const TilePlan& p) { return p.S > 1 ? (size_t)(p.units - p.full) * TG_PART * 4 : 0; }
+size_t part_bytes(const TilePlan& p) { return p.parts ? (size_t)(p.units - p.full) * TG_PART * 4 : 0; }
 
 // bfloat16 matrix, `rows` rows of `cols` with row stride ld (elements): boxes of 64 columns and `box` rows, 128-byte swizzle
 bool encode_operand(CUtensorMap* map, const void* p, int64_t rows, int64_t cols, int64_t ld, int box) {
@@ -105,7 +106,7 @@ bool encode_operand(CUtensorMap* map, const void* p, int64_t rows, int64_t cols,
 
 void set_problem(TileProblem& t, const TilePlan& p) {
     t.M = (int)p.M; t.N = (int)p.N;
-    t.mt = p.mt; t.nt = p.nt; t.kb = p.kb; t.bn = p.bn; t.full = p.full; t.S = p.S; t.kbps = p.kbps; t.tail = p.tail; t.units = p.units; t.gm = p.gm;
+    t.mt = p.mt; t.nt = p.nt; t.kb = p.kb; t.bn = p.bn; t.full = p.full; t.S = p.S; t.kbps = p.kbps; t.tail = p.tail; t.parts = p.parts; t.units = p.units; t.gm = p.gm;
     t.by_group = fast_div((unsigned)p.gm * p.nt); t.by_gm = fast_div(p.gm); t.by_rest = fast_div(std::max(1, p.mt % p.gm)); t.by_tail = fast_div(std::max(1, p.tail));
 }
 
@@ -166,7 +167,7 @@ psgd_status launch_products(int count, const Operand (&A)[2], const Operand (&B)
     }
     allow_smem(k_tile<EPI_STORE>, tile_smem_bytes());
     if (!launch_after(k_tile<EPI_STORE>, dim3(2 * n), dim3(TG_THREADS), tile_smem_bytes(), st, early, m[0], m[1], m[2], m[3], a)) return PSGD_E_CUDA;
-    const int joins = (p[0].S > 1 ? p[0].tail : 0) + (count == 2 && p[1].S > 1 ? p[1].tail : 0);
+    const int joins = (p[0].parts ? p[0].tail : 0) + (count == 2 && p[1].parts ? p[1].tail : 0);
     const int wide = std::max(p[0].bn, count == 2 ? p[1].bn : 0);
     if (joins && !launch_after(k_join, dim3(joins, wide / 32, TG_BM / 32), dim3(128), 0, st, true, a)) return PSGD_E_CUDA;
     return PSGD_OK;
@@ -359,11 +360,20 @@ bool dtype_ok(int dtype) { return dtype == PSGD_DT_F32 || dtype == PSGD_DT_BF16;
 bool ckpt_ok(const void* q) { return ((uintptr_t)q & 15) == 0; }
 
 struct WgradPlan { int pairs; int64_t ldx; TilePlan p; size_t x, part, total; };
-WgradPlan plan_wgrad(int64_t T, int64_t O, int64_t F) {
+// `by_parts`: a float32 result whose rows are not 16-byte aligned and whose tiles are summed in several steps: the steps add up in
+// partial tiles (5284 x 3300 x 2789: unaligned read-add-write made the product 277 us, against 97 us of an aligned one of that size; all of
+// it 374 -> 164 us)
+WgradPlan plan_wgrad(int64_t T, int64_t O, int64_t F, bool by_parts) {
     WgradPlan g{};
     g.pairs = std::max(1, device_sms() / 2);
     g.ldx = (int64_t)align_up(F, ACT_GROUP);
     g.p = plan_tiles(O, F, T, g.pairs, true);
+    if (by_parts && g.p.kb > KACC_F32) {
+        if (g.p.S == 1) { g.p.tail = g.p.mt * g.p.nt; g.p.full = 0; }
+        else if (g.p.full) { g.p.tail += g.p.full; g.p.full = 0; g.p.S = 1; g.p.kbps = g.p.kb; }
+        g.p.parts = 1;
+        finish_plan(g.p, g.pairs);
+    }
     size_t at = 256;
     auto take = [&](size_t bytes) { const size_t o = at; at = align_up(at + bytes, 256); return o; };
     g.x = take((size_t)T * g.ldx * 2);
@@ -424,10 +434,21 @@ psgd_status psgd_act_unpack(const int8_t* q, const uint8_t* scales, int64_t T, i
     return last_error();
 }
 
+psgd_status psgd_copy_rows(const void* src, int64_t lds, int64_t rows, int64_t cols, void* dst, int64_t ldd, psgd_stream stream) {
+    if (rows < 0 || rows > MAX_EXTENT || !extent_ok(cols)) return PSGD_E_INVALID;
+    if (rows == 0) return PSGD_OK;
+    if (!src || !dst) return PSGD_E_NULL;
+    if (lds < cols || ldd < cols) return PSGD_E_INVALID;
+    const ActShape s{rows, (int)cols, ceil_div(cols, ACT_GROUP)};
+    const ActGrid g = lane_grid(rows, s.G);
+    k_copy_rows<<<g.grid, g.block, 0, (cudaStream_t)stream>>>(s, (const unsigned short*)src, lds, (unsigned short*)dst, ldd);
+    return last_error();
+}
+
 psgd_status psgd_act_wgrad_workspace(int64_t T, int64_t O, int64_t F, size_t* bytes) {
     if (!bytes) return PSGD_E_NULL;
     if (!act_ok(T, F) || !extent_ok(O) || !tiles_ok(O, F)) return PSGD_E_INVALID;
-    *bytes = T == 0 ? 256 : plan_wgrad(T, O, F).total;
+    *bytes = T == 0 ? 256 : std::max(plan_wgrad(T, O, F, false).total, F % 4 ? plan_wgrad(T, O, F, true).total : 0);
     return PSGD_OK;
 }
 
@@ -441,7 +462,9 @@ psgd_status psgd_act_wgrad(const void* dY, int64_t lddy, const int8_t* q, const 
         const size_t es = dtype == PSGD_DT_F32 ? 4 : 2;
         return cudaMemset2DAsync(dW, (size_t)lddw * es, 0, (size_t)F * es, (size_t)O, st) == cudaSuccess ? PSGD_OK : PSGD_E_CUDA;
     }
-    const WgradPlan g = plan_wgrad(T, O, F);
+    const bool vec = aligned16(dW) && lddw % (dtype == PSGD_DT_F32 ? 4 : 8) == 0;
+    WgradPlan g = plan_wgrad(T, O, F, dtype == PSGD_DT_F32 && !vec);
+    if (ws_bytes < g.total) g = plan_wgrad(T, O, F, false);       // (an aligned width whose result starts or steps unaligned)
     if (ws_bytes < g.total) return PSGD_E_WORKSPACE;
     char* w = (char*)ws;
     const ActShape s{T, (int)F, ceil_div(F, ACT_GROUP)};
@@ -450,7 +473,7 @@ psgd_status psgd_act_wgrad(const void* dY, int64_t lddy, const int8_t* q, const 
     a.status = status ? status : (int*)w;
     TileProblem& t = a.p[0];
     t.out = dW; t.ldo = lddw; t.out_f32 = dtype == PSGD_DT_F32;
-    t.vec = aligned16(dW) && lddw % (t.out_f32 ? 4 : 8) == 0;
+    t.vec = vec;
     t.kacc = t.out_f32 ? KACC_F32 : 0;
     t.part = (float*)(w + g.part);
     const Operand A[2] = {{dY, lddy, true}, {}}, B[2] = {{w + g.x, g.ldx, true}, {}};

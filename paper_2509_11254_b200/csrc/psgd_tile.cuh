@@ -59,6 +59,7 @@ struct TileProblem {
     int full;                  // tiles done in one piece (the first `full` in raster order)
     int S, kbps;               // pieces and stages per piece of every later tile
     int tail;                  // later tiles
+    int parts;                 // later tiles go through memory as partial tiles and k_join: always where S > 1
     int units;
     int gm;                    // raster: groups of gm row tiles, column by column
     FastDiv by_group, by_gm, by_rest, by_tail;   // gm * nt, gm, rows of the last group, tail
@@ -205,7 +206,7 @@ __device__ __forceinline__ bool tile_unit(const TileArgs& a, int j, TileUnit& w)
     w.kb0 = 0;
     w.kb1 = p.kb;
     w.piece = -1;
-    if (u >= p.full && p.S > 1) {
+    if (u >= p.full && p.parts) {
         // all tiles' first pieces, then all second pieces: pairs at work together read the same range of k and share operands in L2
         w.piece = u - p.full;
         const int s = w.piece / p.by_tail;
@@ -602,7 +603,7 @@ __global__ void __launch_bounds__(128) k_join(const __grid_constant__ TileArgs a
     grid_trigger();
     grid_wait();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int first = a.p[0].S > 1 ? a.p[0].tail : 0;
+    const int first = a.p[0].parts ? a.p[0].tail : 0;
     const int which = (int)blockIdx.x < first ? 0 : 1, tile = blockIdx.x - (which ? first : 0);
     const TileProblem& p = a.p[which];
     int m0, n0;

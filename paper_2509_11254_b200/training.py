@@ -70,12 +70,14 @@ def _status(t, device):
     return _vector(t, "status", torch.int32, 1, device) if t is not None else None
 
 
-def _operand(t, rows, cols, ld):
+def _operand(t, rows, cols, ld, stream):
     """(tensor, row stride): `t` itself where the tensor cores' loads can read it in place (16-byte aligned rows), else a copy with padded rows."""
     if t.data_ptr() % 16 == 0 and (rows <= 1 or ld % 8 == 0):
         return t, ld
-    ld = -(-cols // 8) * 8
-    return _empty((rows, ld), dtype=t.dtype, device=t.device)[:, :cols].copy_(t), ld
+    pad = -(-cols // 8) * 8
+    copy = _empty((rows, pad), dtype=t.dtype, device=t.device)
+    _check(lib().psgd_copy_rows(t.data_ptr(), ld, rows, cols, copy.data_ptr(), pad, stream))
+    return copy, pad
 
 
 @contextlib.contextmanager
@@ -134,8 +136,8 @@ def _xent(grad, hidden, weight, labels, token_weight, ignore_index, d_hidden, d_
     at_status = _status(status, dev)
     with _on(dev, stream) as s:
         nbytes = _workspace_bytes("psgd_xent_workspace", T, V, D, int(grad), dev.index)
-        hidden, ldh = _operand(hidden, T, D, ldh)
-        weight, ldw = _operand(weight, V, D, ldw)
+        hidden, ldh = _operand(hidden, T, D, ldh, s)
+        weight, ldw = _operand(weight, V, D, ldw, s)
         ws = _empty(nbytes, dtype=torch.uint8, device=dev)
         out = _empty(2 * T + 1, dtype=torch.float32, device=dev)
         at = out.data_ptr()                         # token_loss, lse, loss side by side
@@ -249,7 +251,7 @@ def weight_gradient(dy, kept, dtype=torch.float32, out=None, status=None, stream
     at_status = _status(status, dev)
     with _on(dev, stream) as s:
         nbytes = _workspace_bytes("psgd_act_wgrad_workspace", T, O, F, dev.index)
-        dy, ldy = _operand(dy, T, O, ldy)
+        dy, ldy = _operand(dy, T, O, ldy, s)
         ws = _empty(nbytes, dtype=torch.uint8, device=dev)
         if out is None:
             out = _empty((O, F), dtype=dtype, device=dev)

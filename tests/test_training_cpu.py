@@ -71,6 +71,12 @@ def test_calls_refuse_before_any_launch(L):
     assert L.psgd_swiglu_backward(p, 64, p, p, p, p, 8, 64, p, 64, p, 64, p, 10, None) == -1
 
 
+def test_copy_rows_refuses(L):
+    p = 1 << 20
+    assert L.psgd_copy_rows(p, 7, 4, 8, p, 8, None) == -1 and L.psgd_copy_rows(p, 8, 4, 8, p, 7, None) == -1 and L.psgd_copy_rows(p, 8, -1, 8, p, 8, None) == -1
+    assert L.psgd_copy_rows(None, 8, 4, 8, p, 8, None) == -2 and L.psgd_copy_rows(None, 8, 0, 8, None, 8, None) == 0
+
+
 def test_python_refuses_host_tensors():
     import torch
 

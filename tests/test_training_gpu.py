@@ -401,6 +401,23 @@ def test_weight_gradient_matches_definition(torch, ops, T, O, F, dtype):
     assert torch.equal(out, ops.weight_gradient(dy, kept, dtype=getattr(torch, dtype)))
 
 
+@pytest.mark.parametrize("T,O,F", [(2049, 300, 131), (5000, 1027, 770), (9001, 70, 3), (4100, 2600, 1533)])
+def test_weight_gradient_with_rows_of_odd_length(torch, ops, T, O, F):
+    """Results whose rows are not 16-byte aligned, with more terms than one accumulator takes (T > 2048)."""
+    g = gen(torch, T + O)
+    x = torch.randn(T, F, generator=g, device="cuda").to(torch.bfloat16)
+    dy = torch.randn(T, O, generator=g, device="cuda").to(torch.bfloat16)
+    kept = ops.pack_activation(x)
+    xs, dyd = kept.unpack(torch.float32).double(), dy.double()
+    ref, size = dyd.T @ xs, dyd.abs().T @ xs.abs()
+    out = ops.weight_gradient(dy, kept)
+    within(out, ref, sum_bound(T) * size)
+    wide = torch.full((O, F + 2), 9.0, device="cuda")                    # a result that starts at an odd place, whatever its width
+    ops.weight_gradient(dy, kept, out=wide[:, 1:1 + F])
+    within(wide[:, 1:1 + F], ref, sum_bound(T) * size)
+    assert bool((wide[:, 0] == 9).all()) and bool((wide[:, 1 + F] == 9).all())
+
+
 @pytest.mark.parametrize("T", [1, 64, 65, 130])
 def test_weight_gradient_of_groups_that_are_not_numbers(torch, ops, T):
     """An infinity in the last row makes the 32 input columns of its group NaN, and no others (rows behind the last one count as zeros)."""
