@@ -54,14 +54,14 @@ def _matrix(t, name, dtypes=(_BF16,), shape=None, device=None):
         ld = cols                                   # the stride of a single row is never used
     if one != 1 and cols > 1 or ld < cols:
         raise PSGDError(f"{name} must have unit column stride and rows that do not overlap")
-    if device is not None and t.device != device:
+    if device is not None and t.get_device() != device.index:
         raise PSGDError(f"{name} is on {t.device}, expected {device}")
     return rows, cols, ld
 
 
 def _vector(t, name, dtype, n, device):
     """The address of a contiguous CUDA vector."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != dtype or t.shape != (n,) or not t.is_contiguous() or t.device != device:
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.ndim != 1 or len(t) != n or not t.is_contiguous() or t.get_device() != device.index:
         raise PSGDError(f"{name} must be a contiguous {_name(dtype)} tensor of {n} elements on {device}")
     return t.data_ptr()
 
@@ -80,38 +80,28 @@ def _operand(t, rows, cols, ld, stream):
     return copy, pad
 
 
-@contextlib.contextmanager
-def _on_other(device, stream):
-    with torch.cuda.device(device), torch.cuda.stream(stream):
-        yield stream.cuda_stream
-
-
-class _OnCurrent:
-    """The common case without the cost of switching: the tensor's device is current and so is its stream."""
-
-    __slots__ = ("stream",)
-
-    def __init__(self, stream):
-        self.stream = stream
-
-    def __enter__(self):
-        return self.stream
-
-    def __exit__(self, *a):
-        return False
-
-
-# the handle of the current stream without the object around it, where torch has it
+# the handle of the current stream and the current device without the objects around them, where torch has it so
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
-def _on(device, stream):
-    """Makes `device` and `stream` current, so that what is allocated inside belongs to that stream."""
-    if stream is None:
-        if device.index == torch.cuda.current_device():
-            return _OnCurrent(_raw_stream(device.index))
-        stream = torch.cuda.current_stream(device)
-    return _on_other(device, stream)
+def _here(device, stream):
+    """The current stream's handle where `device` is current and no other stream is asked for, else None."""
+    return _raw_stream(device.index) if stream is None and device.index == _current_device() else None
+
+
+@contextlib.contextmanager
+def _there(device, stream, *inputs):
+    """Makes `device` and `stream` current, so that what is allocated inside belongs to that stream; the call is then made again inside.
+
+    The inputs may have been allocated on another stream: their memory is not given away before this stream has read them.
+    """
+    stream = stream if stream is not None else torch.cuda.current_stream(device)
+    with torch.cuda.device(device), torch.cuda.stream(stream):
+        yield
+        for t in inputs:
+            if t is not None:
+                t.record_stream(stream)
 
 
 @lru_cache(maxsize=256)
@@ -134,22 +124,26 @@ def _xent(grad, hidden, weight, labels, token_weight, ignore_index, d_hidden, d_
     lddh = _matrix(d_hidden, "d_hidden", shape=(T, D), device=dev)[2] if d_hidden is not None else D
     lddw = _matrix(d_weight, "d_weight", shape=(V, D), device=dev)[2] if d_weight is not None else D
     at_status = _status(status, dev)
-    with _on(dev, stream) as s:
-        nbytes = _workspace_bytes("psgd_xent_workspace", T, V, D, int(grad), dev.index)
-        hidden, ldh = _operand(hidden, T, D, ldh, s)
-        weight, ldw = _operand(weight, V, D, ldw, s)
-        ws = _empty(nbytes, dtype=torch.uint8, device=dev)
-        out = _empty(2 * T + 1, dtype=torch.float32, device=dev)
-        at = out.data_ptr()                         # token_loss, lse, loss side by side
-        args = (hidden.data_ptr(), ldh, weight.data_ptr(), ldw, at_labels, at_weight, ignore_index, T, V, D, at + 8 * T, at, at + 4 * T)
-        if grad:
-            if d_hidden is None:
-                d_hidden = _empty((T, D), dtype=_BF16, device=dev)
-            if d_weight is None:
-                d_weight = _empty((V, D), dtype=_BF16, device=dev)
-            _check(lib().psgd_xent_grad(*args, d_hidden.data_ptr(), lddh, d_weight.data_ptr(), lddw, at_status, ws.data_ptr(), nbytes, s))
-        else:
-            _check(lib().psgd_xent_loss(*args, at_status, ws.data_ptr(), nbytes, s))
+    s = _here(dev, stream)
+    if s is None:
+        with _there(dev, stream, hidden, weight, labels, token_weight, d_hidden, d_weight, status):
+            return _xent(grad, hidden, weight, labels, token_weight, ignore_index, d_hidden, d_weight, status, None)
+    nbytes = _workspace_bytes("psgd_xent_workspace", T, V, D, int(grad), dev.index)
+    hidden, ldh = _operand(hidden, T, D, ldh, s)
+    weight, ldw = _operand(weight, V, D, ldw, s)
+    ws = _empty(nbytes, dtype=torch.uint8, device=dev)
+    out = _empty(2 * T + 1, dtype=torch.float32, device=dev)
+    at = out.data_ptr()                             # token_loss, lse, loss side by side
+    if grad:
+        if d_hidden is None:
+            d_hidden = _empty((T, D), dtype=_BF16, device=dev)
+        if d_weight is None:
+            d_weight = _empty((V, D), dtype=_BF16, device=dev)
+        _check(lib().psgd_xent_grad(hidden.data_ptr(), ldh, weight.data_ptr(), ldw, at_labels, at_weight, ignore_index, T, V, D, at + 8 * T, at, at + 4 * T,
+                                    d_hidden.data_ptr(), lddh, d_weight.data_ptr(), lddw, at_status, ws.data_ptr(), nbytes, s))
+    else:
+        _check(lib().psgd_xent_loss(hidden.data_ptr(), ldh, weight.data_ptr(), ldw, at_labels, at_weight, ignore_index, T, V, D, at + 8 * T, at, at + 4 * T,
+                                    at_status, ws.data_ptr(), nbytes, s))
     token_loss, lse, loss = out.split_with_sizes((T, T, 1))
     loss = loss.view(())
     return CrossEntropyGrad(loss, token_loss, lse, d_hidden, d_weight) if grad else CrossEntropy(loss, token_loss, lse)
@@ -210,19 +204,25 @@ class ActivationCheckpoint:
             ld = _matrix(out, "out", tuple(_DTYPES), self.shape, self.device)[2]
         elif dtype not in _DTYPES:
             raise PSGDError("dtype must be float32 or bfloat16")
-        with _on(self.device, stream) as s:
-            if out is None:
-                out = _empty((T, F), dtype=dtype, device=self.device)
-            _check(lib().psgd_act_unpack(self._q, self._s, T, F, out.data_ptr(), ld, _DTYPES[out.dtype], s))
+        s = _here(self.device, stream)
+        if s is None:
+            with _there(self.device, stream, self._buf, out):
+                return self.unpack(dtype, out)
+        if out is None:
+            out = _empty((T, F), dtype=dtype, device=self.device)
+        _check(lib().psgd_act_unpack(self._q, self._s, T, F, out.data_ptr(), ld, _DTYPES[out.dtype], s))
         return out
 
 
 def pack_activation(x, stream=None):
     """x [T, F] (bfloat16 or float32) in 8 bits: an ActivationCheckpoint."""
     T, F, ld = _matrix(x, "x", tuple(_DTYPES))
-    with _on(x.device, stream) as s:
-        kept = ActivationCheckpoint(T, F, x.device)
-        _check(lib().psgd_act_pack(x.data_ptr(), ld, _DTYPES[x.dtype], T, F, kept._q, kept._s, s))
+    s = _here(x.device, stream)
+    if s is None:
+        with _there(x.device, stream, x):
+            return pack_activation(x)
+    kept = ActivationCheckpoint(T, F, x.device)
+    _check(lib().psgd_act_pack(x.data_ptr(), ld, _DTYPES[x.dtype], T, F, kept._q, kept._s, s))
     return kept
 
 
@@ -249,13 +249,16 @@ def weight_gradient(dy, kept, dtype=torch.float32, out=None, status=None, stream
     elif dtype not in _DTYPES:
         raise PSGDError("dtype must be float32 or bfloat16")
     at_status = _status(status, dev)
-    with _on(dev, stream) as s:
-        nbytes = _workspace_bytes("psgd_act_wgrad_workspace", T, O, F, dev.index)
-        dy, ldy = _operand(dy, T, O, ldy, s)
-        ws = _empty(nbytes, dtype=torch.uint8, device=dev)
-        if out is None:
-            out = _empty((O, F), dtype=dtype, device=dev)
-        _check(lib().psgd_act_wgrad(dy.data_ptr(), ldy, kept._q, kept._s, T, O, F, out.data_ptr(), ldo, _DTYPES[out.dtype], at_status, ws.data_ptr(), nbytes, s))
+    s = _here(dev, stream)
+    if s is None:
+        with _there(dev, stream, dy, kept._buf, out, status):
+            return weight_gradient(dy, kept, dtype, out, status)
+    nbytes = _workspace_bytes("psgd_act_wgrad_workspace", T, O, F, dev.index)
+    dy, ldy = _operand(dy, T, O, ldy, s)
+    ws = _empty(nbytes, dtype=torch.uint8, device=dev)
+    if out is None:
+        out = _empty((O, F), dtype=dtype, device=dev)
+    _check(lib().psgd_act_wgrad(dy.data_ptr(), ldy, kept._q, kept._s, T, O, F, out.data_ptr(), ldo, _DTYPES[out.dtype], at_status, ws.data_ptr(), nbytes, s))
     return out
 
 
@@ -264,12 +267,15 @@ def swiglu_forward(gate, up, stream=None):
     T, F, ldg = _matrix(gate, "gate")
     dev = gate.device
     ldu = _matrix(up, "up", shape=(T, F), device=dev)[2]
-    with _on(dev, stream) as s:
-        h = _empty((T, F), dtype=_BF16, device=dev)
-        size = -(-T * -(-F // GROUP) * (GROUP + 1) // 256) * 256
-        kg = ActivationCheckpoint(T, F, dev, _empty(2 * size, dtype=torch.uint8, device=dev))      # they are kept and used together
-        ku = ActivationCheckpoint(T, F, dev, kg._buf, size)
-        _check(lib().psgd_swiglu_forward(gate.data_ptr(), ldg, up.data_ptr(), ldu, T, F, h.data_ptr(), F, kg._q, kg._s, ku._q, ku._s, s))
+    s = _here(dev, stream)
+    if s is None:
+        with _there(dev, stream, gate, up):
+            return swiglu_forward(gate, up)
+    h = _empty((T, F), dtype=_BF16, device=dev)
+    size = -(-T * -(-F // GROUP) * (GROUP + 1) // 256) * 256
+    kg = ActivationCheckpoint(T, F, dev, _empty(2 * size, dtype=torch.uint8, device=dev))      # they are kept and used together
+    ku = ActivationCheckpoint(T, F, dev, kg._buf, size)
+    _check(lib().psgd_swiglu_forward(gate.data_ptr(), ldg, up.data_ptr(), ldu, T, F, h.data_ptr(), F, kg._q, kg._s, ku._q, ku._s, s))
     return h, kg, ku
 
 
@@ -279,10 +285,13 @@ def swiglu_backward(dh, gate, up, recompute=False, stream=None):
     dev = dh.device
     _kept(gate, "gate", dev, (T, F))
     _kept(up, "up", dev, (T, F))
-    with _on(dev, stream) as s:
-        d_gate = _empty((T, F), dtype=_BF16, device=dev)
-        d_up = torch.empty_like(d_gate)
-        h = torch.empty_like(d_gate) if recompute else None
-        _check(lib().psgd_swiglu_backward(dh.data_ptr(), ld, gate._q, gate._s, up._q, up._s, T, F, d_gate.data_ptr(), F, d_up.data_ptr(), F,
-                                          h.data_ptr() if recompute else None, F, s))
+    s = _here(dev, stream)
+    if s is None:
+        with _there(dev, stream, dh, gate._buf, up._buf):
+            return swiglu_backward(dh, gate, up, recompute)
+    d_gate = _empty((T, F), dtype=_BF16, device=dev)
+    d_up = torch.empty_like(d_gate)
+    h = torch.empty_like(d_gate) if recompute else None
+    _check(lib().psgd_swiglu_backward(dh.data_ptr(), ld, gate._q, gate._s, up._q, up._s, T, F, d_gate.data_ptr(), F, d_up.data_ptr(), F,
+                                      h.data_ptr() if recompute else None, F, s))
     return (d_gate, d_up, h) if recompute else (d_gate, d_up)

@@ -607,6 +607,33 @@ def test_calls_on_two_streams_at_once(torch, ops):
                 assert torch.equal(u, v)
 
 
+def test_inputs_freed_before_another_stream_has_read_them(torch, ops):
+    """The caller drops its inputs while the call's stream is still busy: their memory is not given to the next allocation before they are read."""
+    h, w, labels = xent_inputs(torch, 300, 1100, 200, seed=25)
+    x = torch.randn(300, 264, generator=gen(torch, 26), device="cuda").to(torch.bfloat16)
+
+    def work(h, w, labels, x, stream=None):
+        y, kg, ku = ops.swiglu_forward(x, x, stream=stream)
+        return [*ops.linear_cross_entropy_grad(h, w, labels, stream=stream), y, *ops.swiglu_backward(x, kg, ku, recompute=True, stream=stream),
+                ops.weight_gradient(x, ops.pack_activation(x, stream=stream), stream=stream)]
+
+    want = work(h, w, labels, x)
+    s = torch.cuda.Stream()
+    mine = [t.clone() for t in (h, w, labels, x)]
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(20_000_000)               # about ten milliseconds
+    got = work(*mine, stream=s)
+    sizes = [(t.shape, t.dtype) for t in mine]
+    del mine
+    torch.cuda.current_stream().synchronize()
+    others = [torch.full(shape, 3, dtype=dtype, device="cuda") for shape, dtype in sizes for _ in range(4)]
+    torch.cuda.synchronize()
+    assert len(others) == 16
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+
+
 def test_calls_in_a_cuda_graph(torch, ops):
     """Captured once, replayed with other inputs in the same places."""
     h, w, labels = xent_inputs(torch, 300, 1100, 200, seed=31)
