@@ -22,7 +22,9 @@ constexpr int ROUND_COST = 6;      // of a unit beside its stages (epilogue not 
 
 struct TilePlan { int64_t M, N, K; int mt, nt, kb, bn, full, S, kbps, tail, parts, units, gm; };
 
-double stage_cost(int bn) { return bn == 256 ? 1.0 : bn == 192 ? 0.80 : 0.60; }      // narrower tiles fetch more bytes per product
+// Of a stage of 64 of k, in those of 256 columns.  A stage is bound by shared memory: 16 KB of A and bn / 16 KB of B per CTA are written by the copies
+// and read by the MMAs (measured 0.31 us with 256 columns, 0.25 with 192, 0.23 with 128 on 48 pairs, 0.36, 0.26 and 0.24 on all of them).
+double stage_cost(int bn) { return bn == 256 ? 1.0 : bn == 192 ? 0.80 : 0.70; }
 
 void finish_plan(TilePlan& p, int pairs) {
     p.parts = p.parts || p.S > 1;
@@ -51,7 +53,7 @@ TilePlan plan_tiles(int64_t M, int64_t N, int64_t K, int pairs, bool store) {
             const int kbps = ceil_div(p.kb, S);
             if (ceil_div(p.kb, kbps) != S) continue;                           // no empty pieces
             double cost = whole + (R > 0 ? (double)ceil_div((int64_t)R * S, pairs) * (kbps + ROUND_COST) * stage : 0.0);
-            if (S > 1) cost += 12 + 0.06 * R * S;
+            if (S > 1) cost += 20 + 0.06 * R * S;         // 2048 x 768 x 4096 in three pieces of 256 columns: 25.6 us, whole with 128 columns: 23.2
             if (cost < best) { best = cost; p.bn = bn; p.nt = nt; p.S = S; p.kbps = kbps; p.tail = R; p.full = (int)(tiles - R); }
         }
     }
@@ -361,8 +363,7 @@ bool ckpt_ok(const void* q) { return ((uintptr_t)q & 15) == 0; }
 
 struct WgradPlan { int pairs; int64_t ldx; TilePlan p; size_t x, part, total; };
 // `by_parts`: a float32 result whose rows are not 16-byte aligned and whose tiles are summed in several steps: the steps add up in
-// partial tiles (5284 x 3300 x 2789: unaligned read-add-write made the product 277 us, against 97 us of an aligned one of that size; all of
-// it 374 -> 164 us)
+// partial tiles (5284 x 3300 x 2789: the whole call 225 us with unaligned read-add-write, 135 us so)
 WgradPlan plan_wgrad(int64_t T, int64_t O, int64_t F, bool by_parts) {
     WgradPlan g{};
     g.pairs = std::max(1, device_sms() / 2);

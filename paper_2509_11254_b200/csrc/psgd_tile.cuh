@@ -221,11 +221,38 @@ __device__ __forceinline__ bool tile_unit(const TileArgs& a, int j, TileUnit& w)
 // Half a staging buffer holds 32 rows of four 16-byte units; unit j of row r lies where neither side meets a bank twice.
 __device__ __forceinline__ int staged(int r, int j) { return r * 4 + (j ^ ((r >> 1) & 3)); }
 
-// A 32 x 32 block of C, a row per lane -> rows of 64 bytes through the warp's staging buffer -> out (+ addend, * scale).
+// A 32 x 32 block of C, a row per lane -> rows through the warp's staging buffer -> out (+ addend, * scale).
 // Row-per-lane stores would touch 32 lines per instruction.
 __device__ __forceinline__ void emit_block(const TileProblem& a, uint4* xb, float (&v)[32], int row0, int col0, const float* addend, long long lda, float scale) {
     const int lane = threadIdx.x & 31, lrow = lane >> 2, lch = lane & 3;        // row-contiguous phase: row within a group of 8, unit
-    if (!a.out_f32 && !addend && a.vec && col0 + 32 <= a.N) {                   // 32 columns of bfloat16
+    const int rows = a.M - row0;
+    // the last columns, or rows without alignment: a column per lane, a row per store (the block of 1001 x 771 float32: 7400 cycles with two half
+    // rows per store and the row's address formed each time, 3000 so; an aligned one of bfloat16 1050)
+    if (!a.vec || col0 + 32 > a.N) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            xb[lane * 8 + (j ^ (lane & 7))] = make_uint4(__float_as_uint(v[4 * j]), __float_as_uint(v[4 * j + 1]), __float_as_uint(v[4 * j + 2]), __float_as_uint(v[4 * j + 3]));
+        __syncwarp();
+        const float* xf = reinterpret_cast<const float*>(xb) + (lane & 3);
+        const int top = min(rows, 32);
+        const long long ldo = a.ldo;
+        const size_t at = (size_t)row0 * ldo + col0 + lane;
+        const float* y = addend ? addend + (size_t)row0 * lda + col0 + lane : nullptr;
+        if (col0 + lane < a.N) {
+            if (a.out_f32) {
+                float* out = (float*)a.out + at;
+#pragma unroll 8
+                for (int r = 0; r < top; ++r) out[r * ldo] = (xf[(r * 8 + ((lane >> 2) ^ (r & 7))) * 4] + (y ? y[r * lda] : 0.f)) * scale;
+            } else {
+                __nv_bfloat16* out = (__nv_bfloat16*)a.out + at;
+#pragma unroll 8
+                for (int r = 0; r < top; ++r) out[r * ldo] = __float2bfloat16_rn((xf[(r * 8 + ((lane >> 2) ^ (r & 7))) * 4] + (y ? y[r * lda] : 0.f)) * scale);
+            }
+        }
+        __syncwarp();
+        return;
+    }
+    if (!a.out_f32 && !addend) {                                                // 32 columns of bfloat16
 #pragma unroll
         for (int j = 0; j < 4; ++j)
             xb[staged(lane, j)] = make_uint4(pack_bf16(v[8 * j] * scale, v[8 * j + 1] * scale), pack_bf16(v[8 * j + 2] * scale, v[8 * j + 3] * scale),
@@ -234,7 +261,7 @@ __device__ __forceinline__ void emit_block(const TileProblem& a, uint4* xb, floa
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int br = 8 * i + lrow;
-            if (row0 + br < a.M) *reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + (size_t)(row0 + br) * a.ldo + col0 + 8 * lch) = xb[staged(br, lch)];
+            if (br < rows) *reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + (size_t)(row0 + br) * a.ldo + col0 + 8 * lch) = xb[staged(br, lch)];
         }
         __syncwarp();
         return;
@@ -242,45 +269,27 @@ __device__ __forceinline__ void emit_block(const TileProblem& a, uint4* xb, floa
 #pragma unroll
     for (int h = 0; h < 2; ++h) {                                               // 16 columns of float32 at a time
         const int col1 = col0 + 16 * h;
-        if (col1 >= a.N) break;
-        const bool wide = a.vec && col1 + 16 <= a.N;
         float4 y[4];
-        if (addend && wide) {
+        if (addend) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int row = row0 + 8 * i + lrow;
-                if (row < a.M) y[i] = *reinterpret_cast<const float4*>(addend + (size_t)row * lda + col1 + 4 * lch);
-            }
+            for (int i = 0; i < 4; ++i)
+                if (8 * i + lrow < rows) y[i] = *reinterpret_cast<const float4*>(addend + (size_t)(row0 + 8 * i + lrow) * lda + col1 + 4 * lch);
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j)
             xb[staged(lane, j)] = make_uint4(__float_as_uint(v[16 * h + 4 * j]), __float_as_uint(v[16 * h + 4 * j + 1]), __float_as_uint(v[16 * h + 4 * j + 2]),
                                              __float_as_uint(v[16 * h + 4 * j + 3]));
         __syncwarp();
-        if (wide) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int br = 8 * i + lrow, row = row0 + br;
-                const uint4 u = xb[staged(br, lch)];
-                float4 x = make_float4(__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w));
-                if (row < a.M) {
-                    if (addend) { x.x += y[i].x; x.y += y[i].y; x.z += y[i].z; x.w += y[i].w; }
-                    x.x *= scale; x.y *= scale; x.z *= scale; x.w *= scale;
-                    if (a.out_f32) *reinterpret_cast<float4*>((float*)a.out + (size_t)row * a.ldo + col1 + 4 * lch) = x;
-                    else *reinterpret_cast<uint2*>((__nv_bfloat16*)a.out + (size_t)row * a.ldo + col1 + 4 * lch) = make_uint2(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w));
-                }
-            }
-        } else {                                      // the last columns, or rows without alignment: a column per lane, two rows
-            const float* xf = reinterpret_cast<const float*>(xb);
-            const int cl = lane & 15, col = col1 + cl;
-#pragma unroll 4
-            for (int i = 0; i < 16; ++i) {
-                const int br = 2 * i + (lane >> 4), row = row0 + br;
-                if (row < a.M && col < a.N) {
-                    const float x = (xf[staged(br, cl >> 2) * 4 + (cl & 3)] + (addend ? addend[(size_t)row * lda + col] : 0.f)) * scale;
-                    if (a.out_f32) ((float*)a.out)[(size_t)row * a.ldo + col] = x;
-                    else ((__nv_bfloat16*)a.out)[(size_t)row * a.ldo + col] = __float2bfloat16_rn(x);
-                }
+        for (int i = 0; i < 4; ++i) {
+            const int br = 8 * i + lrow, row = row0 + br;
+            const uint4 u = xb[staged(br, lch)];
+            float4 x = make_float4(__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w));
+            if (br < rows) {
+                if (addend) { x.x += y[i].x; x.y += y[i].y; x.z += y[i].z; x.w += y[i].w; }
+                x.x *= scale; x.y *= scale; x.z *= scale; x.w *= scale;
+                if (a.out_f32) *reinterpret_cast<float4*>((float*)a.out + (size_t)row * a.ldo + col1 + 4 * lch) = x;
+                else *reinterpret_cast<uint2*>((__nv_bfloat16*)a.out + (size_t)row * a.ldo + col1 + 4 * lch) = make_uint2(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w));
             }
         }
         __syncwarp();
