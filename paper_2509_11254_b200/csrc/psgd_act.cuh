@@ -6,13 +6,14 @@
 // 1 + 1/32 bytes per value.  With a power of two as scale every stored value is exact in bfloat16, so that
 // products of checkpoints run on the tensor cores without another rounding.
 //
-// All kernels here are one pass over their operands and bound by HBM.  Aligned operands: a thread moves 8 values (16 bytes of
-// bfloat16, 8 of int8), four neighbouring threads share a group, and the group's maximum is two shuffles.  Rows of any
-// other length or alignment: a lane per value and a warp per group, whose 2-byte accesses still come as whole sectors (with
-// 8 values per thread there, stores of 2 bytes 16 bytes apart made the backward pass of 4096 x 2051 72 us, against 18 of 4096 x 2048).
+// All kernels here are one pass over their operands and bound by HBM.  A thread moves 8 values (16 bytes of bfloat16, 8 of int8), four
+// neighbouring threads share a group, and the group's maximum is two shuffles.  Rows of bfloat16 of any other length or alignment (ANY): a warp
+// takes 256 values of a row, loads and stores the aligned 16-byte units that they lie in, and shifts between those and
+// its lanes' values with shuffles (in) and through shared memory (out).  Float32 rows without alignment: a lane per value.
 //
 // Measured (8.06, 10.06, 3.03 and 3.03 bytes per value; of the 6533 GB/s of a copy), 16384 x 5504: gated unit forward 128 us (87 %), backward with h
-// 157 us (88 %), pack 52 us (80 %), unpack 50 us (84 %).
+// 151 us (91 %), pack 54 us (77 %; float32, 5.03 bytes: 70 us, 99 %), unpack 47 us (89 %).  16384 x 5461: 201, 213, 74 and 61 us, bound by instructions (a lane per value
+// there: 313, 320, 112 and 147 us; value-by-value stores at the ends of each warp's part instead of shared memory: 333 and 343 us).
 #pragma once
 #include <cuda_bf16.h>
 #include <stdint.h>
@@ -46,19 +47,81 @@ __device__ __forceinline__ void widen(const Raw32& r, float (&x)[8]) {
     x[0] = r.a.x; x[1] = r.a.y; x[2] = r.a.z; x[3] = r.a.w;
     x[4] = r.b.x; x[5] = r.b.y; x[6] = r.b.z; x[7] = r.b.w;
 }
-template <typename X> struct RawOf { typedef Raw32 type; };
-template <> struct RawOf<__nv_bfloat16> { typedef Raw16 type; };
+__device__ __forceinline__ uint4 pack_bf16x8(const float (&x)[8]) {
+    return make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+}
 __device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&x)[8]) {
-    *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+    *reinterpret_cast<uint4*>(p) = pack_bf16x8(x);
 }
 __device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
     reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
     reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
 }
-__device__ __forceinline__ float load1(const float* p) { return __ldg(p); }
-__device__ __forceinline__ float load1(const __nv_bfloat16* p) { return __uint_as_float((unsigned)__ldg(reinterpret_cast<const unsigned short*>(p)) << 16); }
-__device__ __forceinline__ void store1(float* p, float x) { *p = x; }
-__device__ __forceinline__ void store1(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
+
+// Rows of bfloat16 that start at any even address.  The lanes of a warp (256 values of a row) load the aligned 16-byte units that its values lie
+// in, lane 31 also the 33rd; a lane's eight values are cut out of its own and the next lane's unit when they are used.
+struct RawAny { uint4 a, b; };
+__device__ __forceinline__ unsigned shift_of(const __nv_bfloat16* p) { return (unsigned)reinterpret_cast<uintptr_t>(p) & 15u; }
+// The unit at halfword `at` of a row (from 1 - 8 on), `len` halfwords long.  `inner`: seven halfwords on either side of the row belong to the matrix
+// too and may come along; else only the row's own values are read, the others are zeros.
+__device__ __forceinline__ void load_unit(uint4& u, const __nv_bfloat16* row, int at, int len, bool inner) {
+    if (at >= len) return;
+    if (inner) {
+        u = __ldg(reinterpret_cast<const uint4*>(row + at));
+        return;
+    }
+    const unsigned short* h = reinterpret_cast<const unsigned short*>(row);
+    unsigned w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int j = at + 2 * i;
+        const unsigned x = j >= 0 && j < len ? __ldg(h + j) : 0u, y = j + 1 >= 0 && j + 1 < len ? __ldg(h + j + 1) : 0u;
+        w[i] = x | y << 16;
+    }
+    u = make_uint4(w[0], w[1], w[2], w[3]);
+}
+// 16 bytes of a and b from byte `sh` (even, below 16) on
+__device__ __forceinline__ uint4 cut_out(const uint4& a, const uint4& b, unsigned sh) {
+    const unsigned w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    unsigned t[6], u[5];
+#pragma unroll
+    for (int i = 0; i < 6; ++i) t[i] = sh & 8 ? w[i + 2] : w[i];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) u[i] = sh & 4 ? t[i + 1] : t[i];
+    const unsigned bits = (sh & 2) * 8;
+    return make_uint4(__funnelshift_r(u[0], u[1], bits), __funnelshift_r(u[1], u[2], bits), __funnelshift_r(u[2], u[3], bits), __funnelshift_r(u[3], u[4], bits));
+}
+// A lane's eight values to p; the lanes of a warp hold a row's values one after the other, `valid` of which exist from lane 0 on (all lanes call).
+// The warp's bytes go through shared memory, laid out there as they fall on 16-byte units in memory: whole units are written as such, the
+// one or two that belong to the warp in part value by value.
+constexpr int ANY_UNITS = 34;
+__device__ __forceinline__ void store_any(__nv_bfloat16* p, const uint4& v, int valid, uint4* image) {
+    const int lane = threadIdx.x & 31;                // blockDim.x is a multiple of 32
+    const unsigned sh = shift_of(p);                  // the same in all lanes
+    unsigned* word = reinterpret_cast<unsigned*>(image) + sh / 4 + 4 * lane;
+    if (sh & 2) {                                     // halves of words: the lane before has the first one
+        const unsigned before = __shfl_up_sync(0xffffffffu, v.w, 1);
+        word[0] = __funnelshift_r(before, v.x, 16);
+        word[1] = __funnelshift_r(v.x, v.y, 16);
+        word[2] = __funnelshift_r(v.y, v.z, 16);
+        word[3] = __funnelshift_r(v.z, v.w, 16);
+        if (lane == 31) word[4] = v.w >> 16;
+    } else {
+        word[0] = v.x;
+        word[1] = v.y;
+        word[2] = v.z;
+        word[3] = v.w;
+    }
+    __syncwarp();
+    const int from = (int)sh, to = from + 2 * valid;  // bytes of the image that exist
+    unsigned char* out = reinterpret_cast<unsigned char*>(p) - sh - 16 * lane;
+    if (16 * lane >= from && 16 * lane + 16 <= to) *reinterpret_cast<uint4*>(out + 16 * lane) = image[lane];
+    const int last = to / 16;                         // lanes 0-7: the first unit, where it begins before the warp; 8-15: the last, where it ends behind it
+    const int at = (lane < 8 ? 0 : 16 * last) + 2 * (lane & 7);
+    if (lane < 16 && (lane < 8 ? from > 0 : last > 0 || from == 0) && at >= from && at < to)
+        *reinterpret_cast<unsigned short*>(out + at) = reinterpret_cast<const unsigned short*>(image)[at / 2];
+    __syncwarp();
+}
 
 // The largest magnitude of eight raw values as float32 bits; a NaN wins over everything.
 __device__ __forceinline__ unsigned top_of(const Raw16& r) {
@@ -140,12 +203,13 @@ __device__ __forceinline__ void gated_backward(float d, float g, float u, float&
     h = act * u;
 }
 
-// ---- aligned operands: F a multiple of 8, every operand 16-byte aligned in every row ----
+// ---- eight values per thread ----
 // threadIdx.x (and blockIdx.x) runs over the 4 G units of 8 values of a row, the rest over rows, as many CTAs as are resident at
 // once.  A thread keeps D of its rows on their way: it asks for row i + D before it works on row i, so that bytes are
 // under way all the time and not only between two bursts of work.  Rows in flight times CTAs per multiprocessor is held
-// by registers; the pairs below were the best of six each (forward 156 us with bursts of two rows, 128 us so).
-constexpr int PACK_DEPTH = 4, PACK_CTAS = 4, FORWARD_DEPTH = 3, FORWARD_CTAS = 3, BACKWARD_DEPTH = 2, BACKWARD_CTAS = 3;
+// by registers; the pairs below were the best of six each (forward 156 us with bursts of two rows, 128 us so).  Rows of any alignment need
+// their registers for the cutting: one row on its way (16384 x 5461, forward and backward: 201 and 213 us, with two 298 and 241).
+constexpr int PACK_DEPTH = 4, PACK32_DEPTH = 2, PACK_CTAS = 4, FORWARD_DEPTH = 3, FORWARD_CTAS = 3, BACKWARD_DEPTH = 2, BACKWARD_CTAS = 3;
 struct ActCursor { int col; long long row, step; };
 __device__ __forceinline__ ActCursor act_cursor() {
     ActCursor c;
@@ -172,63 +236,149 @@ __device__ __forceinline__ void act_rows(long long T, const ActCursor& c, Work& 
     }
 }
 
-template <typename X>
-struct PackWork {
-    typedef typename RawOf<X>::type In;
+// What a thread has of a row of bfloat16, and where its values go: aligned rows (ANY false), or rows of any length and alignment, whose warps stay
+// within a row (blockDim.x a multiple of 32) and keep all their lanes.
+template <bool ANY> struct Row16 {
+    typedef Raw16 Raw;
+    const __nv_bfloat16* p;
+    long long ld;
+    int F;
+    __device__ __forceinline__ Row16(const __nv_bfloat16* p, long long ld, long long, int F) : p(p), ld(ld), F(F) {}
+    __device__ __forceinline__ void load(Raw& r, long long row, int col) const {
+        if (col < F) load8(r, p + row * ld + col);    // (a unit behind the row's end belongs to the padding of its last group)
+    }
+    __device__ __forceinline__ Raw16 values(const Raw& r, long long, int) const { return r; }
+};
+template <> struct Row16<true> {
+    typedef RawAny Raw;
+    const __nv_bfloat16* p;
+    long long ld, rows;
+    int F, edge;                                      // edge: rows at either end of the matrix that are not inner ones
+    __device__ __forceinline__ Row16(const __nv_bfloat16* p, long long ld, long long rows, int F) : p(p), ld(ld), rows(rows), F(F), edge(ld >= 7 ? 1 : 7) {}
+    __device__ __forceinline__ void load(Raw& r, long long row, int col) const {
+        const __nv_bfloat16* x = p + row * ld;
+        const int at = col - (int)shift_of(x) / 2;
+        const bool inner = row >= edge && row + edge < rows;
+        load_unit(r.a, x, at, F, inner);
+        if ((threadIdx.x & 31) == 31) load_unit(r.b, x, at + 8, F, inner);
+    }
+    __device__ __forceinline__ Raw16 values(const Raw& r, long long row, int col) const {
+        uint4 next = make_uint4(__shfl_down_sync(0xffffffffu, r.a.x, 1), __shfl_down_sync(0xffffffffu, r.a.y, 1), __shfl_down_sync(0xffffffffu, r.a.z, 1),
+                                __shfl_down_sync(0xffffffffu, r.a.w, 1));
+        if ((threadIdx.x & 31) == 31) next = r.b;
+        uint4 v = cut_out(r.a, next, shift_of(p + row * ld));
+        const int n = F - col;
+        if (n < 8) {                                  // zeros behind the row's end
+            unsigned w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = n > 2 * i + 1 ? w[i] : n > 2 * i ? w[i] & 0xffffu : 0u;
+            v = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+        return {v};
+    }
+};
+// n: how many of the thread's eight values exist; of its warp's, if ANY
+template <bool ANY>
+__device__ __forceinline__ void store16(__nv_bfloat16* p, const float (&x)[8], int n, uint4* image) {
+    if (ANY) store_any(p, pack_bf16x8(x), n, image);
+    else if (n > 0) store8(p, x);
+}
+__device__ __forceinline__ int valid_of(int F, int col, int of) { return min(max(F - col, 0), of); }
+template <bool ANY>
+__device__ __forceinline__ int valid_out(int F, int col) { return ANY ? valid_of(F, col & ~255, 256) : valid_of(F, col, 8); }
+template <bool ANY>
+__device__ __forceinline__ uint4* warp_image() {
+    __shared__ uint4 image[ANY ? 8 * ANY_UNITS : 1];
+    return ANY ? image + ((threadIdx.y * blockDim.x + threadIdx.x) >> 5) * ANY_UNITS : nullptr;
+}
+// the checkpoint of a thread's eight values, row group g
+__device__ __forceinline__ void keep8(const float (&x)[8], unsigned top, long long g, int col, bool live, int8_t* q, uint8_t* scales) {
+    uint2 b;
+    int sb;
+    pack8(x, top, b, sb);
+    if (!live) return;
+    *reinterpret_cast<uint2*>(q + g * ACT_GROUP + (col & 31)) = b;
+    if ((col & 31) == 0) scales[g] = (uint8_t)sb;
+}
+
+template <bool ANY>
+struct PackWork16 {
+    typedef typename Row16<ANY>::Raw In;
+    int col, G;
+    Row16<ANY> x;
+    int8_t* q;
+    uint8_t* scales;
+    __device__ __forceinline__ void load(In& in, long long r) const {
+        x.load(in, r, col);
+    }
+    __device__ __forceinline__ void work(const In& in, long long r) const {
+        const Raw16 raw = x.values(in, r, col);
+        float v[8];
+        widen(raw, v);
+        keep8(v, top_of(raw), r * G + (col >> 5), col, col < G * ACT_GROUP, q, scales);
+    }
+};
+struct PackWork32 {
+    typedef Raw32 In;
     int col, F, G;
-    const X* x;
+    const float* x;
     long long ldx;
     int8_t* q;
     uint8_t* scales;
     __device__ __forceinline__ void load(In& in, long long r) const {
-        if (col < F) load8(in, x + r * ldx + col);    // (a unit behind the row's end belongs to the padding of its last group)
+        if (col < F) load8(in, x + r * ldx + col);
     }
     __device__ __forceinline__ void work(const In& in, long long r) const {
         float v[8];
         widen(in, v);
-        uint2 b;
-        int sb;
-        pack8(v, top_of(in), b, sb);
-        const long long g = r * G + (col >> 5);
-        *reinterpret_cast<uint2*>(q + g * ACT_GROUP + (col & 31)) = b;
-        if ((col & 31) == 0) scales[g] = (uint8_t)sb;
+        keep8(v, top_of(in), r * G + (col >> 5), col, true, q, scales);
     }
 };
-template <typename X>
-__global__ void __launch_bounds__(256, PACK_CTAS) k_act_pack(ActShape s, const X* __restrict__ x, long long ldx, int8_t* __restrict__ q, uint8_t* __restrict__ scales) {
+template <bool ANY>
+__global__ void __launch_bounds__(256, PACK_CTAS) k_act_pack(ActShape s, const __nv_bfloat16* __restrict__ x, long long ldx, int8_t* __restrict__ q, uint8_t* __restrict__ scales) {
     const ActCursor c = act_cursor();
-    if (c.col >= s.G * ACT_GROUP) return;             // whole groups of four lanes leave together
-    PackWork<X> k{c.col, s.F, s.G, x, ldx, q, scales};
-    act_rows<PACK_DEPTH>(s.T, c, k);
+    if (!ANY && c.col >= s.G * ACT_GROUP) return;     // whole groups of four lanes leave together
+    PackWork16<ANY> k{c.col, s.G, Row16<ANY>(x, ldx, s.T, s.F), q, scales};
+    act_rows<ANY ? 1 : PACK_DEPTH>(s.T, c, k);
+}
+__global__ void __launch_bounds__(256, PACK_CTAS) k_act_pack32(ActShape s, const float* __restrict__ x, long long ldx, int8_t* __restrict__ q, uint8_t* __restrict__ scales) {
+    const ActCursor c = act_cursor();
+    if (c.col >= s.G * ACT_GROUP) return;
+    PackWork32 k{c.col, s.F, s.G, x, ldx, q, scales};
+    act_rows<PACK32_DEPTH>(s.T, c, k);
 }
 
 struct Kept8 { uint2 b; int scale; };
-template <typename X>
+__device__ __forceinline__ void load_kept(Kept8& k, const int8_t* q, const uint8_t* scales, long long g, int col) {
+    k.b = __ldg(reinterpret_cast<const uint2*>(q + g * ACT_GROUP + (col & 31)));
+    k.scale = __ldg(scales + g);
+}
+template <typename X, bool ANY>
 struct UnpackWork {
     typedef Kept8 In;
-    int col, G;
+    int col, out, G;
     const int8_t* q;
     const uint8_t* scales;
     X* x;
     long long ldx;
+    uint4* image;
     __device__ __forceinline__ void load(In& in, long long r) const {
-        const long long g = r * G + (col >> 5);
-        in.b = __ldg(reinterpret_cast<const uint2*>(q + g * ACT_GROUP + (col & 31)));
-        in.scale = __ldg(scales + g);
+        if (col < G * ACT_GROUP) load_kept(in, q, scales, r * G + (col >> 5), col);
     }
     __device__ __forceinline__ void work(const In& in, long long r) const {
         float v[8];
         unpack8(in.b, in.scale, v);
-        store8(x + r * ldx + col, v);
+        if constexpr (sizeof(X) == 2) store16<ANY>(x + r * ldx + col, v, out, image);
+        else store8(x + r * ldx + col, v);
     }
 };
-template <typename X>
+template <typename X, bool ANY>
 __global__ void __launch_bounds__(256, PACK_CTAS) k_act_unpack(ActShape s, const int8_t* __restrict__ q, const uint8_t* __restrict__ scales, X* __restrict__ x, long long ldx) {
     grid_trigger();                                   // (before a product in the same call)
     const ActCursor c = act_cursor();
-    if (c.col >= s.F) return;
-    UnpackWork<X> k{c.col, s.G, q, scales, x, ldx};
-    act_rows<PACK_DEPTH>(s.T, c, k);
+    if (!ANY && c.col >= s.F) return;
+    UnpackWork<X, ANY> k{c.col, valid_out<ANY>(s.F, c.col), s.G, q, scales, x, ldx, warp_image<ANY>()};
+    act_rows<ANY ? 1 : PACK_DEPTH>(s.T, c, k);
 }
 
 // h = gate sigmoid(gate) up from the unrounded inputs, both inputs packed in the same pass
@@ -239,38 +389,37 @@ struct GatedForward {
     int8_t *qg, *qu;
     uint8_t *sg, *su;
 };
+template <bool ANY>
 struct ForwardWork {
-    struct In { Raw16 g, u; };
-    int col, F, G;
+    struct In { typename Row16<ANY>::Raw g, u; };
+    int col, out, G;
+    Row16<ANY> gate, up;
     const GatedForward& a;
+    uint4* image;
     __device__ __forceinline__ void load(In& in, long long r) const {
-        if (col >= F) return;
-        load8(in.g, a.gate + r * a.ldg + col);
-        load8(in.u, a.up + r * a.ldu + col);
+        gate.load(in.g, r, col);
+        up.load(in.u, r, col);
     }
     __device__ __forceinline__ void work(const In& in, long long r) const {
+        const Raw16 rg = gate.values(in.g, r, col), ru = up.values(in.u, r, col);
         float x[8], u[8], y[8];
-        widen(in.g, x);
-        widen(in.u, u);
+        widen(rg, x);
+        widen(ru, u);
 #pragma unroll
         for (int j = 0; j < 8; ++j) y[j] = x[j] * sigmoid(x[j]) * u[j];
-        if (col < F) store8(a.h + r * a.ldh + col, y);
-        const long long g = r * G + (col >> 5), at = g * ACT_GROUP + (col & 31);
-        uint2 b;
-        int sb;
-        pack8(x, top_of(in.g), b, sb);
-        *reinterpret_cast<uint2*>(a.qg + at) = b;
-        if ((col & 31) == 0) a.sg[g] = (uint8_t)sb;
-        pack8(u, top_of(in.u), b, sb);
-        *reinterpret_cast<uint2*>(a.qu + at) = b;
-        if ((col & 31) == 0) a.su[g] = (uint8_t)sb;
+        store16<ANY>(a.h + r * a.ldh + col, y, out, image);
+        const long long g = r * G + (col >> 5);
+        const bool live = !ANY || col < G * ACT_GROUP;
+        keep8(x, top_of(rg), g, col, live, a.qg, a.sg);
+        keep8(u, top_of(ru), g, col, live, a.qu, a.su);
     }
 };
+template <bool ANY>
 __global__ void __launch_bounds__(256, FORWARD_CTAS) k_swiglu_forward(ActShape s, const __grid_constant__ GatedForward a) {
     const ActCursor c = act_cursor();
-    if (c.col >= s.G * ACT_GROUP) return;
-    ForwardWork k{c.col, s.F, s.G, a};
-    act_rows<FORWARD_DEPTH>(s.T, c, k);
+    if (!ANY && c.col >= s.G * ACT_GROUP) return;
+    ForwardWork<ANY> k{c.col, valid_out<ANY>(s.F, c.col), s.G, Row16<ANY>(a.gate, a.ldg, s.T, s.F), Row16<ANY>(a.up, a.ldu, s.T, s.F), a, warp_image<ANY>()};
+    act_rows<ANY ? 1 : FORWARD_DEPTH>(s.T, c, k);
 }
 
 // d_gate = dh up s (1 + gate (1 - s)),  d_up = dh gate s,  h = gate s up  (s = sigmoid(gate)), gate and up from their checkpoints
@@ -281,40 +430,58 @@ struct GatedBackward {
     __nv_bfloat16 *dg, *du, *h;
     long long lddh, lddg, lddu, ldh;
 };
-template <bool H>
+template <bool H, bool ANY>
 struct BackwardWork {
-    struct In { Raw16 d; Kept8 g, u; };
-    int col, G;
+    struct In { typename Row16<ANY>::Raw d; Kept8 g, u; };
+    int col, out, G;
+    Row16<ANY> dh;
     const GatedBackward& a;
+    uint4* image;
     __device__ __forceinline__ void load(In& in, long long r) const {
-        const long long g = r * G + (col >> 5), at = g * ACT_GROUP + (col & 31);
-        load8(in.d, a.dh + r * a.lddh + col);
-        in.g.b = __ldg(reinterpret_cast<const uint2*>(a.qg + at));
-        in.u.b = __ldg(reinterpret_cast<const uint2*>(a.qu + at));
-        in.g.scale = __ldg(a.sg + g);
-        in.u.scale = __ldg(a.su + g);
+        dh.load(in.d, r, col);
+        if (col >= G * ACT_GROUP) return;
+        const long long g = r * G + (col >> 5);
+        load_kept(in.g, a.qg, a.sg, g, col);
+        load_kept(in.u, a.qu, a.su, g, col);
     }
     __device__ __forceinline__ void work(const In& in, long long r) const {
         float d[8], x[8], u[8], o[8], p[8], y[8];
-        widen(in.d, d);
+        widen(dh.values(in.d, r, col), d);
         unpack8(in.g.b, in.g.scale, x);
         unpack8(in.u.b, in.u.scale, u);
 #pragma unroll
         for (int j = 0; j < 8; ++j) gated_backward(d[j], x[j], u[j], o[j], p[j], y[j]);
-        store8(a.dg + r * a.lddg + col, o);
-        store8(a.du + r * a.lddu + col, p);
-        if (H) store8(a.h + r * a.ldh + col, y);
+        store16<ANY>(a.dg + r * a.lddg + col, o, out, image);
+        store16<ANY>(a.du + r * a.lddu + col, p, out, image);
+        if (H) store16<ANY>(a.h + r * a.ldh + col, y, out, image);
     }
 };
-template <bool H>
+template <bool H, bool ANY>
 __global__ void __launch_bounds__(256, BACKWARD_CTAS) k_swiglu_backward(ActShape s, const __grid_constant__ GatedBackward a) {
     const ActCursor c = act_cursor();
-    if (c.col >= s.F) return;
-    BackwardWork<H> k{c.col, s.G, a};
-    act_rows<BACKWARD_DEPTH>(s.T, c, k);
+    if (!ANY && c.col >= s.F) return;
+    BackwardWork<H, ANY> k{c.col, valid_out<ANY>(s.F, c.col), s.G, Row16<ANY>(a.dh, a.lddh, s.T, s.F), a, warp_image<ANY>()};
+    act_rows<ANY ? 1 : BACKWARD_DEPTH>(s.T, c, k);
 }
 
-// ---- any length and alignment: a lane per value, a warp per group, LANE_GROUPS groups of a row at a time ----
+// rows of 16-bit values to another alignment and row stride
+struct CopyWork {
+    typedef RawAny In;
+    int col, out;
+    Row16<true> src;
+    __nv_bfloat16* dst;
+    long long ldd;
+    uint4* image;
+    __device__ __forceinline__ void load(In& in, long long r) const { src.load(in, r, col); }
+    __device__ __forceinline__ void work(const In& in, long long r) const { store_any(dst + r * ldd + col, src.values(in, r, col).a, out, image); }
+};
+__global__ void __launch_bounds__(256, PACK_CTAS) k_copy_rows(ActShape s, const __nv_bfloat16* __restrict__ src, long long lds, __nv_bfloat16* __restrict__ dst, long long ldd) {
+    const ActCursor c = act_cursor();
+    CopyWork k{c.col, valid_out<true>(s.F, c.col), Row16<true>(src, lds, s.T, s.F), dst, ldd, warp_image<true>()};
+    act_rows<1>(s.T, c, k);
+}
+
+// ---- float32 rows of any length and alignment: a lane per value, a warp per group, LANE_GROUPS groups of a row at a time ----
 // blockDim = (32, 8); blockIdx.x, threadIdx.y: groups of a row, blockIdx.y: rows
 constexpr int LANE_GROUPS = 4;
 template <typename Body>
@@ -323,31 +490,26 @@ __device__ __forceinline__ void lane_groups(const ActShape& s, Body&& body) {
     if (g0 >= s.G) return;
     for (long long r = blockIdx.y; r < s.T; r += gridDim.y) body(r, g0);
 }
-// the checkpoint of LANE_GROUPS groups whose values the lanes hold (zeros behind the row's end)
-__device__ __forceinline__ void pack_lanes(const float (&x)[LANE_GROUPS], long long row_group, int g0, int G, int8_t* q, uint8_t* scales) {
-#pragma unroll
-    for (int i = 0; i < LANE_GROUPS; ++i) {
-        if (g0 + i >= G) break;
-        const GroupScale s = group_scale(__reduce_max_sync(0xffffffffu, __float_as_uint(x[i]) & 0x7fffffffu));
-        const unsigned b = s.over ? quantize_clamped(x[i], s) : quantize(x[i], s);
-        q[(row_group + i) * ACT_GROUP + threadIdx.x] = (int8_t)(s.fine ? b & 0xffu : 0u);
-        if (threadIdx.x == 0) scales[row_group + i] = (uint8_t)s.byte;
-    }
-}
-template <typename X>
-__global__ void __launch_bounds__(256) k_act_pack_any(ActShape s, const X* __restrict__ x, long long ldx, int8_t* __restrict__ q, uint8_t* __restrict__ scales) {
+__global__ void __launch_bounds__(256) k_act_pack32_any(ActShape s, const float* __restrict__ x, long long ldx, int8_t* __restrict__ q, uint8_t* __restrict__ scales) {
     lane_groups(s, [&](long long r, int g0) {
         float v[LANE_GROUPS];
 #pragma unroll
         for (int i = 0; i < LANE_GROUPS; ++i) {
             const int col = (g0 + i) * ACT_GROUP + threadIdx.x;
-            v[i] = col < s.F ? load1(x + r * ldx + col) : 0.f;
+            v[i] = col < s.F ? __ldg(x + r * ldx + col) : 0.f;             // zeros behind the row's end
         }
-        pack_lanes(v, r * s.G + g0, g0, s.G, q, scales);
+#pragma unroll
+        for (int i = 0; i < LANE_GROUPS; ++i) {
+            if (g0 + i >= s.G) break;
+            const long long g = r * s.G + g0 + i;
+            const GroupScale gs = group_scale(__reduce_max_sync(0xffffffffu, __float_as_uint(v[i]) & 0x7fffffffu));
+            const unsigned b = gs.over ? quantize_clamped(v[i], gs) : quantize(v[i], gs);
+            q[g * ACT_GROUP + threadIdx.x] = (int8_t)(gs.fine ? b & 0xffu : 0u);
+            if (threadIdx.x == 0) scales[g] = (uint8_t)gs.byte;
+        }
     });
 }
-template <typename X>
-__global__ void __launch_bounds__(256) k_act_unpack_any(ActShape s, const int8_t* __restrict__ q, const uint8_t* __restrict__ scales, X* __restrict__ x, long long ldx) {
+__global__ void __launch_bounds__(256) k_act_unpack32_any(ActShape s, const int8_t* __restrict__ q, const uint8_t* __restrict__ scales, float* __restrict__ x, long long ldx) {
     lane_groups(s, [&](long long r, int g0) {
         float v[LANE_GROUPS];
 #pragma unroll
@@ -358,67 +520,7 @@ __global__ void __launch_bounds__(256) k_act_unpack_any(ActShape s, const int8_t
 #pragma unroll
         for (int i = 0; i < LANE_GROUPS; ++i) {
             const int col = (g0 + i) * ACT_GROUP + threadIdx.x;
-            if (col < s.F) store1(x + r * ldx + col, v[i]);
-        }
-    });
-}
-__global__ void __launch_bounds__(256) k_swiglu_forward_any(ActShape s, const __grid_constant__ GatedForward a) {
-    lane_groups(s, [&](long long r, int g0) {
-        float x[LANE_GROUPS], u[LANE_GROUPS];
-#pragma unroll
-        for (int i = 0; i < LANE_GROUPS; ++i) {
-            const int col = (g0 + i) * ACT_GROUP + threadIdx.x;
-            x[i] = col < s.F ? load1(a.gate + r * a.ldg + col) : 0.f;
-            u[i] = col < s.F ? load1(a.up + r * a.ldu + col) : 0.f;
-        }
-#pragma unroll
-        for (int i = 0; i < LANE_GROUPS; ++i) {
-            const int col = (g0 + i) * ACT_GROUP + threadIdx.x;
-            if (col < s.F) store1(a.h + r * a.ldh + col, x[i] * sigmoid(x[i]) * u[i]);
-        }
-        pack_lanes(x, r * s.G + g0, g0, s.G, a.qg, a.sg);
-        pack_lanes(u, r * s.G + g0, g0, s.G, a.qu, a.su);
-    });
-}
-template <bool H>
-__global__ void __launch_bounds__(256) k_swiglu_backward_any(ActShape s, const __grid_constant__ GatedBackward a) {
-    lane_groups(s, [&](long long r, int g0) {
-        float d[LANE_GROUPS], x[LANE_GROUPS], u[LANE_GROUPS];
-#pragma unroll
-        for (int i = 0; i < LANE_GROUPS; ++i) {
-            const int col = (g0 + i) * ACT_GROUP + threadIdx.x;
-            const long long g = r * s.G + min(g0 + i, s.G - 1);
-            d[i] = col < s.F ? load1(a.dh + r * a.lddh + col) : 0.f;
-            x[i] = (float)__ldg(a.qg + g * ACT_GROUP + threadIdx.x) * scale_of(__ldg(a.sg + g));
-            u[i] = (float)__ldg(a.qu + g * ACT_GROUP + threadIdx.x) * scale_of(__ldg(a.su + g));
-        }
-#pragma unroll
-        for (int i = 0; i < LANE_GROUPS; ++i) {
-            const int col = (g0 + i) * ACT_GROUP + threadIdx.x;
-            float o, p, y;
-            gated_backward(d[i], x[i], u[i], o, p, y);
-            if (col < s.F) {
-                store1(a.dg + r * a.lddg + col, o);
-                store1(a.du + r * a.lddu + col, p);
-                if (H) store1(a.h + r * a.ldh + col, y);
-            }
-        }
-    });
-}
-
-// rows of 16-bit values to another alignment and row stride
-__global__ void __launch_bounds__(256) k_copy_rows(ActShape s, const unsigned short* __restrict__ src, long long lds, unsigned short* __restrict__ dst, long long ldd) {
-    lane_groups(s, [&](long long r, int g0) {
-        unsigned short v[LANE_GROUPS];
-#pragma unroll
-        for (int i = 0; i < LANE_GROUPS; ++i) {
-            const int col = (g0 + i) * ACT_GROUP + threadIdx.x;
-            v[i] = col < s.F ? __ldg(src + r * lds + col) : (unsigned short)0;
-        }
-#pragma unroll
-        for (int i = 0; i < LANE_GROUPS; ++i) {
-            const int col = (g0 + i) * ACT_GROUP + threadIdx.x;
-            if (col < s.F) dst[r * ldd + col] = v[i];
+            if (col < s.F) x[r * ldx + col] = v[i];
         }
     });
 }

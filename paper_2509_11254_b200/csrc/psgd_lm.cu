@@ -328,10 +328,10 @@ psgd_status xent(const void* H, int64_t ldh, const void* W, int64_t ldw, const i
 
 // ---- 8-bit activations ----
 struct ActGrid { dim3 grid, block; };
-// 256 threads: a row's units side by side, as many rows as fit; CTAs for `resident` of them per multiprocessor
-ActGrid act_grid(int64_t T, int G, int resident) {
+// 256 threads, CTAs for `resident` of them per multiprocessor: a row's units side by side, as many rows as fit.  `any`: a warp per 32 units of a row.
+ActGrid act_grid(int64_t T, int G, int resident, bool any) {
     const int units = 4 * G, across = ceil_div(units, 256);
-    const int bx = (int)align_up(ceil_div(units, across), 4);
+    const int bx = any ? 32 : (int)align_up(ceil_div(units, across), 4);
     const int by = std::max(1, 256 / bx);
     const int nx = ceil_div(units, bx);
     const int64_t y = std::min<int64_t>({ceil_div(T, by), 65535, std::max(1, device_sms() * resident / nx)});
@@ -346,17 +346,29 @@ ActGrid lane_grid(int64_t T, int G) {
 bool act_ok(int64_t T, int64_t F) { return T >= 0 && T <= MAX_EXTENT && extent_ok(F); }
 bool vec8(const void* p, int64_t ld, int64_t F, int dtype) { return F % 8 == 0 && aligned16(p) && ld % (dtype == PSGD_DT_BF16 ? 8 : 4) == 0; }
 
-template <typename X>
-void launch_pack(const ActShape& s, const X* x, int64_t ldx, bool vec, int8_t* q, uint8_t* scales, cudaStream_t st) {
-    const ActGrid g = vec ? act_grid(s.T, s.G, PACK_CTAS) : lane_grid(s.T, s.G);
-    if (vec) k_act_pack<X><<<g.grid, g.block, 0, st>>>(s, x, ldx, q, scales);
-    else k_act_pack_any<X><<<g.grid, g.block, 0, st>>>(s, x, ldx, q, scales);
+void launch_pack(const ActShape& s, const void* x, int64_t ldx, int dtype, int8_t* q, uint8_t* scales, cudaStream_t st) {
+    const bool vec = vec8(x, ldx, s.F, dtype);
+    const auto run = [&](auto kernel, const ActGrid& g, auto* p) { kernel<<<g.grid, g.block, 0, st>>>(s, p, ldx, q, scales); };
+    if (dtype == PSGD_DT_BF16) {
+        const ActGrid g = act_grid(s.T, s.G, PACK_CTAS, !vec);
+        run(vec ? k_act_pack<false> : k_act_pack<true>, g, (const __nv_bfloat16*)x);
+    } else if (vec) {
+        run(k_act_pack32, act_grid(s.T, s.G, PACK_CTAS, false), (const float*)x);
+    } else {
+        run(k_act_pack32_any, lane_grid(s.T, s.G), (const float*)x);
+    }
 }
-template <typename X>
-void launch_unpack(const ActShape& s, const int8_t* q, const uint8_t* scales, X* x, int64_t ldx, bool vec, cudaStream_t st) {
-    const ActGrid g = vec ? act_grid(s.T, s.G, PACK_CTAS) : lane_grid(s.T, s.G);
-    if (vec) k_act_unpack<X><<<g.grid, g.block, 0, st>>>(s, q, scales, x, ldx);
-    else k_act_unpack_any<X><<<g.grid, g.block, 0, st>>>(s, q, scales, x, ldx);
+void launch_unpack(const ActShape& s, const int8_t* q, const uint8_t* scales, void* x, int64_t ldx, int dtype, cudaStream_t st) {
+    const bool vec = vec8(x, ldx, s.F, dtype);
+    const auto run = [&](auto kernel, const ActGrid& g, auto* p) { kernel<<<g.grid, g.block, 0, st>>>(s, q, scales, p, ldx); };
+    if (dtype == PSGD_DT_BF16) {
+        const ActGrid g = act_grid(s.T, s.G, PACK_CTAS, !vec);
+        run(vec ? k_act_unpack<__nv_bfloat16, false> : k_act_unpack<__nv_bfloat16, true>, g, (__nv_bfloat16*)x);
+    } else if (vec) {
+        run(k_act_unpack<float, false>, act_grid(s.T, s.G, PACK_CTAS, false), (float*)x);
+    } else {
+        run(k_act_unpack32_any, lane_grid(s.T, s.G), (float*)x);
+    }
 }
 bool dtype_ok(int dtype) { return dtype == PSGD_DT_F32 || dtype == PSGD_DT_BF16; }
 bool ckpt_ok(const void* q) { return ((uintptr_t)q & 15) == 0; }
@@ -417,9 +429,7 @@ psgd_status psgd_act_pack(const void* x, int64_t ldx, int dtype, int64_t T, int6
     if (!x || !q || !scales) return PSGD_E_NULL;
     if (ldx < F || !ckpt_ok(q)) return PSGD_E_INVALID;
     const ActShape s{T, (int)F, ceil_div(F, ACT_GROUP)};
-    const bool vec = vec8(x, ldx, F, dtype);
-    if (dtype == PSGD_DT_BF16) launch_pack(s, (const __nv_bfloat16*)x, ldx, vec, q, scales, (cudaStream_t)stream);
-    else launch_pack(s, (const float*)x, ldx, vec, q, scales, (cudaStream_t)stream);
+    launch_pack(s, x, ldx, dtype, q, scales, (cudaStream_t)stream);
     return last_error();
 }
 
@@ -429,9 +439,7 @@ psgd_status psgd_act_unpack(const int8_t* q, const uint8_t* scales, int64_t T, i
     if (!x || !q || !scales) return PSGD_E_NULL;
     if (ldx < F || !ckpt_ok(q)) return PSGD_E_INVALID;
     const ActShape s{T, (int)F, ceil_div(F, ACT_GROUP)};
-    const bool vec = vec8(x, ldx, F, dtype);
-    if (dtype == PSGD_DT_BF16) launch_unpack(s, q, scales, (__nv_bfloat16*)x, ldx, vec, (cudaStream_t)stream);
-    else launch_unpack(s, q, scales, (float*)x, ldx, vec, (cudaStream_t)stream);
+    launch_unpack(s, q, scales, x, ldx, dtype, (cudaStream_t)stream);
     return last_error();
 }
 
@@ -441,8 +449,8 @@ psgd_status psgd_copy_rows(const void* src, int64_t lds, int64_t rows, int64_t c
     if (!src || !dst) return PSGD_E_NULL;
     if (lds < cols || ldd < cols) return PSGD_E_INVALID;
     const ActShape s{rows, (int)cols, ceil_div(cols, ACT_GROUP)};
-    const ActGrid g = lane_grid(rows, s.G);
-    k_copy_rows<<<g.grid, g.block, 0, (cudaStream_t)stream>>>(s, (const unsigned short*)src, lds, (unsigned short*)dst, ldd);
+    const ActGrid g = act_grid(rows, s.G, PACK_CTAS, true);
+    k_copy_rows<<<g.grid, g.block, 0, (cudaStream_t)stream>>>(s, (const __nv_bfloat16*)src, lds, (__nv_bfloat16*)dst, ldd);
     return last_error();
 }
 
@@ -469,7 +477,7 @@ psgd_status psgd_act_wgrad(const void* dY, int64_t lddy, const int8_t* q, const 
     if (ws_bytes < g.total) return PSGD_E_WORKSPACE;
     char* w = (char*)ws;
     const ActShape s{T, (int)F, ceil_div(F, ACT_GROUP)};
-    launch_unpack(ActShape{T, (int)g.ldx, s.G}, q, scales, (__nv_bfloat16*)(w + g.x), g.ldx, true, st);     // the padding too: its values are zeros
+    launch_unpack(ActShape{T, (int)g.ldx, s.G}, q, scales, w + g.x, g.ldx, PSGD_DT_BF16, st);     // the padding too: its values are zeros
     TileArgs a{};
     a.status = status ? status : (int*)w;
     TileProblem& t = a.p[0];
@@ -493,9 +501,9 @@ psgd_status psgd_swiglu_forward(const void* gate, int64_t ldg, const void* up, i
     const ActShape s{T, (int)F, ceil_div(F, ACT_GROUP)};
     const GatedForward a{(const __nv_bfloat16*)gate, (const __nv_bfloat16*)up, (__nv_bfloat16*)h, ldg, ldu, ldh, q_gate, q_up, s_gate, s_up};
     const bool vec = vec8(gate, ldg, F, PSGD_DT_BF16) && vec8(up, ldu, F, PSGD_DT_BF16) && vec8(h, ldh, F, PSGD_DT_BF16);
-    const ActGrid g = vec ? act_grid(T, s.G, FORWARD_CTAS) : lane_grid(T, s.G);
-    if (vec) k_swiglu_forward<<<g.grid, g.block, 0, (cudaStream_t)stream>>>(s, a);
-    else k_swiglu_forward_any<<<g.grid, g.block, 0, (cudaStream_t)stream>>>(s, a);
+    const ActGrid g = act_grid(T, s.G, FORWARD_CTAS, !vec);
+    const auto kernel = vec ? k_swiglu_forward<false> : k_swiglu_forward<true>;
+    kernel<<<g.grid, g.block, 0, (cudaStream_t)stream>>>(s, a);
     return last_error();
 }
 
@@ -508,10 +516,10 @@ psgd_status psgd_swiglu_backward(const void* dh, int64_t lddh, const int8_t* q_g
     const ActShape s{T, (int)F, ceil_div(F, ACT_GROUP)};
     const GatedBackward a{(const __nv_bfloat16*)dh, q_gate, q_up, s_gate, s_up, (__nv_bfloat16*)d_gate, (__nv_bfloat16*)d_up, (__nv_bfloat16*)h, lddh, ldg, ldu, ldh};
     const bool vec = vec8(dh, lddh, F, PSGD_DT_BF16) && vec8(d_gate, ldg, F, PSGD_DT_BF16) && vec8(d_up, ldu, F, PSGD_DT_BF16) && (!h || vec8(h, ldh, F, PSGD_DT_BF16));
-    const ActGrid g = vec ? act_grid(T, s.G, BACKWARD_CTAS) : lane_grid(T, s.G);
+    const ActGrid g = act_grid(T, s.G, BACKWARD_CTAS, !vec);
     const auto run = [&](auto kernel) { kernel<<<g.grid, g.block, 0, (cudaStream_t)stream>>>(s, a); };
-    if (h) vec ? run(k_swiglu_backward<true>) : run(k_swiglu_backward_any<true>);
-    else vec ? run(k_swiglu_backward<false>) : run(k_swiglu_backward_any<false>);
+    if (h) run(vec ? k_swiglu_backward<true, false> : k_swiglu_backward<true, true>);
+    else run(vec ? k_swiglu_backward<false, false> : k_swiglu_backward<false, true>);
     return last_error();
 }
 

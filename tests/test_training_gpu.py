@@ -584,6 +584,43 @@ def test_c_entry_points_refuse(torch, ops):
     assert L.psgd_swiglu_backward(h.data_ptr(), 64, None, None, None, None, 8, 64, dh.data_ptr(), 64, dh.data_ptr(), 64, None, 0, None) == -2
 
 
+@pytest.mark.parametrize("T", [1, 2, 3, 19])
+@pytest.mark.parametrize("F", [1, 2, 5, 7, 8, 9, 31, 33, 250, 256, 257, 263, 505, 521, 1031])
+def test_rows_of_any_alignment_equal_aligned_ones(torch, ops, T, F):
+    """Every start within 16 bytes and strides that move it from row to row: the same bits as from aligned copies, and nothing around the rows changes."""
+    g = gen(torch, 100 * F + T)
+    wide = (F + 7) // 8 * 8
+    for start, gap in [(0, 0), (1, 0), (2, 1), (3, 2), (5, 3), (6, 4), (7, 7), (8, 1), (4, 8)]:
+        ld = F + gap
+        flat = torch.randn(start + T * ld + 16, generator=g, device="cuda").to(torch.bfloat16)
+        x, y = (flat.as_strided((T, F), (ld, 1), start), flat.as_strided((T, F), (ld, 1), start + (1 if gap else 0)))
+
+        def aligned(t):                             # padded with zeros to whole units of 8: the same groups, the same values
+            a = torch.zeros(T, wide, device="cuda", dtype=torch.bfloat16)
+            a[:, :F] = t
+            return a
+
+        ax, ay = aligned(x), aligned(y)
+        k, ak = ops.pack_activation(x), ops.pack_activation(ax)
+        assert torch.equal(k.q, ak.q) and torch.equal(k.scales, ak.scales)
+        out = torch.full((start + T * ld + 24,), 7.0, device="cuda", dtype=torch.bfloat16)
+        before = out.clone()
+        view = out.as_strided((T, F), (ld, 1), start)
+        k.unpack(out=view)
+        assert torch.equal(view, ak.unpack()[:, :F])
+        view.copy_(before.as_strided((T, F), (ld, 1), start))
+        assert torch.equal(out, before)
+        h, kg, ku = ops.swiglu_forward(x, y)
+        ah, akg, aku = ops.swiglu_forward(ax, ay)
+        assert torch.equal(h, ah[:, :F]) and torch.equal(kg.q, akg.q) and torch.equal(ku.q, aku.q) and torch.equal(kg.scales, akg.scales) and torch.equal(ku.scales, aku.scales)
+        for a, b in zip(ops.swiglu_backward(x, kg, ku, recompute=True), ops.swiglu_backward(ax, akg, aku, recompute=True)):
+            assert torch.equal(a, b[:, :F])
+        for a, b in zip(ops.swiglu_backward(y, kg, ku), ops.swiglu_backward(ay, akg, aku)):
+            assert torch.equal(a, b[:, :F])
+        dw, adw = ops.weight_gradient(y, k), ops.weight_gradient(ay, ak)
+        assert torch.equal(dw, adw[:F, :F])
+
+
 # ---- streams, graphs, long offsets --------------------------------------------------------------------------------
 def test_calls_on_two_streams_at_once(torch, ops):
     sets = [xent_inputs(torch, 700, 3000, 256, seed=s) for s in (21, 22)]
