@@ -30,10 +30,10 @@ struct ActShape { long long T; int F, G; };      // G = groups per row; the int8
 // Eight values as they lie in memory, and as float32.
 struct Raw16 { uint4 a; };
 struct Raw32 { float4 a, b; };
-__device__ __forceinline__ void load8(Raw16& r, const __nv_bfloat16* p) { r.a = __ldg(reinterpret_cast<const uint4*>(p)); }
+__device__ __forceinline__ void load8(Raw16& r, const __nv_bfloat16* p) { r.a = *reinterpret_cast<const uint4*>(p); }
 __device__ __forceinline__ void load8(Raw32& r, const float* p) {
-    r.a = __ldg(reinterpret_cast<const float4*>(p));
-    r.b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+    r.a = *reinterpret_cast<const float4*>(p);
+    r.b = reinterpret_cast<const float4*>(p)[1];
 }
 __device__ __forceinline__ void widen(const Raw16& r, float (&x)[8]) {
     const unsigned w[4] = {r.a.x, r.a.y, r.a.z, r.a.w};
@@ -67,7 +67,7 @@ __device__ __forceinline__ unsigned shift_of(const __nv_bfloat16* p) { return (u
 __device__ __forceinline__ void load_unit(uint4& u, const __nv_bfloat16* row, int at, int len, bool inner) {
     if (at >= len) return;
     if (inner) {
-        u = __ldg(reinterpret_cast<const uint4*>(row + at));
+        u = *reinterpret_cast<const uint4*>(row + at);
         return;
     }
     const unsigned short* h = reinterpret_cast<const unsigned short*>(row);
@@ -75,7 +75,7 @@ __device__ __forceinline__ void load_unit(uint4& u, const __nv_bfloat16* row, in
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int j = at + 2 * i;
-        const unsigned x = j >= 0 && j < len ? __ldg(h + j) : 0u, y = j + 1 >= 0 && j + 1 < len ? __ldg(h + j + 1) : 0u;
+        const unsigned x = j >= 0 && j < len ? h[j] : 0u, y = j + 1 >= 0 && j + 1 < len ? h[j + 1] : 0u;
         w[i] = x | y << 16;
     }
     u = make_uint4(w[0], w[1], w[2], w[3]);
@@ -212,6 +212,8 @@ __device__ __forceinline__ void gated_backward(float d, float g, float u, float&
 constexpr int PACK_DEPTH = 4, PACK32_DEPTH = 2, PACK_CTAS = 4, FORWARD_DEPTH = 3, FORWARD_CTAS = 3, BACKWARD_DEPTH = 2, BACKWARD_CTAS = 3;
 struct ActCursor { int col; long long row, step; };
 __device__ __forceinline__ ActCursor act_cursor() {
+    grid_trigger();
+    grid_wait();
     ActCursor c;
     c.col = (blockIdx.x * blockDim.x + threadIdx.x) * 8;
     c.row = (long long)blockIdx.y * blockDim.y + threadIdx.y;
@@ -335,13 +337,13 @@ struct PackWork32 {
     }
 };
 template <bool ANY>
-__global__ void __launch_bounds__(256, PACK_CTAS) k_act_pack(ActShape s, const __nv_bfloat16* __restrict__ x, long long ldx, int8_t* __restrict__ q, uint8_t* __restrict__ scales) {
+__global__ void __launch_bounds__(256, PACK_CTAS) k_act_pack(ActShape s, const __nv_bfloat16* x, long long ldx, int8_t* q, uint8_t* scales) {
     const ActCursor c = act_cursor();
     if (!ANY && c.col >= s.G * ACT_GROUP) return;     // whole groups of four lanes leave together
     PackWork16<ANY> k{c.col, s.G, Row16<ANY>(x, ldx, s.T, s.F), q, scales};
     act_rows<ANY ? 1 : PACK_DEPTH>(s.T, c, k);
 }
-__global__ void __launch_bounds__(256, PACK_CTAS) k_act_pack32(ActShape s, const float* __restrict__ x, long long ldx, int8_t* __restrict__ q, uint8_t* __restrict__ scales) {
+__global__ void __launch_bounds__(256, PACK_CTAS) k_act_pack32(ActShape s, const float* x, long long ldx, int8_t* q, uint8_t* scales) {
     const ActCursor c = act_cursor();
     if (c.col >= s.G * ACT_GROUP) return;
     PackWork32 k{c.col, s.F, s.G, x, ldx, q, scales};
@@ -350,8 +352,8 @@ __global__ void __launch_bounds__(256, PACK_CTAS) k_act_pack32(ActShape s, const
 
 struct Kept8 { uint2 b; int scale; };
 __device__ __forceinline__ void load_kept(Kept8& k, const int8_t* q, const uint8_t* scales, long long g, int col) {
-    k.b = __ldg(reinterpret_cast<const uint2*>(q + g * ACT_GROUP + (col & 31)));
-    k.scale = __ldg(scales + g);
+    k.b = *reinterpret_cast<const uint2*>(q + g * ACT_GROUP + (col & 31));
+    k.scale = scales[g];
 }
 template <typename X, bool ANY>
 struct UnpackWork {
@@ -373,8 +375,7 @@ struct UnpackWork {
     }
 };
 template <typename X, bool ANY>
-__global__ void __launch_bounds__(256, PACK_CTAS) k_act_unpack(ActShape s, const int8_t* __restrict__ q, const uint8_t* __restrict__ scales, X* __restrict__ x, long long ldx) {
-    grid_trigger();                                   // (before a product in the same call)
+__global__ void __launch_bounds__(256, PACK_CTAS) k_act_unpack(ActShape s, const int8_t* q, const uint8_t* scales, X* x, long long ldx) {
     const ActCursor c = act_cursor();
     if (!ANY && c.col >= s.F) return;
     UnpackWork<X, ANY> k{c.col, valid_out<ANY>(s.F, c.col), s.G, q, scales, x, ldx, warp_image<ANY>()};
@@ -475,7 +476,7 @@ struct CopyWork {
     __device__ __forceinline__ void load(In& in, long long r) const { src.load(in, r, col); }
     __device__ __forceinline__ void work(const In& in, long long r) const { store_any(dst + r * ldd + col, src.values(in, r, col).a, out, image); }
 };
-__global__ void __launch_bounds__(256, PACK_CTAS) k_copy_rows(ActShape s, const __nv_bfloat16* __restrict__ src, long long lds, __nv_bfloat16* __restrict__ dst, long long ldd) {
+__global__ void __launch_bounds__(256, PACK_CTAS) k_copy_rows(ActShape s, const __nv_bfloat16* src, long long lds, __nv_bfloat16* dst, long long ldd) {
     const ActCursor c = act_cursor();
     CopyWork k{c.col, valid_out<true>(s.F, c.col), Row16<true>(src, lds, s.T, s.F), dst, ldd, warp_image<true>()};
     act_rows<1>(s.T, c, k);
@@ -486,17 +487,19 @@ __global__ void __launch_bounds__(256, PACK_CTAS) k_copy_rows(ActShape s, const 
 constexpr int LANE_GROUPS = 4;
 template <typename Body>
 __device__ __forceinline__ void lane_groups(const ActShape& s, Body&& body) {
+    grid_trigger();
+    grid_wait();
     const int g0 = (blockIdx.x * 8 + threadIdx.y) * LANE_GROUPS;
     if (g0 >= s.G) return;
     for (long long r = blockIdx.y; r < s.T; r += gridDim.y) body(r, g0);
 }
-__global__ void __launch_bounds__(256) k_act_pack32_any(ActShape s, const float* __restrict__ x, long long ldx, int8_t* __restrict__ q, uint8_t* __restrict__ scales) {
+__global__ void __launch_bounds__(256) k_act_pack32_any(ActShape s, const float* x, long long ldx, int8_t* q, uint8_t* scales) {
     lane_groups(s, [&](long long r, int g0) {
         float v[LANE_GROUPS];
 #pragma unroll
         for (int i = 0; i < LANE_GROUPS; ++i) {
             const int col = (g0 + i) * ACT_GROUP + threadIdx.x;
-            v[i] = col < s.F ? __ldg(x + r * ldx + col) : 0.f;             // zeros behind the row's end
+            v[i] = col < s.F ? x[r * ldx + col] : 0.f;             // zeros behind the row's end
         }
 #pragma unroll
         for (int i = 0; i < LANE_GROUPS; ++i) {
@@ -509,13 +512,13 @@ __global__ void __launch_bounds__(256) k_act_pack32_any(ActShape s, const float*
         }
     });
 }
-__global__ void __launch_bounds__(256) k_act_unpack32_any(ActShape s, const int8_t* __restrict__ q, const uint8_t* __restrict__ scales, float* __restrict__ x, long long ldx) {
+__global__ void __launch_bounds__(256) k_act_unpack32_any(ActShape s, const int8_t* q, const uint8_t* scales, float* x, long long ldx) {
     lane_groups(s, [&](long long r, int g0) {
         float v[LANE_GROUPS];
 #pragma unroll
         for (int i = 0; i < LANE_GROUPS; ++i) {
             const long long g = r * s.G + min(g0 + i, s.G - 1);
-            v[i] = (float)__ldg(q + g * ACT_GROUP + threadIdx.x) * scale_of(__ldg(scales + g));
+            v[i] = (float)q[g * ACT_GROUP + threadIdx.x] * scale_of(scales[g]);
         }
 #pragma unroll
         for (int i = 0; i < LANE_GROUPS; ++i) {

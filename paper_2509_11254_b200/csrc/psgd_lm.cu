@@ -113,16 +113,16 @@ void set_problem(TileProblem& t, const TilePlan& p) {
 }
 
 // Launch that may start before the kernel in front of it on the stream has finished (the kernels wait for that themselves).
-template <typename... Args>
-bool launch_after(void (*kernel)(Args...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, bool early, const Args&... args) {
+template <typename... Params, typename... Args>
+bool launch(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, const Args&... args) {
     cudaLaunchConfig_t c{};
     c.gridDim = grid; c.blockDim = block; c.dynamicSmemBytes = smem; c.stream = st;
     cudaLaunchAttribute at{};
     at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at.val.programmaticStreamSerializationAllowed = 1;
     c.attrs = &at;
-    c.numAttrs = early ? 1 : 0;
-    if (cudaLaunchKernelEx(&c, kernel, args...) == cudaSuccess) return true;
+    c.numAttrs = 1;
+    if (cudaLaunchKernelEx(&c, kernel, Params(args)...) == cudaSuccess) return true;
     cudaGetLastError();                               // not left for whoever asks next
     return false;
 }
@@ -134,7 +134,7 @@ bool encode(CUtensorMap* map, const Operand& o, int64_t rows, int64_t K, int box
 
 // One product of K-major operands with a softmax epilogue.
 template <int EPI>
-psgd_status launch_softmax(const Operand& A, const Operand& B, const TilePlan& p, TileArgs& a, int pairs, bool early, cudaStream_t st) {
+psgd_status launch_softmax(const Operand& A, const Operand& B, const TilePlan& p, TileArgs& a, int pairs, cudaStream_t st) {
     CUtensorMap ma, mb;
     // Few tokens: only their rows are loaded, so that the TMA unit is left to the stream of B, of which each byte is used once (1 row against
     // 131072 x 2048: 137 -> 97 us, 5.5 TB/s; 64 rows against 32000 x 4096: 58.5 us with whole boxes, 60 without)
@@ -146,12 +146,12 @@ psgd_status launch_softmax(const Operand& A, const Operand& B, const TilePlan& p
     const int n = std::min(p.units, pairs);
     a.first_q = p.units / n; a.first_r = p.units % n;
     allow_smem(k_tile<EPI>, tile_smem_bytes());
-    return launch_after(k_tile<EPI>, dim3(2 * n), dim3(TG_THREADS), tile_smem_bytes(), st, early, ma, mb, ma, mb, a) ? PSGD_OK : PSGD_E_CUDA;
+    return launch(k_tile<EPI>, dim3(2 * n), dim3(TG_THREADS), tile_smem_bytes(), st, ma, mb, ma, mb, a) ? PSGD_OK : PSGD_E_CUDA;
 }
 
 // One or two products (B MN-major) in one launch, then the pieces of their split tiles.  Two: the units of the first go round the pairs; the
 // pairs that have one unit fewer of it do as many units of the second meanwhile as fit in that time.
-psgd_status launch_products(int count, const Operand (&A)[2], const Operand (&B)[2], const TilePlan (&p)[2], TileArgs& a, int pairs, bool early, cudaStream_t st) {
+psgd_status launch_products(int count, const Operand (&A)[2], const Operand (&B)[2], const TilePlan (&p)[2], TileArgs& a, int pairs, cudaStream_t st) {
     CUtensorMap m[4];
     for (int i = 0; i < count; ++i) {
         if (!encode(&m[2 * i], A[i], p[i].M, p[i].K, 128) || !encode(&m[2 * i + 1], B[i], p[i].N, p[i].K, p[i].bn / 2)) return PSGD_E_CUDA;
@@ -168,10 +168,10 @@ psgd_status launch_products(int count, const Operand (&A)[2], const Operand (&B)
         a.extra = std::min((c0 + c1 / 2) / c1, second / (n - a.first_r));
     }
     allow_smem(k_tile<EPI_STORE>, tile_smem_bytes());
-    if (!launch_after(k_tile<EPI_STORE>, dim3(2 * n), dim3(TG_THREADS), tile_smem_bytes(), st, early, m[0], m[1], m[2], m[3], a)) return PSGD_E_CUDA;
+    if (!launch(k_tile<EPI_STORE>, dim3(2 * n), dim3(TG_THREADS), tile_smem_bytes(), st, m[0], m[1], m[2], m[3], a)) return PSGD_E_CUDA;
     const int joins = (p[0].parts ? p[0].tail : 0) + (count == 2 && p[1].parts ? p[1].tail : 0);
     const int wide = std::max(p[0].bn, count == 2 ? p[1].bn : 0);
-    if (joins && !launch_after(k_join, dim3(joins, wide / 32, TG_BM / 32), dim3(128), 0, st, true, a)) return PSGD_E_CUDA;
+    if (joins && !launch(k_join, dim3(joins, wide / 32, TG_BM / 32), dim3(128), 0, st, a)) return PSGD_E_CUDA;
     return PSGD_OK;
 }
 
@@ -285,7 +285,7 @@ psgd_status xent(const void* H, int64_t ldh, const void* W, int64_t ldw, const i
         const bool whole = rows == x.piece;
         const TilePlan pl = whole ? x.logits : plan_tiles(rows, V, D, x.pairs, false);
         const Operand oh{h, ldh, false}, ow{W, ldw, false};
-        psgd_status s = grad ? launch_softmax<EPI_SOFTMAX>(oh, ow, pl, a, x.pairs, !first, st) : launch_softmax<EPI_LOSS>(oh, ow, pl, a, x.pairs, false, st);
+        psgd_status s = grad ? launch_softmax<EPI_SOFTMAX>(oh, ow, pl, a, x.pairs, st) : launch_softmax<EPI_LOSS>(oh, ow, pl, a, x.pairs, st);
         if (s != PSGD_OK) return s;
         r.rows = (int)rows;
         r.first_sum = (int)t0;                        // (without gradients there is one piece)
@@ -294,10 +294,10 @@ psgd_status xent(const void* H, int64_t ldh, const void* W, int64_t ldw, const i
         r.loss = token_loss + t0;
         r.lse = lse + t0;
         if (!grad) {
-            if (!launch_after(k_xent_loss, dim3(ceil_div(rows, XE_THREADS / 32)), dim3(XE_THREADS), 0, st, true, r)) return PSGD_E_CUDA;
+            if (!launch(k_xent_loss, dim3(ceil_div(rows, XE_THREADS / 32)), dim3(XE_THREADS), 0, st, r)) return PSGD_E_CUDA;
             continue;
         }
-        if (!launch_after(k_xent_rows, dim3((unsigned)rows, parts_of(rows)), dim3(XE_THREADS), 0, st, true, r)) return PSGD_E_CUDA;
+        if (!launch(k_xent_rows, dim3((unsigned)rows, parts_of(rows)), dim3(XE_THREADS), 0, st, r)) return PSGD_E_CUDA;
         // dH = dL W: contraction over the vocabulary;  dW = dL^T H: over the tokens
         TilePlan p[2] = {x.two[0], x.two[1]};
         if (!whole) plan_gradients(p, rows, V, D, x.pairs);
@@ -320,10 +320,10 @@ psgd_status xent(const void* H, int64_t ldh, const void* W, int64_t ldw, const i
             pw.out = acc; pw.ldo = D; pw.out_f32 = 1; pw.scale = nullptr;
             pw.vec = D % 4 == 0;
         }
-        s = launch_products(2, A, B, p, g, x.pairs, true, st);
+        s = launch_products(2, A, B, p, g, x.pairs, st);
         if (s != PSGD_OK) return s;
     }
-    return cudaGetLastError() == cudaSuccess ? PSGD_OK : PSGD_E_CUDA;
+    return PSGD_OK;
 }
 
 // ---- 8-bit activations ----
@@ -346,29 +346,23 @@ ActGrid lane_grid(int64_t T, int G) {
 bool act_ok(int64_t T, int64_t F) { return T >= 0 && T <= MAX_EXTENT && extent_ok(F); }
 bool vec8(const void* p, int64_t ld, int64_t F, int dtype) { return F % 8 == 0 && aligned16(p) && ld % (dtype == PSGD_DT_BF16 ? 8 : 4) == 0; }
 
-void launch_pack(const ActShape& s, const void* x, int64_t ldx, int dtype, int8_t* q, uint8_t* scales, cudaStream_t st) {
+bool launch_pack(const ActShape& s, const void* x, int64_t ldx, int dtype, int8_t* q, uint8_t* scales, cudaStream_t st) {
     const bool vec = vec8(x, ldx, s.F, dtype);
-    const auto run = [&](auto kernel, const ActGrid& g, auto* p) { kernel<<<g.grid, g.block, 0, st>>>(s, p, ldx, q, scales); };
+    const auto run = [&](auto kernel, const ActGrid& g, auto* p) { return launch(kernel, g.grid, g.block, 0, st, s, p, ldx, q, scales); };
     if (dtype == PSGD_DT_BF16) {
         const ActGrid g = act_grid(s.T, s.G, PACK_CTAS, !vec);
-        run(vec ? k_act_pack<false> : k_act_pack<true>, g, (const __nv_bfloat16*)x);
-    } else if (vec) {
-        run(k_act_pack32, act_grid(s.T, s.G, PACK_CTAS, false), (const float*)x);
-    } else {
-        run(k_act_pack32_any, lane_grid(s.T, s.G), (const float*)x);
+        return run(vec ? k_act_pack<false> : k_act_pack<true>, g, (const __nv_bfloat16*)x);
     }
+    return vec ? run(k_act_pack32, act_grid(s.T, s.G, PACK_CTAS, false), (const float*)x) : run(k_act_pack32_any, lane_grid(s.T, s.G), (const float*)x);
 }
-void launch_unpack(const ActShape& s, const int8_t* q, const uint8_t* scales, void* x, int64_t ldx, int dtype, cudaStream_t st) {
+bool launch_unpack(const ActShape& s, const int8_t* q, const uint8_t* scales, void* x, int64_t ldx, int dtype, cudaStream_t st) {
     const bool vec = vec8(x, ldx, s.F, dtype);
-    const auto run = [&](auto kernel, const ActGrid& g, auto* p) { kernel<<<g.grid, g.block, 0, st>>>(s, q, scales, p, ldx); };
+    const auto run = [&](auto kernel, const ActGrid& g, auto* p) { return launch(kernel, g.grid, g.block, 0, st, s, q, scales, p, ldx); };
     if (dtype == PSGD_DT_BF16) {
         const ActGrid g = act_grid(s.T, s.G, PACK_CTAS, !vec);
-        run(vec ? k_act_unpack<__nv_bfloat16, false> : k_act_unpack<__nv_bfloat16, true>, g, (__nv_bfloat16*)x);
-    } else if (vec) {
-        run(k_act_unpack<float, false>, act_grid(s.T, s.G, PACK_CTAS, false), (float*)x);
-    } else {
-        run(k_act_unpack32_any, lane_grid(s.T, s.G), (float*)x);
+        return run(vec ? k_act_unpack<__nv_bfloat16, false> : k_act_unpack<__nv_bfloat16, true>, g, (__nv_bfloat16*)x);
     }
+    return vec ? run(k_act_unpack<float, false>, act_grid(s.T, s.G, PACK_CTAS, false), (float*)x) : run(k_act_unpack32_any, lane_grid(s.T, s.G), (float*)x);
 }
 bool dtype_ok(int dtype) { return dtype == PSGD_DT_F32 || dtype == PSGD_DT_BF16; }
 bool ckpt_ok(const void* q) { return ((uintptr_t)q & 15) == 0; }
@@ -394,8 +388,6 @@ WgradPlan plan_wgrad(int64_t T, int64_t O, int64_t F, bool by_parts) {
     g.total = at;
     return g;
 }
-
-psgd_status last_error() { return cudaGetLastError() == cudaSuccess ? PSGD_OK : PSGD_E_CUDA; }
 
 }  // namespace
 
@@ -429,8 +421,7 @@ psgd_status psgd_act_pack(const void* x, int64_t ldx, int dtype, int64_t T, int6
     if (!x || !q || !scales) return PSGD_E_NULL;
     if (ldx < F || !ckpt_ok(q)) return PSGD_E_INVALID;
     const ActShape s{T, (int)F, ceil_div(F, ACT_GROUP)};
-    launch_pack(s, x, ldx, dtype, q, scales, (cudaStream_t)stream);
-    return last_error();
+    return launch_pack(s, x, ldx, dtype, q, scales, (cudaStream_t)stream) ? PSGD_OK : PSGD_E_CUDA;
 }
 
 psgd_status psgd_act_unpack(const int8_t* q, const uint8_t* scales, int64_t T, int64_t F, void* x, int64_t ldx, int dtype, psgd_stream stream) {
@@ -439,8 +430,7 @@ psgd_status psgd_act_unpack(const int8_t* q, const uint8_t* scales, int64_t T, i
     if (!x || !q || !scales) return PSGD_E_NULL;
     if (ldx < F || !ckpt_ok(q)) return PSGD_E_INVALID;
     const ActShape s{T, (int)F, ceil_div(F, ACT_GROUP)};
-    launch_unpack(s, q, scales, x, ldx, dtype, (cudaStream_t)stream);
-    return last_error();
+    return launch_unpack(s, q, scales, x, ldx, dtype, (cudaStream_t)stream) ? PSGD_OK : PSGD_E_CUDA;
 }
 
 psgd_status psgd_copy_rows(const void* src, int64_t lds, int64_t rows, int64_t cols, void* dst, int64_t ldd, psgd_stream stream) {
@@ -450,8 +440,7 @@ psgd_status psgd_copy_rows(const void* src, int64_t lds, int64_t rows, int64_t c
     if (lds < cols || ldd < cols) return PSGD_E_INVALID;
     const ActShape s{rows, (int)cols, ceil_div(cols, ACT_GROUP)};
     const ActGrid g = act_grid(rows, s.G, PACK_CTAS, true);
-    k_copy_rows<<<g.grid, g.block, 0, (cudaStream_t)stream>>>(s, (const __nv_bfloat16*)src, lds, (__nv_bfloat16*)dst, ldd);
-    return last_error();
+    return launch(k_copy_rows, g.grid, g.block, 0, (cudaStream_t)stream, s, (const __nv_bfloat16*)src, lds, (__nv_bfloat16*)dst, ldd) ? PSGD_OK : PSGD_E_CUDA;
 }
 
 psgd_status psgd_act_wgrad_workspace(int64_t T, int64_t O, int64_t F, size_t* bytes) {
@@ -477,7 +466,7 @@ psgd_status psgd_act_wgrad(const void* dY, int64_t lddy, const int8_t* q, const 
     if (ws_bytes < g.total) return PSGD_E_WORKSPACE;
     char* w = (char*)ws;
     const ActShape s{T, (int)F, ceil_div(F, ACT_GROUP)};
-    launch_unpack(ActShape{T, (int)g.ldx, s.G}, q, scales, w + g.x, g.ldx, PSGD_DT_BF16, st);     // the padding too: its values are zeros
+    if (!launch_unpack(ActShape{T, (int)g.ldx, s.G}, q, scales, w + g.x, g.ldx, PSGD_DT_BF16, st)) return PSGD_E_CUDA;     // the padding too: its values are zeros
     TileArgs a{};
     a.status = status ? status : (int*)w;
     TileProblem& t = a.p[0];
@@ -487,7 +476,7 @@ psgd_status psgd_act_wgrad(const void* dY, int64_t lddy, const int8_t* q, const 
     t.part = (float*)(w + g.part);
     const Operand A[2] = {{dY, lddy, true}, {}}, B[2] = {{w + g.x, g.ldx, true}, {}};
     const TilePlan p[2] = {g.p, {}};
-    return launch_products(1, A, B, p, a, g.pairs, true, st);
+    return launch_products(1, A, B, p, a, g.pairs, st);
 } catch (...) {
     return PSGD_E_CUDA;
 }
@@ -502,9 +491,7 @@ psgd_status psgd_swiglu_forward(const void* gate, int64_t ldg, const void* up, i
     const GatedForward a{(const __nv_bfloat16*)gate, (const __nv_bfloat16*)up, (__nv_bfloat16*)h, ldg, ldu, ldh, q_gate, q_up, s_gate, s_up};
     const bool vec = vec8(gate, ldg, F, PSGD_DT_BF16) && vec8(up, ldu, F, PSGD_DT_BF16) && vec8(h, ldh, F, PSGD_DT_BF16);
     const ActGrid g = act_grid(T, s.G, FORWARD_CTAS, !vec);
-    const auto kernel = vec ? k_swiglu_forward<false> : k_swiglu_forward<true>;
-    kernel<<<g.grid, g.block, 0, (cudaStream_t)stream>>>(s, a);
-    return last_error();
+    return launch(vec ? k_swiglu_forward<false> : k_swiglu_forward<true>, g.grid, g.block, 0, (cudaStream_t)stream, s, a) ? PSGD_OK : PSGD_E_CUDA;
 }
 
 psgd_status psgd_swiglu_backward(const void* dh, int64_t lddh, const int8_t* q_gate, const uint8_t* s_gate, const int8_t* q_up, const uint8_t* s_up, int64_t T, int64_t F,
@@ -517,10 +504,9 @@ psgd_status psgd_swiglu_backward(const void* dh, int64_t lddh, const int8_t* q_g
     const GatedBackward a{(const __nv_bfloat16*)dh, q_gate, q_up, s_gate, s_up, (__nv_bfloat16*)d_gate, (__nv_bfloat16*)d_up, (__nv_bfloat16*)h, lddh, ldg, ldu, ldh};
     const bool vec = vec8(dh, lddh, F, PSGD_DT_BF16) && vec8(d_gate, ldg, F, PSGD_DT_BF16) && vec8(d_up, ldu, F, PSGD_DT_BF16) && (!h || vec8(h, ldh, F, PSGD_DT_BF16));
     const ActGrid g = act_grid(T, s.G, BACKWARD_CTAS, !vec);
-    const auto run = [&](auto kernel) { kernel<<<g.grid, g.block, 0, (cudaStream_t)stream>>>(s, a); };
-    if (h) run(vec ? k_swiglu_backward<true, false> : k_swiglu_backward<true, true>);
-    else run(vec ? k_swiglu_backward<false, false> : k_swiglu_backward<false, true>);
-    return last_error();
+    const auto run = [&](auto kernel) { return launch(kernel, g.grid, g.block, 0, (cudaStream_t)stream, s, a) ? PSGD_OK : PSGD_E_CUDA; };
+    if (h) return run(vec ? k_swiglu_backward<true, false> : k_swiglu_backward<true, true>);
+    return run(vec ? k_swiglu_backward<false, false> : k_swiglu_backward<false, true>);
 }
 
 }  // extern "C"

@@ -296,8 +296,9 @@ __device__ __forceinline__ void emit_block(const TileProblem& a, uint4* xb, floa
     }
 }
 
-// Dependent launches: a kernel of a call's chain may start while the one before it still runs; `grid_wait` returns when that one has
-// finished and its writes are visible, so everything that touches global memory comes after it.  `grid_trigger` lets the next start.
+// Dependent launches: a kernel may start while the one before it on the stream still runs (its set-up and its CTAs' start then cost nothing); `grid_wait`
+// returns when that one has finished and its writes are visible, so everything that touches global memory comes after it, and nothing
+// is loaded through the read-only path, which expects memory that no one writes while the kernel lives.  `grid_trigger` lets the next start.
 __device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;\n" ::: "memory"); }
 __device__ __forceinline__ void grid_trigger() { asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory"); }
 
@@ -446,8 +447,8 @@ k_tile(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtenso
 #pragma unroll
                 for (int j = 0; j < UN; ++j) {                 // no branch around the loads: all under way together
                     const long long i = min(i0 + 32 * j, a.norm_rows - 1);
-                    label[j] = __ldg(a.norm_labels + i);
-                    wt[j] = a.norm_weight ? __ldg(a.norm_weight + i) : 1.f;
+                    label[j] = a.norm_labels[i];
+                    wt[j] = a.norm_weight ? a.norm_weight[i] : 1.f;
                 }
 #pragma unroll
                 for (int j = 0; j < UN; ++j) {
@@ -471,7 +472,7 @@ k_tile(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtenso
             TileUnit w;
             for (int j = 0; tile_unit(a, j, w); ++j) {
                 const TileProblem& p = a.p[w.which];
-                const float scale = p.scale ? __ldg(p.scale) : 1.f;
+                const float scale = p.scale ? *p.scale : 1.f;
                 const int row0 = w.m0 + rank * 128 + quarter * 32;
                 const int chunks = row0 < p.M ? (min(p.bn, p.N - w.n0) + 31) / 32 : 0;      // blocks of 32 columns that exist
                 // partial tiles: lanes of a warp (rows) side by side
@@ -631,7 +632,7 @@ __global__ void __launch_bounds__(128) k_join(const __grid_constant__ TileArgs a
 #pragma unroll
     for (int j = 0; j < 8; ++j) xs[lane][8 * warp + j] = v[j];
     __syncthreads();
-    const float scale = p.scale ? __ldg(p.scale) : 1.f;
+    const float scale = p.scale ? *p.scale : 1.f;
     const int col = n0 + c0 + lane;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {

@@ -172,7 +172,7 @@ __global__ void __launch_bounds__(XE_THREADS, XE_ROW_CTAS) k_xent_rows(const __g
 #pragma unroll
         for (int i = 0; i < UN; ++i) {
             const int u = b + i * XE_THREADS;
-            if (u < u1) { v[i] = q[u]; ref[i] = __ldg(&st[u / (XE_SEG / 8)].x); }
+            if (u < u1) { v[i] = q[u]; ref[i] = st[u / (XE_SEG / 8)].x; }
         }
 #pragma unroll
         for (int i = 0; i < UN; ++i) {
