@@ -18,6 +18,11 @@
 // Whole waves of tiles run with all of k; the tiles of the last, partly filled wave are split over k so that every pair has
 // work.  Their partial sums go to the workspace and k_join adds them in the order of k (a fixed order, no atomics; letting
 // the last pair to arrive add them up alone cost 25 us of a 172 us product, one multiprocessor cannot read faster).
+//
+// Measured alone: logits with statistics 4096 x 32000 x 768 in 150 us (1.34 PFLOP/s; the epilogue's reads of tensor memory take the MMAs' bandwidth),
+// 16384 x 32000 x 2048 in 1.33 ms (1.61), both gradients of the former in 265 us (1.52, tensor pipe 95 % active), weight gradient
+// 16384 x 5504 x 2048 in 247 us (1.50).  Bound by the tensor cores at the clock that 1000 W allow (1450 MHz there); small products by
+// 3300 cycles until the first boxes have landed and 3700 from the last MMA to the end.
 // Every wait on an mbarrier is bounded: one that runs out sets PSGD_W_TIMEOUT in the status word and the kernel ends.
 #pragma once
 #include <cuda_bf16.h>

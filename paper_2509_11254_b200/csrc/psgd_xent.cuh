@@ -10,6 +10,10 @@
 // rewrites the 16 bits of every logit as the bfloat16 gradient w_t (p - [v = y_t]), the one rounding between the logits and the
 // products that follow.  1 / Z is left to those products' epilogues: it would put the same rounding error on every row.
 // Sums over rows and segments are formed in a fixed order; the last CTA to finish adds up the loss.
+//
+// Bound by HBM: k_xent_rows reads and writes 2 bytes per logit, a CTA per row (or part of one where rows are few), whose statistics it joins
+// first.  Measured: 4096 x 32000 in 95 us, 5.5 TB/s, 84 % of a copy; forming the logits a second time instead would take
+// 123 us of tensor-core time at a width of 768 and more at larger ones.  k_xent_loss reads 8 bytes per 128 logits: 16384 x 32000 in 15 us, 1 % of the product.
 #pragma once
 #include "psgd_tile.cuh"
 
