@@ -565,20 +565,28 @@ k_tile(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtenso
                     for (int j = 0; j < XE_SEG; ++j) t[j & 3] = fmaxf(t[j & 3], v[j >> 5][j & 31]);
                     const float top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
                     const float ref = top == -INFINITY ? 0.f : top;                // nothing but -inf: exp(-inf - 0) = 0
-                    float part[4] = {EPI == EPI_LOSS ? last_sum * ex2((last_top - ref) * LOG2E) : 0.f, 0.f, 0.f, 0.f};
+                    // eight at a time, so that the small terms meet before they meet the maximum's 1: it takes part in at most seven additions
+                    float part[4];
                     unsigned pk[XE_SEG / 2];
 #pragma unroll
-                    for (int j = 0; j < XE_SEG; j += 2) {
-                        const float t0 = (v[j >> 5][j & 31] - ref) * LOG2E, t1 = (v[j >> 5][(j & 31) + 1] - ref) * LOG2E;     // <= 0
-                        part[j & 2] += ex2(t0);
-                        part[(j & 2) + 1] += ex2(t1);
-                        if (EPI == EPI_SOFTMAX) {
-                            const float q0 = fminf(fmaf(t0, -XE_STEPS, XE_MAGIC), XE_MAGIC + 65535.f);
-                            const float q1 = fminf(fmaf(t1, -XE_STEPS, XE_MAGIC), XE_MAGIC + 65535.f);
-                            pk[j / 2] = __byte_perm(__float_as_uint(q0), __float_as_uint(q1), 0x5410);
+                    for (int j = 0; j < XE_SEG; j += 8) {
+                        float e[8];
+#pragma unroll
+                        for (int i = 0; i < 8; i += 2) {
+                            const float t0 = (v[j >> 5][(j & 31) + i] - ref) * LOG2E, t1 = (v[j >> 5][(j & 31) + i + 1] - ref) * LOG2E;     // <= 0
+                            e[i] = ex2(t0);
+                            e[i + 1] = ex2(t1);
+                            if (EPI == EPI_SOFTMAX) {
+                                const float q0 = fminf(fmaf(t0, -XE_STEPS, XE_MAGIC), XE_MAGIC + 65535.f);
+                                const float q1 = fminf(fmaf(t1, -XE_STEPS, XE_MAGIC), XE_MAGIC + 65535.f);
+                                pk[(j + i) / 2] = __byte_perm(__float_as_uint(q0), __float_as_uint(q1), 0x5410);
+                            }
                         }
+                        const float eight = ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+                        part[j / 8 & 3] = j < 32 ? eight : part[j / 8 & 3] + eight;
                     }
-                    const float sum = (part[0] + part[1]) + (part[2] + part[3]);
+                    float sum = (part[0] + part[1]) + (part[2] + part[3]);
+                    if (EPI == EPI_LOSS) sum = fmaf(last_sum, ex2((last_top - ref) * LOG2E), sum);
                     if (EPI == EPI_LOSS) {
                         last_top = top;
                         last_sum = sum;

@@ -7,8 +7,10 @@
 // The product kernel leaves, per row and segment of 64 columns (128 without gradients), the maximum and the sum of exp(l - maximum), and per logit the
 // distance from its segment's maximum in steps of 2^-10 in the base-two exponent (16 bits, at most 3.4e-4 of relative error in p,
 // a sixth of the rounding of a bfloat16; the sums come from the unrounded logits).  k_xent_rows joins the segments of a row and
-// rewrites the 16 bits of every logit as the bfloat16 gradient w_t (p - [v = y_t]), the one rounding between the logits and the
-// products that follow.  1 / Z is left to those products' epilogues: it would put the same rounding error on every row.
+// rewrites the 16 bits of every logit as the bfloat16 gradient w_t (p - [v = y_t]), rounded once more so.  The label's own gradient comes from its unrounded
+// logit.  1 / Z is left to the epilogues of the products that follow: it would put the same rounding error on every row.
+// The losses and the label's p - 1 are formed from the maximum and the logarithm of the sum apart: their sum, the log-sum-exp, is rounded at
+// the size of the logits, which for a token with 1 - p of 1e-5 was up to a fifth of its loss and gradient (now 7 roundings of 2^-24).
 // Sums over rows and segments are formed in a fixed order; the last CTA to finish adds up the loss.
 //
 // Bound by HBM: k_xent_rows reads and writes 2 bytes per logit, a CTA per row (or part of one where rows are few), whose statistics it joins
@@ -88,27 +90,30 @@ __device__ __forceinline__ void report_rows(const RowsArgs& a) {
     if (threadIdx.x == 0) *a.mean = (s.y != 0.0 || s.x != s.x) ? (float)(s.x / s.y) : 0.f;
 }
 
-__device__ __forceinline__ void merge_stat(float& top, float& sum, float t, float s) {
-    const float m = fmaxf(top, t), r = m == -INFINITY ? 0.f : m;
-    sum = sum * ex2((top - r) * LOG2E) + s * ex2((t - r) * LOG2E);
-    top = m;
+// Statistics of a row: its maximum `top` and `rest`, the sum of exp(l - top) less the 1 of the maximum itself (-1 where there is nothing). Where
+// one logit stands far above the others, rest is 1 - p of it and keeps all its bits, which a sum next to 1 would lose.
+__device__ __forceinline__ void merge_stat(float& top, float& rest, float t, float r) {
+    const bool first = top >= t;
+    const float high = first ? top : t, low = first ? t : top, from = high == -INFINITY ? 0.f : high;
+    rest = fmaf(1.f + (first ? r : rest), ex2((low - from) * LOG2E), first ? rest : r);
+    top = high;
 }
-__device__ __forceinline__ void warp_stat(float& top, float& sum) {
+__device__ __forceinline__ void warp_stat(float& top, float& rest) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
-        const float t = __shfl_xor_sync(0xffffffffu, top, o), s = __shfl_xor_sync(0xffffffffu, sum, o);
-        merge_stat(top, sum, t, s);
+        const float t = __shfl_xor_sync(0xffffffffu, top, o), r = __shfl_xor_sync(0xffffffffu, rest, o);
+        merge_stat(top, rest, t, r);
     }
 }
-// the row's outputs; returns its share of the loss and of the weight
-__device__ __forceinline__ double2 write_loss(const RowsArgs& a, int row, float lse) {
+// the row's outputs (the loss not from lse, whose rounding is one of the size of the logits); returns its share of the loss and of the weight
+__device__ __forceinline__ double2 write_loss(const RowsArgs& a, int row, float top, float log_sum) {
     const long long label = a.labels[row];
     bool bad;
     const float w = row_weight(a.weight, row, label, a.ignore, a.V, bad);
     float loss = 0.f;
     if (bad) { loss = NAN; atomicOr(a.status, XE_W_LABEL); }
-    else if (label != a.ignore) loss = lse - a.label_logit[row];
-    a.lse[row] = lse;
+    else if (label != a.ignore) loss = (top - a.label_logit[row]) + log_sum;
+    a.lse[row] = top + log_sum;
     a.loss[row] = loss;
     return make_double2(bad ? (double)loss : label != a.ignore ? (double)w * (double)loss : 0.0, (double)w);     // a bad row's NaN reaches the mean
 }
@@ -121,16 +126,16 @@ __global__ void __launch_bounds__(XE_THREADS) k_xent_loss(const __grid_constant_
     const int warp = threadIdx.x >> 5, row = blockIdx.x * (XE_THREADS / 32) + warp, lane = threadIdx.x & 31;
     double2 share = make_double2(0.0, 0.0);
     if (row < a.rows) {
-        float top = -INFINITY, sum = 0.f;
+        float top = -INFINITY, rest = -1.f;
         for (int j = lane; j < a.nseg; j += 8 * 32) {
             float2 s[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) s[i] = j + 32 * i < a.nseg ? a.stats[(size_t)row * a.nseg + j + 32 * i] : make_float2(-INFINITY, 0.f);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) merge_stat(top, sum, s[i].x, s[i].y);
+            for (int i = 0; i < 8; ++i) merge_stat(top, rest, s[i].x, s[i].y - 1.f);
         }
-        warp_stat(top, sum);
-        if (lane == 0) share = write_loss(a, row, top + logf(sum));
+        warp_stat(top, rest);
+        if (lane == 0) share = write_loss(a, row, top, log1pf(rest));
     }
     if (lane == 0) mine[warp] = share;
     __syncthreads();
@@ -148,27 +153,26 @@ __global__ void __launch_bounds__(XE_THREADS, XE_ROW_CTAS) k_xent_rows(const __g
     __shared__ float2 ws[XE_THREADS / 32];
     const int row = blockIdx.x, tid = threadIdx.x;
     const float2* st = a.stats + (size_t)row * a.nseg;
-    float top = -INFINITY, sum = 0.f;
-    for (int j = tid; j < a.nseg; j += XE_THREADS) merge_stat(top, sum, st[j].x, st[j].y);
-    warp_stat(top, sum);
-    if ((tid & 31) == 0) ws[tid >> 5] = make_float2(top, sum);
+    float top = -INFINITY, rest = -1.f;
+    for (int j = tid; j < a.nseg; j += XE_THREADS) merge_stat(top, rest, st[j].x, st[j].y - 1.f);
+    warp_stat(top, rest);
+    if ((tid & 31) == 0) ws[tid >> 5] = make_float2(top, rest);
     __syncthreads();
     top = ws[0].x;
-    sum = ws[0].y;
+    rest = ws[0].y;
 #pragma unroll
-    for (int i = 1; i < XE_THREADS / 32; ++i) merge_stat(top, sum, ws[i].x, ws[i].y);
-    const float lse = top + logf(sum);
-    if (blockIdx.y == 0 && tid == 0) a.sums[a.first_sum + row] = write_loss(a, row, lse);
+    for (int i = 1; i < XE_THREADS / 32; ++i) merge_stat(top, rest, ws[i].x, ws[i].y);
+    const float log_sum = log1pf(rest);
+    if (blockIdx.y == 0 && tid == 0) a.sums[a.first_sum + row] = write_loss(a, row, top, log_sum);
 
     const long long label = a.labels[row];
     bool bad;
     const float w = row_weight(a.weight, row, label, a.ignore, a.V, bad);
     const bool counts = !bad && label != a.ignore;
-    const float poison = lse - lse;                               // 0, or NaN where the row's logits were not finite
+    const float poison = (top + log_sum) - (top + log_sum);       // 0, or NaN where the row's logits were not finite
     uint4* q = reinterpret_cast<uint4*>(a.q + (size_t)row * a.ldq);
     const int units = (a.V + 7) / 8, per = (units + gridDim.y - 1) / gridDim.y;
     const int u0 = blockIdx.y * per, u1 = min(units, u0 + per);
-    const int lunit = counts ? (int)(label >> 3) : -1;
     constexpr int UN = 4;
     for (int b = u0 + tid; b < u1; b += XE_THREADS * UN) {
         uint4 v[UN];
@@ -182,7 +186,7 @@ __global__ void __launch_bounds__(XE_THREADS, XE_ROW_CTAS) k_xent_rows(const __g
         for (int i = 0; i < UN; ++i) {
             const int u = b + i * XE_THREADS;
             if (u >= u1) break;
-            const float off = (ref[i] - lse) * LOG2E + poison;    // exponent of the segment's largest p
+            const float off = ((ref[i] - top) - log_sum) * LOG2E + poison;     // exponent of the segment's largest p
             const unsigned x[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
             float d[8];
 #pragma unroll
@@ -192,15 +196,17 @@ __global__ void __launch_bounds__(XE_THREADS, XE_ROW_CTAS) k_xent_rows(const __g
                 const float p = ex2(fmaf(steps, -1.f / XE_STEPS, off));
                 d[j] = (bits == XE_NONE ? poison : p) * w;
             }
-            if (u == lunit) {
-                const int at = (int)(label & 7);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) if (j == at) d[j] -= w;
-            }
             uint4 o = make_uint4(pack_bf16(d[0], d[1]), pack_bf16(d[2], d[3]), pack_bf16(d[4], d[5]), pack_bf16(d[6], d[7]));
             if (!counts) o = make_uint4(0u, 0u, 0u, 0u);
             q[u] = o;
         }
+    }
+    // the label's column again, by the thread that has just written it: p - 1 = (exp(l_y - top) - 1 - rest) / (1 + rest), without cancellation where
+    // the label is the maximum
+    const int lunit = counts ? (int)(label >> 3) : -1;
+    if (lunit >= u0 && lunit < u1 && (lunit - u0) % XE_THREADS == tid) {
+        const float d = ((ex2((a.label_logit[row] - top) * LOG2E) - 1.f) - rest) / (1.f + rest) + poison;
+        reinterpret_cast<__nv_bfloat16*>(q)[label] = __float2bfloat16_rn(d * w);
     }
     report_rows(a);
 }

@@ -735,3 +735,47 @@ def test_operators_feed_the_compressor(torch, ops):
     spec.loader.exec_module(example)
     losses = example.train(steps=60, log=None)
     assert abs(losses[0] - math.log(2000)) < 0.2 and losses[-1] < 0.1 and all(math.isfinite(v) for v in losses)
+
+
+# ---- tokens that the model is sure of -----------------------------------------------------------------------------
+@pytest.mark.parametrize("base", [-60, 0, 20, 60, 100])
+@pytest.mark.parametrize("V", [90, 700, 50257])
+def test_xent_of_confident_tokens(torch, ops, V, base):
+    """Tokens whose label has 1 - p of 1e-3 to 1e-5, at logits of any size: the label's gradient and the loss are good relative to 1 - p.
+
+    Column 0 of the weight lifts every logit of a token by `base`, and every token has a label and a column of its own that lifts it further, so that
+    d_hidden[t, own column] and d_weight[label, own column] / lift are the gradient of the label's logit alone and d_hidden[t, 0] is the
+    sum of all the gradients of the token's logits, which is 0.
+    Bounds: a logit is good to l_err, which moves 1 - p by 2 l_err of itself; the sum of the exponentials is 1 + (1 - p) / p and meets, beside
+    the 1, at most 8 roundings of 2^-24; the gradient is rounded to bfloat16 once before and once after the product; p of the other columns by 3.4e-4 for the
+    stored exponents and once to bfloat16.
+    """
+    T, D = 24, 64
+    g = gen(torch, V + base)
+    h = torch.zeros(T, D, device="cuda")
+    w = torch.zeros(V, D, device="cuda")
+    own = torch.arange(1, T + 1, device="cuda")
+    rows = torch.arange(T, device="cuda")
+    h[:, T + 1:] = torch.randn(T, D - T - 1, generator=g, device="cuda") * 0.15
+    w[:, T + 1:] = torch.randn(V, D - T - 1, generator=g, device="cuda")
+    labels = torch.randperm(V, generator=g, device="cuda")[:T]
+    h[:, 0], w[:, 0] = base, 1
+    rest = 10.0 ** -torch.linspace(3, 5, T, device="cuda")
+    h[rows, own] = math.log(V) + 0.4 - torch.log(rest)
+    w[labels, own] = 1
+    w[labels, T + 1:] = 0                                                # the label stands at base + lift exactly
+    h, w = h.to(torch.bfloat16), w.to(torch.bfloat16)
+    lift = h[rows, own].double()
+    ref = xent_reference(torch, h, w, labels, None, -100)
+    miss = -torch.expm1(-ref["token"])                                   # 1 - p
+    assert bool(((miss > 3e-6) & (miss < 3e-3)).all())
+    l_err = sum_bound(D) * ref["size"]
+    off = 2 * l_err * miss + 8 * 2.0 ** -24
+    for r in (ops.linear_cross_entropy(h, w, labels), ops.linear_cross_entropy_grad(h, w, labels)):
+        within(r.token_loss, ref["token"], off + 2.0 ** -21 * ref["token"])
+        within(r.lse, ref["lse"], l_err + 2.0 ** -22 * ref["lse"].abs() + 2.0 ** -21)
+    grad = -miss / T
+    bound = (off * (1 + 2 * BF16) + 2 * BF16 * miss) / T
+    within(r.d_hidden[rows, own], grad, bound)
+    within(r.d_weight[labels, own].double() / lift, grad, bound)
+    within(r.d_hidden[:, 0], torch.zeros_like(grad), (off + (2 * BF16 + 3.4e-4 + 2.0 ** -12 + 2 * l_err) * 2 * miss) / T)
