@@ -327,7 +327,8 @@ psgd_status psgd_backproject_static(const float* M /*DEVICE*/, const float* P_ha
  * gradients as given.)  All calls are stream-ordered, allocate nothing and never synchronise; every DEVICE buffer is the
  * caller's.  Matrices are row-major with unit column stride and a row stride ld.. in elements; "aligned operand" means a
  * 16-byte aligned pointer and, with more than one row, a row stride that is a multiple of 8 elements.  `status` (DEVICE, one int, may
- * be NULL) collects PSGD_W_* bits and is never cleared by the library.  `workspace` (DEVICE, 256-byte aligned) holds at least
+ * be NULL) collects PSGD_W_* bits and is never cleared by the library.  Results that depend on a wait which ran out (PSGD_W_TIMEOUT) are NaN,
+ * with or without a status word.  `workspace` (DEVICE, 256-byte aligned) holds at least
  * the bytes the matching query reports, may hold anything before the call, and is free again for later work on the stream.
  * Sizes are at most 2^30 per dimension and 2^45 for a product of two; T = 0 is allowed (loss 0, weight gradients 0).
  */

@@ -7,6 +7,9 @@ namespace psgd {
 
 constexpr unsigned FU_WAIT_LIMIT = 1u << 20;   // polls of one mbarrier wait before giving up
 constexpr int FU_W_TIMEOUT = 4;                // == PSGD_W_TIMEOUT
+#ifndef PSGD_WARP_WAIT_LIMIT
+#define PSGD_WARP_WAIT_LIMIT FU_WAIT_LIMIT     // of mbar_wait_warp; a build with 0 gives up every such wait at once (test of what then happens)
+#endif
 
 // ---- PTX wrappers ---------------------------------------------------------------------------
 __device__ __forceinline__ unsigned smem_u32(const void* p) { return (unsigned)__cvta_generic_to_shared(p); }
@@ -63,7 +66,7 @@ __device__ __forceinline__ void mbar_wait_warp(unsigned bar, unsigned parity, in
     int gave_up = 0;
     if ((threadIdx.x & 31) == 0) {
         bool ok = false;
-        for (unsigned it = 0; it < FU_WAIT_LIMIT && !ok; ++it) {
+        for (unsigned it = 0; it < PSGD_WARP_WAIT_LIMIT && !ok; ++it) {
             ok = mbar_try_wait(bar, parity);
             if (!ok) __nanosleep(40);
         }

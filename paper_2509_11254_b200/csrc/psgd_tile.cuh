@@ -23,7 +23,8 @@
 // 16384 x 32000 x 2048 in 1.33 ms (1.61), both gradients of the former in 265 us (1.52, tensor pipe 95 % active), weight gradient
 // 16384 x 5504 x 2048 in 247 us (1.50).  Bound by the tensor cores at the clock that 1000 W allow (1450 MHz there); small products by
 // 3300 cycles until the first boxes have landed and 3700 from the last MMA to the end.
-// Every wait on an mbarrier is bounded: one that runs out sets PSGD_W_TIMEOUT in the status word and the kernel ends.
+// Every wait on an mbarrier is bounded: one that runs out sets PSGD_W_TIMEOUT in the status word and the kernel ends.  A warp of the epilogue whose wait
+// for an accumulator has run out (because the warps before it gave up, or by itself) writes NaN from then on, so that no call's results look good by mistake.
 #pragma once
 #include <cuda_bf16.h>
 
@@ -505,9 +506,9 @@ k_tile(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtenso
                                 for (int i = 0; i < 32; ++i) v[i] += q[i * 128];
                             }
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) q[i * 128] = v[i];
+                            for (int i = 0; i < 32; ++i) q[i * 128] = dead ? NAN : v[i];
                         } else {
-                            emit_block(p, xb, v, row0, w.n0 + 32 * c, more ? (const float*)p.out : p.addend, more ? p.ldo : (long long)p.N, scale);
+                            emit_block(p, xb, v, row0, w.n0 + 32 * c, more ? (const float*)p.out : p.addend, more ? p.ldo : (long long)p.N, dead ? NAN : scale);
                         }
                     }
                     k0 = k1;
@@ -587,6 +588,7 @@ k_tile(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtenso
                     }
                     float sum = (part[0] + part[1]) + (part[2] + part[3]);
                     if (EPI == EPI_LOSS) sum = fmaf(last_sum, ex2((last_top - ref) * LOG2E), sum);
+                    if (dead) sum = NAN;
                     if (EPI == EPI_LOSS) {
                         last_top = top;
                         last_sum = sum;

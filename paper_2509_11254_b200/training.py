@@ -8,7 +8,8 @@
 Weight gradients can be written straight into a slot of a compressor's gradient stack G [count, N, m, n] (`d_weight=G[c, i]`,
 `out=G[c, i]`).  The arithmetic runs in the CUDA library (psgd_xent_*, psgd_act_*, psgd_swiglu_* of include/psgd.h); this module checks
 arguments and hands over pointers.  Every call is stream-ordered on `stream` (default: the current stream) and does not
-synchronise.  `status`, an int32 tensor with one element, collects the library's warning bits (PSGD_W_TIMEOUT, PSGD_W_LABEL).
+synchronise.  `status`, an int32 tensor with one element, collects the library's warning bits (PSGD_W_TIMEOUT, PSGD_W_LABEL); what a wait
+that ran out should have produced is NaN, with or without `status`.
 """
 from __future__ import annotations
 

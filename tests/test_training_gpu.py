@@ -779,3 +779,39 @@ def test_xent_of_confident_tokens(torch, ops, V, base):
     within(r.d_hidden[rows, own], grad, bound)
     within(r.d_weight[labels, own].double() / lift, grad, bound)
     within(r.d_hidden[:, 0], torch.zeros_like(grad), (off + (2 * BF16 + 3.4e-4 + 2.0 ** -12 + 2 * l_err) * 2 * miss) / T)
+
+
+# ---- waits that run out -------------------------------------------------------------------------------------------
+def test_results_behind_a_wait_that_ran_out_are_nan(torch, ops, tmp_path, monkeypatch):
+    """A build whose epilogue gives up every wait for an accumulator at once (the products themselves run to their end; no pair has more than two
+    accumulators here, so none waits for this epilogue): every result is NaN, without a status word too, and the status word says why."""
+    import ctypes as C
+    import subprocess
+
+    from paper_2509_11254_b200 import binding, build
+
+    so = str(tmp_path / "gives_up.so")
+    src = [s for s in build.SRCS if s.endswith("psgd_lm.cu")]
+    subprocess.run([build.nvcc_path(), "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-Xcompiler", "-fPIC", "-shared", "-DPSGD_WARP_WAIT_LIMIT=0",
+                    "-o", so, *src], check=True, capture_output=True)
+    L = C.CDLL(so)
+    for name, (res, args) in binding.SIGNATURES.items():
+        if hasattr(L, name):
+            getattr(L, name).restype, getattr(L, name).argtypes = res, args
+    h, w, labels = xent_inputs(torch, 300, 700, 64, seed=3)
+    x = torch.randn(100, 136, generator=gen(torch, 4), device="cuda").to(torch.bfloat16)
+    dy = torch.randn(100, 264, generator=gen(torch, 5), device="cuda").to(torch.bfloat16)
+    kept = ops.pack_activation(x)
+    monkeypatch.setattr(binding, "_lib", L)
+    only, full = ops.linear_cross_entropy(h, w, labels), ops.linear_cross_entropy_grad(h, w, labels)
+    counts = labels != -100
+    for r in (only, full):
+        assert bool(torch.isnan(r.loss)) and bool(torch.isnan(r.lse).all()) and bool(torch.isnan(r.token_loss[counts]).all())
+    assert bool(torch.isnan(full.d_hidden).all()) and bool(torch.isnan(full.d_weight).all())
+    for dtype in (torch.float32, torch.bfloat16):
+        assert bool(torch.isnan(ops.weight_gradient(dy, kept, dtype=dtype)).all())
+    assert bool(torch.isnan(ops.weight_gradient(dy[:, :263], kept, out=torch.zeros(263, 137, device="cuda")[:, 1:])).all())
+    for call in (lambda s: ops.linear_cross_entropy(h, w, labels, status=s), lambda s: ops.linear_cross_entropy_grad(h, w, labels, status=s), lambda s: ops.weight_gradient(dy, kept, status=s)):
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        call(status)
+        assert int(status) == ops.PSGD_W_TIMEOUT
