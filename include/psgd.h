@@ -330,6 +330,8 @@ psgd_status psgd_backproject_static(const float* M /*DEVICE*/, const float* P_ha
  * be NULL) collects PSGD_W_* bits and is never cleared by the library.  Results that depend on a wait which ran out (PSGD_W_TIMEOUT) are NaN,
  * with or without a status word.  `workspace` (DEVICE, 256-byte aligned) holds at least
  * the bytes the matching query reports, may hold anything before the call, and is free again for later work on the stream.
+ * No output may overlap an input or another output (columns of one wider matrix may lie side by side): dH and dW with H, W and each other and
+ * psgd_act_wgrad's dW with dY are checked (PSGD_E_INVALID).
  * Sizes are at most 2^30 per dimension and 2^45 for a product of two; T = 0 is allowed (loss 0, weight gradients 0).
  */
 #define PSGD_DT_F32 0

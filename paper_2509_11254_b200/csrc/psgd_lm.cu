@@ -177,6 +177,26 @@ psgd_status launch_products(int count, const Operand (&A)[2], const Operand (&B)
 
 bool operand_ok(const void* p, int64_t rows, int64_t cols, int64_t ld) { return aligned16(p) && ld >= cols && (rows == 1 || ld % 8 == 0); }
 bool extent_ok(int64_t v) { return v >= 1 && v <= MAX_EXTENT; }
+// Bytes of a matrix in memory: `rows` stretches of `width`, `step` apart (width <= step).
+struct Stretch { const void* p; int64_t rows, width, step; };
+bool overlap(const Stretch& a, const Stretch& b) {
+    if (!a.p || !b.p || a.rows < 1 || b.rows < 1) return false;
+    if (a.rows > b.rows) return overlap(b, a);
+    const int64_t at = (int64_t)((uintptr_t)a.p - (uintptr_t)b.p);               // of a's first row, from b's
+    const int64_t end_a = at + (a.rows - 1) * a.step + a.width, end_b = (b.rows - 1) * b.step + b.width;
+    if (at >= end_b || end_a <= 0) return false;
+    // rows that lie between one another (columns of one wider matrix): row by row; with equal steps the first rows that face each other speak for all but the ends
+    const auto meets = [&](int64_t i) {
+        const int64_t x = at + i * a.step;                                       // the first row of b that ends behind x
+        const int64_t j = x < b.width ? 0 : (x - b.width) / b.step + 1;
+        return j < b.rows && j * b.step < x + a.width;
+    };
+    const int64_t first = at >= 0 ? 0 : std::min(a.rows - 1, -at / a.step);
+    for (int64_t i = first; i < (a.step == b.step ? std::min(a.rows, first + 2) : a.rows); ++i)
+        if (meets(i)) return true;
+    return a.step == b.step && meets(a.rows - 1);
+}
+Stretch stretch(const void* p, int64_t rows, int64_t cols, int64_t ld, int bytes) { return {p, rows, cols * bytes, (rows == 1 ? cols : ld) * bytes}; }
 bool tiles_ok(int64_t M, int64_t N) { return ((M + 255) / 256) * ((N + 127) / 128) <= MAX_EXTENT; }     // units are counted in 32 bits
 
 // ---- cross entropy ----
@@ -239,6 +259,10 @@ psgd_status xent(const void* H, int64_t ldh, const void* W, int64_t ldw, const i
     if (!W || !loss || !ws || (T > 0 && (!H || !labels || !token_loss || !lse)) || (grad && (!dW || (T > 0 && !dH)))) return PSGD_E_NULL;
     if (!operand_ok(W, V, D, ldw) || (T > 0 && !operand_ok(H, T, D, ldh)) || (grad && ((T > 0 && lddh < D) || lddw < D))) return PSGD_E_INVALID;
     if ((uintptr_t)ws & 255) return PSGD_E_INVALID;
+    if (grad) {                                       // both products run at once: one reads H and W while the other writes
+        const Stretch h = stretch(H, T, D, ldh, 2), v = stretch(W, V, D, ldw, 2), dh = stretch(dH, T, D, lddh, 2), dw = stretch(dW, V, D, lddw, 2);
+        if (overlap(dh, h) || overlap(dh, v) || overlap(dw, h) || overlap(dw, v) || overlap(dh, dw)) return PSGD_E_INVALID;
+    }
     if (T == 0) {                                     // no token: loss 0, no gradient
         if (cudaMemsetAsync(loss, 0, 4, st) != cudaSuccess) return PSGD_E_CUDA;
         if (grad && cudaMemset2DAsync(dW, (size_t)lddw * 2, 0, (size_t)D * 2, (size_t)V, st) != cudaSuccess) return PSGD_E_CUDA;
@@ -464,6 +488,7 @@ psgd_status psgd_act_wgrad(const void* dY, int64_t lddy, const int8_t* q, const 
     WgradPlan g = plan_wgrad(T, O, F, dtype == PSGD_DT_F32 && !vec);
     if (ws_bytes < g.total) g = plan_wgrad(T, O, F, false);       // (an aligned width whose result starts or steps unaligned)
     if (ws_bytes < g.total) return PSGD_E_WORKSPACE;
+    if (overlap(stretch(dW, O, F, lddw, dtype == PSGD_DT_F32 ? 4 : 2), stretch(dY, T, O, lddy, 2))) return PSGD_E_INVALID;
     char* w = (char*)ws;
     const ActShape s{T, (int)F, ceil_div(F, ACT_GROUP)};
     if (!launch_unpack(ActShape{T, (int)g.ldx, s.G}, q, scales, w + g.x, g.ldx, PSGD_DT_BF16, st)) return PSGD_E_CUDA;     // the padding too: its values are zeros

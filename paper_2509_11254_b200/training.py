@@ -163,7 +163,8 @@ def linear_cross_entropy(hidden, weight, labels, token_weight=None, ignore_index
 def linear_cross_entropy_grad(hidden, weight, labels, token_weight=None, ignore_index=-100, d_hidden=None, d_weight=None, status=None, stream=None):
     """The same with the gradients of the loss: returns (loss, token_loss, lse, d_hidden [T, D], d_weight [V, D]), the gradients bfloat16.
 
-    d_hidden, d_weight: where to write them (matrices with unit column stride), for instance a slot of a gradient stack.
+    d_hidden, d_weight: where to write them (matrices with unit column stride), for instance a slot of a gradient stack; they may not overlap
+    `hidden`, `weight` or each other.
     """
     return _xent(True, hidden, weight, labels, token_weight, ignore_index, d_hidden, d_weight, status, stream)
 
@@ -237,7 +238,7 @@ def _kept(c, name, device, shape=None):
 def weight_gradient(dy, kept, dtype=torch.float32, out=None, status=None, stream=None):
     """dy.T @ x for dy [T, O] bfloat16 and the checkpoint of x [T, F]: the weight gradient [O, F] of y = x W.T.
 
-    float32 sums of exact products, written as `dtype` (float32 or bfloat16) or into `out` (for instance a slot of a gradient stack).
+    float32 sums of exact products, written as `dtype` (float32 or bfloat16) or into `out` (for instance a slot of a gradient stack), which may not overlap dy.
     """
     T, O, ldy = _matrix(dy, "dy")
     dev = dy.device

@@ -87,3 +87,35 @@ def test_python_refuses_host_tensors():
                  lambda: p.weight_gradient(h, None), lambda: p.swiglu_backward(h, None, None)):
         with pytest.raises(p.PSGDError):
             call()
+
+
+def test_overlapping_outputs_are_refused(L):
+    """Outputs that share a byte with an operand or with each other are refused; rows that only lie between one another's (columns of one wider matrix) are not.
+    Placements at random against sets of bytes; the workspace is too small (-3) wherever the arguments pass, so that nothing is launched."""
+    import random
+
+    rng = random.Random(1)
+    p = 1 << 20
+
+    def cells(at, rows, cols, ld, size):
+        return {at + r * ld * size + b for r in range(rows) for b in range(cols * size)}
+
+    seen = {-1: 0, -3: 0}
+    for _ in range(4000):
+        T, V, D = rng.choice([1, 2, 3, 7]), rng.choice([1, 2, 5, 9]), rng.choice([8, 24])
+        ld = [D + 8 * rng.randrange(6) for _ in range(2)] + [D + rng.randrange(40) for _ in range(2)]
+        if rng.random() < 0.6:
+            ld = [rng.choice([64, 72])] * 4                             # columns of one buffer
+        at = [p + 16 * rng.randrange(40) * rng.choice([0, 1, 4, 16]) for _ in range(2)] + [p + 2 * rng.randrange(320) * rng.choice([0, 1, 4, 16]) for _ in range(2)]
+        h, w, dh, dw = (cells(a, n, D, s, 2) for a, n, s in zip(at, (T, V, T, V), ld))
+        want = -1 if dh & h or dh & w or dw & h or dw & w or dh & dw else -3
+        got = L.psgd_xent_grad(at[0], ld[0], at[1], ld[1], p, None, -100, T, V, D, p, p, p, at[2], ld[2], at[3], ld[3], None, p, 0, None)
+        assert got == want, (T, V, D, at, ld)
+        seen[got] += 1
+    assert min(seen.values()) > 400
+    import torch
+
+    if torch.cuda.is_available():           # (the addresses are made up: where there is a GPU, only calls that end at the workspace's size are made)
+        return
+    for size, dw in ((4, p), (2, p + 2 * 7), (4, p + 5 * 48 - 8)):         # dY: 6 rows of 16, 24 apart
+        assert L.psgd_act_wgrad(p, 24, p, p, 6, 16, 9, dw, 24, 0 if size == 4 else 1, None, p, 1 << 40, None) == -1

@@ -815,3 +815,23 @@ def test_results_behind_a_wait_that_ran_out_are_nan(torch, ops, tmp_path, monkey
         status = torch.zeros(1, dtype=torch.int32, device="cuda")
         call(status)
         assert int(status) == ops.PSGD_W_TIMEOUT
+
+
+# ---- outputs in the way of inputs ---------------------------------------------------------------------------------
+def test_outputs_beside_inputs_but_not_over_them(torch, ops):
+    """Gradients in the other columns of the buffers that hold the operands are right; over the operands they are refused before anything is launched."""
+    T, V, D = 260, 520, 64
+    h, w, labels = xent_inputs(torch, T, V, D, seed=51)
+    want = ops.linear_cross_entropy_grad(h, w, labels)
+    H, W = (torch.cat([t, torch.full_like(t, 7)], 1) for t in (h, w))
+    got = ops.linear_cross_entropy_grad(H[:, :D], W[:, :D], labels, d_hidden=H[:, D:], d_weight=W[:, D:])
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+    assert torch.equal(H[:, :D], h) and torch.equal(W[:, :D], w)
+    for bad in (dict(d_hidden=h), dict(d_weight=w), dict(d_hidden=w[:T]), dict(d_weight=W[:, D:], d_hidden=W[3:3 + T, D:])):
+        with pytest.raises(ops.PSGDError):
+            ops.linear_cross_entropy_grad(h, w, labels, **bad)
+    dy = torch.randn(T, T, generator=gen(torch, 52), device="cuda").to(torch.bfloat16)
+    kept = ops.pack_activation(h)
+    with pytest.raises(ops.PSGDError):
+        ops.weight_gradient(dy, kept, out=dy[:, :D])
