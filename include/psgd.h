@@ -337,6 +337,9 @@ psgd_status psgd_backproject_static(const float* M /*DEVICE*/, const float* P_ha
 #define PSGD_DT_F32 0
 #define PSGD_DT_BF16 1
 
+/* 1 where two matrices share a byte, else 0: `rows` stretches of `width` bytes, `step` >= width bytes apart.  Reads nothing behind the addresses. */
+int psgd_overlap(const void* a, int64_t rows_a, int64_t width_a, int64_t step_a, const void* b, int64_t rows_b, int64_t width_b, int64_t step_b);
+
 /*
  * Softmax cross entropy of the last layer.  H [T][D] hidden states, W [V][D] vocabulary matrix (both bfloat16, aligned operands),
  * labels [T] in 0..V-1 or `ignore`, weight [T] float32 or NULL (1 everywhere):

@@ -417,6 +417,10 @@ WgradPlan plan_wgrad(int64_t T, int64_t O, int64_t F, bool by_parts) {
 
 extern "C" {
 
+int psgd_overlap(const void* a, int64_t rows_a, int64_t width_a, int64_t step_a, const void* b, int64_t rows_b, int64_t width_b, int64_t step_b) {
+    return overlap({a, rows_a, width_a, rows_a == 1 ? width_a : step_a}, {b, rows_b, width_b, rows_b == 1 ? width_b : step_b});
+}
+
 psgd_status psgd_xent_workspace(int64_t T, int64_t V, int64_t D, int grad, size_t* bytes) {
     if (!bytes) return PSGD_E_NULL;
     if (T < 0 || T > MAX_EXTENT || !extent_ok(V) || !extent_ok(D) || !tiles_ok(T, V) || !tiles_ok(V, D)) return PSGD_E_INVALID;

@@ -71,10 +71,22 @@ def _status(t, device):
     return _vector(t, "status", torch.int32, 1, device) if t is not None else None
 
 
-def _operand(t, rows, cols, ld, stream):
-    """(tensor, row stride): `t` itself where the tensor cores' loads can read it in place (16-byte aligned rows), else a copy with padded rows."""
+def _stretch(t):
+    """A matrix as the library's psgd_overlap takes it: address, rows, bytes per row, bytes from row to row."""
+    rows, cols = t.shape
+    return t.data_ptr(), rows, cols * t.element_size(), t.stride(0) * t.element_size()
+
+
+def _operand(t, rows, cols, ld, stream, *outputs):
+    """(tensor, row stride): `t` itself where the tensor cores' loads can read it in place (16-byte aligned rows), else a copy with padded rows.
+
+    The library refuses outputs over the operands that it is given; over an operand that is copied they are refused here.
+    """
     if t.data_ptr() % 16 == 0 and (rows <= 1 or ld % 8 == 0):
         return t, ld
+    for out in outputs:
+        if out is not None and lib().psgd_overlap(*_stretch(t), *_stretch(out)):
+            raise PSGDError("an output overlaps an operand")
     pad = -(-cols // 8) * 8
     copy = _empty((rows, pad), dtype=t.dtype, device=t.device)
     _check(lib().psgd_copy_rows(t.data_ptr(), ld, rows, cols, copy.data_ptr(), pad, stream))
@@ -130,8 +142,8 @@ def _xent(grad, hidden, weight, labels, token_weight, ignore_index, d_hidden, d_
         with _there(dev, stream, hidden, weight, labels, token_weight, d_hidden, d_weight, status):
             return _xent(grad, hidden, weight, labels, token_weight, ignore_index, d_hidden, d_weight, status, None)
     nbytes = _workspace_bytes("psgd_xent_workspace", T, V, D, int(grad), dev.index)
-    hidden, ldh = _operand(hidden, T, D, ldh, s)
-    weight, ldw = _operand(weight, V, D, ldw, s)
+    hidden, ldh = _operand(hidden, T, D, ldh, s, d_hidden, d_weight)
+    weight, ldw = _operand(weight, V, D, ldw, s, d_hidden, d_weight)
     ws = _empty(nbytes, dtype=torch.uint8, device=dev)
     out = _empty(2 * T + 1, dtype=torch.float32, device=dev)
     at = out.data_ptr()                             # token_loss, lse, loss side by side
@@ -256,7 +268,7 @@ def weight_gradient(dy, kept, dtype=torch.float32, out=None, status=None, stream
         with _there(dev, stream, dy, kept._buf, out, status):
             return weight_gradient(dy, kept, dtype, out, status)
     nbytes = _workspace_bytes("psgd_act_wgrad_workspace", T, O, F, dev.index)
-    dy, ldy = _operand(dy, T, O, ldy, s)
+    dy, ldy = _operand(dy, T, O, ldy, s, out)
     ws = _empty(nbytes, dtype=torch.uint8, device=dev)
     if out is None:
         out = _empty((O, F), dtype=dtype, device=dev)
