@@ -202,14 +202,16 @@ bool tiles_ok(int64_t M, int64_t N) { return ((M + 255) / 256) * ((N + 127) / 12
 // ---- cross entropy ----
 constexpr int64_t XENT_PIECE_LOGITS = (int64_t)1 << 29;   // logits whose 16-bit form the workspace holds at a time (1 GiB; half as many: 3 to 4 % slower)
 
+constexpr int64_t XENT_PIECE_STATS = (int64_t)1 << 25;    // loss alone: statistics of 128 logits that it holds at a time (256 MiB)
+
 struct XentPlan {
     int pairs, nseg;
     int64_t ldq, piece, pieces;
     TilePlan logits, two[2];          // of a whole piece; two: dH and dW
     size_t inv, done, sums, stats, label_logit, q, part, acc, total;
 };
-// Tokens are taken in pieces, all columns at a time, so that the stored exponents stay within a fixed size however many
-// tokens there are; a piece has at least 1024 tokens, below which the products with the vocabulary matrix would be bound by reading it.
+// Tokens are taken in pieces, all columns at a time, so that the stored exponents (loss alone: the statistics) stay within a fixed size however
+// many tokens there are; a piece has at least 1024 tokens, below which the products with the vocabulary matrix would be bound by reading it.
 void plan_gradients(TilePlan (&p)[2], int64_t rows, int64_t V, int64_t D, int pairs) {
     const int64_t M[2] = {rows, V}, K[2] = {V, rows};
     plan_two(p, M, D, K, pairs);
@@ -219,14 +221,10 @@ XentPlan plan_xent(int64_t T, int64_t V, int64_t D, bool grad) {
     x.pairs = std::max(1, device_sms() / 2);
     x.nseg = ceil_div(V, grad ? XE_SEG : XE_SEG_LOSS);
     x.ldq = (int64_t)align_up(V, XE_SEG);
-    x.pieces = 1;
-    x.piece = T;
-    if (grad) {
-        const int64_t fit = std::max<int64_t>(1024, XENT_PIECE_LOGITS / x.ldq / TG_BM * TG_BM);
-        x.pieces = ceil_div(T, fit);
-        x.piece = std::min<int64_t>(T, align_up(ceil_div(T, x.pieces), TG_BM));
-        x.pieces = ceil_div(T, x.piece);
-    }
+    const int64_t fit = std::max<int64_t>(1024, (grad ? XENT_PIECE_LOGITS / x.ldq : XENT_PIECE_STATS / x.nseg) / TG_BM * TG_BM);
+    x.pieces = ceil_div(T, fit);
+    x.piece = std::min<int64_t>(T, align_up(ceil_div(T, x.pieces), TG_BM));
+    x.pieces = ceil_div(T, x.piece);
     x.logits = plan_tiles(x.piece, V, D, x.pairs, false);
     size_t at = 256;                                  // the status word of calls that bring none
     auto take = [&](size_t bytes) { const size_t o = at; at = align_up(at + bytes, 256); return o; };
@@ -312,7 +310,7 @@ psgd_status xent(const void* H, int64_t ldh, const void* W, int64_t ldw, const i
         psgd_status s = grad ? launch_softmax<EPI_SOFTMAX>(oh, ow, pl, a, x.pairs, st) : launch_softmax<EPI_LOSS>(oh, ow, pl, a, x.pairs, st);
         if (s != PSGD_OK) return s;
         r.rows = (int)rows;
-        r.first_sum = (int)t0;                        // (without gradients there is one piece)
+        r.first_sum = (int)(grad ? t0 : t0 / (XE_THREADS / 32));      // (pieces are whole row tiles)
         r.labels = (const long long*)labels + t0;
         r.weight = weight ? weight + t0 : nullptr;
         r.loss = token_loss + t0;

@@ -119,3 +119,12 @@ def test_overlapping_outputs_are_refused(L):
         return
     for size, dw in ((4, p), (2, p + 2 * 7), (4, p + 5 * 48 - 8)):         # dY: 6 rows of 16, 24 apart
         assert L.psgd_act_wgrad(p, 24, p, p, 6, 16, 9, dw, 24, 0 if size == 4 else 1, None, p, 1 << 40, None) == -1
+
+
+def test_loss_workspace_is_bounded_in_tokens(L):
+    """Statistics (8 bytes per 128 logits) of at most 2^25 x 128 logits at a time, and 16 bytes per 8 tokens; never more than the gradients need."""
+    for V in (32000, 131072):
+        for T in (1 << 17, 1 << 20, 1 << 24):
+            n = size(L, "psgd_xent_workspace", T, V, 2048, 0)
+            assert n <= (1 << 28) + (1 << 25) // (V // 128) * 4 + 2 * T + 4096
+            assert n <= size(L, "psgd_xent_workspace", T, V, 2048, 1)

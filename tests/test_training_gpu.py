@@ -835,3 +835,22 @@ def test_outputs_beside_inputs_but_not_over_them(torch, ops):
     kept = ops.pack_activation(h)
     with pytest.raises(ops.PSGDError):
         ops.weight_gradient(dy, kept, out=dy[:, :D])
+
+
+def test_loss_of_many_tokens_in_pieces(torch, ops):
+    """More statistics than the workspace holds at a time: three pieces of tokens, the same bits per token as from calls that take one, and the mean over all of them."""
+    T, V, D = 70001, 131072 - 5, 16
+    h, w, labels = xent_inputs(torch, T, V, D, seed=61)
+    labels[12345] = V - 1
+    tw = torch.rand(T, generator=gen(torch, 62), device="cuda")
+    r = ops.linear_cross_entropy(h, w, labels, token_weight=tw)
+    for a in range(0, T, 20000):
+        s = slice(a, min(T, a + 20000))
+        one = ops.linear_cross_entropy(h[s], w, labels[s], token_weight=tw[s])
+        assert torch.equal(r.lse[s], one.lse) and torch.equal(r.token_loss[s], one.token_loss)
+    tail = slice(T - 500, T)
+    z = h[tail].double() @ w.double().T
+    within(r.lse[tail], torch.logsumexp(z, 1), sum_bound(D) * (h[tail].double().abs() @ w.double().abs().T).amax(1) + 2.0 ** -18 + 2.0 ** -22 * 16)
+    wt = tw.double() * (labels != -100)
+    loss = float((wt * r.token_loss.double()).sum() / wt.sum())
+    assert abs(float(r.loss) - loss) <= 2.0 ** -23 * abs(loss) * 2
