@@ -47,7 +47,7 @@ typedef enum {
     PSGD_E_INVALID = -1,    /* argument out of range (m < n, r > n, r > 128, ...) */
     PSGD_E_NULL = -2,       /* required pointer is NULL */
     PSGD_E_WORKSPACE = -3,  /* workspace too small or buffers not attached */
-    PSGD_E_CUDA = -4,       /* a CUDA runtime call failed; see psgd_last_cuda_error */
+    PSGD_E_CUDA = -4,       /* a CUDA runtime call failed; see psgd_last_cuda_error, psgd_training_cuda_error */
     PSGD_E_STATE = -5,      /* call not valid in the handle's current state */
     PSGD_E_TOO_LARGE = -6   /* problem does not fit the fixed scratch of psgd_backproject_static */
 } psgd_status;
@@ -336,6 +336,9 @@ psgd_status psgd_backproject_static(const float* M /*DEVICE*/, const float* P_ha
  */
 #define PSGD_DT_F32 0
 #define PSGD_DT_BF16 1
+
+/* Text of the CUDA error behind the last of the calling thread's calls below that returned PSGD_E_CUDA (static storage; never NULL). */
+const char* psgd_training_cuda_error(void);
 
 /* 1 where two matrices share a byte, else 0: `rows` stretches of `width` bytes, `step` >= width bytes apart.  Reads nothing behind the addresses. */
 int psgd_overlap(const void* a, int64_t rows_a, int64_t width_a, int64_t step_a, const void* b, int64_t rows_b, int64_t width_b, int64_t step_b);

@@ -58,6 +58,7 @@ SIGNATURES = {
     "psgd_group_create": (_int, [C.POINTER(_vp), _int, C.POINTER(_vp)]),
     "psgd_group_step": (_int, [_vp, C.POINTER(_vp), C.POINTER(_vp), _vp]),
     "psgd_group_destroy": (_int, [_vp]),
+    "psgd_training_cuda_error": (C.c_char_p, []),
     "psgd_overlap": (_int, [_vp, _i64, _i64, _i64, _vp, _i64, _i64, _i64]),
     "psgd_xent_workspace": (_int, [_i64, _i64, _i64, _int, C.POINTER(_sz)]),
     "psgd_xent_loss": (_int, [_vp, _i64, _vp, _i64, _vp, _vp, _i64, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),

@@ -3,6 +3,8 @@
 // layout and the stream-ordered sequence of kernels; nothing here allocates, synchronises or keeps anything between calls.
 #include "../../include/psgd.h"
 
+#include <stdio.h>
+
 #include <algorithm>
 
 #include "psgd_act.cuh"
@@ -13,6 +15,19 @@
 using namespace psgd;
 
 namespace {
+
+// What is behind the last PSGD_E_CUDA of this thread's calls (there is no handle to keep it in).
+thread_local char call_error[160] = "no error";
+psgd_status cuda_error(const char* what, const char* why) {
+    snprintf(call_error, sizeof(call_error), "%s: %s", what, why);
+    return PSGD_E_CUDA;
+}
+bool succeeded(const char* what, cudaError_t e) {
+    if (e == cudaSuccess) return true;
+    cuda_error(what, cudaGetErrorString(e));
+    cudaGetLastError();                               // not left for whoever asks next
+    return false;
+}
 
 constexpr int64_t MAX_EXTENT = (int64_t)1 << 30;
 constexpr int KACC_F32 = 32;       // stages (2048 of k) per accumulator where the result is float32: the tensor cores' additions truncate, and the
@@ -96,14 +111,19 @@ size_t part_bytes(const TilePlan& p) { return p.parts ? (size_t)(p.units - p.ful
 // bfloat16 matrix, `rows` rows of `cols` with row stride ld (elements): boxes of 64 columns and `box` rows, 128-byte swizzle
 bool encode_operand(CUtensorMap* map, const void* p, int64_t rows, int64_t cols, int64_t ld, int box) {
     EncodeTiledFn fn = encode_tiled_fn();
-    if (!fn) return false;
+    if (!fn) {
+        cuda_error("cuTensorMapEncodeTiled", "not found in the driver");
+        return false;
+    }
     if (rows == 1) ld = align_up(cols, 8);                             // the stride of a single row is never used
     cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
     cuuint64_t strides[1] = {(cuuint64_t)ld * 2};
     cuuint32_t b[2] = {64, (cuuint32_t)box};
     cuuint32_t es[2] = {1, 1};
-    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, (void*)p, dims, strides, b, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    if (fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, (void*)p, dims, strides, b, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS) return true;
+    cuda_error("cuTensorMapEncodeTiled", "operand refused");
+    return false;
 }
 
 void set_problem(TileProblem& t, const TilePlan& p) {
@@ -122,9 +142,7 @@ bool launch(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, cudaS
     at.val.programmaticStreamSerializationAllowed = 1;
     c.attrs = &at;
     c.numAttrs = 1;
-    if (cudaLaunchKernelEx(&c, kernel, Params(args)...) == cudaSuccess) return true;
-    cudaGetLastError();                               // not left for whoever asks next
-    return false;
+    return succeeded("kernel launch", cudaLaunchKernelEx(&c, kernel, Params(args)...));
 }
 
 struct Operand { const void* p; int64_t ld; bool mn; };      // mn: stored [K][rows], else [rows][K]
@@ -262,8 +280,8 @@ psgd_status xent(const void* H, int64_t ldh, const void* W, int64_t ldw, const i
         if (overlap(dh, h) || overlap(dh, v) || overlap(dw, h) || overlap(dw, v) || overlap(dh, dw)) return PSGD_E_INVALID;
     }
     if (T == 0) {                                     // no token: loss 0, no gradient
-        if (cudaMemsetAsync(loss, 0, 4, st) != cudaSuccess) return PSGD_E_CUDA;
-        if (grad && cudaMemset2DAsync(dW, (size_t)lddw * 2, 0, (size_t)D * 2, (size_t)V, st) != cudaSuccess) return PSGD_E_CUDA;
+        if (!succeeded("cudaMemsetAsync", cudaMemsetAsync(loss, 0, 4, st))) return PSGD_E_CUDA;
+        if (grad && !succeeded("cudaMemset2DAsync", cudaMemset2DAsync(dW, (size_t)lddw * 2, 0, (size_t)D * 2, (size_t)V, st))) return PSGD_E_CUDA;
         return PSGD_OK;
     }
     const XentPlan x = plan_xent(T, V, D, grad);
@@ -415,6 +433,8 @@ WgradPlan plan_wgrad(int64_t T, int64_t O, int64_t F, bool by_parts) {
 
 extern "C" {
 
+const char* psgd_training_cuda_error(void) { return call_error; }
+
 int psgd_overlap(const void* a, int64_t rows_a, int64_t width_a, int64_t step_a, const void* b, int64_t rows_b, int64_t width_b, int64_t step_b) {
     return overlap({a, rows_a, width_a, rows_a == 1 ? width_a : step_a}, {b, rows_b, width_b, rows_b == 1 ? width_b : step_b});
 }
@@ -430,7 +450,7 @@ psgd_status psgd_xent_loss(const void* H, int64_t ldh, const void* W, int64_t ld
                            int64_t D, float* loss, float* token_loss, float* lse, int* status, void* ws, size_t ws_bytes, psgd_stream stream) try {
     return xent(H, ldh, W, ldw, labels, weight, ignore, T, V, D, loss, token_loss, lse, false, nullptr, 0, nullptr, 0, status, ws, ws_bytes, (cudaStream_t)stream);
 } catch (...) {
-    return PSGD_E_CUDA;
+    return cuda_error("host", "exception");
 }
 
 psgd_status psgd_xent_grad(const void* H, int64_t ldh, const void* W, int64_t ldw, const int64_t* labels, const float* weight, int64_t ignore, int64_t T, int64_t V,
@@ -438,7 +458,7 @@ psgd_status psgd_xent_grad(const void* H, int64_t ldh, const void* W, int64_t ld
                            psgd_stream stream) try {
     return xent(H, ldh, W, ldw, labels, weight, ignore, T, V, D, loss, token_loss, lse, true, dH, lddh, dW, lddw, status, ws, ws_bytes, (cudaStream_t)stream);
 } catch (...) {
-    return PSGD_E_CUDA;
+    return cuda_error("host", "exception");
 }
 
 psgd_status psgd_act_pack(const void* x, int64_t ldx, int dtype, int64_t T, int64_t F, int8_t* q, uint8_t* scales, psgd_stream stream) {
@@ -484,7 +504,7 @@ psgd_status psgd_act_wgrad(const void* dY, int64_t lddy, const int8_t* q, const 
     if (lddw < F || ((uintptr_t)ws & 255) || (T > 0 && (!operand_ok(dY, T, O, lddy) || !ckpt_ok(q)))) return PSGD_E_INVALID;
     if (T == 0) {
         const size_t es = dtype == PSGD_DT_F32 ? 4 : 2;
-        return cudaMemset2DAsync(dW, (size_t)lddw * es, 0, (size_t)F * es, (size_t)O, st) == cudaSuccess ? PSGD_OK : PSGD_E_CUDA;
+        return succeeded("cudaMemset2DAsync", cudaMemset2DAsync(dW, (size_t)lddw * es, 0, (size_t)F * es, (size_t)O, st)) ? PSGD_OK : PSGD_E_CUDA;
     }
     const bool vec = aligned16(dW) && lddw % (dtype == PSGD_DT_F32 ? 4 : 8) == 0;
     WgradPlan g = plan_wgrad(T, O, F, dtype == PSGD_DT_F32 && !vec);
@@ -505,7 +525,7 @@ psgd_status psgd_act_wgrad(const void* dY, int64_t lddy, const int8_t* q, const 
     const TilePlan p[2] = {g.p, {}};
     return launch_products(1, A, B, p, a, g.pairs, st);
 } catch (...) {
-    return PSGD_E_CUDA;
+    return cuda_error("host", "exception");
 }
 
 psgd_status psgd_swiglu_forward(const void* gate, int64_t ldg, const void* up, int64_t ldu, int64_t T, int64_t F, void* h, int64_t ldh, int8_t* q_gate, uint8_t* s_gate,

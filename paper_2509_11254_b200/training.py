@@ -20,7 +20,8 @@ from functools import lru_cache
 
 import torch
 
-from .binding import PSGDError, _check, lib
+from . import binding
+from .binding import PSGDError, lib
 
 PSGD_W_LABEL = 8
 GROUP = 32
@@ -31,6 +32,14 @@ CrossEntropy = namedtuple("CrossEntropy", "loss token_loss lse")
 CrossEntropyGrad = namedtuple("CrossEntropyGrad", "loss token_loss lse d_hidden d_weight")
 
 _empty = torch.empty
+
+
+def _check(code):
+    """Raises PSGDError for a call that failed; these calls have no handle, the library keeps the text of a CUDA error per thread."""
+    if code == -4:
+        raise PSGDError("PSGD_E_CUDA: " + lib().psgd_training_cuda_error().decode())
+    if code != 0:
+        binding._check(code)
 
 
 # ---- arguments ----------------------------------------------------------------------------------------------------

@@ -128,3 +128,25 @@ def test_loss_workspace_is_bounded_in_tokens(L):
             n = size(L, "psgd_xent_workspace", T, V, 2048, 0)
             assert n <= (1 << 28) + (1 << 25) // (V // 128) * 4 + 2 * T + 4096
             assert n <= size(L, "psgd_xent_workspace", T, V, 2048, 1)
+
+
+def test_failed_launch_says_why(L):
+    """Without a GPU every launch fails: the exception carries the runtime's text, and it is this thread's."""
+    import threading
+
+    import torch
+
+    from paper_2509_11254_b200 import PSGDError, training
+
+    if torch.cuda.is_available():
+        pytest.skip("the address below is made up")
+    p = 1 << 20
+    code = L.psgd_act_pack(p, 64, 1, 8, 64, p, p, None)
+    assert code == -4
+    with pytest.raises(PSGDError, match="PSGD_E_CUDA: kernel launch: .*(device|driver)"):
+        training._check(code)
+    other = []
+    t = threading.Thread(target=lambda: other.append(L.psgd_training_cuda_error()))
+    t.start()
+    t.join()
+    assert other == [b"no error"]
