@@ -36,9 +36,9 @@ _empty = torch.empty
 
 def _check(code):
     """Raises PSGDError for a call that failed; these calls have no handle, the library keeps the text of a CUDA error per thread."""
-    if code == -4:
-        raise PSGDError("PSGD_E_CUDA: " + lib().psgd_training_cuda_error().decode())
     if code != 0:
+        if code == -4:
+            raise PSGDError("PSGD_E_CUDA: " + lib().psgd_training_cuda_error().decode())
         binding._check(code)
 
 
