@@ -10,11 +10,15 @@ Weight gradients can be written straight into a slot of a compressor's gradient 
 arguments and hands over pointers.  Every call is stream-ordered on `stream` (default: the current stream) and does not
 synchronise.  `status`, an int32 tensor with one element, collects the library's warning bits (PSGD_W_TIMEOUT, PSGD_W_LABEL); what a wait
 that ran out should have produced is NaN, with or without `status`.
+
+None of these calls takes part in autograd: gradients are results of their own (d_hidden, d_weight, swiglu_backward, weight_gradient), and what a call returns has no
+graph behind it.  linear_cross_entropy and swiglu_forward, whose results could be taken for differentiable ones, warn where an input requires a gradient.
 """
 from __future__ import annotations
 
 import contextlib
 import ctypes as C
+import warnings
 from collections import namedtuple
 from functools import lru_cache
 
@@ -102,6 +106,12 @@ def _operand(t, rows, cols, ld, stream, *outputs):
     return copy, pad
 
 
+def _no_graph(name, a, b, instead, depth):
+    """Warns, `depth` calls up, where autograd would lose the gradient of `a` or `b` without a word."""
+    if (a.requires_grad or b.requires_grad) and torch.is_grad_enabled():
+        warnings.warn(f"{name}: the results have no autograd graph, no gradient will reach its inputs; {instead}, or call it under torch.no_grad()", stacklevel=depth)
+
+
 # the handle of the current stream and the current device without the objects around them, where torch has it so
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
@@ -146,9 +156,11 @@ def _xent(grad, hidden, weight, labels, token_weight, ignore_index, d_hidden, d_
     lddh = _matrix(d_hidden, "d_hidden", shape=(T, D), device=dev)[2] if d_hidden is not None else D
     lddw = _matrix(d_weight, "d_weight", shape=(V, D), device=dev)[2] if d_weight is not None else D
     at_status = _status(status, dev)
+    if not grad:
+        _no_graph("linear_cross_entropy", hidden, weight, "linear_cross_entropy_grad returns the gradients", 4)
     s = _here(dev, stream)
     if s is None:
-        with _there(dev, stream, hidden, weight, labels, token_weight, d_hidden, d_weight, status):
+        with _there(dev, stream, hidden, weight, labels, token_weight, d_hidden, d_weight, status), torch.no_grad():
             return _xent(grad, hidden, weight, labels, token_weight, ignore_index, d_hidden, d_weight, status, None)
     nbytes = _workspace_bytes("psgd_xent_workspace", T, V, D, int(grad), dev.index)
     hidden, ldh = _operand(hidden, T, D, ldh, s, d_hidden, d_weight)
@@ -290,9 +302,10 @@ def swiglu_forward(gate, up, stream=None):
     T, F, ldg = _matrix(gate, "gate")
     dev = gate.device
     ldu = _matrix(up, "up", shape=(T, F), device=dev)[2]
+    _no_graph("swiglu_forward", gate, up, "swiglu_backward makes the gradients", 3)
     s = _here(dev, stream)
     if s is None:
-        with _there(dev, stream, gate, up):
+        with _there(dev, stream, gate, up), torch.no_grad():
             return swiglu_forward(gate, up)
     h = _empty((T, F), dtype=_BF16, device=dev)
     size = -(-T * -(-F // GROUP) * (GROUP + 1) // 256) * 256

@@ -854,3 +854,29 @@ def test_loss_of_many_tokens_in_pieces(torch, ops):
     wt = tw.double() * (labels != -100)
     loss = float((wt * r.token_loss.double()).sum() / wt.sum())
     assert abs(float(r.loss) - loss) <= 2.0 ** -23 * abs(loss) * 2
+
+
+# ---- autograd -----------------------------------------------------------------------------------------------------
+def test_lost_autograd_graph_is_warned_about(torch, ops):
+    """Results that look differentiable and are not: a warning where an input requires a gradient, none under no_grad, none from the calls that return gradients."""
+    import warnings
+
+    h, w, labels = xent_inputs(torch, 40, 90, 64, seed=71)
+    leaf = h.clone().requires_grad_()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for call in (lambda: ops.linear_cross_entropy(leaf, w, labels), lambda: ops.linear_cross_entropy(h, w.clone().requires_grad_(), labels, stream=side),
+                 lambda: ops.swiglu_forward(h, leaf), lambda: ops.swiglu_forward(leaf, h, stream=side)):
+        with pytest.warns(UserWarning, match="no autograd graph") as seen:
+            call()
+        assert len(seen) == 1 and seen[0].filename == __file__
+    with warnings.catch_warnings():
+        warnings.simplefilter("error")
+        with torch.no_grad():
+            ops.linear_cross_entropy(leaf, w, labels)
+            ops.swiglu_forward(leaf, leaf)
+        ops.linear_cross_entropy(h, w, labels)
+        ops.swiglu_forward(h, h)
+        ops.linear_cross_entropy_grad(leaf, w, labels)
+        ops.pack_activation(leaf)
+    torch.cuda.synchronize()
