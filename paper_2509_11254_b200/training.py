@@ -129,6 +129,8 @@ def _there(device, stream, *inputs):
     The inputs may have been allocated on another stream: their memory is not given away before this stream has read them.
     """
     stream = stream if stream is not None else torch.cuda.current_stream(device)
+    if stream.device != device:
+        raise PSGDError(f"stream is on {stream.device}, the tensors are on {device}")
     with torch.cuda.device(device), torch.cuda.stream(stream):
         yield
         for t in inputs:

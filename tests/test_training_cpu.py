@@ -150,3 +150,17 @@ def test_failed_launch_says_why(L):
     t.start()
     t.join()
     assert other == [b"no error"]
+
+
+def test_stream_of_another_device_is_refused():
+    """(It would make its own device current, on which the call would never find itself at home.)"""
+    import types
+
+    import torch
+
+    from paper_2509_11254_b200 import PSGDError, training
+
+    stream = types.SimpleNamespace(device=torch.device("cuda", 1), cuda_stream=0)
+    with pytest.raises(PSGDError, match="stream is on cuda:1"):
+        with training._there(torch.device("cuda", 0), stream):
+            pass
