@@ -880,3 +880,27 @@ def test_lost_autograd_graph_is_warned_about(torch, ops):
         ops.linear_cross_entropy_grad(leaf, w, labels)
         ops.pack_activation(leaf)
     torch.cuda.synchronize()
+
+
+def test_two_streams_at_once_with_inputs_made_before(torch, ops):
+    """Both streams find their inputs complete: nothing but the operators runs between the synchronisations."""
+    sets = [xent_inputs(torch, 700, 3000, 256, seed=s) for s in (81, 82)]
+    x = [torch.randn(500, 776, generator=gen(torch, s), device="cuda").to(torch.bfloat16) for s in (83, 84)]
+    dy = [t[:, :520].contiguous() for t in x]
+
+    def work(i, stream=None):
+        r = ops.linear_cross_entropy_grad(*sets[i], stream=stream)
+        only = ops.linear_cross_entropy(*sets[i], stream=stream)
+        kept = ops.pack_activation(x[i], stream=stream)
+        h, kg, ku = ops.swiglu_forward(x[i], x[i], stream=stream)
+        return [*r, *only, ops.weight_gradient(dy[i], kept, stream=stream), h, *ops.swiglu_backward(h, kg, ku, recompute=True, stream=stream), kept.unpack(stream=stream)]
+
+    want = [work(0), work(1)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    got = [[work(i, streams[i]) for i in (0, 1)] for _ in range(5)]
+    torch.cuda.synchronize()
+    for both in got:
+        for a, b in zip(both, want):
+            for u, v in zip(a, b):
+                assert torch.equal(u, v)
