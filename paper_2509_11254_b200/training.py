@@ -5,8 +5,8 @@
   weight_gradient                                    a linear layer's weight gradient from the 8-bit checkpoint of its input
   swiglu_forward, swiglu_backward                    the gated unit of a feed-forward block, its inputs kept in 8 bits
 
-Weight gradients can be written straight into a slot of a compressor's gradient stack G [count, N, m, n] (`d_weight=G[c, i]`,
-`out=G[c, i]`).  The arithmetic runs in the CUDA library (psgd_xent_*, psgd_act_*, psgd_swiglu_* of include/psgd.h); this module checks
+Weight gradients can be written straight into a slot of a compressor's gradient stack G [count, N, m, n] (`out=G[c, i]`, float32 or bfloat16;
+`d_weight=G[c, i]` of the last layer, a bfloat16 stack: `grad_dtype="bfloat16"`).  The arithmetic runs in the CUDA library (psgd_xent_*, psgd_act_*, psgd_swiglu_* of include/psgd.h); this module checks
 arguments and hands over pointers.  Every call is stream-ordered on `stream` (default: the current stream) and does not
 synchronise.  `status`, an int32 tensor with one element, collects the library's warning bits (PSGD_W_TIMEOUT, PSGD_W_LABEL); what a wait
 that ran out should have produced is NaN, with or without `status`.
@@ -198,7 +198,7 @@ def linear_cross_entropy(hidden, weight, labels, token_weight=None, ignore_index
 def linear_cross_entropy_grad(hidden, weight, labels, token_weight=None, ignore_index=-100, d_hidden=None, d_weight=None, status=None, stream=None):
     """The same with the gradients of the loss: returns (loss, token_loss, lse, d_hidden [T, D], d_weight [V, D]), the gradients bfloat16.
 
-    d_hidden, d_weight: where to write them (matrices with unit column stride), for instance a slot of a gradient stack; they may not overlap
+    d_hidden, d_weight: where to write them (bfloat16 matrices with unit column stride), for instance a slot of a bfloat16 gradient stack; they may not overlap
     `hidden`, `weight` or each other.
     """
     return _xent(True, hidden, weight, labels, token_weight, ignore_index, d_hidden, d_weight, status, stream)
