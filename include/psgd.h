@@ -399,6 +399,43 @@ psgd_status psgd_swiglu_backward(const void* dh /*DEVICE*/, int64_t lddh, const 
                                  const int8_t* q_up /*DEVICE*/, const uint8_t* s_up /*DEVICE*/, int64_t T, int64_t F, void* d_gate /*DEVICE*/, int64_t ldg,
                                  void* d_up /*DEVICE*/, int64_t ldu, void* h /*DEVICE*/, int64_t ldh, psgd_stream stream);
 
+/*
+ * Layer norm of the rows of x [T][F], with a residual sum on the way in and an 8-bit form of the result on the way out:
+ *     s = x + r (rounded to x's type; r may be NULL: s = x),  m = mean(s) (center = 0: 0),  f = 1 / sqrt(mean((s - m)^2) + eps),
+ *     y = (s - m) f w + b.
+ * x, r, s float32 or bfloat16 (x_dtype), y the same or bfloat16 beside a float32 x (y_dtype); w [F] and b [F] (or NULL) float32 or bfloat16 (w_dtype).
+ * s: required where r is given, else written where it is not NULL.  mean (required where center is not 0), rstd: [T] float32, m and f of every row.
+ * q, scales: where q is not NULL, the 8-bit form of y as psgd_act_pack of y makes it.
+ *
+ * The gradients from dy [T][F] (types as y's), x = the s of the forward pass, and its mean (NULL: without centring) and rstd:
+ *     dx = f (g - mean(g) [with centring] - xh mean(g xh)) + add,  g = dy w,  xh = (x - m) f,   dw = sum_t dy xh,  db = sum_t dy.
+ * add [T][F] (x_dtype, may be NULL) is what reaches x from elsewhere, dx (x_dtype) the gradient of both x and r.  dw, db (may be NULL): [F] float32, summed
+ * in a fixed order.  Rows of any stride and alignment; outputs over inputs or over each other are refused.
+ */
+psgd_status psgd_norm_forward(const void* x /*DEVICE*/, int64_t ldx, int x_dtype, const void* r /*DEVICE*/, int64_t ldr, const void* w /*DEVICE*/, const void* b /*DEVICE*/,
+                              int w_dtype, float eps, int center, int64_t T, int64_t F, void* s /*DEVICE*/, int64_t lds, void* y /*DEVICE*/, int64_t ldy, int y_dtype,
+                              float* mean /*DEVICE*/, float* rstd /*DEVICE*/, int8_t* q /*DEVICE*/, uint8_t* scales /*DEVICE*/, psgd_stream stream);
+psgd_status psgd_norm_workspace(int64_t T, int64_t F, size_t* bytes /*HOST*/);
+psgd_status psgd_norm_backward(const void* dy /*DEVICE*/, int64_t lddy, int dy_dtype, const void* x /*DEVICE*/, int64_t ldx, int x_dtype, const void* w /*DEVICE*/, int w_dtype,
+                               const float* mean /*DEVICE*/, const float* rstd /*DEVICE*/, const void* add /*DEVICE*/, int64_t ldadd, int64_t T, int64_t F,
+                               void* dx /*DEVICE*/, int64_t lddx, float* dw /*DEVICE*/, float* db /*DEVICE*/, void* workspace /*DEVICE*/, size_t workspace_bytes,
+                               psgd_stream stream);
+
+/*
+ * Rotary positions of queries q [T][heads_q][head] and keys k [T][heads_k][head] (heads_k = 0: none) in one launch, float32 or bfloat16 (dtype).  The
+ * pairs of the first `rotated` values of every head, (i, i + rotated/2) or (2i, 2i + 1), are turned by the angle a = positions[t] frequencies[i] and scaled:
+ *     (u, v) -> scale (u cos a - v sin a, u sin a + v cos a);      backward != 0: the gradient's way, by -a.
+ * The other values are copied.  Strides of tokens and heads in elements, any for the inputs (values used several times included); no two values of an output
+ * may share a place.  positions [T] (any int64), frequencies [rotated/2] float64 radians per position; angles are exact modulo a turn up to the rounding of
+ * the frequencies.  An output may be its own input (same address and strides); any other overlap is refused.  rotated <= 4096, heads * head <= 2^30.
+ */
+#define PSGD_ROTARY_HALF 0
+#define PSGD_ROTARY_INTERLEAVED 1
+psgd_status psgd_rotary(const void* q /*DEVICE*/, int64_t q_token, int64_t q_head, int64_t heads_q, void* out_q /*DEVICE*/, int64_t oq_token, int64_t oq_head,
+                        const void* k /*DEVICE*/, int64_t k_token, int64_t k_head, int64_t heads_k, void* out_k /*DEVICE*/, int64_t ok_token, int64_t ok_head,
+                        const int64_t* positions /*DEVICE*/, const double* frequencies /*DEVICE*/, int64_t T, int64_t head, int64_t rotated, int layout, int backward,
+                        float scale, int dtype, psgd_stream stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -28,4 +28,13 @@ from .training import (  # noqa: F401,E402
     swiglu_forward,
     weight_gradient,
 )
+from .layers import (  # noqa: F401,E402
+    LayerNorm,
+    LayerNormGrad,
+    layer_norm_backward,
+    layer_norm_forward,
+    rotary_backward,
+    rotary_forward,
+    rotary_frequencies,
+)
 from .exchange import ExchangedStack, slot_offsets  # noqa: F401,E402

@@ -70,6 +70,10 @@ SIGNATURES = {
     "psgd_copy_rows": (_int, [_vp, _i64, _i64, _i64, _vp, _i64, _vp]),
     "psgd_swiglu_forward": (_int, [_vp, _i64, _vp, _i64, _i64, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp]),
     "psgd_swiglu_backward": (_int, [_vp, _i64, _vp, _vp, _vp, _vp, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp]),
+    "psgd_norm_forward": (_int, [_vp, _i64, _int, _vp, _i64, _vp, _vp, _int, C.c_float, _int, _i64, _i64, _vp, _i64, _vp, _i64, _int, _vp, _vp, _vp, _vp, _vp]),
+    "psgd_norm_workspace": (_int, [_i64, _i64, C.POINTER(_sz)]),
+    "psgd_norm_backward": (_int, [_vp, _i64, _int, _vp, _i64, _int, _vp, _int, _vp, _vp, _vp, _i64, _i64, _i64, _vp, _i64, _vp, _vp, _vp, _sz, _vp]),
+    "psgd_rotary": (_int, [_vp, _i64, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _i64, _i64, _vp, _i64, _i64, _vp, _vp, _i64, _i64, _i64, _int, _int, C.c_float, _int, _vp]),
 }
 
 

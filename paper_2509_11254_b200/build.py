@@ -6,7 +6,7 @@ import subprocess
 import sys
 
 HERE = os.path.dirname(os.path.abspath(__file__))
-SRCS = [os.path.join(HERE, "csrc", f) for f in ("psgd_api.cu", "psgd_lm.cu")]     # compiled side by side
+SRCS = [os.path.join(HERE, "csrc", f) for f in ("psgd_api.cu", "psgd_lm.cu", "psgd_layer.cu")]     # compiled side by side
 LIB = os.path.join(HERE, "libpsgd.so")
 OBJ_DIR = os.path.join(HERE, "_build")
 HEADER = os.path.join(os.path.dirname(HERE), "include", "psgd.h")

@@ -1,0 +1,214 @@
+// Host side of the operators between a layer's matrix products, declared in include/psgd.h: layer norm and rotary positions, forward and backward.
+// Argument checks, workspace layout and launches; nothing here allocates, synchronises or keeps anything between calls.
+#include "psgd_norm.cuh"
+#include "psgd_rotary.cuh"
+#include "psgd_train.cuh"
+
+using namespace psgd;
+
+namespace {
+
+typedef __nv_bfloat16 bf16;
+
+// Rows of 16-byte units: the address, the stride and the width allow eight values at a time.
+bool whole_units(const void* p, int64_t ld, int64_t F, int dtype) { return !p || (F % 8 == 0 && aligned16(p) && ld % (16 / size_of(dtype)) == 0); }
+bool rows_ok(int64_t T, int64_t F) { return T >= 0 && T <= MAX_EXTENT && extent_ok(F); }
+
+// ---- layer norm ----
+constexpr int NORM_WIDE = 2 * NORM_THREADS;         // units of a row from which it no longer fits its threads' registers
+
+// How a row's units are shared: `vpt` per thread, `threads` per row (whole warps), `rows` at a time per CTA.
+struct NormPlan { int vpt, threads, rows; bool wide; int64_t ctas; };
+NormPlan plan_norm(int64_t T, int64_t F, bool vec, int per_sm) {
+    NormPlan p{};
+    const int64_t units = vec ? (F + 7) / 8 : (F + 255) / 256 * 32;
+    p.wide = units > NORM_WIDE;
+    p.vpt = units > 256 ? 2 : 1;
+    p.threads = p.wide ? NORM_THREADS : (int)align_up(ceil_div(units, p.vpt), 32);
+    p.rows = p.wide ? 1 : std::max(1, 256 / p.threads);
+    p.ctas = std::min<int64_t>((T + p.rows - 1) / p.rows, (int64_t)device_sms() * std::max(1, per_sm / (p.threads * p.rows)));
+    return p;
+}
+constexpr int FORWARD_THREADS = 1024, BACKWARD_THREADS = 512;     // per multiprocessor
+
+struct NormGrad { NormPlan p; int64_t parts; size_t part, sums, total; };
+NormGrad plan_norm_grad(int64_t T, int64_t F, bool vec) {
+    NormGrad g{};
+    g.p = plan_norm(T, F, vec, BACKWARD_THREADS);
+    const int64_t tiles = (F + 2047) / 2048;
+    g.parts = g.p.wide ? std::min<int64_t>({T, 65535, std::max<int64_t>(1, device_sms() * 4 / tiles)}) : g.p.ctas;
+    g.part = 0;
+    g.sums = align_up((size_t)g.parts * 2 * F * 4, 256);
+    g.total = g.sums + (g.p.wide ? align_up((size_t)T * 8, 256) : 0);
+    return g;
+}
+
+template <typename X, typename Y, bool VEC>
+bool norm_forward(const NormForward& a, const NormPlan& p, cudaStream_t st) {
+    const dim3 grid((unsigned)p.ctas), block(p.threads, p.rows);
+    if (p.wide) return launch(k_norm_forward_wide<X, Y, VEC>, grid, block, 0, st, a);
+    return p.vpt == 1 ? launch(k_norm_forward<X, Y, VEC, 1>, grid, block, 0, st, a) : launch(k_norm_forward<X, Y, VEC, 2>, grid, block, 0, st, a);
+}
+template <typename X, typename Y, bool VEC>
+bool norm_backward(NormBackward a, const NormGrad& g, cudaStream_t st) {
+    const NormPlan& p = g.p;
+    const dim3 grid((unsigned)p.ctas), block(p.threads, p.rows);
+    if (p.wide) {
+        return launch(k_norm_sums_wide<X, Y, VEC>, grid, block, 0, st, a) &&
+               launch(k_norm_apply_wide<X, Y, VEC>, dim3(ceil_div(a.F, 2048), (unsigned)g.parts), dim3(256), 0, st, a);
+    }
+    const size_t smem = p.rows > 1 ? (size_t)2 * a.F * 4 : 0;
+    return p.vpt == 1 ? launch(k_norm_backward<X, Y, VEC, 1>, grid, block, smem, st, a) : launch(k_norm_backward<X, Y, VEC, 2>, grid, block, smem, st, a);
+}
+// the pairs of types: x and y (dy) alike, or x float32 and y bfloat16
+bool types_ok(int x, int y) { return dtype_ok(x) && dtype_ok(y) && (x == y || x == PSGD_DT_F32); }
+template <typename Call>
+bool by_type(int x, int y, bool vec, Call&& call) {
+    if (x == PSGD_DT_BF16) return vec ? call((bf16*)0, (bf16*)0, std::true_type()) : call((bf16*)0, (bf16*)0, std::false_type());
+    if (y == PSGD_DT_BF16) return vec ? call((float*)0, (bf16*)0, std::true_type()) : call((float*)0, (bf16*)0, std::false_type());
+    return vec ? call((float*)0, (float*)0, std::true_type()) : call((float*)0, (float*)0, std::false_type());
+}
+
+// ---- rotary positions ----
+// A tensor [T][heads][head] as stretches of bytes: rows of tokens with their heads in them, or rows of heads with their tokens; else (values that are used
+// several times, orders that mix) one stretch from its first byte to its last.  `once`: no value lies in two places.
+Stretch extent_of(const void* p, int64_t T, int64_t heads, int64_t head, int64_t token, int64_t step, int bytes, bool& once) {
+    if (heads <= 1) step = head;                       // (the stride of an extent of one is never used)
+    const int64_t in_token = (heads - 1) * step + head;
+    if (T <= 1) token = in_token;
+    const int64_t in_head = (T - 1) * token + head;
+    once = true;
+    if (step >= head && token >= in_token) return {p, T, in_token * bytes, token * bytes};
+    if (token >= head && step >= in_head) return {p, heads, in_head * bytes, step * bytes};
+    once = false;
+    const int64_t all = ((T - 1) * token + in_token) * bytes;
+    return {p, 1, all, all};
+}
+
+}  // namespace
+
+extern "C" {
+
+psgd_status psgd_norm_forward(const void* x, int64_t ldx, int x_dtype, const void* r, int64_t ldr, const void* w, const void* b, int w_dtype, float eps, int center, int64_t T,
+                              int64_t F, void* s, int64_t lds, void* y, int64_t ldy, int y_dtype, float* mean, float* rstd, int8_t* q, uint8_t* scales, psgd_stream stream) {
+    if (!rows_ok(T, F) || !types_ok(x_dtype, y_dtype) || !dtype_ok(w_dtype) || !(eps >= 0.f)) return PSGD_E_INVALID;
+    if (T == 0) return PSGD_OK;
+    if (!x || !w || !y || !rstd || (r && !s) || (center && !mean) || (q && !scales)) return PSGD_E_NULL;
+    if (ldx < F || ldy < F || (r && ldr < F) || (s && lds < F) || ((uintptr_t)q & 15)) return PSGD_E_INVALID;
+    const Stretch in[2] = {stretch(x, T, F, ldx, size_of(x_dtype)), stretch(r, T, F, ldr, size_of(x_dtype))};
+    const Stretch sum = stretch(s, T, F, lds, size_of(x_dtype)), out = stretch(y, T, F, ldy, size_of(y_dtype));
+    if (overlap(in[0], sum) || overlap(in[0], out) || overlap(in[1], sum) || overlap(in[1], out) || overlap(sum, out)) return PSGD_E_INVALID;
+    const bool vec = whole_units(x, ldx, F, x_dtype) && whole_units(r, ldr, F, x_dtype) && whole_units(s, lds, F, x_dtype) && whole_units(y, ldy, F, y_dtype);
+    NormForward a{};
+    a.T = T; a.F = (int)F; a.center = center != 0; a.eps = eps;
+    a.x = x; a.r = r; a.s = s; a.y = y;
+    a.ldx = ldx; a.ldr = ldr; a.lds = lds; a.ldy = ldy;
+    a.w = {w, w_dtype == PSGD_DT_BF16}; a.b = {b, w_dtype == PSGD_DT_BF16};
+    a.mean = center ? mean : nullptr; a.rstd = rstd; a.q = q; a.scales = scales;
+    const NormPlan p = plan_norm(T, F, vec, FORWARD_THREADS);
+    const bool ok = by_type(x_dtype, y_dtype, vec, [&](auto* tx, auto* ty, auto v) {
+        return norm_forward<std::remove_pointer_t<decltype(tx)>, std::remove_pointer_t<decltype(ty)>, decltype(v)::value>(a, p, (cudaStream_t)stream);
+    });
+    return ok ? PSGD_OK : PSGD_E_CUDA;
+}
+
+psgd_status psgd_norm_workspace(int64_t T, int64_t F, size_t* bytes) {
+    if (!bytes) return PSGD_E_NULL;
+    if (!rows_ok(T, F)) return PSGD_E_INVALID;
+    *bytes = T == 0 ? 256 : std::max(plan_norm_grad(T, F, true).total, plan_norm_grad(T, F, false).total);
+    return PSGD_OK;
+}
+
+psgd_status psgd_norm_backward(const void* dy, int64_t lddy, int dy_dtype, const void* x, int64_t ldx, int x_dtype, const void* w, int w_dtype, const float* mean,
+                               const float* rstd, const void* add, int64_t ldadd, int64_t T, int64_t F, void* dx, int64_t lddx, float* dw, float* db, void* ws,
+                               size_t ws_bytes, psgd_stream stream) {
+    cudaStream_t st = (cudaStream_t)stream;
+    if (!rows_ok(T, F) || !types_ok(x_dtype, dy_dtype) || !dtype_ok(w_dtype)) return PSGD_E_INVALID;
+    if (!dw || !ws || (T > 0 && (!dy || !x || !w || !rstd || !dx))) return PSGD_E_NULL;
+    if (T == 0)
+        return succeeded("cudaMemsetAsync", cudaMemsetAsync(dw, 0, (size_t)F * 4, st)) && (!db || succeeded("cudaMemsetAsync", cudaMemsetAsync(db, 0, (size_t)F * 4, st))) ? PSGD_OK
+                                                                                                                                                          : PSGD_E_CUDA;
+    if (lddy < F || ldx < F || (add && ldadd < F) || lddx < F || ((uintptr_t)ws & 255)) return PSGD_E_INVALID;
+    const int size = size_of(x_dtype);
+    const Stretch out = stretch(dx, T, F, lddx, size);
+    if (overlap(out, stretch(dy, T, F, lddy, size_of(dy_dtype))) || overlap(out, stretch(x, T, F, ldx, size)) || overlap(out, stretch(add, T, F, ldadd, size))) return PSGD_E_INVALID;
+    const bool vec = whole_units(dy, lddy, F, dy_dtype) && whole_units(x, ldx, F, x_dtype) && whole_units(add, ldadd, F, x_dtype) && whole_units(dx, lddx, F, x_dtype);
+    const NormGrad g = plan_norm_grad(T, F, vec);
+    if (ws_bytes < g.total) return PSGD_E_WORKSPACE;
+    NormBackward a{};
+    a.T = T; a.F = (int)F; a.center = mean != nullptr;
+    a.dy = dy; a.x = x; a.add = add; a.dx = dx;
+    a.lddy = lddy; a.ldx = ldx; a.ldadd = ldadd; a.lddx = lddx;
+    a.w = {w, w_dtype == PSGD_DT_BF16};
+    a.mean = mean; a.rstd = rstd;
+    a.part = (float*)((char*)ws + g.part);
+    a.sums = (float2*)((char*)ws + g.sums);
+    const bool ok = by_type(x_dtype, dy_dtype, vec, [&](auto* tx, auto* ty, auto v) {
+        return norm_backward<std::remove_pointer_t<decltype(tx)>, std::remove_pointer_t<decltype(ty)>, decltype(v)::value>(a, g, st);
+    });
+    if (!ok) return PSGD_E_CUDA;
+    const NormJoin j{(int)F, (int)g.parts, a.part, dw, db};
+    return launch(k_norm_join, dim3(ceil_div(F, 32), db ? 2 : 1), dim3(1024), 0, st, j) ? PSGD_OK : PSGD_E_CUDA;
+}
+
+psgd_status psgd_rotary(const void* q, int64_t q_token, int64_t q_head, int64_t heads_q, void* out_q, int64_t oq_token, int64_t oq_head, const void* k, int64_t k_token,
+                        int64_t k_head, int64_t heads_k, void* out_k, int64_t ok_token, int64_t ok_head, const int64_t* positions, const double* frequencies, int64_t T,
+                        int64_t head, int64_t rotated, int layout, int backward, float scale, int dtype, psgd_stream stream) {
+    if (T < 0 || T > MAX_EXTENT || heads_q < 0 || heads_k < 0 || heads_q + heads_k > 65536 || head < 1 || (heads_q + heads_k) * head > MAX_EXTENT) return PSGD_E_INVALID;
+    if (rotated < 2 || rotated % 2 || rotated > head || rotated > 2 * ROT_PAIRS || !dtype_ok(dtype)) return PSGD_E_INVALID;
+    if (layout != PSGD_ROTARY_HALF && layout != PSGD_ROTARY_INTERLEAVED) return PSGD_E_INVALID;
+    const int64_t strides[8] = {q_token, q_head, oq_token, oq_head, k_token, k_head, ok_token, ok_head};
+    for (int64_t s : strides)
+        if (s < 0) return PSGD_E_INVALID;
+    const int64_t heads = heads_q + heads_k;
+    if (T == 0 || heads == 0) return PSGD_OK;
+    if (!positions || !frequencies || (heads_q && (!q || !out_q)) || (heads_k && (!k || !out_k))) return PSGD_E_NULL;
+    const RotaryTensor t[2] = {{q, out_q, q_token, q_head, oq_token, oq_head}, {k, out_k, k_token, k_head, ok_token, ok_head}};
+    const int64_t count[2] = {heads_q, heads_k};
+    bool vec = true, in_place = true;
+    const int64_t unit = 16 / size_of(dtype);
+    Stretch in[2] = {}, out[2] = {};
+    for (int i = 0; i < 2; ++i) {
+        if (!count[i]) continue;
+        bool once;
+        in[i] = extent_of(t[i].in, T, count[i], head, t[i].in_token, t[i].in_head, size_of(dtype), once);
+        out[i] = extent_of(t[i].out, T, count[i], head, t[i].out_token, t[i].out_head, size_of(dtype), once);
+        if (!once) return PSGD_E_INVALID;              // two values would be written to one place
+        const auto even = [&](int64_t token, int64_t step) { return (T == 1 || token % unit == 0) && (count[i] == 1 || step % unit == 0); };
+        vec = vec && aligned16(t[i].in) && aligned16(t[i].out) && even(t[i].in_token, t[i].in_head) && even(t[i].out_token, t[i].out_head);
+        in_place = in_place && t[i].in == t[i].out;
+    }
+    for (int i = 0; i < 2; ++i)
+        for (int j = 0; j < 2; ++j) {
+            // in place: the very tensor, so that every value is read and written by one thread
+            const bool same = i == j && t[i].in == t[i].out && (T == 1 || t[i].in_token == t[i].out_token) && (count[i] <= 1 || t[i].in_head == t[i].out_head);
+            if (count[i] && count[j] && !same && overlap(out[i], in[j])) return PSGD_E_INVALID;
+        }
+    if (heads_q && heads_k && overlap(out[0], out[1])) return PSGD_E_INVALID;
+    const bool half = layout == PSGD_ROTARY_HALF;
+    vec = vec && head % 8 == 0 && rotated % (half ? 16 : 8) == 0;
+    RotaryArgs a{};
+    a.T = T; a.heads_q = (int)heads_q; a.heads = (int)heads; a.rotated = (int)rotated; a.head = (int)head;
+    a.turned = (int)(vec ? (half ? rotated / 16 : rotated / 8) : rotated / 2);
+    a.per_head = a.turned + (in_place ? 0 : (int)((head - rotated) / (vec ? 8 : 1)));
+    const int64_t items = heads * a.per_head;          // per token
+    const int sms = device_sms();
+    // tokens of a CTA at a time: two rounds of items where there are enough tokens for every CTA, as many angles as shared memory is set aside for
+    a.tokens = (int)std::max<int64_t>(1, std::min<int64_t>({2 * ROT_THREADS * ROT_ITEMS / items, T / (4 * sms), ROT_PAIRS / (rotated / 2)}));
+    a.by_head = fast_div((unsigned)a.per_head); a.by_heads = fast_div((unsigned)heads); a.by_pairs = fast_div((unsigned)(rotated / 2));
+    a.q = t[0]; a.k = t[1];
+    a.positions = (const long long*)positions;
+    a.frequencies = frequencies;
+    a.scale = scale;
+    a.sign = backward ? -1.f : 1.f;
+    const dim3 grid((unsigned)std::min<int64_t>((T + a.tokens - 1) / a.tokens, (int64_t)sms * 8));
+    const auto run = [&](auto kernel) { return launch(kernel, grid, dim3(ROT_THREADS), 0, (cudaStream_t)stream, a) ? PSGD_OK : PSGD_E_CUDA; };
+    if (dtype == PSGD_DT_BF16) {
+        if (vec) return half ? run(k_rotary<bf16, 8, true>) : run(k_rotary<bf16, 8, false>);
+        return half ? run(k_rotary<bf16, 1, true>) : run(k_rotary<bf16, 1, false>);
+    }
+    if (vec) return half ? run(k_rotary<float, 8, true>) : run(k_rotary<float, 8, false>);
+    return half ? run(k_rotary<float, 1, true>) : run(k_rotary<float, 1, false>);
+}
+
+}  // extern "C"

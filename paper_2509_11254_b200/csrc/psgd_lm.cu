@@ -10,26 +10,20 @@
 #include "psgd_act.cuh"
 #include "psgd_host.cuh"
 #include "psgd_tile.cuh"
+#include "psgd_train.cuh"
 #include "psgd_xent.cuh"
 
 using namespace psgd;
 
-namespace {
-
 // What is behind the last PSGD_E_CUDA of this thread's calls (there is no handle to keep it in).
-thread_local char call_error[160] = "no error";
-psgd_status cuda_error(const char* what, const char* why) {
+static thread_local char call_error[160] = "no error";
+psgd_status psgd::cuda_error(const char* what, const char* why) {
     snprintf(call_error, sizeof(call_error), "%s: %s", what, why);
     return PSGD_E_CUDA;
 }
-bool succeeded(const char* what, cudaError_t e) {
-    if (e == cudaSuccess) return true;
-    cuda_error(what, cudaGetErrorString(e));
-    cudaGetLastError();                               // not left for whoever asks next
-    return false;
-}
 
-constexpr int64_t MAX_EXTENT = (int64_t)1 << 30;
+namespace {
+
 constexpr int KACC_F32 = 32;       // stages (2048 of k) per accumulator where the result is float32: the tensor cores' additions truncate, and the
                                    // error grows with the number of additions into one running sum (16384 of k: 1.3e-6 with 64, 0.6e-6 with 32).
                                    // A bfloat16 result keeps one sum over all of k: its rounding, 2e-3, is far above that.
@@ -133,19 +127,6 @@ void set_problem(TileProblem& t, const TilePlan& p) {
     t.by_group = fast_div((unsigned)p.gm * p.nt); t.by_gm = fast_div(p.gm); t.by_rest = fast_div(std::max(1, p.mt % p.gm)); t.by_tail = fast_div(std::max(1, p.tail));
 }
 
-// Launch that may start before the kernel in front of it on the stream has finished (the kernels wait for that themselves).
-template <typename... Params, typename... Args>
-bool launch(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, const Args&... args) {
-    cudaLaunchConfig_t c{};
-    c.gridDim = grid; c.blockDim = block; c.dynamicSmemBytes = smem; c.stream = st;
-    cudaLaunchAttribute at{};
-    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at.val.programmaticStreamSerializationAllowed = 1;
-    c.attrs = &at;
-    c.numAttrs = 1;
-    return succeeded("kernel launch", cudaLaunchKernelEx(&c, kernel, Params(args)...));
-}
-
 struct Operand { const void* p; int64_t ld; bool mn; };      // mn: stored [K][rows], else [rows][K]
 bool encode(CUtensorMap* map, const Operand& o, int64_t rows, int64_t K, int box) {
     return o.mn ? encode_operand(map, o.p, K, rows, o.ld, TG_BK) : encode_operand(map, o.p, rows, K, o.ld, box);
@@ -195,27 +176,6 @@ psgd_status launch_products(int count, const Operand (&A)[2], const Operand (&B)
 }
 
 bool operand_ok(const void* p, int64_t rows, int64_t cols, int64_t ld) { return aligned16(p) && ld >= cols && (rows == 1 || ld % 8 == 0); }
-bool extent_ok(int64_t v) { return v >= 1 && v <= MAX_EXTENT; }
-// Bytes of a matrix in memory: `rows` stretches of `width`, `step` apart (width <= step).
-struct Stretch { const void* p; int64_t rows, width, step; };
-bool overlap(const Stretch& a, const Stretch& b) {
-    if (!a.p || !b.p || a.rows < 1 || b.rows < 1) return false;
-    if (a.rows > b.rows) return overlap(b, a);
-    const int64_t at = (int64_t)((uintptr_t)a.p - (uintptr_t)b.p);               // of a's first row, from b's
-    const int64_t end_a = at + (a.rows - 1) * a.step + a.width, end_b = (b.rows - 1) * b.step + b.width;
-    if (at >= end_b || end_a <= 0) return false;
-    // rows that lie between one another (columns of one wider matrix): row by row; with equal steps the first rows that face each other speak for all but the ends
-    const auto meets = [&](int64_t i) {
-        const int64_t x = at + i * a.step;                                       // the first row of b that ends behind x
-        const int64_t j = x < b.width ? 0 : (x - b.width) / b.step + 1;
-        return j < b.rows && j * b.step < x + a.width;
-    };
-    const int64_t first = at >= 0 ? 0 : std::min(a.rows - 1, -at / a.step);
-    for (int64_t i = first; i < (a.step == b.step ? std::min(a.rows, first + 2) : a.rows); ++i)
-        if (meets(i)) return true;
-    return a.step == b.step && meets(a.rows - 1);
-}
-Stretch stretch(const void* p, int64_t rows, int64_t cols, int64_t ld, int bytes) { return {p, rows, cols * bytes, (rows == 1 ? cols : ld) * bytes}; }
 bool tiles_ok(int64_t M, int64_t N) { return ((M + 255) / 256) * ((N + 127) / 128) <= MAX_EXTENT; }     // units are counted in 32 bits
 
 // ---- cross entropy ----
@@ -405,7 +365,6 @@ bool launch_unpack(const ActShape& s, const int8_t* q, const uint8_t* scales, vo
     }
     return vec ? run(k_act_unpack<float, false>, act_grid(s.T, s.G, PACK_CTAS, false), (float*)x) : run(k_act_unpack32_any, lane_grid(s.T, s.G), (float*)x);
 }
-bool dtype_ok(int dtype) { return dtype == PSGD_DT_F32 || dtype == PSGD_DT_BF16; }
 bool ckpt_ok(const void* q) { return ((uintptr_t)q & 15) == 0; }
 
 struct WgradPlan { int pairs; int64_t ldx; TilePlan p; size_t x, part, total; };

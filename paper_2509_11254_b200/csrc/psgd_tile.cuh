@@ -29,6 +29,7 @@
 #include <cuda_bf16.h>
 
 #include "psgd_ptx.cuh"
+#include "psgd_values.cuh"
 
 namespace psgd {
 
@@ -47,15 +48,6 @@ constexpr int XE_SEG = 64, XE_SEG_LOSS = 128; // columns per softmax statistic: 
 inline size_t tile_smem_bytes() { return (size_t)TG_STAGES * TG_STAGE_BYTES + TG_EPI_WARPS * TG_STAGING + 1024 + 256; }
 
 enum TileEpilogue { EPI_LOSS = 0, EPI_SOFTMAX = 1, EPI_STORE = 2 };
-
-// Division by a launch constant: q = n * mul >> shift for 0 <= n < 2^31 (mul = floor(2^shift / d) + 1, shift = 31 + ceil(log2 d)).
-struct FastDiv { unsigned mul, shift; };
-inline FastDiv fast_div(unsigned d) {
-    unsigned l = 0;
-    while ((1ull << l) < d) ++l;
-    return {(unsigned)(((unsigned long long)1 << (31 + l)) / d + 1), 31 + l};
-}
-__device__ __forceinline__ int operator/(int n, FastDiv d) { return (int)(((unsigned long long)(unsigned)n * d.mul) >> d.shift); }
 
 // One product and how it is cut.
 struct TileProblem {
@@ -172,16 +164,6 @@ __device__ __forceinline__ void mbar_wait_all(unsigned bar, unsigned parity, int
         dead = __any_sync(0xffffffffu, dead);
     }
 }
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ unsigned pack_bf16(float lo, float hi) {
-    __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<unsigned*>(&h);
-}
-
 __device__ __forceinline__ void tile_origin(const TileProblem& p, int tile, int& m0, int& n0) {
     const int g = tile / p.by_group, in = tile - g * (p.gm * p.nt);
     const bool rest = (g + 1) * p.gm > p.mt;
@@ -302,15 +284,7 @@ __device__ __forceinline__ void emit_block(const TileProblem& a, uint4* xb, floa
     }
 }
 
-// Dependent launches: a kernel may start while the one before it on the stream still runs (its set-up and its CTAs' start then cost nothing); `grid_wait`
-// returns when that one has finished and its writes are visible, so everything that touches global memory comes after it, and nothing
-// is loaded through the read-only path, which expects memory that no one writes while the kernel lives.  `grid_trigger` lets the next start.
-__device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;\n" ::: "memory"); }
-__device__ __forceinline__ void grid_trigger() { asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory"); }
-
-constexpr float LOG2E = 1.4426950408889634f;
 constexpr float XE_STEPS = 1024.f;            // steps per factor of two in the stored exponents
-constexpr float XE_MAGIC = 8388608.f;         // 2^23: adding it leaves the rounded whole number in the low mantissa bits
 constexpr unsigned XE_NONE = 65535u;
 
 // EPI_LOSS, EPI_SOFTMAX: one product of K-major operands.  EPI_STORE: products whose B is MN-major, A either.

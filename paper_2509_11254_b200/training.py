@@ -106,9 +106,9 @@ def _operand(t, rows, cols, ld, stream, *outputs):
     return copy, pad
 
 
-def _no_graph(name, a, b, instead, depth):
-    """Warns, `depth` calls up, where autograd would lose the gradient of `a` or `b` without a word."""
-    if (a.requires_grad or b.requires_grad) and torch.is_grad_enabled():
+def _no_graph(name, inputs, instead, depth):
+    """Warns, `depth` calls up, where autograd would lose the gradient of one of `inputs` without a word."""
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in inputs):
         warnings.warn(f"{name}: the results have no autograd graph, no gradient will reach its inputs; {instead}, or call it under torch.no_grad()", stacklevel=depth)
 
 
@@ -159,7 +159,7 @@ def _xent(grad, hidden, weight, labels, token_weight, ignore_index, d_hidden, d_
     lddw = _matrix(d_weight, "d_weight", shape=(V, D), device=dev)[2] if d_weight is not None else D
     at_status = _status(status, dev)
     if not grad:
-        _no_graph("linear_cross_entropy", hidden, weight, "linear_cross_entropy_grad returns the gradients", 4)
+        _no_graph("linear_cross_entropy", (hidden, weight), "linear_cross_entropy_grad returns the gradients", 4)
     s = _here(dev, stream)
     if s is None:
         with _there(dev, stream, hidden, weight, labels, token_weight, d_hidden, d_weight, status), torch.no_grad():
@@ -304,7 +304,7 @@ def swiglu_forward(gate, up, stream=None):
     T, F, ldg = _matrix(gate, "gate")
     dev = gate.device
     ldu = _matrix(up, "up", shape=(T, F), device=dev)[2]
-    _no_graph("swiglu_forward", gate, up, "swiglu_backward makes the gradients", 3)
+    _no_graph("swiglu_forward", (gate, up), "swiglu_backward makes the gradients", 3)
     s = _here(dev, stream)
     if s is None:
         with _there(dev, stream, gate, up), torch.no_grad():
