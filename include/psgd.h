@@ -363,6 +363,25 @@ psgd_status psgd_xent_grad(const void* H /*DEVICE*/, int64_t ldh, const void* W 
                            int64_t lddw, int* status /*DEVICE*/, void* workspace /*DEVICE*/, size_t workspace_bytes, psgd_stream stream);
 
 /*
+ * Distance of the last layer from a teacher of whom K entries per row are known (1 <= K <= 1024): logits [T][K] float32 or bfloat16 (dtype, row stride ldl)
+ * of the columns index [T][K] (row stride ldi).  An entry with a negative index or the logit -infinity is none; the same column may be listed twice.  With
+ * l = H W^T, p = softmax(l / temperature) over all columns and q = softmax(logits / temperature) over the row's entries:
+ *     token_loss_t = temperature^2 sum_k q_k (log q_k - log p_{t,index_k})   (0 for a row without an entry),   lse_t = log sum_v exp(l_tv / temperature),
+ *     loss = sum_t weight_t token_loss_t / Z,  Z = sum of weight_t over the rows that have an entry (loss 0 where Z = 0),
+ * dH and dW the gradients of loss.  A column outside 0..V-1 makes its row's loss NaN, its gradients 0, and sets PSGD_W_LABEL.  temperature within 10^-3..10^3.  Everything else
+ * as for psgd_xent_*; the workspace has 16 bytes per entry and 4 per 32 rows and 128 columns more.
+ */
+psgd_status psgd_distill_workspace(int64_t T, int64_t V, int64_t D, int64_t K, int grad, size_t* bytes /*HOST*/);
+psgd_status psgd_distill_loss(const void* H /*DEVICE*/, int64_t ldh, const void* W /*DEVICE*/, int64_t ldw, const void* logits /*DEVICE*/, int64_t ldl, int dtype,
+                              const int64_t* index /*DEVICE*/, int64_t ldi, int64_t K, float temperature, const float* weight /*DEVICE*/, int64_t T, int64_t V, int64_t D,
+                              float* loss /*DEVICE*/, float* token_loss /*DEVICE*/, float* lse /*DEVICE*/, int* status /*DEVICE*/, void* workspace /*DEVICE*/,
+                              size_t workspace_bytes, psgd_stream stream);
+psgd_status psgd_distill_grad(const void* H /*DEVICE*/, int64_t ldh, const void* W /*DEVICE*/, int64_t ldw, const void* logits /*DEVICE*/, int64_t ldl, int dtype,
+                              const int64_t* index /*DEVICE*/, int64_t ldi, int64_t K, float temperature, const float* weight /*DEVICE*/, int64_t T, int64_t V, int64_t D,
+                              float* loss /*DEVICE*/, float* token_loss /*DEVICE*/, float* lse /*DEVICE*/, void* dH /*DEVICE*/, int64_t lddh, void* dW /*DEVICE*/,
+                              int64_t lddw, int* status /*DEVICE*/, void* workspace /*DEVICE*/, size_t workspace_bytes, psgd_stream stream);
+
+/*
  * Activation checkpoints in 8 bits.  A checkpoint of x [T][F] is q [T][32 G] int8 (16-byte aligned; G = ceil(F / 32), padded with
  * zeros) and scales [T][G] bytes: per row and group of 32 values a power of two 2^e, e the smallest integer with
  * max|x| <= 127 * 2^e (kept within -126..121; byte e + 127), and q = rint(x / 2^e), ties to even, within -127..127.  A group

@@ -20,9 +20,13 @@ from .training import (  # noqa: F401,E402
     ActivationCheckpoint,
     CrossEntropy,
     CrossEntropyGrad,
+    Distillation,
+    DistillationGrad,
     PSGD_W_LABEL,
     linear_cross_entropy,
     linear_cross_entropy_grad,
+    linear_distillation,
+    linear_distillation_grad,
     pack_activation,
     swiglu_backward,
     swiglu_forward,

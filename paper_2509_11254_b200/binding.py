@@ -63,6 +63,9 @@ SIGNATURES = {
     "psgd_xent_workspace": (_int, [_i64, _i64, _i64, _int, C.POINTER(_sz)]),
     "psgd_xent_loss": (_int, [_vp, _i64, _vp, _i64, _vp, _vp, _i64, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
     "psgd_xent_grad": (_int, [_vp, _i64, _vp, _i64, _vp, _vp, _i64, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _i64, _vp, _i64, _vp, _vp, _sz, _vp]),
+    "psgd_distill_workspace": (_int, [_i64, _i64, _i64, _i64, _int, C.POINTER(_sz)]),
+    "psgd_distill_loss": (_int, [_vp, _i64, _vp, _i64, _vp, _i64, _int, _vp, _i64, _i64, C.c_float, _vp, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "psgd_distill_grad": (_int, [_vp, _i64, _vp, _i64, _vp, _i64, _int, _vp, _i64, _i64, C.c_float, _vp, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _i64, _vp, _i64, _vp, _vp, _sz, _vp]),
     "psgd_act_pack": (_int, [_vp, _i64, _int, _i64, _i64, _vp, _vp, _vp]),
     "psgd_act_unpack": (_int, [_vp, _vp, _i64, _i64, _vp, _i64, _int, _vp]),
     "psgd_act_wgrad_workspace": (_int, [_i64, _i64, _i64, C.POINTER(_sz)]),

@@ -1,4 +1,4 @@
-// Host side of the training operators declared in include/psgd.h: softmax cross entropy of the last layer with its
+// Host side of the training operators declared in include/psgd.h: softmax cross entropy of the last layer and its distance from a teacher, with their
 // gradients, 8-bit activation checkpoints, the weight gradient from them, and the gated unit.  Argument checks, workspace
 // layout and the stream-ordered sequence of kernels; nothing here allocates, synchronises or keeps anything between calls.
 #include "../../include/psgd.h"
@@ -9,6 +9,7 @@
 
 #include "psgd_act.cuh"
 #include "psgd_host.cuh"
+#include "psgd_teach.cuh"
 #include "psgd_tile.cuh"
 #include "psgd_train.cuh"
 #include "psgd_xent.cuh"
@@ -188,6 +189,8 @@ struct XentPlan {
     int64_t ldq, piece, pieces;
     TilePlan logits, two[2];          // of a whole piece; two: dH and dW
     size_t inv, done, sums, stats, label_logit, q, part, acc, total;
+    int nbins;                        // with a teacher: segments of 128 columns
+    size_t z, col, rest, label, bins, entries;
 };
 // Tokens are taken in pieces, all columns at a time, so that the stored exponents (loss alone: the statistics) stay within a fixed size however
 // many tokens there are; a piece has at least 1024 tokens, below which the products with the vocabulary matrix would be bound by reading it.
@@ -195,7 +198,8 @@ void plan_gradients(TilePlan (&p)[2], int64_t rows, int64_t V, int64_t D, int pa
     const int64_t M[2] = {rows, V}, K[2] = {V, rows};
     plan_two(p, M, D, K, pairs);
 }
-XentPlan plan_xent(int64_t T, int64_t V, int64_t D, bool grad) {
+// `K`: entries of a row of the teacher's list, 0: labels
+XentPlan plan_xent(int64_t T, int64_t V, int64_t D, bool grad, int64_t K) {
     XentPlan x{};
     x.pairs = std::max(1, device_sms() / 2);
     x.nseg = ceil_div(V, grad ? XE_SEG : XE_SEG_LOSS);
@@ -214,7 +218,17 @@ XentPlan plan_xent(int64_t T, int64_t V, int64_t D, bool grad) {
     }
     x.sums = take((size_t)(grad ? T : ceil_div(T, XE_THREADS / 32)) * sizeof(double2));
     x.stats = take((size_t)x.piece * x.nseg * 8);
-    x.label_logit = take((size_t)x.piece * 4);
+    x.label_logit = take((size_t)x.piece * std::max<int64_t>(1, K) * 4);
+    if (K > 0) {
+        const int64_t blocks = (T + TEACH_ROWS - 1) / TEACH_ROWS;
+        x.nbins = ceil_div(V, TEACH_COLS);
+        x.z = take((size_t)T * K * 4);
+        x.col = take((size_t)T * K * 4);
+        x.rest = take((size_t)T * 4);
+        x.label = take((size_t)T * 8);
+        x.bins = take((size_t)blocks * (x.nbins + 1) * 4);
+        x.entries = take((size_t)blocks * TEACH_ROWS * K * 4);
+    }
     if (grad) {
         x.q = take((size_t)x.piece * x.ldq * 2);
         size_t part = part_bytes(x.two[0]) + part_bytes(x.two[1]);
@@ -230,10 +244,13 @@ XentPlan plan_xent(int64_t T, int64_t V, int64_t D, bool grad) {
     return x;
 }
 
-psgd_status xent(const void* H, int64_t ldh, const void* W, int64_t ldw, const int64_t* labels, const float* weight, int64_t ignore, int64_t T, int64_t V, int64_t D,
+struct Teacher { const void* logits; int64_t ldl; int dtype; const int64_t* index; int64_t ldi, K; float tau; };
+
+// `teacher`: nullptr where there are labels
+psgd_status xent(const void* H, int64_t ldh, const void* W, int64_t ldw, const int64_t* labels, const Teacher* teacher, const float* weight, int64_t ignore, int64_t T, int64_t V, int64_t D,
                  float* loss, float* token_loss, float* lse, bool grad, void* dH, int64_t lddh, void* dW, int64_t lddw, int* status, void* ws, size_t ws_bytes, cudaStream_t st) {
     if (T < 0 || T > MAX_EXTENT || !extent_ok(V) || !extent_ok(D) || !tiles_ok(T, V) || !tiles_ok(V, D)) return PSGD_E_INVALID;
-    if (!W || !loss || !ws || (T > 0 && (!H || !labels || !token_loss || !lse)) || (grad && (!dW || (T > 0 && !dH)))) return PSGD_E_NULL;
+    if (!W || !loss || !ws || (T > 0 && (!H || !(teacher ? teacher->logits && teacher->index : labels != nullptr) || !token_loss || !lse)) || (grad && (!dW || (T > 0 && !dH)))) return PSGD_E_NULL;
     if (!operand_ok(W, V, D, ldw) || (T > 0 && !operand_ok(H, T, D, ldh)) || (grad && ((T > 0 && lddh < D) || lddw < D))) return PSGD_E_INVALID;
     if ((uintptr_t)ws & 255) return PSGD_E_INVALID;
     if (grad) {                                       // both products run at once: one reads H and W while the other writes
@@ -245,13 +262,29 @@ psgd_status xent(const void* H, int64_t ldh, const void* W, int64_t ldw, const i
         if (grad && !succeeded("cudaMemset2DAsync", cudaMemset2DAsync(dW, (size_t)lddw * 2, 0, (size_t)D * 2, (size_t)V, st))) return PSGD_E_CUDA;
         return PSGD_OK;
     }
-    const XentPlan x = plan_xent(T, V, D, grad);
+    const XentPlan x = plan_xent(T, V, D, grad, teacher ? teacher->K : 0);
     if (ws_bytes < x.total) return PSGD_E_WORKSPACE;
     char* w = (char*)ws;
     int* stat = status ? status : (int*)w;
     float* inv = (float*)(w + x.inv);
     int* done = (int*)(w + x.done);
 
+    TeachArgs teach{};
+    TeachRows listed{};
+    if (teacher) {
+        const float inv_tau = (float)(1.0 / (double)teacher->tau);
+        teach.T = T; teach.V = (int)V; teach.K = (int)teacher->K;
+        teach.logits = teacher->logits; teach.bf16 = teacher->dtype == PSGD_DT_BF16; teach.ldl = teacher->ldl;
+        teach.index = (const long long*)teacher->index; teach.ldi = teacher->ldi;
+        teach.inv_tau = inv_tau; teach.nbins = x.nbins;
+        teach.z = (float*)(w + x.z); teach.col = (int*)(w + x.col); teach.rest = (float*)(w + x.rest); teach.label = (long long*)(w + x.label);
+        teach.bins = (int*)(w + x.bins); teach.entries = (unsigned*)(w + x.entries);
+        listed.K = teach.K; listed.tau = teacher->tau; listed.inv_tau = inv_tau;
+        listed.logit = (const float*)(w + x.label_logit);
+        labels = (const int64_t*)teach.label;                 // 0 where a row counts
+        ignore = -1;
+        if (!launch(k_teach, dim3(ceil_div(T, TEACH_ROWS)), dim3(256), 0, st, teach)) return PSGD_E_CUDA;
+    }
     RowsArgs r{};
     r.V = (int)V; r.nseg = x.nseg;
     r.stats = (const float2*)(w + x.stats);
@@ -283,10 +316,21 @@ psgd_status xent(const void* H, int64_t ldh, const void* W, int64_t ldw, const i
             a.done = done;
             a.norm = inv; a.norm_labels = (const long long*)labels; a.norm_weight = weight; a.norm_rows = T; a.ignore = ignore;
         }
+        if (teacher) {
+            const int64_t block = t0 / TEACH_ROWS;            // (pieces are whole row tiles)
+            a.bins = teach.bins + block * (x.nbins + 1);
+            a.entries = teach.entries + block * TEACH_ROWS * teach.K;
+            a.entry_logit = a.label_logit;
+            a.nbins = x.nbins; a.K = teach.K;
+            a.temperature = teacher->tau; a.log2e = LOG2E * teach.inv_tau;
+            listed.z = teach.z + t0 * teach.K; listed.col = teach.col + t0 * teach.K; listed.rest = teach.rest + t0;
+        }
         const bool whole = rows == x.piece;
         const TilePlan pl = whole ? x.logits : plan_tiles(rows, V, D, x.pairs, false);
         const Operand oh{h, ldh, false}, ow{W, ldw, false};
-        psgd_status s = grad ? launch_softmax<EPI_SOFTMAX>(oh, ow, pl, a, x.pairs, st) : launch_softmax<EPI_LOSS>(oh, ow, pl, a, x.pairs, st);
+        psgd_status s;
+        if (teacher) s = grad ? launch_softmax<EPI_TEACH>(oh, ow, pl, a, x.pairs, st) : launch_softmax<EPI_TEACH_LOSS>(oh, ow, pl, a, x.pairs, st);
+        else s = grad ? launch_softmax<EPI_SOFTMAX>(oh, ow, pl, a, x.pairs, st) : launch_softmax<EPI_LOSS>(oh, ow, pl, a, x.pairs, st);
         if (s != PSGD_OK) return s;
         r.rows = (int)rows;
         r.first_sum = (int)(grad ? t0 : t0 / (XE_THREADS / 32));      // (pieces are whole row tiles)
@@ -295,10 +339,12 @@ psgd_status xent(const void* H, int64_t ldh, const void* W, int64_t ldw, const i
         r.loss = token_loss + t0;
         r.lse = lse + t0;
         if (!grad) {
-            if (!launch(k_xent_loss, dim3(ceil_div(rows, XE_THREADS / 32)), dim3(XE_THREADS), 0, st, r)) return PSGD_E_CUDA;
+            const dim3 grid(ceil_div(rows, XE_THREADS / 32));
+            if (!(teacher ? launch(k_teach_loss, grid, dim3(XE_THREADS), 0, st, r, listed) : launch(k_xent_loss, grid, dim3(XE_THREADS), 0, st, r))) return PSGD_E_CUDA;
             continue;
         }
-        if (!launch(k_xent_rows, dim3((unsigned)rows, parts_of(rows)), dim3(XE_THREADS), 0, st, r)) return PSGD_E_CUDA;
+        const dim3 grid((unsigned)rows, parts_of(rows));
+        if (!(teacher ? launch(k_teach_rows, grid, dim3(XE_THREADS), 0, st, r, listed) : launch(k_xent_rows, grid, dim3(XE_THREADS), 0, st, r))) return PSGD_E_CUDA;
         // dH = dL W: contraction over the vocabulary;  dW = dL^T H: over the tokens
         TilePlan p[2] = {x.two[0], x.two[1]};
         if (!whole) plan_gradients(p, rows, V, D, x.pairs);
@@ -325,6 +371,11 @@ psgd_status xent(const void* H, int64_t ldh, const void* W, int64_t ldw, const i
         if (s != PSGD_OK) return s;
     }
     return PSGD_OK;
+}
+
+// (a temperature whose reciprocal is not a normal number would leave nothing of the logits)
+bool teacher_ok(const Teacher& t) {
+    return t.K >= 1 && t.K <= TEACH_MOST && dtype_ok(t.dtype) && t.ldl >= t.K && t.ldi >= t.K && t.tau >= 1e-3f && t.tau <= 1e3f;
 }
 
 // ---- 8-bit activations ----
@@ -402,13 +453,13 @@ int psgd_overlap(const void* a, int64_t rows_a, int64_t width_a, int64_t step_a,
 psgd_status psgd_xent_workspace(int64_t T, int64_t V, int64_t D, int grad, size_t* bytes) {
     if (!bytes) return PSGD_E_NULL;
     if (T < 0 || T > MAX_EXTENT || !extent_ok(V) || !extent_ok(D) || !tiles_ok(T, V) || !tiles_ok(V, D)) return PSGD_E_INVALID;
-    *bytes = T == 0 ? 256 : plan_xent(T, V, D, grad != 0).total;
+    *bytes = T == 0 ? 256 : plan_xent(T, V, D, grad != 0, 0).total;
     return PSGD_OK;
 }
 
 psgd_status psgd_xent_loss(const void* H, int64_t ldh, const void* W, int64_t ldw, const int64_t* labels, const float* weight, int64_t ignore, int64_t T, int64_t V,
                            int64_t D, float* loss, float* token_loss, float* lse, int* status, void* ws, size_t ws_bytes, psgd_stream stream) try {
-    return xent(H, ldh, W, ldw, labels, weight, ignore, T, V, D, loss, token_loss, lse, false, nullptr, 0, nullptr, 0, status, ws, ws_bytes, (cudaStream_t)stream);
+    return xent(H, ldh, W, ldw, labels, nullptr, weight, ignore, T, V, D, loss, token_loss, lse, false, nullptr, 0, nullptr, 0, status, ws, ws_bytes, (cudaStream_t)stream);
 } catch (...) {
     return cuda_error("host", "exception");
 }
@@ -416,7 +467,34 @@ psgd_status psgd_xent_loss(const void* H, int64_t ldh, const void* W, int64_t ld
 psgd_status psgd_xent_grad(const void* H, int64_t ldh, const void* W, int64_t ldw, const int64_t* labels, const float* weight, int64_t ignore, int64_t T, int64_t V,
                            int64_t D, float* loss, float* token_loss, float* lse, void* dH, int64_t lddh, void* dW, int64_t lddw, int* status, void* ws, size_t ws_bytes,
                            psgd_stream stream) try {
-    return xent(H, ldh, W, ldw, labels, weight, ignore, T, V, D, loss, token_loss, lse, true, dH, lddh, dW, lddw, status, ws, ws_bytes, (cudaStream_t)stream);
+    return xent(H, ldh, W, ldw, labels, nullptr, weight, ignore, T, V, D, loss, token_loss, lse, true, dH, lddh, dW, lddw, status, ws, ws_bytes, (cudaStream_t)stream);
+} catch (...) {
+    return cuda_error("host", "exception");
+}
+
+psgd_status psgd_distill_workspace(int64_t T, int64_t V, int64_t D, int64_t K, int grad, size_t* bytes) {
+    if (!bytes) return PSGD_E_NULL;
+    if (T < 0 || T > MAX_EXTENT || !extent_ok(V) || !extent_ok(D) || !tiles_ok(T, V) || !tiles_ok(V, D) || K < 1 || K > TEACH_MOST) return PSGD_E_INVALID;
+    *bytes = T == 0 ? 256 : plan_xent(T, V, D, grad != 0, K).total;
+    return PSGD_OK;
+}
+
+psgd_status psgd_distill_loss(const void* H, int64_t ldh, const void* W, int64_t ldw, const void* logits, int64_t ldl, int dtype, const int64_t* index, int64_t ldi, int64_t K,
+                              float temperature, const float* weight, int64_t T, int64_t V, int64_t D, float* loss, float* token_loss, float* lse, int* status, void* ws,
+                              size_t ws_bytes, psgd_stream stream) try {
+    const Teacher t{logits, ldl, dtype, index, ldi, K, temperature};
+    if (!teacher_ok(t)) return PSGD_E_INVALID;
+    return xent(H, ldh, W, ldw, nullptr, &t, weight, -1, T, V, D, loss, token_loss, lse, false, nullptr, 0, nullptr, 0, status, ws, ws_bytes, (cudaStream_t)stream);
+} catch (...) {
+    return cuda_error("host", "exception");
+}
+
+psgd_status psgd_distill_grad(const void* H, int64_t ldh, const void* W, int64_t ldw, const void* logits, int64_t ldl, int dtype, const int64_t* index, int64_t ldi, int64_t K,
+                              float temperature, const float* weight, int64_t T, int64_t V, int64_t D, float* loss, float* token_loss, float* lse, void* dH, int64_t lddh,
+                              void* dW, int64_t lddw, int* status, void* ws, size_t ws_bytes, psgd_stream stream) try {
+    const Teacher t{logits, ldl, dtype, index, ldi, K, temperature};
+    if (!teacher_ok(t)) return PSGD_E_INVALID;
+    return xent(H, ldh, W, ldw, nullptr, &t, weight, -1, T, V, D, loss, token_loss, lse, true, dH, lddh, dW, lddw, status, ws, ws_bytes, (cudaStream_t)stream);
 } catch (...) {
     return cuda_error("host", "exception");
 }

@@ -47,7 +47,9 @@ constexpr int XE_SEG = 64, XE_SEG_LOSS = 128; // columns per softmax statistic: 
 
 inline size_t tile_smem_bytes() { return (size_t)TG_STAGES * TG_STAGE_BYTES + TG_EPI_WARPS * TG_STAGING + 1024 + 256; }
 
-enum TileEpilogue { EPI_LOSS = 0, EPI_SOFTMAX = 1, EPI_STORE = 2 };
+// EPI_LOSS, EPI_SOFTMAX: statistics of the logits without and with their stored exponents, the labels' logits on the way.  EPI_TEACH_LOSS, EPI_TEACH: the same of logits
+// divided by a temperature, the logits of a list of columns per row on the way.  EPI_STORE: the product itself.
+enum TileEpilogue { EPI_LOSS = 0, EPI_SOFTMAX = 1, EPI_STORE = 2, EPI_TEACH_LOSS = 3, EPI_TEACH = 4 };
 
 // One product and how it is cut.
 struct TileProblem {
@@ -77,7 +79,7 @@ struct TileArgs {
     // pairs do `extra` units of p[1] each, and the rest of those go round all pairs.
     int first_q, first_r, extra;
     int* status;               // device status word
-    // EPI_LOSS, EPI_SOFTMAX
+    // all but EPI_STORE
     int a_rows, a_odd;         // rows of A in a box, a multiple of 8, and whether the odd CTA has any: 128 and 1, less where all of M is one short
                                // tile.  The rows that no box brings are zeros for good (not garbage: that would cost the MMAs' power).
     const long long* labels;
@@ -87,7 +89,14 @@ struct TileArgs {
     long long ldq;
     int nseg;                  // statistics per row
     int* done;                 // counter to clear for the next kernel, or nullptr
-    // EPI_SOFTMAX: 1 / (sum of the weights of the rows that count), formed by a warp that has nothing else to do
+    // EPI_TEACH_LOSS, EPI_TEACH: the listed entries by block of 32 rows and segment of 128 columns (k_teach)
+    const int* bins;           // [blocks][nbins + 1]: where a segment's entries begin among its block's
+    const unsigned* entries;   // [blocks][32 K]: place in the row's list << 12 | row of the block << 7 | column of the segment
+    float* entry_logit;        // [M][K]
+    int nbins, K;
+    float log2e;               // log2(e) / temperature
+    float temperature;
+    // EPI_SOFTMAX, EPI_TEACH: 1 (temperature) / (sum of the weights of the rows that count), formed by a warp that has nothing else to do
     float* norm;               // or nullptr
     const long long* norm_labels;
     const float* norm_weight;
@@ -287,12 +296,12 @@ __device__ __forceinline__ void emit_block(const TileProblem& a, uint4* xb, floa
 constexpr float XE_STEPS = 1024.f;            // steps per factor of two in the stored exponents
 constexpr unsigned XE_NONE = 65535u;
 
-// EPI_LOSS, EPI_SOFTMAX: one product of K-major operands.  EPI_STORE: products whose B is MN-major, A either.
+// EPI_STORE: one or two products whose B is MN-major, A either.  The others: one product of K-major operands.
 template <int EPI>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TG_THREADS, 1)
 k_tile(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtensorMap tmB0, const __grid_constant__ CUtensorMap tmA1, const __grid_constant__ CUtensorMap tmB1,
        const __grid_constant__ TileArgs a) {
-    constexpr bool BMN = EPI == EPI_STORE;
+    constexpr bool BMN = EPI == EPI_STORE, TEACH = EPI == EPI_TEACH_LOSS || EPI == EPI_TEACH, LOSS_ONLY = EPI == EPI_LOSS || EPI == EPI_TEACH_LOSS;
     extern __shared__ __align__(16) unsigned char tg_smem_raw[];
     // the offset of everything in shared memory is the same in both CTAs of the pair (descriptors and commits rely on it)
     unsigned char* base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(tg_smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -418,7 +427,7 @@ k_tile(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtenso
                     k0 = k1;
                 }
             }
-        } else if (EPI == EPI_SOFTMAX && blockIdx.x == 1 && a.norm) {
+        } else if (!BMN && !LOSS_ONLY && blockIdx.x == 1 && a.norm) {
             double z = 0.0;
             constexpr int UN = 8;
             for (long long i0 = lane; i0 < a.norm_rows; i0 += 32 * UN) {
@@ -438,7 +447,7 @@ k_tile(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtenso
             }
 #pragma unroll
             for (int o = 16; o; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
-            if (lane == 0) *a.norm = z != 0.0 ? (float)(1.0 / z) : 0.f;
+            if (lane == 0) *a.norm = z != 0.0 ? (float)((TEACH ? (double)a.temperature : 1.0) / z) : 0.f;
         }
     } else {
         // ---- epilogue: two warps per quarter of the rows, which share the columns ----
@@ -498,21 +507,35 @@ k_tile(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtenso
                 const int row = w.m0 + rank * 128 + quarter * 32 + lane;
                 return row < p.M ? a.labels[row] : -1ll;
             };
+            // the entries of this warp's block of rows and columns: where they begin and end is asked for a tile ahead, the first 32 with the tile
+            auto bin_of = [&](const TileUnit& w) {
+                const int row = w.m0 + rank * 128 + quarter * 32, col = w.n0 + share * 128;
+                if (row >= p.M || col >= p.N) return make_int2(0, 0);
+                const int* at = a.bins + (size_t)(row >> 5) * (a.nbins + 1) + (col >> 7);
+                return make_int2(at[0], at[1]);
+            };
+            const float log2e = TEACH ? a.log2e : LOG2E;
             TileUnit next;
             bool going = tile_unit(a, 0, next);
-            long long next_label = going ? label_of(next) : -1ll;
+            long long next_label = !TEACH && going ? label_of(next) : -1ll;
+            int2 next_bin = TEACH && going ? bin_of(next) : make_int2(0, 0);
             for (; going; ++it) {
                 const TileUnit w = next;
                 const int row0 = w.m0 + rank * 128 + quarter * 32, col_base = w.n0 + share * 128, row = row0 + lane;
                 const int b = it & 1;
                 const int label_col = (int)min(max(next_label - (long long)col_base, -1ll), 128ll);   // among this warp's columns
+                const int2 bin = next_bin;
+                const unsigned* listed = a.entries + (size_t)(row0 >> 5) * 32 * a.K;
+                unsigned entry = ~0u;                          // (no list reaches that far: its place would be 2^20 - 1)
+                if (TEACH && bin.x + lane < bin.y) entry = listed[bin.x + lane];
                 going = tile_unit(a, it + 1, next);
-                if (going) next_label = label_of(next);        // asked for a tile ahead
+                if (!TEACH && going) next_label = label_of(next);        // asked for a tile ahead
+                if (TEACH && going) next_bin = bin_of(next);
                 mbar_wait_warp(bar_accf + 8 * b, (unsigned)((it >> 1) & 1), a.status, dead);
                 asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
                 const unsigned taddr = lane_base + (unsigned)(b * TG_BN + share * 128);
                 const int ncols = row0 < p.M ? min(128, p.N - col_base) : 0;       // (<= 0: none of these columns exists, or none of the rows)
-                float last_top = -INFINITY, last_sum = 0.f;    // EPI_LOSS: of the first 64 columns
+                float last_top = -INFINITY, last_sum = 0.f;    // loss only: of the first 64 columns
 #pragma unroll
                 for (int c = 0; c < 128 / XE_SEG; ++c) {
                     const int left = ncols - XE_SEG * c;
@@ -531,11 +554,35 @@ k_tile(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtenso
 #pragma unroll
                         for (int j = 0; j < XE_SEG; ++j) if (j >= left) v[j >> 5][j & 31] = -INFINITY;
                     }
-                    if (__any_sync(0xffffffffu, (label_col >> 6) == c)) {
+                    if constexpr (TEACH) {
+                        // 32 columns at a time through shared memory, where any entry lies among them: a lane per entry fetches its row's
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            bool here = false;
+                            for (int e0 = bin.x; e0 < bin.y; e0 += 32) {
+                                const unsigned e = e0 == bin.x ? entry : e0 + lane < bin.y ? listed[e0 + lane] : ~0u;
+                                const bool mine = e != ~0u && (int)(e >> 5 & 3u) == 2 * c + h;
+                                if (!__any_sync(0xffffffffu, mine)) continue;
+                                if (!here) {
+#pragma unroll
+                                    for (int j = 0; j < 8; ++j)
+                                        xb[lane * 8 + (j ^ (lane & 7))] = make_uint4(__float_as_uint(v[h][4 * j]), __float_as_uint(v[h][4 * j + 1]), __float_as_uint(v[h][4 * j + 2]),
+                                                                                     __float_as_uint(v[h][4 * j + 3]));
+                                    __syncwarp();
+                                    here = true;
+                                }
+                                if (mine) {
+                                    const int r = e >> 7 & 31u, col = e & 31u;
+                                    a.entry_logit[(size_t)(row0 + r) * a.K + (e >> 12)] = reinterpret_cast<const float*>(xb)[(r * 8 + ((col >> 2) ^ (r & 7))) * 4 + (col & 3)];
+                                }
+                            }
+                            if (here) __syncwarp();
+                        }
+                    } else if (__any_sync(0xffffffffu, (label_col >> 6) == c)) {
 #pragma unroll
                         for (int j = 0; j < XE_SEG; ++j) if (label_col == XE_SEG * c + j) a.label_logit[row] = v[j >> 5][j & 31];
                     }
-                    float t[4] = {EPI == EPI_LOSS ? last_top : -INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                    float t[4] = {LOSS_ONLY ? last_top : -INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
                     for (int j = 0; j < XE_SEG; ++j) t[j & 3] = fmaxf(t[j & 3], v[j >> 5][j & 31]);
                     const float top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
@@ -548,10 +595,10 @@ k_tile(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtenso
                         float e[8];
 #pragma unroll
                         for (int i = 0; i < 8; i += 2) {
-                            const float t0 = (v[j >> 5][(j & 31) + i] - ref) * LOG2E, t1 = (v[j >> 5][(j & 31) + i + 1] - ref) * LOG2E;     // <= 0
+                            const float t0 = (v[j >> 5][(j & 31) + i] - ref) * log2e, t1 = (v[j >> 5][(j & 31) + i + 1] - ref) * log2e;     // <= 0
                             e[i] = ex2(t0);
                             e[i + 1] = ex2(t1);
-                            if (EPI == EPI_SOFTMAX) {
+                            if (!LOSS_ONLY) {
                                 const float q0 = fminf(fmaf(t0, -XE_STEPS, XE_MAGIC), XE_MAGIC + 65535.f);
                                 const float q1 = fminf(fmaf(t1, -XE_STEPS, XE_MAGIC), XE_MAGIC + 65535.f);
                                 pk[(j + i) / 2] = __byte_perm(__float_as_uint(q0), __float_as_uint(q1), 0x5410);
@@ -561,9 +608,9 @@ k_tile(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtenso
                         part[j / 8 & 3] = j < 32 ? eight : part[j / 8 & 3] + eight;
                     }
                     float sum = (part[0] + part[1]) + (part[2] + part[3]);
-                    if (EPI == EPI_LOSS) sum = fmaf(last_sum, ex2((last_top - ref) * LOG2E), sum);
+                    if (LOSS_ONLY) sum = fmaf(last_sum, ex2((last_top - ref) * log2e), sum);
                     if (dead) sum = NAN;
-                    if (EPI == EPI_LOSS) {
+                    if (LOSS_ONLY) {
                         last_top = top;
                         last_sum = sum;
                     } else {
@@ -580,7 +627,7 @@ k_tile(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtenso
                         __syncwarp();
                     }
                 }
-                if (EPI == EPI_LOSS && ncols > 0 && row < p.M) a.stats[(size_t)row * a.nseg + col_base / XE_SEG_LOSS] = make_float2(last_top, last_sum);
+                if (LOSS_ONLY && ncols > 0 && row < p.M) a.stats[(size_t)row * a.nseg + col_base / XE_SEG_LOSS] = make_float2(last_top, last_sum);
                 if (ncols <= 0 && lane == 0) mbar_arrive_cluster(acce0 + 8 * b);
             }
         }

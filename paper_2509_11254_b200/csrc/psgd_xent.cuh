@@ -92,17 +92,17 @@ __device__ __forceinline__ void report_rows(const RowsArgs& a) {
 
 // Statistics of a row: its maximum `top` and `rest`, the sum of exp(l - top) less the 1 of the maximum itself (-1 where there is nothing). Where
 // one logit stands far above the others, rest is 1 - p of it and keeps all its bits, which a sum next to 1 would lose.
-__device__ __forceinline__ void merge_stat(float& top, float& rest, float t, float r) {
+__device__ __forceinline__ void merge_stat(float& top, float& rest, float t, float r, float log2e = LOG2E) {
     const bool first = top >= t;
     const float high = first ? top : t, low = first ? t : top, from = high == -INFINITY ? 0.f : high;
-    rest = fmaf(1.f + (first ? r : rest), ex2((low - from) * LOG2E), first ? rest : r);
+    rest = fmaf(1.f + (first ? r : rest), ex2((low - from) * log2e), first ? rest : r);
     top = high;
 }
-__device__ __forceinline__ void warp_stat(float& top, float& rest) {
+__device__ __forceinline__ void warp_stat(float& top, float& rest, float log2e = LOG2E) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
         const float t = __shfl_xor_sync(0xffffffffu, top, o), r = __shfl_xor_sync(0xffffffffu, rest, o);
-        merge_stat(top, rest, t, r);
+        merge_stat(top, rest, t, r, log2e);
     }
 }
 // the row's outputs (the loss not from lse, whose rounding is one of the size of the logits); returns its share of the loss and of the weight
@@ -146,6 +146,40 @@ __global__ void __launch_bounds__(XE_THREADS) k_xent_loss(const __grid_constant_
     report_rows(a);
 }
 
+// A row's stored exponents, units u0.. of eight, to w p in bfloat16 (zeros where the row does not count); `exponent`: of the largest p of a segment, from its maximum.
+template <typename Exponent>
+__device__ __forceinline__ void rewrite_exponents(uint4* q, const float2* st, int u0, int u1, float w, bool counts, float poison, Exponent&& exponent) {
+    const int tid = threadIdx.x;
+    constexpr int UN = 4;
+    for (int b = u0 + tid; b < u1; b += XE_THREADS * UN) {
+        uint4 v[UN];
+        float ref[UN];
+#pragma unroll
+        for (int i = 0; i < UN; ++i) {
+            const int u = b + i * XE_THREADS;
+            if (u < u1) { v[i] = q[u]; ref[i] = st[u / (XE_SEG / 8)].x; }
+        }
+#pragma unroll
+        for (int i = 0; i < UN; ++i) {
+            const int u = b + i * XE_THREADS;
+            if (u >= u1) break;
+            const float off = exponent(ref[i]);
+            const unsigned x[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+            float d[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const unsigned bits = (j & 1) ? x[j / 2] >> 16 : x[j / 2] & 0xffffu;
+                const float steps = __uint_as_float(0x4B000000u | bits) - XE_MAGIC;
+                const float p = ex2(fmaf(steps, -1.f / XE_STEPS, off));
+                d[j] = (bits == XE_NONE ? poison : p) * w;
+            }
+            uint4 o = make_uint4(pack_bf16(d[0], d[1]), pack_bf16(d[2], d[3]), pack_bf16(d[4], d[5]), pack_bf16(d[6], d[7]));
+            if (!counts) o = make_uint4(0u, 0u, 0u, 0u);
+            q[u] = o;
+        }
+    }
+}
+
 // Loss and gradient of the logits: blockIdx.x = row, blockIdx.y = part of its columns.
 __global__ void __launch_bounds__(XE_THREADS, XE_ROW_CTAS) k_xent_rows(const __grid_constant__ RowsArgs a) {
     grid_trigger();
@@ -173,34 +207,7 @@ __global__ void __launch_bounds__(XE_THREADS, XE_ROW_CTAS) k_xent_rows(const __g
     uint4* q = reinterpret_cast<uint4*>(a.q + (size_t)row * a.ldq);
     const int units = (a.V + 7) / 8, per = (units + gridDim.y - 1) / gridDim.y;
     const int u0 = blockIdx.y * per, u1 = min(units, u0 + per);
-    constexpr int UN = 4;
-    for (int b = u0 + tid; b < u1; b += XE_THREADS * UN) {
-        uint4 v[UN];
-        float ref[UN];
-#pragma unroll
-        for (int i = 0; i < UN; ++i) {
-            const int u = b + i * XE_THREADS;
-            if (u < u1) { v[i] = q[u]; ref[i] = st[u / (XE_SEG / 8)].x; }
-        }
-#pragma unroll
-        for (int i = 0; i < UN; ++i) {
-            const int u = b + i * XE_THREADS;
-            if (u >= u1) break;
-            const float off = ((ref[i] - top) - log_sum) * LOG2E + poison;     // exponent of the segment's largest p
-            const unsigned x[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
-            float d[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const unsigned bits = (j & 1) ? x[j / 2] >> 16 : x[j / 2] & 0xffffu;
-                const float steps = __uint_as_float(0x4B000000u | bits) - XE_MAGIC;
-                const float p = ex2(fmaf(steps, -1.f / XE_STEPS, off));
-                d[j] = (bits == XE_NONE ? poison : p) * w;
-            }
-            uint4 o = make_uint4(pack_bf16(d[0], d[1]), pack_bf16(d[2], d[3]), pack_bf16(d[4], d[5]), pack_bf16(d[6], d[7]));
-            if (!counts) o = make_uint4(0u, 0u, 0u, 0u);
-            q[u] = o;
-        }
-    }
+    rewrite_exponents(q, st, u0, u1, w, counts, poison, [&](float ref) { return ((ref - top) - log_sum) * LOG2E + poison; });
     // the label's column again, by the thread that has just written it: p - 1 = (exp(l_y - top) - 1 - rest) / (1 + rest), without cancellation where
     // the label is the maximum
     const int lunit = counts ? (int)(label >> 3) : -1;

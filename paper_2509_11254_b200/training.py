@@ -1,18 +1,19 @@
 """Training operators around the compressor: where the weight gradients that it takes come from.
 
   linear_cross_entropy, linear_cross_entropy_grad    softmax cross entropy of the last layer without its logits, and its gradients
+  linear_distillation, linear_distillation_grad      the last layer's distance from a teacher's top logits, likewise
   pack_activation, ActivationCheckpoint.unpack       activations kept in 8 bits between the forward and the backward pass
   weight_gradient                                    a linear layer's weight gradient from the 8-bit checkpoint of its input
   swiglu_forward, swiglu_backward                    the gated unit of a feed-forward block, its inputs kept in 8 bits
 
 Weight gradients can be written straight into a slot of a compressor's gradient stack G [count, N, m, n] (`out=G[c, i]`, float32 or bfloat16;
-`d_weight=G[c, i]` of the last layer, a bfloat16 stack: `grad_dtype="bfloat16"`).  The arithmetic runs in the CUDA library (psgd_xent_*, psgd_act_*, psgd_swiglu_* of include/psgd.h); this module checks
+`d_weight=G[c, i]` of the last layer, a bfloat16 stack: `grad_dtype="bfloat16"`).  The arithmetic runs in the CUDA library (psgd_xent_*, psgd_distill_*, psgd_act_*, psgd_swiglu_* of include/psgd.h); this module checks
 arguments and hands over pointers.  Every call is stream-ordered on `stream` (default: the current stream) and does not
 synchronise.  `status`, an int32 tensor with one element, collects the library's warning bits (PSGD_W_TIMEOUT, PSGD_W_LABEL); what a wait
 that ran out should have produced is NaN, with or without `status`.
 
 None of these calls takes part in autograd: gradients are results of their own (d_hidden, d_weight, swiglu_backward, weight_gradient), and what a call returns has no
-graph behind it.  linear_cross_entropy and swiglu_forward, whose results could be taken for differentiable ones, warn where an input requires a gradient.
+graph behind it.  linear_cross_entropy, linear_distillation and swiglu_forward, whose results could be taken for differentiable ones, warn where an input requires a gradient.
 """
 from __future__ import annotations
 
@@ -29,11 +30,14 @@ from .binding import PSGDError, lib
 
 PSGD_W_LABEL = 8
 GROUP = 32
+_MOST_ENTRIES = 1024           # of a token's teacher
 _BF16 = torch.bfloat16
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1}
 
 CrossEntropy = namedtuple("CrossEntropy", "loss token_loss lse")
 CrossEntropyGrad = namedtuple("CrossEntropyGrad", "loss token_loss lse d_hidden d_weight")
+Distillation = namedtuple("Distillation", "loss token_loss lse")
+DistillationGrad = namedtuple("DistillationGrad", "loss token_loss lse d_hidden d_weight")
 
 _empty = torch.empty
 
@@ -146,43 +150,60 @@ def _workspace_bytes(call, *args):
     return n.value
 
 
-# ---- cross entropy ------------------------------------------------------------------------------------------------
-def _xent(grad, hidden, weight, labels, token_weight, ignore_index, d_hidden, d_weight, status, stream):
+# ---- cross entropy and distillation -------------------------------------------------------------------------------
+def _last_layer(grad, hidden, weight, target, token_weight, d_hidden, d_weight, status, stream):
+    """target: (labels, ignore_index) or (teacher_logits, teacher_index, temperature)."""
     T, D, ldh = _matrix(hidden, "hidden")
     dev = hidden.device
     V, Dw, ldw = _matrix(weight, "weight", device=dev)
     if Dw != D or V < 1:
         raise PSGDError(f"weight must have shape (vocabulary, {D}), not {tuple(weight.shape)}")
-    at_labels = _vector(labels, "labels", torch.int64, T, dev)
+    teacher = len(target) == 3
+    if teacher:
+        logits, index, temperature = target
+        _, K, ldl = _matrix(logits, "teacher_logits", tuple(_DTYPES), device=dev)
+        if not 1 <= K <= _MOST_ENTRIES or len(logits) != T:
+            raise PSGDError(f"teacher_logits must have shape ({T}, 1 to {_MOST_ENTRIES}), not {tuple(logits.shape)}")
+        ldi = _matrix(index, "teacher_index", (torch.int64,), (T, K), dev)[2]
+        if not 1e-3 <= temperature <= 1e3:
+            raise PSGDError(f"temperature must lie within 0.001..1000, not {temperature}")
+        inputs = (logits, index)
+        at_target = logits.data_ptr(), ldl, _DTYPES[logits.dtype], index.data_ptr(), ldi, K, temperature
+    else:
+        labels, ignore_index = target
+        inputs = (labels,)
+        at_target = (_vector(labels, "labels", torch.int64, T, dev),)
     at_weight = _vector(token_weight, "token_weight", torch.float32, T, dev) if token_weight is not None else None
     lddh = _matrix(d_hidden, "d_hidden", shape=(T, D), device=dev)[2] if d_hidden is not None else D
     lddw = _matrix(d_weight, "d_weight", shape=(V, D), device=dev)[2] if d_weight is not None else D
     at_status = _status(status, dev)
+    name = "linear_distillation" if teacher else "linear_cross_entropy"
     if not grad:
-        _no_graph("linear_cross_entropy", (hidden, weight), "linear_cross_entropy_grad returns the gradients", 4)
+        _no_graph(name, (hidden, weight), f"{name}_grad returns the gradients", 4)
     s = _here(dev, stream)
     if s is None:
-        with _there(dev, stream, hidden, weight, labels, token_weight, d_hidden, d_weight, status), torch.no_grad():
-            return _xent(grad, hidden, weight, labels, token_weight, ignore_index, d_hidden, d_weight, status, None)
-    nbytes = _workspace_bytes("psgd_xent_workspace", T, V, D, int(grad), dev.index)
+        with _there(dev, stream, hidden, weight, *inputs, token_weight, d_hidden, d_weight, status), torch.no_grad():
+            return _last_layer(grad, hidden, weight, target, token_weight, d_hidden, d_weight, status, None)
+    call = "psgd_distill_" if teacher else "psgd_xent_"
+    nbytes = _workspace_bytes(call + "workspace", T, V, D, *((K,) if teacher else ()), int(grad), dev.index)
     hidden, ldh = _operand(hidden, T, D, ldh, s, d_hidden, d_weight)
     weight, ldw = _operand(weight, V, D, ldw, s, d_hidden, d_weight)
     ws = _empty(nbytes, dtype=torch.uint8, device=dev)
     out = _empty(2 * T + 1, dtype=torch.float32, device=dev)
     at = out.data_ptr()                             # token_loss, lse, loss side by side
+    args = hidden.data_ptr(), ldh, weight.data_ptr(), ldw, *at_target, at_weight, *(() if teacher else (ignore_index,)), T, V, D, at + 8 * T, at, at + 4 * T
     if grad:
         if d_hidden is None:
             d_hidden = _empty((T, D), dtype=_BF16, device=dev)
         if d_weight is None:
             d_weight = _empty((V, D), dtype=_BF16, device=dev)
-        _check(lib().psgd_xent_grad(hidden.data_ptr(), ldh, weight.data_ptr(), ldw, at_labels, at_weight, ignore_index, T, V, D, at + 8 * T, at, at + 4 * T,
-                                    d_hidden.data_ptr(), lddh, d_weight.data_ptr(), lddw, at_status, ws.data_ptr(), nbytes, s))
-    else:
-        _check(lib().psgd_xent_loss(hidden.data_ptr(), ldh, weight.data_ptr(), ldw, at_labels, at_weight, ignore_index, T, V, D, at + 8 * T, at, at + 4 * T,
-                                    at_status, ws.data_ptr(), nbytes, s))
+        args += d_hidden.data_ptr(), lddh, d_weight.data_ptr(), lddw
+    _check(getattr(lib(), call + ("grad" if grad else "loss"))(*args, at_status, ws.data_ptr(), nbytes, s))
     token_loss, lse, loss = out.split_with_sizes((T, T, 1))
     loss = loss.view(())
-    return CrossEntropyGrad(loss, token_loss, lse, d_hidden, d_weight) if grad else CrossEntropy(loss, token_loss, lse)
+    if grad:
+        return (DistillationGrad if teacher else CrossEntropyGrad)(loss, token_loss, lse, d_hidden, d_weight)
+    return (Distillation if teacher else CrossEntropy)(loss, token_loss, lse)
 
 
 def linear_cross_entropy(hidden, weight, labels, token_weight=None, ignore_index=-100, status=None, stream=None):
@@ -192,7 +213,7 @@ def linear_cross_entropy(hidden, weight, labels, token_weight=None, ignore_index
     the weighted mean over the rows whose label is not `ignore_index` (0 if there is none), the loss of every row (0 where
     ignored) and every row's log-sum-exp, float32.  A label outside 0..V-1 gives NaN and sets PSGD_W_LABEL.
     """
-    return _xent(False, hidden, weight, labels, token_weight, ignore_index, None, None, status, stream)
+    return _last_layer(False, hidden, weight, (labels, ignore_index), token_weight, None, None, status, stream)
 
 
 def linear_cross_entropy_grad(hidden, weight, labels, token_weight=None, ignore_index=-100, d_hidden=None, d_weight=None, status=None, stream=None):
@@ -201,7 +222,27 @@ def linear_cross_entropy_grad(hidden, weight, labels, token_weight=None, ignore_
     d_hidden, d_weight: where to write them (bfloat16 matrices with unit column stride), for instance a slot of a bfloat16 gradient stack; they may not overlap
     `hidden`, `weight` or each other.
     """
-    return _xent(True, hidden, weight, labels, token_weight, ignore_index, d_hidden, d_weight, status, stream)
+    return _last_layer(True, hidden, weight, (labels, ignore_index), token_weight, d_hidden, d_weight, status, stream)
+
+
+def linear_distillation(hidden, weight, teacher_logits, teacher_index, temperature=1.0, token_weight=None, status=None, stream=None):
+    """How far the last layer's probabilities are from a teacher's of whom a few logits per token are known; logits hidden @ weight.T are never stored.
+
+    hidden [T, D] and weight [V, D] bfloat16; teacher_logits [T, K] bfloat16 or float32, K up to 1024, of the columns teacher_index [T, K] int64; token_weight [T] float32 or
+    None.  With p = softmax(logits / temperature) over the vocabulary and q = softmax(teacher_logits / temperature) over a token's entries, token_loss is
+    temperature^2 sum q (log q - log p).  An entry with a negative index or the logit -inf is none, and a token without an entry does not count (as padding).
+    Returns (loss, token_loss, lse): the weighted mean over the tokens that count (0 if there is none), every token's loss and log-sum-exp of logits / temperature, float32.
+    An index beyond the vocabulary gives NaN and sets PSGD_W_LABEL.
+    """
+    return _last_layer(False, hidden, weight, (teacher_logits, teacher_index, temperature), token_weight, None, None, status, stream)
+
+
+def linear_distillation_grad(hidden, weight, teacher_logits, teacher_index, temperature=1.0, token_weight=None, d_hidden=None, d_weight=None, status=None, stream=None):
+    """The same with the gradients of the loss: returns (loss, token_loss, lse, d_hidden [T, D], d_weight [V, D]), the gradients bfloat16.
+
+    d_hidden, d_weight: where to write them, as for linear_cross_entropy_grad.
+    """
+    return _last_layer(True, hidden, weight, (teacher_logits, teacher_index, temperature), token_weight, d_hidden, d_weight, status, stream)
 
 
 # ---- 8-bit activations --------------------------------------------------------------------------------------------

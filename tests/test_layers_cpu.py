@@ -100,3 +100,30 @@ def test_frequencies():
                 dict(rotated=8, original_length=10, low=4.0, high=4.0)):
         with pytest.raises(p.PSGDError):
             p.rotary_frequencies(device="cpu", **bad)
+
+
+# ---- distillation -------------------------------------------------------------------------------------------------
+def test_distillation_refuses_before_any_launch(L):
+    n = C.c_size_t()
+    for bad in ((-1, 10, 10, 4), (10, 0, 10, 4), (10, 10, 0, 4), (10, 10, 10, 0), (10, 10, 10, 1025), (1 << 31, 10, 10, 4)):
+        assert L.psgd_distill_workspace(*bad, 1, C.byref(n)) == -1
+    assert L.psgd_distill_workspace(8, 8, 8, 4, 1, None) == -2
+
+    def f(H=P, ldh=64, W=P, ldw=64, z=P, ldl=4, dt=0, i=P, ldi=4, K=4, tau=1.0, T=8, V=16, D=64, loss=P, ws=P, nb=0):
+        a = L.psgd_distill_loss(H, ldh, W, ldw, z, ldl, dt, i, ldi, K, tau, None, T, V, D, loss, P, P, None, ws, nb, None)
+        b = L.psgd_distill_grad(H, ldh, W, ldw, z, ldl, dt, i, ldi, K, tau, None, T, V, D, loss, P, P, 2 * FAR, D, 3 * FAR, D, None, ws, nb, None)
+        assert a == b
+        return a
+
+    assert f() == -3 and f(H=None) == -2 and f(W=None) == -2 and f(z=None) == -2 and f(i=None) == -2 and f(loss=None) == -2 and f(ws=None) == -2
+    assert f(H=P + 8) == -1 and f(ldh=63) == -1 and f(ldl=3) == -1 and f(ldi=3) == -1 and f(dt=5) == -1 and f(K=0) == -1 and f(K=1025, ldl=2000, ldi=2000) == -1
+    assert f(tau=0.0) == -1 and f(tau=float("nan")) == -1 and f(tau=float("inf")) == -1 and f(tau=-1.0) == -1 and f(T=-1) == -1 and f(V=0) == -1 and f(D=0) == -1
+
+
+def test_distillation_workspace(L):
+    """Beyond the cross entropy's: 16 bytes per entry, 12 per token, 4 per 32 rows and 128 columns."""
+    a, b = C.c_size_t(), C.c_size_t()
+    for T, V, D, K, grad in ((1, 32000, 768, 8, 0), (777, 50257, 768, 50, 0), (4096, 32000, 768, 64, 1), (1 << 20, 131072, 1024, 32, 1)):
+        assert L.psgd_distill_workspace(T, V, D, K, grad, C.byref(a)) == 0 and L.psgd_xent_workspace(T, V, D, grad, C.byref(b)) == 0
+        blocks = (T + 31) // 32
+        assert b.value <= a.value <= b.value + T * (12 * K + 12) + blocks * (128 * K + 4 * (V // 128 + 2)) + 4096
