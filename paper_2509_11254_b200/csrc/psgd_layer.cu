@@ -15,26 +15,54 @@ bool whole_units(const void* p, int64_t ld, int64_t F, int dtype) { return !p ||
 bool rows_ok(int64_t T, int64_t F) { return T >= 0 && T <= MAX_EXTENT && extent_ok(F); }
 
 // ---- layer norm ----
-constexpr int NORM_WIDE = 2 * NORM_THREADS;         // units of a row from which it no longer fits its threads' registers
+// How a row's units are shared: `vpt` per thread, `threads` per row (whole warps), `rows` side by side per CTA, `stages` rows of the ring.
+struct NormPlan { int vpt, threads, rows, stages; bool wide; int64_t ctas; size_t smem; };
+constexpr int NORM_SMEM = 200 << 10;                // of a multiprocessor's, for rings
 
-// How a row's units are shared: `vpt` per thread, `threads` per row (whole warps), `rows` at a time per CTA.
-struct NormPlan { int vpt, threads, rows; bool wide; int64_t ctas; };
-NormPlan plan_norm(int64_t T, int64_t F, bool vec, int per_sm) {
+// `row_bytes`: of all operands of a row that are read.  `backward`: more registers per unit
+NormPlan plan_norm(int64_t T, int64_t F, bool ring, int64_t row_bytes, bool backward) {
     NormPlan p{};
-    const int64_t units = vec ? (F + 7) / 8 : (F + 255) / 256 * 32;
-    p.wide = units > NORM_WIDE;
-    p.vpt = units > 256 ? 2 : 1;
-    p.threads = p.wide ? NORM_THREADS : (int)align_up(ceil_div(units, p.vpt), 32);
-    p.rows = p.wide ? 1 : std::max(1, 256 / p.threads);
-    p.ctas = std::min<int64_t>((T + p.rows - 1) / p.rows, (int64_t)device_sms() * std::max(1, per_sm / (p.threads * p.rows)));
+    const int64_t sms = device_sms();
+    if (!ring) {                                    // a value per lane: one unit per thread
+        const int64_t units = (F + 255) / 256 * 32;
+        p.wide = units > NORM_THREADS;
+        p.vpt = 1;
+        p.threads = p.wide ? NORM_THREADS : (int)units;
+        p.rows = p.wide ? 1 : std::max(1, 256 / p.threads);
+        p.smem = backward && p.rows > 1 ? (size_t)p.rows * 2 * F * 4 : 0;
+        p.ctas = std::min<int64_t>((T + p.rows - 1) / p.rows, sms * std::max(1, (backward ? 512 : 1024) / (p.threads * p.rows)));
+        return p;
+    }
+    const int64_t units = F / 8;
+    // Several units per thread cost fewer exchanges (a warp's shuffles take as long as half a unit).  The number of rows has no say: a row's bits do not depend on its batch.
+    double best = 1e300;
+    for (int vpt = 1; vpt <= 4; ++vpt) {
+        const int64_t g = (int64_t)align_up((size_t)ceil_div(units, vpt), 32);
+        if (g > NORM_THREADS) continue;
+        const double cost = g * (vpt + 0.5);
+        if (cost < best) { best = cost; p.vpt = vpt; p.threads = (int)g; }
+    }
+    const size_t row = (size_t)row_bytes / F * (size_t)(p.threads * p.vpt * 8);      // in the ring, with the places of units that do not exist
+    p.wide = p.threads == 0 || 2 * row > (size_t)NORM_SMEM;
+    if (p.wide) {
+        p.threads = NORM_THREADS;
+        p.rows = 1;
+        p.ctas = std::min<int64_t>(T, sms * 2);
+        return p;
+    }
+    p.rows = std::max(1, 256 / p.threads);
+    const int resident = std::max(1, (p.vpt == 1 ? 1024 : p.vpt == 2 ? 768 : 512) / (p.threads * p.rows));       // CTAs per multiprocessor, by registers
+    p.stages = (int)std::max<size_t>(2, std::min<size_t>(4, NORM_SMEM / (row * p.rows * resident)));
+    p.smem = row * p.rows * p.stages;
+    if (backward && p.rows > 1) p.smem = std::max(p.smem, (size_t)p.rows * 2 * F * 4);
+    p.ctas = std::min<int64_t>((T + p.rows - 1) / p.rows, sms * std::max<int64_t>(1, std::min<int64_t>(resident, NORM_SMEM / p.smem)));
     return p;
 }
-constexpr int FORWARD_THREADS = 1024, BACKWARD_THREADS = 512;     // per multiprocessor
 
 struct NormGrad { NormPlan p; int64_t parts; size_t part, sums, total; };
-NormGrad plan_norm_grad(int64_t T, int64_t F, bool vec) {
+NormGrad plan_norm_grad(int64_t T, int64_t F, bool ring, int64_t row_bytes) {
     NormGrad g{};
-    g.p = plan_norm(T, F, vec, BACKWARD_THREADS);
+    g.p = plan_norm(T, F, ring, row_bytes, true);
     const int64_t tiles = (F + 2047) / 2048;
     g.parts = g.p.wide ? std::min<int64_t>({T, 65535, std::max<int64_t>(1, device_sms() * 4 / tiles)}) : g.p.ctas;
     g.part = 0;
@@ -43,22 +71,41 @@ NormGrad plan_norm_grad(int64_t T, int64_t F, bool vec) {
     return g;
 }
 
-template <typename X, typename Y, bool VEC>
-bool norm_forward(const NormForward& a, const NormPlan& p, cudaStream_t st) {
+template <typename X, typename Y, bool RING>
+bool norm_forward(NormForward a, const NormPlan& p, cudaStream_t st) {
     const dim3 grid((unsigned)p.ctas), block(p.threads, p.rows);
-    if (p.wide) return launch(k_norm_forward_wide<X, Y, VEC>, grid, block, 0, st, a);
-    return p.vpt == 1 ? launch(k_norm_forward<X, Y, VEC, 1>, grid, block, 0, st, a) : launch(k_norm_forward<X, Y, VEC, 2>, grid, block, 0, st, a);
+    a.stages = p.stages;
+    const auto run = [&](auto kernel) {
+        if (p.smem > 40 << 10) set_smem_attr((const void*)kernel, p.smem);      // (static shared memory comes on top)
+        return launch(kernel, grid, block, p.smem, st, a);
+    };
+    if (p.wide) return launch(k_norm_forward_wide<X, Y, RING>, grid, block, 0, st, a);
+    if constexpr (RING) {
+        if (p.vpt == 2) return run(k_norm_forward<X, Y, true, 2>);
+        if (p.vpt == 3) return run(k_norm_forward<X, Y, true, 3>);
+        if (p.vpt == 4) return run(k_norm_forward<X, Y, true, 4>);
+    }
+    return run(k_norm_forward<X, Y, RING, 1>);
 }
-template <typename X, typename Y, bool VEC>
+template <typename X, typename Y, bool RING>
 bool norm_backward(NormBackward a, const NormGrad& g, cudaStream_t st) {
     const NormPlan& p = g.p;
     const dim3 grid((unsigned)p.ctas), block(p.threads, p.rows);
+    a.stages = p.stages;
     if (p.wide) {
-        return launch(k_norm_sums_wide<X, Y, VEC>, grid, block, 0, st, a) &&
-               launch(k_norm_apply_wide<X, Y, VEC>, dim3(ceil_div(a.F, 2048), (unsigned)g.parts), dim3(256), 0, st, a);
+        return launch(k_norm_sums_wide<X, Y, RING>, grid, block, 0, st, a) &&
+               launch(k_norm_apply_wide<X, Y, RING>, dim3(ceil_div(a.F, 2048), (unsigned)g.parts), dim3(256), 0, st, a);
     }
-    const size_t smem = p.rows > 1 ? (size_t)2 * a.F * 4 : 0;
-    return p.vpt == 1 ? launch(k_norm_backward<X, Y, VEC, 1>, grid, block, smem, st, a) : launch(k_norm_backward<X, Y, VEC, 2>, grid, block, smem, st, a);
+    const auto run = [&](auto kernel) {
+        if (p.smem > 40 << 10) set_smem_attr((const void*)kernel, p.smem);      // (static shared memory comes on top)
+        return launch(kernel, grid, block, p.smem, st, a);
+    };
+    if constexpr (RING) {
+        if (p.vpt == 2) return run(k_norm_backward<X, Y, true, 2>);
+        if (p.vpt == 3) return run(k_norm_backward<X, Y, true, 3>);
+        if (p.vpt == 4) return run(k_norm_backward<X, Y, true, 4>);
+    }
+    return run(k_norm_backward<X, Y, RING, 1>);
 }
 // the pairs of types: x and y (dy) alike, or x float32 and y bfloat16
 bool types_ok(int x, int y) { return dtype_ok(x) && dtype_ok(y) && (x == y || x == PSGD_DT_F32); }
@@ -105,7 +152,7 @@ psgd_status psgd_norm_forward(const void* x, int64_t ldx, int x_dtype, const voi
     a.ldx = ldx; a.ldr = ldr; a.lds = lds; a.ldy = ldy;
     a.w = {w, w_dtype == PSGD_DT_BF16}; a.b = {b, w_dtype == PSGD_DT_BF16};
     a.mean = center ? mean : nullptr; a.rstd = rstd; a.q = q; a.scales = scales;
-    const NormPlan p = plan_norm(T, F, vec, FORWARD_THREADS);
+    const NormPlan p = plan_norm(T, F, vec, F * size_of(x_dtype) * (r ? 2 : 1), false);
     const bool ok = by_type(x_dtype, y_dtype, vec, [&](auto* tx, auto* ty, auto v) {
         return norm_forward<std::remove_pointer_t<decltype(tx)>, std::remove_pointer_t<decltype(ty)>, decltype(v)::value>(a, p, (cudaStream_t)stream);
     });
@@ -115,7 +162,12 @@ psgd_status psgd_norm_forward(const void* x, int64_t ldx, int x_dtype, const voi
 psgd_status psgd_norm_workspace(int64_t T, int64_t F, size_t* bytes) {
     if (!bytes) return PSGD_E_NULL;
     if (!rows_ok(T, F)) return PSGD_E_INVALID;
-    *bytes = T == 0 ? 256 : std::max(plan_norm_grad(T, F, true).total, plan_norm_grad(T, F, false).total);
+    *bytes = 256;
+    if (T > 0) {
+        // whatever the types, the alignment and the operands (2 + 2, 4 + 2, 4 + 4 bytes per column, and x's again)
+        *bytes = plan_norm_grad(T, F, false, 0).total;
+        for (int each : {4, 6, 8, 10, 12}) *bytes = std::max(*bytes, F % 8 ? 0 : plan_norm_grad(T, F, true, F * each).total);
+    }
     return PSGD_OK;
 }
 
@@ -133,7 +185,7 @@ psgd_status psgd_norm_backward(const void* dy, int64_t lddy, int dy_dtype, const
     const Stretch out = stretch(dx, T, F, lddx, size);
     if (overlap(out, stretch(dy, T, F, lddy, size_of(dy_dtype))) || overlap(out, stretch(x, T, F, ldx, size)) || overlap(out, stretch(add, T, F, ldadd, size))) return PSGD_E_INVALID;
     const bool vec = whole_units(dy, lddy, F, dy_dtype) && whole_units(x, ldx, F, x_dtype) && whole_units(add, ldadd, F, x_dtype) && whole_units(dx, lddx, F, x_dtype);
-    const NormGrad g = plan_norm_grad(T, F, vec);
+    const NormGrad g = plan_norm_grad(T, F, vec, F * (size_of(dy_dtype) + size * (add ? 2 : 1)));
     if (ws_bytes < g.total) return PSGD_E_WORKSPACE;
     NormBackward a{};
     a.T = T; a.F = (int)F; a.center = mean != nullptr;
@@ -142,11 +194,13 @@ psgd_status psgd_norm_backward(const void* dy, int64_t lddy, int dy_dtype, const
     a.w = {w, w_dtype == PSGD_DT_BF16};
     a.mean = mean; a.rstd = rstd;
     a.part = (float*)((char*)ws + g.part);
+    a.dw = dw; a.db = db;
     a.sums = (float2*)((char*)ws + g.sums);
     const bool ok = by_type(x_dtype, dy_dtype, vec, [&](auto* tx, auto* ty, auto v) {
         return norm_backward<std::remove_pointer_t<decltype(tx)>, std::remove_pointer_t<decltype(ty)>, decltype(v)::value>(a, g, st);
     });
     if (!ok) return PSGD_E_CUDA;
+    if (g.parts == 1) return PSGD_OK;                  // (the one CTA has written the results)
     const NormJoin j{(int)F, (int)g.parts, a.part, dw, db};
     return launch(k_norm_join, dim3(ceil_div(F, 32), db ? 2 : 1), dim3(1024), 0, st, j) ? PSGD_OK : PSGD_E_CUDA;
 }

@@ -5,11 +5,15 @@
 //   g = dy w,  xh = (s - m) f,  ds = f (g - mean(g) - xh mean(g xh)) + what reaches s from elsewhere  (mean(g) only with centring),
 //   dw = sum over rows of dy xh,  db = sum over rows of dy.
 //
-// One pass over the operands, bound by HBM.  blockDim.x threads share a row (blockDim.y rows per CTA), each holds VPT units of eight values of it in
-// registers between the statistics and the result.  The sum of squares is taken about the warp's own mean and the warps' results are
-// joined exactly (squares about the joint mean = sum of the warps' squares + n_w (mean_w - mean)^2), so that a large mean costs no bits and
-// a row takes one exchange between its warps.  The CTAs stay and walk over the rows: weights are loaded once, and in the backward pass every
-// thread sums dw and db of its columns over the CTA's rows; those partial sums are added by k_norm_join in a fixed order.
+// One pass over the operands, bound by HBM.  blockDim.x threads share a row (blockDim.y rows per CTA side by side), each works on VPT units of eight
+// values of it.  The sum of squares is taken about the warp's own mean and the warps' results are joined exactly (squares about the joint mean = sum of the
+// warps' squares + n_w (mean_w - mean)^2), so that a large mean costs no bits and a row takes one exchange between its warps, none where a warp has it alone.
+// The CTAs stay and walk over the rows: weights are loaded once, and in the backward pass every thread sums dw and db of its columns over its
+// rows; the CTA adds its rows' sums, k_norm_join those of the CTAs, in a fixed order.
+//
+// Rows of whole 16-byte units go through a ring in shared memory (RING): every thread copies its own units of the rows to come asynchronously (cp.async) and reads back only
+// what it copied itself, so that there is nothing to wait for but its own copies, several rows per group are under way whatever the registers hold, and the
+// backward pass reads a row a second time from there.  Rows of any other width or alignment: a value per lane, the next row's values in registers.
 // Sums and statistics are float32.  Rounded once: s to x's type, y, ds; the 8-bit form is that of the rounded y.
 #pragma once
 #include "psgd_values.cuh"
@@ -100,6 +104,7 @@ __device__ __forceinline__ void cell_keep(const float (&x)[8], int col, long lon
     }
 }
 
+__device__ __forceinline__ unsigned smem_addr(const void* p) { return (unsigned)__cvta_generic_to_shared(p); }
 // Waits for the threads that share a row (threadIdx.y); a warp alone needs no barrier.
 __device__ __forceinline__ void row_sync() {
     if (blockDim.x == 32) __syncwarp();
@@ -131,6 +136,7 @@ struct NormForward {
     long long ldx, ldr, lds, ldy;
     NormParam w, b;
     float *mean, *rstd;                                // mean: or nullptr
+    int stages;                                        // rows of a ring
     int8_t* q;                                         // the 8-bit form of y, or nullptr
     uint8_t* scales;
 };
@@ -174,9 +180,51 @@ __device__ __forceinline__ RowStats row_stats(const float (&v)[VPT][8], const in
     return s;
 }
 
-template <typename X, typename Y, bool VEC, int VPT>
+// A thread's share of a ring: `stages` rows of its group, of each up to three operands.  Unit i of an operand lies at its plane + (i * blockDim.x + threadIdx.x) * 16; the second
+// halves of float32 units follow in a plane of their own, so that a warp's accesses are side by side.
+template <typename X> __device__ __forceinline__ int plane_bytes(int vpt) { return vpt * (int)blockDim.x * 8 * (int)sizeof(X); }
+__device__ __forceinline__ void copy16(unsigned to, const void* from) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"(to), "l"(from) : "memory"); }
+__device__ __forceinline__ uint4 shared16(unsigned at) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
+}
+template <typename X, int VPT>
+__device__ __forceinline__ void ring_ask(unsigned plane, const X* row, const int (&col)[VPT], const int (&n)[VPT]) {
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+        if (!n[i]) continue;
+        const unsigned to = plane + (i * blockDim.x + threadIdx.x) * 16;
+        copy16(to, row + col[i]);
+        if (sizeof(X) == 4) copy16(to + VPT * blockDim.x * 16, row + col[i] + 4);
+    }
+}
+template <typename X, int VPT>
+__device__ __forceinline__ void ring_read(unsigned plane, int i, int n, float (&v)[8]) {
+    const unsigned at = plane + (i * blockDim.x + threadIdx.x) * 16;
+    uint4 a = make_uint4(0u, 0u, 0u, 0u), b = a;
+    if (n) a = shared16(at);
+    if (sizeof(X) == 4) {
+        if (n) b = shared16(at + VPT * blockDim.x * 16);
+        const unsigned w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(w[j]);
+    } else {
+        widen(Raw16{a}, v);
+    }
+}
+// One group of copies per row, empty ones behind the last row included: a row's have landed when at most stages - 1 younger groups are under way.
+__device__ __forceinline__ void ring_commit() { asm volatile("cp.async.commit_group;\n" ::: "memory"); }
+__device__ __forceinline__ void ring_wait(int stages) {
+    if (stages == 4) asm volatile("cp.async.wait_group 3;\n" ::: "memory");
+    else if (stages == 3) asm volatile("cp.async.wait_group 2;\n" ::: "memory");
+    else asm volatile("cp.async.wait_group 1;\n" ::: "memory");
+}
+
+template <typename X, typename Y, bool RING, int VPT>
 __global__ void __launch_bounds__(NORM_THREADS) k_norm_forward(const __grid_constant__ NormForward a) {
-    typedef typename Cell<X, VEC>::Raw Raw;
+    typedef typename Cell<X, RING>::Raw Raw;
+    extern __shared__ __align__(16) unsigned char ring_raw[];
     __shared__ float2 stat[2][NORM_WARPS];             // by rows taken in turn: a row's exchange is over when the next but one writes
     __shared__ float counts[NORM_WARPS];
     grid_trigger();
@@ -185,54 +233,79 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_forward(const __grid_cons
     int have = 0;
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
-        col[i] = cell_col<VEC>(tid + i * (int)blockDim.x);
-        n[i] = cell_count<VEC>(col[i], F);
+        col[i] = cell_col<RING>(tid + i * (int)blockDim.x);
+        n[i] = cell_count<RING>(col[i], F);
         have += n[i];
     }
     const float in_warp = (float)__reduce_add_sync(0xffffffffu, have);
     if (threadIdx.y == 0 && (tid & 31) == 0) counts[tid >> 5] = in_warp;
     __syncthreads();
     grid_wait();
-    float w[VPT][8], b[VPT][8];
-#pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-        param_cell<VEC>(w[i], a.w, col[i], n[i], 1.f);
-        param_cell<VEC>(b[i], a.b, col[i], n[i], 0.f);
-    }
-    const int G = (F + ACT_GROUP - 1) / ACT_GROUP;
     const X *x = (const X*)a.x, *r = (const X*)a.r;
     X* s = (X*)a.s;
     Y* y = (Y*)a.y;
     const long long step = (long long)gridDim.x * blockDim.y;
     long long row = (long long)blockIdx.x * blockDim.y + threadIdx.y;
+    const int plane = plane_bytes<X>(VPT), stage = r ? 2 * plane : plane;
+    const unsigned ring = RING ? smem_addr(ring_raw) + threadIdx.y * a.stages * stage : 0u;
     Raw next[VPT], add[VPT];
-    const auto ask = [&](long long at) {
+    const auto ask = [&](long long at, unsigned to) {
+        if constexpr (RING) {
+            if (at < a.T) {
+                ring_ask<X, VPT>(to, x + at * a.ldx, col, n);
+                if (r) ring_ask<X, VPT>(to + plane, r + at * a.ldr, col, n);
+            }
+            ring_commit();
+        } else if (at < a.T) {
 #pragma unroll
-        for (int i = 0; i < VPT; ++i) {
-            cell_load(next[i], x + at * a.ldx + col[i], n[i]);
-            if (r) cell_load(add[i], r + at * a.ldr + col[i], n[i]);
+            for (int i = 0; i < VPT; ++i) {
+                cell_load(next[i], x + at * a.ldx + col[i], n[i]);
+                if (r) cell_load(add[i], r + at * a.ldr + col[i], n[i]);
+            }
         }
     };
-    if (row < a.T) ask(row);
+    if constexpr (RING) {
+        for (int k = 0; k < a.stages; ++k) ask(row + k * step, ring + k * stage);
+    } else {
+        ask(row, 0u);
+    }
+    float w[VPT][8], b[VPT][8];
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+        param_cell<RING>(w[i], a.w, col[i], n[i], 1.f);
+        param_cell<RING>(b[i], a.b, col[i], n[i], 0.f);
+    }
+    const int G = (F + ACT_GROUP - 1) / ACT_GROUP;
+    unsigned from = ring;
     for (int turn = 0; row < a.T; row += step, turn ^= 1) {
         float v[VPT][8];
+        if constexpr (RING) ring_wait(a.stages);
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
-            widen(next[i], v[i]);
+            float u[8];
+            if constexpr (RING) {
+                ring_read<X, VPT>(from, i, n[i], v[i]);
+                if (r) ring_read<X, VPT>(from + plane, i, n[i], u);
+            } else {
+                widen(next[i], v[i]);
+                if (r) widen(add[i], u);
+            }
             if (r) {
-                float u[8];
-                widen(add[i], u);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[i][j] += u[j];
                 round_to<X>(v[i]);
             }
         }
-        if (row + step < a.T) ask(row + step);
+        if constexpr (!RING) ask(row + step, 0u);
         if (s) {
 #pragma unroll
-            for (int i = 0; i < VPT; ++i) cell_store<VEC>(s + row * a.lds + col[i], v[i], n[i]);
+            for (int i = 0; i < VPT; ++i) cell_store<RING>(s + row * a.lds + col[i], v[i], n[i]);
         }
         const RowStats st = row_stats<VPT>(v, n, in_warp, F, a.center, stat[turn] + threadIdx.y * warps, counts);
+        if constexpr (RING) {                          // (every value has been used)
+            ask(row + a.stages * step, from);
+            from = from + stage == ring + a.stages * stage ? ring : from + stage;
+        }
         const float f = rsqrtf(st.m2 / (float)F + a.eps);
         if (tid == 0) {
             a.rstd[row] = f;
@@ -243,12 +316,12 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_forward(const __grid_cons
             float o[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) o[j] = fmaf((v[i][j] - st.mean) * f, w[i][j], b[i][j]);
-            cell_store<VEC>(y + row * a.ldy + col[i], o, n[i]);
+            cell_store<RING>(y + row * a.ldy + col[i], o, n[i]);
             if (a.q) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) o[j] = j < n[i] ? o[j] : 0.f;
                 round_to<Y>(o);
-                cell_keep<VEC>(o, col[i], row * G, G, a.q, a.scales);
+                cell_keep<RING>(o, col[i], row * G, G, a.q, a.scales);
             }
         }
     }
@@ -341,67 +414,101 @@ struct NormBackward {
     long long lddy, ldx, ldadd, lddx;
     NormParam w;
     const float *mean, *rstd;                          // mean: nullptr without centring
+    int stages;                                        // rows of a ring
     float* part;                                       // [CTAs][2][F]: dw, db
+    float *dw, *db;                                    // db: or nullptr
     float2* sums;                                      // wide rows: [T] mean(g), mean(g xh)
-    int chunks;                                        // wide rows: CTAs that share a column
 };
 struct NormJoin { int F, parts; const float* part; float *dw, *db; };      // db: or nullptr
 
-template <typename X, typename Y, bool VEC, int VPT>
+template <typename X, typename Y, bool RING, int VPT>
 __global__ void __launch_bounds__(NORM_THREADS) k_norm_backward(const __grid_constant__ NormBackward a) {
-    typedef typename Cell<X, VEC>::Raw RawX;
-    typedef typename Cell<Y, VEC>::Raw RawY;
-    extern __shared__ float columns[];                 // [2][F] where a CTA takes several rows at a time
+    typedef typename Cell<X, RING>::Raw RawX;
+    typedef typename Cell<Y, RING>::Raw RawY;
+    extern __shared__ __align__(16) unsigned char ring_raw[];      // the ring; at the end the sums of the rows side by side, [blockDim.y][2][F]
     __shared__ float2 stat[2][NORM_WARPS];
     grid_trigger();
     const int F = a.F, tid = threadIdx.x, warps = blockDim.x >> 5;
     int col[VPT], n[VPT];
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
-        col[i] = cell_col<VEC>(tid + i * (int)blockDim.x);
-        n[i] = cell_count<VEC>(col[i], F);
+        col[i] = cell_col<RING>(tid + i * (int)blockDim.x);
+        n[i] = cell_count<RING>(col[i], F);
     }
     grid_wait();
-    float w[VPT][8], dw[VPT][8], db[VPT][8];
-#pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-        param_cell<VEC>(w[i], a.w, col[i], n[i], 1.f);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) dw[i][j] = db[i][j] = 0.f;
-    }
     const Y* dy = (const Y*)a.dy;
     const X *x = (const X*)a.x, *add = (const X*)a.add;
     X* dx = (X*)a.dx;
     const long long step = (long long)gridDim.x * blockDim.y;
     long long row = (long long)blockIdx.x * blockDim.y + threadIdx.y;
+    const int plane = plane_bytes<X>(VPT), plane_dy = plane_bytes<Y>(VPT), stage = plane_dy + (add ? 2 : 1) * plane;
+    const unsigned ring = RING ? smem_addr(ring_raw) + threadIdx.y * a.stages * stage : 0u;
     RawX nx[VPT], na[VPT];
     RawY ny[VPT];
-    float nm = 0.f, nf = 0.f;
-    const auto ask = [&](long long at) {
+    float nm = 0.f, nf = 0.f;                          // the next row's mean and rstd
+    const auto ask_stats = [&](long long at) {
+        if (at >= a.T) return;
         nf = a.rstd[at];
         if (a.mean) nm = a.mean[at];
+    };
+    const auto ask = [&](long long at, unsigned to) {
+        if constexpr (RING) {
+            if (at < a.T) {
+                ring_ask<Y, VPT>(to, dy + at * a.lddy, col, n);
+                ring_ask<X, VPT>(to + plane_dy, x + at * a.ldx, col, n);
+                if (add) ring_ask<X, VPT>(to + plane_dy + plane, add + at * a.ldadd, col, n);
+            }
+            ring_commit();
+        } else if (at < a.T) {
 #pragma unroll
-        for (int i = 0; i < VPT; ++i) {
-            cell_load(nx[i], x + at * a.ldx + col[i], n[i]);
-            cell_load(ny[i], dy + at * a.lddy + col[i], n[i]);
-            if (add) cell_load(na[i], add + at * a.ldadd + col[i], n[i]);
+            for (int i = 0; i < VPT; ++i) {
+                cell_load(nx[i], x + at * a.ldx + col[i], n[i]);
+                cell_load(ny[i], dy + at * a.lddy + col[i], n[i]);
+                if (add) cell_load(na[i], add + at * a.ldadd + col[i], n[i]);
+            }
         }
     };
-    if (row < a.T) ask(row);
+    if constexpr (RING) {
+        for (int k = 0; k < a.stages; ++k) ask(row + k * step, ring + k * stage);
+    } else {
+        ask(row, 0u);
+    }
+    ask_stats(row);
+    float w[VPT][8], dw[VPT][8], db[VPT][8];
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+        param_cell<RING>(w[i], a.w, col[i], n[i], 1.f);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) dw[i][j] = db[i][j] = 0.f;
+    }
     const float per = 1.f / (float)F;
+    unsigned from = ring;
     for (int turn = 0; row < a.T; row += step, turn ^= 1) {
         RawX cx[VPT], ca[VPT];
         RawY cy[VPT];
+        if constexpr (!RING) {
 #pragma unroll
-        for (int i = 0; i < VPT; ++i) { cx[i] = nx[i]; cy[i] = ny[i]; ca[i] = na[i]; }
+            for (int i = 0; i < VPT; ++i) { cx[i] = nx[i]; cy[i] = ny[i]; ca[i] = na[i]; }
+            ask(row + step, 0u);
+        }
         const float f = nf, m = nm;
-        if (row + step < a.T) ask(row + step);
+        ask_stats(row + step);
+        if constexpr (RING) ring_wait(a.stages);
+        // a unit's x and dy, both times they are needed
+        const auto values = [&](int i, float (&v)[8], float (&d)[8]) {
+            if constexpr (RING) {
+                ring_read<Y, VPT>(from, i, n[i], d);
+                ring_read<X, VPT>(from + plane_dy, i, n[i], v);
+            } else {
+                widen(cx[i], v);
+                widen(cy[i], d);
+            }
+        };
         float s1 = 0.f, s2 = 0.f;
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             float v[8], d[8];
-            widen(cx[i], v);
-            widen(cy[i], d);
+            values(i, v, d);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {              // (dy and w are zeros where there is no value)
                 const float xh = (v[j] - m) * f, g = d[j] * w[i][j];
@@ -425,40 +532,50 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_backward(const __grid_con
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             float v[8], d[8];
-            widen(cx[i], v);
-            widen(cy[i], d);
+            values(i, v, d);
 #pragma unroll
             for (int j = 0; j < 8; ++j) d[j] = f * (fmaf(-((v[j] - m) * f), s2, d[j] * w[i][j]) - s1);
             if (add) {
-                widen(ca[i], v);
+                if constexpr (RING) ring_read<X, VPT>(from + plane_dy + plane, i, n[i], v);
+                else widen(ca[i], v);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) d[j] += v[j];
             }
-            cell_store<VEC>(dx + row * a.lddx + col[i], d, n[i]);
+            cell_store<RING>(dx + row * a.lddx + col[i], d, n[i]);
+        }
+        if constexpr (RING) {
+            ask(row + a.stages * step, from);
+            from = from + stage == ring + a.stages * stage ? ring : from + stage;
         }
     }
-    // the CTA's sums: its rows side by side (threadIdx.y) one after the other
-    float* part = a.part + (size_t)blockIdx.x * 2 * F;
-    for (int k = 0; k < (int)blockDim.y; ++k) {
-        const bool first = k == 0, last = k + 1 == (int)blockDim.y;
-        if ((int)threadIdx.y == k) {
+    // the CTA's sums: its rows side by side (threadIdx.y) through shared memory; a CTA alone writes the results
+    float* pw = gridDim.x == 1 ? a.dw : a.part + (size_t)blockIdx.x * 2 * F;
+    float* pb = gridDim.x == 1 ? a.db : pw + F;
+    const bool alone = blockDim.y == 1;
+    float* sums = reinterpret_cast<float*>(ring_raw) + (size_t)threadIdx.y * 2 * F;
+    if (RING) asm volatile("cp.async.wait_all;\n" ::: "memory");
+    if (!alone) __syncthreads();
+    float *to_w = alone ? pw : sums, *to_b = alone ? pb : sums + F;
 #pragma unroll
-            for (int i = 0; i < VPT; ++i)
+    for (int i = 0; i < VPT; ++i)
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (j < n[i]) {
-                        const int c = col[i] + (VEC ? j : 32 * j);
-                        const float p = (first ? 0.f : columns[c]) + dw[i][j], q = (first ? 0.f : columns[F + c]) + db[i][j];
-                        float* to = last ? part : columns;
-                        to[c] = p;
-                        to[F + c] = q;
-                    }
-        }
-        if (!last) __syncthreads();
+        for (int j = 0; j < 8; ++j)
+            if (j < n[i]) {
+                const int c = col[i] + (RING ? j : 32 * j);
+                to_w[c] = dw[i][j];
+                if (to_b) to_b[c] = db[i][j];
+            }
+    if (alone) return;
+    __syncthreads();
+    for (int c = threadIdx.y * blockDim.x + tid; c < 2 * F; c += blockDim.x * blockDim.y) {
+        float sum = 0.f;
+        for (int k = 0; k < (int)blockDim.y; ++k) sum += reinterpret_cast<float*>(ring_raw)[(size_t)k * 2 * F + c];
+        if (c < F) pw[c] = sum;
+        else if (pb) pb[c - F] = sum;
     }
 }
 
-// Wide rows: first the two sums of every row (a CTA per row), then dx and the sums over rows (256 units of the columns per CTA, `chunks` CTAs share the rows).
+// Wide rows: first the two sums of every row (a CTA per row), then dx and the sums over rows (256 units of the columns per CTA, gridDim.y CTAs share the rows).
 template <typename X, typename Y, bool VEC>
 __global__ void __launch_bounds__(NORM_THREADS) k_norm_sums_wide(const __grid_constant__ NormBackward a) {
     __shared__ float2 part[NORM_WARPS];
@@ -533,13 +650,14 @@ __global__ void __launch_bounds__(256) k_norm_apply_wide(const __grid_constant__
         }
         cell_store<VEC>((X*)a.dx + row * a.lddx + col, o, n);
     }
-    float* part = a.part + (size_t)blockIdx.y * 2 * F;
+    float* pw = gridDim.y == 1 ? a.dw : a.part + (size_t)blockIdx.y * 2 * F;
+    float* pb = gridDim.y == 1 ? a.db : pw + F;
 #pragma unroll
     for (int j = 0; j < 8; ++j)
         if (j < n) {
             const int c = col + (VEC ? j : 32 * j);
-            part[c] = dw[j];
-            part[F + c] = db[j];
+            pw[c] = dw[j];
+            if (pb) pb[c] = db[j];
         }
 }
 

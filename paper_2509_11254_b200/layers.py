@@ -22,14 +22,22 @@ LayerNorm = namedtuple("LayerNorm", "y x mean rstd kept")
 LayerNormGrad = namedtuple("LayerNormGrad", "d_x d_weight d_bias")
 
 _LAYOUTS = {"half": 0, "interleaved": 1}
+_BOTH = tuple(_DTYPES)
+_empty_like = torch.empty_like
+
+
+def _like(x, rows, cols):
+    """A new matrix of x's shape and type whose rows lie one after the other (the shortest way to it where x's own do)."""
+    return _empty_like(x) if x.is_contiguous() else _empty((rows, cols), dtype=x.dtype, device=x.device)
 
 
 # ---- layer norm ---------------------------------------------------------------------------------------------------
 def _param(t, name, n, device, dtype=None):
-    """(address, dtype code) of a vector over the columns, float32 or bfloat16."""
-    if not isinstance(t, torch.Tensor) or t.dtype not in _DTYPES or (dtype is not None and t.dtype != dtype):
-        raise PSGDError(f"{name} must be a {'float32 or bfloat16' if dtype is None else _name(dtype)} tensor")
-    return _vector(t, name, t.dtype, n, device), _DTYPES[t.dtype]
+    """(address, dtype code) of a vector over the columns, float32 or bfloat16 (or `dtype`)."""
+    code = _DTYPES.get(t.dtype) if isinstance(t, torch.Tensor) else None
+    if code is None or (dtype is not None and t.dtype != dtype) or t.shape != (n,) or not t.is_contiguous() or t.get_device() != device.index:
+        raise PSGDError(f"{name} must be a contiguous {'float32 or bfloat16' if dtype is None else _name(dtype)} tensor of {n} elements on {device}")
+    return t.data_ptr(), code
 
 
 def layer_norm_forward(x, weight, bias=None, residual=None, eps=1e-5, center=True, keep=False, dtype=None, stream=None):
@@ -40,7 +48,7 @@ def layer_norm_forward(x, weight, bias=None, residual=None, eps=1e-5, center=Tru
     Returns (y, x, mean, rstd, kept): x is s (the very tensor `x` without a residual), which the backward pass reads; mean (None without centring) and rstd float32 [T];
     kept the 8-bit checkpoint of y, what pack_activation(y) makes, where `keep` asks for it.
     """
-    T, F, ldx = _matrix(x, "x", tuple(_DTYPES))
+    T, F, ldx = _matrix(x, "x", _BOTH)
     dev = x.device
     at_w, w_type = _param(weight, "weight", F, dev)
     at_b = _param(bias, "bias", F, dev, weight.dtype)[0] if bias is not None else None
@@ -55,11 +63,10 @@ def layer_norm_forward(x, weight, bias=None, residual=None, eps=1e-5, center=Tru
     if at is None:
         with _there(dev, stream, x, weight, bias, residual), torch.no_grad():
             return layer_norm_forward(x, weight, bias, residual, eps, center, keep, dtype)
-    y = _empty((T, F), dtype=dtype, device=dev)
-    s = _empty((T, F), dtype=x.dtype, device=dev) if residual is not None else None
-    stats = _empty((2 if center else 1, T), dtype=torch.float32, device=dev)
-    rstd = stats[0]
-    mean = stats[1] if center else None
+    y = _like(x, T, F) if dtype == x.dtype else _empty((T, F), dtype=dtype, device=dev)
+    s = _like(x, T, F) if residual is not None else None
+    rstd = _empty(T, dtype=torch.float32, device=dev)
+    mean = _empty_like(rstd) if center else None
     kept = ActivationCheckpoint(T, F, dev) if keep else None
     _check(lib().psgd_norm_forward(x.data_ptr(), ldx, _DTYPES[x.dtype], residual.data_ptr() if residual is not None else None, ldr, at_w, at_b, w_type, eps, int(center), T, F,
                                    s.data_ptr() if s is not None else None, F, y.data_ptr(), F, _DTYPES[dtype], mean.data_ptr() if center else None, rstd.data_ptr(),
@@ -73,9 +80,9 @@ def layer_norm_backward(dy, x, weight, mean, rstd, d_x=None, bias=False, stream=
     `d_x` [T, F] (x's type): what reaches x from elsewhere, as around the layers of a residual path; it is added.  Returns (d_x, d_weight, d_bias): d_x in x's type is
     the gradient of x and of the residual alike, d_weight and d_bias (None unless `bias`) float32 [F], summed in a fixed order.
     """
-    T, F, ldx = _matrix(x, "x", tuple(_DTYPES))
+    T, F, ldx = _matrix(x, "x", _BOTH)
     dev = x.device
-    lddy = _matrix(dy, "dy", (_BF16,) if x.dtype == _BF16 else tuple(_DTYPES), (T, F), dev)[2]
+    lddy = _matrix(dy, "dy", (_BF16,) if x.dtype == _BF16 else _BOTH, (T, F), dev)[2]
     at_w, w_type = _param(weight, "weight", F, dev)
     at_mean = _vector(mean, "mean", torch.float32, T, dev) if mean is not None else None
     at_rstd = _vector(rstd, "rstd", torch.float32, T, dev)
@@ -86,13 +93,13 @@ def layer_norm_backward(dy, x, weight, mean, rstd, d_x=None, bias=False, stream=
             return layer_norm_backward(dy, x, weight, mean, rstd, d_x, bias)
     nbytes = _workspace_bytes("psgd_norm_workspace", T, F, dev.index)
     ws = _empty(nbytes, dtype=torch.uint8, device=dev)
-    out = _empty((T, F), dtype=x.dtype, device=dev)
-    sums = _empty((2 if bias else 1, F), dtype=torch.float32, device=dev)
-    # (one row of `mean` would have no address of its own where T = 0; nothing is read there)
+    out = _like(x, T, F)
+    dw = _empty(F, dtype=torch.float32, device=dev)
+    db = _empty_like(dw) if bias else None
     _check(lib().psgd_norm_backward(dy.data_ptr(), lddy, _DTYPES[dy.dtype], x.data_ptr(), ldx, _DTYPES[x.dtype], at_w, w_type, at_mean, at_rstd,
-                                    d_x.data_ptr() if d_x is not None else None, lda, T, F, out.data_ptr(), F, sums.data_ptr(), sums[1].data_ptr() if bias else None,
+                                    d_x.data_ptr() if d_x is not None else None, lda, T, F, out.data_ptr(), F, dw.data_ptr(), db.data_ptr() if bias else None,
                                     ws.data_ptr(), nbytes, at))
-    return LayerNormGrad(out, sums[0], sums[1] if bias else None)
+    return LayerNormGrad(out, dw, db)
 
 
 # ---- rotary positions ---------------------------------------------------------------------------------------------
@@ -132,6 +139,16 @@ def _heads(t, name, like=None):
     return T, H, D, token, head
 
 
+def _heads_like(t):
+    """A new tensor of t's shape and type without gaps, tokens and heads in t's order, and its strides."""
+    out = _empty_like(t)
+    token, head, one = out.stride()
+    if one != 1:                                    # (values used several times in an order that mixes)
+        out = _empty(t.shape, dtype=t.dtype, device=t.device)
+        token, head, one = out.stride()
+    return out, token, head
+
+
 def _rotary(backward, q, k, positions, frequencies, layout, scale, in_place, stream):
     T, H, D, qt, qh = _heads(q, "dq" if backward else "q")
     dev = q.device
@@ -152,10 +169,8 @@ def _rotary(backward, q, k, positions, frequencies, layout, scale, in_place, str
     if in_place:
         oq, ok, oqt, oqh, okt, okh = q, k, qt, qh, kt, kh
     else:
-        both = _empty((T, H + K, D), dtype=q.dtype, device=dev)
-        oq, ok = both[:, :H], both[:, H:] if k is not None else None
-        oqt = okt = (H + K) * D
-        oqh = okh = D
+        oq, oqt, oqh = _heads_like(q)
+        ok, okt, okh = _heads_like(k) if k is not None else (None, 0, 0)
     none = k is None or K == 0
     _check(lib().psgd_rotary(q.data_ptr(), qt, qh, H, oq.data_ptr(), oqt, oqh, None if none else k.data_ptr(), kt, kh, K, None if none else ok.data_ptr(), okt, okh,
                              at_positions, at_frequencies, T, D, R, _LAYOUTS[layout], int(backward), scale, _DTYPES[q.dtype], at))
@@ -168,7 +183,7 @@ def rotary_forward(q, k, positions, frequencies, layout="half", scale=1.0, in_pl
     bfloat16 or float32 with unit stride within a head; tokens and heads may have any strides (parts of one projection's result, tokens or heads first).  positions [T]
     int64; frequencies [R/2] float64 radians per position (rotary_frequencies), R <= head: the values behind the first R pass through.  layout "half": pairs
     (i, i + R/2); "interleaved": (2i, 2i + 1).  `scale` multiplies what is turned.  Angles are formed in 64 bits, so that far positions keep theirs.
-    in_place: q and k themselves are overwritten, else the results are new tensors that lie side by side, [T, heads + key heads, head].
+    in_place: q and k themselves are overwritten, else the results are new tensors without gaps, tokens and heads in the order in which the inputs have them.
     """
     return _rotary(False, q, k, positions, frequencies, layout, scale, in_place, stream)
 

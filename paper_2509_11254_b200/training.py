@@ -112,8 +112,11 @@ def _operand(t, rows, cols, ld, stream, *outputs):
 
 def _no_graph(name, inputs, instead, depth):
     """Warns, `depth` calls up, where autograd would lose the gradient of one of `inputs` without a word."""
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in inputs):
-        warnings.warn(f"{name}: the results have no autograd graph, no gradient will reach its inputs; {instead}, or call it under torch.no_grad()", stacklevel=depth)
+    if torch.is_grad_enabled():
+        for t in inputs:
+            if t is not None and t.requires_grad:
+                warnings.warn(f"{name}: the results have no autograd graph, no gradient will reach its inputs; {instead}, or call it under torch.no_grad()", stacklevel=depth)
+                return
 
 
 # the handle of the current stream and the current device without the objects around them, where torch has it so
