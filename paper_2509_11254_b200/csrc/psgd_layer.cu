@@ -15,12 +15,12 @@ bool whole_units(const void* p, int64_t ld, int64_t F, int dtype) { return !p ||
 bool rows_ok(int64_t T, int64_t F) { return T >= 0 && T <= MAX_EXTENT && extent_ok(F); }
 
 // ---- layer norm ----
-// How a row's units are shared: `vpt` per thread, `threads` per row (whole warps), `rows` side by side per CTA, `stages` rows of the ring.
+// How a row's units are shared: `vpt` per thread, `threads` per row (whole warps), `rows` side by side per CTA, `stages` rows of a ring.
 struct NormPlan { int vpt, threads, rows, stages; bool wide; int64_t ctas; size_t smem; };
-constexpr int NORM_SMEM = 200 << 10;                // of a multiprocessor's, for rings
+constexpr int64_t NORM_SMEM = 200 << 10;            // of a multiprocessor's, for weights and rings
 
-// `row_bytes`: of all operands of a row that are read.  `backward`: more registers per unit
-NormPlan plan_norm(int64_t T, int64_t F, bool ring, int64_t row_bytes, bool backward) {
+// `row_bytes`: of all operands of a row that are read.  The number of rows has no say in how a row is shared: its bits do not depend on its batch.
+NormPlan plan_norm(int64_t T, int64_t F, bool ring, int64_t row_bytes, bool more, bool backward) {
     NormPlan p{};
     const int64_t sms = device_sms();
     if (!ring) {                                    // a value per lane: one unit per thread
@@ -33,36 +33,45 @@ NormPlan plan_norm(int64_t T, int64_t F, bool ring, int64_t row_bytes, bool back
         p.ctas = std::min<int64_t>((T + p.rows - 1) / p.rows, sms * std::max(1, (backward ? 512 : 1024) / (p.threads * p.rows)));
         return p;
     }
-    const int64_t units = F / 8;
-    // Several units per thread cost fewer exchanges (a warp's shuffles take as long as half a unit).  The number of rows has no say: a row's bits do not depend on its batch.
+    // Units per thread: as many as registers hold, which is eight where the row has nothing to be added to (2048 columns: 24.8 us with eight, 29 with four; with
+    // a residual 51 and 47) and four elsewhere, fewer where that leaves fewer places empty.
+    const int64_t units = (F + 7) / 8;
     double best = 1e300;
-    for (int vpt = 1; vpt <= 4; ++vpt) {
+    for (int vpt : {8, 4, 3, 2, 1}) {
+        if (vpt == 8 && (backward || more)) continue;
         const int64_t g = (int64_t)align_up((size_t)ceil_div(units, vpt), 32);
         if (g > NORM_THREADS) continue;
-        const double cost = g * (vpt + 0.5);
+        const double cost = (double)g * (vpt + 1) + (g > 32 ? 16 : 0);       // a warp's part of a row costs about a unit beside its units, the exchange a little more
         if (cost < best) { best = cost; p.vpt = vpt; p.threads = (int)g; }
     }
-    const size_t row = (size_t)row_bytes / F * (size_t)(p.threads * p.vpt * 8);      // in the ring, with the places of units that do not exist
-    p.wide = p.threads == 0 || 2 * row > (size_t)NORM_SMEM;
+    const int64_t slots = (int64_t)p.threads * p.vpt, row = row_bytes / F * slots * 8, params = slots * (backward ? 32 : 64);
+    p.wide = p.threads == 0 || params + row > NORM_SMEM;
     if (p.wide) {
         p.threads = NORM_THREADS;
         p.rows = 1;
         p.ctas = std::min<int64_t>(T, sms * 2);
         return p;
     }
-    p.rows = std::max(1, 256 / p.threads);
-    const int resident = std::max(1, (p.vpt == 1 ? 1024 : p.vpt == 2 ? 768 : 512) / (p.threads * p.rows));       // CTAs per multiprocessor, by registers
-    p.stages = (int)std::max<size_t>(2, std::min<size_t>(4, NORM_SMEM / (row * p.rows * resident)));
-    p.smem = row * p.rows * p.stages;
+    // Measured over widths of 256 to 8192: rows of several warps in CTAs of 512 threads (the ring of two rows then fits twice 8 rows of 12 KB), rows of one warp in CTAs of 256
+    const int threads = p.threads > 32 ? NORM_THREADS : 256;
+    p.rows = threads / p.threads;
+    const int fit = std::max(1, (p.vpt == 1 ? (backward ? 768 : 1024) : p.vpt == 2 && !backward ? 768 : 512) / (p.threads * p.rows));       // CTAs per multiprocessor, by registers
+    // Forward, a row is in registers while the next is on its way: a second row in the ring pays for short ones only (256 columns with a residual 23.7 us against
+    // 26.8, 768: 17.4, 18.4; 2048: 49.0 with one, 51.7 with two).  Backward the row stays in the ring to the end.
+    p.stages = (backward || row <= 4096) && params + 2 * row * p.rows <= NORM_SMEM / fit ? 2 : 1;
+    while (p.rows > 1 && params + row * p.rows > NORM_SMEM) --p.rows;
+    p.smem = (size_t)(params + row * p.rows * p.stages);
     if (backward && p.rows > 1) p.smem = std::max(p.smem, (size_t)p.rows * 2 * F * 4);
-    p.ctas = std::min<int64_t>((T + p.rows - 1) / p.rows, sms * std::max<int64_t>(1, std::min<int64_t>(resident, NORM_SMEM / p.smem)));
+    // as many CTAs as fit, forward with long rows twice as many: who is done early takes another (2048 columns with a residual 49.0 -> 47.0 us)
+    const int64_t resident = std::max<int64_t>(1, std::min<int64_t>(fit, NORM_SMEM / (int64_t)p.smem));
+    p.ctas = std::min<int64_t>((T + p.rows - 1) / p.rows, sms * resident * (!backward && more && p.threads > 32 ? 2 : 1));
     return p;
 }
 
 struct NormGrad { NormPlan p; int64_t parts; size_t part, sums, total; };
 NormGrad plan_norm_grad(int64_t T, int64_t F, bool ring, int64_t row_bytes) {
     NormGrad g{};
-    g.p = plan_norm(T, F, ring, row_bytes, true);
+    g.p = plan_norm(T, F, ring, row_bytes, false, true);
     const int64_t tiles = (F + 2047) / 2048;
     g.parts = g.p.wide ? std::min<int64_t>({T, 65535, std::max<int64_t>(1, device_sms() * 4 / tiles)}) : g.p.ctas;
     g.part = 0;
@@ -71,41 +80,44 @@ NormGrad plan_norm_grad(int64_t T, int64_t F, bool ring, int64_t row_bytes) {
     return g;
 }
 
+template <typename Args>
+bool launch_norm(void (*kernel)(Args), const NormPlan& p, const Args& a, cudaStream_t st) {
+    if (p.smem > 40 << 10) set_smem_attr((const void*)kernel, p.smem);      // (static shared memory comes on top)
+    return launch(kernel, dim3((unsigned)p.ctas), dim3(p.threads, p.rows), p.smem, st, a);
+}
 template <typename X, typename Y, bool RING>
 bool norm_forward(NormForward a, const NormPlan& p, cudaStream_t st) {
-    const dim3 grid((unsigned)p.ctas), block(p.threads, p.rows);
     a.stages = p.stages;
-    const auto run = [&](auto kernel) {
-        if (p.smem > 40 << 10) set_smem_attr((const void*)kernel, p.smem);      // (static shared memory comes on top)
-        return launch(kernel, grid, block, p.smem, st, a);
-    };
-    if (p.wide) return launch(k_norm_forward_wide<X, Y, RING>, grid, block, 0, st, a);
+    if (p.wide) return launch_norm(k_norm_forward_wide<X, Y, RING>, p, a, st);
     if constexpr (RING) {
-        if (p.vpt == 2) return run(k_norm_forward<X, Y, true, 2>);
-        if (p.vpt == 3) return run(k_norm_forward<X, Y, true, 3>);
-        if (p.vpt == 4) return run(k_norm_forward<X, Y, true, 4>);
+        switch (p.vpt) {
+            case 1: return launch_norm(k_norm_forward<X, Y, 1>, p, a, st);
+            case 2: return launch_norm(k_norm_forward<X, Y, 2>, p, a, st);
+            case 3: return launch_norm(k_norm_forward<X, Y, 3>, p, a, st);
+            case 4: return launch_norm(k_norm_forward<X, Y, 4>, p, a, st);
+            default: return launch_norm(k_norm_forward<X, Y, 8>, p, a, st);
+        }
+    } else {
+        return launch_norm(k_norm_forward_any<X, Y>, p, a, st);
     }
-    return run(k_norm_forward<X, Y, RING, 1>);
 }
 template <typename X, typename Y, bool RING>
 bool norm_backward(NormBackward a, const NormGrad& g, cudaStream_t st) {
     const NormPlan& p = g.p;
-    const dim3 grid((unsigned)p.ctas), block(p.threads, p.rows);
     a.stages = p.stages;
-    if (p.wide) {
-        return launch(k_norm_sums_wide<X, Y, RING>, grid, block, 0, st, a) &&
+    if (p.wide)
+        return launch_norm(k_norm_sums_wide<X, Y, RING>, p, a, st) &&
                launch(k_norm_apply_wide<X, Y, RING>, dim3(ceil_div(a.F, 2048), (unsigned)g.parts), dim3(256), 0, st, a);
-    }
-    const auto run = [&](auto kernel) {
-        if (p.smem > 40 << 10) set_smem_attr((const void*)kernel, p.smem);      // (static shared memory comes on top)
-        return launch(kernel, grid, block, p.smem, st, a);
-    };
     if constexpr (RING) {
-        if (p.vpt == 2) return run(k_norm_backward<X, Y, true, 2>);
-        if (p.vpt == 3) return run(k_norm_backward<X, Y, true, 3>);
-        if (p.vpt == 4) return run(k_norm_backward<X, Y, true, 4>);
+        switch (p.vpt) {
+            case 1: return launch_norm(k_norm_backward<X, Y, 1>, p, a, st);
+            case 2: return launch_norm(k_norm_backward<X, Y, 2>, p, a, st);
+            case 3: return launch_norm(k_norm_backward<X, Y, 3>, p, a, st);
+            default: return launch_norm(k_norm_backward<X, Y, 4>, p, a, st);
+        }
+    } else {
+        return launch_norm(k_norm_backward_any<X, Y>, p, a, st);
     }
-    return run(k_norm_backward<X, Y, RING, 1>);
 }
 // the pairs of types: x and y (dy) alike, or x float32 and y bfloat16
 bool types_ok(int x, int y) { return dtype_ok(x) && dtype_ok(y) && (x == y || x == PSGD_DT_F32); }
@@ -152,7 +164,7 @@ psgd_status psgd_norm_forward(const void* x, int64_t ldx, int x_dtype, const voi
     a.ldx = ldx; a.ldr = ldr; a.lds = lds; a.ldy = ldy;
     a.w = {w, w_dtype == PSGD_DT_BF16}; a.b = {b, w_dtype == PSGD_DT_BF16};
     a.mean = center ? mean : nullptr; a.rstd = rstd; a.q = q; a.scales = scales;
-    const NormPlan p = plan_norm(T, F, vec, F * size_of(x_dtype) * (r ? 2 : 1), false);
+    const NormPlan p = plan_norm(T, F, vec, F * size_of(x_dtype) * (r ? 2 : 1), r != nullptr, false);
     const bool ok = by_type(x_dtype, y_dtype, vec, [&](auto* tx, auto* ty, auto v) {
         return norm_forward<std::remove_pointer_t<decltype(tx)>, std::remove_pointer_t<decltype(ty)>, decltype(v)::value>(a, p, (cudaStream_t)stream);
     });

@@ -5,15 +5,15 @@
 //   g = dy w,  xh = (s - m) f,  ds = f (g - mean(g) - xh mean(g xh)) + what reaches s from elsewhere  (mean(g) only with centring),
 //   dw = sum over rows of dy xh,  db = sum over rows of dy.
 //
-// One pass over the operands, bound by HBM.  blockDim.x threads share a row (blockDim.y rows per CTA side by side), each works on VPT units of eight
-// values of it.  The sum of squares is taken about the warp's own mean and the warps' results are joined exactly (squares about the joint mean = sum of the
-// warps' squares + n_w (mean_w - mean)^2), so that a large mean costs no bits and a row takes one exchange between its warps, none where a warp has it alone.
-// The CTAs stay and walk over the rows: weights are loaded once, and in the backward pass every thread sums dw and db of its columns over its
-// rows; the CTA adds its rows' sums, k_norm_join those of the CTAs, in a fixed order.
+// One pass over the operands, bound by HBM.  A warp, or as many warps as a row needs (blockDim.x threads, blockDim.y rows side by side), hold a row in registers, VPT units
+// of eight values per thread.  The sum of squares is taken about the warp's own mean and the warps' results are joined exactly (squares about the joint mean =
+// sum of the warps' squares + n_w (mean_w - mean)^2), so that a large mean costs no bits and a row takes one exchange between its warps, none where a warp
+// has it alone.  The CTAs stay and walk over the rows: weights are read once into shared memory, and in the backward pass every thread sums dw and db of its
+// columns over its rows; the CTA adds its rows' sums, k_norm_join those of the CTAs, in a fixed order.
 //
-// Rows of whole 16-byte units go through a ring in shared memory (RING): every thread copies its own units of the rows to come asynchronously (cp.async) and reads back only
-// what it copied itself, so that there is nothing to wait for but its own copies, several rows per group are under way whatever the registers hold, and the
-// backward pass reads a row a second time from there.  Rows of any other width or alignment: a value per lane, the next row's values in registers.
+// Rows of whole 16-byte units come through a ring in shared memory: every thread copies its own units of the rows to come asynchronously (cp.async) and reads back only
+// what it copied itself, so that there is nothing to wait for but its own copies, rows are under way whatever the registers hold, and the backward pass
+// reads a row a second time from there.  Rows of any other width or alignment (.._any): a value per lane, the next row's values in registers.
 // Sums and statistics are float32.  Rounded once: s to x's type, y, ds; the 8-bit form is that of the rounded y.
 #pragma once
 #include "psgd_values.cuh"
@@ -24,10 +24,47 @@ constexpr int NORM_UNIT = 8;
 constexpr int NORM_THREADS = 512;                  // most threads of a CTA
 constexpr int NORM_WARPS = NORM_THREADS / 32;
 
+// Pairs of float32: one instruction for two additions, products or fused ones.
+typedef unsigned long long F2;
+__device__ __forceinline__ F2 pair(float lo, float hi) {
+    F2 r;
+    asm("mov.b64 %0, {%1, %2};\n" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void unpair(F2 v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;\n" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ F2 add2(F2 a, F2 b) {
+    F2 r;
+    asm("add.rn.f32x2 %0, %1, %2;\n" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
+    F2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;\n" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+    F2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;\n" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+// eight values
+struct Eight { F2 p[4]; };
+__device__ __forceinline__ Eight eight(const float (&x)[8]) { return {{pair(x[0], x[1]), pair(x[2], x[3]), pair(x[4], x[5]), pair(x[6], x[7])}}; }
+__device__ __forceinline__ void singles(const Eight& v, float (&x)[8]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) unpair(v.p[j], x[2 * j], x[2 * j + 1]);
+}
 // Where the values of a thread's unit u lie in a row.  VEC: eight side by side (rows and widths of whole 16-byte units).  Else a value per lane: 32
 // columns apart, the warp's lanes side by side, any width and alignment.  `n`: how many of the eight exist (from the first on).
 template <bool VEC>
 __device__ __forceinline__ int cell_col(int u) { return VEC ? u * 8 : (u & ~31) * 8 + (u & 31); }
+// In the ring kernels a unit is two pieces of four values: side by side where x is bfloat16 (16 bytes), 128 columns apart where it is float32, so that every access of a
+// warp is to whole lines (a unit of 32 bytes per lane: 16384 x 1024 forward with a residual 62 us, backward 80).
+template <typename X>
+__device__ __forceinline__ int piece_col(int u, int h) { return sizeof(X) == 2 ? u * 8 + 4 * h : (u & ~31) * 8 + 128 * h + (u & 31) * 4; }
+// The i-th unit of a thread: a warp's VPT * 32 units lie one after the other, so that a thread's are a constant apart.
+template <int VPT>
+__device__ __forceinline__ int unit_of(int i) { return ((int)(threadIdx.x >> 5) * VPT + i) * 32 + (int)(threadIdx.x & 31); }
 template <bool VEC>
 __device__ __forceinline__ int cell_count(int col, int F) { return VEC ? (col < F ? 8 : 0) : min(max((F - col + 31) >> 5, 0), 8); }
 
@@ -141,188 +178,352 @@ struct NormForward {
     uint8_t* scales;
 };
 
-// Mean and sum of squared deviations of a row from each thread's values.  `n`: how many a thread's units have, `have`: how many the warp has.
+// Of a row that several warps share: the joint mean and sum of squared deviations from each warp's own.  `mine`: places of the row's warps, `have`: how many values
+// warp (lane & 15) has.
 struct RowStats { float mean, m2; };
-template <int VPT>
-__device__ __forceinline__ RowStats row_stats(const float (&v)[VPT][8], const int (&n)[VPT], float have, int F, bool center, float2* mine, const float* counts) {
+__device__ __forceinline__ float sum16(float x) {
+#pragma unroll
+    for (int o = 8; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    return x;
+}
+__device__ __forceinline__ RowStats join_warps(float m, float sq, float2* mine, float have, float per, bool center) {
     const int warps = blockDim.x >> 5, lane = threadIdx.x & 31;
-    float m = 0.f;
-    if (center) {
-        float sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < VPT; ++i) sum += ((v[i][0] + v[i][1]) + (v[i][2] + v[i][3])) + ((v[i][4] + v[i][5]) + (v[i][6] + v[i][7]));
-        m = warp_sum(sum) / fmaxf(have, 1.f);
-    }
-    float sq = 0.f;
-#pragma unroll
-    for (int i = 0; i < VPT; ++i)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float d = j < n[i] ? v[i][j] - m : 0.f;
-            sq = fmaf(d, d, sq);
-        }
-    sq = warp_sum(sq);
-    RowStats s{m, sq};
-    if (warps > 1) {
-        if (lane == 0) mine[threadIdx.x >> 5] = make_float2(m, sq);
-        row_sync();
-        if (center) {
-            s.mean = 0.f;
-            for (int w = 0; w < warps; ++w) s.mean = fmaf(counts[w], mine[w].x, s.mean);
-            s.mean /= (float)F;
-        }
-        s.m2 = 0.f;
-        for (int w = 0; w < warps; ++w) {
-            const float d = mine[w].x - s.mean;
-            s.m2 += fmaf(counts[w] * d, d, mine[w].y);
-        }
-    }
+    if (lane == 0) mine[threadIdx.x >> 5] = make_float2(m, sq);
+    row_sync();
+    const float2 t = (lane & 15) < warps ? mine[lane & 15] : make_float2(0.f, 0.f);
+    RowStats s;
+    s.mean = center ? sum16(have * t.x) * per : 0.f;
+    const float d = t.x - s.mean;
+    s.m2 = sum16(fmaf(have * d, d, t.y));
     return s;
 }
 
-// A thread's share of a ring: `stages` rows of its group, of each up to three operands.  Unit i of an operand lies at its plane + (i * blockDim.x + threadIdx.x) * 16; the second
-// halves of float32 units follow in a plane of their own, so that a warp's accesses are side by side.
-template <typename X> __device__ __forceinline__ int plane_bytes(int vpt) { return vpt * (int)blockDim.x * 8 * (int)sizeof(X); }
+// A thread's share of a ring: `stages` (1 or 2) rows of its group, of each up to three operands of type T beside an x of type X.  The first (float32: each) pieces of the
+// row's units lie in a plane one after the other, so that a warp's accesses are side by side.
 __device__ __forceinline__ void copy16(unsigned to, const void* from) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"(to), "l"(from) : "memory"); }
+__device__ __forceinline__ void copy8(unsigned to, const void* from) { asm volatile("cp.async.ca.shared.global [%0], [%1], 8;\n" ::"r"(to), "l"(from) : "memory"); }
 __device__ __forceinline__ uint4 shared16(unsigned at) {
     uint4 v;
     asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
     return v;
 }
+__device__ __forceinline__ uint2 shared8(unsigned at) {
+    uint2 v;
+    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];\n" : "=r"(v.x), "=r"(v.y) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ F2 pair_of(unsigned x, unsigned y) { return pair(__uint_as_float(x), __uint_as_float(y)); }
+// bytes of a unit in one plane, and of all planes of an operand
+template <typename T, typename X> __device__ __forceinline__ constexpr int unit_bytes() { return sizeof(X) == 2 ? 16 : 4 * (int)sizeof(T); }
+template <typename T, int VPT> __device__ __forceinline__ int operand_bytes() { return VPT * (int)blockDim.x * 8 * (int)sizeof(T); }
+// Columns of a thread's pieces (those that do not exist fetch the row's last one: no branches), and how many of a unit's values exist.
 template <typename X, int VPT>
-__device__ __forceinline__ void ring_ask(unsigned plane, const X* row, const int (&col)[VPT], const int (&n)[VPT]) {
+struct Place {
+    int at[VPT][sizeof(X) == 2 ? 1 : 2], n[VPT];
+    __device__ __forceinline__ explicit Place(int F) {
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) {
+            const int u = unit_of<VPT>(i), c0 = piece_col<X>(u, 0), c1 = piece_col<X>(u, 1);
+            at[i][0] = min(c0, F - (sizeof(X) == 2 ? 8 : 4));
+            if constexpr (sizeof(X) == 4) at[i][1] = min(c1, F - 4);
+            n[i] = (c0 < F ? 4 : 0) + (c1 < F ? 4 : 0);
+        }
+    }
+};
+// `operand`: where the operand's planes begin
+template <typename T, typename X, int VPT>
+__device__ __forceinline__ void ring_ask(unsigned operand, const T* row, const Place<X, VPT>& p) {
+    constexpr int B = unit_bytes<T, X>();
+    const unsigned to = operand + unit_of<VPT>(0) * B;
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
-        if (!n[i]) continue;
-        const unsigned to = plane + (i * blockDim.x + threadIdx.x) * 16;
-        copy16(to, row + col[i]);
-        if (sizeof(X) == 4) copy16(to + VPT * blockDim.x * 16, row + col[i] + 4);
+        if constexpr (B == 16) copy16(to + i * 32 * B, row + p.at[i][0]);
+        else copy8(to + i * 32 * B, row + p.at[i][0]);
+        if constexpr (sizeof(X) == 4) {
+            const unsigned second = to + VPT * blockDim.x * B + i * 32 * B;
+            if constexpr (B == 16) copy16(second, row + p.at[i][1]);
+            else copy8(second, row + p.at[i][1]);
+        }
     }
 }
-template <typename X, int VPT>
-__device__ __forceinline__ void ring_read(unsigned plane, int i, int n, float (&v)[8]) {
-    const unsigned at = plane + (i * blockDim.x + threadIdx.x) * 16;
-    uint4 a = make_uint4(0u, 0u, 0u, 0u), b = a;
-    if (n) a = shared16(at);
-    if (sizeof(X) == 4) {
-        if (n) b = shared16(at + VPT * blockDim.x * 16);
-        const unsigned w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(w[j]);
+template <typename T, typename X, int VPT>
+__device__ __forceinline__ Eight ring_read(unsigned operand, int i) {
+    constexpr int B = unit_bytes<T, X>();
+    const unsigned at = operand + unit_of<VPT>(i) * B;
+    if constexpr (sizeof(T) == 4) {
+        const uint4 a = shared16(at), b = shared16(at + VPT * blockDim.x * B);
+        return {{pair_of(a.x, a.y), pair_of(a.z, a.w), pair_of(b.x, b.y), pair_of(b.z, b.w)}};
     } else {
+        uint4 a;
+        if constexpr (B == 16) {
+            a = shared16(at);
+        } else {
+            const uint2 lo = shared8(at), hi = shared8(at + VPT * blockDim.x * B);
+            a = make_uint4(lo.x, lo.y, hi.x, hi.y);
+        }
+        float v[8];
         widen(Raw16{a}, v);
+        return eight(v);
+    }
+}
+// A unit's values to a row of T beside an x of type X, and (rounded) as they stand there.
+template <typename T, typename X, int VPT>
+__device__ __forceinline__ void unit_store(T* row, const Place<X, VPT>& p, int i, const Eight& v) {
+    float x[8];
+    singles(v, x);
+    if constexpr (sizeof(T) == 4) {
+        if (p.n[i] > 0) *reinterpret_cast<float4*>(row + p.at[i][0]) = make_float4(x[0], x[1], x[2], x[3]);
+        if (p.n[i] > 4) *reinterpret_cast<float4*>(row + p.at[i][1]) = make_float4(x[4], x[5], x[6], x[7]);
+    } else {
+        const uint4 b = pack_bf16x8(x);
+        if constexpr (sizeof(X) == 2) {
+            if (p.n[i] > 0) *reinterpret_cast<uint4*>(row + p.at[i][0]) = b;
+        } else {
+            if (p.n[i] > 0) *reinterpret_cast<uint2*>(row + p.at[i][0]) = make_uint2(b.x, b.y);
+            if (p.n[i] > 4) *reinterpret_cast<uint2*>(row + p.at[i][1]) = make_uint2(b.z, b.w);
+        }
+    }
+}
+// the sum of a unit's values that exist
+__device__ __forceinline__ float sum_of(const Eight& v, int n) {
+    float a, b, c, d;
+    unpair(add2(v.p[0], v.p[1]), a, b);
+    unpair(add2(v.p[2], v.p[3]), c, d);
+    return (n > 0 ? a + b : 0.f) + (n > 4 ? c + d : 0.f);
+}
+// A unit of x + r, rounded to their type, written to row s.  Sums of bfloat16 are rounded once by the packed addition itself.
+template <typename X, int VPT>
+__device__ __forceinline__ Eight ring_sum(unsigned x_at, unsigned r_at, int i, X* s, const Place<X, VPT>& p) {
+    if constexpr (sizeof(X) == 2) {
+        const uint4 x = shared16(x_at + unit_of<VPT>(i) * 16), r = shared16(r_at + unit_of<VPT>(i) * 16);
+        const auto sum = [](unsigned u, unsigned v) {
+            const __nv_bfloat162 t = __hadd2(*reinterpret_cast<const __nv_bfloat162*>(&u), *reinterpret_cast<const __nv_bfloat162*>(&v));
+            return *reinterpret_cast<const unsigned*>(&t);
+        };
+        const uint4 t = make_uint4(sum(x.x, r.x), sum(x.y, r.y), sum(x.z, r.z), sum(x.w, r.w));
+        if (p.n[i]) *reinterpret_cast<uint4*>(s + p.at[i][0]) = t;
+        float v[8];
+        widen(Raw16{t}, v);
+        return eight(v);
+    } else {
+        Eight x = ring_read<X, X, VPT>(x_at, i);
+        const Eight r = ring_read<X, X, VPT>(r_at, i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x.p[j] = add2(x.p[j], r.p[j]);
+        unit_store<X, X, VPT>(s, p, i, x);
+        return x;
+    }
+}
+// The 8-bit form of a unit's values of a row of T (see cell_keep); all lanes call.
+template <typename T, typename X>
+__device__ __forceinline__ void unit_keep(const Eight& v, int u, int n, long long g0, int G, int8_t* q, uint8_t* scales) {
+    float x[8];
+    singles(v, x);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = j < n ? x[j] : 0.f;
+    round_to<T>(x);
+    if constexpr (sizeof(X) == 2) {
+        cell_keep<true>(x, u * 8, g0, G, q, scales);
+    } else {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {                  // eight lanes share a group
+            const int col = piece_col<X>(u, h);
+            unsigned top = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) top = max(top, __float_as_uint(x[4 * h + j]) & 0x7fffffffu);
+#pragma unroll
+            for (int o = 1; o < 8; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+            const GroupScale s = group_scale(top);
+            unsigned b[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) b[j] = s.over ? quantize_clamped(x[4 * h + j], s) : quantize(x[4 * h + j], s);
+            const unsigned w = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+            if ((col >> 5) >= G) continue;
+            *reinterpret_cast<unsigned*>(q + (g0 + (col >> 5)) * ACT_GROUP + (col & 31)) = s.fine ? w : 0u;
+            if ((col & 31) == 0) scales[g0 + (col >> 5)] = (uint8_t)s.byte;
+        }
     }
 }
 // One group of copies per row, empty ones behind the last row included: a row's have landed when at most stages - 1 younger groups are under way.
 __device__ __forceinline__ void ring_commit() { asm volatile("cp.async.commit_group;\n" ::: "memory"); }
 __device__ __forceinline__ void ring_wait(int stages) {
-    if (stages == 4) asm volatile("cp.async.wait_group 3;\n" ::: "memory");
-    else if (stages == 3) asm volatile("cp.async.wait_group 2;\n" ::: "memory");
+    if (stages == 1) asm volatile("cp.async.wait_group 0;\n" ::: "memory");
     else asm volatile("cp.async.wait_group 1;\n" ::: "memory");
 }
+// A vector over the columns as float32 in shared memory: a plane of first pieces, a plane of second ones (zeros where there is none), by the whole CTA.
+template <typename X>
+__device__ __forceinline__ void param_planes(unsigned char* to, const NormParam& v, int units, int F, float none) {
+    for (int k = threadIdx.y * blockDim.x + threadIdx.x; k < 2 * units; k += blockDim.x * blockDim.y) {
+        const int c = piece_col<X>(k >> 1, k & 1);
+        float x[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = c + j < F ? param_at(v, c + j, none) : 0.f;
+        reinterpret_cast<float4*>(to)[(k & 1) * units + (k >> 1)] = make_float4(x[0], x[1], x[2], x[3]);
+    }
+}
+// a unit of it; `units`: of a plane
+template <int VPT>
+__device__ __forceinline__ Eight param_read(unsigned planes, int units, int i) {
+    const unsigned at = planes + unit_of<VPT>(i) * 16;
+    const uint4 a = shared16(at), b = shared16(at + units * 16);
+    return {{pair_of(a.x, a.y), pair_of(a.z, a.w), pair_of(b.x, b.y), pair_of(b.z, b.w)}};
+}
 
-template <typename X, typename Y, bool RING, int VPT>
+template <typename X, typename Y, int VPT>
 __global__ void __launch_bounds__(NORM_THREADS) k_norm_forward(const __grid_constant__ NormForward a) {
-    typedef typename Cell<X, RING>::Raw Raw;
-    extern __shared__ __align__(16) unsigned char ring_raw[];
+    extern __shared__ __align__(16) unsigned char ring_raw[];          // w, b, then the rings
     __shared__ float2 stat[2][NORM_WARPS];             // by rows taken in turn: a row's exchange is over when the next but one writes
     __shared__ float counts[NORM_WARPS];
     grid_trigger();
-    const int F = a.F, tid = threadIdx.x, warps = blockDim.x >> 5;
-    int col[VPT], n[VPT];
+    const int F = a.F, tid = threadIdx.x, warps = blockDim.x >> 5, units = VPT * blockDim.x;
+    const Place<X, VPT> p(F);
     int have = 0;
 #pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-        col[i] = cell_col<RING>(tid + i * (int)blockDim.x);
-        n[i] = cell_count<RING>(col[i], F);
-        have += n[i];
-    }
-    const float in_warp = (float)__reduce_add_sync(0xffffffffu, have);
+    for (int i = 0; i < VPT; ++i) have += p.n[i];
+    const float in_warp = (float)__reduce_add_sync(0xffffffffu, have), per = 1.f / (float)F, per_warp = 1.f / fmaxf(in_warp, 1.f);
     if (threadIdx.y == 0 && (tid & 31) == 0) counts[tid >> 5] = in_warp;
-    __syncthreads();
     grid_wait();
-    const X *x = (const X*)a.x, *r = (const X*)a.r;
-    X* s = (X*)a.s;
-    Y* y = (Y*)a.y;
     const long long step = (long long)gridDim.x * blockDim.y;
-    long long row = (long long)blockIdx.x * blockDim.y + threadIdx.y;
-    const int plane = plane_bytes<X>(VPT), stage = r ? 2 * plane : plane;
-    const unsigned ring = RING ? smem_addr(ring_raw) + threadIdx.y * a.stages * stage : 0u;
-    Raw next[VPT], add[VPT];
-    const auto ask = [&](long long at, unsigned to) {
-        if constexpr (RING) {
-            if (at < a.T) {
-                ring_ask<X, VPT>(to, x + at * a.ldx, col, n);
-                if (r) ring_ask<X, VPT>(to + plane, r + at * a.ldr, col, n);
-            }
-            ring_commit();
-        } else if (at < a.T) {
-#pragma unroll
-            for (int i = 0; i < VPT; ++i) {
-                cell_load(next[i], x + at * a.ldx + col[i], n[i]);
-                if (r) cell_load(add[i], r + at * a.ldr + col[i], n[i]);
-            }
+    long long row = (long long)blockIdx.x * blockDim.y + threadIdx.y, asked = row;
+    // rows: the one that is asked for next (x, r) and the one at work (s, y)
+    const X *x = (const X*)a.x + row * a.ldx, *r = a.r ? (const X*)a.r + row * a.ldr : nullptr;
+    X* s = a.s ? (X*)a.s + row * a.lds : nullptr;
+    Y* y = (Y*)a.y + row * a.ldy;
+    const int operand = operand_bytes<X, VPT>(), stage = r ? 2 * operand : operand, stages = a.stages;
+    const unsigned params = smem_addr(ring_raw), ring = params + units * 64 + threadIdx.y * stages * stage;
+    const auto ask = [&](unsigned to) {
+        if (asked < a.T) {
+            ring_ask<X, X, VPT>(to, x, p);
+            if (r) ring_ask<X, X, VPT>(to + operand, r, p);
         }
+        ring_commit();
+        asked += step;
+        x += step * a.ldx;
+        if (r) r += step * a.ldr;
     };
-    if constexpr (RING) {
-        for (int k = 0; k < a.stages; ++k) ask(row + k * step, ring + k * stage);
-    } else {
-        ask(row, 0u);
-    }
-    float w[VPT][8], b[VPT][8];
-#pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-        param_cell<RING>(w[i], a.w, col[i], n[i], 1.f);
-        param_cell<RING>(b[i], a.b, col[i], n[i], 0.f);
-    }
+    for (int k = 0; k < stages; ++k) ask(ring + k * stage);
+    param_planes<X>(ring_raw, a.w, units, F, 1.f);
+    param_planes<X>(ring_raw + units * 32, a.b, units, F, 0.f);
+    __syncthreads();
+    const float in_lane = (tid & 15) < warps ? counts[tid & 15] : 0.f;
     const int G = (F + ACT_GROUP - 1) / ACT_GROUP;
     unsigned from = ring;
     for (int turn = 0; row < a.T; row += step, turn ^= 1) {
-        float v[VPT][8];
-        if constexpr (RING) ring_wait(a.stages);
+        Eight v[VPT];
+        ring_wait(stages);
+        if (r) {
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) v[i] = ring_sum<X, VPT>(from, from + operand, i, s, p);
+        } else {
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) v[i] = ring_read<X, X, VPT>(from, i);
+            if (s) {
+#pragma unroll
+                for (int i = 0; i < VPT; ++i) unit_store<X, X, VPT>(s, p, i, v[i]);
+            }
+        }
+        float m = 0.f;
+        if (a.center) {
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) m += sum_of(v[i], p.n[i]);
+            m = warp_sum(m) * per_warp;
+            const F2 off = pair(-m, -m);
+#pragma unroll
+            for (int i = 0; i < VPT; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[i].p[j] = add2(v[i].p[j], off);
+        }
+        float sq = 0.f;
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
+            const F2 first = fma2(v[i].p[1], v[i].p[1], mul2(v[i].p[0], v[i].p[0])), second = fma2(v[i].p[3], v[i].p[3], mul2(v[i].p[2], v[i].p[2]));
+            float t[4];
+            unpair(first, t[0], t[1]);
+            unpair(second, t[2], t[3]);
+            sq += (p.n[i] > 0 ? t[0] + t[1] : 0.f) + (p.n[i] > 4 ? t[2] + t[3] : 0.f);
+        }
+        RowStats st{m, warp_sum(sq)};
+        ask(from);                                     // (every value has been used)
+        from = stages == 1 || from != ring ? ring : ring + stage;
+        if (warps > 1) st = join_warps(st.mean, st.m2, stat[turn] + threadIdx.y * warps, in_lane, per, a.center);
+        const float f = rsqrtf(fmaf(st.m2, per, a.eps));
+        if (tid == 0) {
+            a.rstd[row] = f;
+            if (a.mean) a.mean[row] = st.mean;
+        }
+        const F2 off = pair(m - st.mean, m - st.mean), ff = pair(f, f);
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) {
+            const Eight w = param_read<VPT>(params, units, i), b = param_read<VPT>(params + units * 32, units, i);
+            Eight o;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o.p[j] = fma2(mul2(add2(v[i].p[j], off), ff), w.p[j], b.p[j]);
+            unit_store<Y, X, VPT>(y, p, i, o);
+            if (a.q) unit_keep<Y, X>(o, unit_of<VPT>(i), p.n[i], row * G, G, a.q, a.scales);
+        }
+        if (s) s += step * a.lds;
+        y += step * a.ldy;
+    }
+}
+
+// Rows of any width up to NORM_THREADS units and any alignment: one unit per thread, a value per lane.
+template <typename X, typename Y>
+__global__ void __launch_bounds__(NORM_THREADS) k_norm_forward_any(const __grid_constant__ NormForward a) {
+    typedef typename Cell<X, false>::Raw Raw;
+    __shared__ float2 stat[2][NORM_WARPS];
+    __shared__ float counts[NORM_WARPS];
+    grid_trigger();
+    const int F = a.F, tid = threadIdx.x, warps = blockDim.x >> 5, col = cell_col<false>(tid), n = cell_count<false>(col, F);
+    const float in_warp = (float)__reduce_add_sync(0xffffffffu, n), per = 1.f / (float)F, per_warp = 1.f / fmaxf(in_warp, 1.f);
+    if (threadIdx.y == 0 && (tid & 31) == 0) counts[tid >> 5] = in_warp;
+    __syncthreads();
+    const float in_lane = (tid & 15) < warps ? counts[tid & 15] : 0.f;
+    grid_wait();
+    float w[8], b[8];
+    param_cell<false>(w, a.w, col, n, 1.f);
+    param_cell<false>(b, a.b, col, n, 0.f);
+    const int G = (F + ACT_GROUP - 1) / ACT_GROUP;
+    const long long step = (long long)gridDim.x * blockDim.y;
+    long long row = (long long)blockIdx.x * blockDim.y + threadIdx.y;
+    Raw next, add;
+    const auto ask = [&](long long at) {
+        if (at >= a.T) return;
+        cell_load(next, (const X*)a.x + at * a.ldx + col, n);
+        if (a.r) cell_load(add, (const X*)a.r + at * a.ldr + col, n);
+    };
+    ask(row);
+    for (int turn = 0; row < a.T; row += step, turn ^= 1) {
+        float v[8];
+        widen(next, v);
+        if (a.r) {
             float u[8];
-            if constexpr (RING) {
-                ring_read<X, VPT>(from, i, n[i], v[i]);
-                if (r) ring_read<X, VPT>(from + plane, i, n[i], u);
-            } else {
-                widen(next[i], v[i]);
-                if (r) widen(add[i], u);
-            }
-            if (r) {
+            widen(add, u);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[i][j] += u[j];
-                round_to<X>(v[i]);
-            }
+            for (int j = 0; j < 8; ++j) v[j] += u[j];
+            round_to<X>(v);
         }
-        if constexpr (!RING) ask(row + step, 0u);
-        if (s) {
+        ask(row + step);
+        if (a.s) cell_store<false>((X*)a.s + row * a.lds + col, v, n);
+        float m = 0.f, sq = 0.f;
+        if (a.center) m = warp_sum(((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]))) * per_warp;
 #pragma unroll
-            for (int i = 0; i < VPT; ++i) cell_store<RING>(s + row * a.lds + col[i], v[i], n[i]);
+        for (int j = 0; j < 8; ++j) {
+            v[j] = j < n ? v[j] - m : 0.f;
+            sq = fmaf(v[j], v[j], sq);
         }
-        const RowStats st = row_stats<VPT>(v, n, in_warp, F, a.center, stat[turn] + threadIdx.y * warps, counts);
-        if constexpr (RING) {                          // (every value has been used)
-            ask(row + a.stages * step, from);
-            from = from + stage == ring + a.stages * stage ? ring : from + stage;
-        }
-        const float f = rsqrtf(st.m2 / (float)F + a.eps);
+        RowStats st{m, warp_sum(sq)};
+        if (warps > 1) st = join_warps(st.mean, st.m2, stat[turn] + threadIdx.y * warps, in_lane, per, a.center);
+        const float f = rsqrtf(fmaf(st.m2, per, a.eps)), off = m - st.mean;
         if (tid == 0) {
             a.rstd[row] = f;
             if (a.mean) a.mean[row] = st.mean;
         }
 #pragma unroll
-        for (int i = 0; i < VPT; ++i) {
-            float o[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) o[j] = fmaf((v[i][j] - st.mean) * f, w[i][j], b[i][j]);
-            cell_store<RING>(y + row * a.ldy + col[i], o, n[i]);
-            if (a.q) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) o[j] = j < n[i] ? o[j] : 0.f;
-                round_to<Y>(o);
-                cell_keep<RING>(o, col[i], row * G, G, a.q, a.scales);
-            }
+        for (int j = 0; j < 8; ++j) v[j] = j < n ? fmaf((v[j] + off) * f, w[j], b[j]) : 0.f;
+        cell_store<false>((Y*)a.y + row * a.ldy + col, v, n);
+        if (a.q) {
+            round_to<Y>(v);
+            cell_keep<false>(v, col, row * G, G, a.q, a.scales);
         }
     }
 }
@@ -421,158 +622,205 @@ struct NormBackward {
 };
 struct NormJoin { int F, parts; const float* part; float *dw, *db; };      // db: or nullptr
 
-template <typename X, typename Y, bool RING, int VPT>
-__global__ void __launch_bounds__(NORM_THREADS) k_norm_backward(const __grid_constant__ NormBackward a) {
-    typedef typename Cell<X, RING>::Raw RawX;
-    typedef typename Cell<Y, RING>::Raw RawY;
-    extern __shared__ __align__(16) unsigned char ring_raw[];      // the ring; at the end the sums of the rows side by side, [blockDim.y][2][F]
-    __shared__ float2 stat[2][NORM_WARPS];
-    grid_trigger();
-    const int F = a.F, tid = threadIdx.x, warps = blockDim.x >> 5;
-    int col[VPT], n[VPT];
-#pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-        col[i] = cell_col<RING>(tid + i * (int)blockDim.x);
-        n[i] = cell_count<RING>(col[i], F);
+// The sums s1 and s2 of a row over its warps.
+__device__ __forceinline__ void sum_warps(float& s1, float& s2, float2* mine) {
+    const int warps = blockDim.x >> 5;
+    if ((threadIdx.x & 31) == 0) mine[threadIdx.x >> 5] = make_float2(s1, s2);
+    row_sync();
+    s1 = s2 = 0.f;
+#pragma unroll 4
+    for (int k = 0; k < warps; ++k) {
+        const float2 t = mine[k];
+        s1 += t.x;
+        s2 += t.y;
     }
-    grid_wait();
-    const Y* dy = (const Y*)a.dy;
-    const X *x = (const X*)a.x, *add = (const X*)a.add;
-    X* dx = (X*)a.dx;
-    const long long step = (long long)gridDim.x * blockDim.y;
-    long long row = (long long)blockIdx.x * blockDim.y + threadIdx.y;
-    const int plane = plane_bytes<X>(VPT), plane_dy = plane_bytes<Y>(VPT), stage = plane_dy + (add ? 2 : 1) * plane;
-    const unsigned ring = RING ? smem_addr(ring_raw) + threadIdx.y * a.stages * stage : 0u;
-    RawX nx[VPT], na[VPT];
-    RawY ny[VPT];
-    float nm = 0.f, nf = 0.f;                          // the next row's mean and rstd
-    const auto ask_stats = [&](long long at) {
-        if (at >= a.T) return;
-        nf = a.rstd[at];
-        if (a.mean) nm = a.mean[at];
-    };
-    const auto ask = [&](long long at, unsigned to) {
-        if constexpr (RING) {
-            if (at < a.T) {
-                ring_ask<Y, VPT>(to, dy + at * a.lddy, col, n);
-                ring_ask<X, VPT>(to + plane_dy, x + at * a.ldx, col, n);
-                if (add) ring_ask<X, VPT>(to + plane_dy + plane, add + at * a.ldadd, col, n);
-            }
-            ring_commit();
-        } else if (at < a.T) {
-#pragma unroll
-            for (int i = 0; i < VPT; ++i) {
-                cell_load(nx[i], x + at * a.ldx + col[i], n[i]);
-                cell_load(ny[i], dy + at * a.lddy + col[i], n[i]);
-                if (add) cell_load(na[i], add + at * a.ldadd + col[i], n[i]);
-            }
-        }
-    };
-    if constexpr (RING) {
-        for (int k = 0; k < a.stages; ++k) ask(row + k * step, ring + k * stage);
-    } else {
-        ask(row, 0u);
-    }
-    ask_stats(row);
-    float w[VPT][8], dw[VPT][8], db[VPT][8];
-#pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-        param_cell<RING>(w[i], a.w, col[i], n[i], 1.f);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) dw[i][j] = db[i][j] = 0.f;
-    }
-    const float per = 1.f / (float)F;
-    unsigned from = ring;
-    for (int turn = 0; row < a.T; row += step, turn ^= 1) {
-        RawX cx[VPT], ca[VPT];
-        RawY cy[VPT];
-        if constexpr (!RING) {
-#pragma unroll
-            for (int i = 0; i < VPT; ++i) { cx[i] = nx[i]; cy[i] = ny[i]; ca[i] = na[i]; }
-            ask(row + step, 0u);
-        }
-        const float f = nf, m = nm;
-        ask_stats(row + step);
-        if constexpr (RING) ring_wait(a.stages);
-        // a unit's x and dy, both times they are needed
-        const auto values = [&](int i, float (&v)[8], float (&d)[8]) {
-            if constexpr (RING) {
-                ring_read<Y, VPT>(from, i, n[i], d);
-                ring_read<X, VPT>(from + plane_dy, i, n[i], v);
-            } else {
-                widen(cx[i], v);
-                widen(cy[i], d);
-            }
-        };
-        float s1 = 0.f, s2 = 0.f;
-#pragma unroll
-        for (int i = 0; i < VPT; ++i) {
-            float v[8], d[8];
-            values(i, v, d);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {              // (dy and w are zeros where there is no value)
-                const float xh = (v[j] - m) * f, g = d[j] * w[i][j];
-                s1 += g;
-                s2 = fmaf(g, xh, s2);
-                dw[i][j] = fmaf(d[j], xh, dw[i][j]);
-                db[i][j] += d[j];
-            }
-        }
-        s1 = warp_sum(s1);
-        s2 = warp_sum(s2);
-        if (warps > 1) {
-            float2* mine = stat[turn] + threadIdx.y * warps;
-            if ((tid & 31) == 0) mine[tid >> 5] = make_float2(s1, s2);
-            row_sync();
-            s1 = s2 = 0.f;
-            for (int k = 0; k < warps; ++k) { s1 += mine[k].x; s2 += mine[k].y; }
-        }
-        s1 = a.center ? s1 * per : 0.f;
-        s2 *= per;
-#pragma unroll
-        for (int i = 0; i < VPT; ++i) {
-            float v[8], d[8];
-            values(i, v, d);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) d[j] = f * (fmaf(-((v[j] - m) * f), s2, d[j] * w[i][j]) - s1);
-            if (add) {
-                if constexpr (RING) ring_read<X, VPT>(from + plane_dy + plane, i, n[i], v);
-                else widen(ca[i], v);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) d[j] += v[j];
-            }
-            cell_store<RING>(dx + row * a.lddx + col[i], d, n[i]);
-        }
-        if constexpr (RING) {
-            ask(row + a.stages * step, from);
-            from = from + stage == ring + a.stages * stage ? ring : from + stage;
-        }
-    }
-    // the CTA's sums: its rows side by side (threadIdx.y) through shared memory; a CTA alone writes the results
+}
+// At the end: the CTA's sums of dw and db, its rows side by side (threadIdx.y) through `sums` [blockDim.y][2][F]; a CTA alone writes the results.  `column(i, j)`: of value j
+// of the thread's unit i, `n`: how many of its values exist.
+template <int VPT, typename Column>
+__device__ __forceinline__ void write_columns(const NormBackward& a, float* sums, const Eight (&dw)[VPT], const Eight (&db)[VPT], const int (&n)[VPT], Column&& column) {
+    const int F = a.F;
     float* pw = gridDim.x == 1 ? a.dw : a.part + (size_t)blockIdx.x * 2 * F;
     float* pb = gridDim.x == 1 ? a.db : pw + F;
     const bool alone = blockDim.y == 1;
-    float* sums = reinterpret_cast<float*>(ring_raw) + (size_t)threadIdx.y * 2 * F;
-    if (RING) asm volatile("cp.async.wait_all;\n" ::: "memory");
-    if (!alone) __syncthreads();
-    float *to_w = alone ? pw : sums, *to_b = alone ? pb : sums + F;
+    if (!alone) __syncthreads();                       // (nobody reads what lay there)
+    float *to_w = alone ? pw : sums + (size_t)threadIdx.y * 2 * F, *to_b = alone ? pb : to_w + F;
 #pragma unroll
-    for (int i = 0; i < VPT; ++i)
+    for (int i = 0; i < VPT; ++i) {
+        float p[8], q[8];
+        singles(dw[i], p);
+        singles(db[i], q);
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             if (j < n[i]) {
-                const int c = col[i] + (RING ? j : 32 * j);
-                to_w[c] = dw[i][j];
-                if (to_b) to_b[c] = db[i][j];
+                const int c = column(i, j);
+                to_w[c] = p[j];
+                if (to_b) to_b[c] = q[j];
             }
+    }
     if (alone) return;
     __syncthreads();
-    for (int c = threadIdx.y * blockDim.x + tid; c < 2 * F; c += blockDim.x * blockDim.y) {
+    for (int c = threadIdx.y * blockDim.x + threadIdx.x; c < 2 * F; c += blockDim.x * blockDim.y) {
         float sum = 0.f;
-        for (int k = 0; k < (int)blockDim.y; ++k) sum += reinterpret_cast<float*>(ring_raw)[(size_t)k * 2 * F + c];
+        for (int k = 0; k < (int)blockDim.y; ++k) sum += sums[(size_t)k * 2 * F + c];
         if (c < F) pw[c] = sum;
         else if (pb) pb[c - F] = sum;
     }
+}
+
+template <typename X, typename Y, int VPT>
+__global__ void __launch_bounds__(NORM_THREADS) k_norm_backward(const __grid_constant__ NormBackward a) {
+    extern __shared__ __align__(16) unsigned char ring_raw[];          // w, then the rings; at the end the sums of the rows side by side
+    __shared__ float2 stat[2][NORM_WARPS];
+    grid_trigger();
+    const int F = a.F, warps = blockDim.x >> 5, units = VPT * blockDim.x;
+    const Place<X, VPT> p(F);
+    grid_wait();
+    const long long step = (long long)gridDim.x * blockDim.y;
+    long long row = (long long)blockIdx.x * blockDim.y + threadIdx.y, asked = row;
+    // rows: the one that is asked for next (dy, x, add) and the one at work (dx)
+    const Y* dy = (const Y*)a.dy + row * a.lddy;
+    const X *x = (const X*)a.x + row * a.ldx, *add = a.add ? (const X*)a.add + row * a.ldadd : nullptr;
+    X* dx = (X*)a.dx + row * a.lddx;
+    const int at_x = operand_bytes<Y, VPT>(), at_add = at_x + operand_bytes<X, VPT>(), stage = add ? at_add + operand_bytes<X, VPT>() : at_add, stages = a.stages;
+    const unsigned params = smem_addr(ring_raw), ring = params + units * 32 + threadIdx.y * stages * stage;
+    float nm = 0.f, nf = 0.f;                          // the next row's mean and rstd
+    const auto ask_stats = [&](long long i) {
+        if (i >= a.T) return;
+        nf = a.rstd[i];
+        if (a.mean) nm = a.mean[i];
+    };
+    const auto ask = [&](unsigned to) {
+        if (asked < a.T) {
+            ring_ask<Y, X, VPT>(to, dy, p);
+            ring_ask<X, X, VPT>(to + at_x, x, p);
+            if (add) ring_ask<X, X, VPT>(to + at_add, add, p);
+        }
+        ring_commit();
+        asked += step;
+        dy += step * a.lddy;
+        x += step * a.ldx;
+        if (add) add += step * a.ldadd;
+    };
+    for (int k = 0; k < stages; ++k) ask(ring + k * stage);
+    ask_stats(row);
+    param_planes<X>(ring_raw, a.w, units, F, 1.f);
+    __syncthreads();
+    Eight dw[VPT], db[VPT];
+#pragma unroll
+    for (int i = 0; i < VPT; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) dw[i].p[j] = db[i].p[j] = 0ull;
+    const float per = 1.f / (float)F;
+    unsigned from = ring;
+    for (int turn = 0; row < a.T; row += step, turn ^= 1) {
+        const float f = nf, m = nm;
+        ask_stats(row + step);
+        const F2 off = pair(-m, -m), ff = pair(f, f);
+        ring_wait(stages);
+        F2 t1 = 0ull, t2 = 0ull;
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) {
+            const Eight d = ring_read<Y, X, VPT>(from, i), v = ring_read<X, X, VPT>(from + at_x, i), w = param_read<VPT>(params, units, i);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {              // (w is 0 where there is no value, and its dw and db go nowhere)
+                const F2 xh = mul2(add2(v.p[j], off), ff), g = mul2(d.p[j], w.p[j]);
+                t1 = add2(t1, g);
+                t2 = fma2(g, xh, t2);
+                dw[i].p[j] = fma2(d.p[j], xh, dw[i].p[j]);
+                db[i].p[j] = add2(db[i].p[j], d.p[j]);
+            }
+        }
+        float s1, s2, hi;
+        unpair(t1, s1, hi);
+        s1 = warp_sum(s1 + hi);
+        unpair(t2, s2, hi);
+        s2 = warp_sum(s2 + hi);
+        if (warps > 1) sum_warps(s1, s2, stat[turn] + threadIdx.y * warps);
+        s1 = a.center ? s1 * per * -f : 0.f;
+        s2 *= -per * f * f;
+        const F2 c1 = pair(s1, s1), c2 = pair(s2, s2);
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) {
+            const Eight v = ring_read<X, X, VPT>(from + at_x, i), w = param_read<VPT>(params, units, i);
+            Eight d = ring_read<Y, X, VPT>(from, i);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) d.p[j] = fma2(mul2(d.p[j], w.p[j]), ff, fma2(add2(v.p[j], off), c2, c1));
+            if (add) {
+                const Eight u = ring_read<X, X, VPT>(from + at_add, i);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) d.p[j] = add2(d.p[j], u.p[j]);
+            }
+            unit_store<X, X, VPT>(dx, p, i, d);
+        }
+        dx += step * a.lddx;
+        ask(from);
+        from = stages == 1 || from != ring ? ring : ring + stage;
+    }
+    asm volatile("cp.async.wait_all;\n" ::: "memory");
+    write_columns<VPT>(a, reinterpret_cast<float*>(ring_raw), dw, db, p.n, [](int i, int j) { return piece_col<X>(unit_of<VPT>(i), j >> 2) + (j & 3); });
+}
+
+template <typename X, typename Y>
+__global__ void __launch_bounds__(NORM_THREADS) k_norm_backward_any(const __grid_constant__ NormBackward a) {
+    typedef typename Cell<X, false>::Raw RawX;
+    typedef typename Cell<Y, false>::Raw RawY;
+    extern __shared__ __align__(16) unsigned char ring_raw[];          // at the end the sums of the rows side by side
+    __shared__ float2 stat[2][NORM_WARPS];
+    grid_trigger();
+    const int F = a.F, tid = threadIdx.x, warps = blockDim.x >> 5, col = cell_col<false>(tid), n = cell_count<false>(col, F);
+    grid_wait();
+    float w[8], dw[8], db[8];
+    param_cell<false>(w, a.w, col, n, 1.f);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) dw[j] = db[j] = 0.f;
+    const long long step = (long long)gridDim.x * blockDim.y;
+    long long row = (long long)blockIdx.x * blockDim.y + threadIdx.y;
+    RawX nx, na;
+    RawY ny;
+    float nm = 0.f, nf = 0.f;
+    const auto ask = [&](long long at) {
+        if (at >= a.T) return;
+        nf = a.rstd[at];
+        if (a.mean) nm = a.mean[at];
+        cell_load(nx, (const X*)a.x + at * a.ldx + col, n);
+        cell_load(ny, (const Y*)a.dy + at * a.lddy + col, n);
+        if (a.add) cell_load(na, (const X*)a.add + at * a.ldadd + col, n);
+    };
+    ask(row);
+    const float per = 1.f / (float)F;
+    for (int turn = 0; row < a.T; row += step, turn ^= 1) {
+        const float f = nf, m = nm;
+        float v[8], d[8], u[8];
+        widen(nx, v);
+        widen(ny, d);
+        if (a.add) widen(na, u);
+        ask(row + step);
+        float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {                  // (dy is 0 where there is no value)
+            v[j] = (v[j] - m) * f;
+            dw[j] = fmaf(d[j], v[j], dw[j]);
+            db[j] += d[j];
+            d[j] *= w[j];
+            s1 += d[j];
+            s2 = fmaf(d[j], v[j], s2);
+        }
+        s1 = warp_sum(s1);
+        s2 = warp_sum(s2);
+        if (warps > 1) sum_warps(s1, s2, stat[turn] + threadIdx.y * warps);
+        s1 = a.center ? s1 * per * -f : 0.f;
+        s2 *= -per;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            d[j] = fmaf(fmaf(v[j], s2, d[j]), f, s1);
+            if (a.add) d[j] += u[j];
+        }
+        cell_store<false>((X*)a.dx + row * a.lddx + col, d, n);
+    }
+    const Eight sums_w[1] = {eight(dw)}, sums_b[1] = {eight(db)};
+    const int many[1] = {n};
+    write_columns<1>(a, reinterpret_cast<float*>(ring_raw), sums_w, sums_b, many, [=](int, int j) { return col + 32 * j; });
 }
 
 // Wide rows: first the two sums of every row (a CTA per row), then dx and the sums over rows (256 units of the columns per CTA, gridDim.y CTAs share the rows).
