@@ -15,15 +15,17 @@ bool whole_units(const void* p, int64_t ld, int64_t F, int dtype) { return !p ||
 bool rows_ok(int64_t T, int64_t F) { return T >= 0 && T <= MAX_EXTENT && extent_ok(F); }
 
 // ---- layer norm ----
+// How the rows go: RING (16-byte units), SHIFT (bfloat16 of any width and alignment through the ring, forward), LANES (anything else, a value per lane)
+enum NormRows { RING, SHIFT, LANES };
 // How a row's units are shared: `vpt` per thread, `threads` per row (whole warps), `rows` side by side per CTA, `stages` rows of a ring.
 struct NormPlan { int vpt, threads, rows, stages; bool wide; int64_t ctas; size_t smem; };
 constexpr int64_t NORM_SMEM = 200 << 10;            // of a multiprocessor's, for weights and rings
 
 // `row_bytes`: of all operands of a row that are read.  The number of rows has no say in how a row is shared: its bits do not depend on its batch.
-NormPlan plan_norm(int64_t T, int64_t F, bool ring, int64_t row_bytes, bool more, bool backward) {
+NormPlan plan_norm(int64_t T, int64_t F, NormRows rows, int64_t row_bytes, bool more, bool backward) {
     NormPlan p{};
     const int64_t sms = device_sms();
-    if (!ring) {                                    // a value per lane: one unit per thread
+    if (rows == LANES) {                                    // a value per lane: one unit per thread
         const int64_t units = (F + 255) / 256 * 32;
         p.wide = units > NORM_THREADS;
         p.vpt = 1;
@@ -38,13 +40,16 @@ NormPlan plan_norm(int64_t T, int64_t F, bool ring, int64_t row_bytes, bool more
     const int64_t units = (F + 7) / 8;
     double best = 1e300;
     for (int vpt : {8, 4, 3, 2, 1}) {
-        if (vpt == 8 && (backward || more)) continue;
+        if (vpt == 8 && (rows == SHIFT || backward || more)) continue;
         const int64_t g = (int64_t)align_up((size_t)ceil_div(units, vpt), 32);
         if (g > NORM_THREADS) continue;
         const double cost = (double)g * (vpt + 1) + (g > 32 ? 16 : 0);       // a warp's part of a row costs about a unit beside its units, the exchange a little more
         if (cost < best) { best = cost; p.vpt = vpt; p.threads = (int)g; }
     }
-    const int64_t slots = (int64_t)p.threads * p.vpt, row = row_bytes / F * slots * 8, params = slots * (backward ? 32 : 64);
+    const int64_t slots = (int64_t)p.threads * p.vpt, params = slots * (backward ? 32 : 64);
+    int64_t row = row_bytes / F * slots * 8;
+    const int64_t margin = rows == SHIFT ? p.threads / 32 * 48 : 0;          // a unit more per warp and operand, up to three operands
+    row += margin;
     p.wide = p.threads == 0 || params + row > NORM_SMEM;
     if (p.wide) {
         p.threads = NORM_THREADS;
@@ -69,9 +74,9 @@ NormPlan plan_norm(int64_t T, int64_t F, bool ring, int64_t row_bytes, bool more
 }
 
 struct NormGrad { NormPlan p; int64_t parts; size_t part, sums, total; };
-NormGrad plan_norm_grad(int64_t T, int64_t F, bool ring, int64_t row_bytes) {
+NormGrad plan_norm_grad(int64_t T, int64_t F, NormRows rows, int64_t row_bytes) {
     NormGrad g{};
-    g.p = plan_norm(T, F, ring, row_bytes, false, true);
+    g.p = plan_norm(T, F, rows, row_bytes, false, true);
     const int64_t tiles = (F + 2047) / 2048;
     g.parts = g.p.wide ? std::min<int64_t>({T, 65535, std::max<int64_t>(1, device_sms() * 4 / tiles)}) : g.p.ctas;
     g.part = 0;
@@ -82,51 +87,49 @@ NormGrad plan_norm_grad(int64_t T, int64_t F, bool ring, int64_t row_bytes) {
 
 template <typename Args>
 bool launch_norm(void (*kernel)(Args), const NormPlan& p, const Args& a, cudaStream_t st) {
-    if (p.smem > 40 << 10) set_smem_attr((const void*)kernel, p.smem);      // (static shared memory comes on top)
+    if (p.smem > 32 << 10) set_smem_attr((const void*)kernel, p.smem);      // (static shared memory comes on top)
     return launch(kernel, dim3((unsigned)p.ctas), dim3(p.threads, p.rows), p.smem, st, a);
 }
-template <typename X, typename Y, bool RING>
-bool norm_forward(NormForward a, const NormPlan& p, cudaStream_t st) {
-    a.stages = p.stages;
-    if (p.wide) return launch_norm(k_norm_forward_wide<X, Y, RING>, p, a, st);
-    if constexpr (RING) {
-        switch (p.vpt) {
-            case 1: return launch_norm(k_norm_forward<X, Y, 1>, p, a, st);
-            case 2: return launch_norm(k_norm_forward<X, Y, 2>, p, a, st);
-            case 3: return launch_norm(k_norm_forward<X, Y, 3>, p, a, st);
-            case 4: return launch_norm(k_norm_forward<X, Y, 4>, p, a, st);
-            default: return launch_norm(k_norm_forward<X, Y, 8>, p, a, st);
-        }
-    } else {
-        return launch_norm(k_norm_forward_any<X, Y>, p, a, st);
+template <typename X, typename Y, bool SHIFTED>
+bool ring_forward(const NormForward& a, const NormPlan& p, cudaStream_t st) {
+    switch (p.vpt) {
+        case 1: return launch_norm(k_norm_forward<X, Y, 1, SHIFTED>, p, a, st);
+        case 2: return launch_norm(k_norm_forward<X, Y, 2, SHIFTED>, p, a, st);
+        case 3: return launch_norm(k_norm_forward<X, Y, 3, SHIFTED>, p, a, st);
+        case 4: return launch_norm(k_norm_forward<X, Y, 4, SHIFTED>, p, a, st);
     }
+    if constexpr (!SHIFTED) return launch_norm(k_norm_forward<X, Y, 8, false>, p, a, st);
+    return false;
 }
-template <typename X, typename Y, bool RING>
-bool norm_backward(NormBackward a, const NormGrad& g, cudaStream_t st) {
+template <typename X, typename Y>
+bool norm_forward(NormForward a, const NormPlan& p, NormRows rows, cudaStream_t st) {
+    a.stages = p.stages;
+    if (p.wide) return rows == RING ? launch_norm(k_norm_forward_wide<X, Y, true>, p, a, st) : launch_norm(k_norm_forward_wide<X, Y, false>, p, a, st);
+    if (rows == RING) return ring_forward<X, Y, false>(a, p, st);
+    if constexpr (sizeof(X) == 2) return ring_forward<X, Y, true>(a, p, st);
+    else return launch_norm(k_norm_forward_any<X, Y>, p, a, st);
+}
+template <typename X, typename Y>
+bool norm_backward(NormBackward a, const NormGrad& g, NormRows rows, cudaStream_t st) {
     const NormPlan& p = g.p;
     a.stages = p.stages;
-    if (p.wide)
-        return launch_norm(k_norm_sums_wide<X, Y, RING>, p, a, st) &&
-               launch(k_norm_apply_wide<X, Y, RING>, dim3(ceil_div(a.F, 2048), (unsigned)g.parts), dim3(256), 0, st, a);
-    if constexpr (RING) {
-        switch (p.vpt) {
-            case 1: return launch_norm(k_norm_backward<X, Y, 1>, p, a, st);
-            case 2: return launch_norm(k_norm_backward<X, Y, 2>, p, a, st);
-            case 3: return launch_norm(k_norm_backward<X, Y, 3>, p, a, st);
-            default: return launch_norm(k_norm_backward<X, Y, 4>, p, a, st);
-        }
-    } else {
-        return launch_norm(k_norm_backward_any<X, Y>, p, a, st);
+    if (p.wide) {
+        const dim3 grid(ceil_div(a.F, 2048), (unsigned)g.parts), block(256);
+        if (rows == RING) return launch_norm(k_norm_sums_wide<X, Y, true>, p, a, st) && launch(k_norm_apply_wide<X, Y, true>, grid, block, 0, st, a);
+        return launch_norm(k_norm_sums_wide<X, Y, false>, p, a, st) && launch(k_norm_apply_wide<X, Y, false>, grid, block, 0, st, a);
+    }
+    if (rows == LANES) return launch_norm(k_norm_backward_any<X, Y>, p, a, st);
+    switch (p.vpt) {
+        case 1: return launch_norm(k_norm_backward<X, Y, 1>, p, a, st);
+        case 2: return launch_norm(k_norm_backward<X, Y, 2>, p, a, st);
+        case 3: return launch_norm(k_norm_backward<X, Y, 3>, p, a, st);
+        default: return launch_norm(k_norm_backward<X, Y, 4>, p, a, st);
     }
 }
 // the pairs of types: x and y (dy) alike, or x float32 and y bfloat16
 bool types_ok(int x, int y) { return dtype_ok(x) && dtype_ok(y) && (x == y || x == PSGD_DT_F32); }
 template <typename Call>
-bool by_type(int x, int y, bool vec, Call&& call) {
-    if (x == PSGD_DT_BF16) return vec ? call((bf16*)0, (bf16*)0, std::true_type()) : call((bf16*)0, (bf16*)0, std::false_type());
-    if (y == PSGD_DT_BF16) return vec ? call((float*)0, (bf16*)0, std::true_type()) : call((float*)0, (bf16*)0, std::false_type());
-    return vec ? call((float*)0, (float*)0, std::true_type()) : call((float*)0, (float*)0, std::false_type());
-}
+bool by_type(int x, int y, Call&& call) { return x == PSGD_DT_BF16 ? call((bf16*)0, (bf16*)0) : y == PSGD_DT_BF16 ? call((float*)0, (bf16*)0) : call((float*)0, (float*)0); }
 
 // ---- rotary positions ----
 // A tensor [T][heads][head] as stretches of bytes: rows of tokens with their heads in them, or rows of heads with their tokens; else (values that are used
@@ -157,16 +160,17 @@ psgd_status psgd_norm_forward(const void* x, int64_t ldx, int x_dtype, const voi
     const Stretch in[2] = {stretch(x, T, F, ldx, size_of(x_dtype)), stretch(r, T, F, ldr, size_of(x_dtype))};
     const Stretch sum = stretch(s, T, F, lds, size_of(x_dtype)), out = stretch(y, T, F, ldy, size_of(y_dtype));
     if (overlap(in[0], sum) || overlap(in[0], out) || overlap(in[1], sum) || overlap(in[1], out) || overlap(sum, out)) return PSGD_E_INVALID;
-    const bool vec = whole_units(x, ldx, F, x_dtype) && whole_units(r, ldr, F, x_dtype) && whole_units(s, lds, F, x_dtype) && whole_units(y, ldy, F, y_dtype);
+    const bool whole = whole_units(x, ldx, F, x_dtype) && whole_units(r, ldr, F, x_dtype) && whole_units(s, lds, F, x_dtype) && whole_units(y, ldy, F, y_dtype);
+    const NormRows rows = whole ? RING : x_dtype == PSGD_DT_BF16 ? SHIFT : LANES;
     NormForward a{};
     a.T = T; a.F = (int)F; a.center = center != 0; a.eps = eps;
     a.x = x; a.r = r; a.s = s; a.y = y;
     a.ldx = ldx; a.ldr = ldr; a.lds = lds; a.ldy = ldy;
     a.w = {w, w_dtype == PSGD_DT_BF16}; a.b = {b, w_dtype == PSGD_DT_BF16};
     a.mean = center ? mean : nullptr; a.rstd = rstd; a.q = q; a.scales = scales;
-    const NormPlan p = plan_norm(T, F, vec, F * size_of(x_dtype) * (r ? 2 : 1), r != nullptr, false);
-    const bool ok = by_type(x_dtype, y_dtype, vec, [&](auto* tx, auto* ty, auto v) {
-        return norm_forward<std::remove_pointer_t<decltype(tx)>, std::remove_pointer_t<decltype(ty)>, decltype(v)::value>(a, p, (cudaStream_t)stream);
+    const NormPlan p = plan_norm(T, F, rows, F * size_of(x_dtype) * (r ? 2 : 1), r != nullptr, false);
+    const bool ok = by_type(x_dtype, y_dtype, [&](auto* tx, auto* ty) {
+        return norm_forward<std::remove_pointer_t<decltype(tx)>, std::remove_pointer_t<decltype(ty)>>(a, p, rows, (cudaStream_t)stream);
     });
     return ok ? PSGD_OK : PSGD_E_CUDA;
 }
@@ -177,8 +181,8 @@ psgd_status psgd_norm_workspace(int64_t T, int64_t F, size_t* bytes) {
     *bytes = 256;
     if (T > 0) {
         // whatever the types, the alignment and the operands (2 + 2, 4 + 2, 4 + 4 bytes per column, and x's again)
-        *bytes = plan_norm_grad(T, F, false, 0).total;
-        for (int each : {4, 6, 8, 10, 12}) *bytes = std::max(*bytes, F % 8 ? 0 : plan_norm_grad(T, F, true, F * each).total);
+        *bytes = plan_norm_grad(T, F, LANES, 0).total;
+        for (int each : {4, 6, 8, 10, 12}) *bytes = std::max(*bytes, plan_norm_grad(T, F, RING, F * each).total);
     }
     return PSGD_OK;
 }
@@ -196,8 +200,9 @@ psgd_status psgd_norm_backward(const void* dy, int64_t lddy, int dy_dtype, const
     const int size = size_of(x_dtype);
     const Stretch out = stretch(dx, T, F, lddx, size);
     if (overlap(out, stretch(dy, T, F, lddy, size_of(dy_dtype))) || overlap(out, stretch(x, T, F, ldx, size)) || overlap(out, stretch(add, T, F, ldadd, size))) return PSGD_E_INVALID;
-    const bool vec = whole_units(dy, lddy, F, dy_dtype) && whole_units(x, ldx, F, x_dtype) && whole_units(add, ldadd, F, x_dtype) && whole_units(dx, lddx, F, x_dtype);
-    const NormGrad g = plan_norm_grad(T, F, vec, F * (size_of(dy_dtype) + size * (add ? 2 : 1)));
+    const bool whole = whole_units(dy, lddy, F, dy_dtype) && whole_units(x, ldx, F, x_dtype) && whole_units(add, ldadd, F, x_dtype) && whole_units(dx, lddx, F, x_dtype);
+    const NormRows rows = whole ? RING : LANES;
+    const NormGrad g = plan_norm_grad(T, F, rows, F * (size_of(dy_dtype) + size * (add ? 2 : 1)));
     if (ws_bytes < g.total) return PSGD_E_WORKSPACE;
     NormBackward a{};
     a.T = T; a.F = (int)F; a.center = mean != nullptr;
@@ -208,8 +213,8 @@ psgd_status psgd_norm_backward(const void* dy, int64_t lddy, int dy_dtype, const
     a.part = (float*)((char*)ws + g.part);
     a.dw = dw; a.db = db;
     a.sums = (float2*)((char*)ws + g.sums);
-    const bool ok = by_type(x_dtype, dy_dtype, vec, [&](auto* tx, auto* ty, auto v) {
-        return norm_backward<std::remove_pointer_t<decltype(tx)>, std::remove_pointer_t<decltype(ty)>, decltype(v)::value>(a, g, st);
+    const bool ok = by_type(x_dtype, dy_dtype, [&](auto* tx, auto* ty) {
+        return norm_backward<std::remove_pointer_t<decltype(tx)>, std::remove_pointer_t<decltype(ty)>>(a, g, rows, st);
     });
     if (!ok) return PSGD_E_CUDA;
     if (g.parts == 1) return PSGD_OK;                  // (the one CTA has written the results)

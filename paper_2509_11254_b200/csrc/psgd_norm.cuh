@@ -13,7 +13,9 @@
 //
 // Rows of whole 16-byte units come through a ring in shared memory: every thread copies its own units of the rows to come asynchronously (cp.async) and reads back only
 // what it copied itself, so that there is nothing to wait for but its own copies, rows are under way whatever the registers hold, and the backward pass
-// reads a row a second time from there.  Rows of any other width or alignment (.._any): a value per lane, the next row's values in registers.
+// reads a row a second time from there.  Rows of bfloat16 of any other width or alignment go the same way forward (SHIFT), the units of memory that they lie in being cut to
+// the threads' values (16384 x 2051 with a residual 91 us, a value per lane 104); backward, where every row is read twice, that costs more than it saves (119 against
+// 115 us; 16384 x 771: 50, 38).  There and for float32 (.._any): a value per lane, the next row's values in registers.
 // Sums and statistics are float32.  Rounded once: s to x's type, y, ds; the 8-bit form is that of the rounded y.
 #pragma once
 #include "psgd_values.cuh"
@@ -212,27 +214,61 @@ __device__ __forceinline__ uint2 shared8(unsigned at) {
     asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];\n" : "=r"(v.x), "=r"(v.y) : "r"(at) : "memory");
     return v;
 }
+// the first `bytes` of 16, zeros behind them
+__device__ __forceinline__ void copy16_of(unsigned to, const void* from, int bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+}
 __device__ __forceinline__ F2 pair_of(unsigned x, unsigned y) { return pair(__uint_as_float(x), __uint_as_float(y)); }
 // bytes of a unit in one plane, and of all planes of an operand
 template <typename T, typename X> __device__ __forceinline__ constexpr int unit_bytes() { return sizeof(X) == 2 ? 16 : 4 * (int)sizeof(T); }
-template <typename T, int VPT> __device__ __forceinline__ int operand_bytes() { return VPT * (int)blockDim.x * 8 * (int)sizeof(T); }
+template <typename T, int VPT, bool SHIFT> __device__ __forceinline__ int operand_bytes() {
+    return VPT * (int)blockDim.x * 8 * (int)sizeof(T) + (SHIFT ? (int)(blockDim.x >> 5) * 16 : 0);
+}
 // Columns of a thread's pieces (those that do not exist fetch the row's last one: no branches), and how many of a unit's values exist.
-template <typename X, int VPT>
+template <typename X, int VPT, bool SHIFT>
 struct Place {
     int at[VPT][sizeof(X) == 2 ? 1 : 2], n[VPT];
     __device__ __forceinline__ explicit Place(int F) {
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             const int u = unit_of<VPT>(i), c0 = piece_col<X>(u, 0), c1 = piece_col<X>(u, 1);
+            if constexpr (SHIFT) {
+                at[i][0] = c0;
+                n[i] = min(max(F - c0, 0), 8);
+                continue;
+            }
             at[i][0] = min(c0, F - (sizeof(X) == 2 ? 8 : 4));
             if constexpr (sizeof(X) == 4) at[i][1] = min(c1, F - 4);
             n[i] = (c0 < F ? 4 : 0) + (c1 < F ? 4 : 0);
         }
     }
 };
+// SHIFT: rows of bfloat16 of any width and alignment.  The ring holds the 16-byte units of memory that a row lies in, as many as it has units of eight values and one more
+// per warp, so that a warp's values are among its own copies and a lane cuts its eight out of its unit and the next lane's.  Nothing behind the row's end is read (the
+// copy ends there and fills up with zeros); what lies before its beginning in its first unit are rows before it, and where that would be before the matrix, the unit is read value by value.
+__device__ __forceinline__ unsigned image_unit(unsigned operand, int vpt, int k) { return operand + ((threadIdx.x >> 5) * (32 * vpt + 1) + k) * 16; }       // k-th unit of the warp's
+__device__ __forceinline__ void image_ask(unsigned to, const __nv_bfloat16* row, int u, int F, const __nv_bfloat16* matrix) {
+    const unsigned sh = shift_of(row);
+    const int bytes = min(max((int)sh + 2 * F - 16 * u, 0), 16);
+    const char* from = reinterpret_cast<const char*>(row) - sh;
+    if (u == 0 && from < reinterpret_cast<const char*>(matrix)) {
+        for (int b = 0; b < 16; b += 2) {
+            const unsigned short h = b >= (int)sh && b < (int)sh + 2 * F ? reinterpret_cast<const unsigned short*>(row)[(b - (int)sh) / 2] : (unsigned short)0;
+            asm volatile("st.shared.u16 [%0], %1;\n" ::"r"(to + b), "h"(h) : "memory");
+        }
+        return;
+    }
+    copy16_of(to, bytes ? from + 16 * (size_t)u : from, bytes);
+}
 // `operand`: where the operand's planes begin
-template <typename T, typename X, int VPT>
-__device__ __forceinline__ void ring_ask(unsigned operand, const T* row, const Place<X, VPT>& p) {
+template <typename T, typename X, int VPT, bool SHIFT>
+__device__ __forceinline__ void ring_ask(unsigned operand, const T* row, const Place<X, VPT, SHIFT>& p, int F, const T* matrix) {
+    if constexpr (SHIFT) {
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) image_ask(image_unit(operand, VPT, 32 * i + (threadIdx.x & 31)), row, unit_of<VPT>(i), F, matrix);
+        if ((threadIdx.x & 31) == 31) image_ask(image_unit(operand, VPT, 32 * VPT), row, unit_of<VPT>(VPT - 1) + 1, F, matrix);
+        return;
+    }
     constexpr int B = unit_bytes<T, X>();
     const unsigned to = operand + unit_of<VPT>(0) * B;
 #pragma unroll
@@ -246,8 +282,19 @@ __device__ __forceinline__ void ring_ask(unsigned operand, const T* row, const P
         }
     }
 }
-template <typename T, typename X, int VPT>
-__device__ __forceinline__ Eight ring_read(unsigned operand, int i) {
+// a unit of a shifted row (`row`: where it lies in memory) as eight bfloat16
+template <int VPT>
+__device__ __forceinline__ uint4 image_read(unsigned operand, int i, const __nv_bfloat16* row) {
+    const unsigned at = image_unit(operand, VPT, 32 * i + (threadIdx.x & 31));
+    return cut_out(shared16(at), shared16(at + 16), shift_of(row));
+}
+template <typename T, typename X, int VPT, bool SHIFT>
+__device__ __forceinline__ Eight ring_read(unsigned operand, int i, const T* row) {
+    if constexpr (SHIFT) {
+        float v[8];
+        widen(Raw16{image_read<VPT>(operand, i, row)}, v);
+        return eight(v);
+    }
     constexpr int B = unit_bytes<T, X>();
     const unsigned at = operand + unit_of<VPT>(i) * B;
     if constexpr (sizeof(T) == 4) {
@@ -267,11 +314,19 @@ __device__ __forceinline__ Eight ring_read(unsigned operand, int i) {
     }
 }
 // A unit's values to a row of T beside an x of type X, and (rounded) as they stand there.
-template <typename T, typename X, int VPT>
-__device__ __forceinline__ void unit_store(T* row, const Place<X, VPT>& p, int i, const Eight& v) {
+// `image`: SHIFT, the warp's 34 units to turn its values into units of memory.
+template <int VPT>
+__device__ __forceinline__ void image_store(__nv_bfloat16* row, int i, int F, const uint4& v, uint4* image) {
+    const int first = unit_of<VPT>(i) * 8 - (int)(threadIdx.x & 31) * 8;                        // the same in all lanes
+    if (first < F) store_any(row + unit_of<VPT>(i) * 8, v, min(F - first, 256), image);
+}
+template <typename T, typename X, int VPT, bool SHIFT>
+__device__ __forceinline__ void unit_store(T* row, const Place<X, VPT, SHIFT>& p, int i, const Eight& v, int F, uint4* image) {
     float x[8];
     singles(v, x);
-    if constexpr (sizeof(T) == 4) {
+    if constexpr (SHIFT) {
+        image_store<VPT>(row, i, F, pack_bf16x8(x), image);
+    } else if constexpr (sizeof(T) == 4) {
         if (p.n[i] > 0) *reinterpret_cast<float4*>(row + p.at[i][0]) = make_float4(x[0], x[1], x[2], x[3]);
         if (p.n[i] > 4) *reinterpret_cast<float4*>(row + p.at[i][1]) = make_float4(x[4], x[5], x[6], x[7]);
     } else {
@@ -292,25 +347,26 @@ __device__ __forceinline__ float sum_of(const Eight& v, int n) {
     return (n > 0 ? a + b : 0.f) + (n > 4 ? c + d : 0.f);
 }
 // A unit of x + r, rounded to their type, written to row s.  Sums of bfloat16 are rounded once by the packed addition itself.
-template <typename X, int VPT>
-__device__ __forceinline__ Eight ring_sum(unsigned x_at, unsigned r_at, int i, X* s, const Place<X, VPT>& p) {
+template <typename X, int VPT, bool SHIFT>
+__device__ __forceinline__ Eight ring_sum(unsigned x_at, unsigned r_at, int i, X* s, const Place<X, VPT, SHIFT>& p, const X* x_row, const X* r_row, int F, uint4* image) {
     if constexpr (sizeof(X) == 2) {
-        const uint4 x = shared16(x_at + unit_of<VPT>(i) * 16), r = shared16(r_at + unit_of<VPT>(i) * 16);
+        const uint4 x = SHIFT ? image_read<VPT>(x_at, i, x_row) : shared16(x_at + unit_of<VPT>(i) * 16), r = SHIFT ? image_read<VPT>(r_at, i, r_row) : shared16(r_at + unit_of<VPT>(i) * 16);
         const auto sum = [](unsigned u, unsigned v) {
             const __nv_bfloat162 t = __hadd2(*reinterpret_cast<const __nv_bfloat162*>(&u), *reinterpret_cast<const __nv_bfloat162*>(&v));
             return *reinterpret_cast<const unsigned*>(&t);
         };
         const uint4 t = make_uint4(sum(x.x, r.x), sum(x.y, r.y), sum(x.z, r.z), sum(x.w, r.w));
-        if (p.n[i]) *reinterpret_cast<uint4*>(s + p.at[i][0]) = t;
+        if constexpr (SHIFT) image_store<VPT>(s, i, F, t, image);
+        else if (p.n[i]) *reinterpret_cast<uint4*>(s + p.at[i][0]) = t;
         float v[8];
         widen(Raw16{t}, v);
         return eight(v);
     } else {
-        Eight x = ring_read<X, X, VPT>(x_at, i);
-        const Eight r = ring_read<X, X, VPT>(r_at, i);
+        Eight x = ring_read<X, X, VPT, SHIFT>(x_at, i, x_row);
+        const Eight r = ring_read<X, X, VPT, SHIFT>(r_at, i, r_row);
 #pragma unroll
         for (int j = 0; j < 4; ++j) x.p[j] = add2(x.p[j], r.p[j]);
-        unit_store<X, X, VPT>(s, p, i, x);
+        unit_store<X, X, VPT, SHIFT>(s, p, i, x, F, image);
         return x;
     }
 }
@@ -369,14 +425,22 @@ __device__ __forceinline__ Eight param_read(unsigned planes, int units, int i) {
     return {{pair_of(a.x, a.y), pair_of(a.z, a.w), pair_of(b.x, b.y), pair_of(b.z, b.w)}};
 }
 
-template <typename X, typename Y, int VPT>
+// the warp's units for image_store
+template <bool SHIFT>
+__device__ __forceinline__ uint4* norm_image() {
+    __shared__ uint4 image[SHIFT ? NORM_WARPS * ANY_UNITS : 1];
+    return SHIFT ? image + ((threadIdx.y * blockDim.x + threadIdx.x) >> 5) * ANY_UNITS : nullptr;
+}
+
+template <typename X, typename Y, int VPT, bool SHIFT>
 __global__ void __launch_bounds__(NORM_THREADS) k_norm_forward(const __grid_constant__ NormForward a) {
     extern __shared__ __align__(16) unsigned char ring_raw[];          // w, b, then the rings
     __shared__ float2 stat[2][NORM_WARPS];             // by rows taken in turn: a row's exchange is over when the next but one writes
     __shared__ float counts[NORM_WARPS];
     grid_trigger();
     const int F = a.F, tid = threadIdx.x, warps = blockDim.x >> 5, units = VPT * blockDim.x;
-    const Place<X, VPT> p(F);
+    const Place<X, VPT, SHIFT> p(F);
+    uint4* image = norm_image<SHIFT>();
     int have = 0;
 #pragma unroll
     for (int i = 0; i < VPT; ++i) have += p.n[i];
@@ -389,12 +453,12 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_forward(const __grid_cons
     const X *x = (const X*)a.x + row * a.ldx, *r = a.r ? (const X*)a.r + row * a.ldr : nullptr;
     X* s = a.s ? (X*)a.s + row * a.lds : nullptr;
     Y* y = (Y*)a.y + row * a.ldy;
-    const int operand = operand_bytes<X, VPT>(), stage = r ? 2 * operand : operand, stages = a.stages;
+    const int operand = operand_bytes<X, VPT, SHIFT>(), stage = r ? 2 * operand : operand, stages = a.stages;
     const unsigned params = smem_addr(ring_raw), ring = params + units * 64 + threadIdx.y * stages * stage;
     const auto ask = [&](unsigned to) {
         if (asked < a.T) {
-            ring_ask<X, X, VPT>(to, x, p);
-            if (r) ring_ask<X, X, VPT>(to + operand, r, p);
+            ring_ask<X, X, VPT, SHIFT>(to, x, p, F, (const X*)a.x);
+            if (r) ring_ask<X, X, VPT, SHIFT>(to + operand, r, p, F, (const X*)a.r);
         }
         ring_commit();
         asked += step;
@@ -411,15 +475,17 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_forward(const __grid_cons
     for (int turn = 0; row < a.T; row += step, turn ^= 1) {
         Eight v[VPT];
         ring_wait(stages);
+        if (SHIFT) __syncwarp();                       // (values of other lanes' copies)
+        const X *x_row = SHIFT ? (const X*)a.x + row * a.ldx : nullptr, *r_row = SHIFT && r ? (const X*)a.r + row * a.ldr : nullptr;
         if (r) {
 #pragma unroll
-            for (int i = 0; i < VPT; ++i) v[i] = ring_sum<X, VPT>(from, from + operand, i, s, p);
+            for (int i = 0; i < VPT; ++i) v[i] = ring_sum<X, VPT, SHIFT>(from, from + operand, i, s, p, x_row, r_row, F, image);
         } else {
 #pragma unroll
-            for (int i = 0; i < VPT; ++i) v[i] = ring_read<X, X, VPT>(from, i);
+            for (int i = 0; i < VPT; ++i) v[i] = ring_read<X, X, VPT, SHIFT>(from, i, x_row);
             if (s) {
 #pragma unroll
-                for (int i = 0; i < VPT; ++i) unit_store<X, X, VPT>(s, p, i, v[i]);
+                for (int i = 0; i < VPT; ++i) unit_store<X, X, VPT, SHIFT>(s, p, i, v[i], F, image);
             }
         }
         float m = 0.f;
@@ -432,6 +498,17 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_forward(const __grid_cons
             for (int i = 0; i < VPT; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) v[i].p[j] = add2(v[i].p[j], off);
+            if constexpr (SHIFT) {
+#pragma unroll
+                for (int i = 0; i < VPT; ++i) {
+                    if (p.n[i] == 8) continue;         // the row's end: zeros again
+                    float t[8];
+                    singles(v[i], t);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) t[j] = j < p.n[i] ? t[j] : 0.f;
+                    v[i] = eight(t);
+                }
+            }
         }
         float sq = 0.f;
 #pragma unroll
@@ -443,6 +520,7 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_forward(const __grid_cons
             sq += (p.n[i] > 0 ? t[0] + t[1] : 0.f) + (p.n[i] > 4 ? t[2] + t[3] : 0.f);
         }
         RowStats st{m, warp_sum(sq)};
+        if (SHIFT) __syncwarp();
         ask(from);                                     // (every value has been used)
         from = stages == 1 || from != ring ? ring : ring + stage;
         if (warps > 1) st = join_warps(st.mean, st.m2, stat[turn] + threadIdx.y * warps, in_lane, per, a.center);
@@ -458,7 +536,7 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_forward(const __grid_cons
             Eight o;
 #pragma unroll
             for (int j = 0; j < 4; ++j) o.p[j] = fma2(mul2(add2(v[i].p[j], off), ff), w.p[j], b.p[j]);
-            unit_store<Y, X, VPT>(y, p, i, o);
+            unit_store<Y, X, VPT, SHIFT>(y, p, i, o, F, image);
             if (a.q) unit_keep<Y, X>(o, unit_of<VPT>(i), p.n[i], row * G, G, a.q, a.scales);
         }
         if (s) s += step * a.lds;
@@ -674,7 +752,7 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_backward(const __grid_con
     __shared__ float2 stat[2][NORM_WARPS];
     grid_trigger();
     const int F = a.F, warps = blockDim.x >> 5, units = VPT * blockDim.x;
-    const Place<X, VPT> p(F);
+    const Place<X, VPT, false> p(F);
     grid_wait();
     const long long step = (long long)gridDim.x * blockDim.y;
     long long row = (long long)blockIdx.x * blockDim.y + threadIdx.y, asked = row;
@@ -682,7 +760,7 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_backward(const __grid_con
     const Y* dy = (const Y*)a.dy + row * a.lddy;
     const X *x = (const X*)a.x + row * a.ldx, *add = a.add ? (const X*)a.add + row * a.ldadd : nullptr;
     X* dx = (X*)a.dx + row * a.lddx;
-    const int at_x = operand_bytes<Y, VPT>(), at_add = at_x + operand_bytes<X, VPT>(), stage = add ? at_add + operand_bytes<X, VPT>() : at_add, stages = a.stages;
+    const int at_x = operand_bytes<Y, VPT, false>(), at_add = at_x + operand_bytes<X, VPT, false>(), stage = add ? at_add + operand_bytes<X, VPT, false>() : at_add, stages = a.stages;
     const unsigned params = smem_addr(ring_raw), ring = params + units * 32 + threadIdx.y * stages * stage;
     float nm = 0.f, nf = 0.f;                          // the next row's mean and rstd
     const auto ask_stats = [&](long long i) {
@@ -692,9 +770,9 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_backward(const __grid_con
     };
     const auto ask = [&](unsigned to) {
         if (asked < a.T) {
-            ring_ask<Y, X, VPT>(to, dy, p);
-            ring_ask<X, X, VPT>(to + at_x, x, p);
-            if (add) ring_ask<X, X, VPT>(to + at_add, add, p);
+            ring_ask<Y, X, VPT, false>(to, dy, p, F, dy);
+            ring_ask<X, X, VPT, false>(to + at_x, x, p, F, x);
+            if (add) ring_ask<X, X, VPT, false>(to + at_add, add, p, F, add);
         }
         ring_commit();
         asked += step;
@@ -721,7 +799,7 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_backward(const __grid_con
         F2 t1 = 0ull, t2 = 0ull;
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
-            const Eight d = ring_read<Y, X, VPT>(from, i), v = ring_read<X, X, VPT>(from + at_x, i), w = param_read<VPT>(params, units, i);
+            const Eight d = ring_read<Y, X, VPT, false>(from, i, nullptr), v = ring_read<X, X, VPT, false>(from + at_x, i, nullptr), w = param_read<VPT>(params, units, i);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {              // (w is 0 where there is no value, and its dw and db go nowhere)
                 const F2 xh = mul2(add2(v.p[j], off), ff), g = mul2(d.p[j], w.p[j]);
@@ -742,16 +820,16 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_backward(const __grid_con
         const F2 c1 = pair(s1, s1), c2 = pair(s2, s2);
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
-            const Eight v = ring_read<X, X, VPT>(from + at_x, i), w = param_read<VPT>(params, units, i);
-            Eight d = ring_read<Y, X, VPT>(from, i);
+            const Eight v = ring_read<X, X, VPT, false>(from + at_x, i, nullptr), w = param_read<VPT>(params, units, i);
+            Eight d = ring_read<Y, X, VPT, false>(from, i, nullptr);
 #pragma unroll
             for (int j = 0; j < 4; ++j) d.p[j] = fma2(mul2(d.p[j], w.p[j]), ff, fma2(add2(v.p[j], off), c2, c1));
             if (add) {
-                const Eight u = ring_read<X, X, VPT>(from + at_add, i);
+                const Eight u = ring_read<X, X, VPT, false>(from + at_add, i, nullptr);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) d.p[j] = add2(d.p[j], u.p[j]);
             }
-            unit_store<X, X, VPT>(dx, p, i, d);
+            unit_store<X, X, VPT, false>(dx, p, i, d, F, nullptr);
         }
         dx += step * a.lddx;
         ask(from);

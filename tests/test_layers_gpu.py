@@ -533,3 +533,22 @@ def test_layer_calls_refuse(torch, ops):
     for call in bad:
         with pytest.raises(ops.PSGDError):
             call()
+
+
+@pytest.mark.parametrize("T", [1, 2, 9])
+@pytest.mark.parametrize("F", [1, 2, 3, 7, 8, 9, 31, 255, 256, 257, 263, 511, 1000, 1537, 2057, 5003])
+def test_norm_rows_of_every_alignment(torch, ops, T, F):
+    """Every start within 16 bytes, strides that move it from row to row (down to rows of one value side by side), NaN everywhere else in the buffers."""
+    w, b = 1 + 0.3 * torch.randn(F, generator=gen(torch, 1), device="cuda"), 0.2 * torch.randn(F, generator=gen(torch, 2), device="cuda")
+    for start, gap in ((0, 0), (1, 0), (2, 1), (3, 2), (5, 3), (7, 7), (4, 8)):
+        def part(seed):
+            flat = torch.full((start + T * (F + gap) + 16,), float("nan"), device="cuda", dtype=torch.bfloat16)
+            t = flat.as_strided((T, F), (F + gap, 1), start)
+            t.copy_(torch.randn(T, F, generator=gen(torch, seed), device="cuda"))
+            return t
+
+        x, r, dy, d_x = (part(s) for s in (3, 4, 5, 6))
+        fwd = check_forward(torch, ops, x, w, b, r, 1e-5, True, True, None)
+        check_backward(torch, ops, fwd, w, dy, d_x, True, True)
+        fwd = check_forward(torch, ops, x, w, None, None, 1e-5, False, False, None)
+        check_backward(torch, ops, fwd, w, dy, None, False, False)
