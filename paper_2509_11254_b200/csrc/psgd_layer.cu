@@ -236,8 +236,10 @@ psgd_status psgd_rotary(const void* q, int64_t q_token, int64_t q_head, int64_t 
     if (!positions || !frequencies || (heads_q && (!q || !out_q)) || (heads_k && (!k || !out_k))) return PSGD_E_NULL;
     const RotaryTensor t[2] = {{q, out_q, q_token, q_head, oq_token, oq_head}, {k, out_k, k_token, k_head, ok_token, ok_head}};
     const int64_t count[2] = {heads_q, heads_k};
-    bool vec = true, in_place = true;
-    const int64_t unit = 16 / size_of(dtype);
+    bool in_place = true;
+    // the most values that a thread can move at a time: every address, stride and width is a multiple of it (of 16 bytes at most)
+    const bool half = layout == PSGD_ROTARY_HALF;
+    uint64_t all = (uint64_t)head | (uint64_t)rotated / (half ? 2 : 1);
     Stretch in[2] = {}, out[2] = {};
     for (int i = 0; i < 2; ++i) {
         if (!count[i]) continue;
@@ -245,8 +247,10 @@ psgd_status psgd_rotary(const void* q, int64_t q_token, int64_t q_head, int64_t 
         in[i] = extent_of(t[i].in, T, count[i], head, t[i].in_token, t[i].in_head, size_of(dtype), once);
         out[i] = extent_of(t[i].out, T, count[i], head, t[i].out_token, t[i].out_head, size_of(dtype), once);
         if (!once) return PSGD_E_INVALID;              // two values would be written to one place
-        const auto even = [&](int64_t token, int64_t step) { return (T == 1 || token % unit == 0) && (count[i] == 1 || step % unit == 0); };
-        vec = vec && aligned16(t[i].in) && aligned16(t[i].out) && even(t[i].in_token, t[i].in_head) && even(t[i].out_token, t[i].out_head);
+        if (T > 1) all |= (uint64_t)(t[i].in_token | t[i].out_token);
+        if (count[i] > 1) all |= (uint64_t)(t[i].in_head | t[i].out_head);
+        const uint64_t at = (uint64_t)(uintptr_t)t[i].in | (uint64_t)(uintptr_t)t[i].out;
+        all |= at % 16 ? at / size_of(dtype) : 0;
         in_place = in_place && t[i].in == t[i].out;
     }
     for (int i = 0; i < 2; ++i)
@@ -256,17 +260,18 @@ psgd_status psgd_rotary(const void* q, int64_t q_token, int64_t q_head, int64_t 
             if (count[i] && count[j] && !same && overlap(out[i], in[j])) return PSGD_E_INVALID;
         }
     if (heads_q && heads_k && overlap(out[0], out[1])) return PSGD_E_INVALID;
-    const bool half = layout == PSGD_ROTARY_HALF;
-    vec = vec && head % 8 == 0 && rotated % (half ? 16 : 8) == 0;
+    int V = 8;
+    while (V > 1 && all % V) V /= 2;
     RotaryArgs a{};
     a.T = T; a.heads_q = (int)heads_q; a.heads = (int)heads; a.rotated = (int)rotated; a.head = (int)head;
-    a.turned = (int)(vec ? (half ? rotated / 16 : rotated / 8) : rotated / 2);
-    a.per_head = a.turned + (in_place ? 0 : (int)((head - rotated) / (vec ? 8 : 1)));
-    const int64_t items = heads * a.per_head;          // per token
+    a.turned = (int)(half || V == 1 ? rotated / 2 / V : rotated / V);
+    a.per_head = a.turned + (in_place ? 0 : (int)((head - rotated) / V));
+    a.groups = ceil_div(heads, ROT_HEADS);
+    const int64_t items = (int64_t)a.groups * a.per_head;         // per token
     const int sms = device_sms();
     // tokens of a CTA at a time: two rounds of items where there are enough tokens for every CTA, as many angles as shared memory is set aside for
-    a.tokens = (int)std::max<int64_t>(1, std::min<int64_t>({2 * ROT_THREADS * ROT_ITEMS / items, T / (4 * sms), ROT_PAIRS / (rotated / 2)}));
-    a.by_head = fast_div((unsigned)a.per_head); a.by_heads = fast_div((unsigned)heads); a.by_pairs = fast_div((unsigned)(rotated / 2));
+    a.tokens = (int)std::max<int64_t>(1, std::min<int64_t>({2 * ROT_THREADS / items, T / (4 * sms), ROT_PAIRS / (rotated / 2)}));
+    a.by_head = fast_div((unsigned)a.per_head); a.by_groups = fast_div((unsigned)a.groups); a.by_pairs = fast_div((unsigned)(rotated / 2));
     a.q = t[0]; a.k = t[1];
     a.positions = (const long long*)positions;
     a.frequencies = frequencies;
@@ -274,12 +279,14 @@ psgd_status psgd_rotary(const void* q, int64_t q_token, int64_t q_head, int64_t 
     a.sign = backward ? -1.f : 1.f;
     const dim3 grid((unsigned)std::min<int64_t>((T + a.tokens - 1) / a.tokens, (int64_t)sms * 8));
     const auto run = [&](auto kernel) { return launch(kernel, grid, dim3(ROT_THREADS), 0, (cudaStream_t)stream, a) ? PSGD_OK : PSGD_E_CUDA; };
-    if (dtype == PSGD_DT_BF16) {
-        if (vec) return half ? run(k_rotary<bf16, 8, true>) : run(k_rotary<bf16, 8, false>);
-        return half ? run(k_rotary<bf16, 1, true>) : run(k_rotary<bf16, 1, false>);
-    }
-    if (vec) return half ? run(k_rotary<float, 8, true>) : run(k_rotary<float, 8, false>);
-    return half ? run(k_rotary<float, 1, true>) : run(k_rotary<float, 1, false>);
+    const auto by_width = [&](auto* x) {
+        typedef std::remove_pointer_t<decltype(x)> X;
+        if (V == 8) return half ? run(k_rotary<X, 8, true>) : run(k_rotary<X, 8, false>);
+        if (V == 4) return half ? run(k_rotary<X, 4, true>) : run(k_rotary<X, 4, false>);
+        if (V == 2) return half ? run(k_rotary<X, 2, true>) : run(k_rotary<X, 2, false>);
+        return half ? run(k_rotary<X, 1, true>) : run(k_rotary<X, 1, false>);
+    };
+    return dtype == PSGD_DT_BF16 ? by_width((bf16*)0) : by_width((float*)0);
 }
 
 }  // extern "C"

@@ -7,7 +7,8 @@
 // the position modulo 2^64, is the angle modulo a turn without a rounding of its own; its upper 32 bits as float32 are within 2^-25 of a turn.  A token's sines and
 // cosines are formed once per CTA, in shared memory, for all heads.
 //
-// Bound by HBM: every value read once and written once.  A thread moves 16 bytes at a time (half: 16 of the first half and the 16 that belong to them).
+// Bound by HBM: every value read once and written once.  A thread moves V values at a time, 16 bytes of bfloat16 where widths and addresses allow (half: V of the first half and
+// the V that belong to them), of the same place in ROT_HEADS heads, whose loads are under way together and which share the sines and cosines that it reads.
 #pragma once
 #include <type_traits>
 
@@ -16,16 +17,17 @@
 namespace psgd {
 
 constexpr int ROT_THREADS = 256;
-constexpr int ROT_ITEMS = 4;                       // items of a thread under way at a time
+constexpr int ROT_HEADS = 4;                       // heads of an item
 constexpr int ROT_PAIRS = 2048;                    // angles of a CTA in shared memory
 
 struct RotaryTensor { const void* in; void* out; long long in_token, in_head, out_token, out_head; };     // strides in elements
 struct RotaryArgs {
     long long T;
     int heads_q, heads, rotated, head;             // heads: of both tensors
-    int per_head, turned;                          // items per head, and how many of them hold pairs
+    int per_head, turned;                          // places of V values in a head, and how many of them hold (first values of) pairs
+    int groups;                                    // of ROT_HEADS heads
     int tokens;                                    // per CTA at a time
-    FastDiv by_head, by_heads;                     // per_head, heads
+    FastDiv by_head, by_groups;                    // per_head, groups
     FastDiv by_pairs;                              // rotated / 2
     RotaryTensor q, k;
     const long long* positions;
@@ -40,14 +42,43 @@ __device__ __forceinline__ float turns_of(long long position, double frequency) 
     return (float)(int)((step * (unsigned long long)position) >> 32) * 2.3283064365386963e-10f;          // 2^-32
 }
 
-// V: values of a thread's item side by side (half: twice), 8 or 1
+// V values side by side: 2 to 32 bytes
+template <typename X, int V> struct Some {
+    static constexpr int BYTES = V * (int)sizeof(X);
+    typedef typename std::conditional<BYTES == 2, unsigned short, typename std::conditional<BYTES == 4, unsigned, typename std::conditional<BYTES == 8, uint2, uint4>::type>::type>::type Word;
+    Word w[BYTES == 32 ? 2 : 1];
+    __device__ __forceinline__ void load(const X* p) {
+        w[0] = reinterpret_cast<const Word*>(p)[0];
+        if constexpr (BYTES == 32) w[1] = reinterpret_cast<const Word*>(p)[1];
+    }
+    __device__ __forceinline__ void store(X* p) const {
+        reinterpret_cast<Word*>(p)[0] = w[0];
+        if constexpr (BYTES == 32) reinterpret_cast<Word*>(p)[1] = w[1];
+    }
+    __device__ __forceinline__ void get(float (&x)[V]) const {
+        const X* v = reinterpret_cast<const X*>(w);
+#pragma unroll
+        for (int j = 0; j < V; ++j) x[j] = (float)v[j];
+    }
+    __device__ __forceinline__ void set(const float (&x)[V]) {
+        if constexpr (sizeof(X) == 2 && V > 1) {
+#pragma unroll
+            for (int j = 0; j < V; j += 2) reinterpret_cast<unsigned*>(w)[j / 2] = pack_bf16(x[j], x[j + 1]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < V; ++j) reinterpret_cast<X*>(w)[j] = (X)x[j];
+        }
+    }
+};
+
 template <typename X, int V, bool HALF>
 __global__ void __launch_bounds__(ROT_THREADS) k_rotary(const __grid_constant__ RotaryArgs a) {
-    typedef typename std::conditional<V == 1, X, typename std::conditional<sizeof(X) == 2, Raw16, Raw32>::type>::type Raw;
-    __shared__ float2 turn[ROT_PAIRS];                                       // cosine, sine
+    constexpr int PAIRS = HALF ? V : (V == 1 ? 1 : V / 2);                   // of a place
+    constexpr bool SPLIT = HALF || V == 1;                                   // a pair's values lie in two places
+    __shared__ __align__(16) float2 turn[ROT_PAIRS];                         // cosine, sine; two pairs of a place side by side, then those of the next place: no bank twice
     grid_trigger();
     grid_wait();
-    const int pairs = a.rotated / 2;
+    const int pairs = a.rotated / 2, places = pairs / PAIRS, second = HALF ? pairs : 1;
     for (long long t0 = (long long)blockIdx.x * a.tokens; t0 < a.T; t0 += (long long)gridDim.x * a.tokens) {
         const int tokens = (int)min((long long)a.tokens, a.T - t0);
         __syncthreads();
@@ -55,73 +86,74 @@ __global__ void __launch_bounds__(ROT_THREADS) k_rotary(const __grid_constant__ 
             const int t = i / a.by_pairs, p = i - t * pairs;
             float s, c;
             sincospif(2.f * turns_of(a.positions[t0 + t], a.frequencies[p]), &s, &c);
-            turn[i] = make_float2(c * a.scale, s * a.scale * a.sign);
+            const int at = PAIRS == 1 ? p : ((p % PAIRS / 2) * places + p / PAIRS) * 2 + (p & 1);
+            turn[t * pairs + at] = make_float2(c * a.scale, s * a.scale * a.sign);
         }
         __syncthreads();
-        const int items = tokens * a.heads * a.per_head;
-        for (int i0 = threadIdx.x; i0 < items; i0 += ROT_THREADS * ROT_ITEMS) {
-            Raw u[ROT_ITEMS], v[ROT_ITEMS];
-            X* to[ROT_ITEMS];
-            int at[ROT_ITEMS];                                               // first angle; -1: values that pass through
+        const int items = tokens * a.groups * a.per_head;
+        for (int i = threadIdx.x; i < items; i += ROT_THREADS) {
+            const int tg = i / a.by_head, place = i - tg * a.per_head;
+            const int t = tg / a.by_groups, h0 = (tg - t * a.groups) * ROT_HEADS;
+            const bool turned = place < a.turned;
+            const int col = turned ? place * (SPLIT && !HALF ? 2 : V) : a.rotated + (place - a.turned) * V;
+            Some<X, V> u[ROT_HEADS], v[SPLIT ? ROT_HEADS : 1];
+            const auto at = [&](int h, bool out) -> X* {
+                const RotaryTensor& x = h >= a.heads_q ? a.k : a.q;
+                const long long head = h >= a.heads_q ? h - a.heads_q : h;
+                return out ? (X*)x.out + (t0 + t) * x.out_token + head * x.out_head + col : (X*)x.in + (t0 + t) * x.in_token + head * x.in_head + col;
+            };
 #pragma unroll
-            for (int j = 0; j < ROT_ITEMS; ++j) {
-                const int i = i0 + j * ROT_THREADS;
-                if (i >= items) break;
-                const int hh = i / a.by_head, unit = i - hh * a.per_head;
-                const int t = hh / a.by_heads, h = hh - t * a.heads;
-                const bool key = h >= a.heads_q;
-                const RotaryTensor& x = key ? a.k : a.q;
-                const int head = key ? h - a.heads_q : h;
-                const bool turned = unit < a.turned;
-                int col;
-                if (turned) col = HALF ? unit * V : unit * (V == 1 ? 2 : V);
-                else col = a.rotated + (unit - a.turned) * V;
-                const X* from = (const X*)x.in + (t0 + t) * x.in_token + head * x.in_head + col;
-                to[j] = (X*)x.out + (t0 + t) * x.out_token + head * x.out_head + col;
-                at[j] = turned ? t * pairs + (HALF ? col : col / 2) : -1;
-                if constexpr (V == 8) {
-                    load8(u[j], from);
-                    if (HALF && turned) load8(v[j], from + pairs);
+            for (int j = 0; j < ROT_HEADS; ++j) {
+                if (h0 + j >= a.heads) break;
+                const X* from = at(h0 + j, false);
+                u[j].load(from);
+                if constexpr (SPLIT) {
+                    if (turned) v[j].load(from + second);
+                }
+            }
+            float c[PAIRS], s[PAIRS];
+            if (turned) {
+                const float2* cs = turn + t * pairs;
+                if constexpr (PAIRS == 1) {
+                    c[0] = cs[place].x;
+                    s[0] = cs[place].y;
                 } else {
-                    u[j] = from[0];
-                    if (turned) v[j] = from[HALF ? pairs : 1];
+#pragma unroll
+                    for (int k = 0; k < PAIRS; k += 2) {
+                        const float4 two = *reinterpret_cast<const float4*>(cs + (k / 2 * places + place) * 2);
+                        c[k] = two.x; s[k] = two.y; c[k + 1] = two.z; s[k + 1] = two.w;
+                    }
                 }
             }
 #pragma unroll
-            for (int j = 0; j < ROT_ITEMS; ++j) {
-                if (i0 + j * ROT_THREADS >= items) break;
-                const float2* cs = turn + at[j];
-                if constexpr (V == 1) {
-                    if (at[j] < 0) {
-                        to[j][0] = u[j];
-                    } else {
-                        const float p = (float)u[j], q = (float)v[j];
-                        to[j][0] = (X)(p * cs[0].x - q * cs[0].y);
-                        to[j][HALF ? pairs : 1] = (X)(p * cs[0].y + q * cs[0].x);
-                    }
-                } else {
-                    float p[8];
-                    widen(u[j], p);
-                    if (at[j] >= 0 && HALF) {
-                        float q[8];
-                        widen(v[j], q);
+            for (int j = 0; j < ROT_HEADS; ++j) {
+                if (h0 + j >= a.heads) break;
+                X* to = at(h0 + j, true);
+                if (turned) {
+                    float p[V];
+                    u[j].get(p);
+                    if constexpr (SPLIT) {
+                        float q[V];
+                        v[j].get(q);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
+                        for (int e = 0; e < V; ++e) {
                             const float x = p[e], y = q[e];
-                            p[e] = x * cs[e].x - y * cs[e].y;
-                            q[e] = x * cs[e].y + y * cs[e].x;
+                            p[e] = x * c[e] - y * s[e];
+                            q[e] = x * s[e] + y * c[e];
                         }
-                        store8(to[j] + pairs, q);
-                    } else if (at[j] >= 0) {
+                        v[j].set(q);
+                        v[j].store(to + second);
+                    } else {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
+                        for (int e = 0; e < PAIRS; ++e) {
                             const float x = p[2 * e], y = p[2 * e + 1];
-                            p[2 * e] = x * cs[e].x - y * cs[e].y;
-                            p[2 * e + 1] = x * cs[e].y + y * cs[e].x;
+                            p[2 * e] = x * c[e] - y * s[e];
+                            p[2 * e + 1] = x * s[e] + y * c[e];
                         }
                     }
-                    store8(to[j], p);
+                    u[j].set(p);
                 }
+                u[j].store(to);
             }
         }
     }
