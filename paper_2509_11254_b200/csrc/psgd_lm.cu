@@ -283,7 +283,7 @@ psgd_status xent(const void* H, int64_t ldh, const void* W, int64_t ldw, const i
         listed.logit = (const float*)(w + x.label_logit);
         labels = (const int64_t*)teach.label;                 // 0 where a row counts
         ignore = -1;
-        if (!launch(k_teach, dim3(ceil_div(T, TEACH_ROWS)), dim3(256), 0, st, teach)) return PSGD_E_CUDA;
+        if (!launch(k_teach, dim3(ceil_div(T, TEACH_ROWS)), dim3(TEACH_THREADS), 0, st, teach)) return PSGD_E_CUDA;
     }
     RowsArgs r{};
     r.V = (int)V; r.nseg = x.nseg;

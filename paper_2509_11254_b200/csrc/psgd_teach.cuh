@@ -12,7 +12,7 @@
 // maximum: p - q of a column of which both are sure is ((e_p - e_q) + e_p rest_q - e_q rest_p) / ((1 + rest_p) (1 + rest_q)), e the exponential relative to the maximum.
 // tau / Z is left to the epilogues of the products that follow.
 //
-// Bound as the cross entropy's kernels are (k_teach_rows: 2 bytes per logit read and written); k_teach reads 10 or 12 bytes per entry.
+// Bound as the cross entropy's kernels are (k_teach_rows: 2 bytes per logit read and written).
 #pragma once
 #include "psgd_xent.cuh"
 
@@ -21,6 +21,8 @@ namespace psgd {
 constexpr int TEACH_ROWS = 32;     // rows of a block of entries
 constexpr int TEACH_COLS = 128;    // columns of a segment
 constexpr int TEACH_BINS = 2048;   // segments that k_teach counts at a time
+constexpr int TEACH_THREADS = 1024;
+constexpr int TEACH_HELD = 4;      // entries per lane that k_teach keeps in registers
 constexpr int TEACH_MOST = 1024;   // entries of a row (k_teach_rows holds a row's in shared memory)
 
 struct TeachArgs {
@@ -41,31 +43,53 @@ struct TeachArgs {
     unsigned* entries;             // [blocks][32 K]
 };
 
-// One CTA per 32 rows.
-__global__ void __launch_bounds__(256) k_teach(const __grid_constant__ TeachArgs a) {
-    __shared__ int count[TEACH_BINS], warps[8];
-    __shared__ int base, total;
+// One CTA per 32 rows, a warp per row.  Bound by latency (10 or 12 bytes per entry are read and 12 written): a row's entries are all asked for at once and held in
+// registers where there are up to 128 of them, longer lists are read again.  4096 rows of 64 entries: 12 us with four rows per warp one after the other, 6 us so.
+__global__ void __launch_bounds__(TEACH_THREADS) k_teach(const __grid_constant__ TeachArgs a) {
+    __shared__ int count[TEACH_BINS], warps[TEACH_THREADS / 32];
+    __shared__ int base;
+    constexpr int EACH = TEACH_BINS / TEACH_THREADS;
     grid_trigger();
-    grid_wait();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, K = a.K;
-    const long long row0 = (long long)blockIdx.x * TEACH_ROWS;
-    const int rows = (int)min((long long)TEACH_ROWS, a.T - row0);
-    const auto logit = [&](long long row, int k) {
-        return a.bf16 ? __bfloat162float(((const __nv_bfloat16*)a.logits)[row * a.ldl + k]) : ((const float*)a.logits)[row * a.ldl + k];
+    for (int i = tid; i < TEACH_BINS; i += TEACH_THREADS) count[i] = 0;
+    if (tid == 0) base = 0;
+    __syncthreads();
+    grid_wait();
+    const long long row = (long long)blockIdx.x * TEACH_ROWS + warp;
+    const bool held = K <= 32 * TEACH_HELD, live = row < a.T;
+    const long long* index = a.index + row * a.ldi;
+    const auto logit = [&](int k) { return a.bf16 ? __bfloat162float(((const __nv_bfloat16*)a.logits)[row * a.ldl + k]) : ((const float*)a.logits)[row * a.ldl + k]; };
+    long long mine[TEACH_HELD];
+    float z[TEACH_HELD];
+    int col[TEACH_HELD];
+    if (live && held) {
+#pragma unroll
+        for (int j = 0; j < TEACH_HELD; ++j) {
+            const int k = lane + 32 * j;
+            mine[j] = k < K ? index[k] : -1;
+            z[j] = k < K ? logit(k) : -INFINITY;
+        }
+    }
+    // calls f(k, its index, its logit, place among the held ones)
+    const auto entries = [&](auto&& f) {
+        if (held) {
+#pragma unroll
+            for (int j = 0; j < TEACH_HELD; ++j)
+                if (lane + 32 * j < K) f(lane + 32 * j, mine[j], z[j], j);
+        } else {
+            for (int k = lane; k < K; k += 32) f(k, index[k], logit(k), 0);
+        }
     };
-    for (int r = warp; r < rows; r += 8) {
-        const long long row = row0 + r;
+    if (live) {
         float top = -INFINITY;
         int first = K;                                 // of the entries with the largest logit
         bool any = false, bad = false;
-        for (int k = lane; k < K; k += 32) {
-            const long long i = a.index[row * a.ldi + k];
-            const float z = logit(row, k);
-            if (i < 0 || z == -INFINITY) continue;
+        entries([&](int k, long long i, float v, int) {
+            if (i < 0 || v == -INFINITY) return;
             any = true;
             bad = bad || i >= a.V;
-            if (z > top) { top = z; first = k; }
-        }
+            if (v > top) { top = v; first = k; }
+        });
 #pragma unroll
         for (int o = 16; o; o >>= 1) {
             const float t = __shfl_xor_sync(0xffffffffu, top, o);
@@ -75,16 +99,16 @@ __global__ void __launch_bounds__(256) k_teach(const __grid_constant__ TeachArgs
         any = __any_sync(0xffffffffu, any);
         bad = __any_sync(0xffffffffu, bad);
         float rest = 0.f;
-        for (int k = lane; k < K; k += 32) {
-            const long long i = a.index[row * a.ldi + k];
-            const float z = logit(row, k);
-            const bool there = !bad && i >= 0 && z != -INFINITY;
+        entries([&](int k, long long i, float v, int j) {
+            const bool there = !bad && i >= 0 && v != -INFINITY;
             // (a maximum that is not finite leaves NaN behind; so does a NaN)
-            const float x = there ? (z - top) * a.inv_tau : -INFINITY;
+            const float x = there ? (v - top) * a.inv_tau : -INFINITY;
             if (there && (k != first || x != x)) rest += expf(x);
+            const int c = there ? (int)i : -1;
+            if (held) col[j] = c;
             a.z[row * K + k] = x;
-            a.col[row * K + k] = there ? (int)i : -1;
-        }
+            a.col[row * K + k] = c;
+        });
 #pragma unroll
         for (int o = 16; o; o >>= 1) rest += __shfl_xor_sync(0xffffffffu, rest, o);
         if (lane == 0) {
@@ -92,26 +116,33 @@ __global__ void __launch_bounds__(256) k_teach(const __grid_constant__ TeachArgs
             a.label[row] = bad ? -2 : any ? 0 : -1;
         }
     }
-    __syncthreads();
     // the block's entries by segment, TEACH_BINS segments at a time
     int* bins = a.bins + (size_t)blockIdx.x * (a.nbins + 1);
     unsigned* out = a.entries + (size_t)blockIdx.x * TEACH_ROWS * K;
-    const int* col = a.col + row0 * K;
-    const int n = rows * K;
-    if (tid == 0) base = 0;
+    const int* cols = a.col + row * K;
+    // calls f(k, column) for the row's entries (a lane's own ones, which it has written itself)
+    const auto columns = [&](auto&& f) {
+        if (!live) return;
+        if (held) {
+#pragma unroll
+            for (int j = 0; j < TEACH_HELD; ++j)
+                if (lane + 32 * j < K && col[j] >= 0) f(lane + 32 * j, col[j]);
+        } else {
+            for (int k = lane; k < K; k += 32)
+                if (cols[k] >= 0) f(k, cols[k]);
+        }
+    };
     for (int b0 = 0; b0 < a.nbins; b0 += TEACH_BINS) {
         const int here = min(TEACH_BINS, a.nbins - b0);
-        for (int i = tid; i < TEACH_BINS; i += 256) count[i] = 0;
+        columns([&](int, int c) {
+            const int b = c / TEACH_COLS - b0;
+            if (b >= 0 && b < here) atomicAdd(count + b, 1);
+        });
         __syncthreads();
-        for (int e = tid; e < n; e += 256) {
-            const int b = col[e] / TEACH_COLS - b0;
-            if (col[e] >= 0 && b >= 0 && b < here) atomicAdd(count + b, 1);
-        }
-        __syncthreads();
-        // where each begins: eight per thread, then the threads of a warp, then the warps
-        int mine[TEACH_BINS / 256], sum = 0;
+        // where each begins: a few per thread, then the threads of a warp, then the warps
+        int mine_of[EACH], sum = 0;
 #pragma unroll
-        for (int i = 0; i < TEACH_BINS / 256; ++i) { mine[i] = count[tid * (TEACH_BINS / 256) + i]; sum += mine[i]; }
+        for (int i = 0; i < EACH; ++i) { mine_of[i] = count[tid * EACH + i]; sum += mine_of[i]; }
         int upto = sum;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -120,27 +151,36 @@ __global__ void __launch_bounds__(256) k_teach(const __grid_constant__ TeachArgs
         }
         if (lane == 31) warps[warp] = upto;
         __syncthreads();
-        int at = base + upto - sum;
-        for (int w = 0; w < warp; ++w) at += warps[w];
+        int before = lane < warp ? warps[lane] : 0, all = warps[lane];
 #pragma unroll
-        for (int i = 0; i < TEACH_BINS / 256; ++i) {
-            const int b = tid * (TEACH_BINS / 256) + i;
+        for (int o = 16; o; o >>= 1) {
+            before += __shfl_xor_sync(0xffffffffu, before, o);
+            all += __shfl_xor_sync(0xffffffffu, all, o);
+        }
+        const int begin = base;
+        int at = begin + before + upto - sum;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const int b = tid * EACH + i;
             count[b] = at;
             if (b < here) bins[b0 + b] = at;
-            at += mine[i];
+            at += mine_of[i];
         }
-        if (tid == 255) total = at;
         __syncthreads();
-        for (int e = tid; e < n; e += 256) {
-            const int c = col[e], b = c / TEACH_COLS - b0;
-            if (c < 0 || b < 0 || b >= here) continue;
-            const int r = e / K;
-            out[atomicAdd(count + b, 1)] = (unsigned)(e - r * K) << 12 | (unsigned)r << 7 | (unsigned)(c % TEACH_COLS);       // (their order within a segment does not matter)
+        columns([&](int k, int c) {
+            const int b = c / TEACH_COLS - b0;
+            if (b < 0 || b >= here) return;
+            out[atomicAdd(count + b, 1)] = (unsigned)k << 12 | (unsigned)warp << 7 | (unsigned)(c % TEACH_COLS);       // (their order within a segment does not matter)
+        });
+        if (tid == 0) {
+            base = begin + all;
+            if (b0 + TEACH_BINS >= a.nbins) bins[a.nbins] = begin + all;
         }
-        if (tid == 0) base = total;
+        if (b0 + TEACH_BINS >= a.nbins) break;
+        __syncthreads();
+        for (int i = tid; i < TEACH_BINS; i += TEACH_THREADS) count[i] = 0;
         __syncthreads();
     }
-    if (tid == 0) bins[a.nbins] = base;
 }
 
 struct TeachRows {
@@ -153,17 +193,17 @@ struct TeachRows {
 };
 
 // An entry's share of (1 + rest_q) sum q (log q - log p); nothing where q is 0, whatever p is.
-__device__ __forceinline__ double teach_term(float z, float logit, float top, float inv_tau, float log_q, float log_p) {
+__device__ __forceinline__ float teach_term(float z, float logit, float top, float inv_tau, float log_q, float log_p) {
     const float e = expf(z);
-    return e == 0.f ? 0.0 : (double)e * (double)((z - log_q) - ((logit - top) * inv_tau - log_p));
+    return e == 0.f ? 0.f : e * ((z - log_q) - ((logit - top) * inv_tau - log_p));
 }
 // the row's outputs from the sum of its terms; returns its share of the loss and of the weight
-__device__ __forceinline__ double2 write_distance(const RowsArgs& a, const TeachRows& t, int row, float top, float log_sum, double sum) {
+__device__ __forceinline__ double2 write_distance(const RowsArgs& a, const TeachRows& t, int row, float top, float log_sum, float sum) {
     const long long label = a.labels[row];
     const float w = label == 0 ? (a.weight ? a.weight[row] : 1.f) : 0.f;
     float loss = 0.f;
     if (label == -2) { loss = NAN; atomicOr(a.status, XE_W_LABEL); }
-    else if (label == 0) loss = (float)((double)t.tau * t.tau * sum / (1.0 + (double)t.rest[row]));
+    else if (label == 0) loss = t.tau * t.tau * (sum / (1.f + t.rest[row]));
     const float lse = top * t.inv_tau + log_sum;
     a.lse[row] = lse;
     if (label == 0) loss += lse - lse == 0.f ? 0.f : NAN;          // a row whose logits are not finite
@@ -180,6 +220,18 @@ __global__ void __launch_bounds__(XE_THREADS) k_teach_loss(const __grid_constant
     const float log2e = LOG2E * t.inv_tau;
     double2 share = make_double2(0.0, 0.0);
     if (row < a.rows) {
+        constexpr int HELD = 2;                        // entries per lane that are asked for before the statistics
+        const int* col = t.col + (size_t)row * t.K;
+        const float *z = t.z + (size_t)row * t.K, *logit = t.logit + (size_t)row * t.K, rest_q = t.rest[row];
+        int c[HELD];
+        float zs[HELD], ls[HELD];
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) {
+            const int k = lane + 32 * i;
+            c[i] = k < t.K ? col[k] : -1;
+            zs[i] = k < t.K ? z[k] : 0.f;
+            ls[i] = k < t.K ? logit[k] : 0.f;
+        }
         float top = -INFINITY, rest = -1.f;
         for (int j = lane; j < a.nseg; j += 8 * 32) {
             float2 s[8];
@@ -189,12 +241,13 @@ __global__ void __launch_bounds__(XE_THREADS) k_teach_loss(const __grid_constant
             for (int i = 0; i < 8; ++i) merge_stat(top, rest, s[i].x, s[i].y - 1.f, log2e);
         }
         warp_stat(top, rest, log2e);
-        const float log_p = log1pf(rest), log_q = log1pf(t.rest[row]);
-        double sum = 0.0;
-        for (int k = lane; k < t.K; k += 32) {
-            const size_t at = (size_t)row * t.K + k;
-            if (t.col[at] >= 0) sum += teach_term(t.z[at], t.logit[at], top, t.inv_tau, log_q, log_p);
-        }
+        const float log_p = log1pf(rest), log_q = log1pf(rest_q);
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < HELD; ++i)
+            if (c[i] >= 0) sum += teach_term(zs[i], ls[i], top, t.inv_tau, log_q, log_p);
+        for (int k = lane + 32 * HELD; k < t.K; k += 32)
+            if (col[k] >= 0) sum += teach_term(z[k], logit[k], top, t.inv_tau, log_q, log_p);
 #pragma unroll
         for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
         if (lane == 0) share = write_distance(a, t, row, top, log_p, sum);
@@ -213,17 +266,27 @@ __global__ void __launch_bounds__(XE_THREADS, XE_ROW_CTAS) k_teach_rows(const __
     grid_trigger();
     grid_wait();
     __shared__ float2 ws[XE_THREADS / 32];
-    __shared__ int cols[TEACH_MOST];
+    __shared__ __align__(16) int cols[TEACH_MOST];
     __shared__ float es[TEACH_MOST];                   // exp(z)
-    const int row = blockIdx.x, tid = threadIdx.x;
+    __shared__ float terms[XE_THREADS / 32];
+    const int row = blockIdx.x, tid = threadIdx.x, K = t.K;
     const float log2e = LOG2E * t.inv_tau;
     const float2* st = a.stats + (size_t)row * a.nseg;
-    for (int k = tid; k < t.K; k += XE_THREADS) {
-        cols[k] = t.col[(size_t)row * t.K + k];
-        es[k] = expf(t.z[(size_t)row * t.K + k]);
-    }
+    const float *z = t.z + (size_t)row * K, *logit = t.logit + (size_t)row * K;
+    // entry `tid` in registers, asked for before the statistics
+    int c0 = -1;
+    float z0 = -INFINITY, l0 = 0.f;
+    if (tid < K) { c0 = t.col[(size_t)row * K + tid]; z0 = z[tid]; l0 = logit[tid]; }
+    const float rest_q = t.rest[row];
+    const bool counts = a.labels[row] == 0;
+    const float w = counts ? (a.weight ? a.weight[row] : 1.f) : 0.f;
     float top = -INFINITY, rest = -1.f;
     for (int j = tid; j < a.nseg; j += XE_THREADS) merge_stat(top, rest, st[j].x, st[j].y - 1.f, log2e);
+    const int padded = (K + 3) / 4 * 4;
+    for (int k = tid; k < padded; k += XE_THREADS) {
+        cols[k] = k >= K ? -1 : k == tid ? c0 : t.col[(size_t)row * K + k];
+        es[k] = k >= K ? 0.f : expf(k == tid ? z0 : z[k]);
+    }
     warp_stat(top, rest, log2e);
     if ((tid & 31) == 0) ws[tid >> 5] = make_float2(top, rest);
     __syncthreads();
@@ -231,39 +294,45 @@ __global__ void __launch_bounds__(XE_THREADS, XE_ROW_CTAS) k_teach_rows(const __
     rest = ws[0].y;
 #pragma unroll
     for (int i = 1; i < XE_THREADS / 32; ++i) merge_stat(top, rest, ws[i].x, ws[i].y, log2e);
-    const float log_sum = log1pf(rest), rest_q = t.rest[row];
-    const float* logit = t.logit + (size_t)row * t.K;
-    if (blockIdx.y == 0) {
+    const float log_sum = log1pf(rest);
+    if (blockIdx.y == 0 && (tid & ~31) < K) {          // warps with entries
         const float log_q = log1pf(rest_q);
-        double sum = 0.0;
-        for (int k = tid; k < t.K; k += XE_THREADS)
-            if (cols[k] >= 0) sum += teach_term(t.z[(size_t)row * t.K + k], logit[k], top, t.inv_tau, log_q, log_sum);
-        const double2 s = block_sum2<XE_THREADS>(sum, 0.0);
-        if (tid == 0) a.sums[a.first_sum + row] = write_distance(a, t, row, top, log_sum, s.x);
+        float sum = c0 >= 0 ? teach_term(z0, l0, top, t.inv_tau, log_q, log_sum) : 0.f;
+        for (int k = tid + XE_THREADS; k < K; k += XE_THREADS)
+            if (cols[k] >= 0) sum += teach_term(z[k], logit[k], top, t.inv_tau, log_q, log_sum);
+#pragma unroll
+        for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if ((tid & 31) == 0) terms[tid >> 5] = sum;
     }
-    const bool counts = a.labels[row] == 0;
-    const float w = counts ? (a.weight ? a.weight[row] : 1.f) : 0.f;
     const float lse = top * t.inv_tau + log_sum, poison = lse - lse;         // 0, or NaN where the row's logits were not finite
     uint4* q = reinterpret_cast<uint4*>(a.q + (size_t)row * a.ldq);
     const int units = (a.V + 7) / 8, per = (units + gridDim.y - 1) / gridDim.y;
     const int u0 = blockIdx.y * per, u1 = min(units, u0 + per);
     rewrite_exponents(q, st, u0, u1, w, counts, poison, [&](float ref) { return ((ref - top) * t.inv_tau - log_sum) * LOG2E + poison; });
     __syncthreads();
+    if (blockIdx.y == 0 && tid == XE_THREADS - 1) {    // (a thread without an entry, mostly)
+        float sum = 0.f;
+        for (int i = 0; i < XE_THREADS / 32 && 32 * i < K; ++i) sum += terms[i];
+        a.sums[a.first_sum + row] = write_distance(a, t, row, top, log_sum, sum);
+    }
     // the entries' columns again; a column that is listed more than once by the first of its entries
     if (counts) {
         const float both = 1.f / ((1.f + rest) * (1.f + rest_q));
-        for (int k = tid; k < t.K; k += XE_THREADS) {
+        for (int k = tid; k < K; k += XE_THREADS) {
             const int c = cols[k];
             if (c < 0 || (c >> 3) < u0 || (c >> 3) >= u1) continue;
-            bool first = true;
-            float e_q = 0.f;
-            for (int j = 0; j < t.K; ++j)
-                if (cols[j] == c) {
-                    first = first && j >= k;
-                    e_q += es[j];
-                }
-            if (!first) continue;
-            const float e_p = ex2((logit[k] - top) * log2e);
+            int same = 0, before = 0;                  // entries of this column, and those of them before this one
+#pragma unroll 4
+            for (int j = 0; j < K; j += 4) {
+                const int4 four = *reinterpret_cast<const int4*>(cols + j);
+                same += (four.x == c) + (four.y == c) + (four.z == c) + (four.w == c);
+                before += (four.x == c && j < k) + (four.y == c && j + 1 < k) + (four.z == c && j + 2 < k) + (four.w == c && j + 3 < k);
+            }
+            if (before) continue;
+            float e_q = es[k];
+            if (same > 1)
+                for (int j = k + 1; j < K; ++j) e_q += cols[j] == c ? es[j] : 0.f;
+            const float e_p = ex2(((k == tid ? l0 : logit[k]) - top) * log2e);
             const float d = (((e_p - e_q) + e_p * rest_q) - e_q * rest) * both + poison;
             reinterpret_cast<__nv_bfloat16*>(q)[c] = __float2bfloat16_rn(d * w);
         }

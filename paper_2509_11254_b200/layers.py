@@ -16,13 +16,12 @@ from collections import namedtuple
 import torch
 
 from .binding import PSGDError, lib
-from .training import _BF16, _DTYPES, ActivationCheckpoint, _check, _empty, _here, _matrix, _name, _no_graph, _there, _vector, _workspace_bytes
+from .training import _BF16, _BOTH, _DTYPES, ActivationCheckpoint, _check, _empty, _here, _matrix, _name, _no_graph, _there, _vector, _workspace_bytes
 
 LayerNorm = namedtuple("LayerNorm", "y x mean rstd kept")
 LayerNormGrad = namedtuple("LayerNormGrad", "d_x d_weight d_bias")
 
 _LAYOUTS = {"half": 0, "interleaved": 1}
-_BOTH = tuple(_DTYPES)
 _empty_like = torch.empty_like
 
 

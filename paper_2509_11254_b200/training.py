@@ -33,6 +33,7 @@ GROUP = 32
 _MOST_ENTRIES = 1024           # of a token's teacher
 _BF16 = torch.bfloat16
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1}
+_BOTH = tuple(_DTYPES)
 
 CrossEntropy = namedtuple("CrossEntropy", "loss token_loss lse")
 CrossEntropyGrad = namedtuple("CrossEntropyGrad", "loss token_loss lse d_hidden d_weight")
@@ -79,7 +80,7 @@ def _matrix(t, name, dtypes=(_BF16,), shape=None, device=None):
 
 def _vector(t, name, dtype, n, device):
     """The address of a contiguous CUDA vector."""
-    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.ndim != 1 or len(t) != n or not t.is_contiguous() or t.get_device() != device.index:
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.shape != (n,) or not t.is_contiguous() or t.get_device() != device.index:
         raise PSGDError(f"{name} must be a contiguous {_name(dtype)} tensor of {n} elements on {device}")
     return t.data_ptr()
 
@@ -164,8 +165,8 @@ def _last_layer(grad, hidden, weight, target, token_weight, d_hidden, d_weight, 
     teacher = len(target) == 3
     if teacher:
         logits, index, temperature = target
-        _, K, ldl = _matrix(logits, "teacher_logits", tuple(_DTYPES), device=dev)
-        if not 1 <= K <= _MOST_ENTRIES or len(logits) != T:
+        entries, K, ldl = _matrix(logits, "teacher_logits", _BOTH, device=dev)
+        if not 1 <= K <= _MOST_ENTRIES or entries != T:
             raise PSGDError(f"teacher_logits must have shape ({T}, 1 to {_MOST_ENTRIES}), not {tuple(logits.shape)}")
         ldi = _matrix(index, "teacher_index", (torch.int64,), (T, K), dev)[2]
         if not 1e-3 <= temperature <= 1e3:
@@ -282,7 +283,7 @@ class ActivationCheckpoint:
         T, F = self.shape
         ld = F
         if out is not None:
-            ld = _matrix(out, "out", tuple(_DTYPES), self.shape, self.device)[2]
+            ld = _matrix(out, "out", _BOTH, self.shape, self.device)[2]
         elif dtype not in _DTYPES:
             raise PSGDError("dtype must be float32 or bfloat16")
         s = _here(self.device, stream)
@@ -297,7 +298,7 @@ class ActivationCheckpoint:
 
 def pack_activation(x, stream=None):
     """x [T, F] (bfloat16 or float32) in 8 bits: an ActivationCheckpoint."""
-    T, F, ld = _matrix(x, "x", tuple(_DTYPES))
+    T, F, ld = _matrix(x, "x", _BOTH)
     s = _here(x.device, stream)
     if s is None:
         with _there(x.device, stream, x):
@@ -326,7 +327,7 @@ def weight_gradient(dy, kept, dtype=torch.float32, out=None, status=None, stream
         raise PSGDError(f"dy has {T} rows, the checkpoint {kept.shape[0]}")
     F = ldo = kept.shape[1]
     if out is not None:
-        ldo = _matrix(out, "out", tuple(_DTYPES), (O, F), dev)[2]
+        ldo = _matrix(out, "out", _BOTH, (O, F), dev)[2]
     elif dtype not in _DTYPES:
         raise PSGDError("dtype must be float32 or bfloat16")
     at_status = _status(status, dev)
