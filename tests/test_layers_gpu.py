@@ -552,3 +552,17 @@ def test_norm_rows_of_every_alignment(torch, ops, T, F):
         check_backward(torch, ops, fwd, w, dy, d_x, True, True)
         fwd = check_forward(torch, ops, x, w, None, None, 1e-5, False, False, None)
         check_backward(torch, ops, fwd, w, dy, None, False, False)
+
+
+def test_norm_sums_of_bfloat16_are_rounded_once(torch, ops):
+    """x + residual over all exponents: subnormal numbers, zeros of either sign, overflow, infinities, ties between two neighbours."""
+    g = gen(torch, 1)
+    bits = torch.randint(-(1 << 15), 1 << 15, (2, 64, 2048), generator=g, device="cuda", dtype=torch.int32).to(torch.int16)
+    x, r = bits.view(torch.bfloat16)
+    r[::2] = (x[::2].float() * (torch.randint(-9, 10, x[::2].shape, generator=g, device="cuda") / 512)).bfloat16()      # near enough for ties
+    r[0, :4], x[0, :4] = torch.tensor([0.0, -0.0, 0.0, -0.0]).bfloat16(), torch.tensor([0.0, 0.0, -0.0, -0.0]).bfloat16()
+    w = torch.ones(2048, device="cuda")
+    for F in (2048, 2047):
+        got, want = ops.layer_norm_forward(x[:, :F], w[:F], residual=r[:, :F]).x, (x[:, :F].float() + r[:, :F].float()).bfloat16()
+        nan = torch.isnan(want)
+        assert torch.equal(torch.isnan(got), nan) and torch.equal(got.view(torch.int16)[~nan], want.contiguous().view(torch.int16)[~nan])
