@@ -189,7 +189,7 @@ struct XentPlan {
     int64_t ldq, piece, pieces;
     TilePlan logits, two[2];          // of a whole piece; two: dH and dW
     size_t inv, done, sums, stats, label_logit, q, part, acc, total;
-    int nbins;                        // with a teacher: segments of 128 columns
+    int nbins;                        // with a teacher: blocks of 32 columns
     size_t z, col, rest, label, bins, entries;
 };
 // Tokens are taken in pieces, all columns at a time, so that the stored exponents (loss alone: the statistics) stay within a fixed size however
@@ -220,11 +220,11 @@ XentPlan plan_xent(int64_t T, int64_t V, int64_t D, bool grad, int64_t K) {
     x.stats = take((size_t)x.piece * x.nseg * 8);
     x.label_logit = take((size_t)x.piece * std::max<int64_t>(1, K) * 4);
     if (K > 0) {
-        const int64_t blocks = (T + TEACH_ROWS - 1) / TEACH_ROWS;
+        const int64_t blocks = ceil_div(x.piece, TEACH_ROWS);
         x.nbins = ceil_div(V, TEACH_COLS);
-        x.z = take((size_t)T * K * 4);
-        x.col = take((size_t)T * K * 4);
-        x.rest = take((size_t)T * 4);
+        x.z = take((size_t)x.piece * K * 4);
+        x.col = take((size_t)x.piece * K * 4);
+        x.rest = take((size_t)x.piece * 4);
         x.label = take((size_t)T * 8);
         x.bins = take((size_t)blocks * (x.nbins + 1) * 4);
         x.entries = take((size_t)blocks * TEACH_ROWS * K * 4);
@@ -269,22 +269,27 @@ psgd_status xent(const void* H, int64_t ldh, const void* W, int64_t ldw, const i
     float* inv = (float*)(w + x.inv);
     int* done = (int*)(w + x.done);
 
-    TeachArgs teach{};
+    TeachArgs teach{};                                // of a piece
     TeachRows listed{};
     if (teacher) {
         const float inv_tau = (float)(1.0 / (double)teacher->tau);
-        teach.T = T; teach.V = (int)V; teach.K = (int)teacher->K;
-        teach.logits = teacher->logits; teach.bf16 = teacher->dtype == PSGD_DT_BF16; teach.ldl = teacher->ldl;
-        teach.index = (const long long*)teacher->index; teach.ldi = teacher->ldi;
+        teach.V = (int)V; teach.K = (int)teacher->K;
+        teach.bf16 = teacher->dtype == PSGD_DT_BF16; teach.ldl = teacher->ldl; teach.ldi = teacher->ldi;
         teach.inv_tau = inv_tau; teach.nbins = x.nbins;
-        teach.z = (float*)(w + x.z); teach.col = (int*)(w + x.col); teach.rest = (float*)(w + x.rest); teach.label = (long long*)(w + x.label);
-        teach.bins = (int*)(w + x.bins); teach.entries = (unsigned*)(w + x.entries);
+        teach.z = (float*)(w + x.z); teach.col = (int*)(w + x.col); teach.rest = (float*)(w + x.rest);
         listed.K = teach.K; listed.tau = teacher->tau; listed.inv_tau = inv_tau;
+        listed.z = teach.z; listed.col = teach.col; listed.rest = teach.rest;
         listed.logit = (const float*)(w + x.label_logit);
-        labels = (const int64_t*)teach.label;                 // 0 where a row counts
+        labels = (const int64_t*)(w + x.label);       // 0 where a row counts
         ignore = -1;
-        if (!launch(k_teach, dim3(ceil_div(T, TEACH_ROWS)), dim3(TEACH_THREADS), 0, st, teach)) return PSGD_E_CUDA;
+        if (grad && x.pieces > 1) {                   // the first piece's gradients are divided by all rows' weights
+            TeachArgs all = teach;
+            all.T = T; all.logits = teacher->logits; all.index = (const long long*)teacher->index; all.label = (long long*)(w + x.label);
+            if (!launch(k_teach, dim3(ceil_div(T, TEACH_ROWS)), dim3(TEACH_THREADS), 0, st, all)) return PSGD_E_CUDA;
+        }
+        teach.bins = (int*)(w + x.bins); teach.entries = (unsigned*)(w + x.entries);
     }
+
     RowsArgs r{};
     r.V = (int)V; r.nseg = x.nseg;
     r.stats = (const float2*)(w + x.stats);
@@ -317,13 +322,16 @@ psgd_status xent(const void* H, int64_t ldh, const void* W, int64_t ldw, const i
             a.norm = inv; a.norm_labels = (const long long*)labels; a.norm_weight = weight; a.norm_rows = T; a.ignore = ignore;
         }
         if (teacher) {
-            const int64_t block = t0 / TEACH_ROWS;            // (pieces are whole row tiles)
-            a.bins = teach.bins + block * (x.nbins + 1);
-            a.entries = teach.entries + block * TEACH_ROWS * teach.K;
+            teach.T = rows;
+            teach.logits = (const char*)teacher->logits + (size_t)t0 * teacher->ldl * size_of(teacher->dtype);
+            teach.index = (const long long*)teacher->index + (size_t)t0 * teacher->ldi;
+            teach.label = (long long*)(w + x.label) + t0;
+            if (!launch(k_teach, dim3(ceil_div(rows, TEACH_ROWS)), dim3(TEACH_THREADS), 0, st, teach)) return PSGD_E_CUDA;
+            a.bins = teach.bins;
+            a.entries = teach.entries;
             a.entry_logit = a.label_logit;
             a.nbins = x.nbins; a.K = teach.K;
             a.temperature = teacher->tau; a.log2e = LOG2E * teach.inv_tau;
-            listed.z = teach.z + t0 * teach.K; listed.col = teach.col + t0 * teach.K; listed.rest = teach.rest + t0;
         }
         const bool whole = rows == x.piece;
         const TilePlan pl = whole ? x.logits : plan_tiles(rows, V, D, x.pairs, false);

@@ -5,8 +5,8 @@
 //   loss = sum_t w_t loss_t / Z,   Z = sum of w_t over the rows that have an entry   (0 where Z = 0),
 //   d loss / d l_tv = w_t tau (p_tv - sum of q_k over the entries of column v) / Z.
 //
-// k_teach goes before the product: the teacher's probabilities, and the entries of every 32 rows ordered by segments of 128 columns, which is what a warp of
-// the product's epilogue holds at a time, so that it finds the entries whose logits it has without a search.  It leaves the logits of all entries
+// k_teach goes before the product: the teacher's probabilities, and the entries of every 32 rows ordered by blocks of 32 columns, which is what a warp of
+// the product's epilogue turns into rows at a time, so that it finds the entries whose logits it has without a search.  It leaves the logits of all entries
 // in float32; the other columns take the way of the cross entropy (psgd_xent.cuh): exponents in 16 bits, rewritten in place as bfloat16 gradients, here of
 // l / tau.  At the entries' columns the gradient comes from the unrounded logit.  As there, sums of exponentials are kept without the 1 of their
 // maximum: p - q of a column of which both are sure is ((e_p - e_q) + e_p rest_q - e_q rest_p) / ((1 + rest_p) (1 + rest_q)), e the exponential relative to the maximum.
@@ -19,10 +19,11 @@
 namespace psgd {
 
 constexpr int TEACH_ROWS = 32;     // rows of a block of entries
-constexpr int TEACH_COLS = 128;    // columns of a segment
-constexpr int TEACH_BINS = 2048;   // segments that k_teach counts at a time
+constexpr int TEACH_COLS = 32;     // columns of a block
+constexpr int TEACH_BINS = 4096;   // blocks of columns that k_teach counts at a time
 constexpr int TEACH_THREADS = 1024;
 constexpr int TEACH_HELD = 4;      // entries per lane that k_teach keeps in registers
+constexpr int TEACH_PAIRS = 128;   // entries of a row up to which k_teach_rows compares every pair
 constexpr int TEACH_MOST = 1024;   // entries of a row (k_teach_rows holds a row's in shared memory)
 
 struct TeachArgs {
@@ -39,8 +40,8 @@ struct TeachArgs {
     int* col;                      // [T][K] column, -1: no entry
     float* rest;                   // [T] sum of exp(z) without the maximum's 1
     long long* label;              // [T] 0: the row counts, -1: it has no entry, -2: an entry's column does not exist
-    int* bins;                     // [blocks][nbins + 1]
-    unsigned* entries;             // [blocks][32 K]
+    int* bins;                     // [row blocks][nbins + 1]; nullptr: only `label` is written
+    unsigned* entries;             // [row blocks][32 K]
 };
 
 // One CTA per 32 rows, a warp per row.  Bound by latency (10 or 12 bytes per entry are read and 12 written): a row's entries are all asked for at once and held in
@@ -98,6 +99,8 @@ __global__ void __launch_bounds__(TEACH_THREADS) k_teach(const __grid_constant__
         }
         any = __any_sync(0xffffffffu, any);
         bad = __any_sync(0xffffffffu, bad);
+        if (lane == 0) a.label[row] = bad ? -2 : any ? 0 : -1;
+        if (!a.bins) return;
         float rest = 0.f;
         entries([&](int k, long long i, float v, int j) {
             const bool there = !bad && i >= 0 && v != -INFINITY;
@@ -111,12 +114,10 @@ __global__ void __launch_bounds__(TEACH_THREADS) k_teach(const __grid_constant__
         });
 #pragma unroll
         for (int o = 16; o; o >>= 1) rest += __shfl_xor_sync(0xffffffffu, rest, o);
-        if (lane == 0) {
-            a.rest[row] = rest;
-            a.label[row] = bad ? -2 : any ? 0 : -1;
-        }
+        if (lane == 0) a.rest[row] = rest;
     }
-    // the block's entries by segment, TEACH_BINS segments at a time
+    if (!a.bins) return;
+    // the rows' entries by block of columns, TEACH_BINS blocks at a time
     int* bins = a.bins + (size_t)blockIdx.x * (a.nbins + 1);
     unsigned* out = a.entries + (size_t)blockIdx.x * TEACH_ROWS * K;
     const int* cols = a.col + row * K;
@@ -170,7 +171,7 @@ __global__ void __launch_bounds__(TEACH_THREADS) k_teach(const __grid_constant__
         columns([&](int k, int c) {
             const int b = c / TEACH_COLS - b0;
             if (b < 0 || b >= here) return;
-            out[atomicAdd(count + b, 1)] = (unsigned)k << 12 | (unsigned)warp << 7 | (unsigned)(c % TEACH_COLS);       // (their order within a segment does not matter)
+            out[atomicAdd(count + b, 1)] = (unsigned)k << 10 | (unsigned)warp << 5 | (unsigned)(c % TEACH_COLS);       // (their order within a block does not matter)
         });
         if (tid == 0) {
             base = begin + all;
@@ -198,12 +199,10 @@ __device__ __forceinline__ float teach_term(float z, float logit, float top, flo
     return e == 0.f ? 0.f : e * ((z - log_q) - ((logit - top) * inv_tau - log_p));
 }
 // the row's outputs from the sum of its terms; returns its share of the loss and of the weight
-__device__ __forceinline__ double2 write_distance(const RowsArgs& a, const TeachRows& t, int row, float top, float log_sum, float sum) {
-    const long long label = a.labels[row];
-    const float w = label == 0 ? (a.weight ? a.weight[row] : 1.f) : 0.f;
+__device__ __forceinline__ double2 write_distance(const RowsArgs& a, const TeachRows& t, int row, long long label, float w, float rest_q, float top, float log_sum, float sum) {
     float loss = 0.f;
     if (label == -2) { loss = NAN; atomicOr(a.status, XE_W_LABEL); }
-    else if (label == 0) loss = t.tau * t.tau * (sum / (1.f + t.rest[row]));
+    else if (label == 0) loss = t.tau * t.tau * (sum / (1.f + rest_q));
     const float lse = top * t.inv_tau + log_sum;
     a.lse[row] = lse;
     if (label == 0) loss += lse - lse == 0.f ? 0.f : NAN;          // a row whose logits are not finite
@@ -223,6 +222,8 @@ __global__ void __launch_bounds__(XE_THREADS) k_teach_loss(const __grid_constant
         constexpr int HELD = 2;                        // entries per lane that are asked for before the statistics
         const int* col = t.col + (size_t)row * t.K;
         const float *z = t.z + (size_t)row * t.K, *logit = t.logit + (size_t)row * t.K, rest_q = t.rest[row];
+        const long long label = a.labels[row];
+        const float weight = a.weight ? a.weight[row] : 1.f;
         int c[HELD];
         float zs[HELD], ls[HELD];
 #pragma unroll
@@ -250,7 +251,7 @@ __global__ void __launch_bounds__(XE_THREADS) k_teach_loss(const __grid_constant
             if (col[k] >= 0) sum += teach_term(z[k], logit[k], top, t.inv_tau, log_q, log_p);
 #pragma unroll
         for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        if (lane == 0) share = write_distance(a, t, row, top, log_p, sum);
+        if (lane == 0) share = write_distance(a, t, row, label, label == 0 ? weight : 0.f, rest_q, top, log_p, sum);
     }
     if (lane == 0) mine[warp] = share;
     __syncthreads();
@@ -261,13 +262,19 @@ __global__ void __launch_bounds__(XE_THREADS) k_teach_loss(const __grid_constant
     report_rows(a);
 }
 
-// Loss and gradient of the logits: blockIdx.x = row, blockIdx.y = part of its columns.
+__device__ __forceinline__ unsigned first_slot(int column) { return (unsigned)column * 2654435761u >> 16; }     // (multiplied by 2^32 / golden ratio: its upper bits spread)
+
+// Loss and gradient of the logits: blockIdx.x = row, blockIdx.y = part of its columns.  Columns that a row lists more than once are found by comparing every pair of its
+// entries where there are up to TEACH_PAIRS, else through a hash table (64 entries: 104 us on 4096 x 32000, 112 with the table; 1024 entries: a step of 4096 x 32000 x 768
+// in 2060 us by pairs, 770 with the table).
 __global__ void __launch_bounds__(XE_THREADS, XE_ROW_CTAS) k_teach_rows(const __grid_constant__ RowsArgs a, const __grid_constant__ TeachRows t) {
     grid_trigger();
     grid_wait();
     __shared__ float2 ws[XE_THREADS / 32];
     __shared__ __align__(16) int cols[TEACH_MOST];
     __shared__ float es[TEACH_MOST];                   // exp(z)
+    __shared__ int seen[2 * TEACH_MOST];               // hash table of the listed columns, -1: free; bit 30: listed more than once
+    constexpr int TWICE = 1 << 30;
     __shared__ float terms[XE_THREADS / 32];
     const int row = blockIdx.x, tid = threadIdx.x, K = t.K;
     const float log2e = LOG2E * t.inv_tau;
@@ -277,15 +284,17 @@ __global__ void __launch_bounds__(XE_THREADS, XE_ROW_CTAS) k_teach_rows(const __
     int c0 = -1;
     float z0 = -INFINITY, l0 = 0.f;
     if (tid < K) { c0 = t.col[(size_t)row * K + tid]; z0 = z[tid]; l0 = logit[tid]; }
-    const float rest_q = t.rest[row];
-    const bool counts = a.labels[row] == 0;
-    const float w = counts ? (a.weight ? a.weight[row] : 1.f) : 0.f;
+    const float rest_q = t.rest[row], weight = a.weight ? a.weight[row] : 1.f;
+    const long long label = a.labels[row];
+    const bool counts = label == 0, hashed = K > TEACH_PAIRS;
+    const float w = counts ? weight : 0.f;
     float top = -INFINITY, rest = -1.f;
     for (int j = tid; j < a.nseg; j += XE_THREADS) merge_stat(top, rest, st[j].x, st[j].y - 1.f, log2e);
-    const int padded = (K + 3) / 4 * 4;
-    for (int k = tid; k < padded; k += XE_THREADS) {
-        cols[k] = k >= K ? -1 : k == tid ? c0 : t.col[(size_t)row * K + k];
-        es[k] = k >= K ? 0.f : expf(k == tid ? z0 : z[k]);
+    const unsigned slots = 2u << (32 - __clz(K - 1));  // the power of two from 2 K on
+    for (int k = tid; hashed && k < (int)slots; k += XE_THREADS) seen[k] = -1;
+    for (int k = tid; k < (K + 3) / 4 * 4; k += XE_THREADS) {
+        cols[k] = k == tid ? c0 : k < K ? t.col[(size_t)row * K + k] : -1;
+        es[k] = k == tid ? expf(z0) : k < K ? expf(z[k]) : 0.f;
     }
     warp_stat(top, rest, log2e);
     if ((tid & 31) == 0) ws[tid >> 5] = make_float2(top, rest);
@@ -308,12 +317,21 @@ __global__ void __launch_bounds__(XE_THREADS, XE_ROW_CTAS) k_teach_rows(const __
     uint4* q = reinterpret_cast<uint4*>(a.q + (size_t)row * a.ldq);
     const int units = (a.V + 7) / 8, per = (units + gridDim.y - 1) / gridDim.y;
     const int u0 = blockIdx.y * per, u1 = min(units, u0 + per);
+    for (int k = tid; hashed && counts && k < K; k += XE_THREADS) {
+        const int c = cols[k];
+        if (c < 0 || (c >> 3) < u0 || (c >> 3) >= u1) continue;
+        for (unsigned at = first_slot(c), n = 0; n < slots; ++at, ++n) {     // (half of the table stays free: it ends long before)
+            const int old = atomicCAS(seen + (at & (slots - 1)), -1, c);
+            if (old == -1) break;
+            if ((old & ~TWICE) == c) { atomicOr(seen + (at & (slots - 1)), TWICE); break; }
+        }
+    }
     rewrite_exponents(q, st, u0, u1, w, counts, poison, [&](float ref) { return ((ref - top) * t.inv_tau - log_sum) * LOG2E + poison; });
     __syncthreads();
     if (blockIdx.y == 0 && tid == XE_THREADS - 1) {    // (a thread without an entry, mostly)
         float sum = 0.f;
         for (int i = 0; i < XE_THREADS / 32 && 32 * i < K; ++i) sum += terms[i];
-        a.sums[a.first_sum + row] = write_distance(a, t, row, top, log_sum, sum);
+        a.sums[a.first_sum + row] = write_distance(a, t, row, label, w, rest_q, top, log_sum, sum);
     }
     // the entries' columns again; a column that is listed more than once by the first of its entries
     if (counts) {
@@ -321,16 +339,26 @@ __global__ void __launch_bounds__(XE_THREADS, XE_ROW_CTAS) k_teach_rows(const __
         for (int k = tid; k < K; k += XE_THREADS) {
             const int c = cols[k];
             if (c < 0 || (c >> 3) < u0 || (c >> 3) >= u1) continue;
-            int same = 0, before = 0;                  // entries of this column, and those of them before this one
+            bool many = false, first = true;           // whether its column is listed more than once, and not before
+            if (hashed) {
+                unsigned at = first_slot(c);
+                for (unsigned n = 0; n < slots && (seen[at & (slots - 1)] & ~TWICE) != c; ++n) ++at;
+                many = seen[at & (slots - 1)] & TWICE;
+                for (int j = 0; many && j < k; ++j) first = first && cols[j] != c;
+            } else {
+                int same = 0, before = 0;
 #pragma unroll 4
-            for (int j = 0; j < K; j += 4) {
-                const int4 four = *reinterpret_cast<const int4*>(cols + j);
-                same += (four.x == c) + (four.y == c) + (four.z == c) + (four.w == c);
-                before += (four.x == c && j < k) + (four.y == c && j + 1 < k) + (four.z == c && j + 2 < k) + (four.w == c && j + 3 < k);
+                for (int j = 0; j < K; j += 4) {
+                    const int4 four = *reinterpret_cast<const int4*>(cols + j);
+                    same += (four.x == c) + (four.y == c) + (four.z == c) + (four.w == c);
+                    before += (four.x == c && j < k) + (four.y == c && j + 1 < k) + (four.z == c && j + 2 < k) + (four.w == c && j + 3 < k);
+                }
+                many = same > 1;
+                first = before == 0;
             }
-            if (before) continue;
+            if (!first) continue;
             float e_q = es[k];
-            if (same > 1)
+            if (many)
                 for (int j = k + 1; j < K; ++j) e_q += cols[j] == c ? es[j] : 0.f;
             const float e_p = ex2(((k == tid ? l0 : logit[k]) - top) * log2e);
             const float d = (((e_p - e_q) + e_p * rest_q) - e_q * rest) * both + poison;

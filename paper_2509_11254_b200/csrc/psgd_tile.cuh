@@ -89,9 +89,9 @@ struct TileArgs {
     long long ldq;
     int nseg;                  // statistics per row
     int* done;                 // counter to clear for the next kernel, or nullptr
-    // EPI_TEACH_LOSS, EPI_TEACH: the listed entries by block of 32 rows and segment of 128 columns (k_teach)
-    const int* bins;           // [blocks][nbins + 1]: where a segment's entries begin among its block's
-    const unsigned* entries;   // [blocks][32 K]: place in the row's list << 12 | row of the block << 7 | column of the segment
+    // EPI_TEACH_LOSS, EPI_TEACH: the listed entries by block of 32 rows and 32 columns (k_teach)
+    const int* bins;           // [row blocks][nbins + 1]: where a block's entries begin among those of its rows
+    const unsigned* entries;   // [row blocks][32 K]: place in the row's list << 10 | row of the block << 5 | column of the block
     float* entry_logit;        // [M][K]
     int nbins, K;
     float log2e;               // log2(e) / temperature
@@ -507,27 +507,29 @@ k_tile(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtenso
                 const int row = w.m0 + rank * 128 + quarter * 32 + lane;
                 return row < p.M ? a.labels[row] : -1ll;
             };
-            // the entries of this warp's block of rows and columns: where they begin and end is asked for a tile ahead, the first 32 with the tile
+            // where the entries of this warp's four blocks begin (lanes 0-3) and end (lane 4): asked for a tile ahead, the first 32 entries with the tile
             auto bin_of = [&](const TileUnit& w) {
                 const int row = w.m0 + rank * 128 + quarter * 32, col = w.n0 + share * 128;
-                if (row >= p.M || col >= p.N) return make_int2(0, 0);
-                const int* at = a.bins + (size_t)(row >> 5) * (a.nbins + 1) + (col >> 7);
-                return make_int2(at[0], at[1]);
+                return row < p.M && col < p.N && lane < 5 ? a.bins[(size_t)(row >> 5) * (a.nbins + 1) + min((col >> 5) + lane, a.nbins)] : 0;
             };
             const float log2e = TEACH ? a.log2e : LOG2E;
             TileUnit next;
             bool going = tile_unit(a, 0, next);
             long long next_label = !TEACH && going ? label_of(next) : -1ll;
-            int2 next_bin = TEACH && going ? bin_of(next) : make_int2(0, 0);
+            int next_bin = TEACH && going ? bin_of(next) : 0;
             for (; going; ++it) {
                 const TileUnit w = next;
                 const int row0 = w.m0 + rank * 128 + quarter * 32, col_base = w.n0 + share * 128, row = row0 + lane;
                 const int b = it & 1;
                 const int label_col = (int)min(max(next_label - (long long)col_base, -1ll), 128ll);   // among this warp's columns
-                const int2 bin = next_bin;
+                const int bin = next_bin;
                 const unsigned* listed = a.entries + (size_t)(row0 >> 5) * 32 * a.K;
-                unsigned entry = ~0u;                          // (no list reaches that far: its place would be 2^20 - 1)
-                if (TEACH && bin.x + lane < bin.y) entry = listed[bin.x + lane];
+                int held = 0;                                  // the place of `entry` among its rows' entries
+                unsigned entry = 0u;
+                if constexpr (TEACH) {
+                    held = __shfl_sync(0xffffffffu, bin, 0) + lane;
+                    if (held < __shfl_sync(0xffffffffu, bin, 4)) entry = listed[held];
+                }
                 going = tile_unit(a, it + 1, next);
                 if (!TEACH && going) next_label = label_of(next);        // asked for a tile ahead
                 if (TEACH && going) next_bin = bin_of(next);
@@ -558,25 +560,27 @@ k_tile(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtenso
                         // 32 columns at a time through shared memory, where any entry lies among them: a lane per entry fetches its row's
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
-                            bool here = false;
-                            for (int e0 = bin.x; e0 < bin.y; e0 += 32) {
-                                const unsigned e = e0 == bin.x ? entry : e0 + lane < bin.y ? listed[e0 + lane] : ~0u;
-                                const bool mine = e != ~0u && (int)(e >> 5 & 3u) == 2 * c + h;
-                                if (!__any_sync(0xffffffffu, mine)) continue;
-                                if (!here) {
+                            const int lo = __shfl_sync(0xffffffffu, bin, 2 * c + h), hi = __shfl_sync(0xffffffffu, bin, 2 * c + h + 1);
+                            if (lo == hi) continue;
 #pragma unroll
-                                    for (int j = 0; j < 8; ++j)
-                                        xb[lane * 8 + (j ^ (lane & 7))] = make_uint4(__float_as_uint(v[h][4 * j]), __float_as_uint(v[h][4 * j + 1]), __float_as_uint(v[h][4 * j + 2]),
-                                                                                     __float_as_uint(v[h][4 * j + 3]));
-                                    __syncwarp();
-                                    here = true;
-                                }
-                                if (mine) {
-                                    const int r = e >> 7 & 31u, col = e & 31u;
-                                    a.entry_logit[(size_t)(row0 + r) * a.K + (e >> 12)] = reinterpret_cast<const float*>(xb)[(r * 8 + ((col >> 2) ^ (r & 7))) * 4 + (col & 3)];
-                                }
+                            for (int j = 0; j < 8; ++j)
+                                xb[lane * 8 + (j ^ (lane & 7))] = make_uint4(__float_as_uint(v[h][4 * j]), __float_as_uint(v[h][4 * j + 1]), __float_as_uint(v[h][4 * j + 2]),
+                                                                             __float_as_uint(v[h][4 * j + 3]));
+                            __syncwarp();
+                            const auto fetch = [&](unsigned e) {
+                                const int r = e >> 5 & 31u, col = e & 31u;
+                                a.entry_logit[(size_t)(row0 + r) * a.K + (e >> 10)] = reinterpret_cast<const float*>(xb)[(r * 8 + ((col >> 2) ^ (r & 7))) * 4 + (col & 3)];
+                            };
+                            if (held >= lo && held < hi) fetch(entry);
+                            for (int e0 = max(lo + lane, held + 32); e0 < hi; e0 += 4 * 32) {      // (the places of a lane are 32 apart) more than a warp holds: four at a time
+                                unsigned e[4];
+#pragma unroll
+                                for (int j = 0; j < 4; ++j) e[j] = e0 + 32 * j < hi ? listed[e0 + 32 * j] : 0u;
+#pragma unroll
+                                for (int j = 0; j < 4; ++j)
+                                    if (e0 + 32 * j < hi) fetch(e[j]);
                             }
-                            if (here) __syncwarp();
+                            __syncwarp();
                         }
                     } else if (__any_sync(0xffffffffu, (label_col >> 6) == c)) {
 #pragma unroll

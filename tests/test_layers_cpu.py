@@ -121,9 +121,11 @@ def test_distillation_refuses_before_any_launch(L):
 
 
 def test_distillation_workspace(L):
-    """Beyond the cross entropy's: 16 bytes per entry, 12 per token, 4 per 32 rows and 128 columns."""
+    """Beyond the cross entropy's: 8 bytes per token, and for the tokens of a piece 16 bytes per entry, 4 per token and 4 per 32 tokens and 32 columns; a piece has at most 2^29 logits
+    (with gradients) or 2^32 (loss alone), or 1024 tokens."""
     a, b = C.c_size_t(), C.c_size_t()
-    for T, V, D, K, grad in ((1, 32000, 768, 8, 0), (777, 50257, 768, 50, 0), (4096, 32000, 768, 64, 1), (1 << 20, 131072, 1024, 32, 1)):
+    for T, V, D, K, grad in ((1, 32000, 768, 8, 0), (777, 50257, 768, 50, 0), (4096, 32000, 768, 64, 1), (1 << 20, 131072, 1024, 32, 1), (1 << 22, 131072, 1024, 64, 0), (1 << 20, 1000, 64, 1024, 1)):
         assert L.psgd_distill_workspace(T, V, D, K, grad, C.byref(a)) == 0 and L.psgd_xent_workspace(T, V, D, grad, C.byref(b)) == 0
-        blocks = (T + 31) // 32
-        assert b.value <= a.value <= b.value + T * (12 * K + 12) + blocks * (128 * K + 4 * (V // 128 + 2)) + 4096
+        piece = min(T, max(1024, (1 << (29 if grad else 32)) // V) + 256)
+        blocks = (piece + 31) // 32
+        assert b.value <= a.value <= b.value + 8 * T + piece * (12 * K + 4) + blocks * (128 * K + 4 * (V // 32 + 2)) + 4096
