@@ -714,8 +714,8 @@ __device__ __forceinline__ void sum_warps(float& s1, float& s2, float2* mine) {
     }
 }
 // At the end: the CTA's sums of dw and db, its rows side by side (threadIdx.y) through `sums` [blockDim.y][2][F]; a CTA alone writes the results.  `column(i, j)`: of value j
-// of the thread's unit i, `n`: how many of its values exist.
-template <int VPT, typename Column>
+// of the thread's unit i (FOUR: four of them side by side at a multiple of four), `n`: how many of its values exist.
+template <int VPT, bool FOUR, typename Column>
 __device__ __forceinline__ void write_columns(const NormBackward& a, float* sums, const Eight (&dw)[VPT], const Eight (&db)[VPT], const int (&n)[VPT], Column&& column) {
     const int F = a.F;
     float* pw = gridDim.x == 1 ? a.dw : a.part + (size_t)blockIdx.x * 2 * F;
@@ -723,11 +723,22 @@ __device__ __forceinline__ void write_columns(const NormBackward& a, float* sums
     const bool alone = blockDim.y == 1;
     if (!alone) __syncthreads();                       // (nobody reads what lay there)
     float *to_w = alone ? pw : sums + (size_t)threadIdx.y * 2 * F, *to_b = alone ? pb : to_w + F;
+    const bool whole = (((uintptr_t)to_w | (uintptr_t)to_b) & 15) == 0;
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
         float p[8], q[8];
         singles(dw[i], p);
         singles(db[i], q);
+        if (FOUR && whole) {
+#pragma unroll
+            for (int j = 0; j < 8; j += 4)
+                if (j < n[i]) {
+                    const int c = column(i, j);
+                    *reinterpret_cast<float4*>(to_w + c) = make_float4(p[j], p[j + 1], p[j + 2], p[j + 3]);
+                    if (to_b) *reinterpret_cast<float4*>(to_b + c) = make_float4(q[j], q[j + 1], q[j + 2], q[j + 3]);
+                }
+            continue;
+        }
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             if (j < n[i]) {
@@ -836,7 +847,7 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_backward(const __grid_con
         from = stages == 1 || from != ring ? ring : ring + stage;
     }
     asm volatile("cp.async.wait_all;\n" ::: "memory");
-    write_columns<VPT>(a, reinterpret_cast<float*>(ring_raw), dw, db, p.n, [](int i, int j) { return piece_col<X>(unit_of<VPT>(i), j >> 2) + (j & 3); });
+    write_columns<VPT, true>(a, reinterpret_cast<float*>(ring_raw), dw, db, p.n, [](int i, int j) { return piece_col<X>(unit_of<VPT>(i), j >> 2) + (j & 3); });
 }
 
 template <typename X, typename Y>
@@ -898,7 +909,7 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_backward_any(const __grid
     }
     const Eight sums_w[1] = {eight(dw)}, sums_b[1] = {eight(db)};
     const int many[1] = {n};
-    write_columns<1>(a, reinterpret_cast<float*>(ring_raw), sums_w, sums_b, many, [=](int, int j) { return col + 32 * j; });
+    write_columns<1, false>(a, reinterpret_cast<float*>(ring_raw), sums_w, sums_b, many, [=](int, int j) { return col + 32 * j; });
 }
 
 // Wide rows: first the two sums of every row (a CTA per row), then dx and the sums over rows (256 units of the columns per CTA, gridDim.y CTAs share the rows).
