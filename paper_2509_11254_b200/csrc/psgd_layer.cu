@@ -54,7 +54,7 @@ NormPlan plan_norm(int64_t T, int64_t F, NormRows rows, int64_t row_bytes, bool 
     if (p.wide) {
         p.threads = NORM_THREADS;
         p.rows = 1;
-        p.ctas = std::min<int64_t>(T, sms * 2);
+        p.ctas = std::min<int64_t>(T, sms * 4);
         return p;
     }
     // Measured over widths of 256 to 8192: rows of several warps in CTAs of 512 threads (the ring of two rows then fits twice 8 rows of 12 KB), rows of one warp in CTAs of 256

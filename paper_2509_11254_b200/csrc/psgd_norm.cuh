@@ -22,7 +22,6 @@
 
 namespace psgd {
 
-constexpr int NORM_UNIT = 8;
 constexpr int NORM_THREADS = 512;                  // most threads of a CTA
 constexpr int NORM_WARPS = NORM_THREADS / 32;
 
@@ -313,13 +312,13 @@ __device__ __forceinline__ Eight ring_read(unsigned operand, int i, const T* row
         return eight(v);
     }
 }
-// A unit's values to a row of T beside an x of type X, and (rounded) as they stand there.
-// `image`: SHIFT, the warp's 34 units to turn its values into units of memory.
+// A unit's values (eight bfloat16) to a row of any alignment; `image`: the warp's 34 units to turn its values into units of memory.
 template <int VPT>
 __device__ __forceinline__ void image_store(__nv_bfloat16* row, int i, int F, const uint4& v, uint4* image) {
     const int first = unit_of<VPT>(i) * 8 - (int)(threadIdx.x & 31) * 8;                        // the same in all lanes
     if (first < F) store_any(row + unit_of<VPT>(i) * 8, v, min(F - first, 256), image);
 }
+// A unit's values to a row of T beside an x of type X.
 template <typename T, typename X, int VPT, bool SHIFT>
 __device__ __forceinline__ void unit_store(T* row, const Place<X, VPT, SHIFT>& p, int i, const Eight& v, int F, uint4* image) {
     float x[8];
