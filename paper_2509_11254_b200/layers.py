@@ -7,6 +7,9 @@
 The arithmetic runs in the CUDA library (psgd_norm_*, psgd_rotary of include/psgd.h).  As with the other training operators every call is stream-ordered on
 `stream` (default: the current stream), does not synchronise, can be captured in a CUDA graph and takes no part in autograd: gradients are results of calls of
 their own, and layer_norm_forward and rotary_forward warn where an input requires one.
+
+The plain call (tensors on the current device, the current stream, nothing to refuse or to warn about) goes through _call.so, whose functions answer None where
+it is not one.
 """
 from __future__ import annotations
 
@@ -30,6 +33,22 @@ def _like(x, rows, cols):
     return _empty_like(x) if x.is_contiguous() else _empty((rows, cols), dtype=x.dtype, device=x.device)
 
 
+_call = None
+
+
+def _plain():
+    """The module behind _call.so; like the library it has no stand-in."""
+    global _call
+    if _call is None:
+        lib()
+        try:
+            from . import _call as module
+        except ImportError as e:
+            raise PSGDError(f"_call.so cannot be loaded ({e}): build it with `python -m paper_2509_11254_b200.build`") from e
+        _call = module
+    return _call
+
+
 # ---- layer norm ---------------------------------------------------------------------------------------------------
 def _param(t, name, n, device, dtype=None):
     """(address, dtype code) of a vector over the columns, float32 or bfloat16 (or `dtype`)."""
@@ -47,6 +66,13 @@ def layer_norm_forward(x, weight, bias=None, residual=None, eps=1e-5, center=Tru
     Returns (y, x, mean, rstd, kept): x is s (the very tensor `x` without a residual), which the backward pass reads; mean (None without centring) and rstd float32 [T];
     kept the 8-bit checkpoint of y, what pack_activation(y) makes, where `keep` asks for it.
     """
+    if stream is None and dtype is None:
+        r = (_call or _plain()).norm_forward(x, weight, bias, residual, eps, center, keep)
+        if type(r) is tuple:
+            y, s, mean, rstd, buf = r
+            return LayerNorm(y, s, mean, rstd, ActivationCheckpoint(*x.shape, x.device, buf) if keep else None)
+        if r is not None:
+            _check(r)
     T, F, ldx = _matrix(x, "x", _BOTH)
     dev = x.device
     at_w, w_type = _param(weight, "weight", F, dev)
@@ -79,6 +105,12 @@ def layer_norm_backward(dy, x, weight, mean, rstd, d_x=None, bias=False, stream=
     `d_x` [T, F] (x's type): what reaches x from elsewhere, as around the layers of a residual path; it is added.  Returns (d_x, d_weight, d_bias): d_x in x's type is
     the gradient of x and of the residual alike, d_weight and d_bias (None unless `bias`) float32 [F], summed in a fixed order.
     """
+    if stream is None:
+        r = (_call or _plain()).norm_backward(dy, x, weight, mean, rstd, d_x, bias)
+        if type(r) is tuple:
+            return LayerNormGrad(*r)
+        if r is not None:
+            _check(r)
     T, F, ldx = _matrix(x, "x", _BOTH)
     dev = x.device
     lddy = _matrix(dy, "dy", (_BF16,) if x.dtype == _BF16 else _BOTH, (T, F), dev)[2]
@@ -149,6 +181,12 @@ def _heads_like(t):
 
 
 def _rotary(backward, q, k, positions, frequencies, layout, scale, in_place, stream):
+    if stream is None and layout in _LAYOUTS:
+        r = (_call or _plain()).rotary(backward, q, k, positions, frequencies, _LAYOUTS[layout], scale, in_place)
+        if type(r) is tuple:
+            return r
+        if r is not None:
+            _check(r)
     T, H, D, qt, qh = _heads(q, "dq" if backward else "q")
     dev = q.device
     _, K, _, kt, kh = _heads(k, "dk" if backward else "k", q) if k is not None else (T, 0, D, 0, 0)
