@@ -1,7 +1,7 @@
-// The plain call of layer norm and rotary positions without the interpreter in between: every argument a tensor on the current device, the current stream, no
-// gradient asked for.  Checks, allocation of the outputs and the call of the C entry point take 5 to 8 us here and 13 to 17 in Python, more than the kernels of a small
-// call.  Anything else (another stream or device, no rows, an argument to refuse, a graph that would be lost) is answered by None before anything happened, and layers.py
-// does what it calls for; it owns the documentation and the errors.  An int is the library's error code.
+// The plain call of layer norm, rotary positions and distillation without the interpreter in between: every argument a tensor on the current device, the current stream,
+// no gradient asked for.  Checks, allocation of the outputs and the call of the C entry point take 5 to 9 us here and 13 to 24 in Python, more than the kernels of a
+// small call.  Anything else (another stream or device, no rows, an operand to copy, an argument to refuse, a graph that would be lost) is answered by None before
+// anything happened, and layers.py and training.py do what it calls for; they own the documentation and the errors.  An int is the library's error code.
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
@@ -188,7 +188,65 @@ PyObject* rotary(PyObject*, PyObject* const* o, Py_ssize_t count) {
     END_HANDLE_TH_ERRORS
 }
 
-PyMethodDef methods[] = {{"norm_forward", (PyCFunction)(void (*)(void))norm_forward, METH_FASTCALL, nullptr},
+// an operand that the tensor cores' loads can read in place
+bool operand(const Tensor& t, int64_t rows, int64_t cols, int64_t& ld) {
+    return t.scalar_type() == at::kBFloat16 && matrix(t, rows, cols, ld) && ((uintptr_t)t.data_ptr() & 15) == 0 && (rows == 1 || ld % 8 == 0);
+}
+
+// (grad, hidden, weight, logits, index, temperature, token_weight) -> (loss, token_loss, lse[, d_hidden, d_weight])
+PyObject* distill(PyObject*, PyObject* const* o, Py_ssize_t count) {
+    HANDLE_TH_ERRORS
+    if (count != 7) return none();
+    const Tensor *h = tensor(o[1]), *w = tensor(o[2]), *z = tensor(o[3]), *index = tensor(o[4]), *weight = tensor(o[6]);
+    if (!PyBool_Check(o[0]) || !h || !w || !z || !index || !PyFloat_CheckExact(o[5]) || (!weight && o[6] != Py_None) || !h->is_cuda()) return none();
+    const Here here;
+    const bool grad = o[0] == Py_True;
+    const double tau = PyFloat_AS_DOUBLE(o[5]);
+    if (!here.takes(*h, !grad) || !here.takes(*w, !grad) || !here.takes(*z, false) || h->dim() != 2 || w->dim() != 2 || z->dim() != 2 || index->dim() != 2) return none();
+    const int64_t T = h->size(0), D = h->size(1), V = w->size(0), K = z->size(1);
+    int64_t ldh, ldw, ldl, ldi;
+    if (T < 1 || D < 1 || V < 1 || K < 1 || K > 1024 || !(tau >= 1e-3 && tau <= 1e3) || !operand(*h, T, D, ldh) || !operand(*w, V, D, ldw)) return none();
+    if (!matrix(*z, T, K, ldl) || !index->is_cuda() || index->get_device() != here.device || index->scalar_type() != at::kLong || !matrix(*index, T, K, ldi)) return none();
+    if (weight && !vector(*weight, T, at::kFloat, here.device)) return none();
+    Tensor loss, token_loss, lse, dh, dw, ws;
+    psgd_status e;
+    {
+        const Unlocked unlocked;
+        thread_local struct { int64_t T, V, D, K; int grad, device; size_t bytes; } asked = {-1, 0, 0, 0, 0, 0, 0};
+        e = PSGD_OK;
+        if (asked.T != T || asked.V != V || asked.D != D || asked.K != K || asked.grad != grad || asked.device != here.device) {
+            asked.T = -1;
+            e = psgd_distill_workspace(T, V, D, K, grad, &asked.bytes);
+            if (e == PSGD_OK) asked = {T, V, D, K, grad, here.device, asked.bytes};
+        }
+        if (e == PSGD_OK) {
+            const auto floats = h->options().dtype(at::kFloat);
+            ws = at::empty({(int64_t)asked.bytes}, floats.dtype(at::kByte));
+            loss = at::empty({}, floats);
+            token_loss = at::empty({T}, floats);
+            lse = at::empty({T}, floats);
+            const auto st = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)here.device).stream();
+            const int64_t* at_index = (const int64_t*)index->data_ptr();
+            const float* at_weight = weight ? (const float*)weight->data_ptr() : nullptr;
+            float *at_loss = (float*)loss.data_ptr(), *at_token = (float*)token_loss.data_ptr(), *at_lse = (float*)lse.data_ptr();
+            if (grad) {
+                dh = matrix_like(*h, T, D);
+                dw = matrix_like(*w, V, D);
+                e = psgd_distill_grad(h->data_ptr(), ldh, w->data_ptr(), ldw, z->data_ptr(), ldl, code(*z), at_index, ldi, K, (float)tau, at_weight, T, V, D, at_loss, at_token, at_lse,
+                                      dh.data_ptr(), D, dw.data_ptr(), D, nullptr, ws.data_ptr(), asked.bytes, st);
+            } else {
+                e = psgd_distill_loss(h->data_ptr(), ldh, w->data_ptr(), ldw, z->data_ptr(), ldl, code(*z), at_index, ldi, K, (float)tau, at_weight, T, V, D, at_loss, at_token, at_lse,
+                                      nullptr, ws.data_ptr(), asked.bytes, st);
+            }
+        }
+    }
+    if (e != PSGD_OK) return PyLong_FromLong(e);
+    return grad ? tuple({wrap(loss), wrap(token_loss), wrap(lse), wrap(dh), wrap(dw)}) : tuple({wrap(loss), wrap(token_loss), wrap(lse)});
+    END_HANDLE_TH_ERRORS
+}
+
+PyMethodDef methods[] = {{"distill", (PyCFunction)(void (*)(void))distill, METH_FASTCALL, nullptr},
+                         {"norm_forward", (PyCFunction)(void (*)(void))norm_forward, METH_FASTCALL, nullptr},
                          {"norm_backward", (PyCFunction)(void (*)(void))norm_backward, METH_FASTCALL, nullptr},
                          {"rotary", (PyCFunction)(void (*)(void))rotary, METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};

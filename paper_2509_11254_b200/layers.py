@@ -19,7 +19,7 @@ from collections import namedtuple
 import torch
 
 from .binding import PSGDError, lib
-from .training import _BF16, _BOTH, _DTYPES, ActivationCheckpoint, _check, _empty, _here, _matrix, _name, _no_graph, _there, _vector, _workspace_bytes
+from .training import _BF16, _BOTH, _DTYPES, ActivationCheckpoint, _check, _empty, _here, _matrix, _name, _no_graph, _plain, _there, _vector, _workspace_bytes
 
 LayerNorm = namedtuple("LayerNorm", "y x mean rstd kept")
 LayerNormGrad = namedtuple("LayerNormGrad", "d_x d_weight d_bias")
@@ -31,22 +31,6 @@ _empty_like = torch.empty_like
 def _like(x, rows, cols):
     """A new matrix of x's shape and type whose rows lie one after the other (the shortest way to it where x's own do)."""
     return _empty_like(x) if x.is_contiguous() else _empty((rows, cols), dtype=x.dtype, device=x.device)
-
-
-_call = None
-
-
-def _plain():
-    """The module behind _call.so; like the library it has no stand-in."""
-    global _call
-    if _call is None:
-        lib()
-        try:
-            from . import _call as module
-        except ImportError as e:
-            raise PSGDError(f"_call.so cannot be loaded ({e}): build it with `python -m paper_2509_11254_b200.build`") from e
-        _call = module
-    return _call
 
 
 # ---- layer norm ---------------------------------------------------------------------------------------------------
@@ -67,7 +51,7 @@ def layer_norm_forward(x, weight, bias=None, residual=None, eps=1e-5, center=Tru
     kept the 8-bit checkpoint of y, what pack_activation(y) makes, where `keep` asks for it.
     """
     if stream is None and dtype is None:
-        r = (_call or _plain()).norm_forward(x, weight, bias, residual, eps, center, keep)
+        r = _plain().norm_forward(x, weight, bias, residual, eps, center, keep)
         if type(r) is tuple:
             y, s, mean, rstd, buf = r
             return LayerNorm(y, s, mean, rstd, ActivationCheckpoint(*x.shape, x.device, buf) if keep else None)
@@ -106,7 +90,7 @@ def layer_norm_backward(dy, x, weight, mean, rstd, d_x=None, bias=False, stream=
     the gradient of x and of the residual alike, d_weight and d_bias (None unless `bias`) float32 [F], summed in a fixed order.
     """
     if stream is None:
-        r = (_call or _plain()).norm_backward(dy, x, weight, mean, rstd, d_x, bias)
+        r = _plain().norm_backward(dy, x, weight, mean, rstd, d_x, bias)
         if type(r) is tuple:
             return LayerNormGrad(*r)
         if r is not None:
@@ -182,7 +166,7 @@ def _heads_like(t):
 
 def _rotary(backward, q, k, positions, frequencies, layout, scale, in_place, stream):
     if stream is None and layout in _LAYOUTS:
-        r = (_call or _plain()).rotary(backward, q, k, positions, frequencies, _LAYOUTS[layout], scale, in_place)
+        r = _plain().rotary(backward, q, k, positions, frequencies, _LAYOUTS[layout], scale, in_place)
         if type(r) is tuple:
             return r
         if r is not None:

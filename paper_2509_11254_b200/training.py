@@ -51,6 +51,22 @@ def _check(code):
         binding._check(code)
 
 
+_call = None
+
+
+def _plain():
+    """The module behind _call.so: the plain call of an operator, or None where it is not one; like the library it has no stand-in."""
+    global _call
+    if _call is None:
+        lib()
+        try:
+            from . import _call as module
+        except ImportError as e:
+            raise PSGDError(f"_call.so cannot be loaded ({e}): build it with `python -m paper_2509_11254_b200.build`") from e
+        _call = module
+    return _call
+
+
 # ---- arguments ----------------------------------------------------------------------------------------------------
 def _name(dtype):
     return str(dtype).replace("torch.", "")
@@ -157,6 +173,12 @@ def _workspace_bytes(call, *args):
 # ---- cross entropy and distillation -------------------------------------------------------------------------------
 def _last_layer(grad, hidden, weight, target, token_weight, d_hidden, d_weight, status, stream):
     """target: (labels, ignore_index) or (teacher_logits, teacher_index, temperature)."""
+    if len(target) == 3 and stream is None and d_hidden is None and d_weight is None and status is None:
+        r = _plain().distill(grad, hidden, weight, *target, token_weight)
+        if type(r) is tuple:
+            return DistillationGrad(*r) if grad else Distillation(*r)
+        if r is not None:
+            _check(r)
     T, D, ldh = _matrix(hidden, "hidden")
     dev = hidden.device
     V, Dw, ldw = _matrix(weight, "weight", device=dev)
