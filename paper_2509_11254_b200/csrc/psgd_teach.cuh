@@ -50,12 +50,12 @@ __global__ void __launch_bounds__(TEACH_THREADS) k_teach(const __grid_constant__
     __shared__ int count[TEACH_BINS], warps[TEACH_THREADS / 32];
     __shared__ int base;
     constexpr int EACH = TEACH_BINS / TEACH_THREADS;
-    grid_trigger();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, K = a.K;
     for (int i = tid; i < TEACH_BINS; i += TEACH_THREADS) count[i] = 0;
     if (tid == 0) base = 0;
     __syncthreads();
     grid_wait();
+    grid_trigger();                                    // after the wait: the product's loads begin when this lets it start, and rely on all that came before being done
     const long long row = (long long)blockIdx.x * TEACH_ROWS + warp;
     const bool held = K <= 32 * TEACH_HELD, live = row < a.T;
     const long long* index = a.index + row * a.ldi;

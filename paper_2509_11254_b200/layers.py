@@ -30,7 +30,7 @@ _empty_like = torch.empty_like
 
 def _like(x, rows, cols):
     """A new matrix of x's shape and type whose rows lie one after the other (the shortest way to it where x's own do)."""
-    return _empty_like(x) if x.is_contiguous() else _empty((rows, cols), dtype=x.dtype, device=x.device)
+    return _empty_like(x) if x.stride() == (cols, 1) else _empty((rows, cols), dtype=x.dtype, device=x.device)
 
 
 # ---- layer norm ---------------------------------------------------------------------------------------------------

@@ -77,3 +77,31 @@ def test_layer_gradients(torch, example):
 def test_example_runs(torch, example):
     losses = example.train(steps=4, vocab=300, width=64, heads=2, inner=120, length=33, batch=3, log=None)
     assert len(losses) == 4 and all(math.isfinite(v) and v > 0 for v in losses)
+
+
+def test_distillation_right_behind_the_kernel_that_writes_its_input(torch, example):
+    """The product's loads begin before the kernel in front of it ends: a norm writes the hidden states into memory that held others just before, a hundred times, few tokens
+    and many, the same bits as with a pause between the two."""
+    import paper_2509_11254_b200 as ops
+
+    g = torch.Generator(device="cuda").manual_seed(7)
+    for T, V, D, K in ((1, 3000, 256, 4), (90, 2000, 768, 20), (2100, 900, 512, 7)):
+        w = (torch.randn(V, D, generator=g, device="cuda") * 0.1).bfloat16()
+        xs = [torch.randn(T, D, generator=g, device="cuda").bfloat16() for _ in range(4)]
+        one = torch.ones(D, device="cuda")
+        z, index = torch.randn(T, K, generator=g, device="cuda"), torch.randint(V, (T, K), generator=g, device="cuda")
+        want = []
+        for x in xs:
+            y = ops.layer_norm_forward(x, one).y
+            torch.cuda.synchronize()
+            want.append([*ops.linear_distillation_grad(y, w, z, index), *ops.linear_distillation(y, w, z, index, 2.0)])
+            torch.cuda.synchronize()
+        del y
+        for i in range(100):
+            y = ops.layer_norm_forward(xs[i % 4], one).y             # (the allocator hands out the memory of the last round)
+            got = ops.linear_distillation_grad(y, w, z, index)
+            y = ops.layer_norm_forward(xs[i % 4], one).y
+            got = [*got, *ops.linear_distillation(y, w, z, index, 2.0)]
+            for a, b in zip(got, want[i % 4]):
+                assert torch.equal(a, b), (T, i)
+            del y, got

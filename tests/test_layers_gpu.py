@@ -566,3 +566,81 @@ def test_norm_sums_of_bfloat16_are_rounded_once(torch, ops):
         got, want = ops.layer_norm_forward(x[:, :F], w[:F], residual=r[:, :F]).x, (x[:, :F].float() + r[:, :F].float()).bfloat16()
         nan = torch.isnan(want)
         assert torch.equal(torch.isnan(got), nan) and torch.equal(got.view(torch.int16)[~nan], want.contiguous().view(torch.int16)[~nan])
+
+
+# ---- the plain call and the long way ------------------------------------------------------------------------------
+def test_plain_calls_equal_the_others(torch, ops, monkeypatch):
+    """The same bits and the same refusals whether the call is made by _call.so or by the Python functions behind it, over types, optional parts, strides and single rows."""
+    from paper_2509_11254_b200 import layers, training
+
+    class Never:                                       # answers None to everything
+        def __getattr__(self, name):
+            return lambda *a: None
+
+    took = []
+
+    def both(call):
+        monkeypatch.undo()
+        module = training._plain()
+
+        class Watch:
+            def __getattr__(self, name):
+                def f(*a):
+                    r = getattr(module, name)(*a)
+                    took.append(r is not None)
+                    return r
+                return f
+
+        out = []
+        for stand_in in (Watch(), Never()):
+            monkeypatch.setattr(layers, "_plain", lambda: stand_in)
+            monkeypatch.setattr(training, "_plain", lambda: stand_in)
+            try:
+                out.append(call())
+            except ops.PSGDError as e:
+                out.append(str(e))
+        monkeypatch.undo()
+        a, b = out
+        assert type(a) is type(b)
+        if isinstance(a, str):
+            assert a == b
+            return
+        for u, v in zip(a, b):
+            if u is None or v is None:
+                assert u is v
+            elif isinstance(u, ops.ActivationCheckpoint):
+                assert u.shape == v.shape and torch.equal(u.q, v.q) and torch.equal(u.scales, v.scales)
+            else:
+                assert u.dtype == v.dtype and u.shape == v.shape and u.stride() == v.stride() and torch.equal(u, v)
+
+    for T, F in ((1, 1), (1, 40), (7, 96), (5, 101), (3, 1)):
+        for dtype in (torch.bfloat16, torch.float32):
+            x, r, w, b = norm_inputs(torch, T, F, 3, dtype)
+            wide = torch.zeros(T, F + 8, dtype=dtype, device="cuda")
+            wide[:, :F] = x
+            n = ops.layer_norm_forward(x, w, b)
+            both(lambda: ops.layer_norm_forward(x, w, b))
+            both(lambda: ops.layer_norm_forward(wide[:, :F], w.bfloat16(), None, residual=r, center=False, keep=True))
+            both(lambda: ops.layer_norm_backward(r, x, w, n.mean, n.rstd))
+            both(lambda: ops.layer_norm_backward(r, wide[:, :F], w, None, n.rstd, d_x=x, bias=True))
+            both(lambda: ops.layer_norm_backward(r.bfloat16(), x, w, n.mean, n.rstd))
+            both(lambda: ops.layer_norm_forward(x, w[:-1], b))
+            both(lambda: ops.layer_norm_forward(x, w, b, residual=r[:, 1:]))
+    q = torch.randn(9, 6, 32, device="cuda")
+    at, f = torch.arange(9, device="cuda"), ops.rotary_frequencies(16)
+    for t in (q, q[:, 1:5], q.transpose(0, 1).contiguous().transpose(0, 1), q[:, :1].expand(9, 6, 32), q[:1], q[:, :1]):
+        at_t = at[:t.shape[0]]
+        both(lambda: ops.rotary_forward(t, None, at_t, f))
+        both(lambda: ops.rotary_backward(t, t, at_t, f, layout="interleaved", scale=0.5))
+        both(lambda: ops.rotary_forward(t.clone(), t.clone(), at_t, f, in_place=True))
+    both(lambda: ops.rotary_forward(q, None, at, f, in_place=True)[:0])
+    both(lambda: ops.rotary_forward(q[:, :1].expand(9, 6, 32), None, at, f, in_place=True))
+    both(lambda: ops.rotary_forward(q, q.double(), at, f))
+    for T in (1, 6):
+        h, w = torch.randn(T, 64, device="cuda").bfloat16(), torch.randn(90, 64, device="cuda").bfloat16()
+        z, i = torch.randn(T, 5, device="cuda"), torch.randint(90, (T, 5), device="cuda")
+        both(lambda: ops.linear_distillation(h, w, z, i, 2.0))
+        both(lambda: ops.linear_distillation_grad(h, w, z.bfloat16(), i, token_weight=torch.ones(T, device="cuda")))
+        both(lambda: ops.linear_distillation_grad(h[:, 1:41], w[:, 1:41], z, i))
+        both(lambda: ops.linear_distillation(h, w, z, i, 0.0))
+    assert sum(took) > 60 and len(took) - sum(took) > 20       # both ways were taken
