@@ -244,6 +244,14 @@ XentPlan plan_xent(int64_t T, int64_t V, int64_t D, bool grad, int64_t K) {
     return x;
 }
 
+// The loss of one token, without the tensor cores
+bool launch_one(const TileArgs& t, const void* H, const void* W, int64_t ldw, int64_t V, int64_t D, cudaStream_t st) {
+    const OneArgs a{(const __nv_bfloat16*)H, (const __nv_bfloat16*)W, ldw, (int)V, (int)D, t.nbins, t.log2e, t.stats, t.bins, t.entries, t.entry_logit, t.done};
+    const size_t smem = align_up((size_t)D, 8) * 4;
+    if (smem > 32 << 10) set_smem_attr((const void*)k_teach_one, smem);      // (static shared memory comes on top)
+    return launch(k_teach_one, dim3(ceil_div(V, XE_SEG_LOSS)), dim3(ONE_THREADS), smem, st, a);
+}
+
 struct Teacher { const void* logits; int64_t ldl; int dtype; const int64_t* index; int64_t ldi, K; float tau; };
 
 // `teacher`: nullptr where there are labels
@@ -337,7 +345,8 @@ psgd_status xent(const void* H, int64_t ldh, const void* W, int64_t ldw, const i
         const TilePlan pl = whole ? x.logits : plan_tiles(rows, V, D, x.pairs, false);
         const Operand oh{h, ldh, false}, ow{W, ldw, false};
         psgd_status s;
-        if (teacher) s = grad ? launch_softmax<EPI_TEACH>(oh, ow, pl, a, x.pairs, st) : launch_softmax<EPI_TEACH_LOSS>(oh, ow, pl, a, x.pairs, st);
+        if (teacher && !grad && T == 1 && D <= ONE_WIDTH) s = launch_one(a, h, W, ldw, V, D, st) ? PSGD_OK : PSGD_E_CUDA;
+        else if (teacher) s = grad ? launch_softmax<EPI_TEACH>(oh, ow, pl, a, x.pairs, st) : launch_softmax<EPI_TEACH_LOSS>(oh, ow, pl, a, x.pairs, st);
         else s = grad ? launch_softmax<EPI_SOFTMAX>(oh, ow, pl, a, x.pairs, st) : launch_softmax<EPI_LOSS>(oh, ow, pl, a, x.pairs, st);
         if (s != PSGD_OK) return s;
         r.rows = (int)rows;

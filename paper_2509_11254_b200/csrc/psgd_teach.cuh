@@ -184,6 +184,113 @@ __global__ void __launch_bounds__(TEACH_THREADS) k_teach(const __grid_constant__
     }
 }
 
+// The loss of one token: its logits without the tensor cores, whose tiles of 256 rows would work on one that exists.  A CTA forms those of 128 columns, a warp four of them at a
+// time, every lane 16 bytes of their rows, ONE_UNITS times before it uses them; the hidden state lies in shared memory as float32.  Then the statistics and the listed
+// entries' logits as the product's epilogue leaves them.  Bound by reading the vocabulary matrix once: 32000 x 768 in 12.8 us, of which the bytes take 7.5 (the tiles: 17.4 us);
+// the whole call on 131072 x 2048 in 89 us (97), the bytes 82.  Two tokens at a time cost as much as the tiles.  As k_tile it starts beside k_teach, whose lists it needs at its end only.
+constexpr int ONE_THREADS = 512, ONE_ROWS = 4, ONE_UNITS = 2;
+constexpr int ONE_WIDTH = 16384;   // most columns of a hidden state
+struct OneArgs {
+    const __nv_bfloat16 *h, *w;
+    long long ldw;
+    int V, D, nbins;
+    float log2e;
+    float2* stats;                 // [segments of 128 columns]
+    const int* bins;
+    const unsigned* entries;
+    float* entry_logit;
+    int* done;                     // counter to clear for the next kernel
+};
+__global__ void __launch_bounds__(ONE_THREADS, 2) k_teach_one(const __grid_constant__ OneArgs a) {
+    extern __shared__ __align__(16) float hidden[];                // D rounded up to 8, zeros behind D
+    __shared__ float logit[XE_SEG_LOSS];
+    grid_trigger();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, units = (a.D + 7) / 8, whole = a.D / 8;
+    // (the hidden state and the vocabulary matrix are older than the kernel before this one)
+    for (int d = tid; d < units * 8; d += ONE_THREADS) hidden[d] = d < a.D ? __bfloat162float(a.h[d]) : 0.f;
+    __syncthreads();
+    const int col0 = blockIdx.x * XE_SEG_LOSS;
+    for (int c = warp * ONE_ROWS; c < XE_SEG_LOSS && col0 + c < a.V; c += ONE_THREADS / 32 * ONE_ROWS) {
+        float acc[ONE_ROWS] = {};
+        const __nv_bfloat16* row[ONE_ROWS];
+#pragma unroll
+        for (int r = 0; r < ONE_ROWS; ++r) row[r] = a.w + (long long)min(col0 + c + r, a.V - 1) * a.ldw;
+        const auto add = [&](const Raw16 (&raw)[ONE_ROWS], int u) {
+            const float4 lo = *reinterpret_cast<const float4*>(hidden + u * 8), hi = *reinterpret_cast<const float4*>(hidden + u * 8 + 4);
+            const float y[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+            for (int r = 0; r < ONE_ROWS; ++r) {
+                float x[8];
+                widen(raw[r], x);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[r] = fmaf(x[j], y[j], acc[r]);
+            }
+        };
+        for (int u0 = lane; u0 < whole; u0 += 32 * ONE_UNITS) {
+            Raw16 raw[ONE_UNITS][ONE_ROWS];
+#pragma unroll
+            for (int i = 0; i < ONE_UNITS; ++i)
+#pragma unroll
+                for (int r = 0; r < ONE_ROWS; ++r) {
+                    raw[i][r].a = make_uint4(0u, 0u, 0u, 0u);
+                    if (u0 + 32 * i < whole) load8(raw[i][r], row[r] + (u0 + 32 * i) * 8);
+                }
+#pragma unroll
+            for (int i = 0; i < ONE_UNITS; ++i)
+                if (u0 + 32 * i < whole) add(raw[i], u0 + 32 * i);
+        }
+        if (whole < units && lane == 0) {              // the rows' ends: only their own values are read
+            Raw16 raw[ONE_ROWS];
+#pragma unroll
+            for (int r = 0; r < ONE_ROWS; ++r) {
+                unsigned h[4] = {};
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (whole * 8 + j < a.D) h[j / 2] |= (unsigned)reinterpret_cast<const unsigned short*>(row[r])[whole * 8 + j] << (j & 1) * 16;
+                raw[r].a = make_uint4(h[0], h[1], h[2], h[3]);
+            }
+            add(raw, whole);
+        }
+#pragma unroll
+        for (int r = 0; r < ONE_ROWS; ++r) {
+            float v = acc[r];
+#pragma unroll
+            for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+            if (lane == 0) logit[c + r] = v;
+        }
+    }
+    __syncthreads();
+    grid_wait();
+    if (blockIdx.x == 0 && tid == 0) *a.done = 0;
+    if (warp == 0) {
+        const int cols = min(XE_SEG_LOSS, a.V - col0);
+        float v[XE_SEG_LOSS / 32], top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < XE_SEG_LOSS / 32; ++i) {
+            v[i] = lane + 32 * i < cols ? logit[lane + 32 * i] : -INFINITY;
+            top = fmaxf(top, v[i]);
+        }
+#pragma unroll
+        for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const float ref = top == -INFINITY ? 0.f : top;
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < XE_SEG_LOSS / 32; ++i) sum += ex2((v[i] - ref) * a.log2e);
+#pragma unroll
+        for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (lane == 0) a.stats[blockIdx.x] = make_float2(top, sum);
+    }
+    // the segment's four blocks of columns, whose entries lie one after the other
+    const int* at = a.bins + 4 * blockIdx.x;
+    const int left = a.nbins - 4 * (int)blockIdx.x;
+    const int begin[5] = {at[0], at[min(1, left)], at[min(2, left)], at[min(3, left)], at[min(4, left)]};
+    for (int e = begin[0] + tid; e < begin[4]; e += ONE_THREADS) {
+        const unsigned code = a.entries[e];
+        const int block = (e >= begin[1]) + (e >= begin[2]) + (e >= begin[3]);
+        a.entry_logit[code >> 10] = logit[32 * block + (int)(code & 31u)];
+    }
+}
+
 struct TeachRows {
     int K;
     const float* z;                // of these rows, as all below

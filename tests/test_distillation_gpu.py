@@ -462,3 +462,16 @@ def test_distillation_warns_and_refuses(torch, ops):
     for call in bad:
         with pytest.raises(ops.PSGDError):
             call()
+
+
+@pytest.mark.parametrize("T", [1, 2])
+@pytest.mark.parametrize("V,D,K", [(1, 8, 1), (33, 1, 3), (127, 37, 5), (128, 64, 40), (129, 100, 7), (5000, 768, 64), (700, 2051, 300), (300, 16384, 9), (300, 16392, 9), (4000, 4096, 16), (4001, 8, 1024)])
+def test_distillation_of_one_token(torch, ops, T, V, D, K):
+    """The loss alone goes without tiles (up to a width of 16384), the gradients and two tokens by them; every kind of row end, a vocabulary that ends inside a segment."""
+    h, w, z, index = inputs(torch, T, V, D, K, T + V + D, spread=1.0, empty=0.0)
+    check(torch, ops, h, w, z, index, 1.5)
+    wide_h, wide_w = torch.full((T, D + 24), float("nan"), device="cuda", dtype=torch.bfloat16), torch.full((V, (D + 7) // 8 * 8 + 8), float("nan"), device="cuda", dtype=torch.bfloat16)
+    wide_h[:, 8:8 + D], wide_w[:, 8:8 + D] = h, w                        # NaN on both sides of every row
+    a, b = ops.linear_distillation(h, w, z, index), ops.linear_distillation(wide_h[:, 8:8 + D], wide_w[:, 8:8 + D], z, index)
+    for u, v in zip(a, b):
+        assert torch.equal(u, v)
