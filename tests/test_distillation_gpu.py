@@ -475,3 +475,30 @@ def test_distillation_of_one_token(torch, ops, T, V, D, K):
     a, b = ops.linear_distillation(h, w, z, index), ops.linear_distillation(wide_h[:, 8:8 + D], wide_w[:, 8:8 + D], z, index)
     for u, v in zip(a, b):
         assert torch.equal(u, v)
+
+
+def test_distillation_behind_a_wait_that_ran_out_is_nan(torch, ops, tmp_path, monkeypatch):
+    """A build whose epilogue gives up every wait for an accumulator at once (no pair has more than two accumulators here, so nothing waits for the epilogue in turn): every
+    result is NaN, and the status word says why.  (Calls with a status word take the long way, through the library that is put in its place.)"""
+    import ctypes as C
+    import subprocess
+
+    from paper_2509_11254_b200 import binding, build
+
+    so = str(tmp_path / "gives_up.so")
+    src = [s for s in build.SRCS if s.endswith("psgd_lm.cu")]
+    subprocess.run([build.nvcc_path(), "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-Xcompiler", "-fPIC", "-shared", "-DPSGD_WARP_WAIT_LIMIT=0",
+                    "-o", so, *src], check=True, capture_output=True)
+    L = C.CDLL(so)
+    for name, (res, args) in binding.SIGNATURES.items():
+        if hasattr(L, name):
+            getattr(L, name).restype, getattr(L, name).argtypes = res, args
+    h, w, z, index = inputs(torch, 300, 700, 64, 9, 3)
+    monkeypatch.setattr(binding, "_lib", L)
+    counts = (index >= 0).any(1)
+    for call in (ops.linear_distillation, ops.linear_distillation_grad):
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        r = call(h, w, z, index, 2.0, status=status)
+        assert int(status) == ops.PSGD_W_TIMEOUT
+        assert bool(torch.isnan(r.loss)) and bool(torch.isnan(r.lse).all()) and bool(torch.isnan(r.token_loss[counts]).all())
+    assert bool(torch.isnan(r.d_hidden).all()) and bool(torch.isnan(r.d_weight).all())
