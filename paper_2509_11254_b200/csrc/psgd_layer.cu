@@ -15,14 +15,17 @@ bool whole_units(const void* p, int64_t ld, int64_t F, int dtype) { return !p ||
 bool rows_ok(int64_t T, int64_t F) { return T >= 0 && T <= MAX_EXTENT && extent_ok(F); }
 
 // ---- layer norm ----
-// How the rows go: RING (16-byte units), SHIFT (bfloat16 of any width and alignment through the ring, forward), LANES (anything else, a value per lane)
-enum NormRows { RING, SHIFT, LANES };
+// How the rows go: RING (16-byte units), PHASE (bfloat16 of any width and alignment, all operands alike), LANES (anything else, a value per lane)
+enum NormRows { RING, PHASE, LANES };
+// Whether two matrices of bfloat16 lie alike: the same place within 16 bytes in every row (no matrix lies like any other)
+bool alike(const void* p, int64_t ldp, const void* q, int64_t ldq, int64_t T) { return !q || ((((uintptr_t)p ^ (uintptr_t)q) & 15) == 0 && (T == 1 || (ldp - ldq) % 8 == 0)); }
 // How a row's units are shared: `vpt` per thread, `threads` per row (whole warps), `rows` side by side per CTA, `stages` rows of a ring.
 struct NormPlan { int vpt, threads, rows, stages; bool wide; int64_t ctas; size_t smem; };
 constexpr int64_t NORM_SMEM = 200 << 10;            // of a multiprocessor's, for weights and rings
 
-// `row_bytes`: of all operands of a row that are read.  The number of rows has no say in how a row is shared: its bits do not depend on its batch.
-NormPlan plan_norm(int64_t T, int64_t F, NormRows rows, int64_t row_bytes, bool more, bool backward) {
+// `row_bytes`: of all operands of a row that are read.  The number of rows has no say in how a row is shared: the bits of aligned rows do not depend
+// on their batch.
+NormPlan plan_norm(int64_t T, int64_t F, NormRows rows, int64_t row_bytes, bool more, bool keep, bool backward) {
     NormPlan p{};
     const int64_t sms = device_sms();
     if (rows == LANES) {                                    // a value per lane: one unit per thread
@@ -37,20 +40,18 @@ NormPlan plan_norm(int64_t T, int64_t F, NormRows rows, int64_t row_bytes, bool 
     }
     // Units per thread: as many as registers hold, which is eight where the row has nothing to be added to (2048 columns: 24.8 us with eight, 29 with four; with
     // a residual 51 and 47) and four elsewhere, fewer where that leaves fewer places empty.
-    const int64_t units = (F + 7) / 8;
+    const int64_t units = (F + 7 + (rows == PHASE ? 7 : 0)) / 8;
     double best = 1e300;
     for (int vpt : {8, 4, 3, 2, 1}) {
-        if (vpt == 8 && (rows == SHIFT || backward || more)) continue;
+        if (vpt == 8 && (rows == PHASE || backward || more)) continue;
         const int64_t g = (int64_t)align_up((size_t)ceil_div(units, vpt), 32);
-        if (g > NORM_THREADS) continue;
+        if (g > NORM_THREADS || (vpt == 4 && rows == PHASE && backward && units <= 3 * NORM_THREADS)) continue;      // (four spill there: 8192 x 5003 119 us, three 89)
         const double cost = (double)g * (vpt + 1) + (g > 32 ? 16 : 0);       // a warp's part of a row costs about a unit beside its units, the exchange a little more
         if (cost < best) { best = cost; p.vpt = vpt; p.threads = (int)g; }
     }
     const int64_t slots = (int64_t)p.threads * p.vpt, params = slots * (backward ? 32 : 64);
-    int64_t row = row_bytes / F * slots * 8;
-    const int64_t margin = rows == SHIFT ? p.threads / 32 * 48 : 0;          // a unit more per warp and operand, up to three operands
-    row += margin;
-    p.wide = p.threads == 0 || params + row > NORM_SMEM;
+    const int64_t row = row_bytes / F * slots * 8, image = rows == PHASE && keep ? slots * 16 + 16 : 0;
+    p.wide = p.threads == 0 || params + row + image > NORM_SMEM;
     if (p.wide) {
         p.threads = NORM_THREADS;
         p.rows = 1;
@@ -63,20 +64,22 @@ NormPlan plan_norm(int64_t T, int64_t F, NormRows rows, int64_t row_bytes, bool 
     const int fit = std::max(1, (p.vpt == 1 ? (backward ? 768 : 1024) : p.vpt == 2 && !backward ? 768 : 512) / (p.threads * p.rows));       // CTAs per multiprocessor, by registers
     // Forward, a row is in registers while the next is on its way: a second row in the ring pays for short ones only (256 columns with a residual 23.7 us against
     // 26.8, 768: 17.4, 18.4; 2048: 49.0 with one, 51.7 with two).  Backward the row stays in the ring to the end.
-    p.stages = (backward || row <= 4096) && params + 2 * row * p.rows <= NORM_SMEM / fit ? 2 : 1;
-    while (p.rows > 1 && params + row * p.rows > NORM_SMEM) --p.rows;
-    p.smem = (size_t)(params + row * p.rows * p.stages);
-    if (backward && p.rows > 1) p.smem = std::max(p.smem, (size_t)p.rows * 2 * F * 4);
+    p.stages = (backward || row <= 4096) && params + (2 * row + image) * p.rows <= NORM_SMEM / fit ? 2 : 1;
+    while (p.rows > 1 && params + (row + image) * p.rows > NORM_SMEM) --p.rows;
+    p.smem = (size_t)(params + (row * p.stages + image) * p.rows);
+    if (backward && (p.rows > 1 || rows == PHASE)) p.smem = std::max(p.smem, (size_t)p.rows * 2 * (rows == PHASE ? slots * 8 : F) * 4);
     // as many CTAs as fit, forward with long rows twice as many: who is done early takes another (2048 columns with a residual 49.0 -> 47.0 us)
     const int64_t resident = std::max<int64_t>(1, std::min<int64_t>(fit, NORM_SMEM / (int64_t)p.smem));
-    p.ctas = std::min<int64_t>((T + p.rows - 1) / p.rows, sms * resident * (!backward && more && p.threads > 32 ? 2 : 1));
+    const int64_t some = (T + p.rows - 1) / p.rows, most = sms * resident * (!backward && more && p.threads > 32 ? 2 : 1);
+    // PHASE: rows eight apart begin alike whatever their stride
+    p.ctas = rows == PHASE && T > 1 ? std::min((some + 7) / 8 * 8, std::max<int64_t>(8, most / 8 * 8)) : std::min(some, most);
     return p;
 }
 
 struct NormGrad { NormPlan p; int64_t parts; size_t part, sums, total; };
 NormGrad plan_norm_grad(int64_t T, int64_t F, NormRows rows, int64_t row_bytes) {
     NormGrad g{};
-    g.p = plan_norm(T, F, rows, row_bytes, false, true);
+    g.p = plan_norm(T, F, rows, row_bytes, false, false, true);
     const int64_t tiles = (F + 2047) / 2048;
     g.parts = g.p.wide ? std::min<int64_t>({T, 65535, std::max<int64_t>(1, device_sms() * 4 / tiles)}) : g.p.ctas;
     g.part = 0;
@@ -90,15 +93,15 @@ bool launch_norm(void (*kernel)(Args), const NormPlan& p, const Args& a, cudaStr
     if (p.smem > 32 << 10) set_smem_attr((const void*)kernel, p.smem);      // (static shared memory comes on top)
     return launch(kernel, dim3((unsigned)p.ctas), dim3(p.threads, p.rows), p.smem, st, a);
 }
-template <typename X, typename Y, bool SHIFTED>
+template <typename X, typename Y, bool PHASED>
 bool ring_forward(const NormForward& a, const NormPlan& p, cudaStream_t st) {
     switch (p.vpt) {
-        case 1: return launch_norm(k_norm_forward<X, Y, 1, SHIFTED>, p, a, st);
-        case 2: return launch_norm(k_norm_forward<X, Y, 2, SHIFTED>, p, a, st);
-        case 3: return launch_norm(k_norm_forward<X, Y, 3, SHIFTED>, p, a, st);
-        case 4: return launch_norm(k_norm_forward<X, Y, 4, SHIFTED>, p, a, st);
+        case 1: return launch_norm(k_norm_forward<X, Y, 1, PHASED>, p, a, st);
+        case 2: return launch_norm(k_norm_forward<X, Y, 2, PHASED>, p, a, st);
+        case 3: return launch_norm(k_norm_forward<X, Y, 3, PHASED>, p, a, st);
+        case 4: return launch_norm(k_norm_forward<X, Y, 4, PHASED>, p, a, st);
     }
-    if constexpr (!SHIFTED) return launch_norm(k_norm_forward<X, Y, 8, false>, p, a, st);
+    if constexpr (!PHASED) return launch_norm(k_norm_forward<X, Y, 8, false>, p, a, st);
     return false;
 }
 template <typename X, typename Y>
@@ -106,8 +109,18 @@ bool norm_forward(NormForward a, const NormPlan& p, NormRows rows, cudaStream_t 
     a.stages = p.stages;
     if (p.wide) return rows == RING ? launch_norm(k_norm_forward_wide<X, Y, true>, p, a, st) : launch_norm(k_norm_forward_wide<X, Y, false>, p, a, st);
     if (rows == RING) return ring_forward<X, Y, false>(a, p, st);
-    if constexpr (sizeof(X) == 2) return ring_forward<X, Y, true>(a, p, st);
-    else return launch_norm(k_norm_forward_any<X, Y>, p, a, st);
+    if constexpr (sizeof(X) == 2)
+        if (rows == PHASE) return ring_forward<X, Y, true>(a, p, st);
+    return launch_norm(k_norm_forward_any<X, Y>, p, a, st);
+}
+template <typename X, typename Y, bool PHASED>
+bool ring_backward(const NormBackward& a, const NormPlan& p, cudaStream_t st) {
+    switch (p.vpt) {
+        case 1: return launch_norm(k_norm_backward<X, Y, 1, PHASED>, p, a, st);
+        case 2: return launch_norm(k_norm_backward<X, Y, 2, PHASED>, p, a, st);
+        case 3: return launch_norm(k_norm_backward<X, Y, 3, PHASED>, p, a, st);
+    }
+    return launch_norm(k_norm_backward<X, Y, 4, PHASED>, p, a, st);
 }
 template <typename X, typename Y>
 bool norm_backward(NormBackward a, const NormGrad& g, NormRows rows, cudaStream_t st) {
@@ -118,13 +131,10 @@ bool norm_backward(NormBackward a, const NormGrad& g, NormRows rows, cudaStream_
         if (rows == RING) return launch_norm(k_norm_sums_wide<X, Y, true>, p, a, st) && launch(k_norm_apply_wide<X, Y, true>, grid, block, 0, st, a);
         return launch_norm(k_norm_sums_wide<X, Y, false>, p, a, st) && launch(k_norm_apply_wide<X, Y, false>, grid, block, 0, st, a);
     }
-    if (rows == LANES) return launch_norm(k_norm_backward_any<X, Y>, p, a, st);
-    switch (p.vpt) {
-        case 1: return launch_norm(k_norm_backward<X, Y, 1>, p, a, st);
-        case 2: return launch_norm(k_norm_backward<X, Y, 2>, p, a, st);
-        case 3: return launch_norm(k_norm_backward<X, Y, 3>, p, a, st);
-        default: return launch_norm(k_norm_backward<X, Y, 4>, p, a, st);
-    }
+    if (rows == RING) return ring_backward<X, Y, false>(a, p, st);
+    if constexpr (sizeof(X) == 2)
+        if (rows == PHASE) return ring_backward<X, Y, true>(a, p, st);
+    return launch_norm(k_norm_backward_any<X, Y>, p, a, st);
 }
 // the pairs of types: x and y (dy) alike, or x float32 and y bfloat16
 bool types_ok(int x, int y) { return dtype_ok(x) && dtype_ok(y) && (x == y || x == PSGD_DT_F32); }
@@ -161,14 +171,15 @@ psgd_status psgd_norm_forward(const void* x, int64_t ldx, int x_dtype, const voi
     const Stretch sum = stretch(s, T, F, lds, size_of(x_dtype)), out = stretch(y, T, F, ldy, size_of(y_dtype));
     if (overlap(in[0], sum) || overlap(in[0], out) || overlap(in[1], sum) || overlap(in[1], out) || overlap(sum, out)) return PSGD_E_INVALID;
     const bool whole = whole_units(x, ldx, F, x_dtype) && whole_units(r, ldr, F, x_dtype) && whole_units(s, lds, F, x_dtype) && whole_units(y, ldy, F, y_dtype);
-    const NormRows rows = whole ? RING : x_dtype == PSGD_DT_BF16 ? SHIFT : LANES;
+    const bool same = x_dtype == PSGD_DT_BF16 && alike(x, ldx, r, ldr, T) && alike(x, ldx, s, lds, T) && alike(x, ldx, y, ldy, T);
+    const NormRows rows = whole ? RING : same ? PHASE : LANES;
     NormForward a{};
     a.T = T; a.F = (int)F; a.center = center != 0; a.eps = eps;
     a.x = x; a.r = r; a.s = s; a.y = y;
     a.ldx = ldx; a.ldr = ldr; a.lds = lds; a.ldy = ldy;
     a.w = {w, w_dtype == PSGD_DT_BF16}; a.b = {b, w_dtype == PSGD_DT_BF16};
     a.mean = center ? mean : nullptr; a.rstd = rstd; a.q = q; a.scales = scales;
-    const NormPlan p = plan_norm(T, F, rows, F * size_of(x_dtype) * (r ? 2 : 1), r != nullptr, false);
+    const NormPlan p = plan_norm(T, F, rows, F * size_of(x_dtype) * (r ? 2 : 1), r != nullptr, q != nullptr, false);
     const bool ok = by_type(x_dtype, y_dtype, [&](auto* tx, auto* ty) {
         return norm_forward<std::remove_pointer_t<decltype(tx)>, std::remove_pointer_t<decltype(ty)>>(a, p, rows, (cudaStream_t)stream);
     });
@@ -182,7 +193,7 @@ psgd_status psgd_norm_workspace(int64_t T, int64_t F, size_t* bytes) {
     if (T > 0) {
         // whatever the types, the alignment and the operands (2 + 2, 4 + 2, 4 + 4 bytes per column, and x's again)
         *bytes = plan_norm_grad(T, F, LANES, 0).total;
-        for (int each : {4, 6, 8, 10, 12}) *bytes = std::max(*bytes, plan_norm_grad(T, F, RING, F * each).total);
+        for (int each : {4, 6, 8, 10, 12}) *bytes = std::max({*bytes, plan_norm_grad(T, F, RING, F * each).total, plan_norm_grad(T, F, PHASE, F * each).total});
     }
     return PSGD_OK;
 }
@@ -201,7 +212,9 @@ psgd_status psgd_norm_backward(const void* dy, int64_t lddy, int dy_dtype, const
     const Stretch out = stretch(dx, T, F, lddx, size);
     if (overlap(out, stretch(dy, T, F, lddy, size_of(dy_dtype))) || overlap(out, stretch(x, T, F, ldx, size)) || overlap(out, stretch(add, T, F, ldadd, size))) return PSGD_E_INVALID;
     const bool whole = whole_units(dy, lddy, F, dy_dtype) && whole_units(x, ldx, F, x_dtype) && whole_units(add, ldadd, F, x_dtype) && whole_units(dx, lddx, F, x_dtype);
-    const NormRows rows = whole ? RING : LANES;
+    const bool same = x_dtype == PSGD_DT_BF16 && alike(x, ldx, dy, lddy, T) && alike(x, ldx, add, ldadd, T) && alike(x, ldx, dx, lddx, T);
+    // (16384 rows with two operands to read: 1801 columns 70 us by lanes, 75 by units; 2051: 113, 74; 4099: 591, 156)
+    const NormRows rows = whole ? RING : same && F >= 2048 ? PHASE : LANES;
     const NormGrad g = plan_norm_grad(T, F, rows, F * (size_of(dy_dtype) + size * (add ? 2 : 1)));
     if (ws_bytes < g.total) return PSGD_E_WORKSPACE;
     NormBackward a{};

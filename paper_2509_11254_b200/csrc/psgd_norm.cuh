@@ -13,9 +13,9 @@
 //
 // Rows of whole 16-byte units come through a ring in shared memory: every thread copies its own units of the rows to come asynchronously (cp.async) and reads back only
 // what it copied itself, so that there is nothing to wait for but its own copies, rows are under way whatever the registers hold, and the backward pass
-// reads a row a second time from there.  Rows of bfloat16 of any other width or alignment go the same way forward (SHIFT), the units of memory that they lie in being cut to
-// the threads' values (16384 x 2051 with a residual 91 us, a value per lane 104); backward, where every row is read twice, that costs more than it saves (119 against
-// 115 us; 16384 x 771: 50, 38).  There and for float32 (.._any): a value per lane, the next row's values in registers.
+// reads a row a second time from there.  Rows of bfloat16 of any other width or alignment go the same way where all operands lie alike (PHASE: matrices of one odd width, for
+// instance): the units are then those of memory, and a CTA takes rows that begin at the same place in them.  Anything else (.._any): a value per lane, the next row's values in
+// registers.  16384 x 2051 with a residual: 61 us forward and 74 backward (with a second gradient) by units, 103 and 115 by lanes.
 // Sums and statistics are float32.  Rounded once: s to x's type, y, ds; the 8-bit form is that of the rounded y.
 #pragma once
 #include "psgd_values.cuh"
@@ -220,20 +220,20 @@ __device__ __forceinline__ void copy16_of(unsigned to, const void* from, int byt
 __device__ __forceinline__ F2 pair_of(unsigned x, unsigned y) { return pair(__uint_as_float(x), __uint_as_float(y)); }
 // bytes of a unit in one plane, and of all planes of an operand
 template <typename T, typename X> __device__ __forceinline__ constexpr int unit_bytes() { return sizeof(X) == 2 ? 16 : 4 * (int)sizeof(T); }
-template <typename T, int VPT, bool SHIFT> __device__ __forceinline__ int operand_bytes() {
-    return VPT * (int)blockDim.x * 8 * (int)sizeof(T) + (SHIFT ? (int)(blockDim.x >> 5) * 16 : 0);
-}
-// Columns of a thread's pieces (those that do not exist fetch the row's last one: no branches), and how many of a unit's values exist.
-template <typename X, int VPT, bool SHIFT>
+template <typename T, int VPT> __device__ __forceinline__ int operand_bytes() { return VPT * (int)blockDim.x * 8 * (int)sizeof(T); }
+// Columns of a thread's pieces, and how many of a unit's values exist.  Aligned rows: pieces that do not exist fetch the row's last one: no branches.
+// PHASE: rows of bfloat16 of any width and alignment that all operands share (the same place within 16 bytes in every row).  The units are those of memory: the first one begins
+// `phase` values before the row.  A CTA takes rows whose phase is the same (every gridDim.x-th, a multiple of eight), so that its columns stay its own.
+template <typename X, int VPT, bool PHASE>
 struct Place {
-    int at[VPT][sizeof(X) == 2 ? 1 : 2], n[VPT];
-    __device__ __forceinline__ explicit Place(int F) {
+    int at[VPT][sizeof(X) == 2 ? 1 : 2], n[VPT], phase;
+    __device__ __forceinline__ Place(int F, int phase) : phase(phase) {
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             const int u = unit_of<VPT>(i), c0 = piece_col<X>(u, 0), c1 = piece_col<X>(u, 1);
-            if constexpr (SHIFT) {
-                at[i][0] = c0;
-                n[i] = min(max(F - c0, 0), 8);
+            if constexpr (PHASE) {
+                at[i][0] = c0 - phase;
+                n[i] = min(max(F + phase - c0, 0), 8);             // (from the unit's beginning on, the values before the row included)
                 continue;
             }
             at[i][0] = min(c0, F - (sizeof(X) == 2 ? 8 : 4));
@@ -241,31 +241,37 @@ struct Place {
             n[i] = (c0 < F ? 4 : 0) + (c1 < F ? 4 : 0);
         }
     }
+    __device__ __forceinline__ int low(int i) const { return PHASE && unit_of<VPT>(i) == 0 ? phase : 0; }      // values of the unit that lie before the row
+    __device__ __forceinline__ bool whole(int i) const { return n[i] - low(i) == 8; }
+    // PHASE: zeros where a value is not the row's
+    __device__ __forceinline__ void clear(int i, Eight& v) const {
+        if (!PHASE || whole(i)) return;
+        float x[8];
+        singles(v, x);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = j >= low(i) && j < n[i] ? x[j] : 0.f;
+        v = eight(x);
+    }
 };
-// SHIFT: rows of bfloat16 of any width and alignment.  The ring holds the 16-byte units of memory that a row lies in, as many as it has units of eight values and one more
-// per warp, so that a warp's values are among its own copies and a lane cuts its eight out of its unit and the next lane's.  Nothing behind the row's end is read (the
-// copy ends there and fills up with zeros); what lies before its beginning in its first unit are rows before it, and where that would be before the matrix, the unit is read value by value.
-__device__ __forceinline__ unsigned image_unit(unsigned operand, int vpt, int k) { return operand + ((threadIdx.x >> 5) * (32 * vpt + 1) + k) * 16; }       // k-th unit of the warp's
-__device__ __forceinline__ void image_ask(unsigned to, const __nv_bfloat16* row, int u, int F, const __nv_bfloat16* matrix) {
-    const unsigned sh = shift_of(row);
-    const int bytes = min(max((int)sh + 2 * F - 16 * u, 0), 16);
-    const char* from = reinterpret_cast<const char*>(row) - sh;
-    if (u == 0 && from < reinterpret_cast<const char*>(matrix)) {
-        for (int b = 0; b < 16; b += 2) {
-            const unsigned short h = b >= (int)sh && b < (int)sh + 2 * F ? reinterpret_cast<const unsigned short*>(row)[(b - (int)sh) / 2] : (unsigned short)0;
-            asm volatile("st.shared.u16 [%0], %1;\n" ::"r"(to + b), "h"(h) : "memory");
+// PHASE: how many values before row `row` of matrix `p` its first unit of 16 bytes begins
+__device__ __forceinline__ int phase_of(const void* p, long long row, long long ld) { return (int)((reinterpret_cast<uintptr_t>(p) / 2 + (unsigned long long)(row * ld)) & 7); }
+// PHASE: a unit, up to the row's end (zeros behind it).  What lies before the row in its first unit is the row before it, or, before the matrix, not read.
+__device__ __forceinline__ void phase_ask(unsigned to, const __nv_bfloat16* from, int n, const __nv_bfloat16* matrix) {
+    if (n > 0 && from < matrix) {
+        for (int j = 0; j < 8; ++j) {
+            const unsigned short h = from + j >= matrix && j < n ? reinterpret_cast<const unsigned short*>(from)[j] : (unsigned short)0;
+            asm volatile("st.shared.u16 [%0], %1;\n" ::"r"(to + 2 * j), "h"(h) : "memory");
         }
         return;
     }
-    copy16_of(to, bytes ? from + 16 * (size_t)u : from, bytes);
+    copy16_of(to, n > 0 ? from : matrix + (8 - phase_of(matrix, 0, 0)) % 8, 2 * n);
 }
 // `operand`: where the operand's planes begin
-template <typename T, typename X, int VPT, bool SHIFT>
-__device__ __forceinline__ void ring_ask(unsigned operand, const T* row, const Place<X, VPT, SHIFT>& p, int F, const T* matrix) {
-    if constexpr (SHIFT) {
+template <typename T, typename X, int VPT, bool PHASE>
+__device__ __forceinline__ void ring_ask(unsigned operand, const T* row, const Place<X, VPT, PHASE>& p, const T* matrix) {
+    if constexpr (PHASE) {
 #pragma unroll
-        for (int i = 0; i < VPT; ++i) image_ask(image_unit(operand, VPT, 32 * i + (threadIdx.x & 31)), row, unit_of<VPT>(i), F, matrix);
-        if ((threadIdx.x & 31) == 31) image_ask(image_unit(operand, VPT, 32 * VPT), row, unit_of<VPT>(VPT - 1) + 1, F, matrix);
+        for (int i = 0; i < VPT; ++i) phase_ask(operand + unit_of<VPT>(i) * 16, row + p.at[i][0], p.n[i], matrix);
         return;
     }
     constexpr int B = unit_bytes<T, X>();
@@ -281,19 +287,8 @@ __device__ __forceinline__ void ring_ask(unsigned operand, const T* row, const P
         }
     }
 }
-// a unit of a shifted row (`row`: where it lies in memory) as eight bfloat16
-template <int VPT>
-__device__ __forceinline__ uint4 image_read(unsigned operand, int i, const __nv_bfloat16* row) {
-    const unsigned at = image_unit(operand, VPT, 32 * i + (threadIdx.x & 31));
-    return cut_out(shared16(at), shared16(at + 16), shift_of(row));
-}
-template <typename T, typename X, int VPT, bool SHIFT>
-__device__ __forceinline__ Eight ring_read(unsigned operand, int i, const T* row) {
-    if constexpr (SHIFT) {
-        float v[8];
-        widen(Raw16{image_read<VPT>(operand, i, row)}, v);
-        return eight(v);
-    }
+template <typename T, typename X, int VPT>
+__device__ __forceinline__ Eight ring_read(unsigned operand, int i) {
     constexpr int B = unit_bytes<T, X>();
     const unsigned at = operand + unit_of<VPT>(i) * B;
     if constexpr (sizeof(T) == 4) {
@@ -312,25 +307,26 @@ __device__ __forceinline__ Eight ring_read(unsigned operand, int i, const T* row
         return eight(v);
     }
 }
-// A unit's values (eight bfloat16) to a row of any alignment; `image`: the warp's 34 units to turn its values into units of memory.
-template <int VPT>
-__device__ __forceinline__ void image_store(__nv_bfloat16* row, int i, int F, const uint4& v, uint4* image) {
-    const int first = unit_of<VPT>(i) * 8 - (int)(threadIdx.x & 31) * 8;                        // the same in all lanes
-    if (first < F) store_any(row + unit_of<VPT>(i) * 8, v, min(F - first, 256), image);
-}
 // A unit's values to a row of T beside an x of type X.
-template <typename T, typename X, int VPT, bool SHIFT>
-__device__ __forceinline__ void unit_store(T* row, const Place<X, VPT, SHIFT>& p, int i, const Eight& v, int F, uint4* image) {
+template <typename T, typename X, int VPT, bool PHASE>
+__device__ __forceinline__ void unit_store(T* row, const Place<X, VPT, PHASE>& p, int i, const Eight& v) {
     float x[8];
     singles(v, x);
-    if constexpr (SHIFT) {
-        image_store<VPT>(row, i, F, pack_bf16x8(x), image);
-    } else if constexpr (sizeof(T) == 4) {
+    if constexpr (sizeof(T) == 4) {
         if (p.n[i] > 0) *reinterpret_cast<float4*>(row + p.at[i][0]) = make_float4(x[0], x[1], x[2], x[3]);
         if (p.n[i] > 4) *reinterpret_cast<float4*>(row + p.at[i][1]) = make_float4(x[4], x[5], x[6], x[7]);
     } else {
         const uint4 b = pack_bf16x8(x);
-        if constexpr (sizeof(X) == 2) {
+        if constexpr (PHASE) {
+            if (p.whole(i)) {
+                *reinterpret_cast<uint4*>(row + p.at[i][0]) = b;
+            } else {                                   // the row's beginning or its end
+                const unsigned w[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (j >= p.low(i) && j < p.n[i]) reinterpret_cast<unsigned short*>(row + p.at[i][0])[j] = (unsigned short)(w[j / 2] >> (j & 1) * 16);
+            }
+        } else if constexpr (sizeof(X) == 2) {
             if (p.n[i] > 0) *reinterpret_cast<uint4*>(row + p.at[i][0]) = b;
         } else {
             if (p.n[i] > 0) *reinterpret_cast<uint2*>(row + p.at[i][0]) = make_uint2(b.x, b.y);
@@ -346,28 +342,33 @@ __device__ __forceinline__ float sum_of(const Eight& v, int n) {
     return (n > 0 ? a + b : 0.f) + (n > 4 ? c + d : 0.f);
 }
 // A unit of x + r, rounded to their type, written to row s.  Sums of bfloat16 are rounded once by the packed addition itself.
-template <typename X, int VPT, bool SHIFT>
-__device__ __forceinline__ Eight ring_sum(unsigned x_at, unsigned r_at, int i, X* s, const Place<X, VPT, SHIFT>& p, const X* x_row, const X* r_row, int F, uint4* image) {
+template <typename X, int VPT, bool PHASE>
+__device__ __forceinline__ Eight ring_sum(unsigned x_at, unsigned r_at, int i, X* s, const Place<X, VPT, PHASE>& p) {
+    Eight v;
     if constexpr (sizeof(X) == 2) {
-        const uint4 x = SHIFT ? image_read<VPT>(x_at, i, x_row) : shared16(x_at + unit_of<VPT>(i) * 16), r = SHIFT ? image_read<VPT>(r_at, i, r_row) : shared16(r_at + unit_of<VPT>(i) * 16);
+        const uint4 x = shared16(x_at + unit_of<VPT>(i) * 16), r = shared16(r_at + unit_of<VPT>(i) * 16);
         const auto sum = [](unsigned u, unsigned v) {
             const __nv_bfloat162 t = __hadd2(*reinterpret_cast<const __nv_bfloat162*>(&u), *reinterpret_cast<const __nv_bfloat162*>(&v));
             return *reinterpret_cast<const unsigned*>(&t);
         };
         const uint4 t = make_uint4(sum(x.x, r.x), sum(x.y, r.y), sum(x.z, r.z), sum(x.w, r.w));
-        if constexpr (SHIFT) image_store<VPT>(s, i, F, t, image);
-        else if (p.n[i]) *reinterpret_cast<uint4*>(s + p.at[i][0]) = t;
-        float v[8];
-        widen(Raw16{t}, v);
-        return eight(v);
+        float f[8];
+        widen(Raw16{t}, f);
+        v = eight(f);
+        if constexpr (PHASE) {
+            unit_store<X, X, VPT, PHASE>(s, p, i, v);  // (rounded already: the same bits)
+            p.clear(i, v);
+        } else if (p.n[i]) {
+            *reinterpret_cast<uint4*>(s + p.at[i][0]) = t;
+        }
     } else {
-        Eight x = ring_read<X, X, VPT, SHIFT>(x_at, i, x_row);
-        const Eight r = ring_read<X, X, VPT, SHIFT>(r_at, i, r_row);
+        v = ring_read<X, X, VPT>(x_at, i);
+        const Eight r = ring_read<X, X, VPT>(r_at, i);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) x.p[j] = add2(x.p[j], r.p[j]);
-        unit_store<X, X, VPT, SHIFT>(s, p, i, x, F, image);
-        return x;
+        for (int j = 0; j < 4; ++j) v.p[j] = add2(v.p[j], r.p[j]);
+        unit_store<X, X, VPT, PHASE>(s, p, i, v);
     }
+    return v;
 }
 // The 8-bit form of a unit's values of a row of T (see cell_keep); all lanes call.
 template <typename T, typename X>
@@ -407,12 +408,12 @@ __device__ __forceinline__ void ring_wait(int stages) {
 }
 // A vector over the columns as float32 in shared memory: a plane of first pieces, a plane of second ones (zeros where there is none), by the whole CTA.
 template <typename X>
-__device__ __forceinline__ void param_planes(unsigned char* to, const NormParam& v, int units, int F, float none) {
+__device__ __forceinline__ void param_planes(unsigned char* to, const NormParam& v, int units, int F, int phase, float none) {
     for (int k = threadIdx.y * blockDim.x + threadIdx.x; k < 2 * units; k += blockDim.x * blockDim.y) {
-        const int c = piece_col<X>(k >> 1, k & 1);
+        const int c = piece_col<X>(k >> 1, k & 1) - phase;
         float x[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] = c + j < F ? param_at(v, c + j, none) : 0.f;
+        for (int j = 0; j < 4; ++j) x[j] = c + j >= 0 && c + j < F ? param_at(v, c + j, none) : 0.f;
         reinterpret_cast<float4*>(to)[(k & 1) * units + (k >> 1)] = make_float4(x[0], x[1], x[2], x[3]);
     }
 }
@@ -424,40 +425,33 @@ __device__ __forceinline__ Eight param_read(unsigned planes, int units, int i) {
     return {{pair_of(a.x, a.y), pair_of(a.z, a.w), pair_of(b.x, b.y), pair_of(b.z, b.w)}};
 }
 
-// the warp's units for image_store
-template <bool SHIFT>
-__device__ __forceinline__ uint4* norm_image() {
-    __shared__ uint4 image[SHIFT ? NORM_WARPS * ANY_UNITS : 1];
-    return SHIFT ? image + ((threadIdx.y * blockDim.x + threadIdx.x) >> 5) * ANY_UNITS : nullptr;
-}
-
-template <typename X, typename Y, int VPT, bool SHIFT>
+template <typename X, typename Y, int VPT, bool PHASE>
 __global__ void __launch_bounds__(NORM_THREADS) k_norm_forward(const __grid_constant__ NormForward a) {
-    extern __shared__ __align__(16) unsigned char ring_raw[];          // w, b, then the rings
+    extern __shared__ __align__(16) unsigned char ring_raw[];          // w, b, then the rings; PHASE with an 8-bit form: a row of each group at last
     __shared__ float2 stat[2][NORM_WARPS];             // by rows taken in turn: a row's exchange is over when the next but one writes
     __shared__ float counts[NORM_WARPS];
     grid_trigger();
     const int F = a.F, tid = threadIdx.x, warps = blockDim.x >> 5, units = VPT * blockDim.x;
-    const Place<X, VPT, SHIFT> p(F);
-    uint4* image = norm_image<SHIFT>();
+    const int phase = PHASE ? phase_of(a.x, blockIdx.x, a.ldx) : 0;
+    const Place<X, VPT, PHASE> p(F, phase);
     int have = 0;
 #pragma unroll
-    for (int i = 0; i < VPT; ++i) have += p.n[i];
+    for (int i = 0; i < VPT; ++i) have += max(p.n[i] - p.low(i), 0);
     const float in_warp = (float)__reduce_add_sync(0xffffffffu, have), per = 1.f / (float)F, per_warp = 1.f / fmaxf(in_warp, 1.f);
     if (threadIdx.y == 0 && (tid & 31) == 0) counts[tid >> 5] = in_warp;
     grid_wait();
     const long long step = (long long)gridDim.x * blockDim.y;
-    long long row = (long long)blockIdx.x * blockDim.y + threadIdx.y, asked = row;
+    long long row = PHASE ? blockIdx.x + (long long)gridDim.x * threadIdx.y : (long long)blockIdx.x * blockDim.y + threadIdx.y, asked = row;
     // rows: the one that is asked for next (x, r) and the one at work (s, y)
     const X *x = (const X*)a.x + row * a.ldx, *r = a.r ? (const X*)a.r + row * a.ldr : nullptr;
     X* s = a.s ? (X*)a.s + row * a.lds : nullptr;
     Y* y = (Y*)a.y + row * a.ldy;
-    const int operand = operand_bytes<X, VPT, SHIFT>(), stage = r ? 2 * operand : operand, stages = a.stages;
+    const int operand = operand_bytes<X, VPT>(), stage = r ? 2 * operand : operand, stages = a.stages;
     const unsigned params = smem_addr(ring_raw), ring = params + units * 64 + threadIdx.y * stages * stage;
     const auto ask = [&](unsigned to) {
         if (asked < a.T) {
-            ring_ask<X, X, VPT, SHIFT>(to, x, p, F, (const X*)a.x);
-            if (r) ring_ask<X, X, VPT, SHIFT>(to + operand, r, p, F, (const X*)a.r);
+            ring_ask<X, X, VPT, PHASE>(to, x, p, (const X*)a.x);
+            if (r) ring_ask<X, X, VPT, PHASE>(to + operand, r, p, (const X*)a.r);
         }
         ring_commit();
         asked += step;
@@ -465,26 +459,29 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_forward(const __grid_cons
         if (r) r += step * a.ldr;
     };
     for (int k = 0; k < stages; ++k) ask(ring + k * stage);
-    param_planes<X>(ring_raw, a.w, units, F, 1.f);
-    param_planes<X>(ring_raw + units * 32, a.b, units, F, 0.f);
+    param_planes<X>(ring_raw, a.w, units, F, phase, 1.f);
+    param_planes<X>(ring_raw + units * 32, a.b, units, F, phase, 0.f);
     __syncthreads();
     const float in_lane = (tid & 15) < warps ? counts[tid & 15] : 0.f;
     const int G = (F + ACT_GROUP - 1) / ACT_GROUP;
+    // PHASE: the row's rounded result as it lies in memory, for the groups of its 8-bit form, which begin with the row
+    const unsigned image = params + units * 64 + blockDim.y * stages * stage + threadIdx.y * (units * 16 + 16);
     unsigned from = ring;
     for (int turn = 0; row < a.T; row += step, turn ^= 1) {
         Eight v[VPT];
         ring_wait(stages);
-        if (SHIFT) __syncwarp();                       // (values of other lanes' copies)
-        const X *x_row = SHIFT ? (const X*)a.x + row * a.ldx : nullptr, *r_row = SHIFT && r ? (const X*)a.r + row * a.ldr : nullptr;
         if (r) {
 #pragma unroll
-            for (int i = 0; i < VPT; ++i) v[i] = ring_sum<X, VPT, SHIFT>(from, from + operand, i, s, p, x_row, r_row, F, image);
+            for (int i = 0; i < VPT; ++i) v[i] = ring_sum<X, VPT, PHASE>(from, from + operand, i, s, p);
         } else {
 #pragma unroll
-            for (int i = 0; i < VPT; ++i) v[i] = ring_read<X, X, VPT, SHIFT>(from, i, x_row);
+            for (int i = 0; i < VPT; ++i) {
+                v[i] = ring_read<X, X, VPT>(from, i);
+                p.clear(i, v[i]);
+            }
             if (s) {
 #pragma unroll
-                for (int i = 0; i < VPT; ++i) unit_store<X, X, VPT, SHIFT>(s, p, i, v[i], F, image);
+                for (int i = 0; i < VPT; ++i) unit_store<X, X, VPT, PHASE>(s, p, i, v[i]);
             }
         }
         float m = 0.f;
@@ -497,16 +494,9 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_forward(const __grid_cons
             for (int i = 0; i < VPT; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) v[i].p[j] = add2(v[i].p[j], off);
-            if constexpr (SHIFT) {
+            if constexpr (PHASE) {
 #pragma unroll
-                for (int i = 0; i < VPT; ++i) {
-                    if (p.n[i] == 8) continue;         // the row's end: zeros again
-                    float t[8];
-                    singles(v[i], t);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) t[j] = j < p.n[i] ? t[j] : 0.f;
-                    v[i] = eight(t);
-                }
+                for (int i = 0; i < VPT; ++i) p.clear(i, v[i]);
             }
         }
         float sq = 0.f;
@@ -519,7 +509,6 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_forward(const __grid_cons
             sq += (p.n[i] > 0 ? t[0] + t[1] : 0.f) + (p.n[i] > 4 ? t[2] + t[3] : 0.f);
         }
         RowStats st{m, warp_sum(sq)};
-        if (SHIFT) __syncwarp();
         ask(from);                                     // (every value has been used)
         from = stages == 1 || from != ring ? ring : ring + stage;
         if (warps > 1) st = join_warps(st.mean, st.m2, stat[turn] + threadIdx.y * warps, in_lane, per, a.center);
@@ -535,8 +524,31 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_forward(const __grid_cons
             Eight o;
 #pragma unroll
             for (int j = 0; j < 4; ++j) o.p[j] = fma2(mul2(add2(v[i].p[j], off), ff), w.p[j], b.p[j]);
-            unit_store<Y, X, VPT, SHIFT>(y, p, i, o, F, image);
-            if (a.q) unit_keep<Y, X>(o, unit_of<VPT>(i), p.n[i], row * G, G, a.q, a.scales);
+            unit_store<Y, X, VPT, PHASE>(y, p, i, o);
+            if constexpr (PHASE) {
+                if (a.q) {
+                    float t[8];
+                    singles(o, t);
+                    const uint4 b = pack_bf16x8(t);
+                    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};\n" ::"r"(image + unit_of<VPT>(i) * 16), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w) : "memory");
+                }
+            } else if (a.q) {
+                unit_keep<Y, X>(o, unit_of<VPT>(i), p.n[i], row * G, G, a.q, a.scales);
+            }
+        }
+        if constexpr (PHASE) {
+            if (a.q) {
+                row_sync();
+#pragma unroll
+                for (int i = 0; i < VPT; ++i) {
+                    const int u = unit_of<VPT>(i);
+                    const unsigned at = image + u * 16;
+                    float t[8];
+                    widen(Raw16{cut_out(shared16(at), shared16(at + 16), 2 * phase)}, t);
+                    unit_keep<Y, X>(eight(t), u, min(max(F - u * 8, 0), 8), row * G, G, a.q, a.scales);
+                }
+                if (warps == 1) __syncwarp();          // (several: the next row's exchange comes before its values)
+            }
         }
         if (s) s += step * a.lds;
         y += step * a.ldy;
@@ -712,16 +724,17 @@ __device__ __forceinline__ void sum_warps(float& s1, float& s2, float2* mine) {
         s2 += t.y;
     }
 }
-// At the end: the CTA's sums of dw and db, its rows side by side (threadIdx.y) through `sums` [blockDim.y][2][F]; a CTA alone writes the results.  `column(i, j)`: of value j
-// of the thread's unit i (FOUR: four of them side by side at a multiple of four), `n`: how many of its values exist.
+// At the end: the CTA's sums of dw and db, its rows side by side (threadIdx.y) through `sums` [blockDim.y][2][pitch]; a CTA alone writes the results.  `column(i, j)`: of value j
+// of the thread's unit i (FOUR: four of them side by side at a multiple of four), `n`: how many of its values exist.  The first `phase` columns are not the row's (PHASE, where
+// the pitch is a row's units and a row alone goes that way too: 16 bytes at a time into shared memory, a line at a time out of it).
 template <int VPT, bool FOUR, typename Column>
-__device__ __forceinline__ void write_columns(const NormBackward& a, float* sums, const Eight (&dw)[VPT], const Eight (&db)[VPT], const int (&n)[VPT], Column&& column) {
+__device__ __forceinline__ void write_columns(const NormBackward& a, float* sums, int pitch, int phase, const Eight (&dw)[VPT], const Eight (&db)[VPT], const int (&n)[VPT], Column&& column) {
     const int F = a.F;
     float* pw = gridDim.x == 1 ? a.dw : a.part + (size_t)blockIdx.x * 2 * F;
     float* pb = gridDim.x == 1 ? a.db : pw + F;
-    const bool alone = blockDim.y == 1;
+    const bool alone = blockDim.y == 1 && pitch == F;
     if (!alone) __syncthreads();                       // (nobody reads what lay there)
-    float *to_w = alone ? pw : sums + (size_t)threadIdx.y * 2 * F, *to_b = alone ? pb : to_w + F;
+    float *to_w = alone ? pw : sums + (size_t)threadIdx.y * 2 * pitch, *to_b = alone ? pb : to_w + pitch;
     const bool whole = (((uintptr_t)to_w | (uintptr_t)to_b) & 15) == 0;
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
@@ -748,29 +761,33 @@ __device__ __forceinline__ void write_columns(const NormBackward& a, float* sums
     }
     if (alone) return;
     __syncthreads();
-    for (int c = threadIdx.y * blockDim.x + threadIdx.x; c < 2 * F; c += blockDim.x * blockDim.y) {
-        float sum = 0.f;
-        for (int k = 0; k < (int)blockDim.y; ++k) sum += sums[(size_t)k * 2 * F + c];
-        if (c < F) pw[c] = sum;
-        else if (pb) pb[c - F] = sum;
+    for (int c = threadIdx.y * blockDim.x + threadIdx.x; c < F; c += blockDim.x * blockDim.y) {
+        float w = 0.f, b = 0.f;
+        for (int k = 0; k < (int)blockDim.y; ++k) {
+            w += sums[(size_t)k * 2 * pitch + phase + c];
+            b += sums[(size_t)k * 2 * pitch + pitch + phase + c];
+        }
+        pw[c] = w;
+        if (pb) pb[c] = b;
     }
 }
 
-template <typename X, typename Y, int VPT>
+template <typename X, typename Y, int VPT, bool PHASE>
 __global__ void __launch_bounds__(NORM_THREADS) k_norm_backward(const __grid_constant__ NormBackward a) {
     extern __shared__ __align__(16) unsigned char ring_raw[];          // w, then the rings; at the end the sums of the rows side by side
     __shared__ float2 stat[2][NORM_WARPS];
     grid_trigger();
     const int F = a.F, warps = blockDim.x >> 5, units = VPT * blockDim.x;
-    const Place<X, VPT, false> p(F);
+    const int phase = PHASE ? phase_of(a.x, blockIdx.x, a.ldx) : 0;
+    const Place<X, VPT, PHASE> p(F, phase);
     grid_wait();
     const long long step = (long long)gridDim.x * blockDim.y;
-    long long row = (long long)blockIdx.x * blockDim.y + threadIdx.y, asked = row;
+    long long row = PHASE ? blockIdx.x + (long long)gridDim.x * threadIdx.y : (long long)blockIdx.x * blockDim.y + threadIdx.y, asked = row;
     // rows: the one that is asked for next (dy, x, add) and the one at work (dx)
     const Y* dy = (const Y*)a.dy + row * a.lddy;
     const X *x = (const X*)a.x + row * a.ldx, *add = a.add ? (const X*)a.add + row * a.ldadd : nullptr;
     X* dx = (X*)a.dx + row * a.lddx;
-    const int at_x = operand_bytes<Y, VPT, false>(), at_add = at_x + operand_bytes<X, VPT, false>(), stage = add ? at_add + operand_bytes<X, VPT, false>() : at_add, stages = a.stages;
+    const int at_x = operand_bytes<Y, VPT>(), at_add = at_x + operand_bytes<X, VPT>(), stage = add ? at_add + operand_bytes<X, VPT>() : at_add, stages = a.stages;
     const unsigned params = smem_addr(ring_raw), ring = params + units * 32 + threadIdx.y * stages * stage;
     float nm = 0.f, nf = 0.f;                          // the next row's mean and rstd
     const auto ask_stats = [&](long long i) {
@@ -780,9 +797,9 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_backward(const __grid_con
     };
     const auto ask = [&](unsigned to) {
         if (asked < a.T) {
-            ring_ask<Y, X, VPT, false>(to, dy, p, F, dy);
-            ring_ask<X, X, VPT, false>(to + at_x, x, p, F, x);
-            if (add) ring_ask<X, X, VPT, false>(to + at_add, add, p, F, add);
+            ring_ask<Y, X, VPT, PHASE>(to, dy, p, (const Y*)a.dy);
+            ring_ask<X, X, VPT, PHASE>(to + at_x, x, p, (const X*)a.x);
+            if (add) ring_ask<X, X, VPT, PHASE>(to + at_add, add, p, (const X*)a.add);
         }
         ring_commit();
         asked += step;
@@ -792,7 +809,7 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_backward(const __grid_con
     };
     for (int k = 0; k < stages; ++k) ask(ring + k * stage);
     ask_stats(row);
-    param_planes<X>(ring_raw, a.w, units, F, 1.f);
+    param_planes<X>(ring_raw, a.w, units, F, phase, 1.f);
     __syncthreads();
     Eight dw[VPT], db[VPT];
 #pragma unroll
@@ -809,7 +826,10 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_backward(const __grid_con
         F2 t1 = 0ull, t2 = 0ull;
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
-            const Eight d = ring_read<Y, X, VPT, false>(from, i, nullptr), v = ring_read<X, X, VPT, false>(from + at_x, i, nullptr), w = param_read<VPT>(params, units, i);
+            Eight d = ring_read<Y, X, VPT>(from, i), v = ring_read<X, X, VPT>(from + at_x, i);
+            p.clear(i, d);
+            p.clear(i, v);
+            const Eight w = param_read<VPT>(params, units, i);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {              // (w is 0 where there is no value, and its dw and db go nowhere)
                 const F2 xh = mul2(add2(v.p[j], off), ff), g = mul2(d.p[j], w.p[j]);
@@ -830,23 +850,23 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_backward(const __grid_con
         const F2 c1 = pair(s1, s1), c2 = pair(s2, s2);
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
-            const Eight v = ring_read<X, X, VPT, false>(from + at_x, i, nullptr), w = param_read<VPT>(params, units, i);
-            Eight d = ring_read<Y, X, VPT, false>(from, i, nullptr);
+            const Eight v = ring_read<X, X, VPT>(from + at_x, i), w = param_read<VPT>(params, units, i);
+            Eight d = ring_read<Y, X, VPT>(from, i);
 #pragma unroll
             for (int j = 0; j < 4; ++j) d.p[j] = fma2(mul2(d.p[j], w.p[j]), ff, fma2(add2(v.p[j], off), c2, c1));
             if (add) {
-                const Eight u = ring_read<X, X, VPT, false>(from + at_add, i, nullptr);
+                const Eight u = ring_read<X, X, VPT>(from + at_add, i);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) d.p[j] = add2(d.p[j], u.p[j]);
             }
-            unit_store<X, X, VPT, false>(dx, p, i, d, F, nullptr);
+            unit_store<X, X, VPT, PHASE>(dx, p, i, d);
         }
         dx += step * a.lddx;
         ask(from);
         from = stages == 1 || from != ring ? ring : ring + stage;
     }
     asm volatile("cp.async.wait_all;\n" ::: "memory");
-    write_columns<VPT, true>(a, reinterpret_cast<float*>(ring_raw), dw, db, p.n, [](int i, int j) { return piece_col<X>(unit_of<VPT>(i), j >> 2) + (j & 3); });
+    write_columns<VPT, true>(a, reinterpret_cast<float*>(ring_raw), PHASE ? units * 8 : F, phase, dw, db, p.n, [](int i, int j) { return piece_col<X>(unit_of<VPT>(i), j >> 2) + (j & 3); });
 }
 
 template <typename X, typename Y>
@@ -908,7 +928,7 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_backward_any(const __grid
     }
     const Eight sums_w[1] = {eight(dw)}, sums_b[1] = {eight(db)};
     const int many[1] = {n};
-    write_columns<1, false>(a, reinterpret_cast<float*>(ring_raw), sums_w, sums_b, many, [=](int, int j) { return col + 32 * j; });
+    write_columns<1, false>(a, reinterpret_cast<float*>(ring_raw), F, 0, sums_w, sums_b, many, [=](int, int j) { return col + 32 * j; });
 }
 
 // Wide rows: first the two sums of every row (a CTA per row), then dx and the sums over rows (256 units of the columns per CTA, gridDim.y CTAs share the rows).

@@ -554,6 +554,57 @@ def test_norm_rows_of_every_alignment(torch, ops, T, F):
         check_backward(torch, ops, fwd, w, dy, None, False, False)
 
 
+@pytest.mark.parametrize("T,F", [(700, 40), (2500, 2051), (1201, 2047), (700, 5003), (300, 12345), (40, 16371), (17, 16383)])
+def test_norm_many_rows_of_odd_widths(torch, ops, T, F):
+    """Every thread takes several rows, that begin at eight places within 16 bytes."""
+    x, r, w, b = norm_inputs(torch, T, F, F, torch.bfloat16)
+    dy, d_x = (torch.randn(T, F, generator=gen(torch, s), device="cuda").bfloat16() for s in (5, 6))
+    fwd = check_forward(torch, ops, x, w, b, r, 1e-5, True, True, None)
+    check_backward(torch, ops, fwd, w, dy, d_x, True, True)
+    fwd = check_forward(torch, ops, x, w, None, None, 1e-5, False, False, None)
+    check_backward(torch, ops, fwd, w, dy, None, False, False)
+
+
+@pytest.mark.parametrize("T,F", [(1, 5), (9, 3), (1, 771), (20, 771), (1, 2051), (9, 2051), (30, 2056), (13, 4099)])
+def test_norm_operands_that_begin_alike(torch, ops, T, F):
+    """C entry points, all operands at one place within 16 bytes: the same values as those of aligned copies, and nothing else read or written."""
+    from paper_2509_11254_b200 import binding
+
+    L = binding.lib()
+    x, r, w, b = norm_inputs(torch, T, F, F, torch.bfloat16)
+    dy, add = (torch.randn(T, F, generator=gen(torch, s), device="cuda").bfloat16() for s in (1, 2))
+    want = ops.layer_norm_forward(x, w, b, residual=r, keep=True)
+    grad = ops.layer_norm_backward(dy, want.x, w, want.mean, want.rstd, d_x=add, bias=True)
+    for start, gap in ((0, 0), (1, 0), (3, 5), (7, 8), (4, 1)):
+        def part(t=None):
+            flat = torch.full((start + T * (F + gap) + 16,), float("nan"), device="cuda", dtype=torch.bfloat16)
+            view = flat.as_strided((T, F), (F + gap, 1), start)
+            if t is not None:
+                view.copy_(t)
+            return flat, view
+
+        (_, xv), (_, rv), (_, dv), (_, av), (fs, s), (fy, y), (fd, dx) = part(x), part(r), part(dy), part(add), part(), part(), part()
+        f, sums = torch.empty(2, T, device="cuda"), torch.empty(2, F, device="cuda")
+        q, scales = torch.empty_like(want.kept.q), torch.empty_like(want.kept.scales)
+        n = C.c_size_t()
+        assert L.psgd_norm_workspace(T, F, C.byref(n)) == 0
+        ws = torch.empty(n.value, dtype=torch.uint8, device="cuda")
+        at, ld = torch.cuda.current_stream().cuda_stream, F + gap
+        assert L.psgd_norm_forward(xv.data_ptr(), ld, 1, rv.data_ptr(), ld, w.data_ptr(), b.data_ptr(), 0, 1e-5, 1, T, F, s.data_ptr(), ld, y.data_ptr(), ld, 1,
+                                   f[1].data_ptr(), f[0].data_ptr(), q.data_ptr(), scales.data_ptr(), at) == 0
+        again = ops.pack_activation(y.contiguous())
+        assert torch.equal(q, again.q) and torch.equal(scales, again.scales)
+        assert L.psgd_norm_backward(dv.data_ptr(), ld, 1, s.data_ptr(), ld, 1, w.data_ptr(), 0, f[1].data_ptr(), f[0].data_ptr(), av.data_ptr(), ld, T, F, dx.data_ptr(), ld,
+                                    sums.data_ptr(), sums[1].data_ptr(), ws.data_ptr(), n.value, at) == 0
+        assert torch.equal(s, want.x)
+        for t, ref in ((y, want.y), (dx, grad.d_x)):
+            within(t, ref.double(), 2 * 2.0 ** -8 * ref.double().abs() + 1e-5)             # another order of the sums: another rounding of the result, one step of two halves
+        for t, ref, size in ((sums[0], grad.d_weight, dy.double().abs().sum(0) * 8), (sums[1], grad.d_bias, dy.double().abs().sum(0))):
+            within(t, ref.double(), 200 * U * size + 1e-6)
+        for flat in (fs, fy, fd):
+            assert int(torch.isnan(flat).sum()) == flat.numel() - T * F
+
+
 def test_norm_sums_of_bfloat16_are_rounded_once(torch, ops):
     """x + residual over all exponents: subnormal numbers, zeros of either sign, overflow, infinities, ties between two neighbours."""
     g = gen(torch, 1)
