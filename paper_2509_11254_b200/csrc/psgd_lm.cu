@@ -264,6 +264,10 @@ psgd_status xent(const void* H, int64_t ldh, const void* W, int64_t ldw, const i
     if (grad) {                                       // both products run at once: one reads H and W while the other writes
         const Stretch h = stretch(H, T, D, ldh, 2), v = stretch(W, V, D, ldw, 2), dh = stretch(dH, T, D, lddh, 2), dw = stretch(dW, V, D, lddw, 2);
         if (overlap(dh, h) || overlap(dh, v) || overlap(dw, h) || overlap(dw, v) || overlap(dh, dw)) return PSGD_E_INVALID;
+        if (teacher) {                                // later pieces' entries are read after the first one's gradients are written
+            const Stretch z = stretch(teacher->logits, T, teacher->K, teacher->ldl, size_of(teacher->dtype)), i = stretch(teacher->index, T, teacher->K, teacher->ldi, 8);
+            if (overlap(dh, z) || overlap(dh, i) || overlap(dw, z) || overlap(dw, i)) return PSGD_E_INVALID;
+        }
     }
     if (T == 0) {                                     // no token: loss 0, no gradient
         if (!succeeded("cudaMemsetAsync", cudaMemsetAsync(loss, 0, 4, st))) return PSGD_E_CUDA;

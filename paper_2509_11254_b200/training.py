@@ -266,7 +266,7 @@ def linear_distillation(hidden, weight, teacher_logits, teacher_index, temperatu
 def linear_distillation_grad(hidden, weight, teacher_logits, teacher_index, temperature=1.0, token_weight=None, d_hidden=None, d_weight=None, status=None, stream=None):
     """The same with the gradients of the loss: returns (loss, token_loss, lse, d_hidden [T, D], d_weight [V, D]), the gradients bfloat16.
 
-    d_hidden, d_weight: where to write them, as for linear_cross_entropy_grad.
+    d_hidden, d_weight: where to write them, as for linear_cross_entropy_grad; they may not overlap the teacher's lists either.
     """
     return _last_layer(True, hidden, weight, (teacher_logits, teacher_index, temperature), token_weight, d_hidden, d_weight, status, stream)
 

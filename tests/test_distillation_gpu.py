@@ -464,6 +464,16 @@ def test_distillation_warns_and_refuses(torch, ops):
             call()
 
 
+def test_distillation_refuses_gradients_over_its_lists(torch, ops):
+    h, w, z, index = inputs(torch, 40, 90, 64, 64, 72)
+    z = z.bfloat16().contiguous()
+    over = index.view(torch.bfloat16)                  # (40, 256)
+    for out in ({"d_hidden": z}, {"d_hidden": over[:, 64:128]}, {"d_weight": torch.as_strided(over, (90, 64), (64, 1))}):
+        for status in (None, torch.zeros(1, dtype=torch.int32, device="cuda")):
+            with pytest.raises(ops.PSGDError):
+                ops.linear_distillation_grad(h, w, z, index, status=status, **out)
+
+
 @pytest.mark.parametrize("T", [1, 2])
 @pytest.mark.parametrize("V,D,K", [(1, 8, 1), (33, 1, 3), (127, 37, 5), (128, 64, 40), (129, 100, 7), (5000, 768, 64), (700, 2051, 300), (300, 16384, 9), (300, 16392, 9), (4000, 4096, 16), (4001, 8, 1024)])
 def test_distillation_of_one_token(torch, ops, T, V, D, K):
