@@ -17,7 +17,7 @@ bool rows_ok(int64_t T, int64_t F) { return T >= 0 && T <= MAX_EXTENT && extent_
 // ---- layer norm ----
 // How the rows go: RING (16-byte units), PHASE (bfloat16 of any width and alignment, all operands alike), LANES (anything else, a value per lane)
 enum NormRows { RING, PHASE, LANES };
-// Whether two matrices of bfloat16 lie alike: the same place within 16 bytes in every row (no matrix lies like any other)
+// Whether two matrices of bfloat16 lie alike: the same place within 16 bytes in every row (one that is not there lies like any other)
 bool alike(const void* p, int64_t ldp, const void* q, int64_t ldq, int64_t T) { return !q || ((((uintptr_t)p ^ (uintptr_t)q) & 15) == 0 && (T == 1 || (ldp - ldq) % 8 == 0)); }
 // How a row's units are shared: `vpt` per thread, `threads` per row (whole warps), `rows` side by side per CTA, `stages` rows of a ring.
 struct NormPlan { int vpt, threads, rows, stages; bool wide; int64_t ctas; size_t smem; };
@@ -213,8 +213,9 @@ psgd_status psgd_norm_backward(const void* dy, int64_t lddy, int dy_dtype, const
     if (overlap(out, stretch(dy, T, F, lddy, size_of(dy_dtype))) || overlap(out, stretch(x, T, F, ldx, size)) || overlap(out, stretch(add, T, F, ldadd, size))) return PSGD_E_INVALID;
     const bool whole = whole_units(dy, lddy, F, dy_dtype) && whole_units(x, ldx, F, x_dtype) && whole_units(add, ldadd, F, x_dtype) && whole_units(dx, lddx, F, x_dtype);
     const bool same = x_dtype == PSGD_DT_BF16 && alike(x, ldx, dy, lddy, T) && alike(x, ldx, add, ldadd, T) && alike(x, ldx, dx, lddx, T);
-    // (16384 rows with two operands to read: 1801 columns 70 us by lanes, 75 by units; 2051: 113, 74; 4099: 591, 156)
-    const NormRows rows = whole ? RING : same && F >= 2048 ? PHASE : LANES;
+    // (16384 rows with a residual: 1801 columns 70 us by lanes, 75 by units; 2051: 113, 74; 4099, more than a CTA has lanes for: 591, 156.
+    // 2051 columns of 512 rows: 8.1, 10.2; of 2048: 18.0, 16.3)
+    const NormRows rows = whole ? RING : same && (F > 8 * NORM_THREADS || (F >= 2048 && T >= 2048)) ? PHASE : LANES;
     const NormGrad g = plan_norm_grad(T, F, rows, F * (size_of(dy_dtype) + size * (add ? 2 : 1)));
     if (ws_bytes < g.total) return PSGD_E_WORKSPACE;
     NormBackward a{};

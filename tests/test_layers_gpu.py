@@ -565,7 +565,7 @@ def test_norm_many_rows_of_odd_widths(torch, ops, T, F):
     check_backward(torch, ops, fwd, w, dy, None, False, False)
 
 
-@pytest.mark.parametrize("T,F", [(1, 5), (9, 3), (1, 771), (20, 771), (1, 2051), (9, 2051), (30, 2056), (13, 4099)])
+@pytest.mark.parametrize("T,F", [(1, 5), (9, 3), (1, 771), (20, 771), (1, 2051), (9, 2051), (30, 2056), (13, 4099), (2060, 2051)])
 def test_norm_operands_that_begin_alike(torch, ops, T, F):
     """C entry points, all operands at one place within 16 bytes: the same values as those of aligned copies, and nothing else read or written."""
     from paper_2509_11254_b200 import binding
