@@ -446,7 +446,7 @@ psgd_status psgd_norm_backward(const void* dy /*DEVICE*/, int64_t lddy, int dy_d
  *     (u, v) -> scale (u cos a - v sin a, u sin a + v cos a);      backward != 0: the gradient's way, by -a.
  * The other values are copied.  Strides of tokens and heads in elements, any for the inputs (values used several times included); no two values of an output
  * may share a place.  positions [T] (any int64), frequencies [rotated/2] float64 radians per position; angles are exact modulo a turn up to the rounding of
- * the frequencies.  An output may be its own input (same address and strides); any other overlap is refused.  rotated <= 4096, heads * head <= 2^30.
+ * the frequencies, and a pair whose frequency is NaN or infinite is NaN.  An output may be its own input (same address and strides); any other overlap is refused.  rotated <= 4096, heads * head <= 2^30.
  */
 #define PSGD_ROTARY_HALF 0
 #define PSGD_ROTARY_INTERLEAVED 1

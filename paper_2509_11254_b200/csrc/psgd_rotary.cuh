@@ -35,11 +35,11 @@ struct RotaryArgs {
     float scale, sign;
 };
 
-// the angle position * frequency in turns, within -1/2..1/2
+// the angle position * frequency in turns, within -1/2..1/2; NaN where the frequency is not finite (as an integer that would be some angle)
 __device__ __forceinline__ float turns_of(long long position, double frequency) {
     const double t = frequency * 0.15915494309189533577;                     // 1 / 2 pi
     const unsigned long long step = (unsigned long long)__double2ll_rn((t - rint(t)) * 18446744073709551616.0);
-    return (float)(int)((step * (unsigned long long)position) >> 32) * 2.3283064365386963e-10f;          // 2^-32
+    return (float)(int)((step * (unsigned long long)position) >> 32) * 2.3283064365386963e-10f + (float)(t - t);          // 2^-32
 }
 
 // V values side by side: 2 to 32 bytes
