@@ -181,6 +181,7 @@ PyObject* rotary(PyObject*, PyObject* const* o, Py_ssize_t count) {
     if (e != PSGD_OK) return PyLong_FromLong(e);
     const auto given = [&](int i, const Tensor& t) -> PyObject* {
         if (!in_place) return wrap(t);
+        if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();      // whoever has saved it for its gradients has to know
         Py_INCREF(o[i]);
         return o[i];
     };

@@ -19,7 +19,7 @@ from collections import namedtuple
 import torch
 
 from .binding import PSGDError, lib
-from .training import _BF16, _BOTH, _DTYPES, ActivationCheckpoint, _check, _empty, _here, _matrix, _name, _no_graph, _plain, _there, _vector, _workspace_bytes
+from .training import _BF16, _BOTH, _DTYPES, ActivationCheckpoint, _check, _empty, _here, _matrix, _name, _no_graph, _plain, _there, _vector, _workspace_bytes, _written
 
 LayerNorm = namedtuple("LayerNorm", "y x mean rstd kept")
 LayerNormGrad = namedtuple("LayerNormGrad", "d_x d_weight d_bias")
@@ -195,6 +195,8 @@ def _rotary(backward, q, k, positions, frequencies, layout, scale, in_place, str
     none = k is None or K == 0
     _check(lib().psgd_rotary(q.data_ptr(), qt, qh, H, oq.data_ptr(), oqt, oqh, None if none else k.data_ptr(), kt, kh, K, None if none else ok.data_ptr(), okt, okh,
                              at_positions, at_frequencies, T, D, R, _LAYOUTS[layout], int(backward), scale, _DTYPES[q.dtype], at))
+    if in_place:
+        _written(q, k)
     return oq, ok
 
 
@@ -204,7 +206,8 @@ def rotary_forward(q, k, positions, frequencies, layout="half", scale=1.0, in_pl
     bfloat16 or float32 with unit stride within a head; tokens and heads may have any strides (parts of one projection's result, tokens or heads first).  positions [T]
     int64; frequencies [R/2] float64 radians per position (rotary_frequencies), R <= head: the values behind the first R pass through.  layout "half": pairs
     (i, i + R/2); "interleaved": (2i, 2i + 1).  `scale` multiplies what is turned.  Angles are formed in 64 bits, so that far positions keep theirs.
-    in_place: q and k themselves are overwritten, else the results are new tensors without gaps, tokens and heads in the order in which the inputs have them.
+    in_place: q and k themselves are overwritten (which autograd is told of, as by any operator that works in place), else the results are new tensors without gaps,
+    tokens and heads in the order in which the inputs have them.
     """
     return _rotary(False, q, k, positions, frequencies, layout, scale, in_place, stream)
 

@@ -136,6 +136,11 @@ def _no_graph(name, inputs, instead, depth):
                 return
 
 
+def _written(*tensors):
+    """Tells autograd that a call has written into tensors of the caller's: whoever has saved one for its gradients then raises instead of using what it has become."""
+    torch.autograd.graph.increment_version([t for t in tensors if t is not None])
+
+
 # the handle of the current stream and the current device without the objects around them, where torch has it so
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device

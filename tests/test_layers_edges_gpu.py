@@ -59,3 +59,38 @@ def test_rotary_frequencies_that_are_not_finite(torch, ops, layout, dtype, R):
                 assert bool(torch.isnan(x[..., bad]).all()) and torch.equal(x[..., ~bad], y[..., ~bad])
 
 
+@pytest.mark.parametrize("other_stream", [False, True])
+def test_rotary_in_place_is_seen_by_autograd(torch, ops, other_stream):
+    """What another operator has saved for its gradients and is turned in place raises there, as behind any operator that works in place; calls that write nothing into their
+    inputs, or that are refused, leave them as they are."""
+    g = gen(torch, 1)
+    side = torch.cuda.Stream() if other_stream else None
+    positions, f = torch.arange(5, device="cuda"), ops.rotary_frequencies(16)
+    for call in (ops.rotary_forward, ops.rotary_backward):
+        for which in (0, 1):
+            both = [torch.randn(5, heads, 24, generator=g, device="cuda") for heads in (4, 2)]
+            leaf = torch.randn_like(both[which]).requires_grad_()
+            y = (leaf * both[which]).sum()
+            before = [t._version for t in both]
+            call(*both, positions, f, stream=side)
+            assert [t._version for t in both] == before
+            call(*both, positions, f, in_place=True, stream=side)
+            assert all(t._version > v for t, v in zip(both, before))
+            torch.cuda.synchronize()
+            with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+                y.backward()
+    packed = torch.randn(5, 6, 24, generator=g, device="cuda")
+    before = packed._version
+    ops.rotary_forward(packed[:, :4], packed[:, 4:], positions, f, in_place=True, stream=side)
+    assert packed._version > before                    # (a view's base)
+    before = packed._version
+    with pytest.raises(ops.PSGDError):
+        ops.rotary_forward(packed[:, :4], packed[:, 3:], positions, f, in_place=True, stream=side)
+    assert packed._version == before
+    with torch.inference_mode():
+        x = torch.randn(5, 4, 24, generator=g, device="cuda")
+    want = ops.rotary_forward(x, None, positions, f)[0]
+    assert torch.equal(ops.rotary_forward(x, None, positions, f, in_place=True, stream=side)[0].clone(), want)      # (has no version)
+    torch.cuda.synchronize()
+
+
