@@ -14,6 +14,7 @@ that ran out should have produced is NaN, with or without `status`.
 
 None of these calls takes part in autograd: gradients are results of their own (d_hidden, d_weight, swiglu_backward, weight_gradient), and what a call returns has no
 graph behind it.  linear_cross_entropy, linear_distillation and swiglu_forward, whose results could be taken for differentiable ones, warn where an input requires a gradient.
+Tensors of the caller's that a call writes results into (`out`, `d_hidden`, `d_weight`) count for autograd as changed in place.
 """
 from __future__ import annotations
 
@@ -137,8 +138,11 @@ def _no_graph(name, inputs, instead, depth):
 
 
 def _written(*tensors):
-    """Tells autograd that a call has written into tensors of the caller's: whoever has saved one for its gradients then raises instead of using what it has become."""
-    torch.autograd.graph.increment_version([t for t in tensors if t is not None])
+    """Tells autograd that a call has written into tensors of the caller's (None: none): whoever has saved one for its gradients then raises instead of using what it
+    has become."""
+    tensors = [t for t in tensors if t is not None]
+    if tensors:
+        torch.autograd.graph.increment_version(tensors)
 
 
 # the handle of the current stream and the current device without the objects around them, where torch has it so
@@ -223,6 +227,7 @@ def _last_layer(grad, hidden, weight, target, token_weight, d_hidden, d_weight, 
     out = _empty(2 * T + 1, dtype=torch.float32, device=dev)
     at = out.data_ptr()                             # token_loss, lse, loss side by side
     args = hidden.data_ptr(), ldh, weight.data_ptr(), ldw, *at_target, at_weight, *(() if teacher else (ignore_index,)), T, V, D, at + 8 * T, at, at + 4 * T
+    given = d_hidden, d_weight
     if grad:
         if d_hidden is None:
             d_hidden = _empty((T, D), dtype=_BF16, device=dev)
@@ -230,6 +235,7 @@ def _last_layer(grad, hidden, weight, target, token_weight, d_hidden, d_weight, 
             d_weight = _empty((V, D), dtype=_BF16, device=dev)
         args += d_hidden.data_ptr(), lddh, d_weight.data_ptr(), lddw
     _check(getattr(lib(), call + ("grad" if grad else "loss"))(*args, at_status, ws.data_ptr(), nbytes, s))
+    _written(*given)
     token_loss, lse, loss = out.split_with_sizes((T, T, 1))
     loss = loss.view(())
     if grad:
@@ -317,9 +323,11 @@ class ActivationCheckpoint:
         if s is None:
             with _there(self.device, stream, self._buf, out):
                 return self.unpack(dtype, out)
+        given = out
         if out is None:
             out = _empty((T, F), dtype=dtype, device=self.device)
         _check(lib().psgd_act_unpack(self._q, self._s, T, F, out.data_ptr(), ld, _DTYPES[out.dtype], s))
+        _written(given)
         return out
 
 
@@ -365,9 +373,11 @@ def weight_gradient(dy, kept, dtype=torch.float32, out=None, status=None, stream
     nbytes = _workspace_bytes("psgd_act_wgrad_workspace", T, O, F, dev.index)
     dy, ldy = _operand(dy, T, O, ldy, s, out)
     ws = _empty(nbytes, dtype=torch.uint8, device=dev)
+    given = out
     if out is None:
         out = _empty((O, F), dtype=dtype, device=dev)
     _check(lib().psgd_act_wgrad(dy.data_ptr(), ldy, kept._q, kept._s, T, O, F, out.data_ptr(), ldo, _DTYPES[out.dtype], at_status, ws.data_ptr(), nbytes, s))
+    _written(given)
     return out
 
 

@@ -94,3 +94,32 @@ def test_rotary_in_place_is_seen_by_autograd(torch, ops, other_stream):
     torch.cuda.synchronize()
 
 
+def test_results_in_the_callers_tensors_are_seen_by_autograd(torch, ops):
+    """`out`, `d_hidden` and `d_weight` are tensors of the caller's: what has saved them for its gradients has to know."""
+    T, D, V, K = 40, 64, 90, 5
+    g = gen(torch, 2)
+    h, w = torch.randn(T, D, generator=g, device="cuda").bfloat16(), torch.randn(V, D, generator=g, device="cuda").bfloat16()
+    z, index = torch.randn(T, K, generator=g, device="cuda"), torch.randint(V, (T, K), generator=g, device="cuda")
+    kept = ops.pack_activation(h)
+    G = torch.zeros(2, V, D, device="cuda", dtype=torch.bfloat16)      # a stack, of which a slot is written
+    for side in (None, torch.cuda.Stream()):
+        for shape, write in (((T, D), lambda t: ops.linear_distillation_grad(h, w, z, index, d_hidden=t, stream=side)), ((V, D), lambda t: ops.linear_distillation_grad(h, w, z, index, d_weight=t, stream=side)),
+                             ((T, D), lambda t: ops.linear_cross_entropy_grad(h, w, index[:, 0].contiguous(), d_hidden=t, stream=side)),
+                             ((V, D), lambda t: ops.linear_cross_entropy_grad(h, w, index[:, 0].contiguous(), d_weight=t, stream=side)),
+                             ((D, D), lambda t: ops.weight_gradient(h, kept, out=t, stream=side)), ((T, D), lambda t: kept.unpack(out=t, stream=side))):
+            torch.cuda.synchronize()
+            t = torch.zeros(shape, device="cuda", dtype=torch.bfloat16)
+            y = (torch.ones_like(t).requires_grad_() * t).sum()
+            write(t)
+            torch.cuda.synchronize()
+            with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+                y.backward()
+        before = G._version
+        ops.linear_distillation_grad(h, w, z, index, d_weight=G[1], stream=side)
+        assert G._version > before
+        with torch.inference_mode():
+            t = torch.zeros(T, D, device="cuda", dtype=torch.bfloat16)
+        kept.unpack(out=t, stream=side)                # (has no version)
+    torch.cuda.synchronize()
+
+
