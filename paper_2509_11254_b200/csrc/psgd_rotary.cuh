@@ -4,8 +4,8 @@
 //
 // Pairs are (i, i + R/2) ("half") or (2i, 2i + 1) ("interleaved"); values R.. of a head pass through.  Angles of far positions need more than float32
 // (position 2^20 at frequency 1: half an ulp is 0.03), so they are kept as turns in 64-bit fixed point: frequency / 2 pi as a fraction of 2^64, from float64, times
-// the position modulo 2^64, is the angle modulo a turn without a rounding of its own; its upper 32 bits as float32 are within 2^-25 of a turn.  A token's sines and
-// cosines are formed once per CTA, in shared memory, for all heads.
+// the position modulo 2^64, is the angle modulo a turn without a rounding of its own; its distance from the nearest quarter of a turn as float32 is within 2^-28 of a
+// turn, below the rounding of the sine itself.  A token's sines and cosines are formed once per CTA, in shared memory, for all heads.
 //
 // Bound by HBM: every value read once and written once.  A thread moves V values at a time, 16 bytes of bfloat16 where widths and addresses allow (half: V of the first half and
 // the V that belong to them), of the same place in ROT_HEADS heads, whose loads are under way together and which share the sines and cosines that it reads.
@@ -35,11 +35,16 @@ struct RotaryArgs {
     float scale, sign;
 };
 
-// the angle position * frequency in turns, within -1/2..1/2; NaN where the frequency is not finite (as an integer that would be some angle)
-__device__ __forceinline__ float turns_of(long long position, double frequency) {
+// Cosine and sine of position * frequency; NaN where the frequency is not finite (as an integer that would be some angle).  The angle's upper two bits, rounded, are whole quarters
+// of a turn; what is left, at most an eighth, keeps 24 bits of its own in float32.
+__device__ __forceinline__ float2 turn_of(long long position, double frequency) {
     const double t = frequency * 0.15915494309189533577;                     // 1 / 2 pi
     const unsigned long long step = (unsigned long long)__double2ll_rn((t - rint(t)) * 18446744073709551616.0);
-    return (float)(int)((step * (unsigned long long)position) >> 32) * 2.3283064365386963e-10f + (float)(t - t);          // 2^-32
+    const unsigned long long angle = step * (unsigned long long)position, quarters = (angle + (1ull << 61)) >> 62;
+    float s, c;
+    sincospif((float)(long long)(angle - (quarters << 62)) * 1.0842021724855044e-19f + (float)(t - t), &s, &c);      // 2^-63: half turns
+    if (quarters & 1) { const float u = c; c = -s; s = u; }
+    return quarters & 2 ? make_float2(-c, -s) : make_float2(c, s);
 }
 
 // V values side by side: 2 to 32 bytes
@@ -84,10 +89,9 @@ __global__ void __launch_bounds__(ROT_THREADS) k_rotary(const __grid_constant__ 
         __syncthreads();
         for (int i = threadIdx.x; i < tokens * pairs; i += ROT_THREADS) {
             const int t = i / a.by_pairs, p = i - t * pairs;
-            float s, c;
-            sincospif(2.f * turns_of(a.positions[t0 + t], a.frequencies[p]), &s, &c);
+            const float2 cs = turn_of(a.positions[t0 + t], a.frequencies[p]);
             const int at = PAIRS == 1 ? p : ((p % PAIRS / 2) * places + p / PAIRS) * 2 + (p & 1);
-            turn[t * pairs + at] = make_float2(c * a.scale, s * a.scale * a.sign);
+            turn[t * pairs + at] = make_float2(cs.x * a.scale, cs.y * a.scale * a.sign);
         }
         __syncthreads();
         const int items = tokens * a.groups * a.per_head;

@@ -123,3 +123,36 @@ def test_results_in_the_callers_tensors_are_seen_by_autograd(torch, ops):
     torch.cuda.synchronize()
 
 
+def test_rotary_angles_carry_the_precision_of_float32(torch, ops):
+    """(1, 0) turned is (cos a, sin a), without a rounding of its own.  The angle's distance from the nearest quarter of a turn, at most 1/8, is held in float32: within 2^-28 of a
+    turn; beside it four roundings of position * frequency in float64 (the reference makes some of them), and one unit in the last place of the sine and the cosine (2^-24
+    where they are largest)."""
+    g = gen(torch, 3)
+    T, R = 4096, 64
+    positions = torch.randint(1 << 17, (T,), generator=g, device="cuda")
+    f = ops.rotary_frequencies(R)
+    x = torch.zeros(T, 1, R, device="cuda")
+    x[..., :R // 2] = 1
+    angle = positions.double()[:, None] * f
+    bound = 2 * math.pi * 2.0 ** -28 + 4 * angle.abs() * 2.0 ** -53 + 2.0 ** -24
+    for call, way in ((ops.rotary_forward, 1), (ops.rotary_backward, -1)):
+        got = call(x, None, positions, f)[0][:, 0]
+        within(got[:, :R // 2], torch.cos(angle), bound)
+        within(got[:, R // 2:], way * torch.sin(angle), bound)
+    # whole quarters, and the angles beside the places where the nearest quarter changes (1/8, 3/8, 5/8, 7/8 of a turn)
+    steps = torch.arange(-64, 65, device="cuda")
+    eighth = torch.tensor([2 * math.pi / 1024], dtype=torch.float64, device="cuda")
+    at = torch.cat([steps + 128 * i for i in range(-9, 10)])
+    x = torch.zeros(len(at), 1, 2, device="cuda")
+    x[..., 0] = 1
+    got = ops.rotary_forward(x, None, at, eighth)[0][:, 0]
+    turn = at.double() / 1024 * 2 * math.pi
+    bound = torch.full_like(turn, 2 * math.pi * 2.0 ** -28 + 2.0 ** -24) + 4 * turn.abs() * 2.0 ** -53
+    within(got[:, 0], torch.cos(turn), bound)
+    within(got[:, 1], torch.sin(turn), bound)
+    quarter = at % 256 == 0
+    assert int(quarter.sum()) >= 9
+    whole = torch.stack([torch.cos(turn), torch.sin(turn)], 1)[quarter].round().float()
+    assert bool(((got[quarter] - whole).abs() <= 2.0 ** -40).all())
+
+
