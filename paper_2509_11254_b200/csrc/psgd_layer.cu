@@ -80,8 +80,11 @@ struct NormGrad { NormPlan p; int64_t parts; size_t part, sums, total; };
 NormGrad plan_norm_grad(int64_t T, int64_t F, NormRows rows, int64_t row_bytes) {
     NormGrad g{};
     g.p = plan_norm(T, F, rows, row_bytes, false, false, true);
-    const int64_t tiles = (F + 2047) / 2048;
-    g.parts = g.p.wide ? std::min<int64_t>({T, 65535, std::max<int64_t>(1, device_sms() * 4 / tiles)}) : g.p.ctas;
+    // Wide rows: CTAs of 2048 columns that share the rows, four per multiprocessor; the wider the rows, the fewer for each stretch of columns, but never so few that a thread adds more
+    // than T / 128 + 49 of them into one float32 sum (one round of CTAs alone: 1000 of
+    // 4000 rows of 262144 columns); then several rounds of CTAs (1000 x 131072 bfloat16: 330 us with one, 356 with three).
+    const int64_t tiles = (F + 2047) / 2048, round = std::max<int64_t>(1, device_sms() * 4 / tiles), needed = ceil_div(T, T / 128 + 48);
+    g.parts = g.p.wide ? std::min<int64_t>(T, ceil_div(std::max(needed, round), round) * round) : g.p.ctas;
     g.part = 0;
     g.sums = align_up((size_t)g.parts * 2 * F * 4, 256);
     g.total = g.sums + (g.p.wide ? align_up((size_t)T * 8, 256) : 0);

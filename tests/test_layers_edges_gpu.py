@@ -156,3 +156,16 @@ def test_rotary_angles_carry_the_precision_of_float32(torch, ops):
     assert bool(((got[quarter] - whole).abs() <= 2.0 ** -40).all())
 
 
+# ---- layer norm ---------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("T,F,term", [(4000, 262144, 1.0041199), (8000, 131072, 1.2795105)])
+def test_norm_sums_over_many_wide_rows(torch, ops, T, F, term):
+    """Sums over rows pass every value through at most T / 128 + 65 additions however wide the rows are.  Equal terms are the worst of sums, since all additions of a stretch round
+    the same way; with these two, one running sum of a thread's rows (1000 and 889 of them) would be off by 2.6 and 1.7 times the bound."""
+    x, dy = torch.ones(T, F, device="cuda"), torch.full((T, F), term, device="cuda")
+    # without centring and with a rstd of 1, dy xh is dy
+    d = ops.layer_norm_backward(dy, x, torch.ones(F, device="cuda"), None, torch.ones(T, device="cuda"), bias=True)
+    want = torch.full((F,), T * float(dy[0, 0]), dtype=torch.float64, device="cuda")
+    for got in (d.d_bias, d.d_weight):
+        within(got, want, (T / 128 + 65) * U * want)
+
+
