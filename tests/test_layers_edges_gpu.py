@@ -157,6 +157,93 @@ def test_rotary_angles_carry_the_precision_of_float32(torch, ops):
 
 
 # ---- layer norm ---------------------------------------------------------------------------------------------------
+def check_norm(torch, ops, T, F, x_type, y_type=None, extra=False, center=True, bias=True, rows=500):
+    """Both directions against 64 bits, a few hundred rows at a time; a sum over F values passes each through at most 40 + F / 4096 additions, one over T rows through at
+    most T / 128 + 65."""
+    dtype, out_type = getattr(torch, x_type), getattr(torch, y_type or x_type)
+    g = gen(torch, T + F)
+
+    def normal(*shape):
+        return torch.randn(*shape, generator=g, device="cuda")
+
+    w, b = 1 + 0.3 * normal(F), 0.2 * normal(F) if bias else None
+    x, dy = (normal(T, F) + 0.3 * normal(F)).to(dtype), (1e-2 * normal(T, F)).to(out_type)
+    r, d_x = (normal(T, F).to(dtype), (1e-2 * normal(T, F)).to(dtype)) if extra else (None, None)
+    n = ops.layer_norm_forward(x, w, b, residual=r, center=center, keep=True, dtype=out_type)
+    d = ops.layer_norm_backward(dy, n.x, w, n.mean, n.rstd, d_x=d_x, bias=bias)
+    assert n.y.dtype == out_type and d.d_x.dtype == dtype
+    again = ops.pack_activation(n.y)
+    assert torch.equal(n.kept.q, again.q) and torch.equal(n.kept.scales, again.scales)
+    depth, wd, bd = 40 + F / 4096, w.double(), b.double() if bias else 0.0
+    dw, dw_size, db, db_size = (torch.zeros(F, dtype=torch.float64, device="cuda") for _ in range(4))
+    for a in range(0, T, rows):
+        p = slice(a, a + rows)
+        s = x[p] if r is None else (x[p].float() + r[p].float()).to(dtype)
+        assert torch.equal(n.x[p], s)
+        s = s.double()
+        mean = s.mean(1, keepdim=True) if center else torch.zeros_like(s[:, :1])
+        em = (depth + 1) * U * s.abs().mean(1, keepdim=True) if center else 0.0 * mean
+        v = s - mean
+        var = v.square().mean(1, keepdim=True) + 1e-5
+        rstd = var.rsqrt()
+        er = ((depth + 4) * U + em ** 2 / var + 4 * U) / 2 + 2.0 ** -22
+        if center:
+            within(n.mean[p, None], mean, em + U * mean.abs() + 1e-40)
+        within(n.rstd[p, None], rstd, er * rstd)
+        y = v * rstd * wd + bd
+        step = HALF_STEP[y_type or x_type]
+        within(n.y[p], y, (em * rstd + (er + 6 * U) * (v * rstd).abs()) * wd.abs() * (1 + 1e-3) * (1 + step) + (step + 2 * U) * y.abs() + 1e-38)
+        # the gradients of the statistics that the forward pass returned
+        f, m = n.rstd[p, None].double(), n.mean[p, None].double() if center else 0.0
+        xh, e = (s - m) * f, dy[p].double()
+        dw += (e * xh).sum(0)
+        dw_size += (e * xh).abs().sum(0)
+        db += e.sum(0)
+        db_size += e.abs().sum(0)
+        e = e * wd
+        c1, c2 = e.mean(1, keepdim=True) if center else 0.0, (e * xh).mean(1, keepdim=True)
+        e1, e2 = (depth + 3) * U * e.abs().mean(1, keepdim=True), (depth + 6) * U * (e * xh).abs().mean(1, keepdim=True)
+        dx = f * (e - c1 - xh * c2)
+        bound = f * (8 * U * (e.abs() + (xh * c2).abs() + abs(c1)) + e1 + xh.abs() * e2)
+        if d_x is not None:
+            dx = dx + d_x[p].double()
+            bound = bound + U * (dx.abs() + d_x[p].double().abs())
+        step = HALF_STEP[x_type]
+        within(d.d_x[p], dx, bound * (1 + step) + (step + 2 * U) * dx.abs() + 1e-38)
+    within(d.d_weight, dw, (T / 128 + 68) * U * dw_size + 1e-38)
+    if bias:
+        within(d.d_bias, db, (T / 128 + 65) * U * db_size + 1e-38)
+
+
+@pytest.mark.parametrize("T,F,x_type,y_type,extra", [(2000, 4099, "float32", None, True), (1500, 4099, "float32", "bfloat16", False), (700, 10001, "float32", None, False),
+                                                     (700, 10001, "float32", "bfloat16", True), (1300, 16640, "bfloat16", None, True), (700, 16391, "bfloat16", None, False), (700, 12800, "float32", None, True),
+                                                     (1200, 12288, "float32", "bfloat16", True), (650, 16640, "float32", None, False), (60, 131072, "bfloat16", None, True)])
+@pytest.mark.parametrize("center", [True, False])
+def test_norm_many_rows_beyond_registers(torch, ops, T, F, x_type, y_type, extra, center):
+    """More rows than CTAs where a CTA walks over its row several times: every one takes a second row and a third, and the columns' sums go over several."""
+    check_norm(torch, ops, T, F, x_type, y_type, extra, center, bias=center)
+
+
+@pytest.mark.parametrize("T,F,gap", [(1300, 5003, 3), (700, 4100, 2)])
+def test_norm_many_rows_beyond_registers_that_lie_unlike(torch, ops, T, F, gap):
+    """Bfloat16 rows whose operands lie at different places within 16 bytes: the same values as those of copies that lie alike, to one rounding of the result."""
+    g = gen(torch, F)
+    x, dy = (torch.randn(T, F + gap, generator=g, device="cuda").bfloat16()[:, 1:F + 1] for _ in range(2))
+    r = torch.randn(T, F, generator=g, device="cuda").bfloat16()
+    w, b = 1 + 0.3 * torch.randn(F, generator=g, device="cuda"), 0.2 * torch.randn(F, generator=g, device="cuda")
+    n, m = (ops.layer_norm_forward(t, w, b, residual=r, keep=True) for t in (x, x.contiguous()))
+    d, e = (ops.layer_norm_backward(t, n.x, w, n.mean, n.rstd, d_x=r, bias=True) for t in (dy, dy.contiguous()))
+    assert torch.equal(n.x, m.x)
+    for a, c in ((n.y, m.y), (d.d_x, e.d_x)):
+        within(a, c.double(), 2 * 2.0 ** -8 * c.double().abs() + 1e-5)
+    depth = 40 + F / 4096
+    within(n.mean, m.mean.double(), 2 * (depth + 2) * U * n.x.double().abs().mean(1))
+    within(n.rstd, m.rstd.double(), ((depth + 8) * U + 2.0 ** -21) * m.rstd.double())
+    xh = ((n.x.double() - n.mean.double()[:, None]) * n.rstd.double()[:, None] * dy.double()).abs().sum(0)
+    within(d.d_weight, e.d_weight.double(), 2 * (T / 128 + 68) * U * xh)
+    within(d.d_bias, e.d_bias.double(), 2 * (T / 128 + 65) * U * dy.double().abs().sum(0))
+
+
 @pytest.mark.parametrize("T,F,term", [(4000, 262144, 1.0041199), (8000, 131072, 1.2795105)])
 def test_norm_sums_over_many_wide_rows(torch, ops, T, F, term):
     """Sums over rows pass every value through at most T / 128 + 65 additions however wide the rows are.  Equal terms are the worst of sums, since all additions of a stretch round
