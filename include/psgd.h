@@ -369,7 +369,8 @@ psgd_status psgd_xent_grad(const void* H /*DEVICE*/, int64_t ldh, const void* W 
  *     token_loss_t = temperature^2 sum_k q_k (log q_k - log p_{t,index_k})   (0 for a row without an entry),   lse_t = log sum_v exp(l_tv / temperature),
  *     loss = sum_t weight_t token_loss_t / Z,  Z = sum of weight_t over the rows that have an entry (loss 0 where Z = 0),
  * dH and dW the gradients of loss.  A column outside 0..V-1 makes its row's loss NaN, its gradients 0, and sets PSGD_W_LABEL.  temperature within 10^-3..10^3.  Everything else
- * as for psgd_xent_*; the workspace has 8 bytes per row more, and for the rows of a piece 16 bytes per entry and 4 per 32 rows and 32 columns.
+ * as for psgd_xent_*; the workspace has 8 bytes per row more, and for the rows of a piece 16 bytes per entry (1 GiB at most) and 4 per 32
+ * rows and 32 columns.
  */
 psgd_status psgd_distill_workspace(int64_t T, int64_t V, int64_t D, int64_t K, int grad, size_t* bytes /*HOST*/);
 psgd_status psgd_distill_loss(const void* H /*DEVICE*/, int64_t ldh, const void* W /*DEVICE*/, int64_t ldw, const void* logits /*DEVICE*/, int64_t ldl, int dtype,

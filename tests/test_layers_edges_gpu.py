@@ -256,3 +256,16 @@ def test_norm_sums_over_many_wide_rows(torch, ops, T, F, term):
         within(got, want, (T / 128 + 65) * U * want)
 
 
+# ---- distillation -------------------------------------------------------------------------------------------------
+def test_distillation_of_long_lists_over_many_tokens(torch, ops):
+    """More entries than the workspace holds at a time, with and without gradients, over a vocabulary of less than one tile."""
+    from test_distillation_gpu import check
+
+    T, V, D, K = 70003, 100, 16, 1024
+    g = gen(torch, 4)
+    h, w = torch.randn(T, D, generator=g, device="cuda").bfloat16(), (0.3 * torch.randn(V, D, generator=g, device="cuda")).bfloat16()
+    z, index = torch.randn(T, K, generator=g, device="cuda").bfloat16(), torch.randint(-3, V, (T, K), generator=g, device="cuda")
+    index[::5] = -1
+    check(torch, ops, h, w, z, index, 2.0, torch.rand(T, generator=g, device="cuda"))
+
+
