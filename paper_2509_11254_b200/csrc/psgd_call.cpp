@@ -167,7 +167,7 @@ PyObject* rotary(PyObject*, PyObject* const* o, Py_ssize_t count) {
     if (!here.takes(*q, !backward) || !heads(*q, nullptr) || (k && (!here.takes(*k, !backward) || !heads(*k, q)))) return none();
     const int64_t T = q->size(0), D = q->size(2), H = q->size(1), K = k ? k->size(1) : 0;
     if (T < 1 || H < 1 || (k && K < 1) || f->dim() != 1 || f->size(0) < 1 || 2 * f->size(0) > D) return none();
-    if (!vector(*at, T, at::kLong, here.device) || !vector(*f, f->size(0), at::kDouble, here.device)) return none();
+    if (!vector(*at, T, at::kLong, here.device) || !vector(*f, f->size(0), at::kDouble, here.device) || (!backward && here.grad && f->requires_grad())) return none();
     Tensor oq, ok;
     psgd_status e;
     {
@@ -203,12 +203,12 @@ PyObject* distill(PyObject*, PyObject* const* o, Py_ssize_t count) {
     const Here here;
     const bool grad = o[0] == Py_True;
     const double tau = PyFloat_AS_DOUBLE(o[5]);
-    if (!here.takes(*h, !grad) || !here.takes(*w, !grad) || !here.takes(*z, false) || h->dim() != 2 || w->dim() != 2 || z->dim() != 2 || index->dim() != 2) return none();
+    if (!here.takes(*h, !grad) || !here.takes(*w, !grad) || !here.takes(*z, !grad) || h->dim() != 2 || w->dim() != 2 || z->dim() != 2 || index->dim() != 2) return none();
     const int64_t T = h->size(0), D = h->size(1), V = w->size(0), K = z->size(1);
     int64_t ldh, ldw, ldl, ldi;
     if (T < 1 || D < 1 || V < 1 || K < 1 || K > 1024 || !(tau >= 1e-3 && tau <= 1e3) || !operand(*h, T, D, ldh) || !operand(*w, V, D, ldw)) return none();
     if (!matrix(*z, T, K, ldl) || !index->is_cuda() || index->get_device() != here.device || index->scalar_type() != at::kLong || !matrix(*index, T, K, ldi)) return none();
-    if (weight && !vector(*weight, T, at::kFloat, here.device)) return none();
+    if (weight && (!here.takes(*weight, !grad) || !vector(*weight, T, at::kFloat, here.device))) return none();
     Tensor loss, token_loss, lse, dh, dw, ws;
     psgd_status e;
     {

@@ -182,7 +182,7 @@ def _rotary(backward, q, k, positions, frequencies, layout, scale, in_place, str
     R = 2 * frequencies.numel()
     at_frequencies = _vector(frequencies, "frequencies", torch.float64, R // 2, dev)
     if not backward:
-        _no_graph("rotary_forward", (q, k), "rotary_backward makes the gradients", 4)
+        _no_graph("rotary_forward", (q, k, frequencies), "rotary_backward makes the gradients", 4)
     at = _here(dev, stream)
     if at is None:
         with _there(dev, stream, q, k, positions, frequencies), torch.no_grad():

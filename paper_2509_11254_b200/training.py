@@ -214,7 +214,7 @@ def _last_layer(grad, hidden, weight, target, token_weight, d_hidden, d_weight, 
     at_status = _status(status, dev)
     name = "linear_distillation" if teacher else "linear_cross_entropy"
     if not grad:
-        _no_graph(name, (hidden, weight), f"{name}_grad returns the gradients", 4)
+        _no_graph(name, (hidden, weight, token_weight, *inputs), f"{name}_grad returns the gradients of hidden and weight", 4)
     s = _here(dev, stream)
     if s is None:
         with _there(dev, stream, hidden, weight, *inputs, token_weight, d_hidden, d_weight, status), torch.no_grad():

@@ -269,3 +269,30 @@ def test_distillation_of_long_lists_over_many_tokens(torch, ops):
     check(torch, ops, h, w, z, index, 2.0, torch.rand(T, generator=g, device="cuda"))
 
 
+def test_calls_warn_about_every_gradient_that_is_lost(torch, ops):
+    """Not only the student's: a teacher whose logits are part of a graph, weights of the tokens, frequencies that are learned."""
+    import warnings
+
+    g = gen(torch, 5)
+    h, w = torch.randn(8, 64, generator=g, device="cuda").bfloat16(), torch.randn(90, 64, generator=g, device="cuda").bfloat16()
+    z, index = torch.randn(8, 5, generator=g, device="cuda"), torch.randint(90, (8, 5), generator=g, device="cuda")
+    tw, labels = torch.rand(8, generator=g, device="cuda"), index[:, 0].contiguous()
+    q, at, f = torch.randn(8, 2, 16, generator=g, device="cuda"), torch.arange(8, device="cuda"), ops.rotary_frequencies(16)
+    live = lambda t: t.clone().requires_grad_()  # noqa: E731
+    side = torch.cuda.Stream()
+    calls = [(ops.linear_distillation, (h, w, live(z), index), {}), (ops.linear_distillation, (h, w, z, index), {"token_weight": live(tw)}),
+             (ops.linear_cross_entropy, (h, w, labels), {"token_weight": live(tw)}), (ops.rotary_forward, (q, None, at, live(f)), {})]
+    for call, args, kw in calls:
+        want = None
+        for stream in (None, side):
+            torch.cuda.synchronize()
+            with pytest.warns(UserWarning, match=f"{call.__name__}: the results have no autograd graph") as seen:
+                got = call(*args, **kw, stream=stream)
+            assert len(seen) == 1 and seen[0].filename == __file__
+            torch.cuda.synchronize()
+            with warnings.catch_warnings():
+                warnings.simplefilter("error")
+                with torch.no_grad():
+                    want = call(*args, **kw, stream=stream)
+            torch.cuda.synchronize()
+            assert all(a is b or torch.equal(a, b) for a, b in zip(got, want))
