@@ -330,8 +330,8 @@ psgd_status psgd_backproject_static(const float* M /*DEVICE*/, const float* P_ha
  * be NULL) collects PSGD_W_* bits and is never cleared by the library.  Results that depend on a wait which ran out (PSGD_W_TIMEOUT) are NaN,
  * with or without a status word.  `workspace` (DEVICE, 256-byte aligned) holds at least
  * the bytes the matching query reports, may hold anything before the call, and is free again for later work on the stream.
- * No output may overlap an input or another output (columns of one wider matrix may lie side by side): dH and dW with H, W and each other (a
- * distillation's also with its logits and index) and psgd_act_wgrad's dW with dY are checked (PSGD_E_INVALID).
+ * No output may overlap an input or another output (columns of one wider matrix may lie side by side): dH and dW with H, W, labels, weight and each
+ * other (a distillation's also with its logits and index) and psgd_act_wgrad's dW with dY are checked (PSGD_E_INVALID).
  * Sizes are at most 2^30 per dimension and 2^45 for a product of two; T = 0 is allowed (loss 0, weight gradients 0).
  */
 #define PSGD_DT_F32 0
@@ -430,7 +430,7 @@ psgd_status psgd_swiglu_backward(const void* dh /*DEVICE*/, int64_t lddh, const 
  * The gradients from dy [T][F] (types as y's), x = the s of the forward pass, and its mean (NULL: without centring) and rstd:
  *     dx = f (g - mean(g) [with centring] - xh mean(g xh)) + add,  g = dy w,  xh = (x - m) f,   dw = sum_t dy xh,  db = sum_t dy.
  * add [T][F] (x_dtype, may be NULL) is what reaches x from elsewhere, dx (x_dtype) the gradient of both x and r.  dw, db (may be NULL): [F] float32, summed
- * in a fixed order.  Rows of any stride and alignment; outputs over inputs or over each other are refused.
+ * in a fixed order.  Rows of any stride and alignment; outputs (the backward pass's workspace among them) over inputs or over each other are refused.
  */
 psgd_status psgd_norm_forward(const void* x /*DEVICE*/, int64_t ldx, int x_dtype, const void* r /*DEVICE*/, int64_t ldr, const void* w /*DEVICE*/, const void* b /*DEVICE*/,
                               int w_dtype, float eps, int center, int64_t T, int64_t F, void* s /*DEVICE*/, int64_t lds, void* y /*DEVICE*/, int64_t ldy, int y_dtype,
@@ -447,7 +447,8 @@ psgd_status psgd_norm_backward(const void* dy /*DEVICE*/, int64_t lddy, int dy_d
  *     (u, v) -> scale (u cos a - v sin a, u sin a + v cos a);      backward != 0: the gradient's way, by -a.
  * The other values are copied.  Strides of tokens and heads in elements, any for the inputs (values used several times included); no two values of an output
  * may share a place.  positions [T] (any int64), frequencies [rotated/2] float64 radians per position; angles are exact modulo a turn up to the rounding of
- * the frequencies, and a pair whose frequency is NaN or infinite is NaN.  An output may be its own input (same address and strides); any other overlap is refused.  rotated <= 4096, heads * head <= 2^30.
+ * the frequencies, and a pair whose frequency is NaN or infinite is NaN.  An output may be its own input (same address and strides); any other overlap, with
+ * positions and frequencies too, is refused.  rotated <= 4096, heads * head <= 2^30.
  */
 #define PSGD_ROTARY_HALF 0
 #define PSGD_ROTARY_INTERLEAVED 1

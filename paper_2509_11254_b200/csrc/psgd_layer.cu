@@ -170,9 +170,12 @@ psgd_status psgd_norm_forward(const void* x, int64_t ldx, int x_dtype, const voi
     if (T == 0) return PSGD_OK;
     if (!x || !w || !y || !rstd || (r && !s) || (center && !mean) || (q && !scales)) return PSGD_E_NULL;
     if (ldx < F || ldy < F || (r && ldr < F) || (s && lds < F) || ((uintptr_t)q & 15)) return PSGD_E_INVALID;
-    const Stretch in[2] = {stretch(x, T, F, ldx, size_of(x_dtype)), stretch(r, T, F, ldr, size_of(x_dtype))};
-    const Stretch sum = stretch(s, T, F, lds, size_of(x_dtype)), out = stretch(y, T, F, ldy, size_of(y_dtype));
-    if (overlap(in[0], sum) || overlap(in[0], out) || overlap(in[1], sum) || overlap(in[1], out) || overlap(sum, out)) return PSGD_E_INVALID;
+    const int size = size_of(x_dtype);
+    const int64_t params = F * size_of(w_dtype), groups = T * ((F + ACT_GROUP - 1) / ACT_GROUP);
+    if (outputs_meet({stretch(s, T, F, lds, size), stretch(y, T, F, ldy, size_of(y_dtype)), stretch(center ? mean : nullptr, T * 4), stretch(rstd, T * 4), stretch(q, groups * ACT_GROUP),
+                      stretch(q ? scales : nullptr, groups)},
+                     {stretch(x, T, F, ldx, size), stretch(r, T, F, ldr, size), stretch(w, params), stretch(b, params)}))
+        return PSGD_E_INVALID;
     const bool whole = whole_units(x, ldx, F, x_dtype) && whole_units(r, ldr, F, x_dtype) && whole_units(s, lds, F, x_dtype) && whole_units(y, ldy, F, y_dtype);
     const bool same = x_dtype == PSGD_DT_BF16 && alike(x, ldx, r, ldr, T) && alike(x, ldx, s, lds, T) && alike(x, ldx, y, ldy, T);
     const NormRows rows = whole ? RING : same ? PHASE : LANES;
@@ -221,6 +224,10 @@ psgd_status psgd_norm_backward(const void* dy, int64_t lddy, int dy_dtype, const
     const NormRows rows = whole ? RING : same && (F > 8 * NORM_THREADS || (F >= 2048 && T >= 2048)) ? PHASE : LANES;
     const NormGrad g = plan_norm_grad(T, F, rows, F * (size_of(dy_dtype) + size * (add ? 2 : 1)));
     if (ws_bytes < g.total) return PSGD_E_WORKSPACE;
+    if (outputs_meet({out, stretch(dw, F * 4), stretch(db, F * 4), stretch(ws, (int64_t)g.total)},
+                     {stretch(dy, T, F, lddy, size_of(dy_dtype)), stretch(x, T, F, ldx, size), stretch(add, T, F, ldadd, size), stretch(w, F * size_of(w_dtype)), stretch(mean, T * 4),
+                      stretch(rstd, T * 4)}))
+        return PSGD_E_INVALID;
     NormBackward a{};
     a.T = T; a.F = (int)F; a.center = mean != nullptr;
     a.dy = dy; a.x = x; a.add = add; a.dx = dx;
@@ -277,6 +284,9 @@ psgd_status psgd_rotary(const void* q, int64_t q_token, int64_t q_head, int64_t 
             if (count[i] && count[j] && !same && overlap(out[i], in[j])) return PSGD_E_INVALID;
         }
     if (heads_q && heads_k && overlap(out[0], out[1])) return PSGD_E_INVALID;
+    const Stretch angles[2] = {stretch(positions, T * 8), stretch(frequencies, rotated / 2 * 8)};
+    for (const Stretch& o : out)
+        if (overlap(o, angles[0]) || overlap(o, angles[1])) return PSGD_E_INVALID;
     int V = 8;
     while (V > 1 && all % V) V /= 2;
     RotaryArgs a{};

@@ -280,6 +280,10 @@ psgd_status xent(const void* H, int64_t ldh, const void* W, int64_t ldw, const i
     }
     const XentPlan x = plan_xent(T, V, D, grad, teacher ? teacher->K : 0);
     if (ws_bytes < x.total) return PSGD_E_WORKSPACE;
+    if (grad) {                                       // read for later pieces after the first one's gradients are written, too
+        const Stretch dh = stretch(dH, T, D, lddh, 2), dw = stretch(dW, V, D, lddw, 2), each = stretch(weight, T * 4), of = stretch(labels, T * 8);
+        if (overlap(dh, each) || overlap(dw, each) || overlap(dh, of) || overlap(dw, of)) return PSGD_E_INVALID;
+    }
     char* w = (char*)ws;
     int* stat = status ? status : (int*)w;
     float* inv = (float*)(w + x.inv);

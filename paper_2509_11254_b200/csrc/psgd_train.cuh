@@ -3,6 +3,7 @@
 #include "../../include/psgd.h"
 
 #include <algorithm>
+#include <initializer_list>
 
 #include "psgd_host.cuh"
 
@@ -55,5 +56,20 @@ inline bool overlap(const Stretch& a, const Stretch& b) {
     return a.step == b.step && meets(a.rows - 1);
 }
 inline Stretch stretch(const void* p, int64_t rows, int64_t cols, int64_t ld, int bytes) { return {p, rows, cols * bytes, (rows == 1 ? cols : ld) * bytes}; }
+inline Stretch stretch(const void* p, int64_t bytes) { return {p, 1, bytes, bytes}; }
+// Whether an output lies over an input or over another output (nullptr: not there).
+inline bool outputs_meet(std::initializer_list<Stretch> out, std::initializer_list<Stretch> in) {
+    const auto end = [](const Stretch& s) { return (uintptr_t)s.p + (uintptr_t)((s.rows - 1) * s.step + s.width); };
+    for (const Stretch* o = out.begin(); o != out.end(); ++o) {
+        if (!o->p) continue;
+        const uintptr_t from = (uintptr_t)o->p, to = end(*o);
+        const auto meets = [&](const Stretch& s) { return from < end(s) && (uintptr_t)s.p < to && overlap(*o, s); };     // (mostly far apart)
+        for (const Stretch& i : in)
+            if (meets(i)) return true;
+        for (const Stretch* p = out.begin(); p != o; ++p)
+            if (meets(*p)) return true;
+    }
+    return false;
+}
 
 }  // namespace psgd

@@ -257,7 +257,7 @@ def linear_cross_entropy_grad(hidden, weight, labels, token_weight=None, ignore_
     """The same with the gradients of the loss: returns (loss, token_loss, lse, d_hidden [T, D], d_weight [V, D]), the gradients bfloat16.
 
     d_hidden, d_weight: where to write them (bfloat16 matrices with unit column stride), for instance a slot of a bfloat16 gradient stack; they may not overlap
-    `hidden`, `weight` or each other.
+    `hidden`, `weight`, `labels`, `token_weight` or each other.
     """
     return _last_layer(True, hidden, weight, (labels, ignore_index), token_weight, d_hidden, d_weight, status, stream)
 

@@ -23,3 +23,95 @@ def test_distillation_workspace_is_bounded_in_entries(L):
                     assert L.psgd_distill_workspace(T, V, 64, K, grad, C.byref(a)) == 0 and L.psgd_xent_workspace(T, V, 64, grad, C.byref(b)) == 0
                     # (4 bytes per block of at most 2^32 logits, 4 per token of a piece, float32 sums of the weight gradient once there are several pieces, partial tiles)
                     assert a.value <= b.value + 8 * T + (1 << 30) + 4 * (1 << 22) + (1 << 27) + 4 * min(T, 1 << 25) + 4 * V * 64 + (1 << 26), (T, V, K, grad)
+
+
+P, STEP = 1 << 32, 1 << 30         # made-up device addresses, far apart: only refusals are looked at where there is a GPU
+
+
+def launches(code):
+    """What a call answers that got as far as a launch on a machine without a GPU."""
+    return code == -4
+
+
+def over(places, out, fixed=()):
+    """Every way to put the outputs `out` of {name: (address, bytes)} over another place: over its beginning, its last bytes, and so that it begins within."""
+    for name in out:
+        for other, (at, size) in places.items():
+            if other == name or (name, other) in fixed or (other, name) in fixed:
+                continue
+            mine = places[name][1]
+            for to in {at, at + size - 16, at - mine + 16}:
+                yield name, other, (to + 15) // 16 * 16
+
+
+def test_norm_outputs_over_anything_are_refused(L):
+    """Vectors and the 8-bit form as well as matrices, T = 8 rows of 64."""
+    import torch
+
+    gpu = torch.cuda.is_available()
+    size = dict(x=1024, r=1024, w=256, b=256, s=1024, y=1024, mean=32, rstd=32, q=512, scales=16)
+    at = {k: (P + i * STEP, n) for i, (k, n) in enumerate(size.items())}
+
+    def forward(**kw):
+        p = {k: kw.get(k, v[0]) for k, v in at.items()}
+        return L.psgd_norm_forward(p["x"], 64, 1, p["r"], 64, p["w"], p["b"], 0, 1e-5, 1, 8, 64, p["s"], 64, p["y"], 64, 1, p["mean"], p["rstd"], p["q"], p["scales"], None)
+
+    assert gpu or launches(forward())
+    for name, other, to in over(at, ("s", "y", "mean", "rstd", "q", "scales")):
+        assert forward(**{name: to}) == -1, (name, other)
+    n = C.c_size_t()
+    assert L.psgd_norm_workspace(8, 64, C.byref(n)) == 0
+    size = dict(dy=1024, x=1024, w=256, mean=32, rstd=32, add=1024, dx=1024, dw=256, db=256, ws=512)        # (of the workspace at least two sums per column are used)
+    back = {k: (P + i * STEP, m) for i, (k, m) in enumerate(size.items())}
+
+    def backward(**kw):
+        p = {k: kw.get(k, v[0]) for k, v in back.items()}
+        return L.psgd_norm_backward(p["dy"], 64, 1, p["x"], 64, 1, p["w"], 0, p["mean"], p["rstd"], p["add"], 64, 8, 64, p["dx"], 64, p["dw"], p["db"], p["ws"] // 256 * 256, n.value, None)
+
+    assert gpu or launches(backward())
+    for name, other, to in over(back, ("dx", "dw", "db")):
+        assert backward(**{name: to}) == -1, (name, other)
+    for other, (to, _) in back.items():
+        assert other == "ws" or backward(ws=to) == -1, other
+
+
+def test_rotary_outputs_over_angles_are_refused(L):
+    import torch
+
+    size = dict(q=4096, k=4096, oq=4096, ok=4096, positions=64, frequencies=256)      # 8 tokens of 4 heads of 64 values
+    at = {k: (P + i * STEP, n) for i, (k, n) in enumerate(size.items())}
+
+    def call(**kw):
+        p = {k: kw.get(k, v[0]) for k, v in at.items()}
+        return L.psgd_rotary(p["q"], 256, 64, 4, p["oq"], 256, 64, p["k"], 256, 64, 4, p["ok"], 256, 64, p["positions"], p["frequencies"], 8, 64, 64, 0, 0, 1.0, 1, None)
+
+    assert torch.cuda.is_available() or launches(call())
+    for name, other, to in over(at, ("oq", "ok"), fixed=(("oq", "q"), ("ok", "k"))):
+        assert call(**{name: to}) == -1, (name, other)
+
+
+def test_gradients_over_labels_and_weights_are_refused(L):
+    """They are read for later pieces of the tokens after earlier ones' gradients are written."""
+    import torch
+
+    T, V, D, K = 8, 40, 64, 16
+    size = dict(H=T * D * 2, W=V * D * 2, labels=T * 8, weight=T * 4, logits=T * K * 4, index=T * K * 8, dH=T * D * 2, dW=V * D * 2)
+    at = {k: (P + i * STEP, n) for i, (k, n) in enumerate(size.items())}
+    free = P + 20 * STEP
+    n = C.c_size_t()
+
+    def xent(**kw):
+        p = {k: kw.get(k, v[0]) for k, v in at.items()}
+        assert L.psgd_xent_workspace(T, V, D, 1, C.byref(n)) == 0
+        return L.psgd_xent_grad(p["H"], D, p["W"], D, p["labels"], p["weight"], -100, T, V, D, free, free + 256, free + 512, p["dH"], D, p["dW"], D, None, free + 4096, n.value, None)
+
+    def distill(**kw):
+        p = {k: kw.get(k, v[0]) for k, v in at.items()}
+        assert L.psgd_distill_workspace(T, V, D, K, 1, C.byref(n)) == 0
+        return L.psgd_distill_grad(p["H"], D, p["W"], D, p["logits"], K, 0, p["index"], K, K, 1.0, p["weight"], T, V, D, free, free + 256, free + 512, p["dH"], D, p["dW"], D, None,
+                                   free + 4096, n.value, None)
+
+    assert torch.cuda.is_available() or launches(xent()) and launches(distill())
+    for call, unused in ((xent, ("logits", "index")), (distill, ("labels",))):
+        for name, other, to in over({k: v for k, v in at.items() if k not in unused}, ("dH", "dW")):
+            assert call(**{name: to}) == -1, (name, other)
