@@ -115,3 +115,64 @@ def test_gradients_over_labels_and_weights_are_refused(L):
     for call, unused in ((xent, ("logits", "index")), (distill, ("labels",))):
         for name, other, to in over({k: v for k, v in at.items() if k not in unused}, ("dH", "dW")):
             assert call(**{name: to}) == -1, (name, other)
+
+
+# ---- how the operators are built and reached ----------------------------------------------------------------------
+class Compilers:
+    """In the place of subprocess.Popen: writes what a compiler would write, or fails; keeps the commands."""
+
+    def __init__(self, works):
+        self.works, self.commands = works, []
+
+    def __call__(self, command, **kw):
+        import types
+
+        self.commands.append(command)
+        works = self.works(command)
+        if works is None:
+            raise FileNotFoundError(command[0])
+        if works:
+            open(command[command.index("-o") + 1], "w").close()
+        return types.SimpleNamespace(communicate=lambda: ("said", None), returncode=0 if works else 1)
+
+
+@pytest.fixture
+def elsewhere(monkeypatch, tmp_path):
+    from paper_2509_11254_b200 import build
+
+    for name in ("LIB", "CALL", "OBJ_DIR"):
+        monkeypatch.setattr(build, name, str(tmp_path / name))
+    return build
+
+
+def test_library_needs_nvcc_alone(elsewhere, monkeypatch):
+    """Without torch, and where the C++ compiler of _call.so is missing or fails, the library is built all the same."""
+    import os
+
+    b = elsewhere
+    monkeypatch.setattr(b, "nvcc_path", lambda: "nvcc")
+    monkeypatch.setenv("CXX", "cxx")
+    with monkeypatch.context() as m:
+        run = Compilers(lambda c: True)
+        m.setattr(b.subprocess, "Popen", run)
+        m.setattr(b.importlib.util, "find_spec", lambda name: None)
+        assert b.needs_build() and b.build_library() == b.LIB and os.path.exists(b.LIB) and not os.path.exists(b.CALL)
+        assert len(run.commands) == len(b.SRCS) + 1 and all(c[0] == "nvcc" for c in run.commands)
+        assert not b.needs_build()
+    for works in (None, False):
+        os.remove(b.LIB)
+        with monkeypatch.context() as m:
+            m.setattr(b.subprocess, "Popen", Compilers(lambda c: True if c[0] == "nvcc" else works))
+            with pytest.warns(RuntimeWarning, match="_call.so could not be built"):
+                assert b.build_library() == b.LIB
+            assert os.path.exists(b.LIB) and not os.path.exists(b.CALL)
+            # the library is there: only the other one is tried again
+            again = Compilers(lambda c: True)
+            m.setattr(b.subprocess, "Popen", again)
+            b.build_library()
+            assert os.path.exists(b.CALL) and all(c[0] == "cxx" for c in again.commands) and not b.needs_build()
+            os.remove(b.CALL)
+    with monkeypatch.context() as m:
+        m.setattr(b.subprocess, "Popen", Compilers(lambda c: c[0] != "nvcc"))
+        with pytest.raises(RuntimeError, match="nvcc failed"):
+            b.build_library(force=True)
