@@ -3,6 +3,7 @@ from __future__ import annotations
 
 import importlib.util
 import os
+import re
 import subprocess
 import sys
 import sysconfig
@@ -38,9 +39,25 @@ def needs_library():
     return _older(LIB, [HEADER] + [os.path.join(HERE, "csrc", f) for f in os.listdir(os.path.join(HERE, "csrc")) if not f.endswith(".cpp")])
 
 
+def call_tag():
+    """What _call.so is compiled against, torch's version (without importing it) and the interpreter; it holds this text."""
+    with open(os.path.join(_torch_dir(), "version.py")) as f:
+        version = re.search(r"^__version__ *=.*['\"](.+)['\"]", f.read(), re.M)
+    return f"psgd_call for torch {version.group(1) if version else '?'}, {sys.implementation.cache_tag}"
+
+
+def call_fits():
+    """Whether _call.so is there and was compiled against this torch and this interpreter."""
+    try:
+        with open(CALL, "rb") as f:
+            return call_tag().encode() + b"\0" in f.read()
+    except OSError:
+        return False
+
+
 def needs_call():
     """Where torch is not installed there is nothing to call the library from."""
-    return _torch_dir() is not None and _older(CALL, [HEADER, CALL_SRC])
+    return _torch_dir() is not None and (_older(CALL, [HEADER, CALL_SRC]) or not call_fits())
 
 
 def needs_build():
@@ -55,7 +72,7 @@ def _start_call():
     torch_dir = _torch_dir()
     include = [os.path.join(torch_dir, "include"), os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"), sysconfig.get_path("include"),
                os.path.join(os.path.dirname(os.path.dirname(nvcc_path())), "include")]
-    return _start([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", *(f for p in include for f in ("-isystem", p)), "-c", "-o", os.path.join(OBJ_DIR, "psgd_call.o"), CALL_SRC])
+    return _start([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", f'-DPSGD_CALL_BUILT_FOR="{call_tag()}"', *(f for p in include for f in ("-isystem", p)), "-c", "-o", os.path.join(OBJ_DIR, "psgd_call.o"), CALL_SRC])
 
 
 def _finish_call(job):

@@ -14,6 +14,9 @@
 
 #include "../../include/psgd.h"
 
+// What this was compiled against: build.py looks for it in the file, since nothing compiled against one torch may be loaded into another.
+extern "C" __attribute__((used, visibility("default"))) const char psgd_call_built_for[] = PSGD_CALL_BUILT_FOR;
+
 namespace {
 
 using at::Tensor;

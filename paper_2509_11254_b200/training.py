@@ -52,18 +52,33 @@ def _check(code):
         binding._check(code)
 
 
+class _NoPlainCall:
+    """In the place of _call.so: no call is a plain one, and all take the way through this package."""
+
+    def __getattr__(self, name):
+        return lambda *args: None
+
+
 _call = None
 
 
 def _plain():
-    """The module behind _call.so: the plain call of an operator, or None where it is not one; like the library it has no stand-in."""
+    """The module behind _call.so: the plain call of an operator, or None where it is not one.  Every call works without it, with more time on the host: where it is missing, or
+    compiled against another torch, a warning says so once."""
     global _call
     if _call is None:
+        from . import build
+
         lib()
-        try:
-            from . import _call as module
-        except ImportError as e:
-            raise PSGDError(f"_call.so cannot be loaded ({e}): build it with `python -m paper_2509_11254_b200.build`") from e
+        why, module = "it is missing or compiled against another torch", None
+        if build.call_fits():
+            try:
+                from . import _call as module
+            except ImportError as e:
+                why = str(e)
+        if module is None:
+            warnings.warn(f"_call.so cannot be used ({why}), small calls take 10 to 20 us longer: build it with `python -m paper_2509_11254_b200.build`", RuntimeWarning, stacklevel=4)
+            module = _NoPlainCall()
         _call = module
     return _call
 

@@ -119,7 +119,7 @@ def test_gradients_over_labels_and_weights_are_refused(L):
 
 # ---- how the operators are built and reached ----------------------------------------------------------------------
 class Compilers:
-    """In the place of subprocess.Popen: writes what a compiler would write, or fails; keeps the commands."""
+    """In the place of subprocess.Popen: writes what a compiler would write (of _call.so, what it was compiled against), or fails; keeps the commands."""
 
     def __init__(self, works):
         self.works, self.commands = works, []
@@ -132,7 +132,10 @@ class Compilers:
         if works is None:
             raise FileNotFoundError(command[0])
         if works:
-            open(command[command.index("-o") + 1], "w").close()
+            from paper_2509_11254_b200 import build
+
+            with open(command[command.index("-o") + 1], "w") as f:
+                f.write(build.call_tag() + "\0" if command[0] == "cxx" else "")
         return types.SimpleNamespace(communicate=lambda: ("said", None), returncode=0 if works else 1)
 
 
@@ -176,3 +179,49 @@ def test_library_needs_nvcc_alone(elsewhere, monkeypatch):
         m.setattr(b.subprocess, "Popen", Compilers(lambda c: c[0] != "nvcc"))
         with pytest.raises(RuntimeError, match="nvcc failed"):
             b.build_library(force=True)
+
+
+def test_operators_do_without_the_short_way(monkeypatch, tmp_path):
+    """_call.so missing, compiled against another torch, or impossible to load: a warning, once, and the calls that there are without it."""
+    import sys
+    import types
+    import warnings
+
+    import torch
+
+    import paper_2509_11254_b200 as p
+    from paper_2509_11254_b200 import build, training
+
+    build.build_library()
+    x, w, at = torch.zeros(4, 8), torch.ones(8), torch.arange(4)
+    h, z, i = x.bfloat16(), x[:, :2].contiguous(), torch.zeros(4, 2, dtype=torch.int64)
+    calls = [lambda: p.layer_norm_forward(x, w), lambda: p.layer_norm_backward(x, x, w, None, x[:, 0]), lambda: p.rotary_forward(x.view(4, 1, 8), None, at, p.rotary_frequencies(8, device="cpu")),
+             lambda: p.linear_distillation(h, h, z, i), lambda: p.linear_distillation_grad(h, h, z, i)]
+
+    def without():
+        monkeypatch.setattr(training, "_call", None)
+        with pytest.warns(RuntimeWarning, match="_call.so cannot be used") as seen:
+            for call in calls:
+                with pytest.raises(p.PSGDError, match="must be a CUDA tensor"):
+                    call()
+        assert len(seen) == 1 and seen[0].filename == __file__
+
+    tag, data = build.call_tag().encode(), open(build.CALL, "rb").read()
+    assert torch.__version__ in build.call_tag() and build.call_fits()
+    other = tmp_path / "_call.so"
+    monkeypatch.setattr(build, "CALL", str(other))
+    assert not build.call_fits() and build.needs_call()
+    without()
+    other.write_bytes(data.replace(tag, tag.replace(b"torch 2", b"torch 1")))
+    assert not build.call_fits() and build.needs_call()
+    without()
+    other.write_bytes(data)
+    assert build.call_fits() and not build.needs_call()
+    monkeypatch.setitem(sys.modules, "paper_2509_11254_b200._call", None)
+    monkeypatch.delattr(p, "_call", raising=False)
+    without()
+    monkeypatch.undo()
+    monkeypatch.setattr(training, "_call", None)
+    with warnings.catch_warnings():
+        warnings.simplefilter("error")
+        assert isinstance(training._plain(), types.ModuleType)
