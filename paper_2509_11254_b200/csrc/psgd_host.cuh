@@ -24,17 +24,23 @@ inline int device_sms() {
 }
 
 // Opt a kernel in to `bytes` of dynamic shared memory: the attribute is set once per (device, kernel) and raised
-// only when a larger size is asked for.
-inline void set_smem_attr(const void* kernel, size_t bytes) {
-    static std::mutex mu;
-    static std::map<std::pair<int, const void*>, size_t> done;
+// only when a larger size is asked for.  C entry points call it: where there is no memory to note that down, it is set again every time.
+inline void set_smem_attr(const void* kernel, size_t bytes) noexcept {
+    const auto set = [&] {
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess) return true;
+        cudaGetLastError();                           // (the launch will say why)
+        return false;
+    };
     int dev = 0;
     cudaGetDevice(&dev);
-    std::lock_guard<std::mutex> lock(mu);
-    size_t& have = done[std::make_pair(dev, kernel)];
-    if (bytes > have) {
-        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-        have = bytes;
+    try {
+        static std::mutex mu;
+        static std::map<std::pair<int, const void*>, size_t> done;
+        std::lock_guard<std::mutex> lock(mu);
+        size_t& have = done[std::make_pair(dev, kernel)];
+        if (bytes > have && set()) have = bytes;
+    } catch (...) {
+        set();
     }
 }
 template <typename K>

@@ -225,3 +225,41 @@ def test_operators_do_without_the_short_way(monkeypatch, tmp_path):
     with warnings.catch_warnings():
         warnings.simplefilter("error")
         assert isinstance(training._plain(), types.ModuleType)
+
+
+def test_no_exception_leaves_where_a_kernel_is_opted_in(tmp_path):
+    """C entry points raise the shared memory of their kernels on the way: a failed allocation there must not end the process."""
+    import os
+    import subprocess
+
+    from paper_2509_11254_b200 import build
+
+    src = tmp_path / "new.cpp"
+    src.write_text("""
+#include <cstdio>
+#include <cstdlib>
+#include <new>
+#include "psgd_host.cuh"
+static bool full = false;
+static int asked = 0;
+void* operator new(size_t n) {
+    if (full) { ++asked; throw std::bad_alloc(); }
+    return malloc(n);
+}
+void operator delete(void* p) noexcept { free(p); }
+void operator delete(void* p, size_t) noexcept { free(p); }
+int main() {
+    static int kernel;
+    set_smem_attr(&kernel, 1 << 16);
+    full = true;
+    static int other;
+    set_smem_attr(&other, 1 << 16);
+    full = false;
+    printf("asked %d\\n", asked);
+}
+""")
+    cuda = os.path.dirname(os.path.dirname(build.nvcc_path()))
+    subprocess.run(["g++", "-std=c++17", "-I" + os.path.join(os.path.dirname(build.__file__), "csrc"), "-I" + os.path.join(cuda, "include"), "-o", str(tmp_path / "new"), str(src),
+                    "-L" + os.path.join(cuda, "lib64"), "-lcudart", "-Wl,-rpath," + os.path.join(cuda, "lib64")], check=True, capture_output=True)
+    r = subprocess.run([str(tmp_path / "new")], capture_output=True, text=True)
+    assert r.returncode == 0 and int(r.stdout.split()[1]) > 0
