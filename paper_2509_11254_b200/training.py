@@ -271,6 +271,7 @@ def linear_cross_entropy(hidden, weight, labels, token_weight=None, ignore_index
 def linear_cross_entropy_grad(hidden, weight, labels, token_weight=None, ignore_index=-100, d_hidden=None, d_weight=None, status=None, stream=None):
     """The same with the gradients of the loss: returns (loss, token_loss, lse, d_hidden [T, D], d_weight [V, D]), the gradients bfloat16.
 
+    The gradients of the logits, too, are rounded to bfloat16 before the two products that make these from them, whose sums are float32.
     d_hidden, d_weight: where to write them (bfloat16 matrices with unit column stride), for instance a slot of a bfloat16 gradient stack; they may not overlap
     `hidden`, `weight`, `labels`, `token_weight` or each other.
     """
@@ -290,7 +291,7 @@ def linear_distillation(hidden, weight, teacher_logits, teacher_index, temperatu
 
 
 def linear_distillation_grad(hidden, weight, teacher_logits, teacher_index, temperature=1.0, token_weight=None, d_hidden=None, d_weight=None, status=None, stream=None):
-    """The same with the gradients of the loss: returns (loss, token_loss, lse, d_hidden [T, D], d_weight [V, D]), the gradients bfloat16.
+    """The same with the gradients of the loss: returns (loss, token_loss, lse, d_hidden [T, D], d_weight [V, D]), the gradients bfloat16 (and those of the logits on the way).
 
     d_hidden, d_weight: where to write them, as for linear_cross_entropy_grad; they may not overlap the teacher's lists either.
     """
